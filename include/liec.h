@@ -255,6 +255,96 @@ liec_status liec_mean_params(liec_ctx *ctx, float *out, void *stream);
 liec_status liec_sumsq(liec_ctx *ctx, int32_t which, const void *grads, double *out, void *stream);
 
 /*
+ * Norm of every worker's gradient over all its tensors, and clipping: what stands between a backward
+ * pass and the compressed iteration (the paper's experiments do not clip; training of large models does).
+ * For worker i with entries g_j, j in [0, d):
+ *   norm_i = sqrt(sum_j g_j^2),   c_i = max_norm / norm_i if norm_i > max_norm, else 1,   out_j = c_i g_j
+ * The sum runs in binary64 (squares of binary32 values are exact there and cannot overflow): every
+ * 8192-element tile of a segment over its balanced binary tree, then the tile sums of the row, in
+ * order, over a balanced binary tree padded to a power of two; c_i is divided in binary64 and rounded
+ * once to binary32; c_i g_j is one binary32 product, rounded once more where the rows are bfloat16.
+ * The result does not depend on the launch.
+ *   grads     device, [N][d] of cfg.grad_dtype, 16-byte aligned
+ *   out       device, [N][d] of cfg.grad_dtype, 16-byte aligned: grads itself (a row with c_i = 1 is then
+ *             left alone) or memory that does not overlap it
+ *   max_norm  > 0; infinity asks for the norms alone (and, out of place, a copy)
+ *   zero_nonfinite  != 0: the row of a worker whose norm is infinite or NaN is written as zeros, so
+ *             that one bad gradient does not enter the global error for good; 0: it is treated by the
+ *             formula (c_i = 0 for an infinite norm, 1 for a NaN)
+ *   norms     device, [N] binary32 (rounded once), or NULL
+ * Enqueued on `stream`.  LIEC_ERR_STATE between the stages of an iteration.
+ */
+liec_status liec_clip_grads(liec_ctx *ctx, const void *grads, void *out, float max_norm, int32_t zero_nonfinite,
+                            float *norms, void *stream);
+
+/*
+ * The same from N*T separate tensors, as a backward pass leaves them, into gradient rows: out row i =
+ * c_i times the concatenation of worker i's tensors, in one sweep with the clipping.
+ *   tensors  host, [N][T] device pointers, worker after worker: tensor t of a worker has
+ *            seg_offsets[t+1] - seg_offsets[t] consecutive elements of `dtype` (LIEC_F32 or LIEC_BF16,
+ *            whatever the rows' type) at any element-aligned address; NULL: no gradient, counts as zeros
+ * liec_set_tensors copies the pointers (as kernel arguments: no synchronisation, and it can be
+ * captured), ordered on `stream`; the tensors themselves are read by liec_gather_grads and must not
+ * overlap `out`.  The table serves any number of liec_gather_grads calls until the next
+ * liec_set_tensors.  liec_gather_grads returns LIEC_ERR_STATE when no table was given.
+ */
+liec_status liec_set_tensors(liec_ctx *ctx, const void *const *tensors, int32_t dtype, void *stream);
+liec_status liec_gather_grads(liec_ctx *ctx, void *out, float max_norm, int32_t zero_nonfinite, float *norms,
+                              void *stream);
+
+/*
+ * Layer normalisation of N workers' activations in one call, and its backward pass with the reduction
+ * of the weight's and bias's gradients into the workers' gradient rows.  Per row x of h = cols elements,
+ * with the worker's own weight w and bias b:
+ *   m = mean(x),  r = 1 / sqrt(mean((x - m)^2) + eps),  y = (x - m) r w + b
+ *   xh = (x - m) r,  dx = r (dy w - mean(dy w) - xh mean(dy w xh)),
+ *   dw = sum over the worker's rows of dy xh,  db = sum over the worker's rows of dy
+ * Evaluated in binary32, the variance around the mean; outputs are rounded once to their type.  The
+ * order of the sums depends on the sizes and the GPU's SM count alone (no atomics): equal calls give
+ * equal bits.  A row with an infinity or NaN gives NaN in that row (and in dw, db) only.
+ *
+ * No context is needed.  All strides are in elements and >= 0; the last axis is contiguous.  Rows that
+ * are read may overlap or repeat (stride 0); rows that are written may not.  Any element alignment is
+ * accepted; 16-byte aligned rows are faster.  Outputs must not overlap inputs.
+ */
+#define LIEC_LAYER_NORM_MAX_COLS 65536
+typedef struct {
+    int32_t groups;         /* N >= 1 workers */
+    int64_t rows;           /* rows per worker, >= 0 */
+    int32_t cols;           /* h, 1 .. LIEC_LAYER_NORM_MAX_COLS */
+    int32_t dtype;          /* liec_dtype of x, y, dy, dx */
+    int32_t grad_dtype;     /* liec_dtype of dweight and dbias */
+    float eps;              /* >= 0 */
+    int64_t x_row_stride, x_group_stride;
+    int64_t y_row_stride, y_group_stride;    /* of y in the forward pass, of dy in the backward pass */
+    int64_t dx_row_stride, dx_group_stride;
+    int64_t weight_stride, bias_stride;      /* from worker to worker: d for a range of the parameter rows, 0 = shared */
+    int64_t dweight_stride, dbias_stride;    /* from worker to worker: d for a range of the gradient rows */
+} liec_layer_norm_desc;
+
+/* Bytes of device workspace of the backward pass (column sums of runs of rows); 0 for a bad desc. */
+size_t liec_layer_norm_workspace_bytes(const liec_layer_norm_desc *desc);
+
+/*
+ *   x, y        device, [groups][rows][cols] of dtype
+ *   weight      device, binary32, or NULL for ones;   bias  the same, NULL for zeros
+ *   mean, rstd  device, [groups][rows] binary32: m and r, for the backward pass; either may be NULL
+ */
+liec_status liec_layer_norm_forward(const liec_layer_norm_desc *desc, const void *x, const float *weight, const float *bias,
+                                    void *y, float *mean, float *rstd, void *stream);
+
+/*
+ *   dy, x       device, [groups][rows][cols] of dtype;  mean, rstd  as the forward pass stored them
+ *   dx          device, of dtype;  dweight, dbias  device, [groups][cols] of grad_dtype: overwritten, also
+ *               with rows = 0 (zeros).  Each of the three may be NULL: it is not computed.
+ *   workspace   device, 16-byte aligned, liec_layer_norm_workspace_bytes(desc) bytes, when dweight or dbias is
+ *               wanted; scratch of this call alone
+ */
+liec_status liec_layer_norm_backward(const liec_layer_norm_desc *desc, const void *dy, const void *x, const float *mean,
+                                     const float *rstd, const float *weight, void *dx, void *dweight, void *dbias,
+                                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Telemetry fused into the iteration's own passes: the quantities behind the paper's figure of
  * error norms (||e_t||) and its table of measured delta (Def. 1: delta = 1 - ||x - C(x)||^2 / ||x||^2,
  * worker side x = g^i, server side x = v) at no extra pass over the model-sized arrays.

@@ -32,6 +32,21 @@ cudaError_t configure_average_kernels();  // opt-in shared memory sizes; call on
 cudaError_t launch_sumsq(const Params &p, const void *src, int64_t row_stride, int rows, bool bf16, cudaStream_t st);
 cudaError_t launch_sum_finalize(const Params &p, const double *partials, int rows, double *out, cudaStream_t st);
 
+// norm of every worker's gradient and clipping
+struct ClipArgs {
+    const void *rows;          // [N][d] of src_dtype, used when table is NULL
+    const void *const *table;  // device, [N][T] pointers to the tensors (NULL entry: zeros), or NULL
+    void *out;                 // [N][d] of the context's gradient type
+    float *norms;              // [N] or NULL
+    double *partials;          // [N][TT] tile sums of squares
+    float *factor;             // [N]
+    int32_t *clear;            // [N] the row is written as zeros
+    float max_norm;
+    int32_t src_dtype, in_place, zero_nonfinite;
+};
+cudaError_t launch_clip(const Params &p, const ClipArgs &a, cudaStream_t st, int64_t *launches);
+cudaError_t launch_upload_pointers(const void *const *tensors, const void **table, int64_t count, cudaStream_t st, int64_t *launches);
+
 // worker update
 cudaError_t launch_worker_update(const Params &p, float lr, cudaStream_t st);
 

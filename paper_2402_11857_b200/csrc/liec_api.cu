@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <new>
@@ -11,6 +12,7 @@
 
 #include "../../include/liec.h"
 #include "kernels.h"
+#include "layer_norm.h"
 #include "plan.h"
 #include "topk_common.cuh"
 
@@ -31,6 +33,7 @@ struct Plan {
     std::vector<int32_t> tile_prefix, tile_seg, small_seg, large_seg, ktile_prefix, ktile_seg;
     Region r_seg_off, r_word_off, r_k_off, r_cap_off, r_down_cap_off, r_tile_prefix, r_tile_seg, r_small_seg, r_large_seg, r_status;
     Region r_tel_partials, r_tel_e, r_tel_v, r_tel_g, r_tel_kept, r_ktile_prefix, r_ktile_seg;
+    Region r_tensor_table, r_clip_partials, r_clip_factor, r_clip_clear;
     Region r_up_words, r_up_scales, r_up_partials, r_down_words, r_down_scales, r_down_partials, r_vbuf;
     Region r_up_idx, r_up_val, r_down_idx, r_down_val;
     Region r_up_hist, r_down_hist, r_up_hist2, r_down_hist2, r_up_sel, r_down_sel;
@@ -168,6 +171,10 @@ liec_status make_plan(const liec_config *cfg, Plan &pl, std::string *msg) {
     pl.r_ktile_seg = c.take(sizeof(int32_t) * pl.KTT);
     pl.r_tel_kept = c.take(sizeof(double) * (size_t)pl.N * pl.KTT);
     const size_t N = pl.N;
+    pl.r_tensor_table = c.take(sizeof(void *) * N * T);
+    pl.r_clip_partials = c.take(sizeof(double) * N * pl.TT);
+    pl.r_clip_factor = c.take(sizeof(float) * N);
+    pl.r_clip_clear = c.take(sizeof(int32_t) * N);
     if (cfg->uplink == LIEC_COMP_SCALED_SIGN) {
         pl.r_up_words = c.take(sizeof(uint32_t) * N * pl.W);
         pl.r_up_scales = c.take(sizeof(float) * N * T);
@@ -232,6 +239,7 @@ struct liec_ctx {
     char *ws = nullptr;
     int stage = 0;  // 0 idle, 1 after uplink, 2 after aggregate, 3 after downlink
     int64_t launches = 0;
+    int32_t tensor_dtype = -1;     // type of the tensors given to liec_set_tensors, -1 before the first call
     bool telemetry_valid = false;  // an iteration has completed with the telemetry switched on
     std::string err;
     // top-k: the single-tile segments are selected on a stream of the context's own, forked from
@@ -698,6 +706,65 @@ liec_status liec_sumsq(liec_ctx *c, int32_t which, const void *grads, double *ou
     return LIEC_OK;
 }
 
+// What liec_clip_grads and liec_gather_grads share: arguments checked, kernels enqueued.
+static liec_status clip(liec_ctx *c, const char *name, ClipArgs a, void *stream) {
+    liec_status st = check_stage(c, 0, name);
+    if (st != LIEC_OK) return st;
+    if (!a.out || !aligned16(a.out)) { c->err = "the gradient rows must be non-NULL and 16-byte aligned"; return LIEC_ERR_INVALID_ARG; }
+    if (!(a.max_norm > 0.0f)) { c->err = "max_norm must be positive (infinity: no clipping)"; return LIEC_ERR_INVALID_ARG; }
+    if (reinterpret_cast<uintptr_t>(a.norms) & 3u) { c->err = "norms must be 4-byte aligned"; return LIEC_ERR_INVALID_ARG; }
+    a.partials = at<double>(c, c->plan.r_clip_partials);
+    a.factor = at<float>(c, c->plan.r_clip_factor);
+    a.clear = at<int32_t>(c, c->plan.r_clip_clear);
+    LIEC_CALL(c, launch_clip(c->p, a, static_cast<cudaStream_t>(stream), &c->launches));
+    return LIEC_OK;
+}
+
+liec_status liec_clip_grads(liec_ctx *c, const void *grads, void *out, float max_norm, int32_t zero_nonfinite, float *norms,
+                            void *stream) {
+    if (!c) return LIEC_ERR_INVALID_ARG;
+    if (!grads || !aligned16(grads)) { c->err = "grads must be non-NULL and 16-byte aligned"; return LIEC_ERR_INVALID_ARG; }
+    const uintptr_t bytes = (c->p.gdt == DT_BF16 ? 2 : 4) * (uintptr_t)c->p.N * (uintptr_t)c->p.d;
+    const uintptr_t g = reinterpret_cast<uintptr_t>(grads), o = reinterpret_cast<uintptr_t>(out);
+    if (g != o && g < o + bytes && o < g + bytes) { c->err = "out must be grads itself or not overlap it"; return LIEC_ERR_INVALID_ARG; }
+    ClipArgs a{};
+    a.rows = grads;
+    a.src_dtype = c->p.gdt;
+    a.out = out;
+    a.in_place = grads == out;
+    a.max_norm = max_norm;
+    a.zero_nonfinite = zero_nonfinite != 0;
+    a.norms = norms;
+    return clip(c, "liec_clip_grads", a, stream);
+}
+
+liec_status liec_set_tensors(liec_ctx *c, const void *const *tensors, int32_t dtype, void *stream) {
+    if (!c) return LIEC_ERR_INVALID_ARG;
+    if (!tensors) { c->err = "tensors must be non-NULL"; return LIEC_ERR_INVALID_ARG; }
+    if (dtype != LIEC_F32 && dtype != LIEC_BF16) { c->err = "unknown tensor dtype"; return LIEC_ERR_INVALID_ARG; }
+    const int64_t count = (int64_t)c->p.N * c->p.T;
+    const uintptr_t mask = dtype == LIEC_BF16 ? 1u : 3u;
+    for (int64_t q = 0; q < count; ++q)
+        if (reinterpret_cast<uintptr_t>(tensors[q]) & mask) { c->err = "a tensor is not aligned to its element size"; return LIEC_ERR_INVALID_ARG; }
+    c->tensor_dtype = -1;   // (a table that is only half written is not used)
+    LIEC_CALL(c, launch_upload_pointers(tensors, at<const void *>(c, c->plan.r_tensor_table), count, static_cast<cudaStream_t>(stream), &c->launches));
+    c->tensor_dtype = dtype;
+    return LIEC_OK;
+}
+
+liec_status liec_gather_grads(liec_ctx *c, void *out, float max_norm, int32_t zero_nonfinite, float *norms, void *stream) {
+    if (!c) return LIEC_ERR_INVALID_ARG;
+    if (c->tensor_dtype < 0) { c->err = "liec_gather_grads: no tensors given (liec_set_tensors)"; return LIEC_ERR_STATE; }
+    ClipArgs a{};
+    a.table = at<const void *>(c, c->plan.r_tensor_table);
+    a.src_dtype = c->tensor_dtype;
+    a.out = out;
+    a.max_norm = max_norm;
+    a.zero_nonfinite = zero_nonfinite != 0;
+    a.norms = norms;
+    return clip(c, "liec_gather_grads", a, stream);
+}
+
 liec_status liec_set_telemetry(liec_ctx *c, int32_t on) {
     liec_status st = check_stage(c, 0, "liec_set_telemetry");
     if (st != LIEC_OK) return st;
@@ -837,6 +904,95 @@ liec_status liec_clear_status(liec_ctx *c, void *stream) {
 int64_t liec_launch_count(const liec_ctx *c) { return c ? c->launches : 0; }
 
 const char *liec_last_error(const liec_ctx *c) { return c ? c->err.c_str() : g_no_ctx_error; }
+
+// ---- layer normalisation over N workers (no context) ------------------------------------------------
+
+static liec_status ln_refuse(liec_status st, const char *text) {
+    snprintf(g_no_ctx_error, sizeof(g_no_ctx_error), "%s", text);
+    return st;
+}
+
+static liec_status ln_check(const liec_layer_norm_desc *d) {
+    if (!d) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: desc is NULL");
+    if (d->groups < 1 || d->rows < 0 || d->cols < 1) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: groups and cols must be >= 1, rows >= 0");
+    if (d->groups > 65535) return ln_refuse(LIEC_ERR_UNSUPPORTED, "layer norm: groups above 65535 (grid limit)");
+    if (d->cols > LIEC_LAYER_NORM_MAX_COLS) return ln_refuse(LIEC_ERR_UNSUPPORTED, "layer norm: cols above LIEC_LAYER_NORM_MAX_COLS");
+    if (d->rows >= (int64_t(1) << 31)) return ln_refuse(LIEC_ERR_UNSUPPORTED, "layer norm: rows must be below 2^31");
+    if ((d->dtype != LIEC_F32 && d->dtype != LIEC_BF16) || (d->grad_dtype != LIEC_F32 && d->grad_dtype != LIEC_BF16))
+        return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: unknown dtype");
+    if (!(d->eps >= 0.0f) || !std::isfinite(d->eps)) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: eps must be finite and >= 0");
+    for (int64_t s : {d->x_row_stride, d->x_group_stride, d->y_row_stride, d->y_group_stride, d->dx_row_stride, d->dx_group_stride,
+                      d->weight_stride, d->bias_stride, d->dweight_stride, d->dbias_stride})
+        if (s < 0 || s > (int64_t(1) << 40)) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: strides must be >= 0 (and below 2^40)");
+    return LIEC_OK;
+}
+
+// Rows that are written must not share elements.
+static bool ln_disjoint(const liec_layer_norm_desc *d, int64_t row, int64_t group) {
+    const int64_t h = d->cols;
+    if (d->rows <= 1) return d->groups == 1 || group >= h;
+    if (d->groups == 1) return row >= h;
+    return (row >= h && group >= (d->rows - 1) * row + h) || (group >= h && row >= (d->groups - 1) * group + h);
+}
+
+static bool aligned_to(const void *ptr, int32_t dtype) { return (reinterpret_cast<uintptr_t>(ptr) & (dtype == LIEC_BF16 ? 1u : 3u)) == 0; }
+
+size_t liec_layer_norm_workspace_bytes(const liec_layer_norm_desc *d) {
+    if (ln_check(d) != LIEC_OK) return 0;
+    return align_up(layer_norm_workspace(d->groups, d->rows, d->cols), 256);
+}
+
+liec_status liec_layer_norm_forward(const liec_layer_norm_desc *d, const void *x, const float *weight, const float *bias, void *y,
+                                    float *mean, float *rstd, void *stream) {
+    liec_status st = ln_check(d);
+    if (st != LIEC_OK) return st;
+    if (d->rows == 0) return LIEC_OK;
+    if (!x || !y || x == y) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: x and y must be non-NULL and different");
+    if (!aligned_to(x, d->dtype) || !aligned_to(y, d->dtype) || !aligned_to(weight, LIEC_F32) || !aligned_to(bias, LIEC_F32) ||
+        !aligned_to(mean, LIEC_F32) || !aligned_to(rstd, LIEC_F32))
+        return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: a pointer is not aligned to its element size");
+    if (!ln_disjoint(d, d->y_row_stride, d->y_group_stride)) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: the rows of y overlap");
+    LnForward a{};
+    a.x = x; a.weight = weight; a.bias = bias; a.y = y; a.mean = mean; a.rstd = rstd;
+    a.rows = d->rows; a.groups = d->groups; a.cols = d->cols; a.eps = d->eps;
+    a.x_row = d->x_row_stride; a.x_group = d->x_group_stride; a.y_row = d->y_row_stride; a.y_group = d->y_group_stride;
+    a.weight_stride = d->weight_stride; a.bias_stride = d->bias_stride;
+    const cudaError_t e = launch_layer_norm_forward(a, d->dtype, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return ln_refuse(LIEC_ERR_CUDA, cudaGetErrorString(e));
+    return LIEC_OK;
+}
+
+liec_status liec_layer_norm_backward(const liec_layer_norm_desc *d, const void *dy, const void *x, const float *mean, const float *rstd,
+                                     const float *weight, void *dx, void *dweight, void *dbias, void *workspace, size_t workspace_bytes,
+                                     void *stream) {
+    liec_status st = ln_check(d);
+    if (st != LIEC_OK) return st;
+    if (!dx && !dweight && !dbias) return LIEC_OK;
+    if (d->rows > 0 && (!dy || !x || !mean || !rstd)) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: dy, x, mean and rstd must be non-NULL");
+    if (dx && (dx == dy || dx == x)) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: dx must not be dy or x");
+    if (!aligned_to(x, d->dtype) || !aligned_to(dy, d->dtype) || !aligned_to(dx, d->dtype) || !aligned_to(weight, LIEC_F32) ||
+        !aligned_to(mean, LIEC_F32) || !aligned_to(rstd, LIEC_F32) || !aligned_to(dweight, d->grad_dtype) || !aligned_to(dbias, d->grad_dtype))
+        return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: a pointer is not aligned to its element size");
+    if (dx && d->rows > 0 && !ln_disjoint(d, d->dx_row_stride, d->dx_group_stride)) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: the rows of dx overlap");
+    if (d->groups > 1 && ((dweight && d->dweight_stride < d->cols) || (dbias && d->dbias_stride < d->cols)))
+        return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: the workers' rows of dweight or dbias overlap");
+    const size_t need = layer_norm_workspace(d->groups, d->rows, d->cols);
+    if ((dweight || dbias) && need > 0) {
+        if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15u)) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: workspace must be non-NULL and 16-byte aligned");
+        if (workspace_bytes < need) return ln_refuse(LIEC_ERR_WORKSPACE, "workspace smaller than liec_layer_norm_workspace_bytes()");
+    }
+    LnBackward a{};
+    a.dy = dy; a.x = x; a.mean = mean; a.rstd = rstd; a.weight = weight; a.dx = dx; a.dweight = dweight; a.dbias = dbias;
+    a.part_w = static_cast<float *>(workspace);
+    a.part_b = a.part_w + need / (2 * sizeof(float));
+    a.rows = d->rows; a.groups = d->groups; a.cols = d->cols;
+    a.x_row = d->x_row_stride; a.x_group = d->x_group_stride; a.dy_row = d->y_row_stride; a.dy_group = d->y_group_stride;
+    a.dx_row = d->dx_row_stride; a.dx_group = d->dx_group_stride;
+    a.weight_stride = d->weight_stride; a.dweight_stride = d->dweight_stride; a.dbias_stride = d->dbias_stride;
+    const cudaError_t e = launch_layer_norm_backward(a, d->dtype, d->grad_dtype, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return ln_refuse(LIEC_ERR_CUDA, cudaGetErrorString(e));
+    return LIEC_OK;
+}
 
 void liec_destroy(liec_ctx *c) {
     if (!c) return;

@@ -5,6 +5,7 @@ fallback: if ``libliec.so`` is missing or a call fails, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional, Sequence
@@ -39,6 +40,16 @@ class liec_messages(C.Structure):
                 ("up_val", C.c_void_p), ("down_words", C.c_void_p), ("down_scales", C.c_void_p),
                 ("down_idx", C.c_void_p), ("down_val", C.c_void_p), ("v", C.c_void_p),
                 ("num_words", C.c_int64), ("num_topk", C.c_int64)]
+
+
+class liec_layer_norm_desc(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int32), ("dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("eps", C.c_float),
+                ("x_row_stride", C.c_int64), ("x_group_stride", C.c_int64),
+                ("y_row_stride", C.c_int64), ("y_group_stride", C.c_int64),
+                ("dx_row_stride", C.c_int64), ("dx_group_stride", C.c_int64),
+                ("weight_stride", C.c_int64), ("bias_stride", C.c_int64),
+                ("dweight_stride", C.c_int64), ("dbias_stride", C.c_int64)]
 
 
 def load_library(path: Optional[str] = None) -> C.CDLL:
@@ -91,6 +102,19 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.liec_set_telemetry.restype = C.c_int
     lib.liec_get_telemetry.argtypes = [vp, vp, vp, vp, vp, vp, vp]
     lib.liec_get_telemetry.restype = C.c_int
+    lib.liec_clip_grads.argtypes = [vp, vp, vp, C.c_float, C.c_int32, vp, vp]
+    lib.liec_clip_grads.restype = C.c_int
+    lib.liec_set_tensors.argtypes = [vp, vp, C.c_int32, vp]
+    lib.liec_set_tensors.restype = C.c_int
+    lib.liec_gather_grads.argtypes = [vp, vp, C.c_float, C.c_int32, vp, vp]
+    lib.liec_gather_grads.restype = C.c_int
+    lnp = C.POINTER(liec_layer_norm_desc)
+    lib.liec_layer_norm_workspace_bytes.argtypes = [lnp]
+    lib.liec_layer_norm_workspace_bytes.restype = C.c_size_t
+    lib.liec_layer_norm_forward.argtypes = [lnp, vp, vp, vp, vp, vp, vp, vp]
+    lib.liec_layer_norm_forward.restype = C.c_int
+    lib.liec_layer_norm_backward.argtypes = [lnp, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.liec_layer_norm_backward.restype = C.c_int
     lib.liec_step_host.argtypes = [vp, vp, vp, C.c_float, vp, vp]
     lib.liec_step_host.restype = C.c_int
     lib.liec_get_messages.argtypes = [vp, C.POINTER(liec_messages)]
@@ -178,6 +202,126 @@ def liec_sign_compress_noalloc(x, words, scale, stream=None):
         raise LiecError(st, lib.liec_noalloc_last_error().decode())
 
 
+# ---- layer normalisation over N workers -----------------------------------------------------------
+
+def _on(device, stream):
+    """(raw stream, context manager): where a call on `device` runs and where its outputs are allocated."""
+    import torch
+    if stream is not None:
+        return stream.cuda_stream, torch.cuda.stream(stream)
+    if device.index != torch.cuda.current_device():
+        return torch.cuda.current_stream(device).cuda_stream, torch.cuda.device(device)
+    return torch.cuda.current_stream(device).cuda_stream, _HERE
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _ln_rows(name, t, like=None):
+    """Row and group strides of [N, rows, h] or [rows, h] activations (N = 1)."""
+    import torch
+    if not t.is_cuda or t.dtype not in (torch.float32, torch.bfloat16) or t.dim() not in (2, 3):
+        raise ValueError(f"{name} must be a CUDA tensor [N, rows, h] or [rows, h] of float32 or bfloat16")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name} must have the shape, type and device of x")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the last axis of {name} must be contiguous")
+    return t.stride(-2), (t.stride(0) if t.dim() == 3 else 0)
+
+
+def _ln_vector(name, t, x, dtypes):
+    """Stride from worker to worker of a weight-like [N, h] or [h] tensor (0: one vector for all workers)."""
+    if t is None:
+        return 0
+    if not t.is_cuda or t.device != x.device or t.dtype not in dtypes:
+        raise ValueError(f"{name} must be on x's device and of type {' or '.join(str(d) for d in dtypes)}")
+    h, N = x.shape[-1], (x.shape[0] if x.dim() == 3 else 1)
+    if tuple(t.shape) not in ((h,), (N, h)) or (h > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must be [h] or [N, h] with a contiguous last axis")
+    return t.stride(0) if t.dim() == 2 else 0
+
+
+def liec_layer_norm_workspace_bytes(desc: liec_layer_norm_desc) -> int:
+    return int(load_library().liec_layer_norm_workspace_bytes(C.byref(desc)))
+
+
+def liec_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None, stream=None):
+    """Layer norm of [N, rows, h] (or [rows, h]) activations with per-worker float32 weight and bias
+    [N, h] (any stride between workers, e.g. ``params[:, a:a + h]``) or one [h] vector for all.
+    Returns (y, mean, rstd); mean and rstd [N, rows] float32 are what the backward pass needs."""
+    import torch
+    d = liec_layer_norm_desc()
+    d.x_row_stride, d.x_group_stride = _ln_rows("x", x)
+    d.weight_stride = _ln_vector("weight", weight, x, (torch.float32,))
+    d.bias_stride = _ln_vector("bias", bias, x, (torch.float32,))
+    raw, where = _on(x.device, stream)
+    with where:
+        if y is None:
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        d.y_row_stride, d.y_group_stride = _ln_rows("y", y, x)
+        stats = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device)
+        mean, rstd = stats[0], stats[1]
+        d.groups, d.rows, d.cols = (x.shape[0] if x.dim() == 3 else 1), x.shape[-2], x.shape[-1]
+        d.dtype, d.eps = (BF16 if x.dtype == torch.bfloat16 else F32), eps
+        lib = load_library()
+        st = lib.liec_layer_norm_forward(C.byref(d), x.data_ptr(), None if weight is None else weight.data_ptr(),
+                                         None if bias is None else bias.data_ptr(), y.data_ptr(), mean.data_ptr(),
+                                         rstd.data_ptr(), raw)
+    if st != 0:
+        raise LiecError(st, lib.liec_last_error(None).decode())
+    return y, mean, rstd
+
+
+def liec_layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias=None, workspace=None, stream=None):
+    """Gradients of liec_layer_norm_forward.  dweight and dbias: [N, h] float32 or bfloat16 (any stride between
+    workers, e.g. ``grads[:, a:a + h]``), or [h] for a vector that all workers share (its gradient is summed over
+    the workers too); allocated in float32, shaped like weight, where not given.  Returns (dx, dweight, dbias)."""
+    import torch
+    d = liec_layer_norm_desc()
+    d.x_row_stride, d.x_group_stride = _ln_rows("x", x)
+    d.y_row_stride, d.y_group_stride = _ln_rows("dy", dy, x)
+    d.weight_stride = _ln_vector("weight", weight, x, (torch.float32,))
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t.dtype != torch.float32 or t.shape != x.shape[:-1] or not t.is_contiguous() or t.device != x.device:
+            raise ValueError(f"{name} must be the contiguous float32 tensor that the forward pass returned")
+    N, rows, h = (x.shape[0] if x.dim() == 3 else 1), x.shape[-2], x.shape[-1]
+    raw, where = _on(x.device, stream)
+    with where:
+        if dx is None:
+            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        d.dx_row_stride, d.dx_group_stride = _ln_rows("dx", dx, x)
+        shape = weight.shape if weight is not None else (dweight if dweight is not None else dbias).shape \
+            if (dweight is not None or dbias is not None) else x.shape[:-2] + (h,)
+        if dweight is None:
+            dweight = torch.empty(shape, dtype=torch.float32 if dbias is None else dbias.dtype, device=x.device)
+        if dbias is None:
+            dbias = torch.empty(shape, dtype=dweight.dtype, device=x.device)
+        if dweight.dtype != dbias.dtype or dweight.dim() != dbias.dim():
+            raise ValueError("dweight and dbias must have the same type and number of axes")
+        d.dweight_stride = _ln_vector("dweight", dweight, x, (torch.float32, torch.bfloat16))
+        d.dbias_stride = _ln_vector("dbias", dbias, x, (torch.float32, torch.bfloat16))
+        d.groups, d.rows, d.cols = N, rows, h
+        if dweight.dim() == 1 and N > 1:   # one vector for all workers: its gradient sums over their rows as well
+            if d.weight_stride != 0:
+                raise ValueError("workers with weights of their own need dweight and dbias [N, h]")
+            if any(t.stride(0) != rows * t.stride(1) for t in (x, dy, dx)):
+                raise ValueError("a gradient shared by the workers needs x, dy and dx whose workers follow one another")
+            d.groups, d.rows = 1, N * rows
+        d.dtype = BF16 if x.dtype == torch.bfloat16 else F32
+        d.grad_dtype = BF16 if dweight.dtype == torch.bfloat16 else F32
+        lib = load_library()
+        need = lib.liec_layer_norm_workspace_bytes(C.byref(d))
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        st = lib.liec_layer_norm_backward(C.byref(d), dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                          None if weight is None else weight.data_ptr(), dx.data_ptr(), dweight.data_ptr(),
+                                          dbias.data_ptr(), workspace.data_ptr() if need else None,
+                                          workspace.numel() * workspace.element_size(), raw)
+    if st != 0:
+        raise LiecError(st, lib.liec_last_error(None).decode())
+    return dx, dweight, dbias
+
+
 class Context:
     """Owns a ``liec_ctx`` plus the torch tensors it points into (params, error, workspace)."""
 
@@ -207,6 +351,7 @@ class Context:
             raise LiecError(st, self.lib.liec_last_error(None).decode())
         self.grad_dtype = grad_dtype
         self.T = self.cfg.num_segments
+        self._sizes = np.diff(self._keep[0]).tolist()
 
     # -- helpers ---------------------------------------------------------------------------
     def _stream(self, stream=None) -> int:
@@ -296,6 +441,60 @@ class Context:
             self._check_grads(grads)
             gptr = grads.data_ptr()
         self._check(self.lib.liec_sumsq(self._ctx, int(which), gptr, out.data_ptr(), self._stream(stream)))
+
+    def _norms(self, norms):
+        t = self._torch
+        if norms is None:
+            return t.empty(self.N, dtype=t.float32, device=self.params.device)
+        if not norms.is_cuda or norms.dtype != t.float32 or norms.shape != (self.N,) or not norms.is_contiguous():
+            raise ValueError("norms must be a contiguous float32 CUDA tensor [N]")
+        return norms
+
+    def liec_clip_grads(self, grads, max_norm: float, out=None, norms=None, zero_nonfinite: bool = False, stream=None):
+        """Scales every worker's gradient row to at most max_norm, into `out` (default: in place).
+        Returns the norms before clipping, [N] float32."""
+        self._check_grads(grads)
+        out = grads if out is None else out
+        self._check_grads(out)
+        raw, where = _on(self.params.device, stream)
+        with where:
+            norms = self._norms(norms)
+            self._check(self.lib.liec_clip_grads(self._ctx, grads.data_ptr(), out.data_ptr(), max_norm, 1 if zero_nonfinite else 0,
+                                                 norms.data_ptr(), raw))
+        return norms
+
+    def liec_set_tensors(self, tensors, stream=None):
+        """The N*T gradient tensors of liec_gather_grads: N sequences of T contiguous CUDA tensors (None: no
+        gradient) with the segments' element counts, all float32 or all bfloat16.  They are referenced, not
+        copied; this object keeps them alive."""
+        t = self._torch
+        if len(tensors) != self.N or any(len(ts) != self.T for ts in tensors):
+            raise ValueError("tensors must be N sequences of T tensors")
+        sizes, device = self._sizes, self.params.device
+        dtype, ptrs = None, np.zeros(self.N * self.T, np.uint64)
+        q = 0
+        for ts in tensors:
+            for n, g in zip(sizes, ts):
+                if g is not None:
+                    dtype = g.dtype if dtype is None else dtype
+                    if g.dtype != dtype or g.numel() != n or g.device != device or not g.is_contiguous():
+                        raise ValueError("every tensor must be contiguous, on the context's device, of its segment's size and of one type")
+                    ptrs[q] = g.data_ptr()
+                q += 1
+        if dtype not in (None, t.float32, t.bfloat16):
+            raise ValueError("tensors must be float32 or bfloat16")
+        self._check(self.lib.liec_set_tensors(self._ctx, ptrs.ctypes.data, BF16 if dtype == t.bfloat16 else F32, self._stream(stream)))
+        self._tensors = [list(ts) for ts in tensors]
+
+    def liec_gather_grads(self, out, max_norm: float = float("inf"), norms=None, zero_nonfinite: bool = False, stream=None):
+        """Gradient rows from the tensors of liec_set_tensors, every worker's gradient scaled to at most
+        max_norm.  Returns the norms before clipping, [N] float32."""
+        self._check_grads(out)
+        raw, where = _on(self.params.device, stream)
+        with where:
+            norms = self._norms(norms)
+            self._check(self.lib.liec_gather_grads(self._ctx, out.data_ptr(), max_norm, 1 if zero_nonfinite else 0, norms.data_ptr(), raw))
+        return norms
 
     def liec_set_telemetry(self, on: bool):
         self._check(self.lib.liec_set_telemetry(self._ctx, 1 if on else 0))
