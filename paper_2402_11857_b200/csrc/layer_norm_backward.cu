@@ -1,0 +1,369 @@
+// Layer normalisation, backward pass for rows of up to 8192 columns.  Per row, with xh = (x - m) r and
+// q = dy w:  dx = r (q - mean(q) - xh mean(q xh));  per worker  dw = sum over rows of dy xh,  db = sum over
+// rows of dy.  x and dy cross HBM once: the column sums stay in the registers of the threads that own
+// the columns, for all the rows of a CTA, and meet in two steps (slots of a CTA, then CTAs).
+#include "layer_norm_common.cuh"
+
+namespace liec {
+
+__device__ __forceinline__ void store_grad(void *base, int64_t at, int grad_dtype, float v) {
+    if (grad_dtype == 0) ln_store(reinterpret_cast<float *>(base) + at, v);
+    else ln_store(reinterpret_cast<__nv_bfloat16 *>(base) + at, v);
+}
+
+// A CTA takes its share of all groups * rows rows, group after group.  Its rows of one group leave their
+// column sums as one piece; piece (b, group) lies at b + group, which no other pair on the staircase of
+// CTAs over groups shares.  With a.direct a group is one CTA's and the sums are the gradient.
+// With xc = x - m and g = dy r:  dx = g w - mean(g w) - xc r^2 mean(g w xc),  dw += g xc  (nine operations
+// per element instead of the ten of xh and q).
+template <typename T, int PIECE, int NV, int TPR, int SLOTS, int MINB, int R>
+__global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __grid_constant__ LnBackward a) {
+    using S = LnShape<T, PIECE, NV, TPR, SLOTS, MINB, R, 2>;
+    constexpr int VEC = S::VEC, P = VEC / 2;
+    extern __shared__ __align__(16) char ln_ring[];
+    __shared__ __align__(16) float box[2][SLOTS][S::WARPS][2 * R];
+    const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    const int h = a.cols;
+    const float inv_h = 1.0f / (float)h;
+    LnPipe<T, S, PIECE, NV, TPR> px[R], pd[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        px[j].place(ln_ring, slot * R + j);
+        pd[j].place(ln_ring, (SLOTS + slot) * R + j);
+    }
+    int flip = 0;
+    const int64_t total = (int64_t)a.groups * a.rows;
+    const int64_t u_end = min(total, a.share.first((int64_t)blockIdx.x + 1));
+    for (int64_t u = a.share.first(blockIdx.x); u < u_end;) {
+        const int group = (int)(u / a.rows);
+        const int64_t r0 = u - (int64_t)group * a.rows;
+        const int count = (int)(min(a.rows, r0 + (u_end - u)) - r0);    // rows of this group
+        u += count;
+        const int turns = (count + SLOTS * R - 1) / (SLOTS * R);
+        const T *x_next = reinterpret_cast<const T *>(a.x) + group * a.x_group + (r0 + slot * R) * a.x_row;       // the next row to fetch
+        const T *dy_next = reinterpret_cast<const T *>(a.dy) + group * a.dy_group + (r0 + slot * R) * a.dy_row;
+        T *dx = reinterpret_cast<T *>(a.dx) + group * a.dx_group + (r0 + slot * R) * a.dx_row;
+        const int64_t x_step = (int64_t)SLOTS * R * a.x_row, dy_step = (int64_t)SLOTS * R * a.dy_row, dx_step = (int64_t)SLOTS * R * a.dx_row;
+        const float *mean_at = a.mean + (int64_t)group * a.rows + r0 + slot * R, *rstd_at = a.rstd + (int64_t)group * a.rows + r0 + slot * R;
+        // (a group's first turn: zeros beyond column h; the column sums of the last group lay here)
+        if (h != S::COLS) {
+            for (int q = threadIdx.x; q < S::RING_BYTES / 16; q += S::THREADS) reinterpret_cast<uint4 *>(ln_ring)[q] = make_uint4(0u, 0u, 0u, 0u);
+            __syncthreads();
+        }
+        auto row_of = [&](int turn, int j) { return (turn * SLOTS + slot) * R + j; };
+        auto fetch = [&](int turn, int stage) {
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+                if (row_of(turn, j) < count) {
+                    px[j].fetch(x_next + j * a.x_row, t, h, stage);
+                    pd[j].fetch(dy_next + j * a.dy_row, t, h, stage);
+                }
+            x_next += x_step;
+            dy_next += dy_step;
+        };
+        auto land = [&](int turn, int stage) {
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                px[j].land(t, row_of(turn, j) < count ? h : 0, stage);
+                pd[j].land(t, row_of(turn, j) < count ? h : 0, stage);
+            }
+        };
+#pragma unroll
+        for (int s = 0; s < S::STAGES - 1; ++s) {
+            fetch(s, s);
+            if constexpr (PIECE == 2) land(s, s);
+            else copy_commit();
+        }
+        if constexpr (PIECE == 2) fetch(S::STAGES - 1, 0);
+        float mean_next[R], rstd_next[R];   // of rows that do not exist: zeros, which add nothing
+        auto statistics = [&](int turn) {
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                const bool live = row_of(turn, j) < count;
+                mean_next[j] = live ? __ldg(mean_at + j) : 0.0f;
+                rstd_next[j] = live ? __ldg(rstd_at + j) : 0.0f;
+            }
+            mean_at += SLOTS * R;
+            rstd_at += SLOTS * R;
+        };
+        statistics(0);
+        F2 w[NV][P], gw[NV][P], gb[NV][P];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            ln_parameters<P>(a.weight, group * a.weight_stride, (v * TPR + t) * VEC, h, 1.0f, w[v]);
+#pragma unroll
+            for (int k = 0; k < P; ++k) gw[v][k] = gb[v][k] = f2(0.0f);
+        }
+        for (int i = 0, stage = 0; i < turns; ++i) {
+            const int ahead = i + S::STAGES - 1;                               // turn to fetch now
+            const int into = stage == 0 ? S::STAGES - 1 : stage - 1;
+            if constexpr (PIECE == 16) {
+                fetch(ahead, into);
+                copy_commit();
+                copy_wait<S::STAGES - 1>();
+            } else if constexpr (PIECE == 4) {
+                copy_wait<S::STAGES - 2>();
+                slot_sync<TPR>(slot);      // the rows of turn i are complete, and all are done with turn i - 1
+                fetch(ahead, into);
+                copy_commit();
+            } else {
+                slot_sync<TPR>(slot);
+                land(ahead, into);
+                fetch(ahead + 1, 0);
+            }
+            float rstd[R], along[R], level[R];
+            F2 minus[R];
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                minus[j] = f2(-mean_next[j]);
+                rstd[j] = rstd_next[j];
+            }
+            statistics(i + 1);
+            F2 xc[R][NV][P], q[R][NV][P];
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                F2 along2 = f2(0.0f), level2 = f2(0.0f);
+                if (row_of(i, j) < count) {   // (zeros beyond column h add nothing to any sum)
+                    const F2 scale = f2(rstd[j]);
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) {
+                        F2 dy[P];
+                        LnChunk<T>::read(px[j].chunk(v, t, stage), xc[j][v]);
+                        LnChunk<T>::read(pd[j].chunk(v, t, stage), dy);
+#pragma unroll
+                        for (int k = 0; k < P; ++k) {
+                            xc[j][v][k] = add(xc[j][v][k], minus[j]);
+                            const F2 g = mul(dy[k], scale);
+                            q[j][v][k] = mul(g, w[v][k]);
+                            along2 = fma(q[j][v][k], xc[j][v][k], along2);
+                            level2 = add(level2, q[j][v][k]);
+                            gw[v][k] = fma(g, xc[j][v][k], gw[v][k]);
+                            gb[v][k] = add(gb[v][k], dy[k]);
+                        }
+                    }
+                }
+                along[j] = lo(along2) + hi(along2);
+                level[j] = lo(level2) + hi(level2);
+            }
+            if (a.dx) {
+                slot_sums<TPR, S::WARPS, R>(along, level, t, slot, box[flip]);
+                flip ^= 1;
+#pragma unroll
+                for (int j = 0; j < R; ++j) {
+                    const F2 tilt = f2(-(along[j] * inv_h * rstd[j]) * rstd[j]), shift = f2(-level[j] * inv_h);
+                    if (row_of(i, j) < count) {
+                        T *dxj = dx + j * a.dx_row;
+#pragma unroll
+                        for (int v = 0; v < NV; ++v) {
+                            const int c = (v * TPR + t) * VEC;
+#pragma unroll
+                            for (int k = 0; k < P; ++k) q[j][v][k] = fma(xc[j][v][k], tilt, add(q[j][v][k], shift));
+                            if constexpr (PIECE == 16) {
+                                if (c < h) LnChunk<T>::write(dxj + c, q[j][v]);
+                            } else {
+                                if (c + VEC > h) ln_keep<P>(q[j][v], h - c);   // the ring stays zero beyond the row
+                                LnChunk<T>::write(px[j].chunk(v, t, stage), q[j][v]);
+                            }
+                        }
+                    }
+                }
+                if constexpr (PIECE < 16) {
+                    slot_sync<TPR>(slot);
+#pragma unroll
+                    for (int j = 0; j < R; ++j)
+                        ln_store_row<T, S, PIECE, TPR>(dx + j * a.dx_row, px[j].ring + stage * S::STAGE_BYTES, t, row_of(i, j) < count ? h : 0);
+                }
+                dx += dx_step;
+            }
+            stage = stage + 1 == S::STAGES ? 0 : stage + 1;
+        }
+        if constexpr (PIECE != 2) copy_wait<0>();
+        __syncthreads();   // the ring is free: for the sums of the slots and for the next group
+        if (!a.dweight && !a.dbias) continue;
+        // the slots' sums meet: lanes of one warp by shuffles, then halves of the CTA through shared memory
+        if constexpr (TPR < 32) {
+#pragma unroll
+            for (int m = TPR; m < 32; m <<= 1)
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int k = 0; k < P; ++k) {
+                        gw[v][k].v = add(gw[v][k], F2{__shfl_xor_sync(0xffffffffu, gw[v][k].v, m)}).v;
+                        gb[v][k].v = add(gb[v][k], F2{__shfl_xor_sync(0xffffffffu, gb[v][k].v, m)}).v;
+                    }
+        }
+        constexpr int TEAM = TPR < 32 ? 32 : TPR, TEAMS = S::THREADS / TEAM;   // threads that hold one set of sums
+        const int team = threadIdx.x / TEAM, place = threadIdx.x % TEAM;
+        F2 *meet = reinterpret_cast<F2 *>(ln_ring) + place;   // [TEAMS / 2][E pairs][TEAM]
+#pragma unroll
+        for (int half = TEAMS / 2; half >= 1; half /= 2) {
+            if (team >= half && team < 2 * half) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int k = 0; k < P; ++k) {
+                        meet[((team - half) * S::E + v * P + k) * TEAM] = gw[v][k];
+                        meet[((team - half) * S::E + S::E / 2 + v * P + k) * TEAM] = gb[v][k];
+                    }
+            }
+            __syncthreads();
+            if (team < half) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int k = 0; k < P; ++k) {
+                        gw[v][k] = add(gw[v][k], meet[(team * S::E + v * P + k) * TEAM]);
+                        gb[v][k] = add(gb[v][k], meet[(team * S::E + S::E / 2 + v * P + k) * TEAM]);
+                    }
+            }
+            __syncthreads();
+        }
+        if (team == 0 && (TPR >= 32 || place < TPR)) {
+            const int64_t piece = ((int64_t)blockIdx.x + group) * h;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    const int c = (v * TPR + t) * VEC + k;
+                    const float sw = (k & 1) ? hi(gw[v][k / 2]) : lo(gw[v][k / 2]), sb = (k & 1) ? hi(gb[v][k / 2]) : lo(gb[v][k / 2]);
+                    if (c < h) {
+                        if (a.direct) {
+                            if (a.dweight) store_grad(a.dweight, group * a.dweight_stride + c, a.grad_dtype, sw);
+                            if (a.dbias) store_grad(a.dbias, group * a.dbias_stride + c, a.grad_dtype, sb);
+                        } else {
+                            a.part_w[piece + c] = sw;
+                            a.part_b[piece + c] = sb;
+                        }
+                    }
+                }
+        }
+    }
+}
+
+// Joins the pieces of a group, in binary64 and in a fixed order, and rounds once to the gradient rows'
+// type: 32 columns per CTA, four per thread, 32 threads per column.
+__global__ void __launch_bounds__(256) ln_backward_join_kernel(const __grid_constant__ LnBackward a) {
+    __shared__ double buf[8][32];
+    const int group = blockIdx.y;
+    const bool weight = blockIdx.z == 0;
+    void *out = weight ? a.dweight : a.dbias;
+    if (!out) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, way = threadIdx.x >> 3;
+    const int c = blockIdx.x * 32 + (threadIdx.x & 7) * 4;
+    int64_t first = (int64_t)group * a.runs;   // pieces of the group: runs of rows, or the parts of CTAs' shares
+    int pieces = a.runs;
+    if (a.share.ctas > 0) {
+        first = a.share.owner((int64_t)group * a.rows) + group;
+        pieces = (int)(a.share.owner(((int64_t)group + 1) * a.rows - 1) + group - first) + 1;
+    }
+    const float *p = (weight ? a.part_w : a.part_b) + (first + way) * a.cols + c;
+    const int64_t step = (int64_t)32 * a.cols;
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    if ((a.cols & 3) == 0 && c < a.cols) {
+#pragma unroll 4
+        for (int q = way; q < pieces; q += 32, p += step) {
+            const float4 v = __ldcs(reinterpret_cast<const float4 *>(p));
+            s[0] += (double)v.x; s[1] += (double)v.y; s[2] += (double)v.z; s[3] += (double)v.w;
+        }
+    } else {
+        for (int q = way; q < pieces; q += 32, p += step)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (c + k < a.cols) s[k] += (double)__ldcs(p + k);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        s[k] += __shfl_xor_sync(0xffffffffu, s[k], 8);
+        s[k] += __shfl_xor_sync(0xffffffffu, s[k], 16);
+        if (lane < 8) buf[warp][lane * 4 + k] = s[k];
+    }
+    __syncthreads();
+    const int cl = blockIdx.x * 32 + lane;
+    if (warp == 0 && cl < a.cols) {
+        const double t = ((buf[0][lane] + buf[1][lane]) + (buf[2][lane] + buf[3][lane])) + ((buf[4][lane] + buf[5][lane]) + (buf[6][lane] + buf[7][lane]));
+        store_grad(out, group * (weight ? a.dweight_stride : a.dbias_stride) + cl, a.grad_dtype, (float)t);
+    }
+}
+
+// Rows per turn and slot.  Two rows at once (half the exchanges, twice the registers) measured slower: at
+// 4 x 4096 rows of 4096 bfloat16 columns 95 against 83 us.
+constexpr int LN_BACKWARD_TURN = 1;
+
+struct LnPlan {
+    LnShare share;
+    int64_t pieces;
+    bool direct;
+};
+
+struct LnPlanner {
+    int groups;
+    int64_t rows;
+    template <int TPR, int E, int SLOTS, int MINB>
+    LnPlan operator()() const {
+        constexpr int R = LN_BACKWARD_TURN;
+        const int64_t total = (int64_t)groups * rows;
+        const int resident = LN_SMS * MINB;
+        LnPlan p;
+        // one CTA per group and no second launch: a few turns cost less than the launch; and with many
+        // groups their CTAs fill the GPU several times over anyway
+        p.direct = rows <= 8 * SLOTS * R || (groups >= 4 * resident && rows <= (int64_t)SLOTS * LN_SUM_ROWS);
+        p.share = p.direct ? LnShare{0, 0, rows, groups} : ln_share(total, SLOTS * R, resident, LN_SUM_ROWS / R, false);
+        p.pieces = p.direct ? 0 : p.share.ctas + groups;
+        return p;
+    }
+};
+
+size_t layer_norm_workspace(int groups, int64_t rows, int cols) {
+    if (rows == 0) return 0;
+    const int64_t pieces = cols > LN_REGISTER_COLS ? groups * ln_wide_runs(rows) : ln_backward_shape(cols, LnPlanner{groups, rows}).pieces;
+    return sizeof(float) * 2 * (size_t)std::max<int64_t>(pieces, groups) * (size_t)cols;
+}
+
+template <typename T, int PIECE>
+struct LnBackwardLaunch {
+    LnBackward a;
+    cudaStream_t st;
+    template <int TPR, int E, int SLOTS, int MINB>
+    cudaError_t operator()() {
+        constexpr int NV = E / LnChunk<T>::VEC;
+        constexpr int R = LN_BACKWARD_TURN;
+        using S = LnShape<T, PIECE, NV, TPR, SLOTS, MINB, R, 2>;
+        static_assert(S::THREADS <= 32 || S::RING_BYTES >= S::THREADS * S::E * 4, "half the CTA's column sums meet in the ring");
+        static std::atomic<uint64_t> allowed{0};
+        auto kernel = ln_backward_kernel<T, PIECE, NV, TPR, SLOTS, MINB, R>;
+        const cudaError_t e = ln_allow_smem(kernel, S::RING_BYTES, allowed);
+        if (e != cudaSuccess) return e;
+        kernel<<<(unsigned)a.share.ctas, S::THREADS, S::RING_BYTES, st>>>(a);
+        return cudaGetLastError();
+    }
+};
+
+static cudaError_t backward_rows(LnBackward &a, int dtype, cudaStream_t st) {
+    if (a.cols > LN_REGISTER_COLS) return launch_layer_norm_backward_wide(a, dtype, st);
+    const int esz = dtype == 0 ? 4 : 2;
+    int piece = std::min(ln_piece(a.x, a.x_row, a.x_group, a.rows, a.groups, a.cols, esz),
+                         ln_piece(a.dy, a.dy_row, a.dy_group, a.rows, a.groups, a.cols, esz));
+    if (a.dx) piece = std::min(piece, ln_piece(a.dx, a.dx_row, a.dx_group, a.rows, a.groups, a.cols, esz));
+    const LnPlan p = ln_backward_shape(a.cols, LnPlanner{a.groups, a.rows});
+    a.share = p.share;
+    a.direct = p.direct;
+    if (dtype == 0)
+        return piece == 16 ? ln_backward_shape(a.cols, LnBackwardLaunch<float, 16>{a, st}) : ln_backward_shape(a.cols, LnBackwardLaunch<float, 4>{a, st});
+    if (piece == 16) return ln_backward_shape(a.cols, LnBackwardLaunch<__nv_bfloat16, 16>{a, st});
+    if (piece == 4) return ln_backward_shape(a.cols, LnBackwardLaunch<__nv_bfloat16, 4>{a, st});
+    return ln_backward_shape(a.cols, LnBackwardLaunch<__nv_bfloat16, 2>{a, st});
+}
+
+cudaError_t launch_layer_norm_backward(LnBackward a, int dtype, cudaStream_t st) {
+    if (a.rows > 0) {
+        const cudaError_t e = backward_rows(a, dtype, st);
+        if (e != cudaSuccess) return e;
+    }
+    if ((a.dweight || a.dbias) && !a.direct) {
+        ln_backward_join_kernel<<<dim3((a.cols + 31) / 32, a.groups, 2), 256, 0, st>>>(a);
+        return cudaGetLastError();
+    }
+    return cudaSuccess;
+}
+
+}  // namespace liec

@@ -1,0 +1,208 @@
+// Layer normalisation, forward pass for rows of up to 8192 columns: every element crosses HBM once.
+// Per row: m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps), y = (x - m) r w + b.
+#include "layer_norm_common.cuh"
+
+namespace liec {
+
+// A CTA takes its share of all groups * rows rows, group after group; every thread of the CTA makes the
+// same number of turns, a turn being R consecutive rows for every slot.
+template <typename T, int PIECE, int NV, int TPR, int SLOTS, int MINB, int R>
+__global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __grid_constant__ LnForward a) {
+    using S = LnShape<T, PIECE, NV, TPR, SLOTS, MINB, R, 1>;
+    constexpr int VEC = S::VEC, P = VEC / 2;
+    extern __shared__ __align__(16) char ln_ring[];
+    __shared__ __align__(16) float box[2][SLOTS][S::WARPS][2 * R];
+    const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    const int h = a.cols;
+    const float inv_h = 1.0f / (float)h;
+    LnPipe<T, S, PIECE, NV, TPR> px[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) px[j].place(ln_ring, slot * R + j);
+    if (h != S::COLS)   // zeros beyond column h
+        for (int q = threadIdx.x; q < S::RING_BYTES / 16; q += S::THREADS) reinterpret_cast<uint4 *>(ln_ring)[q] = make_uint4(0u, 0u, 0u, 0u);
+    __syncthreads();
+    int flip = 0;
+    const int64_t total = (int64_t)a.groups * a.rows;
+    const int64_t u_end = min(total, a.share.first((int64_t)blockIdx.x + 1));
+    for (int64_t u = a.share.first(blockIdx.x); u < u_end;) {
+        const int group = (int)(u / a.rows);
+        const int64_t r0 = u - (int64_t)group * a.rows;
+        const int count = (int)(min(a.rows, r0 + (u_end - u)) - r0);    // rows of this group
+        u += count;
+        const int turns = (count + SLOTS * R - 1) / (SLOTS * R);
+        const T *x_next = reinterpret_cast<const T *>(a.x) + group * a.x_group + (r0 + slot * R) * a.x_row;   // the next row to fetch
+        T *y = reinterpret_cast<T *>(a.y) + group * a.y_group + (r0 + slot * R) * a.y_row;
+        int64_t at = (int64_t)group * a.rows + r0 + slot * R;
+        const int64_t x_step = (int64_t)SLOTS * R * a.x_row, y_step = (int64_t)SLOTS * R * a.y_row;
+        auto row_of = [&](int turn, int j) { return (turn * SLOTS + slot) * R + j; };
+        auto fetch = [&](int turn, int stage) {
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+                if (row_of(turn, j) < count) px[j].fetch(x_next + j * a.x_row, t, h, stage);
+            x_next += x_step;
+        };
+        auto land = [&](int turn, int stage) {
+#pragma unroll
+            for (int j = 0; j < R; ++j) px[j].land(t, row_of(turn, j) < count ? h : 0, stage);
+        };
+#pragma unroll
+        for (int s = 0; s < S::STAGES - 1; ++s) {
+            fetch(s, s);
+            if constexpr (PIECE == 2) land(s, s);
+            else copy_commit();
+        }
+        if constexpr (PIECE == 2) fetch(S::STAGES - 1, 0);
+        F2 w[NV][P], b[NV][P];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            ln_parameters<P>(a.weight, group * a.weight_stride, (v * TPR + t) * VEC, h, 1.0f, w[v]);
+            ln_parameters<P>(a.bias, group * a.bias_stride, (v * TPR + t) * VEC, h, 0.0f, b[v]);
+        }
+        for (int i = 0, stage = 0; i < turns; ++i) {
+            const int ahead = i + S::STAGES - 1;                               // turn to fetch now
+            const int into = stage == 0 ? S::STAGES - 1 : stage - 1;
+            if constexpr (PIECE == 16) {
+                fetch(ahead, into);
+                copy_commit();
+                copy_wait<S::STAGES - 1>();
+            } else if constexpr (PIECE == 4) {
+                copy_wait<S::STAGES - 2>();
+                slot_sync<TPR>(slot);      // the rows of turn i are complete, and all are done with turn i - 1
+                fetch(ahead, into);
+                copy_commit();
+            } else {
+                slot_sync<TPR>(slot);
+                land(ahead, into);
+                fetch(ahead + 1, 0);
+            }
+            F2 x[R][NV][P];
+            float mean[R], var[R];
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                F2 s2 = f2(0.0f), q2 = f2(0.0f);
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    LnChunk<T>::read(px[j].chunk(v, t, stage), x[j][v]);   // (zeros beyond column h)
+#pragma unroll
+                    for (int k = 0; k < P; ++k) {
+                        s2 = add(s2, x[j][v][k]);
+                        q2 = fma(x[j][v][k], x[j][v][k], q2);
+                    }
+                }
+                mean[j] = lo(s2) + hi(s2);
+                var[j] = lo(q2) + hi(q2);
+            }
+            slot_sums<TPR, S::WARPS, R>(mean, var, t, slot, box[flip]);
+            flip ^= 1;
+            // var = mean(x^2) - mean^2 keeps its digits while mean^2 is at most a quarter of it (the difference
+            // then carries at most 1.25 times the relative error of the sums) and nothing overflowed; other
+            // rows sum the squares around their mean
+            bool far[R], any_far = false;
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                mean[j] *= inv_h;
+                var[j] = __fmaf_rn(-mean[j], mean[j], var[j] * inv_h);
+                far[j] = !(mean[j] * mean[j] <= 0.25f * var[j] && var[j] < 1e37f);
+                any_far |= far[j];
+                const F2 minus = f2(-mean[j]);
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int k = 0; k < P; ++k) x[j][v][k] = add(x[j][v][k], minus);
+            }
+            if (TPR < 32 ? __any_sync(0xffffffffu, any_far) : any_far) {   // (the same for all threads of a slot)
+                float around[R], unused[R];
+#pragma unroll
+                for (int j = 0; j < R; ++j) {
+                    F2 d2 = f2(0.0f);
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) {
+                        const int left = h - (v * TPR + t) * VEC;
+                        F2 d[P];
+#pragma unroll
+                        for (int k = 0; k < P; ++k) d[k] = x[j][v][k];
+                        if (left < VEC) ln_keep<P>(d, left);
+#pragma unroll
+                        for (int k = 0; k < P; ++k) d2 = fma(d[k], d[k], d2);
+                    }
+                    around[j] = lo(d2) + hi(d2);
+                    unused[j] = 0.0f;
+                }
+                slot_sums<TPR, S::WARPS, R>(around, unused, t, slot, box[flip]);
+                flip ^= 1;
+#pragma unroll
+                for (int j = 0; j < R; ++j)
+                    if (far[j]) var[j] = around[j] * inv_h;
+            }
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                const bool live = row_of(i, j) < count;
+                const float rstd = rsqrtf(var[j] + a.eps);
+                const F2 scale = f2(rstd);
+                T *yj = y + j * a.y_row;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const int c = (v * TPR + t) * VEC;
+#pragma unroll
+                    for (int k = 0; k < P; ++k) x[j][v][k] = fma(mul(x[j][v][k], scale), w[v][k], b[v][k]);
+                    if constexpr (PIECE == 16) {
+                        if (live && c < h) LnChunk<T>::write(yj + c, x[j][v]);
+                    } else {
+                        if (c + VEC > h) ln_keep<P>(x[j][v], h - c);   // the ring stays zero beyond the row
+                        LnChunk<T>::write(px[j].chunk(v, t, stage), x[j][v]);
+                    }
+                }
+                if (live && t == 0) {
+                    if (a.mean) a.mean[at + j] = mean[j];
+                    if (a.rstd) a.rstd[at + j] = rstd;
+                }
+            }
+            if constexpr (PIECE < 16) {
+                slot_sync<TPR>(slot);
+#pragma unroll
+                for (int j = 0; j < R; ++j)
+                    ln_store_row<T, S, PIECE, TPR>(y + j * a.y_row, px[j].ring + stage * S::STAGE_BYTES, t, row_of(i, j) < count ? h : 0);
+            }
+            y += y_step;
+            at += SLOTS * R;
+            stage = stage + 1 == S::STAGES ? 0 : stage + 1;
+        }
+        if constexpr (PIECE != 2) copy_wait<0>();
+        if constexpr (PIECE != 16) __syncthreads();   // the next group's rows go into the same ring
+    }
+}
+
+template <typename T, int PIECE>
+struct LnForwardLaunch {
+    LnForward a;
+    cudaStream_t st;
+    template <int TPR, int E, int SLOTS, int MINB>
+    cudaError_t operator()() {
+        constexpr int NV = E / LnChunk<T>::VEC;
+        constexpr int R = E <= 16 ? 2 : 1;   // rows per turn: two where the registers hold them
+        using S = LnShape<T, PIECE, NV, TPR, SLOTS, MINB, R, 1>;
+        static std::atomic<uint64_t> allowed{0};
+        auto kernel = ln_forward_kernel<T, PIECE, NV, TPR, SLOTS, MINB, R>;
+        const cudaError_t e = ln_allow_smem(kernel, S::RING_BYTES, allowed);
+        if (e != cudaSuccess) return e;
+        // (one CTA per SM: a small share would leave its SM idle while it starts)
+        a.share = ln_share((int64_t)a.groups * a.rows, SLOTS * R, LN_SMS * MINB, 1 << 30, MINB > 1);
+        kernel<<<(unsigned)a.share.ctas, S::THREADS, S::RING_BYTES, st>>>(a);
+        return cudaGetLastError();
+    }
+};
+
+cudaError_t launch_layer_norm_forward(const LnForward &a, int dtype, cudaStream_t st) {
+    if (a.rows == 0) return cudaSuccess;
+    if (a.cols > LN_REGISTER_COLS) return launch_layer_norm_forward_wide(a, dtype, st);
+    const int esz = dtype == 0 ? 4 : 2;
+    const int piece = std::min(ln_piece(a.x, a.x_row, a.x_group, a.rows, a.groups, a.cols, esz),
+                               ln_piece(a.y, a.y_row, a.y_group, a.rows, a.groups, a.cols, esz));
+    if (dtype == 0)
+        return piece == 16 ? ln_forward_shape(a.cols, LnForwardLaunch<float, 16>{a, st}) : ln_forward_shape(a.cols, LnForwardLaunch<float, 4>{a, st});
+    if (piece == 16) return ln_forward_shape(a.cols, LnForwardLaunch<__nv_bfloat16, 16>{a, st});
+    if (piece == 4) return ln_forward_shape(a.cols, LnForwardLaunch<__nv_bfloat16, 4>{a, st});
+    return ln_forward_shape(a.cols, LnForwardLaunch<__nv_bfloat16, 2>{a, st});
+}
+
+}  // namespace liec

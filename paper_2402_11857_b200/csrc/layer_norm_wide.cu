@@ -1,23 +1,8 @@
-// Layer normalisation of N workers' activations at once, and its backward pass.  Per row x of h
-// elements, with the worker's own weight w and bias b:
-//   m = mean(x),  r = 1 / sqrt(mean((x - m)^2) + eps),  xh = (x - m) r,  y = xh w + b
-//   dx = r (dy w - mean(dy w) - xh mean(dy w xh)),  dw = sum over rows of dy xh,  db = sum over rows of dy
-// Sums are binary32 over at most a few hundred terms per accumulator, joined in binary64; the variance
-// is taken around the mean (never as a difference of squares).  The order of every sum is fixed by the
-// sizes alone: no atomics.
-#include "layer_norm.h"
-
-#include <cuda_bf16.h>
-#include <cuda_runtime.h>
+// Layer normalisation of rows wider than 8192 columns: a CTA sweeps a row three times (twice in the backward
+// pass), the later sweeps out of L1 and L2; the column sums of the backward pass are a kernel of their own.
+#include "layer_norm_common.cuh"
 
 namespace liec {
-
-__device__ __forceinline__ float ln_load(const float *p) { return __ldg(p); }
-__device__ __forceinline__ float ln_load(const __nv_bfloat16 *p) {
-    return __uint_as_float((uint32_t)__ldg(reinterpret_cast<const unsigned short *>(p)) << 16);
-}
-__device__ __forceinline__ void ln_store(float *p, float v) { *p = v; }
-__device__ __forceinline__ void ln_store(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -125,66 +110,34 @@ __global__ void __launch_bounds__(LN_THREADS) ln_backward_columns_kernel(const _
     }
 }
 
-// Joins the runs in run order, in binary64, and rounds once to the gradient rows' type.
-template <typename GT>
-__global__ void __launch_bounds__(LN_THREADS) ln_backward_join_kernel(const __grid_constant__ LnBackward a) {
-    const int group = blockIdx.y;
-    const int c = blockIdx.x * LN_THREADS + threadIdx.x;
-    if (c >= a.cols) return;
-    double tw = 0.0, tb = 0.0;
-    for (int run = 0; run < a.runs; ++run) {
-        const int64_t at = ((int64_t)group * a.runs + run) * a.cols + c;
-        tw += (double)a.part_w[at];
-        tb += (double)a.part_b[at];
-    }
-    if (a.dweight) ln_store(reinterpret_cast<GT *>(a.dweight) + (int64_t)group * a.dweight_stride + c, (float)tw);
-    if (a.dbias) ln_store(reinterpret_cast<GT *>(a.dbias) + (int64_t)group * a.dbias_stride + c, (float)tb);
-}
 
-// Rows whose column sums one CTA takes: 1024, i.e. 128 terms per binary32 accumulator, and more only
-// where there would be more than 32768 runs (grid y).
-static int64_t ln_run_rows(int64_t rows) {
+// Rows whose column sums one CTA of ln_backward_columns_kernel takes: 1024, i.e. 128 terms per binary32
+// accumulator, and more only where there would be more than 32768 runs (grid y).
+static int64_t run_rows(int64_t rows) {
     const int64_t even = (rows + 32767) / 32768;
     return even > 1024 ? even : 1024;
 }
-static int64_t ln_runs(int64_t rows) { return (rows + ln_run_rows(rows) - 1) / ln_run_rows(rows); }
+int64_t ln_wide_runs(int64_t rows) { return (rows + run_rows(rows) - 1) / run_rows(rows); }
 
-template <typename T>
-static cudaError_t forward_t(const LnForward &a, cudaStream_t st) {
-    const dim3 grid((unsigned)(a.rows < 65536 ? a.rows : 65536), a.groups);
-    ln_forward_rows_kernel<T><<<grid, LN_THREADS, 0, st>>>(a);
+cudaError_t launch_layer_norm_forward_wide(const LnForward &a, int dtype, cudaStream_t st) {
+    const dim3 grid((unsigned)std::min<int64_t>(a.rows, 65536), a.groups);
+    if (dtype == 0) ln_forward_rows_kernel<float><<<grid, LN_THREADS, 0, st>>>(a);
+    else ln_forward_rows_kernel<__nv_bfloat16><<<grid, LN_THREADS, 0, st>>>(a);
     return cudaGetLastError();
 }
 
-cudaError_t launch_layer_norm_forward(const LnForward &a, int dtype, cudaStream_t st) {
-    if (a.rows == 0) return cudaSuccess;
-    return dtype == 0 ? forward_t<float>(a, st) : forward_t<__nv_bfloat16>(a, st);
-}
-
 template <typename T>
-static cudaError_t backward_t(const LnBackward &a, int grad_dtype, cudaStream_t st) {
-    if (a.rows > 0 && a.dx) {
-        const dim3 grid((unsigned)(a.rows < 65536 ? a.rows : 65536), a.groups);
-        ln_backward_rows_kernel<T><<<grid, LN_THREADS, 0, st>>>(a);
-    }
-    if (a.dweight || a.dbias) {
-        if (a.rows > 0)
-            ln_backward_columns_kernel<T><<<dim3((a.cols + 31) / 32, (unsigned)a.runs, a.groups), LN_THREADS, 0, st>>>(a);
-        const dim3 grid((a.cols + LN_THREADS - 1) / LN_THREADS, a.groups);
-        if (grad_dtype == 0) ln_backward_join_kernel<float><<<grid, LN_THREADS, 0, st>>>(a);
-        else ln_backward_join_kernel<__nv_bfloat16><<<grid, LN_THREADS, 0, st>>>(a);
-    }
+static cudaError_t backward_wide_t(const LnBackward &a, cudaStream_t st) {
+    if (a.dx) ln_backward_rows_kernel<T><<<dim3((unsigned)std::min<int64_t>(a.rows, 65536), a.groups), LN_THREADS, 0, st>>>(a);
+    if (a.dweight || a.dbias)
+        ln_backward_columns_kernel<T><<<dim3((a.cols + 31) / 32, (unsigned)a.runs, a.groups), LN_THREADS, 0, st>>>(a);
     return cudaGetLastError();
 }
 
-cudaError_t launch_layer_norm_backward(LnBackward a, int dtype, int grad_dtype, cudaStream_t st) {
-    a.run_rows = ln_run_rows(a.rows);
-    a.runs = (int)ln_runs(a.rows);
-    return dtype == 0 ? backward_t<float>(a, grad_dtype, st) : backward_t<__nv_bfloat16>(a, grad_dtype, st);
-}
-
-size_t layer_norm_workspace(int groups, int64_t rows, int cols) {
-    return sizeof(float) * 2 * (size_t)groups * (size_t)ln_runs(rows) * (size_t)cols;
+cudaError_t launch_layer_norm_backward_wide(LnBackward &a, int dtype, cudaStream_t st) {
+    a.run_rows = run_rows(a.rows);
+    a.runs = (int)ln_wide_runs(a.rows);
+    return dtype == 0 ? backward_wide_t<float>(a, st) : backward_wide_t<__nv_bfloat16>(a, st);
 }
 
 }  // namespace liec

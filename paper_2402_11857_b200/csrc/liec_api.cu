@@ -985,11 +985,11 @@ liec_status liec_layer_norm_backward(const liec_layer_norm_desc *d, const void *
     a.dy = dy; a.x = x; a.mean = mean; a.rstd = rstd; a.weight = weight; a.dx = dx; a.dweight = dweight; a.dbias = dbias;
     a.part_w = static_cast<float *>(workspace);
     a.part_b = a.part_w + need / (2 * sizeof(float));
-    a.rows = d->rows; a.groups = d->groups; a.cols = d->cols;
+    a.rows = d->rows; a.groups = d->groups; a.cols = d->cols; a.grad_dtype = d->grad_dtype;
     a.x_row = d->x_row_stride; a.x_group = d->x_group_stride; a.dy_row = d->y_row_stride; a.dy_group = d->y_group_stride;
     a.dx_row = d->dx_row_stride; a.dx_group = d->dx_group_stride;
     a.weight_stride = d->weight_stride; a.dweight_stride = d->dweight_stride; a.dbias_stride = d->dbias_stride;
-    const cudaError_t e = launch_layer_norm_backward(a, d->dtype, d->grad_dtype, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_layer_norm_backward(a, d->dtype, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return ln_refuse(LIEC_ERR_CUDA, cudaGetErrorString(e));
     return LIEC_OK;
 }

@@ -5,8 +5,8 @@ fallback: if ``libliec.so`` is missing or a call fails, an exception is raised.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -204,72 +204,143 @@ def liec_sign_compress_noalloc(x, words, scale, stream=None):
 
 # ---- layer normalisation over N workers -----------------------------------------------------------
 
-def _on(device, stream):
-    """(raw stream, context manager): where a call on `device` runs and where its outputs are allocated."""
+def _device_of(name, t) -> int:
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"{name} must be a CUDA tensor (there is no CPU path)")
+    return index
+
+
+def _launch(device: int, stream, fn, *args):
+    """fn(raw stream, *args) on the caller's stream and the tensors' device; what fn allocates belongs to that stream."""
     import torch
     if stream is not None:
-        return stream.cuda_stream, torch.cuda.stream(stream)
-    if device.index != torch.cuda.current_device():
-        return torch.cuda.current_stream(device).cuda_stream, torch.cuda.device(device)
-    return torch.cuda.current_stream(device).cuda_stream, _HERE
+        with torch.cuda.stream(stream):
+            return fn(stream.cuda_stream, *args)
+    if device != torch._C._cuda_getDevice():
+        with torch.cuda.device(device):
+            return fn(torch._C._cuda_getCurrentRawStream(device), *args)
+    return fn(torch._C._cuda_getCurrentRawStream(device), *args)
 
 
-_HERE = contextlib.nullcontext()
+def _layout(t):
+    return None if t is None else (t.shape, t.stride(), t.dtype)
 
 
-def _ln_rows(name, t, like=None):
-    """Row and group strides of [N, rows, h] or [rows, h] activations (N = 1)."""
-    import torch
-    if not t.is_cuda or t.dtype not in (torch.float32, torch.bfloat16) or t.dim() not in (2, 3):
-        raise ValueError(f"{name} must be a CUDA tensor [N, rows, h] or [rows, h] of float32 or bfloat16")
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
-        raise ValueError(f"{name} must have the shape, type and device of x")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+def _ln_rows(name, t, x):
+    """Row and group strides of [N, rows, h] or [rows, h] activations (N = 1), given as a layout."""
+    shape, stride, dtype = t
+    if shape != x[0] or dtype != x[2]:
+        raise ValueError(f"{name} must have the shape and type of x")
+    if shape[-1] > 1 and stride[-1] != 1:
         raise ValueError(f"the last axis of {name} must be contiguous")
-    return t.stride(-2), (t.stride(0) if t.dim() == 3 else 0)
+    return stride[-2], (stride[0] if len(shape) == 3 else 0)
 
 
 def _ln_vector(name, t, x, dtypes):
     """Stride from worker to worker of a weight-like [N, h] or [h] tensor (0: one vector for all workers)."""
     if t is None:
         return 0
-    if not t.is_cuda or t.device != x.device or t.dtype not in dtypes:
-        raise ValueError(f"{name} must be on x's device and of type {' or '.join(str(d) for d in dtypes)}")
-    h, N = x.shape[-1], (x.shape[0] if x.dim() == 3 else 1)
-    if tuple(t.shape) not in ((h,), (N, h)) or (h > 1 and t.stride(-1) != 1):
+    shape, stride, dtype = t
+    h, N = x[0][-1], (x[0][0] if len(x[0]) == 3 else 1)
+    if dtype not in dtypes:
+        raise ValueError(f"{name} must be of type {' or '.join(str(d) for d in dtypes)}")
+    if tuple(shape) not in ((h,), (N, h)) or (h > 1 and stride[-1] != 1):
         raise ValueError(f"{name} must be [h] or [N, h] with a contiguous last axis")
-    return t.stride(0) if t.dim() == 2 else 0
+    return stride[0] if len(shape) == 2 else 0
+
+
+@functools.lru_cache(maxsize=1024)
+def _ln_desc(x, y, dx, weight, bias, dweight, dbias, eps):
+    """Checks the layouts of a call and returns its descriptor and workspace size (both depend on sizes,
+    strides and types alone, so calls of the same form share them)."""
+    import torch
+    both, f32 = (torch.float32, torch.bfloat16), (torch.float32,)
+    shape = x[0]
+    if x[2] not in both or len(shape) not in (2, 3):
+        raise ValueError("x must be [N, rows, h] or [rows, h] of float32 or bfloat16")
+    d = liec_layer_norm_desc()
+    d.groups, d.rows, d.cols = (shape[0] if len(shape) == 3 else 1), shape[-2], shape[-1]
+    d.dtype, d.eps = (BF16 if x[2] == torch.bfloat16 else F32), eps
+    d.x_row_stride, d.x_group_stride = _ln_rows("x", x, x)
+    d.y_row_stride, d.y_group_stride = _ln_rows("y" if dx is None else "dy", y, x)
+    d.weight_stride, d.bias_stride = _ln_vector("weight", weight, x, f32), _ln_vector("bias", bias, x, f32)
+    if dx is None:
+        return d, C.byref(d), 0
+    d.dx_row_stride, d.dx_group_stride = _ln_rows("dx", dx, x)
+    d.dweight_stride, d.dbias_stride = _ln_vector("dweight", dweight, x, both), _ln_vector("dbias", dbias, x, both)
+    if dweight[2] != dbias[2] or len(dweight[0]) != len(dbias[0]):
+        raise ValueError("dweight and dbias must have the same type and number of axes")
+    d.grad_dtype = BF16 if dweight[2] == torch.bfloat16 else F32
+    if len(dweight[0]) == 1 and d.groups > 1:   # one vector for all workers: its gradient sums over their rows as well
+        if d.weight_stride != 0:
+            raise ValueError("workers with weights of their own need dweight and dbias [N, h]")
+        if any(t[1][0] != d.rows * t[1][1] for t in (x, y, dx)):
+            raise ValueError("a gradient shared by the workers needs x, dy and dx whose workers follow one another")
+        d.groups, d.rows = 1, d.groups * d.rows
+    return d, C.byref(d), int(load_library().liec_layer_norm_workspace_bytes(C.byref(d)))
 
 
 def liec_layer_norm_workspace_bytes(desc: liec_layer_norm_desc) -> int:
     return int(load_library().liec_layer_norm_workspace_bytes(C.byref(desc)))
 
 
+def _ln_failed(lib, st):
+    raise LiecError(st, lib.liec_last_error(None).decode())
+
+
+def _empty_like(x):
+    import torch
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
+def _ln_forward(raw, device, x, weight, bias, eps, y):
+    import torch
+    if y is None:
+        y = _empty_like(x)
+    _, ref, _ = _ln_desc(_layout(x), _layout(y), None, _layout(weight), _layout(bias), None, None, eps)
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=device)   # (an index is cheaper than a device object)
+    rstd = torch.empty_like(mean)
+    lib = _LIB or load_library()
+    st = lib.liec_layer_norm_forward(ref, x.data_ptr(), None if weight is None else weight.data_ptr(),
+                                     None if bias is None else bias.data_ptr(), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), raw)
+    if st != 0:
+        _ln_failed(lib, st)
+    return y, mean, rstd
+
+
 def liec_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None, stream=None):
     """Layer norm of [N, rows, h] (or [rows, h]) activations with per-worker float32 weight and bias
     [N, h] (any stride between workers, e.g. ``params[:, a:a + h]``) or one [h] vector for all.
     Returns (y, mean, rstd); mean and rstd [N, rows] float32 are what the backward pass needs."""
+    device = _device_of("x", x)
+    for name, t in (("weight", weight), ("bias", bias), ("y", y)):
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{name} must be on x's device")
+    return _launch(device, stream, _ln_forward, device, x, weight, bias, eps, y)
+
+
+def _ln_backward(raw, device, dy, x, mean, rstd, weight, dx, dweight, dbias, workspace):
     import torch
-    d = liec_layer_norm_desc()
-    d.x_row_stride, d.x_group_stride = _ln_rows("x", x)
-    d.weight_stride = _ln_vector("weight", weight, x, (torch.float32,))
-    d.bias_stride = _ln_vector("bias", bias, x, (torch.float32,))
-    raw, where = _on(x.device, stream)
-    with where:
-        if y is None:
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        d.y_row_stride, d.y_group_stride = _ln_rows("y", y, x)
-        stats = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device)
-        mean, rstd = stats[0], stats[1]
-        d.groups, d.rows, d.cols = (x.shape[0] if x.dim() == 3 else 1), x.shape[-2], x.shape[-1]
-        d.dtype, d.eps = (BF16 if x.dtype == torch.bfloat16 else F32), eps
-        lib = load_library()
-        st = lib.liec_layer_norm_forward(C.byref(d), x.data_ptr(), None if weight is None else weight.data_ptr(),
-                                         None if bias is None else bias.data_ptr(), y.data_ptr(), mean.data_ptr(),
-                                         rstd.data_ptr(), raw)
+    if dx is None:
+        dx = _empty_like(x)
+    if dweight is None or dbias is None:
+        like = weight if weight is not None else dweight if dweight is not None else dbias
+        given = dweight if dweight is not None else dbias
+        shape = given.shape if given is not None else like.shape if like is not None else x.shape[:-2] + x.shape[-1:]
+        dtype = given.dtype if given is not None else torch.float32
+        dweight = torch.empty(shape, dtype=dtype, device=device) if dweight is None else dweight
+        dbias = torch.empty(shape, dtype=dtype, device=device) if dbias is None else dbias
+    _, ref, need = _ln_desc(_layout(x), _layout(dy), _layout(dx), _layout(weight), None, _layout(dweight), _layout(dbias), 0.0)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    lib = _LIB or load_library()
+    st = lib.liec_layer_norm_backward(ref, dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                      None if weight is None else weight.data_ptr(), dx.data_ptr(), dweight.data_ptr(),
+                                      dbias.data_ptr(), workspace.data_ptr(), workspace.nbytes, raw)
     if st != 0:
-        raise LiecError(st, lib.liec_last_error(None).decode())
-    return y, mean, rstd
+        _ln_failed(lib, st)
+    return dx, dweight, dbias
 
 
 def liec_layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias=None, workspace=None, stream=None):
@@ -277,49 +348,15 @@ def liec_layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, dweight=No
     workers, e.g. ``grads[:, a:a + h]``), or [h] for a vector that all workers share (its gradient is summed over
     the workers too); allocated in float32, shaped like weight, where not given.  Returns (dx, dweight, dbias)."""
     import torch
-    d = liec_layer_norm_desc()
-    d.x_row_stride, d.x_group_stride = _ln_rows("x", x)
-    d.y_row_stride, d.y_group_stride = _ln_rows("dy", dy, x)
-    d.weight_stride = _ln_vector("weight", weight, x, (torch.float32,))
+    device = _device_of("x", x)
+    for name, t in (("dy", dy), ("weight", weight), ("dx", dx), ("dweight", dweight), ("dbias", dbias), ("workspace", workspace)):
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{name} must be on x's device")
+    rows = x.shape[:-1]
     for name, t in (("mean", mean), ("rstd", rstd)):
-        if t.dtype != torch.float32 or t.shape != x.shape[:-1] or not t.is_contiguous() or t.device != x.device:
+        if t.dtype != torch.float32 or t.shape != rows or not t.is_contiguous() or t.get_device() != device:
             raise ValueError(f"{name} must be the contiguous float32 tensor that the forward pass returned")
-    N, rows, h = (x.shape[0] if x.dim() == 3 else 1), x.shape[-2], x.shape[-1]
-    raw, where = _on(x.device, stream)
-    with where:
-        if dx is None:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        d.dx_row_stride, d.dx_group_stride = _ln_rows("dx", dx, x)
-        shape = weight.shape if weight is not None else (dweight if dweight is not None else dbias).shape \
-            if (dweight is not None or dbias is not None) else x.shape[:-2] + (h,)
-        if dweight is None:
-            dweight = torch.empty(shape, dtype=torch.float32 if dbias is None else dbias.dtype, device=x.device)
-        if dbias is None:
-            dbias = torch.empty(shape, dtype=dweight.dtype, device=x.device)
-        if dweight.dtype != dbias.dtype or dweight.dim() != dbias.dim():
-            raise ValueError("dweight and dbias must have the same type and number of axes")
-        d.dweight_stride = _ln_vector("dweight", dweight, x, (torch.float32, torch.bfloat16))
-        d.dbias_stride = _ln_vector("dbias", dbias, x, (torch.float32, torch.bfloat16))
-        d.groups, d.rows, d.cols = N, rows, h
-        if dweight.dim() == 1 and N > 1:   # one vector for all workers: its gradient sums over their rows as well
-            if d.weight_stride != 0:
-                raise ValueError("workers with weights of their own need dweight and dbias [N, h]")
-            if any(t.stride(0) != rows * t.stride(1) for t in (x, dy, dx)):
-                raise ValueError("a gradient shared by the workers needs x, dy and dx whose workers follow one another")
-            d.groups, d.rows = 1, N * rows
-        d.dtype = BF16 if x.dtype == torch.bfloat16 else F32
-        d.grad_dtype = BF16 if dweight.dtype == torch.bfloat16 else F32
-        lib = load_library()
-        need = lib.liec_layer_norm_workspace_bytes(C.byref(d))
-        if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-        st = lib.liec_layer_norm_backward(C.byref(d), dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-                                          None if weight is None else weight.data_ptr(), dx.data_ptr(), dweight.data_ptr(),
-                                          dbias.data_ptr(), workspace.data_ptr() if need else None,
-                                          workspace.numel() * workspace.element_size(), raw)
-    if st != 0:
-        raise LiecError(st, lib.liec_last_error(None).decode())
-    return dx, dweight, dbias
+    return _launch(device, stream, _ln_backward, device, dy, x, mean, rstd, weight, dx, dweight, dbias, workspace)
 
 
 class Context:
@@ -352,6 +389,7 @@ class Context:
         self.grad_dtype = grad_dtype
         self.T = self.cfg.num_segments
         self._sizes = np.diff(self._keep[0]).tolist()
+        self._device = params.get_device()
 
     # -- helpers ---------------------------------------------------------------------------
     def _stream(self, stream=None) -> int:
@@ -445,23 +483,26 @@ class Context:
     def _norms(self, norms):
         t = self._torch
         if norms is None:
-            return t.empty(self.N, dtype=t.float32, device=self.params.device)
+            return t.empty(self.N, dtype=t.float32, device=self._device)
         if not norms.is_cuda or norms.dtype != t.float32 or norms.shape != (self.N,) or not norms.is_contiguous():
             raise ValueError("norms must be a contiguous float32 CUDA tensor [N]")
+        return norms
+
+    def _clip(self, raw, fn, args, max_norm, norms, zero_nonfinite):
+        norms = self._norms(norms)
+        self._check(fn(self._ctx, *args, max_norm, 1 if zero_nonfinite else 0, norms.data_ptr(), raw))
         return norms
 
     def liec_clip_grads(self, grads, max_norm: float, out=None, norms=None, zero_nonfinite: bool = False, stream=None):
         """Scales every worker's gradient row to at most max_norm, into `out` (default: in place).
         Returns the norms before clipping, [N] float32."""
         self._check_grads(grads)
-        out = grads if out is None else out
-        self._check_grads(out)
-        raw, where = _on(self.params.device, stream)
-        with where:
-            norms = self._norms(norms)
-            self._check(self.lib.liec_clip_grads(self._ctx, grads.data_ptr(), out.data_ptr(), max_norm, 1 if zero_nonfinite else 0,
-                                                 norms.data_ptr(), raw))
-        return norms
+        if out is None:
+            out = grads
+        else:
+            self._check_grads(out)
+        return _launch(self._device, stream, self._clip, self.lib.liec_clip_grads, (grads.data_ptr(), out.data_ptr()), max_norm, norms,
+                       zero_nonfinite)
 
     def liec_set_tensors(self, tensors, stream=None):
         """The N*T gradient tensors of liec_gather_grads: N sequences of T contiguous CUDA tensors (None: no
@@ -490,11 +531,7 @@ class Context:
         """Gradient rows from the tensors of liec_set_tensors, every worker's gradient scaled to at most
         max_norm.  Returns the norms before clipping, [N] float32."""
         self._check_grads(out)
-        raw, where = _on(self.params.device, stream)
-        with where:
-            norms = self._norms(norms)
-            self._check(self.lib.liec_gather_grads(self._ctx, out.data_ptr(), max_norm, 1 if zero_nonfinite else 0, norms.data_ptr(), raw))
-        return norms
+        return _launch(self._device, stream, self._clip, self.lib.liec_gather_grads, (out.data_ptr(),), max_norm, norms, zero_nonfinite)
 
     def liec_set_telemetry(self, on: bool):
         self._check(self.lib.liec_set_telemetry(self._ctx, 1 if on else 0))
