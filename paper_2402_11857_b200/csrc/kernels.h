@@ -38,12 +38,19 @@ struct ClipArgs {
     const void *const *table;  // device, [N][T] pointers to the tensors (NULL entry: zeros), or NULL
     void *out;                 // [N][d] of the context's gradient type
     float *norms;              // [N] or NULL
-    double *partials;          // [N][TT] tile sums of squares
-    float *factor;             // [N]
-    int32_t *clear;            // [N] the row is written as zeros
+    // for rows that go through the streaming kernel, one block of CLIP_STREAM_BYTES:
+    double *partials;                    // [N][TT] sums of squares
+    unsigned long long *answer;          // [N] a row's factor
+    unsigned long long *gave_up;         // [1] a wait ran out
+    unsigned long long *sum_ticket, *scale_ticket; // [1] tiles handed out for their sums, for scaling
     float max_norm;
     int32_t src_dtype, in_place, zero_nonfinite;
+    // set by the launcher
+    int32_t norms_only;            // nothing to write
+    int32_t batch;                 // tiles per ticket
 };
+constexpr size_t CLIP_STREAM_BYTES(size_t N, size_t TT) { return 8 * (N * TT + N + 3); }
+cudaError_t configure_clip_kernels();  // opt-in shared memory sizes; call once per device
 cudaError_t launch_clip(const Params &p, const ClipArgs &a, cudaStream_t st, int64_t *launches);
 cudaError_t launch_upload_pointers(const void *const *tensors, const void **table, int64_t count, cudaStream_t st, int64_t *launches);
 

@@ -30,10 +30,12 @@ struct Plan {
     int32_t N = 0, T = 0, TT = 0, KTT = 0;
     int64_t d = 0, W = 0, K = 0, CAP = 0, cap_max = 0, down_CAP = 0;
     std::vector<int64_t> seg_off, word_off, k_off, cap_off, down_cap_off, topk_k;
+    std::vector<int64_t> tile_at;
+    std::vector<int32_t> tile_len;
     std::vector<int32_t> tile_prefix, tile_seg, small_seg, large_seg, ktile_prefix, ktile_seg;
     Region r_seg_off, r_word_off, r_k_off, r_cap_off, r_down_cap_off, r_tile_prefix, r_tile_seg, r_small_seg, r_large_seg, r_status;
     Region r_tel_partials, r_tel_e, r_tel_v, r_tel_g, r_tel_kept, r_ktile_prefix, r_ktile_seg;
-    Region r_tensor_table, r_clip_partials, r_clip_factor, r_clip_clear;
+    Region r_tensor_table, r_clip, r_tile_at, r_tile_len;
     Region r_up_words, r_up_scales, r_up_partials, r_down_words, r_down_scales, r_down_partials, r_vbuf;
     Region r_up_idx, r_up_val, r_down_idx, r_down_val;
     Region r_up_hist, r_down_hist, r_up_hist2, r_down_hist2, r_up_sel, r_down_sel;
@@ -143,8 +145,14 @@ liec_status make_plan(const liec_config *cfg, Plan &pl, std::string *msg) {
     pl.down_CAP = pl.down_cap_off[T];
     pl.TT = (int32_t)tiles;
     pl.tile_seg.resize(pl.TT);
+    pl.tile_at.resize(pl.TT);
+    pl.tile_len.resize(pl.TT);
     for (int t = 0; t < T; ++t) {
-        for (int q = pl.tile_prefix[t]; q < pl.tile_prefix[t + 1]; ++q) pl.tile_seg[q] = t;
+        for (int q = pl.tile_prefix[t]; q < pl.tile_prefix[t + 1]; ++q) {
+            pl.tile_seg[q] = t;
+            pl.tile_at[q] = pl.seg_off[t] + (int64_t)(q - pl.tile_prefix[t]) * TILE;
+            pl.tile_len[q] = (int32_t)std::min<int64_t>(TILE, pl.seg_off[t + 1] - pl.tile_at[q]);
+        }
         (pl.tile_prefix[t + 1] - pl.tile_prefix[t] == 1 ? pl.small_seg : pl.large_seg).push_back(t);
     }
     // the per-problem kernels take the largest segments first (their CTAs run longest)
@@ -160,6 +168,8 @@ liec_status make_plan(const liec_config *cfg, Plan &pl, std::string *msg) {
     pl.r_down_cap_off = c.take(sizeof(int64_t) * (T + 1));
     pl.r_tile_prefix = c.take(sizeof(int32_t) * (T + 1));
     pl.r_tile_seg = c.take(sizeof(int32_t) * pl.TT);
+    pl.r_tile_at = c.take(sizeof(int64_t) * pl.TT);
+    pl.r_tile_len = c.take(sizeof(int32_t) * pl.TT);
     pl.r_small_seg = c.take(sizeof(int32_t) * pl.small_seg.size());
     pl.r_large_seg = c.take(sizeof(int32_t) * pl.large_seg.size());
     pl.r_status = c.take(256);
@@ -172,9 +182,7 @@ liec_status make_plan(const liec_config *cfg, Plan &pl, std::string *msg) {
     pl.r_tel_kept = c.take(sizeof(double) * (size_t)pl.N * pl.KTT);
     const size_t N = pl.N;
     pl.r_tensor_table = c.take(sizeof(void *) * N * T);
-    pl.r_clip_partials = c.take(sizeof(double) * N * pl.TT);
-    pl.r_clip_factor = c.take(sizeof(float) * N);
-    pl.r_clip_clear = c.take(sizeof(int32_t) * N);
+    pl.r_clip = c.take(CLIP_STREAM_BYTES(N, pl.TT));
     if (cfg->uplink == LIEC_COMP_SCALED_SIGN) {
         pl.r_up_words = c.take(sizeof(uint32_t) * N * pl.W);
         pl.r_up_scales = c.take(sizeof(float) * N * T);
@@ -388,6 +396,8 @@ liec_status liec_init(const liec_config *cfg, float *params, float *error, void 
     p.down_CAP = pl.down_CAP;
     p.tile_prefix = at<int32_t>(c, pl.r_tile_prefix);
     p.tile_seg = at<int32_t>(c, pl.r_tile_seg);
+    p.tile_at = at<int64_t>(c, pl.r_tile_at);
+    p.tile_len = at<int32_t>(c, pl.r_tile_len);
     p.small_seg = at<int32_t>(c, pl.r_small_seg);
     p.large_seg = at<int32_t>(c, pl.r_large_seg);
     p.n_small = (int32_t)pl.small_seg.size();
@@ -459,7 +469,7 @@ liec_status liec_init(const liec_config *cfg, float *params, float *error, void 
     const Up ups[] = {
         {&pl.r_seg_off, pl.seg_off.data()}, {&pl.r_word_off, pl.word_off.data()}, {&pl.r_k_off, pl.k_off.data()},
         {&pl.r_cap_off, pl.cap_off.data()}, {&pl.r_down_cap_off, pl.down_cap_off.data()}, {&pl.r_tile_prefix, pl.tile_prefix.data()},
-        {&pl.r_tile_seg, pl.tile_seg.data()}, {&pl.r_small_seg, pl.small_seg.data()}, {&pl.r_large_seg, pl.large_seg.data()},
+        {&pl.r_tile_seg, pl.tile_seg.data()}, {&pl.r_tile_at, pl.tile_at.data()}, {&pl.r_tile_len, pl.tile_len.data()}, {&pl.r_small_seg, pl.small_seg.data()}, {&pl.r_large_seg, pl.large_seg.data()},
         {&pl.r_ktile_prefix, pl.ktile_prefix.data()}, {&pl.r_ktile_seg, pl.ktile_seg.data()},
     };
     for (const Up &u : ups) {
@@ -487,6 +497,7 @@ liec_status liec_init(const liec_config *cfg, float *params, float *error, void 
     }
     cudaError_t e = configure_topk_kernels();
     if (e == cudaSuccess) e = configure_average_kernels();
+    if (e == cudaSuccess) e = configure_clip_kernels();
     if (e == cudaSuccess && ((c->plan.K > 0 && (!c->plan.small_seg.empty() || p.n_big > 0)) || p.down == COMP_SIGN)) {
         int prio_low = 0, prio_high = 0;   // the helper stream carries the longest-running CTAs of a stage: they go first
         e = cudaDeviceGetStreamPriorityRange(&prio_low, &prio_high);
@@ -713,9 +724,11 @@ static liec_status clip(liec_ctx *c, const char *name, ClipArgs a, void *stream)
     if (!a.out || !aligned16(a.out)) { c->err = "the gradient rows must be non-NULL and 16-byte aligned"; return LIEC_ERR_INVALID_ARG; }
     if (!(a.max_norm > 0.0f)) { c->err = "max_norm must be positive (infinity: no clipping)"; return LIEC_ERR_INVALID_ARG; }
     if (reinterpret_cast<uintptr_t>(a.norms) & 3u) { c->err = "norms must be 4-byte aligned"; return LIEC_ERR_INVALID_ARG; }
-    a.partials = at<double>(c, c->plan.r_clip_partials);
-    a.factor = at<float>(c, c->plan.r_clip_factor);
-    a.clear = at<int32_t>(c, c->plan.r_clip_clear);
+    a.partials = at<double>(c, c->plan.r_clip);
+    a.answer = reinterpret_cast<unsigned long long *>(a.partials + (int64_t)c->p.N * c->p.TT);
+    a.gave_up = a.answer + c->p.N;
+    a.sum_ticket = a.gave_up + 1;
+    a.scale_ticket = a.gave_up + 2;
     LIEC_CALL(c, launch_clip(c->p, a, static_cast<cudaStream_t>(stream), &c->launches));
     return LIEC_OK;
 }

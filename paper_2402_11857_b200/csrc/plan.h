@@ -36,6 +36,8 @@ struct Params {
     const int64_t *down_cap_off; // [T+1] the same for the downlink (its long segments get more room: see make_plan)
     const int32_t *tile_prefix;  // [T+1] tiles before segment t
     const int32_t *tile_seg;     // [TT] segment of every tile
+    const int64_t *tile_at;      // [TT] first element of every tile within a row
+    const int32_t *tile_len;     // [TT] its valid elements
     const int32_t *small_seg;    // [n_small] segments of one tile (top-k: selected directly by one CTA)
     const int32_t *large_seg;    // [n_large] segments of several tiles
     int32_t n_small, n_large;
