@@ -16,16 +16,16 @@ __device__ __forceinline__ void store_grad(void *base, int64_t at, int grad_dtyp
 // CTAs over groups shares.  With a.direct a group is one CTA's and the sums are the gradient.
 // With xc = x - m and g = dy r:  dx = g w - mean(g w) - xc r^2 mean(g w xc),  dw += g xc  (nine operations
 // per element instead of the ten of xh and q).
-template <typename T, int PIECE, int NV, int TPR, int SLOTS, int MINB, int R>
+template <typename T, bool WHOLE, int NV, int TPR, int SLOTS, int MINB, int R>
 __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __grid_constant__ LnBackward a) {
-    using S = LnShape<T, PIECE, NV, TPR, SLOTS, MINB, R, 2>;
+    using S = LnShape<T, WHOLE, NV, TPR, SLOTS, MINB, R, 2>;
     constexpr int VEC = S::VEC, P = VEC / 2;
     extern __shared__ __align__(16) char ln_ring[];
     __shared__ __align__(16) float box[2][SLOTS][S::WARPS][2 * R];
     const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const int h = a.cols;
     const float inv_h = 1.0f / (float)h;
-    LnPipe<T, S, PIECE, NV, TPR> px[R], pd[R];
+    LnPipe<T, S, WHOLE, NV, TPR> px[R], pd[R];
 #pragma unroll
     for (int j = 0; j < R; ++j) {
         px[j].place(ln_ring, slot * R + j);
@@ -51,30 +51,34 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
             __syncthreads();
         }
         auto row_of = [&](int turn, int j) { return (turn * SLOTS + slot) * R + j; };
-        auto fetch = [&](int turn, int stage) {
-#pragma unroll
-            for (int j = 0; j < R; ++j)
-                if (row_of(turn, j) < count) {
-                    px[j].fetch(x_next + j * a.x_row, t, h, stage);
-                    pd[j].fetch(dy_next + j * a.dy_row, t, h, stage);
-                }
-            x_next += x_step;
-            dy_next += dy_step;
-        };
-        auto land = [&](int turn, int stage) {
+        auto fetch = [&](int turn, int stage, LnHead (&head)[2 * R]) {
 #pragma unroll
             for (int j = 0; j < R; ++j) {
-                px[j].land(t, row_of(turn, j) < count ? h : 0, stage);
-                pd[j].land(t, row_of(turn, j) < count ? h : 0, stage);
+                head[2 * j].to = head[2 * j + 1].to = 0u;
+                if (row_of(turn, j) < count) {
+                    px[j].fetch(x_next + j * a.x_row, t, h, stage, head[2 * j]);
+                    pd[j].fetch(dy_next + j * a.dy_row, t, h, stage, head[2 * j + 1]);
+                }
             }
+            x_next += x_step;
+            dy_next += dy_step;
+            copy_commit();
+        };
+        auto land = [&](const LnHead (&head)[2 * R]) {
+#pragma unroll
+            for (int j = 0; j < 2 * R; ++j) px[0].land(head[j]);
         };
 #pragma unroll
-        for (int s = 0; s < S::STAGES - 1; ++s) {
-            fetch(s, s);
-            if constexpr (PIECE == 2) land(s, s);
-            else copy_commit();
+        for (int j = 0; j < R; ++j) {
+            px[j].now = (uint32_t)reinterpret_cast<uintptr_t>(x_next + j * a.x_row);
+            pd[j].now = (uint32_t)reinterpret_cast<uintptr_t>(dy_next + j * a.dy_row);
         }
-        if constexpr (PIECE == 2) fetch(S::STAGES - 1, 0);
+        LnHead head[S::STAGES - 1][2 * R];
+#pragma unroll
+        for (int s = 0; s < S::STAGES - 1; ++s) fetch(s, s, head[s]);
+#pragma unroll
+        for (int s = 0; s < S::STAGES - 2; ++s) land(head[s]);
+        LnHead (&last)[2 * R] = head[S::STAGES - 2];   // of the turn fetched last
         float mean_next[R], rstd_next[R];   // of rows that do not exist: zeros, which add nothing
         auto statistics = [&](int turn) {
 #pragma unroll
@@ -97,19 +101,14 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
         for (int i = 0, stage = 0; i < turns; ++i) {
             const int ahead = i + S::STAGES - 1;                               // turn to fetch now
             const int into = stage == 0 ? S::STAGES - 1 : stage - 1;
-            if constexpr (PIECE == 16) {
-                fetch(ahead, into);
-                copy_commit();
+            if constexpr (WHOLE) {
+                fetch(ahead, into, last);
                 copy_wait<S::STAGES - 1>();
-            } else if constexpr (PIECE == 4) {
-                copy_wait<S::STAGES - 2>();
-                slot_sync<TPR>(slot);      // the rows of turn i are complete, and all are done with turn i - 1
-                fetch(ahead, into);
-                copy_commit();
             } else {
-                slot_sync<TPR>(slot);
-                land(ahead, into);
-                fetch(ahead + 1, 0);
+                copy_wait<S::STAGES - 2>();
+                land(last);
+                slot_sync<TPR>(slot);      // the rows of turn i are complete, and all are done with turn i - 1
+                fetch(ahead, into, last);
             }
             float rstd[R], along[R], level[R];
             F2 minus[R];
@@ -128,8 +127,8 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
 #pragma unroll
                     for (int v = 0; v < NV; ++v) {
                         F2 dy[P];
-                        LnChunk<T>::read(px[j].chunk(v, t, stage), xc[j][v]);
-                        LnChunk<T>::read(pd[j].chunk(v, t, stage), dy);
+                        px[j].read(v, t, stage, xc[j][v]);
+                        pd[j].read(v, t, stage, dy);
 #pragma unroll
                         for (int k = 0; k < P; ++k) {
                             xc[j][v][k] = add(xc[j][v][k], minus[j]);
@@ -148,6 +147,7 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
             if (a.dx) {
                 slot_sums<TPR, S::WARPS, R>(along, level, t, slot, box[flip]);
                 flip ^= 1;
+                if constexpr (!WHOLE && S::WARPS == 1) __syncwarp();   // all have read the rows, whose place the results take
 #pragma unroll
                 for (int j = 0; j < R; ++j) {
                     const F2 tilt = f2(-(along[j] * inv_h * rstd[j]) * rstd[j]), shift = f2(-level[j] * inv_h);
@@ -158,26 +158,28 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
                             const int c = (v * TPR + t) * VEC;
 #pragma unroll
                             for (int k = 0; k < P; ++k) q[j][v][k] = fma(xc[j][v][k], tilt, add(q[j][v][k], shift));
-                            if constexpr (PIECE == 16) {
-                                if (c < h) LnChunk<T>::write(dxj + c, q[j][v]);
-                            } else {
-                                if (c + VEC > h) ln_keep<P>(q[j][v], h - c);   // the ring stays zero beyond the row
-                                LnChunk<T>::write(px[j].chunk(v, t, stage), q[j][v]);
-                            }
+                            if (c < h) LnChunk<T>::write(WHOLE ? reinterpret_cast<char *>(dxj + c) : px[j].result(v, t, stage), q[j][v]);
                         }
                     }
                 }
-                if constexpr (PIECE < 16) {
+                if constexpr (!WHOLE) {
                     slot_sync<TPR>(slot);
 #pragma unroll
                     for (int j = 0; j < R; ++j)
-                        ln_store_row<T, S, PIECE, TPR>(dx + j * a.dx_row, px[j].ring + stage * S::STAGE_BYTES, t, row_of(i, j) < count ? h : 0);
+                        if (row_of(i, j) < count) ln_store_row<T, NV, TPR>(dx + j * a.dx_row, px[j].ring + stage * S::STAGE_BYTES, t, h);
                 }
                 dx += dx_step;
             }
+            if constexpr (!WHOLE) {
+#pragma unroll
+                for (int j = 0; j < R; ++j) {
+                    px[j].now += (uint32_t)x_step * (uint32_t)sizeof(T);
+                    pd[j].now += (uint32_t)dy_step * (uint32_t)sizeof(T);
+                }
+            }
             stage = stage + 1 == S::STAGES ? 0 : stage + 1;
         }
-        if constexpr (PIECE != 2) copy_wait<0>();
+        copy_wait<0>();
         __syncthreads();   // the ring is free: for the sums of the slots and for the next group
         if (!a.dweight && !a.dbias) continue;
         // the slots' sums meet: lanes of one warp by shuffles, then halves of the CTA through shared memory
@@ -319,7 +321,7 @@ size_t layer_norm_workspace(int groups, int64_t rows, int cols) {
     return sizeof(float) * 2 * (size_t)std::max<int64_t>(pieces, groups) * (size_t)cols;
 }
 
-template <typename T, int PIECE>
+template <typename T, bool WHOLE>
 struct LnBackwardLaunch {
     LnBackward a;
     cudaStream_t st;
@@ -327,10 +329,10 @@ struct LnBackwardLaunch {
     cudaError_t operator()() {
         constexpr int NV = E / LnChunk<T>::VEC;
         constexpr int R = LN_BACKWARD_TURN;
-        using S = LnShape<T, PIECE, NV, TPR, SLOTS, MINB, R, 2>;
+        using S = LnShape<T, WHOLE, NV, TPR, SLOTS, MINB, R, 2>;
         static_assert(S::THREADS <= 32 || S::RING_BYTES >= S::THREADS * S::E * 4, "half the CTA's column sums meet in the ring");
         static std::atomic<uint64_t> allowed{0};
-        auto kernel = ln_backward_kernel<T, PIECE, NV, TPR, SLOTS, MINB, R>;
+        auto kernel = ln_backward_kernel<T, WHOLE, NV, TPR, SLOTS, MINB, R>;
         const cudaError_t e = ln_allow_smem(kernel, S::RING_BYTES, allowed);
         if (e != cudaSuccess) return e;
         kernel<<<(unsigned)a.share.ctas, S::THREADS, S::RING_BYTES, st>>>(a);
@@ -341,17 +343,15 @@ struct LnBackwardLaunch {
 static cudaError_t backward_rows(LnBackward &a, int dtype, cudaStream_t st) {
     if (a.cols > LN_REGISTER_COLS) return launch_layer_norm_backward_wide(a, dtype, st);
     const int esz = dtype == 0 ? 4 : 2;
-    int piece = std::min(ln_piece(a.x, a.x_row, a.x_group, a.rows, a.groups, a.cols, esz),
-                         ln_piece(a.dy, a.dy_row, a.dy_group, a.rows, a.groups, a.cols, esz));
-    if (a.dx) piece = std::min(piece, ln_piece(a.dx, a.dx_row, a.dx_group, a.rows, a.groups, a.cols, esz));
+    const bool whole = ln_whole(a.x, a.x_row, a.x_group, a.rows, a.groups, a.cols, esz) &&
+                       ln_whole(a.dy, a.dy_row, a.dy_group, a.rows, a.groups, a.cols, esz) &&
+                       (!a.dx || ln_whole(a.dx, a.dx_row, a.dx_group, a.rows, a.groups, a.cols, esz));
     const LnPlan p = ln_backward_shape(a.cols, LnPlanner{a.groups, a.rows});
     a.share = p.share;
     a.direct = p.direct;
     if (dtype == 0)
-        return piece == 16 ? ln_backward_shape(a.cols, LnBackwardLaunch<float, 16>{a, st}) : ln_backward_shape(a.cols, LnBackwardLaunch<float, 4>{a, st});
-    if (piece == 16) return ln_backward_shape(a.cols, LnBackwardLaunch<__nv_bfloat16, 16>{a, st});
-    if (piece == 4) return ln_backward_shape(a.cols, LnBackwardLaunch<__nv_bfloat16, 4>{a, st});
-    return ln_backward_shape(a.cols, LnBackwardLaunch<__nv_bfloat16, 2>{a, st});
+        return whole ? ln_backward_shape(a.cols, LnBackwardLaunch<float, true>{a, st}) : ln_backward_shape(a.cols, LnBackwardLaunch<float, false>{a, st});
+    return whole ? ln_backward_shape(a.cols, LnBackwardLaunch<__nv_bfloat16, true>{a, st}) : ln_backward_shape(a.cols, LnBackwardLaunch<__nv_bfloat16, false>{a, st});
 }
 
 cudaError_t launch_layer_norm_backward(LnBackward a, int dtype, cudaStream_t st) {

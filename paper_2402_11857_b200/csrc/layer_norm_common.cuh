@@ -4,16 +4,17 @@
 // TPR threads share a row (a "slot" of a CTA).  A chunk is 16 bytes of elements (VEC = 4 of binary32, 8 of
 // bfloat16); thread t of the slot owns the chunks v TPR + t, v < NV, of its row, whatever the row's
 // alignment, so that the order of every sum, hence every bit of the result, depends on h alone.  Rows
-// pass through a ring in shared memory, STAGES rows deep per slot, where they lie in column order from a
-// 16-byte boundary; what lies beyond column h in the ring is zero.  The bytes in flight so cost no
-// registers, which the backward pass needs for its column sums.  PIECE says how a row is fetched:
-//   16  every row starts on 16 bytes and h is a multiple of VEC: a thread fetches its own chunks with
-//       cp.async and is the only one to read them, so no barrier guards the ring
-//    4  rows start on 4 bytes: 4-byte cp.async, neighbouring threads fetch neighbouring words; a barrier
-//       of the slot per row
-//    2  bfloat16 rows of odd width or at odd places: 2-byte loads through registers
-// Results of the PIECE < 16 forms go back through the ring as well, so that neighbouring threads store
-// neighbouring words.
+// pass through a ring in shared memory, STAGES rows deep per slot; what lies beyond column h there is
+// zero.  The bytes in flight so cost no registers, which the backward pass needs for its column sums.
+// WHOLE says how a row is fetched:
+//   true   every row starts on 16 bytes and h is a multiple of VEC: a thread fetches its own chunks with
+//          16-byte cp.async and is the only one to read them, so no barrier guards the ring
+//   false  rows of any width and place: the ring holds the 16-byte granules of memory that the row touches, as
+//          they lie (cp.async of whole granules, of a part at the end; the elements of a first granule that the
+//          row does not fill one by one), and a thread cuts its chunk out of two of them; results go back through
+//          the ring and leave as granules too.  A barrier of the slot per row.  (32 x 4095 rows of 767 bfloat16:
+//          forward 110 us, backward 192 us; 114 and 846 us with 2-byte loads through registers.  768 columns,
+//          which the first form takes: 69 and 104 us.)
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -54,13 +55,18 @@ __device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
 template <typename T> struct LnChunk;
 template <> struct LnChunk<float> {
     static constexpr int VEC = 4;
-    static __device__ __forceinline__ void read(const void *p, F2 (&out)[2]) {
-        const float4 q = *reinterpret_cast<const float4 *>(p);
-        out[0] = f2(q.x, q.y);
-        out[1] = f2(q.z, q.w);
+    static __device__ __forceinline__ void read(uint4 q, F2 (&out)[2]) {
+        out[0] = f2(__uint_as_float(q.x), __uint_as_float(q.y));
+        out[1] = f2(__uint_as_float(q.z), __uint_as_float(q.w));
     }
     static __device__ __forceinline__ void write(void *p, const F2 (&in)[2]) {
         *reinterpret_cast<float4 *>(p) = make_float4(lo(in[0]), hi(in[0]), lo(in[1]), hi(in[1]));
+    }
+    // 16 bytes from byte `shift` (a multiple of the element's size, below 16) of 32
+    static __device__ __forceinline__ uint4 cut(uint4 a, uint4 b, uint32_t shift) {
+        const bool two = (shift & 8u) != 0, one = (shift & 4u) != 0;
+        const uint32_t w0 = two ? a.z : a.x, w1 = two ? a.w : a.y, w2 = two ? b.x : a.z, w3 = two ? b.y : a.w, w4 = two ? b.z : b.x;
+        return make_uint4(one ? w1 : w0, one ? w2 : w1, one ? w3 : w2, one ? w4 : w3);
     }
 };
 template <> struct LnChunk<__nv_bfloat16> {
@@ -71,19 +77,27 @@ template <> struct LnChunk<__nv_bfloat16> {
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi(a)), "f"(lo(a)));
         return w;
     }
-    static __device__ __forceinline__ void read(const void *p, F2 (&out)[4]) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(p);
+    static __device__ __forceinline__ void read(uint4 q, F2 (&out)[4]) {
         out[0] = pair(q.x); out[1] = pair(q.y); out[2] = pair(q.z); out[3] = pair(q.w);
     }
     static __device__ __forceinline__ void write(void *p, const F2 (&in)[4]) {
         *reinterpret_cast<uint4 *>(p) = make_uint4(word(in[0]), word(in[1]), word(in[2]), word(in[3]));
     }
+    static __device__ __forceinline__ uint4 cut(uint4 a, uint4 b, uint32_t shift) {
+        const bool two = (shift & 8u) != 0, one = (shift & 4u) != 0;
+        const uint32_t half = (shift & 2u) * 8u;
+        const uint32_t v0 = two ? a.z : a.x, v1 = two ? a.w : a.y, v2 = two ? b.x : a.z, v3 = two ? b.y : a.w, v4 = two ? b.z : b.x, v5 = two ? b.w : b.y;
+        const uint32_t w0 = one ? v1 : v0, w1 = one ? v2 : v1, w2 = one ? v3 : v2, w3 = one ? v4 : v3, w4 = one ? v5 : v4;
+        return make_uint4(__funnelshift_r(w0, w1, half), __funnelshift_r(w1, w2, half), __funnelshift_r(w2, w3, half), __funnelshift_r(w3, w4, half));
+    }
 };
 
-template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void *src) {
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// the first `bytes` (0 to 16) of 16, zeros behind them; nothing beyond them is read
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING>
@@ -147,71 +161,110 @@ __device__ __forceinline__ void slot_sums(float (&a)[R], float (&b)[R], int t, i
     }
 }
 
-template <typename T, int PIECE, int NV, int TPR, int SLOTS, int MINB, int R, int ARRAYS>
+template <typename T, bool WHOLE, int NV, int TPR, int SLOTS, int MINB, int R, int ARRAYS>
 struct LnShape {
     static constexpr int VEC = LnChunk<T>::VEC, E = VEC * NV, THREADS = TPR * SLOTS, COLS = TPR * E;
-    static constexpr int ROW_BYTES = COLS * (int)sizeof(T);
+    // (a row that starts inside a granule touches one more; a result lies 16 bytes into its place, see ln_store_row)
+    static constexpr int ROW_BYTES = COLS * (int)sizeof(T) + (WHOLE ? 0 : 32);
     static constexpr int STAGE_BYTES = ARRAYS * SLOTS * R * ROW_BYTES;   // a stage holds the R rows of a turn, for every slot
     // About 40 KB per SM have to be in flight to cover HBM's latency at its bandwidth: 2 to 6 stages
     // give that for every shape within the 200 KB that the MINB CTAs of an SM share.
     static constexpr int FIT = 200 * 1024 / MINB / STAGE_BYTES;
-    static constexpr int STAGES = PIECE == 2 ? 2 : FIT < 2 ? 2 : FIT > 6 ? 6 : FIT;
+    static constexpr int STAGES = FIT < 2 ? 2 : FIT > 6 ? 6 : FIT;
     static constexpr int RING_BYTES = STAGES * STAGE_BYTES;
     static constexpr int WARPS = TPR < 32 ? 1 : TPR / 32;      // warps per slot
-    static constexpr int PIECES = PIECE == 16 ? NV : E * (int)sizeof(T) / PIECE;   // fetches per thread and row
 };
 
+// An element of a row's first granule on its way to the ring (to = 0: none).
+struct LnHead { uint32_t to, value; };
+
 // The rows of one array on their way to one place in the stages.
-template <typename T, typename S, int PIECE, int NV, int TPR>
+template <typename T, typename S, bool WHOLE, int NV, int TPR>
 struct LnPipe {
-    char *ring;                                            // this slot's row of stage 0
+    char *ring;             // this slot's row of stage 0
     uint32_t ring_u32;
-    unsigned short ahead[PIECE == 2 ? S::PIECES : 1];      // PIECE 2: the row after the next, in registers
+    uint32_t now;           // !WHOLE: low bits of the address of this turn's row
     __device__ __forceinline__ void place(char *smem, int row_of_stage) {
         ring = smem + row_of_stage * S::ROW_BYTES;
         ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
     }
-    // start fetching a row into a stage
-    __device__ __forceinline__ void fetch(const T *row, int t, int cols, int stage) {
+    // start fetching a row into a stage; head: what land() still has to put there
+    __device__ __forceinline__ void fetch(const T *row, int t, int cols, int stage, LnHead &head) {
         const uint32_t to = ring_u32 + stage * S::STAGE_BYTES;
-        const char *from = reinterpret_cast<const char *>(row);
         const int bytes = cols * (int)sizeof(T);
-        if constexpr (PIECE >= 4) {
+        if constexpr (WHOLE) {
 #pragma unroll
-            for (int j = 0; j < S::PIECES; ++j) {
-                const int at = (j * TPR + t) * PIECE;
-                if (at < bytes) copy_async<PIECE>(to + at, from + at);
+            for (int v = 0; v < NV; ++v) {
+                const int at = (v * TPR + t) * 16;
+                if (at < bytes) copy_async(to + at, reinterpret_cast<const char *>(row) + at);
             }
         } else {
+            const int shift = (int)(reinterpret_cast<uintptr_t>(row) & 15u), end = shift + bytes;
+            const char *from = reinterpret_cast<const char *>(row) - shift;
+            if (shift == 0 || t > 0) {
+                if (t * 16 + 16 <= end) copy_async(to + t * 16, from + t * 16);
+            }
 #pragma unroll
-            for (int j = 0; j < S::PIECES; ++j) {
-                const int at = (j * TPR + t) * PIECE;
-                if (at < bytes) ahead[j] = __ldg(reinterpret_cast<const unsigned short *>(from + at));
+            for (int v = 1; v <= NV; ++v) {
+                const int at = (v * TPR + t) * 16;
+                if (at + 16 <= end) copy_async(to + at, from + at);
+            }
+            // the granules up to (bytes + 14) / 16 are all that some row of this width touches: with zeros there,
+            // nothing of the row that lay here before is left beyond column h
+            const int tail = (end & ~15) + t * 16;
+            if (t < 2 && tail <= bytes + 14) {
+                if (tail > 0 || shift == 0) copy_async(to + tail, tail < end ? from + tail : from, max(end - tail, 0) & 15);
+            }
+            const int at = t * (int)sizeof(T);
+            head.to = 0u;
+            if (shift != 0 && at >= shift && at < 16) {   // (zeros behind a row that ends in its first granule)
+                head.to = to + at;
+                head.value = 0u;
+                if (at < end) {
+                    if constexpr (sizeof(T) == 4) head.value = __ldg(reinterpret_cast<const unsigned *>(from + at));
+                    else head.value = __ldg(reinterpret_cast<const unsigned short *>(from + at));
+                }
             }
         }
     }
-    // PIECE 2: what fetch brought into the registers goes to a stage
-    __device__ __forceinline__ void land(int t, int cols, int stage) {
-#pragma unroll
-        for (int j = 0; j < S::PIECES; ++j) {
-            const int at = (j * TPR + t) * PIECE;
-            if (at < cols * (int)sizeof(T)) *reinterpret_cast<unsigned short *>(ring + stage * S::STAGE_BYTES + at) = ahead[j];
+    static __device__ __forceinline__ void land(const LnHead &head) {
+        if constexpr (!WHOLE) {
+            if (head.to != 0u) {
+                if constexpr (sizeof(T) == 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(head.to), "r"(head.value) : "memory");
+                else asm volatile("st.shared.b16 [%0], %1;" ::"r"(head.to), "h"((unsigned short)head.value) : "memory");
+            }
         }
     }
-    __device__ __forceinline__ char *chunk(int v, int t, int stage) const { return ring + stage * S::STAGE_BYTES + (v * TPR + t) * 16; }
+    __device__ __forceinline__ void read(int v, int t, int stage, F2 (&out)[S::VEC / 2]) const {
+        const uint4 *g = reinterpret_cast<const uint4 *>(ring + stage * S::STAGE_BYTES + (v * TPR + t) * 16);
+        if constexpr (WHOLE) LnChunk<T>::read(g[0], out);
+        else LnChunk<T>::read(LnChunk<T>::cut(g[0], g[1], now & 15u), out);
+    }
+    // where a result's chunk waits for ln_store_row
+    __device__ __forceinline__ char *result(int v, int t, int stage) const { return ring + stage * S::STAGE_BYTES + 16 + (v * TPR + t) * 16; }
 };
 
-// A finished row leaves the ring's stage in pieces that neighbouring threads store side by side.
-template <typename T, typename S, int PIECE, int TPR>
+// A finished row leaves the ring's stage, where its first element lies at byte 16, in granules of memory; the
+// elements of a first and a last granule that it does not fill go one by one.
+template <typename T, int NV, int TPR>
 __device__ __forceinline__ void ln_store_row(T *row, const char *stage, int t, int cols) {
-    char *to = reinterpret_cast<char *>(row);
+    const int shift = (int)(reinterpret_cast<uintptr_t>(row) & 15u), end = shift + cols * (int)sizeof(T);
+    char *to = reinterpret_cast<char *>(row) - shift;
+    const char *from = stage + 16 - shift;
+    const char *g = stage + (shift == 0 ? 16 : 0);
+    const uint32_t turn = (uint32_t)(16 - shift) & 15u;
 #pragma unroll
-    for (int j = 0; j < S::PIECES; ++j) {
-        const int at = (j * TPR + t) * PIECE;
-        if (at < cols * (int)sizeof(T)) {
-            if constexpr (PIECE == 4) *reinterpret_cast<uint32_t *>(to + at) = *reinterpret_cast<const uint32_t *>(stage + at);
-            else *reinterpret_cast<unsigned short *>(to + at) = *reinterpret_cast<const unsigned short *>(stage + at);
+    for (int v = 0; v <= NV; ++v) {
+        const int at = (v * TPR + t) * 16;
+        if (at + 16 <= end && (v > 0 || at >= shift)) {
+            const uint4 *q = reinterpret_cast<const uint4 *>(g + at);
+            *reinterpret_cast<uint4 *>(to + at) = LnChunk<T>::cut(q[0], q[1], turn);
         }
+    }
+    if (t < LnChunk<T>::VEC) {
+        const int first = t * (int)sizeof(T), last = (end & ~15) + first;
+        if (shift != 0 && first >= shift && first < end) *reinterpret_cast<T *>(to + first) = *reinterpret_cast<const T *>(from + first);
+        if ((last >= 16 || shift == 0) && last < end) *reinterpret_cast<T *>(to + last) = *reinterpret_cast<const T *>(from + last);
     }
 }
 
@@ -268,9 +321,9 @@ inline LnShare ln_share(int64_t total, int turn_rows, int resident, int64_t max_
 // f.template operator()<TPR, E, SLOTS, MINB>().
 template <typename F>
 auto ln_forward_shape(int h, F &&f) {
-    if (h <= 64) return f.template operator()<8, 8, 32, 4>();
-    if (h <= 128) return f.template operator()<16, 8, 16, 4>();
-    if (h <= 256) return f.template operator()<32, 8, 8, 4>();
+    if (h <= 64) return f.template operator()<8, 8, 32, 3>();
+    if (h <= 128) return f.template operator()<16, 8, 16, 3>();
+    if (h <= 256) return f.template operator()<32, 8, 8, 3>();
     if (h <= 512) return f.template operator()<32, 16, 8, 2>();
     if (h <= 768) return f.template operator()<32, 24, 4, 4>();
     if (h <= 1024) return f.template operator()<32, 32, 4, 3>();
@@ -307,12 +360,12 @@ cudaError_t ln_allow_smem(K kernel, int bytes, std::atomic<uint64_t> &done) {
     return e;
 }
 
-// The largest piece (16, 4 or 2 bytes) at which all rows of an array start and end.
-inline int ln_piece(const void *p, int64_t row, int64_t group, int64_t rows, int groups, int cols, int esz) {
+// All rows of an array start and end on 16 bytes.
+inline bool ln_whole(const void *p, int64_t row, int64_t group, int64_t rows, int groups, int cols, int esz) {
     uint64_t bits = reinterpret_cast<uintptr_t>(p) | (uint64_t)cols * esz;
     if (rows > 1) bits |= (uint64_t)row * esz;
     if (groups > 1) bits |= (uint64_t)group * esz;
-    return (bits & 15u) == 0 ? 16 : (bits & 3u) == 0 ? 4 : 2;
+    return (bits & 15u) == 0;
 }
 
 // generic kernels for rows beyond LN_REGISTER_COLS

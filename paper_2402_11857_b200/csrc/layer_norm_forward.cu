@@ -6,16 +6,16 @@ namespace liec {
 
 // A CTA takes its share of all groups * rows rows, group after group; every thread of the CTA makes the
 // same number of turns, a turn being R consecutive rows for every slot.
-template <typename T, int PIECE, int NV, int TPR, int SLOTS, int MINB, int R>
+template <typename T, bool WHOLE, int NV, int TPR, int SLOTS, int MINB, int R>
 __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __grid_constant__ LnForward a) {
-    using S = LnShape<T, PIECE, NV, TPR, SLOTS, MINB, R, 1>;
+    using S = LnShape<T, WHOLE, NV, TPR, SLOTS, MINB, R, 1>;
     constexpr int VEC = S::VEC, P = VEC / 2;
     extern __shared__ __align__(16) char ln_ring[];
     __shared__ __align__(16) float box[2][SLOTS][S::WARPS][2 * R];
     const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const int h = a.cols;
     const float inv_h = 1.0f / (float)h;
-    LnPipe<T, S, PIECE, NV, TPR> px[R];
+    LnPipe<T, S, WHOLE, NV, TPR> px[R];
 #pragma unroll
     for (int j = 0; j < R; ++j) px[j].place(ln_ring, slot * R + j);
     if (h != S::COLS)   // zeros beyond column h
@@ -35,23 +35,27 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __g
         int64_t at = (int64_t)group * a.rows + r0 + slot * R;
         const int64_t x_step = (int64_t)SLOTS * R * a.x_row, y_step = (int64_t)SLOTS * R * a.y_row;
         auto row_of = [&](int turn, int j) { return (turn * SLOTS + slot) * R + j; };
-        auto fetch = [&](int turn, int stage) {
+        auto fetch = [&](int turn, int stage, LnHead (&head)[R]) {
 #pragma unroll
-            for (int j = 0; j < R; ++j)
-                if (row_of(turn, j) < count) px[j].fetch(x_next + j * a.x_row, t, h, stage);
+            for (int j = 0; j < R; ++j) {
+                head[j].to = 0u;
+                if (row_of(turn, j) < count) px[j].fetch(x_next + j * a.x_row, t, h, stage, head[j]);
+            }
             x_next += x_step;
+            copy_commit();
         };
-        auto land = [&](int turn, int stage) {
+        auto land = [&](const LnHead (&head)[R]) {
 #pragma unroll
-            for (int j = 0; j < R; ++j) px[j].land(t, row_of(turn, j) < count ? h : 0, stage);
+            for (int j = 0; j < R; ++j) px[j].land(head[j]);
         };
 #pragma unroll
-        for (int s = 0; s < S::STAGES - 1; ++s) {
-            fetch(s, s);
-            if constexpr (PIECE == 2) land(s, s);
-            else copy_commit();
-        }
-        if constexpr (PIECE == 2) fetch(S::STAGES - 1, 0);
+        for (int j = 0; j < R; ++j) px[j].now = (uint32_t)reinterpret_cast<uintptr_t>(x_next + j * a.x_row);
+        LnHead head[S::STAGES - 1][R];
+#pragma unroll
+        for (int s = 0; s < S::STAGES - 1; ++s) fetch(s, s, head[s]);
+#pragma unroll
+        for (int s = 0; s < S::STAGES - 2; ++s) land(head[s]);
+        LnHead (&last)[R] = head[S::STAGES - 2];   // of the turn fetched last
         F2 w[NV][P], b[NV][P];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -61,19 +65,14 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __g
         for (int i = 0, stage = 0; i < turns; ++i) {
             const int ahead = i + S::STAGES - 1;                               // turn to fetch now
             const int into = stage == 0 ? S::STAGES - 1 : stage - 1;
-            if constexpr (PIECE == 16) {
-                fetch(ahead, into);
-                copy_commit();
+            if constexpr (WHOLE) {
+                fetch(ahead, into, last);
                 copy_wait<S::STAGES - 1>();
-            } else if constexpr (PIECE == 4) {
-                copy_wait<S::STAGES - 2>();
-                slot_sync<TPR>(slot);      // the rows of turn i are complete, and all are done with turn i - 1
-                fetch(ahead, into);
-                copy_commit();
             } else {
-                slot_sync<TPR>(slot);
-                land(ahead, into);
-                fetch(ahead + 1, 0);
+                copy_wait<S::STAGES - 2>();
+                land(last);
+                slot_sync<TPR>(slot);      // the rows of turn i are complete, and all are done with turn i - 1
+                fetch(ahead, into, last);
             }
             F2 x[R][NV][P];
             float mean[R], var[R];
@@ -82,7 +81,7 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __g
                 F2 s2 = f2(0.0f), q2 = f2(0.0f);
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
-                    LnChunk<T>::read(px[j].chunk(v, t, stage), x[j][v]);   // (zeros beyond column h)
+                    px[j].read(v, t, stage, x[j][v]);   // (zeros beyond column h)
 #pragma unroll
                     for (int k = 0; k < P; ++k) {
                         s2 = add(s2, x[j][v][k]);
@@ -94,6 +93,7 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __g
             }
             slot_sums<TPR, S::WARPS, R>(mean, var, t, slot, box[flip]);
             flip ^= 1;
+            if constexpr (!WHOLE && S::WARPS == 1) __syncwarp();   // all have read the rows, whose place the results take
             // var = mean(x^2) - mean^2 keeps its digits while mean^2 is at most a quarter of it (the difference
             // then carries at most 1.25 times the relative error of the sums) and nothing overflowed; other
             // rows sum the squares around their mean
@@ -145,34 +145,31 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __g
                     const int c = (v * TPR + t) * VEC;
 #pragma unroll
                     for (int k = 0; k < P; ++k) x[j][v][k] = fma(mul(x[j][v][k], scale), w[v][k], b[v][k]);
-                    if constexpr (PIECE == 16) {
-                        if (live && c < h) LnChunk<T>::write(yj + c, x[j][v]);
-                    } else {
-                        if (c + VEC > h) ln_keep<P>(x[j][v], h - c);   // the ring stays zero beyond the row
-                        LnChunk<T>::write(px[j].chunk(v, t, stage), x[j][v]);
-                    }
+                    if (live && c < h) LnChunk<T>::write(WHOLE ? reinterpret_cast<char *>(yj + c) : px[j].result(v, t, stage), x[j][v]);
                 }
                 if (live && t == 0) {
                     if (a.mean) a.mean[at + j] = mean[j];
                     if (a.rstd) a.rstd[at + j] = rstd;
                 }
             }
-            if constexpr (PIECE < 16) {
+            if constexpr (!WHOLE) {
                 slot_sync<TPR>(slot);
 #pragma unroll
-                for (int j = 0; j < R; ++j)
-                    ln_store_row<T, S, PIECE, TPR>(y + j * a.y_row, px[j].ring + stage * S::STAGE_BYTES, t, row_of(i, j) < count ? h : 0);
+                for (int j = 0; j < R; ++j) {
+                    if (row_of(i, j) < count) ln_store_row<T, NV, TPR>(y + j * a.y_row, px[j].ring + stage * S::STAGE_BYTES, t, h);
+                    px[j].now += (uint32_t)x_step * (uint32_t)sizeof(T);
+                }
             }
             y += y_step;
             at += SLOTS * R;
             stage = stage + 1 == S::STAGES ? 0 : stage + 1;
         }
-        if constexpr (PIECE != 2) copy_wait<0>();
-        if constexpr (PIECE != 16) __syncthreads();   // the next group's rows go into the same ring
+        copy_wait<0>();
+        if constexpr (!WHOLE) __syncthreads();   // the next group's rows go into the same ring
     }
 }
 
-template <typename T, int PIECE>
+template <typename T, bool WHOLE>
 struct LnForwardLaunch {
     LnForward a;
     cudaStream_t st;
@@ -180,9 +177,9 @@ struct LnForwardLaunch {
     cudaError_t operator()() {
         constexpr int NV = E / LnChunk<T>::VEC;
         constexpr int R = E <= 16 ? 2 : 1;   // rows per turn: two where the registers hold them
-        using S = LnShape<T, PIECE, NV, TPR, SLOTS, MINB, R, 1>;
+        using S = LnShape<T, WHOLE, NV, TPR, SLOTS, MINB, R, 1>;
         static std::atomic<uint64_t> allowed{0};
-        auto kernel = ln_forward_kernel<T, PIECE, NV, TPR, SLOTS, MINB, R>;
+        auto kernel = ln_forward_kernel<T, WHOLE, NV, TPR, SLOTS, MINB, R>;
         const cudaError_t e = ln_allow_smem(kernel, S::RING_BYTES, allowed);
         if (e != cudaSuccess) return e;
         // (one CTA per SM: a small share would leave its SM idle while it starts)
@@ -196,13 +193,11 @@ cudaError_t launch_layer_norm_forward(const LnForward &a, int dtype, cudaStream_
     if (a.rows == 0) return cudaSuccess;
     if (a.cols > LN_REGISTER_COLS) return launch_layer_norm_forward_wide(a, dtype, st);
     const int esz = dtype == 0 ? 4 : 2;
-    const int piece = std::min(ln_piece(a.x, a.x_row, a.x_group, a.rows, a.groups, a.cols, esz),
-                               ln_piece(a.y, a.y_row, a.y_group, a.rows, a.groups, a.cols, esz));
+    const bool whole = ln_whole(a.x, a.x_row, a.x_group, a.rows, a.groups, a.cols, esz) &&
+                       ln_whole(a.y, a.y_row, a.y_group, a.rows, a.groups, a.cols, esz);
     if (dtype == 0)
-        return piece == 16 ? ln_forward_shape(a.cols, LnForwardLaunch<float, 16>{a, st}) : ln_forward_shape(a.cols, LnForwardLaunch<float, 4>{a, st});
-    if (piece == 16) return ln_forward_shape(a.cols, LnForwardLaunch<__nv_bfloat16, 16>{a, st});
-    if (piece == 4) return ln_forward_shape(a.cols, LnForwardLaunch<__nv_bfloat16, 4>{a, st});
-    return ln_forward_shape(a.cols, LnForwardLaunch<__nv_bfloat16, 2>{a, st});
+        return whole ? ln_forward_shape(a.cols, LnForwardLaunch<float, true>{a, st}) : ln_forward_shape(a.cols, LnForwardLaunch<float, false>{a, st});
+    return whole ? ln_forward_shape(a.cols, LnForwardLaunch<__nv_bfloat16, true>{a, st}) : ln_forward_shape(a.cols, LnForwardLaunch<__nv_bfloat16, false>{a, st});
 }
 
 }  // namespace liec

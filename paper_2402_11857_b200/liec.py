@@ -289,6 +289,20 @@ def _ln_failed(lib, st):
     raise LiecError(st, lib.liec_last_error(None).decode())
 
 
+@functools.lru_cache(maxsize=1024)
+def _contiguous(shape):
+    strides = [1]
+    for n in reversed(shape[1:]):
+        strides.append(strides[-1] * max(n, 1))
+    return tuple(shape), tuple(reversed(strides))
+
+
+def _empty(shape, dtype, device: int):
+    """A contiguous tensor.  (torch.empty costs twice as much as empty_strided with plain tuples and a device's index.)"""
+    import torch
+    return torch.empty_strided(*_contiguous(shape), dtype=dtype, device=device)
+
+
 def _empty_like(x):
     import torch
     return torch.empty_like(x, memory_format=torch.contiguous_format)
@@ -299,7 +313,7 @@ def _ln_forward(raw, device, x, weight, bias, eps, y):
     if y is None:
         y = _empty_like(x)
     _, ref, _ = _ln_desc(_layout(x), _layout(y), None, _layout(weight), _layout(bias), None, None, eps)
-    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=device)   # (an index is cheaper than a device object)
+    mean = _empty(x.shape[:-1], torch.float32, device)
     rstd = torch.empty_like(mean)
     lib = _LIB or load_library()
     st = lib.liec_layer_norm_forward(ref, x.data_ptr(), None if weight is None else weight.data_ptr(),
@@ -329,11 +343,11 @@ def _ln_backward(raw, device, dy, x, mean, rstd, weight, dx, dweight, dbias, wor
         given = dweight if dweight is not None else dbias
         shape = given.shape if given is not None else like.shape if like is not None else x.shape[:-2] + x.shape[-1:]
         dtype = given.dtype if given is not None else torch.float32
-        dweight = torch.empty(shape, dtype=dtype, device=device) if dweight is None else dweight
-        dbias = torch.empty(shape, dtype=dtype, device=device) if dbias is None else dbias
+        dweight = _empty(shape, dtype, device) if dweight is None else dweight
+        dbias = _empty(shape, dtype, device) if dbias is None else dbias
     _, ref, need = _ln_desc(_layout(x), _layout(dy), _layout(dx), _layout(weight), None, _layout(dweight), _layout(dbias), 0.0)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace = _empty((need,), torch.uint8, device)
     lib = _LIB or load_library()
     st = lib.liec_layer_norm_backward(ref, dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
                                       None if weight is None else weight.data_ptr(), dx.data_ptr(), dweight.data_ptr(),

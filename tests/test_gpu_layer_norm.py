@@ -152,6 +152,19 @@ def test_two_axes_shared_and_missing_parameters(h, dtype):
     check_backward(dy[1:2], x[1:2], m1[None], r1[None], ones[:1], dtype, "f32", dx3[None], dw3[None], db1[None])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,rows,h", [(2000, 400, 1), (2000, 400, 3), (2000, 400, 5), (2000, 400, 7), (1500, 250, 13), (600, 200, 129),
+                                      (4, 9000, 255), (1, 20000, 511), (3, 5000, 767), (2, 6000, 1019), (1, 4000, 2047), (1, 2500, 4095)])
+def test_odd_rows_through_every_place_of_the_ring(N, rows, h, dtype):
+    """Widths that start each row at another byte of a 16-byte granule (and rows that end in the granule in which
+    they start), with so many rows that every place in shared memory holds many of them one after another."""
+    x, dy, w, b = draw(N, rows, h, dtype, seed=h)
+    y, mean, rstd = liec.liec_layer_norm_forward(x, w, b, 1e-4)
+    check_forward(x, w, b, 1e-4, dtype, y, mean, rstd)
+    dx, dw, db = liec.liec_layer_norm_backward(dy, x, mean, rstd, w)
+    check_backward(dy, x, mean, rstd, w, dtype, "f32", dx, dw, db)
+
+
 @pytest.mark.parametrize("h", [5, 768, 1001, 2048, 10000])
 def test_broadcast_incoming_gradient(h):
     """dy as the gradient of a sum: one value expanded over rows and workers (strides 0)."""
