@@ -29,7 +29,7 @@ struct LnForward {
     float *mean, *rstd;   // [groups][rows], or NULL
     int64_t rows, x_row, x_group, y_row, y_group, weight_stride, bias_stride;
     LnShare share;
-    int32_t groups, cols;
+    int32_t groups, cols, part_cols;   // part_cols: columns per CTA of a row
     float eps;
 };
 
@@ -39,9 +39,8 @@ struct LnBackward {
     void *dx, *dweight, *dbias;   // any may be NULL
     float *part_w, *part_b;       // column sums of pieces of a group's rows, [piece][cols]
     int64_t rows, x_row, x_group, dy_row, dy_group, dx_row, dx_group, weight_stride, dweight_stride, dbias_stride;
-    LnShare share;                // (ctas = 0: the pieces are runs of run_rows rows, counted group by group)
-    int64_t run_rows;
-    int32_t groups, cols, runs, grad_dtype;
+    LnShare share;
+    int32_t groups, cols, part_cols, grad_dtype;
     int32_t direct;               // every group is one CTA's: it writes the gradient itself
 };
 

@@ -1,4 +1,4 @@
-// Layer normalisation, backward pass for rows of up to 8192 columns.  Per row, with xh = (x - m) r and
+// Layer normalisation, backward pass.  Per row, with xh = (x - m) r and
 // q = dy w:  dx = r (q - mean(q) - xh mean(q xh));  per worker  dw = sum over rows of dy xh,  db = sum over
 // rows of dy.  x and dy cross HBM once: the column sums stay in the registers of the threads that own
 // the columns, for all the rows of a CTA, and meet in two steps (slots of a CTA, then CTAs).
@@ -16,15 +16,20 @@ __device__ __forceinline__ void store_grad(void *base, int64_t at, int grad_dtyp
 // CTAs over groups shares.  With a.direct a group is one CTA's and the sums are the gradient.
 // With xc = x - m and g = dy r:  dx = g w - mean(g w) - xc r^2 mean(g w xc),  dw += g xc  (nine operations
 // per element instead of the ten of xh and q).
-template <typename T, bool WHOLE, int NV, int TPR, int SLOTS, int MINB, int R>
+template <typename T, bool WHOLE, bool WIDE, int NV, int TPR, int SLOTS, int MINB, int R>
 __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __grid_constant__ LnBackward a) {
     using S = LnShape<T, WHOLE, NV, TPR, SLOTS, MINB, R, 2>;
     constexpr int VEC = S::VEC, P = VEC / 2;
     extern __shared__ __align__(16) char ln_ring[];
     __shared__ __align__(16) float box[2][SLOTS][S::WARPS][2 * R];
     const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
-    const int h = a.cols;
-    const float inv_h = 1.0f / (float)h;
+    __shared__ float2 meet_rows[2][R][8];
+    // WIDE: this CTA's columns of the cluster's rows
+    const int rank = WIDE ? cluster_rank() : 0, parts = WIDE ? cluster_size() : 1, c0 = WIDE ? rank * a.part_cols : 0;
+    const int64_t cta = WIDE ? blockIdx.x / parts : blockIdx.x;
+    const int h = WIDE ? min(a.part_cols, a.cols - c0) : a.cols;
+    const float inv_h = 1.0f / (float)a.cols;
+    if constexpr (WIDE) cluster_sync();   // (all have started: their shared memory may be written)
     LnPipe<T, S, WHOLE, NV, TPR> px[R], pd[R];
 #pragma unroll
     for (int j = 0; j < R; ++j) {
@@ -33,21 +38,20 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
     }
     int flip = 0;
     const int64_t total = (int64_t)a.groups * a.rows;
-    const int64_t u_end = min(total, a.share.first((int64_t)blockIdx.x + 1));
-    for (int64_t u = a.share.first(blockIdx.x); u < u_end;) {
+    const int64_t u_end = min(total, a.share.first(cta + 1));
+    for (int64_t u = a.share.first(cta); u < u_end;) {
         const int group = (int)(u / a.rows);
         const int64_t r0 = u - (int64_t)group * a.rows;
         const int count = (int)(min(a.rows, r0 + (u_end - u)) - r0);    // rows of this group
         u += count;
         const int turns = (count + SLOTS * R - 1) / (SLOTS * R);
-        const T *x_next = reinterpret_cast<const T *>(a.x) + group * a.x_group + (r0 + slot * R) * a.x_row;       // the next row to fetch
-        const T *dy_next = reinterpret_cast<const T *>(a.dy) + group * a.dy_group + (r0 + slot * R) * a.dy_row;
-        T *dx = reinterpret_cast<T *>(a.dx) + group * a.dx_group + (r0 + slot * R) * a.dx_row;
+        const T *x_next = reinterpret_cast<const T *>(a.x) + group * a.x_group + (r0 + slot * R) * a.x_row + c0;       // the next row to fetch
+        const T *dy_next = reinterpret_cast<const T *>(a.dy) + group * a.dy_group + (r0 + slot * R) * a.dy_row + c0;
+        T *dx = reinterpret_cast<T *>(a.dx) + group * a.dx_group + (r0 + slot * R) * a.dx_row + c0;
         const int64_t x_step = (int64_t)SLOTS * R * a.x_row, dy_step = (int64_t)SLOTS * R * a.dy_row, dx_step = (int64_t)SLOTS * R * a.dx_row;
         const float *mean_at = a.mean + (int64_t)group * a.rows + r0 + slot * R, *rstd_at = a.rstd + (int64_t)group * a.rows + r0 + slot * R;
-        // (a group's first turn: zeros beyond column h; the column sums of the last group lay here)
-        if (h != S::COLS) {
-            for (int q = threadIdx.x; q < S::RING_BYTES / 16; q += S::THREADS) reinterpret_cast<uint4 *>(ln_ring)[q] = make_uint4(0u, 0u, 0u, 0u);
+        if (h != S::COLS) {   // (at every group: the column sums of the last one lay here)
+            ln_clear_tails<S, WHOLE>(ln_ring, h * (int)sizeof(T));
             __syncthreads();
         }
         auto row_of = [&](int turn, int j) { return (turn * SLOTS + slot) * R + j; };
@@ -94,7 +98,7 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
         F2 w[NV][P], gw[NV][P], gb[NV][P];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            ln_parameters<P>(a.weight, group * a.weight_stride, (v * TPR + t) * VEC, h, 1.0f, w[v]);
+            ln_parameters<P>(a.weight, group * a.weight_stride + c0, (v * TPR + t) * VEC, h, 1.0f, w[v]);
 #pragma unroll
             for (int k = 0; k < P; ++k) gw[v][k] = gb[v][k] = f2(0.0f);
         }
@@ -146,6 +150,7 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
             }
             if (a.dx) {
                 slot_sums<TPR, S::WARPS, R>(along, level, t, slot, box[flip]);
+                if constexpr (WIDE) cluster_sums<R>(along, level, rank, parts, meet_rows[flip]);
                 flip ^= 1;
                 if constexpr (!WHOLE && S::WARPS == 1) __syncwarp();   // all have read the rows, whose place the results take
 #pragma unroll
@@ -221,7 +226,7 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
             __syncthreads();
         }
         if (team == 0 && (TPR >= 32 || place < TPR)) {
-            const int64_t piece = ((int64_t)blockIdx.x + group) * h;
+            const int64_t piece = (cta + group) * a.cols + c0;
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
@@ -230,8 +235,8 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
                     const float sw = (k & 1) ? hi(gw[v][k / 2]) : lo(gw[v][k / 2]), sb = (k & 1) ? hi(gb[v][k / 2]) : lo(gb[v][k / 2]);
                     if (c < h) {
                         if (a.direct) {
-                            if (a.dweight) store_grad(a.dweight, group * a.dweight_stride + c, a.grad_dtype, sw);
-                            if (a.dbias) store_grad(a.dbias, group * a.dbias_stride + c, a.grad_dtype, sb);
+                            if (a.dweight) store_grad(a.dweight, group * a.dweight_stride + c0 + c, a.grad_dtype, sw);
+                            if (a.dbias) store_grad(a.dbias, group * a.dbias_stride + c0 + c, a.grad_dtype, sb);
                         } else {
                             a.part_w[piece + c] = sw;
                             a.part_b[piece + c] = sb;
@@ -240,6 +245,7 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
                 }
         }
     }
+    if constexpr (WIDE) cluster_sync();   // none may leave while another still hands it sums
 }
 
 // Joins the pieces of a group, in binary64 and in a fixed order, and rounds once to the gradient rows'
@@ -252,9 +258,9 @@ __global__ void __launch_bounds__(256) ln_backward_join_kernel(const __grid_cons
     if (!out) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, way = threadIdx.x >> 3;
     const int c = blockIdx.x * 32 + (threadIdx.x & 7) * 4;
-    int64_t first = (int64_t)group * a.runs;   // pieces of the group: runs of rows, or the parts of CTAs' shares
-    int pieces = a.runs;
-    if (a.share.ctas > 0) {
+    int64_t first = 0;   // pieces of the group: the parts of CTAs' shares
+    int pieces = 0;
+    if (a.rows > 0) {
         first = a.share.owner((int64_t)group * a.rows) + group;
         pieces = (int)(a.share.owner(((int64_t)group + 1) * a.rows - 1) + group - first) + 1;
     }
@@ -300,11 +306,12 @@ struct LnPlan {
 struct LnPlanner {
     int groups;
     int64_t rows;
+    int parts;
     template <int TPR, int E, int SLOTS, int MINB>
     LnPlan operator()() const {
         constexpr int R = LN_BACKWARD_TURN;
         const int64_t total = (int64_t)groups * rows;
-        const int resident = LN_SMS * MINB;
+        const int resident = ln_resident(MINB, parts);
         LnPlan p;
         // one CTA per group and no second launch: a few turns cost less than the launch; and with many
         // groups their CTAs fill the GPU several times over anyway
@@ -315,13 +322,17 @@ struct LnPlanner {
     }
 };
 
-size_t layer_norm_workspace(int groups, int64_t rows, int cols) {
-    if (rows == 0) return 0;
-    const int64_t pieces = cols > LN_REGISTER_COLS ? groups * ln_wide_runs(rows) : ln_backward_shape(cols, LnPlanner{groups, rows}).pieces;
-    return sizeof(float) * 2 * (size_t)std::max<int64_t>(pieces, groups) * (size_t)cols;
+static LnPlan ln_plan(int groups, int64_t rows, int cols) {
+    const LnPlanner planner{groups, rows, ln_parts(cols)};
+    return planner.parts > 1 ? ln_wide_shape(planner) : ln_backward_shape(cols, planner);
 }
 
-template <typename T, bool WHOLE>
+size_t layer_norm_workspace(int groups, int64_t rows, int cols) {
+    if (rows == 0) return 0;
+    return sizeof(float) * 2 * (size_t)std::max<int64_t>(ln_plan(groups, rows, cols).pieces, groups) * (size_t)cols;
+}
+
+template <typename T, bool WHOLE, bool WIDE = false>
 struct LnBackwardLaunch {
     LnBackward a;
     cudaStream_t st;
@@ -332,31 +343,32 @@ struct LnBackwardLaunch {
         using S = LnShape<T, WHOLE, NV, TPR, SLOTS, MINB, R, 2>;
         static_assert(S::THREADS <= 32 || S::RING_BYTES >= S::THREADS * S::E * 4, "half the CTA's column sums meet in the ring");
         static std::atomic<uint64_t> allowed{0};
-        auto kernel = ln_backward_kernel<T, WHOLE, NV, TPR, SLOTS, MINB, R>;
+        const auto kernel = ln_backward_kernel<T, WHOLE, WIDE, NV, TPR, SLOTS, MINB, R>;
         const cudaError_t e = ln_allow_smem(kernel, S::RING_BYTES, allowed);
         if (e != cudaSuccess) return e;
-        kernel<<<(unsigned)a.share.ctas, S::THREADS, S::RING_BYTES, st>>>(a);
-        return cudaGetLastError();
+        return ln_launch(kernel, a, a.share.ctas, WIDE ? ln_parts(a.cols) : 1, S::THREADS, S::RING_BYTES, st);
     }
 };
 
-static cudaError_t backward_rows(LnBackward &a, int dtype, cudaStream_t st) {
-    if (a.cols > LN_REGISTER_COLS) return launch_layer_norm_backward_wide(a, dtype, st);
-    const int esz = dtype == 0 ? 4 : 2;
-    const bool whole = ln_whole(a.x, a.x_row, a.x_group, a.rows, a.groups, a.cols, esz) &&
-                       ln_whole(a.dy, a.dy_row, a.dy_group, a.rows, a.groups, a.cols, esz) &&
-                       (!a.dx || ln_whole(a.dx, a.dx_row, a.dx_group, a.rows, a.groups, a.cols, esz));
-    const LnPlan p = ln_backward_shape(a.cols, LnPlanner{a.groups, a.rows});
-    a.share = p.share;
-    a.direct = p.direct;
-    if (dtype == 0)
-        return whole ? ln_backward_shape(a.cols, LnBackwardLaunch<float, true>{a, st}) : ln_backward_shape(a.cols, LnBackwardLaunch<float, false>{a, st});
-    return whole ? ln_backward_shape(a.cols, LnBackwardLaunch<__nv_bfloat16, true>{a, st}) : ln_backward_shape(a.cols, LnBackwardLaunch<__nv_bfloat16, false>{a, st});
+template <typename T, bool WHOLE>
+static cudaError_t backward_rows(const LnBackward &a, cudaStream_t st) {
+    if (ln_parts(a.cols) > 1) return ln_wide_shape(LnBackwardLaunch<T, WHOLE, true>{a, st});
+    return ln_backward_shape(a.cols, LnBackwardLaunch<T, WHOLE>{a, st});
 }
 
 cudaError_t launch_layer_norm_backward(LnBackward a, int dtype, cudaStream_t st) {
     if (a.rows > 0) {
-        const cudaError_t e = backward_rows(a, dtype, st);
+        const int esz = dtype == 0 ? 4 : 2;
+        const bool whole = ln_whole(a.x, a.x_row, a.x_group, a.rows, a.groups, a.cols, esz) &&
+                           ln_whole(a.dy, a.dy_row, a.dy_group, a.rows, a.groups, a.cols, esz) &&
+                           (!a.dx || ln_whole(a.dx, a.dx_row, a.dx_group, a.rows, a.groups, a.cols, esz));
+        const LnPlan p = ln_plan(a.groups, a.rows, a.cols);
+        a.share = p.share;
+        a.direct = p.direct;
+        a.part_cols = ln_part_cols(a.cols);
+        const cudaError_t e = dtype == 0 ? whole ? backward_rows<float, true>(a, st) : backward_rows<float, false>(a, st)
+                              : whole    ? backward_rows<__nv_bfloat16, true>(a, st)
+                                         : backward_rows<__nv_bfloat16, false>(a, st);
         if (e != cudaSuccess) return e;
     }
     if ((a.dweight || a.dbias) && !a.direct) {

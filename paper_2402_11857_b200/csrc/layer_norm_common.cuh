@@ -161,6 +161,37 @@ __device__ __forceinline__ void slot_sums(float (&a)[R], float (&b)[R], int t, i
     }
 }
 
+// ---- rows wider than a CTA: a cluster holds one, each CTA a range of its columns ----
+__device__ __forceinline__ int cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return (int)r; }
+__device__ __forceinline__ int cluster_size() { uint32_t r; asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return (int)r; }
+__device__ __forceinline__ void cluster_sync() {   // every thread of every CTA, warps whole
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The CTAs' sums (equal in all threads of a CTA) meet: each hands its own to every other, and all add them up in
+// the same order.  `meet` as the box of slot_sums: two in turn.
+template <int R>
+__device__ __forceinline__ void cluster_sums(float (&a)[R], float (&b)[R], int rank, int size, float2 (*meet)[8]) {
+    if ((int)threadIdx.x < size) {
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            uint32_t to;
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(&meet[j][rank])), "r"(threadIdx.x));
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(a[j]), "f"(b[j]) : "memory");
+        }
+    }
+    __syncwarp();
+    cluster_sync();
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        a[j] = b[j] = 0.0f;
+        for (int q = 0; q < size; ++q) {
+            const float2 v = meet[j][q];
+            a[j] += v.x;
+            b[j] += v.y;
+        }
+    }
+}
+
 template <typename T, bool WHOLE, int NV, int TPR, int SLOTS, int MINB, int R, int ARRAYS>
 struct LnShape {
     static constexpr int VEC = LnChunk<T>::VEC, E = VEC * NV, THREADS = TPR * SLOTS, COLS = TPR * E;
@@ -209,8 +240,7 @@ struct LnPipe {
                 const int at = (v * TPR + t) * 16;
                 if (at + 16 <= end) copy_async(to + at, from + at);
             }
-            // the granules up to (bytes + 14) / 16 are all that some row of this width touches: with zeros there,
-            // nothing of the row that lay here before is left beyond column h
+            // the last granule's first bytes, and zeros behind them and in the granule that a chunk may reach into
             const int tail = (end & ~15) + t * 16;
             if (t < 2 && tail <= bytes + 14) {
                 if (tail > 0 || shift == 0) copy_async(to + tail, tail < end ? from + tail : from, max(end - tail, 0) & 15);
@@ -243,6 +273,14 @@ struct LnPipe {
     // where a result's chunk waits for ln_store_row
     __device__ __forceinline__ char *result(int v, int t, int stage) const { return ring + stage * S::STAGE_BYTES + 16 + (v * TPR + t) * 16; }
 };
+
+// Zeros behind the last granule that a fetch writes, in every place for a row.
+template <typename S, bool WHOLE>
+__device__ __forceinline__ void ln_clear_tails(char *ring, int bytes) {
+    const int first = WHOLE ? bytes / 16 : (bytes + 14) / 16 + 1, left = S::ROW_BYTES / 16 - first;
+    for (int q = threadIdx.x; q < S::RING_BYTES / S::ROW_BYTES * left; q += S::THREADS)
+        *reinterpret_cast<uint4 *>(ring + q / left * S::ROW_BYTES + (first + q % left) * 16) = make_uint4(0u, 0u, 0u, 0u);
+}
 
 // A finished row leaves the ring's stage, where its first element lies at byte 16, in granules of memory; the
 // elements of a first and a last granule that it does not fill go one by one.
@@ -296,7 +334,7 @@ __device__ __forceinline__ void ln_parameters(const float *base, int64_t offset,
 // ---- shapes ----------------------------------------------------------------------------------------
 
 constexpr int LN_SMS = 148;            // a B200's; on another count the grid is only less even
-constexpr int LN_REGISTER_COLS = 8192; // widest row that 512 threads hold
+constexpr int LN_CTA_COLS = 8192;      // widest row that the 512 threads of a CTA hold
 constexpr int LN_SUM_ROWS = 1024;      // rows that one binary32 column accumulator may take
 
 // Rows to CTAs, in whole turns of turn_rows.  SMs do not move data equally fast, so with `uneven` a resident
@@ -316,6 +354,10 @@ inline LnShare ln_share(int64_t total, int turn_rows, int resident, int64_t max_
     s.ctas = s.large + (total - s.large * s.large_rows + s.small_rows - 1) / s.small_rows;
     return s;
 }
+
+// Places for CTAs of minb per SM, or for clusters: not every SM finds a place in a cluster (a cluster lies within
+// one group of SMs), so these get shares of a quarter of the rows that one place would take.
+inline int ln_resident(int minb, int parts) { return parts == 1 ? LN_SMS * minb : (parts == 2 ? 1 : 4) * LN_SMS / parts; }
 
 // Threads per row, elements per thread, slots per CTA and CTAs per SM for h columns:
 // f.template operator()<TPR, E, SLOTS, MINB>().
@@ -345,6 +387,29 @@ auto ln_backward_shape(int h, F &&f) {
     return f.template operator()<512, 16, 1, 1>();
 }
 
+template <typename F>
+auto ln_wide_shape(F &&f) { return f.template operator()<512, 16, 1, 1>(); }   // per CTA of a row's cluster
+
+// CTAs per row, and columns of each (a multiple of 8, so that what starts on 16 bytes does so in every CTA).
+inline int ln_parts(int h) { return (h + LN_CTA_COLS - 1) / LN_CTA_COLS; }
+inline int ln_part_cols(int h) { return ((h + ln_parts(h) - 1) / ln_parts(h) + 7) / 8 * 8; }
+
+template <typename A>
+cudaError_t ln_launch(void (*kernel)(A), const A &a, int64_t ctas, int parts, int threads, int smem, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(ctas * parts));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)parts;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = parts > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 // Dynamic shared memory beyond 48 KB (static included) needs the kernel's consent, once per device.
 template <typename K>
 cudaError_t ln_allow_smem(K kernel, int bytes, std::atomic<uint64_t> &done) {
@@ -367,10 +432,5 @@ inline bool ln_whole(const void *p, int64_t row, int64_t group, int64_t rows, in
     if (groups > 1) bits |= (uint64_t)group * esz;
     return (bits & 15u) == 0;
 }
-
-// generic kernels for rows beyond LN_REGISTER_COLS
-cudaError_t launch_layer_norm_forward_wide(const LnForward &a, int dtype, cudaStream_t st);
-cudaError_t launch_layer_norm_backward_wide(LnBackward &a, int dtype, cudaStream_t st);
-int64_t ln_wide_runs(int64_t rows);
 
 }  // namespace liec

@@ -1,4 +1,4 @@
-// Layer normalisation, forward pass for rows of up to 8192 columns: every element crosses HBM once.
+// Layer normalisation, forward pass every element crosses HBM once.
 // Per row: m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps), y = (x - m) r w + b.
 #include "layer_norm_common.cuh"
 
@@ -6,32 +6,36 @@ namespace liec {
 
 // A CTA takes its share of all groups * rows rows, group after group; every thread of the CTA makes the
 // same number of turns, a turn being R consecutive rows for every slot.
-template <typename T, bool WHOLE, int NV, int TPR, int SLOTS, int MINB, int R>
+template <typename T, bool WHOLE, bool WIDE, int NV, int TPR, int SLOTS, int MINB, int R>
 __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __grid_constant__ LnForward a) {
     using S = LnShape<T, WHOLE, NV, TPR, SLOTS, MINB, R, 1>;
     constexpr int VEC = S::VEC, P = VEC / 2;
     extern __shared__ __align__(16) char ln_ring[];
     __shared__ __align__(16) float box[2][SLOTS][S::WARPS][2 * R];
     const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
-    const int h = a.cols;
-    const float inv_h = 1.0f / (float)h;
+    __shared__ float2 meet[2][R][8];
+    // WIDE: this CTA's columns of the cluster's rows
+    const int rank = WIDE ? cluster_rank() : 0, parts = WIDE ? cluster_size() : 1, c0 = WIDE ? rank * a.part_cols : 0;
+    const int64_t cta = WIDE ? blockIdx.x / parts : blockIdx.x;
+    const int h = WIDE ? min(a.part_cols, a.cols - c0) : a.cols;
+    const float inv_h = 1.0f / (float)a.cols;
     LnPipe<T, S, WHOLE, NV, TPR> px[R];
 #pragma unroll
     for (int j = 0; j < R; ++j) px[j].place(ln_ring, slot * R + j);
-    if (h != S::COLS)   // zeros beyond column h
-        for (int q = threadIdx.x; q < S::RING_BYTES / 16; q += S::THREADS) reinterpret_cast<uint4 *>(ln_ring)[q] = make_uint4(0u, 0u, 0u, 0u);
-    __syncthreads();
+    ln_clear_tails<S, WHOLE>(ln_ring, h * (int)sizeof(T));
+    if constexpr (WIDE) cluster_sync();   // (all have started: their shared memory may be written)
+    else __syncthreads();
     int flip = 0;
     const int64_t total = (int64_t)a.groups * a.rows;
-    const int64_t u_end = min(total, a.share.first((int64_t)blockIdx.x + 1));
-    for (int64_t u = a.share.first(blockIdx.x); u < u_end;) {
+    const int64_t u_end = min(total, a.share.first(cta + 1));
+    for (int64_t u = a.share.first(cta); u < u_end;) {
         const int group = (int)(u / a.rows);
         const int64_t r0 = u - (int64_t)group * a.rows;
         const int count = (int)(min(a.rows, r0 + (u_end - u)) - r0);    // rows of this group
         u += count;
         const int turns = (count + SLOTS * R - 1) / (SLOTS * R);
-        const T *x_next = reinterpret_cast<const T *>(a.x) + group * a.x_group + (r0 + slot * R) * a.x_row;   // the next row to fetch
-        T *y = reinterpret_cast<T *>(a.y) + group * a.y_group + (r0 + slot * R) * a.y_row;
+        const T *x_next = reinterpret_cast<const T *>(a.x) + group * a.x_group + (r0 + slot * R) * a.x_row + c0;   // the next row to fetch
+        T *y = reinterpret_cast<T *>(a.y) + group * a.y_group + (r0 + slot * R) * a.y_row + c0;
         int64_t at = (int64_t)group * a.rows + r0 + slot * R;
         const int64_t x_step = (int64_t)SLOTS * R * a.x_row, y_step = (int64_t)SLOTS * R * a.y_row;
         auto row_of = [&](int turn, int j) { return (turn * SLOTS + slot) * R + j; };
@@ -59,8 +63,8 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __g
         F2 w[NV][P], b[NV][P];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            ln_parameters<P>(a.weight, group * a.weight_stride, (v * TPR + t) * VEC, h, 1.0f, w[v]);
-            ln_parameters<P>(a.bias, group * a.bias_stride, (v * TPR + t) * VEC, h, 0.0f, b[v]);
+            ln_parameters<P>(a.weight, group * a.weight_stride + c0, (v * TPR + t) * VEC, h, 1.0f, w[v]);
+            ln_parameters<P>(a.bias, group * a.bias_stride + c0, (v * TPR + t) * VEC, h, 0.0f, b[v]);
         }
         for (int i = 0, stage = 0; i < turns; ++i) {
             const int ahead = i + S::STAGES - 1;                               // turn to fetch now
@@ -92,6 +96,7 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __g
                 var[j] = lo(q2) + hi(q2);
             }
             slot_sums<TPR, S::WARPS, R>(mean, var, t, slot, box[flip]);
+            if constexpr (WIDE) cluster_sums<R>(mean, var, rank, parts, meet[flip]);
             flip ^= 1;
             if constexpr (!WHOLE && S::WARPS == 1) __syncwarp();   // all have read the rows, whose place the results take
             // var = mean(x^2) - mean^2 keeps its digits while mean^2 is at most a quarter of it (the difference
@@ -129,6 +134,7 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __g
                     unused[j] = 0.0f;
                 }
                 slot_sums<TPR, S::WARPS, R>(around, unused, t, slot, box[flip]);
+                if constexpr (WIDE) cluster_sums<R>(around, unused, rank, parts, meet[flip]);
                 flip ^= 1;
 #pragma unroll
                 for (int j = 0; j < R; ++j)
@@ -147,7 +153,7 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __g
                     for (int k = 0; k < P; ++k) x[j][v][k] = fma(mul(x[j][v][k], scale), w[v][k], b[v][k]);
                     if (live && c < h) LnChunk<T>::write(WHOLE ? reinterpret_cast<char *>(yj + c) : px[j].result(v, t, stage), x[j][v]);
                 }
-                if (live && t == 0) {
+                if (live && t == 0 && rank == 0) {
                     if (a.mean) a.mean[at + j] = mean[j];
                     if (a.rstd) a.rstd[at + j] = rstd;
                 }
@@ -167,9 +173,10 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_forward_kernel(const __g
         copy_wait<0>();
         if constexpr (!WHOLE) __syncthreads();   // the next group's rows go into the same ring
     }
+    if constexpr (WIDE) cluster_sync();   // none may leave while another still hands it sums
 }
 
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, bool WIDE = false>
 struct LnForwardLaunch {
     LnForward a;
     cudaStream_t st;
@@ -179,25 +186,30 @@ struct LnForwardLaunch {
         constexpr int R = E <= 16 ? 2 : 1;   // rows per turn: two where the registers hold them
         using S = LnShape<T, WHOLE, NV, TPR, SLOTS, MINB, R, 1>;
         static std::atomic<uint64_t> allowed{0};
-        auto kernel = ln_forward_kernel<T, WHOLE, NV, TPR, SLOTS, MINB, R>;
+        const auto kernel = ln_forward_kernel<T, WHOLE, WIDE, NV, TPR, SLOTS, MINB, R>;
         const cudaError_t e = ln_allow_smem(kernel, S::RING_BYTES, allowed);
         if (e != cudaSuccess) return e;
+        const int parts = WIDE ? ln_parts(a.cols) : 1;
+        a.part_cols = ln_part_cols(a.cols);
         // (one CTA per SM: a small share would leave its SM idle while it starts)
-        a.share = ln_share((int64_t)a.groups * a.rows, SLOTS * R, LN_SMS * MINB, 1 << 30, MINB > 1);
-        kernel<<<(unsigned)a.share.ctas, S::THREADS, S::RING_BYTES, st>>>(a);
-        return cudaGetLastError();
+        a.share = ln_share((int64_t)a.groups * a.rows, SLOTS * R, ln_resident(MINB, parts), 1 << 30, MINB > 1);
+        return ln_launch(kernel, a, a.share.ctas, parts, S::THREADS, S::RING_BYTES, st);
     }
 };
 
+template <typename T, bool WHOLE>
+static cudaError_t forward_rows(const LnForward &a, cudaStream_t st) {
+    if (ln_parts(a.cols) > 1) return ln_wide_shape(LnForwardLaunch<T, WHOLE, true>{a, st});
+    return ln_forward_shape(a.cols, LnForwardLaunch<T, WHOLE>{a, st});
+}
+
 cudaError_t launch_layer_norm_forward(const LnForward &a, int dtype, cudaStream_t st) {
     if (a.rows == 0) return cudaSuccess;
-    if (a.cols > LN_REGISTER_COLS) return launch_layer_norm_forward_wide(a, dtype, st);
     const int esz = dtype == 0 ? 4 : 2;
     const bool whole = ln_whole(a.x, a.x_row, a.x_group, a.rows, a.groups, a.cols, esz) &&
                        ln_whole(a.y, a.y_row, a.y_group, a.rows, a.groups, a.cols, esz);
-    if (dtype == 0)
-        return whole ? ln_forward_shape(a.cols, LnForwardLaunch<float, true>{a, st}) : ln_forward_shape(a.cols, LnForwardLaunch<float, false>{a, st});
-    return whole ? ln_forward_shape(a.cols, LnForwardLaunch<__nv_bfloat16, true>{a, st}) : ln_forward_shape(a.cols, LnForwardLaunch<__nv_bfloat16, false>{a, st});
+    if (dtype == 0) return whole ? forward_rows<float, true>(a, st) : forward_rows<float, false>(a, st);
+    return whole ? forward_rows<__nv_bfloat16, true>(a, st) : forward_rows<__nv_bfloat16, false>(a, st);
 }
 
 }  // namespace liec
