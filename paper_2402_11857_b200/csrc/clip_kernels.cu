@@ -342,9 +342,10 @@ __device__ __forceinline__ double group_tree(double warp_sum, double *warp_sums,
 }
 
 // Balanced tree over a row's tile sums as they come in (a group; result in its thread 0).  A warp takes 1024
-// consecutive sums as 16 rows of 64, two per lane; `missing` is set when one did not come within the limit.
+// consecutive sums as 16 rows of 64, two per lane; `missing` is set when one did not come within
+// the limit, or the CTA stops.
 __device__ __noinline__ double row_tree(const double *src, int tiles, double *warp_sums /*[4]*/, double *pass_sums /*[ROW_PASSES]*/,
-                                           int g, bool &missing) {
+                                           int g, const volatile int *stop, bool &missing) {
     const int t = threadIdx.x % GROUP, warp = t / 32, lane = t & 31;
     const int passes = (tiles + 8 * GROUP * 4 - 1) / (8 * GROUP * 4);
     missing = false;
@@ -363,7 +364,7 @@ __device__ __noinline__ double row_tree(const double *src, int tiles, double *wa
 #pragma unroll
                 for (int j = 0; j < 8; ++j) unset |= v[j][0] == UNSET64 || v[j][1] == UNSET64;
                 if (!__any_sync(0xffffffffu, unset)) break;
-                if (tries > NORM_WAIT_LIMIT) { missing = true; break; }
+                if (__any_sync(0xffffffffu, tries > NORM_WAIT_LIMIT || *stop)) { missing = true; break; }
                 __nanosleep(40);
             }
             double leaf[8];
@@ -630,11 +631,11 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
                 }
             } else if (o.kind == OP_JOIN) {
                 bool missing;
-                const double sum = row_tree(a.partials + (int64_t)o.row * p.TT, p.TT, warp_sums[g], pass_sums[g], g, missing);
+                const double sum = row_tree(a.partials + (int64_t)o.row * p.TT, p.TT, warp_sums[g], pass_sums[g], g, &stop, missing);
                 if (t == 0) {
                     mbar_arrive(&done[slot]);
                     if (missing) {
-                        atomicOr(p.status, STATUS_NORM_TIMEOUT);
+                        if (!stop) atomicOr(p.status, STATUS_NORM_TIMEOUT);
                         stop = 1;
                     } else {
                         float norm;

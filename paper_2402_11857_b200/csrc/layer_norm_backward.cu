@@ -185,6 +185,7 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
             stage = stage + 1 == S::STAGES ? 0 : stage + 1;
         }
         copy_wait<0>();
+        if (u >= u_end) asm volatile("griddepcontrol.launch_dependents;");   // (the join may take its places)
         __syncthreads();   // the ring is free: for the sums of the slots and for the next group
         if (!a.dweight && !a.dbias) continue;
         // the slots' sums meet: lanes of one warp by shuffles, then halves of the CTA through shared memory
@@ -255,7 +256,7 @@ __global__ void __launch_bounds__(256) ln_backward_join_kernel(const __grid_cons
     const int group = blockIdx.y;
     const bool weight = blockIdx.z == 0;
     void *out = weight ? a.dweight : a.dbias;
-    if (!out) return;
+    if (!out) return;   // (uniform; ends without the wait: it touches nothing)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, way = threadIdx.x >> 3;
     const int c = blockIdx.x * 32 + (threadIdx.x & 7) * 4;
     int64_t first = 0;   // pieces of the group: the parts of CTAs' shares
@@ -264,6 +265,7 @@ __global__ void __launch_bounds__(256) ln_backward_join_kernel(const __grid_cons
         first = a.share.owner((int64_t)group * a.rows) + group;
         pieces = (int)(a.share.owner(((int64_t)group + 1) * a.rows - 1) + group - first) + 1;
     }
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // the pieces are complete
     const float *p = (weight ? a.part_w : a.part_b) + (first + way) * a.cols + c;
     const int64_t step = (int64_t)32 * a.cols;
     double s[4] = {0.0, 0.0, 0.0, 0.0};
@@ -313,9 +315,11 @@ struct LnPlanner {
         const int64_t total = (int64_t)groups * rows;
         const int resident = ln_resident(MINB, parts);
         LnPlan p;
-        // one CTA per group and no second launch: a few turns cost less than the launch; and with many
-        // groups their CTAs fill the GPU several times over anyway
-        p.direct = rows <= 8 * SLOTS * R || (groups >= 4 * resident && rows <= (int64_t)SLOTS * LN_SUM_ROWS);
+        // one CTA (or cluster) per group and no second launch, which costs the host 2 us as well: up to four turns
+        // (4 rows of 8192 binary32 columns, eight groups: 13.6 us, 15.8 us shared and joined; one group 13.5 and
+        // 10.2 us; 16 rows of 768: 6.8 and 5.1 us, 32 rows 9.3 and 5.1 us); or with so many groups that their CTAs
+        // fill the GPU several times over anyway
+        p.direct = rows <= 4 * SLOTS * R || (groups >= 4 * resident && rows <= (int64_t)SLOTS * LN_SUM_ROWS);
         p.share = p.direct ? LnShare{0, 0, rows, groups} : ln_share(total, SLOTS * R, resident, LN_SUM_ROWS / R, false);
         p.pieces = p.direct ? 0 : p.share.ctas + groups;
         return p;
@@ -372,8 +376,17 @@ cudaError_t launch_layer_norm_backward(LnBackward a, int dtype, cudaStream_t st)
         if (e != cudaSuccess) return e;
     }
     if ((a.dweight || a.dbias) && !a.direct) {
-        ln_backward_join_kernel<<<dim3((a.cols + 31) / 32, a.groups, 2), 256, 0, st>>>(a);
-        return cudaGetLastError();
+        // launched while the rows' kernel ends; it waits for that kernel's end before it reads
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((a.cols + 31) / 32, a.groups, 2);
+        cfg.blockDim = dim3(256);
+        cfg.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = a.rows > 0 ? 1 : 0;
+        return cudaLaunchKernelEx(&cfg, ln_backward_join_kernel, a);
     }
     return cudaSuccess;
 }

@@ -173,6 +173,48 @@ def test_extreme_values(gdt, zero_nonfinite):
     assert same(got, torch.from_numpy(norms)) and same(Gd, rounded(want, gdt))
 
 
+@pytest.mark.parametrize("gdt", [liec.F32, liec.BF16])
+@pytest.mark.parametrize("N,tiles", [(300, 3), (150, 7), (150, 8), (40, 20), (300, 12), (40, 33), (2, 700), (1, 4100)])
+def test_many_rows_and_norms_only(N, tiles, gdt):
+    """Rows of a few tiles to a few thousand, few and many of them: clipped, and in place with nothing to clip,
+    where only the norms are wanted and the rows stay as they are."""
+    off = [0, 5 * TILE // 2, tiles * TILE - 9] if tiles > 2 else [0, tiles * TILE]
+    d = off[-1]
+    gen = torch.Generator(device=DEV).manual_seed(tiles)
+    G = (torch.randn(N, d, generator=gen, device=DEV) * torch.linspace(0.5, 1.5, N, device=DEV)[:, None]).to(TDT[gdt])
+    rows = widen(G.cpu())
+    max_norm = float(np.median(np.linalg.norm(rows.astype(np.float64), axis=1)))
+    want, norms = reference(rows, off, max_norm)
+    ctx = context(N, off, gdt)
+    Gd = G.clone()
+    assert same(ctx.liec_clip_grads(Gd, float("inf")), torch.from_numpy(norms)) and torch.equal(Gd, G)
+    out = torch.full((N, d), 7.0, dtype=TDT[gdt], device=DEV)
+    assert same(ctx.liec_clip_grads(Gd, max_norm, out=out), torch.from_numpy(norms))
+    assert same(out, rounded(want, gdt)) and torch.equal(Gd, G)
+    assert same(ctx.liec_clip_grads(Gd, max_norm), torch.from_numpy(norms)) and same(Gd, out)
+    assert ctx.liec_device_status() == 0
+
+
+@pytest.mark.parametrize("gdt", [liec.F32, liec.BF16])
+def test_copy_wait_runs_out(gdt):
+    """A bulk copy whose barrier never completes: the wait ends by its limit, bit 8 is set, no row is written,
+    and the next call with the limit restored is right."""
+    off, N = [0, 40 * TILE], 2
+    G = make_gradients("normal", 0.1, N, off[-1], 0, base_seed=15).to(TDT[gdt])
+    want, norms = reference(widen(G), off, 1.0)
+    ctx = context(N, off, gdt)
+    Gd, out = G.to(DEV), torch.full((N, off[-1]), 7.0, dtype=TDT[gdt], device=DEV)
+    ctx.liec_set_copy_wait(poll_limit=1000, expect_extra_bytes=16)
+    ctx.liec_clip_grads(Gd, 1.0, out=out)
+    torch.cuda.synchronize()
+    assert ctx.liec_device_status() & 8
+    assert (out == 7).all() and same(Gd, G)
+    ctx.liec_set_copy_wait()
+    ctx.liec_clear_status()
+    assert same(ctx.liec_clip_grads(Gd, 1.0, out=out), torch.from_numpy(norms)) and same(out, rounded(want, gdt))
+    assert ctx.liec_device_status() == 0
+
+
 def test_norm_at_the_limit_is_left_alone():
     """norm == max_norm is not clipped; one step of binary32 above it is."""
     off = [0, 4]
