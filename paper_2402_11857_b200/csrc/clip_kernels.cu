@@ -18,6 +18,7 @@
 #include <cmath>
 
 #include "device_common.cuh"
+#include "granule.cuh"
 #include "kernels.h"
 
 namespace liec {
@@ -54,6 +55,30 @@ struct Raw {
                 w[k / 2] = (k < left ? (uint32_t)h[k] : 0u) | (k + 1 < left ? (uint32_t)h[k + 1] << 16 : 0u);
             }
         }
+    }
+    // from any place that is not on 16 bytes: out of the granules that hold them, all of which are read
+    __device__ __forceinline__ void load_cut(const ST *ptr) {
+        const uint32_t shift = (uint32_t)reinterpret_cast<uintptr_t>(ptr) & 15u;
+        if constexpr (WORDS == 2) {
+            const uint32_t *q = reinterpret_cast<const uint32_t *>(reinterpret_cast<const char *>(ptr) - (shift & 2u));
+            const uint32_t w0 = q[0], w1 = q[1], w2 = (shift & 2u) ? q[2] : 0u, half = (shift & 2u) * 8u;
+            w[0] = __funnelshift_r(w0, w1, half);
+            w[1] = __funnelshift_r(w1, w2, half);
+        } else {
+            const uint4 *g = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(ptr) - shift);
+            uint4 a = g[0];
+#pragma unroll
+            for (int k = 0; k < WORDS; k += 4) {
+                const uint4 b = g[k / 4 + 1], q = cut_granules<(int)sizeof(ST)>(a, b, shift);
+                w[k] = q.x; w[k + 1] = q.y; w[k + 2] = q.z; w[k + 3] = q.w;
+                a = b;
+            }
+        }
+    }
+    // whether elements [pos, pos + VEC) of src may be loaded so: all that it reads lies in [0, len)
+    static __device__ __forceinline__ bool can_cut(const ST *src, int pos, int len) {
+        const int over = (int)((uint32_t)reinterpret_cast<uintptr_t>(src + pos) & 15u) / (int)sizeof(ST);
+        return pos >= over && pos - over + VEC + 16 / (int)sizeof(ST) <= len;
     }
     __device__ __forceinline__ float get(int k) const {
         if constexpr (sizeof(ST) == 4) return __uint_as_float(w[k]);
@@ -103,6 +128,7 @@ __device__ __forceinline__ double warp_sumsq(const ST *src, int len, int t) {
         for (int j = 0; j < ROWS; ++j) {
             const int pos = first + j * 32 * VEC;
             if (aligned && pos + VEC <= len) raw[j].template load<false>(src + pos);
+            else if (!aligned && Raw<ST, VEC>::can_cut(src, pos, len)) raw[j].load_cut(src + pos);
             else raw[j].load_guarded(src + pos, len - pos);
         }
     }
@@ -137,6 +163,7 @@ __device__ __forceinline__ void scale_tile(const ST *src, DT *dst, int len, floa
         const int k = t + j * THREADS;
         if (k < chunks) {
             if (aligned) raw[j].template load<true>(src + head + k * VEC);
+            else if (Raw<ST, VEC>::can_cut(src, head + k * VEC, len)) raw[j].load_cut(src + head + k * VEC);
             else raw[j].load_guarded(src + head + k * VEC, VEC);
         }
     }
@@ -322,7 +349,7 @@ __device__ __forceinline__ void read_tile(Raw<ST, VEC> &raw, const ST *src, cons
     constexpr int ALIGN = VEC * (int)sizeof(ST) < 16 ? VEC * (int)sizeof(ST) : 16;
     if (pos >= in.beg && pos + VEC <= in.end) {
         if ((smem_u32(buf + pos) & (ALIGN - 1)) == 0) raw.template load<false>(buf + pos);
-        else raw.load_guarded(buf + pos, VEC);
+        else raw.load_cut(buf + pos);   // (what is staged begins and ends with whole granules)
         return;
     }
     for (int k = 0; k < VEC; ++k) {   // at the ends of the tile
@@ -393,11 +420,20 @@ __device__ __noinline__ double sum_ragged(const ST *src, const ST *buf, int len,
     constexpr int VEC = 16 / (int)sizeof(ST), ROWS = 32 / VEC;
     const Staged<ST> in(src, len);
     double leaf[ROWS];
+    const int base = first - (int)(threadIdx.x & 31) * VEC;
+    if (base >= in.beg && base + 1024 <= in.end && in.shift != 0) {   // all of the warp's elements, off the granules
+        Raw<ST, VEC> raw[ROWS];
 #pragma unroll
-    for (int j = 0; j < ROWS; ++j) {
-        Raw<ST, VEC> raw;
-        read_tile<ST, VEC>(raw, src, buf, in, first + j * 32 * VEC, len);
-        leaf[j] = leaf_sq(raw);
+        for (int j = 0; j < ROWS; ++j) raw[j].load_cut(buf + first + j * 32 * VEC);
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) leaf[j] = leaf_sq(raw[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+            Raw<ST, VEC> raw;
+            read_tile<ST, VEC>(raw, src, buf, in, first + j * 32 * VEC, len);
+            leaf[j] = leaf_sq(raw);
+        }
     }
     return warp_tree_reduce<ROWS>(leaf, threadIdx.x & 31);
 }

@@ -22,6 +22,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "granule.cuh"
 #include "layer_norm.h"
 
 namespace liec {
@@ -62,12 +63,6 @@ template <> struct LnChunk<float> {
     static __device__ __forceinline__ void write(void *p, const F2 (&in)[2]) {
         *reinterpret_cast<float4 *>(p) = make_float4(lo(in[0]), hi(in[0]), lo(in[1]), hi(in[1]));
     }
-    // 16 bytes from byte `shift` (a multiple of the element's size, below 16) of 32
-    static __device__ __forceinline__ uint4 cut(uint4 a, uint4 b, uint32_t shift) {
-        const bool two = (shift & 8u) != 0, one = (shift & 4u) != 0;
-        const uint32_t w0 = two ? a.z : a.x, w1 = two ? a.w : a.y, w2 = two ? b.x : a.z, w3 = two ? b.y : a.w, w4 = two ? b.z : b.x;
-        return make_uint4(one ? w1 : w0, one ? w2 : w1, one ? w3 : w2, one ? w4 : w3);
-    }
 };
 template <> struct LnChunk<__nv_bfloat16> {
     static constexpr int VEC = 8;
@@ -82,13 +77,6 @@ template <> struct LnChunk<__nv_bfloat16> {
     }
     static __device__ __forceinline__ void write(void *p, const F2 (&in)[4]) {
         *reinterpret_cast<uint4 *>(p) = make_uint4(word(in[0]), word(in[1]), word(in[2]), word(in[3]));
-    }
-    static __device__ __forceinline__ uint4 cut(uint4 a, uint4 b, uint32_t shift) {
-        const bool two = (shift & 8u) != 0, one = (shift & 4u) != 0;
-        const uint32_t half = (shift & 2u) * 8u;
-        const uint32_t v0 = two ? a.z : a.x, v1 = two ? a.w : a.y, v2 = two ? b.x : a.z, v3 = two ? b.y : a.w, v4 = two ? b.z : b.x, v5 = two ? b.w : b.y;
-        const uint32_t w0 = one ? v1 : v0, w1 = one ? v2 : v1, w2 = one ? v3 : v2, w3 = one ? v4 : v3, w4 = one ? v5 : v4;
-        return make_uint4(__funnelshift_r(w0, w1, half), __funnelshift_r(w1, w2, half), __funnelshift_r(w2, w3, half), __funnelshift_r(w3, w4, half));
     }
 };
 
@@ -268,7 +256,7 @@ struct LnPipe {
     __device__ __forceinline__ void read(int v, int t, int stage, F2 (&out)[S::VEC / 2]) const {
         const uint4 *g = reinterpret_cast<const uint4 *>(ring + stage * S::STAGE_BYTES + (v * TPR + t) * 16);
         if constexpr (WHOLE) LnChunk<T>::read(g[0], out);
-        else LnChunk<T>::read(LnChunk<T>::cut(g[0], g[1], now & 15u), out);
+        else LnChunk<T>::read(cut_granules<(int)sizeof(T)>(g[0], g[1], now & 15u), out);
     }
     // where a result's chunk waits for ln_store_row
     __device__ __forceinline__ char *result(int v, int t, int stage) const { return ring + stage * S::STAGE_BYTES + 16 + (v * TPR + t) * 16; }
@@ -296,7 +284,7 @@ __device__ __forceinline__ void ln_store_row(T *row, const char *stage, int t, i
         const int at = (v * TPR + t) * 16;
         if (at + 16 <= end && (v > 0 || at >= shift)) {
             const uint4 *q = reinterpret_cast<const uint4 *>(g + at);
-            *reinterpret_cast<uint4 *>(to + at) = LnChunk<T>::cut(q[0], q[1], turn);
+            *reinterpret_cast<uint4 *>(to + at) = cut_granules<(int)sizeof(T)>(q[0], q[1], turn);
         }
     }
     if (t < LnChunk<T>::VEC) {
