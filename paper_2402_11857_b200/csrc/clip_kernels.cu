@@ -75,11 +75,6 @@ struct Raw {
             }
         }
     }
-    // whether elements [pos, pos + VEC) of src may be loaded so: all that it reads lies in [0, len)
-    static __device__ __forceinline__ bool can_cut(const ST *src, int pos, int len) {
-        const int over = (int)((uint32_t)reinterpret_cast<uintptr_t>(src + pos) & 15u) / (int)sizeof(ST);
-        return pos >= over && pos - over + VEC + 16 / (int)sizeof(ST) <= len;
-    }
     __device__ __forceinline__ float get(int k) const {
         if constexpr (sizeof(ST) == 4) return __uint_as_float(w[k]);
         else return __uint_as_float((k & 1) ? (w[k / 2] & 0xffff0000u) : (w[k / 2] << 16));
@@ -128,7 +123,6 @@ __device__ __forceinline__ double warp_sumsq(const ST *src, int len, int t) {
         for (int j = 0; j < ROWS; ++j) {
             const int pos = first + j * 32 * VEC;
             if (aligned && pos + VEC <= len) raw[j].template load<false>(src + pos);
-            else if (!aligned && Raw<ST, VEC>::can_cut(src, pos, len)) raw[j].load_cut(src + pos);
             else raw[j].load_guarded(src + pos, len - pos);
         }
     }
@@ -163,7 +157,6 @@ __device__ __forceinline__ void scale_tile(const ST *src, DT *dst, int len, floa
         const int k = t + j * THREADS;
         if (k < chunks) {
             if (aligned) raw[j].template load<true>(src + head + k * VEC);
-            else if (Raw<ST, VEC>::can_cut(src, head + k * VEC, len)) raw[j].load_cut(src + head + k * VEC);
             else raw[j].load_guarded(src + head + k * VEC, VEC);
         }
     }
@@ -279,6 +272,7 @@ struct Op {
     const void *src;   // the tile's first element, or NULL
     int64_t at;        // the same within the rows
     int kind, row, tile, len, buffer;
+    int open;          // whether the granules at the tile's ends may be read whole: 1 the first, 2 the last
 };
 
 // Before the kernel all counters, sums and factors are filled with bytes 0xC0: a negative number as a sum of
@@ -330,16 +324,20 @@ __device__ __forceinline__ void fetch_bulk(void *dst_smem, const void *src, uint
                  ::"r"(smem_u32(dst_smem)), "l"(src), "r"(bytes), "r"(b) : "memory");
 }
 
-// The part of a tile that a bulk copy can bring: elements [beg, end), 16-byte pieces of the source.
+// The part of a tile that a bulk copy can bring: elements [beg, end), out of 16-byte granules [lo, hi) counted in
+// bytes from the one in which the tile starts.  A granule at an end is among them only where the array goes on
+// beyond the tile (`open`); the neighbour's elements in it, which another group may just be writing, are not used.
 template <typename ST>
 struct Staged {
-    int beg, end, shift;   // shift: the tile's first byte in its buffer
-    __device__ __forceinline__ Staged(const ST *src, int len) {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(src);
-        shift = (int)(at & 15u);
-        beg = (int)((16u - (at & 15u)) & 15u) / (int)sizeof(ST);
-        end = len - (int)((at + (uintptr_t)len * sizeof(ST)) & 15u) / (int)sizeof(ST);
-        if (!src || end <= beg) beg = end = 0;
+    int beg, end, shift, lo, hi;   // shift: the tile's first byte in its buffer
+    __device__ __forceinline__ Staged(const ST *src, int len, int open) {
+        shift = (int)(reinterpret_cast<uintptr_t>(src) & 15u);
+        const int bytes = shift + len * (int)sizeof(ST);
+        lo = (open & 1) ? 0 : (shift + 15) & ~15;
+        hi = (open & 2) ? (bytes + 15) & ~15 : bytes & ~15;
+        if (!src || hi <= lo) lo = hi = shift;   // nothing
+        beg = max(lo - shift, 0) / (int)sizeof(ST);
+        end = min((hi - shift) / (int)sizeof(ST), len);
     }
 };
 
@@ -416,9 +414,9 @@ __device__ __noinline__ double row_tree(const double *src, int tiles, double *wa
 // The two ops on tiles that are not whole or not aligned.  (These and row_tree are functions of their own:
 // inlined, the consumers' code no longer fits the instruction cache and every op waits for instructions.)
 template <typename ST>
-__device__ __noinline__ double sum_ragged(const ST *src, const ST *buf, int len, int first /*this lane's place among 1024 elements*/) {
+__device__ __noinline__ double sum_ragged(const ST *src, const ST *buf, int len, int open, int first /*this lane's place among 1024 elements*/) {
     constexpr int VEC = 16 / (int)sizeof(ST), ROWS = 32 / VEC;
-    const Staged<ST> in(src, len);
+    const Staged<ST> in(src, len, open);
     double leaf[ROWS];
     const int base = first - (int)(threadIdx.x & 31) * VEC;
     if (base >= in.beg && base + 1024 <= in.end && in.shift != 0) {   // all of the warp's elements, off the granules
@@ -439,9 +437,9 @@ __device__ __noinline__ double sum_ragged(const ST *src, const ST *buf, int len,
 }
 
 template <typename ST, typename DT>
-__device__ __noinline__ void scale_ragged(const ST *src, const ST *buf, int len, DT *dst, RowFactor rf) {
+__device__ __noinline__ void scale_ragged(const ST *src, const ST *buf, int len, int open, DT *dst, RowFactor rf) {
     constexpr int VEC = 16 / (int)sizeof(DT);
-    const Staged<ST> in(src, len);
+    const Staged<ST> in(src, len, open);
     const ST *from = rf.clear ? nullptr : src;
     const int t = threadIdx.x % GROUP;
     const int lead = min(len, (int)(((16u - (unsigned)(reinterpret_cast<uintptr_t>(dst) & 15u)) & 15u) / sizeof(DT)));
@@ -492,11 +490,11 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
         // the warp, which executes in order, does not wait for the tables
         struct Look {
             const ST *tensor;         // gather: the tile's tensor ...
-            long long at, tensor_at;  // (the tile's and) its first element within the row
+            long long at, tensor_at, tensor_end;  // (the tile's and) its first element within the row, and its end
             int row, tile, len;
         };
         auto look = [&](bool valid, int row, int tile) {
-            Look l{nullptr, 0, 0, row, tile, 0};
+            Look l{nullptr, 0, 0, 0, row, tile, 0};
             if (valid) {
                 l.at = __ldg(reinterpret_cast<const long long *>(p.tile_at) + tile);
                 l.len = __ldg(p.tile_len + tile);
@@ -504,6 +502,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
                     const int seg = __ldg(p.tile_seg + tile);
                     l.tensor = reinterpret_cast<const ST *>(__ldg(reinterpret_cast<const unsigned long long *>(a.table) + (int64_t)row * p.T + seg));
                     l.tensor_at = __ldg(reinterpret_cast<const long long *>(p.seg_off) + seg);
+                    l.tensor_end = __ldg(reinterpret_cast<const long long *>(p.seg_off) + seg + 1);
                 }
             }
             return l;
@@ -512,12 +511,19 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
             if (a.table) return l.tensor ? l.tensor + (l.at - l.tensor_at) : nullptr;
             return reinterpret_cast<const ST *>(a.rows) + (int64_t)l.row * p.d + l.at;
         };
+        // (the rows as a whole begin on 16 bytes; a tile that does not begin its tensor has 8192 elements before it)
+        auto open_ends = [&](const Look &l, const ST *src) {
+            const int more = (int)(-(intptr_t)(src + l.len) & 15) / (int)sizeof(ST);   // elements after the tile in its last granule
+            if (a.table) return (l.at > l.tensor_at ? 1 : 0) | (l.at + l.len + more <= l.tensor_end ? 2 : 0);
+            return 1 | ((int64_t)l.row * p.d + l.at + l.len + more <= (int64_t)p.N * p.d ? 2 : 0);
+        };
         auto issue = [&](int kind, int count, const Look &l) {
             bool pending = lane < count;
             const uint32_t first_op = next_op, op = first_op + lane, m = next_stream + lane;
             const int slot = op % OP_SLOTS;
             const bool streams = kind == OP_SUM || kind == OP_SCALE;
-            const Op o{source(l), l.at, kind, l.row, l.tile, l.len, (int)(m % Shape::RING)};
+            const ST *src = source(l);
+            const Op o{src, l.at, kind, l.row, l.tile, l.len, (int)(m % Shape::RING), open_ends(l, src)};
             uint32_t before = op;   // the op that the buffer waits for (op itself: none)
             if (pending && streams) stream_op[m % 64] = op;
             __syncwarp();
@@ -531,12 +537,11 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
                 if (pending && !wait_slot && !wait_buffer) {
                     pending = false;
                     ops[slot] = o;
-                    const ST *src = reinterpret_cast<const ST *>(o.src);
-                    const Staged<ST> in(src, o.len);
-                    const uint32_t bytes = (uint32_t)(in.end - in.beg) * (uint32_t)sizeof(ST);
+                    const Staged<ST> in(src, o.len, o.open);
+                    const uint32_t bytes = streams ? (uint32_t)(in.hi - in.lo) : 0u;   // (the other ops have no buffer)
                     if (bytes) {
-                        char *dst = ring + (size_t)o.buffer * Shape::STRIDE + in.shift + in.beg * (int)sizeof(ST);
-                        fetch_bulk(dst, src + in.beg, bytes, bytes + p.copy_expect_extra, &full[slot]);
+                        char *dst = ring + (size_t)o.buffer * Shape::STRIDE + in.lo;
+                        fetch_bulk(dst, reinterpret_cast<const char *>(src) - in.shift + in.lo, bytes, bytes + p.copy_expect_extra, &full[slot]);
                     } else {
                         mbar_arrive(&full[slot]);
                     }
@@ -636,11 +641,11 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
             const Op o = ops[slot];
             if (o.kind == OP_END) break;
             const ST *src = reinterpret_cast<const ST *>(o.src);
-            const Staged<ST> in(src, o.len);
+            const Staged<ST> in(src, o.len, o.open);
             const ST *buf = reinterpret_cast<const ST *>(ring + (size_t)o.buffer * Shape::STRIDE + in.shift);
             if (o.kind == OP_SUM) {
                 constexpr int VEC = 16 / (int)sizeof(ST), ROWS = 32 / VEC, PER_WARP = TILE / (GROUP / 32);
-                const bool plain = o.len == TILE && in.end == TILE;   // (then beg = shift = 0 as well)
+                const bool plain = o.len == TILE && in.end == TILE && in.shift == 0;   // (then beg = 0 as well)
                 static_assert(PER_WARP == 2048, "two subtrees of 1024 elements per warp");
                 double sum = 0.0;
 #pragma unroll 1
@@ -656,7 +661,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
                         for (int j = 0; j < ROWS; ++j) leaf[j] = leaf_sq(raw[j]);
                         part = warp_tree_reduce<ROWS>(leaf, lane);
                     } else {
-                        part = sum_ragged(src, buf, o.len, first);
+                        part = sum_ragged(src, buf, o.len, o.open, first);
                     }
                     sum = half == 0 ? part : __dadd_rn(sum, part);
                 }
@@ -704,7 +709,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
                 if (!(a.in_place && rf.factor == 1.0f && !rf.clear)) {
                     DT *dst = reinterpret_cast<DT *>(a.out) + (int64_t)o.row * p.d + o.at;
                     constexpr int VEC = 16 / (int)sizeof(DT), DEEP = TILE / VEC / GROUP, TURN = 4;
-                    if (o.len == TILE && in.end == TILE && (reinterpret_cast<uintptr_t>(dst) & 15u) == 0 && !rf.clear) {
+                    if (o.len == TILE && in.end == TILE && in.shift == 0 && (reinterpret_cast<uintptr_t>(dst) & 15u) == 0 && !rf.clear) {
 #pragma unroll 1
                         for (int j0 = 0; j0 < DEEP; j0 += TURN) {
                             Raw<ST, VEC> raw[TURN];
@@ -719,7 +724,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
                             }
                         }
                     } else {
-                        scale_ragged<ST, DT>(src, buf, o.len, dst, rf);
+                        scale_ragged<ST, DT>(src, buf, o.len, o.open, dst, rf);
                     }
                 }
                 group_sync(g);
