@@ -16,26 +16,24 @@ __device__ __forceinline__ void store_grad(void *base, int64_t at, int grad_dtyp
 // CTAs over groups shares.  With a.direct a group is one CTA's and the sums are the gradient.
 // With xc = x - m and g = dy r:  dx = g w - mean(g w) - xc r^2 mean(g w xc),  dw += g xc  (nine operations
 // per element instead of the ten of xh and q).
-template <typename T, bool WHOLE, bool WIDE, int NV, int TPR, int SLOTS, int MINB, int R>
+template <typename T, bool WHOLE, bool WIDE, int NV, int TPR, int SLOTS, int MINB>
 __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __grid_constant__ LnBackward a) {
-    using S = LnShape<T, WHOLE, NV, TPR, SLOTS, MINB, R, 2>;
+    using S = LnShape<T, WHOLE, NV, TPR, SLOTS, MINB, 1, 2>;
     constexpr int VEC = S::VEC, P = VEC / 2;
+    constexpr bool KEEP = S::KEEP;   // x - m and g w stay in registers while the sums meet
     extern __shared__ __align__(16) char ln_ring[];
-    __shared__ __align__(16) float box[2][SLOTS][S::WARPS][2 * R];
+    __shared__ __align__(16) float box[2][SLOTS][S::WARPS][2];
+    __shared__ float2 meet_rows[2][1][8];
     const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
-    __shared__ float2 meet_rows[2][R][8];
     // WIDE: this CTA's columns of the cluster's rows
     const int rank = WIDE ? cluster_rank() : 0, parts = WIDE ? cluster_size() : 1, c0 = WIDE ? rank * a.part_cols : 0;
     const int64_t cta = WIDE ? blockIdx.x / parts : blockIdx.x;
     const int h = WIDE ? min(a.part_cols, a.cols - c0) : a.cols;
     const float inv_h = 1.0f / (float)a.cols;
     if constexpr (WIDE) cluster_sync();   // (all have started: their shared memory may be written)
-    LnPipe<T, S, WHOLE, NV, TPR> px[R], pd[R];
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-        px[j].place(ln_ring, slot * R + j);
-        pd[j].place(ln_ring, (SLOTS + slot) * R + j);
-    }
+    LnPipe<T, S, WHOLE, NV, TPR> px, pd;
+    px.place(ln_ring, slot);
+    pd.place(ln_ring, SLOTS + slot);
     int flip = 0;
     const int64_t total = (int64_t)a.groups * a.rows;
     const int64_t u_end = min(total, a.share.first(cta + 1));
@@ -44,55 +42,46 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
         const int64_t r0 = u - (int64_t)group * a.rows;
         const int count = (int)(min(a.rows, r0 + (u_end - u)) - r0);    // rows of this group
         u += count;
-        const int turns = (count + SLOTS * R - 1) / (SLOTS * R);
-        const T *x_next = reinterpret_cast<const T *>(a.x) + group * a.x_group + (r0 + slot * R) * a.x_row + c0;       // the next row to fetch
-        const T *dy_next = reinterpret_cast<const T *>(a.dy) + group * a.dy_group + (r0 + slot * R) * a.dy_row + c0;
-        T *dx = reinterpret_cast<T *>(a.dx) + group * a.dx_group + (r0 + slot * R) * a.dx_row + c0;
-        const int64_t x_step = (int64_t)SLOTS * R * a.x_row, dy_step = (int64_t)SLOTS * R * a.dy_row, dx_step = (int64_t)SLOTS * R * a.dx_row;
-        const float *mean_at = a.mean + (int64_t)group * a.rows + r0 + slot * R, *rstd_at = a.rstd + (int64_t)group * a.rows + r0 + slot * R;
+        const int turns = (count + SLOTS - 1) / SLOTS;
+        const T *x_next = reinterpret_cast<const T *>(a.x) + group * a.x_group + (r0 + slot) * a.x_row + c0;       // the next row to fetch
+        const T *dy_next = reinterpret_cast<const T *>(a.dy) + group * a.dy_group + (r0 + slot) * a.dy_row + c0;
+        T *dx = reinterpret_cast<T *>(a.dx) + group * a.dx_group + (r0 + slot) * a.dx_row + c0;
+        const int64_t x_step = (int64_t)SLOTS * a.x_row, dy_step = (int64_t)SLOTS * a.dy_row, dx_step = (int64_t)SLOTS * a.dx_row;
+        const float *mean_at = a.mean + (int64_t)group * a.rows + r0 + slot, *rstd_at = a.rstd + (int64_t)group * a.rows + r0 + slot;
         if (h != S::COLS) {   // (at every group: the column sums of the last one lay here)
             ln_clear_tails<S, WHOLE>(ln_ring, h * (int)sizeof(T));
             __syncthreads();
         }
-        auto row_of = [&](int turn, int j) { return (turn * SLOTS + slot) * R + j; };
-        auto fetch = [&](int turn, int stage, LnHead (&head)[2 * R]) {
-#pragma unroll
-            for (int j = 0; j < R; ++j) {
-                head[2 * j].to = head[2 * j + 1].to = 0u;
-                if (row_of(turn, j) < count) {
-                    px[j].fetch(x_next + j * a.x_row, t, h, stage, head[2 * j]);
-                    pd[j].fetch(dy_next + j * a.dy_row, t, h, stage, head[2 * j + 1]);
-                }
+        struct Heads { LnHead x, dy; };
+        auto fetch = [&](int turn, int stage, Heads &head) {
+            head.x.to = head.dy.to = 0u;
+            if (turn * SLOTS + slot < count) {
+                px.fetch(x_next, t, h, stage, head.x);
+                pd.fetch(dy_next, t, h, stage, head.dy);
             }
             x_next += x_step;
             dy_next += dy_step;
             copy_commit();
         };
-        auto land = [&](const LnHead (&head)[2 * R]) {
-#pragma unroll
-            for (int j = 0; j < 2 * R; ++j) px[0].land(head[j]);
+        auto land = [&](const Heads &head) {
+            px.land(head.x);
+            px.land(head.dy);
         };
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            px[j].now = (uint32_t)reinterpret_cast<uintptr_t>(x_next + j * a.x_row);
-            pd[j].now = (uint32_t)reinterpret_cast<uintptr_t>(dy_next + j * a.dy_row);
-        }
-        LnHead head[S::STAGES - 1][2 * R];
+        px.now = (uint32_t)reinterpret_cast<uintptr_t>(x_next);
+        pd.now = (uint32_t)reinterpret_cast<uintptr_t>(dy_next);
+        Heads head[S::STAGES - 1];
 #pragma unroll
         for (int s = 0; s < S::STAGES - 1; ++s) fetch(s, s, head[s]);
 #pragma unroll
         for (int s = 0; s < S::STAGES - 2; ++s) land(head[s]);
-        LnHead (&last)[2 * R] = head[S::STAGES - 2];   // of the turn fetched last
-        float mean_next[R], rstd_next[R];   // of rows that do not exist: zeros, which add nothing
+        Heads &last = head[S::STAGES - 2];   // of the turn fetched last
+        float mean_next, rstd_next;
         auto statistics = [&](int turn) {
-#pragma unroll
-            for (int j = 0; j < R; ++j) {
-                const bool live = row_of(turn, j) < count;
-                mean_next[j] = live ? __ldg(mean_at + j) : 0.0f;
-                rstd_next[j] = live ? __ldg(rstd_at + j) : 0.0f;
-            }
-            mean_at += SLOTS * R;
-            rstd_at += SLOTS * R;
+            const bool live = turn * SLOTS + slot < count;
+            mean_next = live ? __ldg(mean_at) : 0.0f;
+            rstd_next = live ? __ldg(rstd_at) : 0.0f;
+            mean_at += SLOTS;
+            rstd_at += SLOTS;
         };
         statistics(0);
         F2 w[NV][P], gw[NV][P], gb[NV][P];
@@ -105,6 +94,7 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
         for (int i = 0, stage = 0; i < turns; ++i) {
             const int ahead = i + S::STAGES - 1;                               // turn to fetch now
             const int into = stage == 0 ? S::STAGES - 1 : stage - 1;
+            const bool live = i * SLOTS + slot < count;
             if constexpr (WHOLE) {
                 fetch(ahead, into, last);
                 copy_wait<S::STAGES - 1>();
@@ -114,73 +104,67 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
                 slot_sync<TPR>(slot);      // the rows of turn i are complete, and all are done with turn i - 1
                 fetch(ahead, into, last);
             }
-            float rstd[R], along[R], level[R];
-            F2 minus[R];
-#pragma unroll
-            for (int j = 0; j < R; ++j) {
-                minus[j] = f2(-mean_next[j]);
-                rstd[j] = rstd_next[j];
-            }
+            const float rstd = rstd_next;
+            const F2 minus = f2(-mean_next), scale = f2(rstd);
             statistics(i + 1);
-            F2 xc[R][NV][P], q[R][NV][P];
+            F2 along2 = f2(0.0f), level2 = f2(0.0f);
+            F2 kept_x[KEEP ? NV : 1][P], kept_q[KEEP ? NV : 1][P];
+            if (live) {   // (zeros beyond column h add nothing to any sum)
 #pragma unroll
-            for (int j = 0; j < R; ++j) {
-                F2 along2 = f2(0.0f), level2 = f2(0.0f);
-                if (row_of(i, j) < count) {   // (zeros beyond column h add nothing to any sum)
-                    const F2 scale = f2(rstd[j]);
+                for (int v = 0; v < NV; ++v) {
+                    F2 dy[P], (&xc)[P] = kept_x[KEEP ? v : 0], (&q)[P] = kept_q[KEEP ? v : 0];
+                    px.read(v, t, stage, xc);
+                    pd.read(v, t, stage, dy);
 #pragma unroll
-                    for (int v = 0; v < NV; ++v) {
-                        F2 dy[P];
-                        px[j].read(v, t, stage, xc[j][v]);
-                        pd[j].read(v, t, stage, dy);
-#pragma unroll
-                        for (int k = 0; k < P; ++k) {
-                            xc[j][v][k] = add(xc[j][v][k], minus[j]);
-                            const F2 g = mul(dy[k], scale);
-                            q[j][v][k] = mul(g, w[v][k]);
-                            along2 = fma(q[j][v][k], xc[j][v][k], along2);
-                            level2 = add(level2, q[j][v][k]);
-                            gw[v][k] = fma(g, xc[j][v][k], gw[v][k]);
-                            gb[v][k] = add(gb[v][k], dy[k]);
-                        }
+                    for (int k = 0; k < P; ++k) {
+                        xc[k] = add(xc[k], minus);
+                        const F2 g = mul(dy[k], scale);
+                        q[k] = mul(g, w[v][k]);
+                        along2 = fma(q[k], xc[k], along2);
+                        level2 = add(level2, q[k]);
+                        gw[v][k] = fma(g, xc[k], gw[v][k]);
+                        gb[v][k] = add(gb[v][k], dy[k]);
                     }
                 }
-                along[j] = lo(along2) + hi(along2);
-                level[j] = lo(level2) + hi(level2);
             }
             if (a.dx) {
-                slot_sums<TPR, S::WARPS, R>(along, level, t, slot, box[flip]);
-                if constexpr (WIDE) cluster_sums<R>(along, level, rank, parts, meet_rows[flip]);
+                float along[1] = {lo(along2) + hi(along2)}, level[1] = {lo(level2) + hi(level2)};
+                slot_sums<TPR, S::WARPS, 1>(along, level, t, slot, box[flip]);
+                if constexpr (WIDE) cluster_sums<1>(along, level, rank, parts, meet_rows[flip]);
                 flip ^= 1;
-                if constexpr (!WHOLE && S::WARPS == 1) __syncwarp();   // all have read the rows, whose place the results take
+                // !WHOLE: a finished row on its way out, in the place of its x once all have read that
+                char *const result = KEEP ? px.ring + stage * S::STAGE_BYTES : ln_ring + S::RING_BYTES + slot * S::ROW_BYTES;
+                if constexpr (!WHOLE && KEEP && S::WARPS == 1) __syncwarp();
+                const F2 tilt = f2(-(along[0] * inv_h * rstd) * rstd), shift = f2(-level[0] * inv_h);
+                if (live) {
 #pragma unroll
-                for (int j = 0; j < R; ++j) {
-                    const F2 tilt = f2(-(along[j] * inv_h * rstd[j]) * rstd[j]), shift = f2(-level[j] * inv_h);
-                    if (row_of(i, j) < count) {
-                        T *dxj = dx + j * a.dx_row;
-#pragma unroll
-                        for (int v = 0; v < NV; ++v) {
-                            const int c = (v * TPR + t) * VEC;
-#pragma unroll
-                            for (int k = 0; k < P; ++k) q[j][v][k] = fma(xc[j][v][k], tilt, add(q[j][v][k], shift));
-                            if (c < h) LnChunk<T>::write(WHOLE ? reinterpret_cast<char *>(dxj + c) : px[j].result(v, t, stage), q[j][v]);
+                    for (int v = 0; v < NV; ++v) {
+                        const int c = (v * TPR + t) * VEC;
+                        F2 (&xc)[P] = kept_x[KEEP ? v : 0], (&q)[P] = kept_q[KEEP ? v : 0];
+                        if constexpr (!KEEP) {
+                            px.read(v, t, stage, xc);
+                            pd.read(v, t, stage, q);
                         }
+#pragma unroll
+                        for (int k = 0; k < P; ++k) {
+                            if constexpr (!KEEP) {
+                                xc[k] = add(xc[k], minus);
+                                q[k] = rounded_mul(mul(q[k], scale), w[v][k]);
+                            }
+                            q[k] = fma(xc[k], tilt, add(q[k], shift));
+                        }
+                        if (c < h) LnChunk<T>::write(WHOLE ? reinterpret_cast<char *>(dx + c) : result + 16 + (v * TPR + t) * 16, q);
                     }
                 }
                 if constexpr (!WHOLE) {
                     slot_sync<TPR>(slot);
-#pragma unroll
-                    for (int j = 0; j < R; ++j)
-                        if (row_of(i, j) < count) ln_store_row<T, NV, TPR>(dx + j * a.dx_row, px[j].ring + stage * S::STAGE_BYTES, t, h);
+                    if (live) ln_store_row<T, NV, TPR>(dx, result, t, h);
                 }
                 dx += dx_step;
             }
             if constexpr (!WHOLE) {
-#pragma unroll
-                for (int j = 0; j < R; ++j) {
-                    px[j].now += (uint32_t)x_step * (uint32_t)sizeof(T);
-                    pd[j].now += (uint32_t)dy_step * (uint32_t)sizeof(T);
-                }
+                px.now += (uint32_t)x_step * (uint32_t)sizeof(T);
+                pd.now += (uint32_t)dy_step * (uint32_t)sizeof(T);
             }
             stage = stage + 1 == S::STAGES ? 0 : stage + 1;
         }
@@ -295,10 +279,6 @@ __global__ void __launch_bounds__(256) ln_backward_join_kernel(const __grid_cons
     }
 }
 
-// Rows per turn and slot.  Two rows at once (half the exchanges, twice the registers) measured slower: at
-// 4 x 4096 rows of 4096 bfloat16 columns 95 against 83 us.
-constexpr int LN_BACKWARD_TURN = 1;
-
 struct LnPlan {
     LnShare share;
     int64_t pieces;
@@ -311,7 +291,6 @@ struct LnPlanner {
     int parts;
     template <int TPR, int E, int SLOTS, int MINB>
     LnPlan operator()() const {
-        constexpr int R = LN_BACKWARD_TURN;
         const int64_t total = (int64_t)groups * rows;
         const int resident = ln_resident(MINB, parts);
         LnPlan p;
@@ -319,8 +298,8 @@ struct LnPlanner {
         // (4 rows of 8192 binary32 columns, eight groups: 13.6 us, 15.8 us shared and joined; one group 13.5 and
         // 10.2 us; 16 rows of 768: 6.8 and 5.1 us, 32 rows 9.3 and 5.1 us); or with so many groups that their CTAs
         // fill the GPU several times over anyway
-        p.direct = rows <= 4 * SLOTS * R || (groups >= 4 * resident && rows <= (int64_t)SLOTS * LN_SUM_ROWS);
-        p.share = p.direct ? LnShare{0, 0, rows, groups} : ln_share(total, SLOTS * R, resident, LN_SUM_ROWS / R, false);
+        p.direct = rows <= 4 * SLOTS || (groups >= 4 * resident && rows <= (int64_t)SLOTS * LN_SUM_ROWS);
+        p.share = p.direct ? LnShare{0, 0, rows, groups} : ln_share(total, SLOTS, resident, LN_SUM_ROWS, false);
         p.pieces = p.direct ? 0 : p.share.ctas + groups;
         return p;
     }
@@ -343,14 +322,14 @@ struct LnBackwardLaunch {
     template <int TPR, int E, int SLOTS, int MINB>
     cudaError_t operator()() {
         constexpr int NV = E / LnChunk<T>::VEC;
-        constexpr int R = LN_BACKWARD_TURN;
-        using S = LnShape<T, WHOLE, NV, TPR, SLOTS, MINB, R, 2>;
+        using S = LnShape<T, WHOLE, NV, TPR, SLOTS, MINB, 1, 2>;
         static_assert(S::THREADS <= 32 || S::RING_BYTES >= S::THREADS * S::E * 4, "half the CTA's column sums meet in the ring");
         static std::atomic<uint64_t> allowed{0};
-        const auto kernel = ln_backward_kernel<T, WHOLE, WIDE, NV, TPR, SLOTS, MINB, R>;
-        const cudaError_t e = ln_allow_smem(kernel, S::RING_BYTES, allowed);
+        const auto kernel = ln_backward_kernel<T, WHOLE, WIDE, NV, TPR, SLOTS, MINB>;
+        constexpr int SMEM = S::RING_BYTES + S::RESULT_BYTES;
+        const cudaError_t e = ln_allow_smem(kernel, SMEM, allowed);
         if (e != cudaSuccess) return e;
-        return ln_launch(kernel, a, a.share.ctas, WIDE ? ln_parts(a.cols) : 1, S::THREADS, S::RING_BYTES, st);
+        return ln_launch(kernel, a, a.share.ctas, WIDE ? ln_parts(a.cols) : 1, S::THREADS, SMEM, st);
     }
 };
 

@@ -51,6 +51,9 @@ __device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
     return r;
 }
+// A product that is rounded before anything is added to it: a packed mul and the packed add behind it come out as
+// one fused operation although both name their rounding (seen as a residue where q - q had to be zero).
+__device__ __forceinline__ F2 rounded_mul(F2 a, F2 b) { return f2(__fmul_rn(lo(a), lo(b)), __fmul_rn(hi(a), hi(b))); }
 
 // ---- a chunk as pairs ----
 template <typename T> struct LnChunk;
@@ -188,7 +191,12 @@ struct LnShape {
     static constexpr int STAGE_BYTES = ARRAYS * SLOTS * R * ROW_BYTES;   // a stage holds the R rows of a turn, for every slot
     // About 40 KB per SM have to be in flight to cover HBM's latency at its bandwidth: 2 to 6 stages
     // give that for every shape within the 200 KB that the MINB CTAs of an SM share.
-    static constexpr int FIT = 200 * 1024 / MINB / STAGE_BYTES;
+    // The backward pass either keeps what the rows gave in registers while their sums meet, or reads the rows once
+    // more: bfloat16 would have to be widened twice (4 x 4096 rows of 4096: 80 us kept, 89 us read again; binary32,
+    // 4 x 8192 rows of 2048: 141 and 139 us, 16 x 8192 of 511: 156 and 145 us).  Results then need a place of their own.
+    static constexpr bool KEEP = ARRAYS == 1 || sizeof(T) == 2;
+    static constexpr int RESULT_BYTES = WHOLE || KEEP ? 0 : SLOTS * R * ROW_BYTES;
+    static constexpr int FIT = (200 * 1024 / MINB - RESULT_BYTES) / STAGE_BYTES;
     static constexpr int STAGES = FIT < 2 ? 2 : FIT > 6 ? 6 : FIT;
     static constexpr int RING_BYTES = STAGES * STAGE_BYTES;
     static constexpr int WARPS = TPR < 32 ? 1 : TPR / 32;      // warps per slot
