@@ -299,9 +299,9 @@ liec_status liec_gather_grads(liec_ctx *ctx, void *out, float max_norm, int32_t 
  *   m = mean(x),  r = 1 / sqrt(mean((x - m)^2) + eps),  y = (x - m) r w + b
  *   xh = (x - m) r,  dx = r (dy w - mean(dy w) - xh mean(dy w xh)),
  *   dw = sum over the worker's rows of dy xh,  db = sum over the worker's rows of dy
- * Evaluated in binary32, the variance around the mean; outputs are rounded once to their type.  The
- * order of the sums depends on the sizes and the GPU's SM count alone (no atomics): equal calls give
- * equal bits.  A row with an infinity or NaN gives NaN in that row (and in dw, db) only.
+ * Evaluated in binary32; outputs are rounded once to their type.  The variance is mean(x^2) - m^2 where
+ * m^2 is at most a quarter of it, and summed around the mean in all other rows.  The order of the sums
+ * depends on the sizes alone, not on strides or alignment (no atomics): equal calls give equal bits.  A row with an infinity or NaN gives NaN in that row (and in dw) only.
  *
  * No context is needed.  All strides are in elements and >= 0; the last axis is contiguous.  Rows that
  * are read may overlap or repeat (stride 0); rows that are written may not.  Any element alignment is
@@ -397,7 +397,8 @@ liec_status liec_get_messages(const liec_ctx *ctx, liec_messages *out);
  * internal check that failed (1 selection rank, 2 candidate buffer, 4 output count, 8 a bulk
  * copy into shared memory that did not complete within its bounded wait; the kernel that saw it
  * returned without touching its outputs; 16 a random-k subset entry outside its segment or out of
- * order).  Returns LIEC_ERR_DEVICE_CHECK when non-zero.
+ * order; 32 a row's norm or another part of the clipping did not come within its bounded wait: the
+ * rows and norms of that call are unspecified).  Returns LIEC_ERR_DEVICE_CHECK when non-zero.
  */
 liec_status liec_device_status(liec_ctx *ctx, void *stream, int32_t *out);
 

@@ -356,7 +356,10 @@ inline LnShare ln_share(int64_t total, int turn_rows, int resident, int64_t max_
 inline int ln_resident(int minb, int parts) { return parts == 1 ? LN_SMS * minb : (parts == 2 ? 1 : 4) * LN_SMS / parts; }
 
 // Threads per row, elements per thread, slots per CTA and CTAs per SM for h columns:
-// f.template operator()<TPR, E, SLOTS, MINB>().
+// f.template operator()<TPR, E, SLOTS, MINB>().  Up to 1024 columns a warp or less takes a row: its sums meet
+// by shuffles alone, without a barrier between warps, and 24 or 32 elements per thread are still faster than two
+// warps per row; beyond, 16 elements per thread, the most with which two rows (forward) or a row and its column
+// sums (backward) fit the registers of two CTAs of 256 threads.
 template <typename F>
 auto ln_forward_shape(int h, F &&f) {
     if (h <= 64) return f.template operator()<8, 8, 32, 3>();
