@@ -27,10 +27,6 @@
 
 namespace liec {
 
-__device__ __forceinline__ float ln_load(const float *p) { return __ldg(p); }
-__device__ __forceinline__ float ln_load(const __nv_bfloat16 *p) {
-    return __uint_as_float((uint32_t)__ldg(reinterpret_cast<const unsigned short *>(p)) << 16);
-}
 __device__ __forceinline__ void ln_store(float *p, float v) { *p = v; }
 __device__ __forceinline__ void ln_store(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
