@@ -17,6 +17,7 @@
 #include <climits>
 #include <cmath>
 
+#include "balanced_join.h"
 #include "device_common.cuh"
 #include "granule.cuh"
 #include "kernels.h"
@@ -254,7 +255,9 @@ __global__ void __launch_bounds__(CLUSTER_TILES / CLUSTER_SIZE * THREADS) clip_c
 // waits only for ops with earlier tickets, which never wait for it, so the CTAs need not all be resident.
 constexpr int GROUPS = 6, GROUP = 128, OP_SLOTS = 32;   // (one slot per producer lane)
 constexpr int STREAM_THREADS = GROUPS * GROUP + 32;
-constexpr int ROW_PASSES = 160;   // passes of row_tree: 2^32 / TILE + 65535 tiles at most, 4096 per pass
+constexpr int PASS_TILES = 8 * GROUP * 4;   // tile sums that row_tree takes in one pass
+constexpr int ROW_PASSES = 160;
+static_assert((int64_t)ROW_PASSES * PASS_TILES >= (int64_t(1) << 32) / TILE + 65535, "passes for the most tiles: dim below 2^32, at most 65535 segments");
 constexpr unsigned STATUS_NORM_TIMEOUT = 32;   // bit of the status word: a row's norm did not arrive within the wait limit
 constexpr unsigned NORM_WAIT_LIMIT = 1u << 21;   // polls of 40 ns and a load
 constexpr unsigned OP_WAIT_LIMIT = 1u << 21;     // polls of 200 ns of the producer for ops to be worked off
@@ -372,13 +375,13 @@ __device__ __forceinline__ double group_tree(double warp_sum, double *warp_sums,
 __device__ __noinline__ double row_tree(const double *src, int tiles, double *warp_sums /*[4]*/, double *pass_sums /*[ROW_PASSES]*/,
                                            int g, const volatile int *stop, bool &missing) {
     const int t = threadIdx.x % GROUP, warp = t / 32, lane = t & 31;
-    const int passes = (tiles + 8 * GROUP * 4 - 1) / (8 * GROUP * 4);
+    const int passes = (tiles + PASS_TILES - 1) / PASS_TILES;
     missing = false;
     for (int q = 0; q < passes; ++q) {
         double part[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int first = q * 4096 + warp * 1024 + half * 512 + lane * 2;
+            const int first = q * PASS_TILES + warp * 1024 + half * 512 + lane * 2;
             unsigned long long v[8][2];
             for (unsigned tries = 0;; ++tries) {   // all sixteen again until they are there
                 bool unset = false;
@@ -402,13 +405,7 @@ __device__ __noinline__ double row_tree(const double *src, int tiles, double *wa
         group_sync(g);
     }
     missing = group_any(g, missing);
-    if (t != 0) return 0.0;
-    int span = 1;
-    while (span < passes) span <<= 1;
-    for (int q = passes; q < span; ++q) pass_sums[q] = 0.0;
-    for (int w = span / 2; w >= 1; w >>= 1)
-        for (int k = 0; k < w; ++k) pass_sums[k] = __dadd_rn(pass_sums[2 * k], pass_sums[2 * k + 1]);
-    return pass_sums[0];
+    return t == 0 ? balanced_join(pass_sums, passes) : 0.0;
 }
 
 // The two ops on tiles that are not whole or not aligned.  (These and row_tree are functions of their own:
