@@ -370,6 +370,8 @@ def liec_layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, dweight=No
     for name, t in (("mean", mean), ("rstd", rstd)):
         if t.dtype != torch.float32 or t.shape != rows or not t.is_contiguous() or t.get_device() != device:
             raise ValueError(f"{name} must be the contiguous float32 tensor that the forward pass returned")
+    if workspace is not None and not workspace.is_contiguous():   # (its bytes are counted by its elements)
+        raise ValueError("workspace must be contiguous")
     return _launch(device, stream, _ln_backward, device, dy, x, mean, rstd, weight, dx, dweight, dbias, workspace)
 
 
