@@ -286,7 +286,11 @@ liec_status liec_clip_grads(liec_ctx *ctx, const void *grads, void *out, float m
  * liec_set_tensors copies the pointers (as kernel arguments: no synchronisation, and it can be
  * captured), ordered on `stream`; the tensors themselves are read by liec_gather_grads and must not
  * overlap `out`.  The table serves any number of liec_gather_grads calls until the next
- * liec_set_tensors.  liec_gather_grads returns LIEC_ERR_STATE when no table was given.
+ * liec_set_tensors.  liec_gather_grads returns LIEC_ERR_STATE when no table was given.  A captured
+ * liec_set_tensors writes the table whenever its graph is replayed (its tensors then have to be there still).  Where the
+ * table on the device is not of the type of the last liec_set_tensors call (a graph that writes it was not
+ * replayed yet, or was replayed after a call for the other type), liec_gather_grads reads no tensor: bit 64 of
+ * the status word is set and the rows are zeros.
  */
 liec_status liec_set_tensors(liec_ctx *ctx, const void *const *tensors, int32_t dtype, void *stream);
 liec_status liec_gather_grads(liec_ctx *ctx, void *out, float max_norm, int32_t zero_nonfinite, float *norms,
@@ -398,7 +402,8 @@ liec_status liec_get_messages(const liec_ctx *ctx, liec_messages *out);
  * copy into shared memory that did not complete within its bounded wait; the kernel that saw it
  * returned without touching its outputs; 16 a random-k subset entry outside its segment or out of
  * order; 32 a row's norm or another part of the clipping did not come within its bounded wait: the
- * rows and norms of that call are unspecified).  Returns LIEC_ERR_DEVICE_CHECK when non-zero.
+ * rows and norms of that call are unspecified; 64 liec_gather_grads found no table of the type that
+ * liec_set_tensors was last called for: its rows are zeros).  Returns LIEC_ERR_DEVICE_CHECK when non-zero.
  */
 liec_status liec_device_status(liec_ctx *ctx, void *stream, int32_t *out);
 

@@ -187,6 +187,15 @@ __device__ __forceinline__ RowFactor row_factor(const ClipArgs &a, double sumsq,
     return f;
 }
 
+// Whether the table holds tensors of the kernel's source type.  If not (see TABLE_F32), no tensor is read: all count
+// as missing, and the status word says so.
+constexpr unsigned STATUS_TENSOR_TABLE = 64;
+template <typename ST>
+__device__ __forceinline__ bool table_fits(const Params &p, const ClipArgs &a) {
+    const void *const *behind = a.table + (int64_t)p.N * p.T;
+    return __ldg(reinterpret_cast<const unsigned long long *>(behind)) == (sizeof(ST) == 4 ? TABLE_F32 : TABLE_BF16);
+}
+
 // ---- rows of at most CLUSTER_TILES tiles: one cluster per row -------------------------------------
 //
 // 256 threads take a tile, up to four tiles a CTA, up to eight CTAs the cluster.  Every tile sum goes to all of
@@ -216,7 +225,10 @@ __global__ void __launch_bounds__(CLUSTER_TILES / CLUSTER_SIZE * THREADS) clip_c
         if (a.table) {
             const int seg = __ldg(p.tile_seg + tile);
             const ST *tensor = reinterpret_cast<const ST *>(__ldg(reinterpret_cast<const unsigned long long *>(a.table) + (int64_t)row * p.T + seg));
-            if (tensor) src = tensor + (at - __ldg(p.seg_off + seg));
+            const int64_t tensor_at = __ldg(p.seg_off + seg);
+            const bool fits = table_fits<ST>(p, a);
+            if (tensor && fits) src = tensor + (at - tensor_at);
+            if (!fits && tile == 0 && t == 0) atomicOr(p.status, STATUS_TENSOR_TABLE);
         } else {
             src = reinterpret_cast<const ST *>(a.rows) + (int64_t)row * p.d + at;
         }
@@ -504,8 +516,10 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
             }
             return l;
         };
+        const bool fits = !a.table || table_fits<ST>(p, a);
+        if (!fits && lane == 0) atomicOr(p.status, STATUS_TENSOR_TABLE);
         auto source = [&](const Look &l) -> const ST * {
-            if (a.table) return l.tensor ? l.tensor + (l.at - l.tensor_at) : nullptr;
+            if (a.table) return l.tensor && fits ? l.tensor + (l.at - l.tensor_at) : nullptr;
             return reinterpret_cast<const ST *>(a.rows) + (int64_t)l.row * p.d + l.at;
         };
         // (the rows as a whole begin on 16 bytes; a tile that does not begin its tensor has 8192 elements before it)
@@ -742,26 +756,29 @@ template <int CAP>
 struct PointerBlock { const void *ptr[CAP]; };
 
 template <int CAP>
-__global__ void upload_pointers_kernel(const __grid_constant__ PointerBlock<CAP> block, const void **table, int count) {
+__global__ void upload_pointers_kernel(const __grid_constant__ PointerBlock<CAP> block, const void **table, int count, unsigned long long *word, unsigned long long tag) {
     for (int q = threadIdx.x; q < count; q += blockDim.x) table[q] = block.ptr[q];
+    if (threadIdx.x == 0) *word = tag;
 }
 
 template <int CAP>
-static cudaError_t upload_block(const void *const *tensors, const void **table, int count, cudaStream_t st) {
+static cudaError_t upload_block(const void *const *tensors, const void **table, int count, unsigned long long *word, unsigned long long tag, cudaStream_t st) {
     PointerBlock<CAP> block;
     for (int q = 0; q < count; ++q) block.ptr[q] = tensors[q];
-    upload_pointers_kernel<CAP><<<1, THREADS, 0, st>>>(block, table, count);
+    upload_pointers_kernel<CAP><<<1, THREADS, 0, st>>>(block, table, count, word, tag);
     return cudaGetLastError();
 }
 
 // Arguments of up to 4 KB are the cheap kind; longer tables go in blocks of 31 KB, near the 32,764-byte limit.
-cudaError_t launch_upload_pointers(const void *const *tensors, const void **table, int64_t count, cudaStream_t st, int64_t *launches) {
+cudaError_t launch_upload_pointers(const void *const *tensors, int dtype, const void **table, int64_t count, cudaStream_t st, int64_t *launches) {
     constexpr int SMALL = 480, LARGE = 3968;
+    unsigned long long *word = reinterpret_cast<unsigned long long *>(table + count);
     for (int64_t at = 0; at < count;) {
         const int64_t left = count - at;
         const int here = (int)(left < LARGE ? left : LARGE);
-        const cudaError_t e = here <= SMALL ? upload_block<SMALL>(tensors + at, table + at, here, st)
-                                            : upload_block<LARGE>(tensors + at, table + at, here, st);
+        const unsigned long long tag = at + here < count ? 0ull : dtype == DT_F32 ? TABLE_F32 : TABLE_BF16;   // (a table that is only half written is none)
+        const cudaError_t e = here <= SMALL ? upload_block<SMALL>(tensors + at, table + at, here, word, tag, st)
+                                            : upload_block<LARGE>(tensors + at, table + at, here, word, tag, st);
         if (e != cudaSuccess) return e;
         ++*launches;
         at += here;

@@ -35,7 +35,8 @@ cudaError_t launch_sum_finalize(const Params &p, const double *partials, int row
 // norm of every worker's gradient and clipping
 struct ClipArgs {
     const void *rows;          // [N][d] of src_dtype, used when table is NULL
-    const void *const *table;  // device, [N][T] pointers to the tensors (NULL entry: zeros), or NULL
+    const void *const *table;  // device, [N][T] pointers to the tensors (NULL entry: zeros) and a word that says of
+                               // what type they are (TABLE_F32, TABLE_BF16), or NULL
     void *out;                 // [N][d] of the context's gradient type
     float *norms;              // [N] or NULL
     // for rows that go through the streaming kernel, one block of CLIP_STREAM_BYTES:
@@ -49,10 +50,13 @@ struct ClipArgs {
     int32_t norms_only;            // nothing to write
     int32_t batch;                 // tiles per ticket
 };
+// The word behind a table: 0 while there is none.  The host's knowledge of the type is not enough: a replayed graph
+// writes the table again without the host, and a captured call has not written it yet.
+constexpr unsigned long long TABLE_F32 = DT_F32 + 1, TABLE_BF16 = DT_BF16 + 1;
 constexpr size_t CLIP_STREAM_BYTES(size_t N, size_t TT) { return 8 * (N * TT + N + 3); }
 cudaError_t configure_clip_kernels();  // opt-in shared memory sizes; call once per device
 cudaError_t launch_clip(const Params &p, const ClipArgs &a, cudaStream_t st, int64_t *launches);
-cudaError_t launch_upload_pointers(const void *const *tensors, const void **table, int64_t count, cudaStream_t st, int64_t *launches);
+cudaError_t launch_upload_pointers(const void *const *tensors, int dtype, const void **table, int64_t count, cudaStream_t st, int64_t *launches);
 
 // worker update
 cudaError_t launch_worker_update(const Params &p, float lr, cudaStream_t st);

@@ -181,7 +181,7 @@ liec_status make_plan(const liec_config *cfg, Plan &pl, std::string *msg) {
     pl.r_ktile_seg = c.take(sizeof(int32_t) * pl.KTT);
     pl.r_tel_kept = c.take(sizeof(double) * (size_t)pl.N * pl.KTT);
     const size_t N = pl.N;
-    pl.r_tensor_table = c.take(sizeof(void *) * N * T);
+    pl.r_tensor_table = c.take(sizeof(void *) * (N * T + 1));
     pl.r_clip = c.take(CLIP_STREAM_BYTES(N, pl.TT));
     if (cfg->uplink == LIEC_COMP_SCALED_SIGN) {
         pl.r_up_words = c.take(sizeof(uint32_t) * N * pl.W);
@@ -481,9 +481,9 @@ liec_status liec_init(const liec_config *cfg, float *params, float *error, void 
             return LIEC_ERR_CUDA;
         }
     }
-    // status word and every selection scratch region start at zero
+    // status word, tensor table (none) and every selection scratch region start at zero
     auto zero = [&](const Region &r) { return r.bytes ? cudaMemset(c->ws + r.off, 0, r.bytes) : cudaSuccess; };
-    const Region *zs[] = {&pl.r_status, &pl.r_up_hist, &pl.r_down_hist, &pl.r_up_hist2, &pl.r_down_hist2,
+    const Region *zs[] = {&pl.r_status, &pl.r_tensor_table, &pl.r_up_hist, &pl.r_down_hist, &pl.r_up_hist2, &pl.r_down_hist2,
                           &pl.r_up_sel, &pl.r_down_sel, &pl.r_up_tile_meta, &pl.r_down_tile_meta,
                           &pl.r_up_outbase, &pl.r_down_outbase,
                           &pl.r_gen_hist, &pl.r_gen_hist2, &pl.r_gen_sel, &pl.r_gen_meta, &pl.r_gen_outbase};
@@ -760,7 +760,7 @@ liec_status liec_set_tensors(liec_ctx *c, const void *const *tensors, int32_t dt
     for (int64_t q = 0; q < count; ++q)
         if (reinterpret_cast<uintptr_t>(tensors[q]) & mask) { c->err = "a tensor is not aligned to its element size"; return LIEC_ERR_INVALID_ARG; }
     c->tensor_dtype = -1;   // (a table that is only half written is not used)
-    LIEC_CALL(c, launch_upload_pointers(tensors, at<const void *>(c, c->plan.r_tensor_table), count, static_cast<cudaStream_t>(stream), &c->launches));
+    LIEC_CALL(c, launch_upload_pointers(tensors, dtype, at<const void *>(c, c->plan.r_tensor_table), count, static_cast<cudaStream_t>(stream), &c->launches));
     c->tensor_dtype = dtype;
     return LIEC_OK;
 }

@@ -68,3 +68,42 @@ def test_norm_of_the_most_tiles():
     del ctx, G
     gc.collect()
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("tiles", [2, 40, 60])
+def test_table_that_is_not_there_yet_or_of_another_type(tiles):
+    """A captured liec_set_tensors has not written the table before its first replay, and a replay brings its own table
+    back: a gather that expects another type reads no tensor, says so, and the next right one is right."""
+    N, d = 2, tiles * TILE + 24
+    off = [0, 1000, d]
+    sets = {dt: [[torch.randint(-3, 4, (b - a,), device=DEV).to(dt) for a, b in zip(off, off[1:])] for _ in range(N)]
+            for dt in (torch.float32, torch.bfloat16)}
+    rows = {dt: torch.stack([torch.cat([t.float() for t in ts]) for ts in s]) for dt, s in sets.items()}
+    ctx = liec.Context(torch.zeros(N, d, device=DEV), torch.zeros(d, device=DEV), off, SIGN, SIGN)
+    out = torch.full((N, d), 7.0, device=DEV)
+
+    def refused():
+        out.fill_(7.0)
+        norms = ctx.liec_gather_grads(out)
+        assert ctx.liec_device_status() == 64 and (out == 0).all() and (norms == 0).all()
+        ctx.liec_clear_status()
+
+    def right(dt):
+        out.fill_(7.0)
+        norms = ctx.liec_gather_grads(out)
+        assert torch.equal(out, rows[dt])
+        assert torch.equal(norms, rows[dt].double().square().sum(1).sqrt().float())
+        assert ctx.liec_device_status() == 0
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.liec_set_tensors(sets[torch.bfloat16])
+    refused()                                   # not replayed yet
+    graph.replay()
+    right(torch.bfloat16)
+    ctx.liec_set_tensors(sets[torch.float32])
+    right(torch.float32)
+    graph.replay()                              # the bfloat16 table is back, the host expects binary32
+    refused()
+    ctx.liec_set_tensors(sets[torch.float32])
+    right(torch.float32)
