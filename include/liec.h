@@ -309,7 +309,9 @@ liec_status liec_gather_grads(liec_ctx *ctx, void *out, float max_norm, int32_t 
  *
  * No context is needed.  All strides are in elements and >= 0; the last axis is contiguous.  Rows that
  * are read may overlap or repeat (stride 0); rows that are written may not.  Any element alignment is
- * accepted; 16-byte aligned rows are faster.  Outputs must not overlap inputs.
+ * accepted; 16-byte aligned rows are faster.  Outputs must not overlap inputs or one another: LIEC_ERR_INVALID_ARG
+ * for y with x, dx with x or dy, and dweight with dbias, where their strides are equal (slices of one buffer) or one
+ * of the two is an array without gaps.
  */
 #define LIEC_LAYER_NORM_MAX_COLS 65536
 typedef struct {

@@ -13,6 +13,7 @@
 #include "../../include/liec.h"
 #include "kernels.h"
 #include "layer_norm.h"
+#include "overlap.h"
 #include "plan.h"
 #include "topk_common.cuh"
 
@@ -948,6 +949,10 @@ static bool ln_disjoint(const liec_layer_norm_desc *d, int64_t row, int64_t grou
     return (row >= h && group >= (d->rows - 1) * row + h) || (group >= h && row >= (d->groups - 1) * group + h);
 }
 
+static Rows ln_rows(const liec_layer_norm_desc *d, const void *base, int64_t row, int64_t group) {
+    return rows_of(base, d->rows, d->groups, row, group, d->cols, d->dtype == LIEC_BF16 ? 2 : 4);
+}
+
 static bool aligned_to(const void *ptr, int32_t dtype) { return (reinterpret_cast<uintptr_t>(ptr) & (dtype == LIEC_BF16 ? 1u : 3u)) == 0; }
 
 size_t liec_layer_norm_workspace_bytes(const liec_layer_norm_desc *d) {
@@ -965,6 +970,8 @@ liec_status liec_layer_norm_forward(const liec_layer_norm_desc *d, const void *x
         !aligned_to(mean, LIEC_F32) || !aligned_to(rstd, LIEC_F32))
         return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: a pointer is not aligned to its element size");
     if (!ln_disjoint(d, d->y_row_stride, d->y_group_stride)) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: the rows of y overlap");
+    if (overlap(ln_rows(d, y, d->y_row_stride, d->y_group_stride), ln_rows(d, x, d->x_row_stride, d->x_group_stride)))
+        return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: y overlaps x");
     LnForward a{};
     a.x = x; a.weight = weight; a.bias = bias; a.y = y; a.mean = mean; a.rstd = rstd;
     a.rows = d->rows; a.groups = d->groups; a.cols = d->cols; a.eps = d->eps;
@@ -993,6 +1000,16 @@ liec_status liec_layer_norm_backward(const liec_layer_norm_desc *d, const void *
     if ((dweight || dbias) && need > 0) {
         if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15u)) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: workspace must be non-NULL and 16-byte aligned");
         if (workspace_bytes < need) return ln_refuse(LIEC_ERR_WORKSPACE, "workspace smaller than liec_layer_norm_workspace_bytes()");
+    }
+    if (dx && d->rows > 0) {
+        const Rows out = ln_rows(d, dx, d->dx_row_stride, d->dx_group_stride);
+        if (overlap(out, ln_rows(d, x, d->x_row_stride, d->x_group_stride)) || overlap(out, ln_rows(d, dy, d->y_row_stride, d->y_group_stride)))
+            return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: dx overlaps x or dy");
+    }
+    if (dweight && dbias) {
+        const int size = d->grad_dtype == LIEC_BF16 ? 2 : 4;
+        if (overlap(rows_of(dweight, d->groups, 1, d->dweight_stride, 0, d->cols, size), rows_of(dbias, d->groups, 1, d->dbias_stride, 0, d->cols, size)))
+            return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: dweight and dbias overlap");
     }
     LnBackward a{};
     a.dy = dy; a.x = x; a.mean = mean; a.rstd = rstd; a.weight = weight; a.dx = dx; a.dweight = dweight; a.dbias = dbias;
