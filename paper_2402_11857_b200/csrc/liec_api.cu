@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <memory>
 #include <new>
 #include <string>
 #include <vector>
@@ -249,6 +250,7 @@ struct liec_ctx {
     int stage = 0;  // 0 idle, 1 after uplink, 2 after aggregate, 3 after downlink
     int64_t launches = 0;
     int32_t tensor_dtype = -1;     // type of the tensors given to liec_set_tensors, -1 before the first call
+    std::unique_ptr<const void *[]> tensors;   // [N][T] what it was given
     bool telemetry_valid = false;  // an iteration has completed with the telemetry switched on
     std::string err;
     // top-k: the single-tile segments are selected on a stream of the context's own, forked from
@@ -760,15 +762,34 @@ liec_status liec_set_tensors(liec_ctx *c, const void *const *tensors, int32_t dt
     const uintptr_t mask = dtype == LIEC_BF16 ? 1u : 3u;
     for (int64_t q = 0; q < count; ++q)
         if (reinterpret_cast<uintptr_t>(tensors[q]) & mask) { c->err = "a tensor is not aligned to its element size"; return LIEC_ERR_INVALID_ARG; }
+    if (!c->tensors) c->tensors.reset(new (std::nothrow) const void *[count]);
+    if (!c->tensors) { c->err = "out of host memory"; return LIEC_ERR_INVALID_ARG; }
     c->tensor_dtype = -1;   // (a table that is only half written is not used)
     LIEC_CALL(c, launch_upload_pointers(tensors, dtype, at<const void *>(c, c->plan.r_tensor_table), count, static_cast<cudaStream_t>(stream), &c->launches));
+    std::copy(tensors, tensors + count, c->tensors.get());
     c->tensor_dtype = dtype;
     return LIEC_OK;
+}
+
+// Whether the gradient rows share memory with a tensor of the table.
+static bool gather_overlaps(const liec_ctx *c, const void *out) {
+    const std::vector<int64_t> &off = c->plan.seg_off;
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(out), hi = lo + (c->p.gdt == DT_BF16 ? 2 : 4) * (uintptr_t)c->p.N * (uintptr_t)c->p.d;
+    const uintptr_t size = c->tensor_dtype == LIEC_BF16 ? 2 : 4;
+    const void *const *q = c->tensors.get();
+    bool any = false;
+    for (int i = 0; i < c->p.N; ++i)
+        for (int t = 0; t < c->p.T; ++t, ++q) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(*q);
+            any |= at != 0 && at < hi && at + size * (uintptr_t)(off[t + 1] - off[t]) > lo;
+        }
+    return any;
 }
 
 liec_status liec_gather_grads(liec_ctx *c, void *out, float max_norm, int32_t zero_nonfinite, float *norms, void *stream) {
     if (!c) return LIEC_ERR_INVALID_ARG;
     if (c->tensor_dtype < 0) { c->err = "liec_gather_grads: no tensors given (liec_set_tensors)"; return LIEC_ERR_STATE; }
+    if (out && gather_overlaps(c, out)) { c->err = "liec_gather_grads: out overlaps a tensor"; return LIEC_ERR_INVALID_ARG; }
     ClipArgs a{};
     a.table = at<const void *>(c, c->plan.r_tensor_table);
     a.src_dtype = c->tensor_dtype;

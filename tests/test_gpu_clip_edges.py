@@ -107,3 +107,35 @@ def test_table_that_is_not_there_yet_or_of_another_type(tiles):
     refused()
     ctx.liec_set_tensors(sets[torch.float32])
     right(torch.float32)
+
+
+@pytest.mark.parametrize("src", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tiles", [1, 50])
+def test_tensors_within_the_rows(tiles, src):
+    """Tensors that share memory with the rows they are gathered into are refused; beside them they are not."""
+    N, off = 2, [0, 24, tiles * TILE]
+    d = off[-1]
+    size = torch.empty(0, dtype=src).element_size()
+    memory = torch.zeros(4 * N * d + 64, device=DEV)
+    rows = memory[:N * d].view(N, d)
+    beyond = memory.view(src)[N * d * 4 // size:]           # begins where the rows end
+    ctx = liec.Context(torch.zeros(N, d, device=DEV), torch.zeros(d, device=DEV), off, SIGN, SIGN)
+
+    def tensors(first):
+        rest = [torch.ones(b - a, dtype=src, device=DEV) for _ in range(N) for a, b in zip(off, off[1:])][1:]
+        return [[first] + rest[:1], rest[1:]]
+
+    inside = memory.view(src)
+    for first in (inside[:24], inside[(N * d - 4) * 4 // size:][:24], inside[d * 4 // size - 5:][:24]):
+        ctx.liec_set_tensors(tensors(first))
+        with pytest.raises(liec.LiecError, match="overlaps") as err:
+            ctx.liec_gather_grads(rows)
+        assert err.value.status == 1
+    assert (memory == 0).all()
+    ctx.liec_set_tensors(tensors(beyond[:24]))
+    norms = ctx.liec_gather_grads(rows)
+    assert torch.equal(norms.cpu(), torch.tensor([(d - 24.0) ** 0.5, d ** 0.5]))
+    assert (rows[0, :24] == 0).all() and (rows[0, 24:] == 1).all() and (rows[1] == 1).all() and (memory[N * d:] == 0).all()
+    ctx.liec_set_tensors([[None, None], [None, None]])      # no tensors at all
+    assert (ctx.liec_gather_grads(rows) == 0).all() and (rows == 0).all()
+    assert ctx.liec_device_status() == 0
