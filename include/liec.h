@@ -326,6 +326,7 @@ typedef struct {
     int64_t dx_row_stride, dx_group_stride;
     int64_t weight_stride, bias_stride;      /* from worker to worker: d for a range of the parameter rows, 0 = shared */
     int64_t dweight_stride, dbias_stride;    /* from worker to worker: d for a range of the gradient rows */
+    int32_t shared_grads;   /* != 0: dweight and dbias are one vector [cols] each, summed over the workers as well (their strides are not used) */
 } liec_layer_norm_desc;
 
 /* Bytes of device workspace of the backward pass (column sums of runs of rows); 0 for a bad desc. */
@@ -341,7 +342,7 @@ liec_status liec_layer_norm_forward(const liec_layer_norm_desc *desc, const void
 
 /*
  *   dy, x       device, [groups][rows][cols] of dtype;  mean, rstd  as the forward pass stored them
- *   dx          device, of dtype;  dweight, dbias  device, [groups][cols] of grad_dtype: overwritten, also
+ *   dx          device, of dtype;  dweight, dbias  device, [groups][cols] of grad_dtype ([cols] with shared_grads): overwritten, also
  *               with rows = 0 (zeros).  Each of the three may be NULL: it is not computed.
  *   workspace   device, 16-byte aligned, liec_layer_norm_workspace_bytes(desc) bytes, when dweight or dbias is
  *               wanted; scratch of this call alone

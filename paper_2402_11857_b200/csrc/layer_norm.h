@@ -42,10 +42,11 @@ struct LnBackward {
     LnShare share;
     int32_t groups, cols, part_cols, grad_dtype;
     int32_t direct;               // every group is one CTA's: it writes the gradient itself
+    int32_t shared;               // one gradient vector for all groups: the pieces of all of them are joined
 };
 
 cudaError_t launch_layer_norm_forward(const LnForward &a, int dtype, cudaStream_t st);
 cudaError_t launch_layer_norm_backward(LnBackward a, int dtype, cudaStream_t st);
-size_t layer_norm_workspace(int groups, int64_t rows, int cols);   // bytes of part_w and part_b together
+size_t layer_norm_workspace(int groups, int64_t rows, int cols, bool shared);   // bytes of part_w and part_b together
 
 }  // namespace liec

@@ -239,8 +239,8 @@ __global__ void __launch_bounds__(TPR * SLOTS, MINB) ln_backward_kernel(const __
     if constexpr (WIDE) cluster_sync();   // none may leave while another still hands it sums
 }
 
-// Joins the pieces of a group, in binary64 and in a fixed order, and rounds once to the gradient rows'
-// type: 32 columns per CTA, four per thread, 32 threads per column.
+// Joins the pieces of a group (of all groups, where they share the gradient), in binary64 and in a fixed order, and
+// rounds once to the gradient rows' type: 32 columns per CTA, four per thread, 32 threads per column.
 __global__ void __launch_bounds__(256) ln_backward_join_kernel(const __grid_constant__ LnBackward a) {
     __shared__ double buf[8][32];
     const int group = blockIdx.y;
@@ -253,7 +253,9 @@ __global__ void __launch_bounds__(256) ln_backward_join_kernel(const __grid_cons
     int pieces = 0;
     if (a.rows > 0) {
         first = a.share.owner((int64_t)group * a.rows) + group;
-        pieces = (int)(a.share.owner(((int64_t)group + 1) * a.rows - 1) + group - first) + 1;
+        // (between two groups that meet where two shares meet lies a place without a piece: it holds zeros)
+        const int end = a.shared ? a.groups : group + 1;
+        pieces = (int)(a.share.owner((int64_t)end * a.rows - 1) + end - 1 - first) + 1;
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");   // the pieces are complete
     const float *p = (weight ? a.part_w : a.part_b) + (first + way) * a.cols + c;
@@ -295,6 +297,7 @@ struct LnPlanner {
     int groups;
     int64_t rows;
     int parts;
+    bool shared;
     template <int TPR, int E, int SLOTS, int MINB>
     LnPlan operator()() const {
         const int64_t total = (int64_t)groups * rows;
@@ -304,21 +307,21 @@ struct LnPlanner {
         // (4 rows of 8192 binary32 columns, eight groups: 13.6 us, 15.8 us shared and joined; one group 13.5 and
         // 10.2 us; 16 rows of 768: 6.8 and 5.1 us, 32 rows 9.3 and 5.1 us); or with so many groups that their CTAs
         // fill the GPU several times over anyway
-        p.direct = rows <= 4 * SLOTS || (groups >= 4 * resident && rows <= (int64_t)SLOTS * LN_SUM_ROWS);
+        p.direct = !shared && (rows <= 4 * SLOTS || (groups >= 4 * resident && rows <= (int64_t)SLOTS * LN_SUM_ROWS));
         p.share = p.direct ? LnShare{0, 0, rows, groups} : ln_share(total, SLOTS, resident, LN_SUM_ROWS, false);
         p.pieces = p.direct ? 0 : p.share.ctas + groups;
         return p;
     }
 };
 
-static LnPlan ln_plan(int groups, int64_t rows, int cols) {
-    const LnPlanner planner{groups, rows, ln_parts(cols)};
+static LnPlan ln_plan(int groups, int64_t rows, int cols, bool shared) {
+    const LnPlanner planner{groups, rows, ln_parts(cols), shared};
     return planner.parts > 1 ? ln_wide_shape(planner) : ln_backward_shape(cols, planner);
 }
 
-size_t layer_norm_workspace(int groups, int64_t rows, int cols) {
+size_t layer_norm_workspace(int groups, int64_t rows, int cols, bool shared) {
     if (rows == 0) return 0;
-    return sizeof(float) * 2 * (size_t)std::max<int64_t>(ln_plan(groups, rows, cols).pieces, groups) * (size_t)cols;
+    return sizeof(float) * 2 * (size_t)std::max<int64_t>(ln_plan(groups, rows, cols, shared).pieces, groups) * (size_t)cols;
 }
 
 template <typename T, bool WHOLE, bool WIDE = false>
@@ -351,7 +354,11 @@ cudaError_t launch_layer_norm_backward(LnBackward a, int dtype, cudaStream_t st)
         const bool whole = ln_whole(a.x, a.x_row, a.x_group, a.rows, a.groups, a.cols, esz) &&
                            ln_whole(a.dy, a.dy_row, a.dy_group, a.rows, a.groups, a.cols, esz) &&
                            (!a.dx || ln_whole(a.dx, a.dx_row, a.dx_group, a.rows, a.groups, a.cols, esz));
-        const LnPlan p = ln_plan(a.groups, a.rows, a.cols);
+        const LnPlan p = ln_plan(a.groups, a.rows, a.cols, a.shared != 0);
+        if (a.shared && (a.dweight || a.dbias)) {   // (the places without a piece)
+            const cudaError_t e = cudaMemsetAsync(a.part_w, 0, layer_norm_workspace(a.groups, a.rows, a.cols, true), st);
+            if (e != cudaSuccess) return e;
+        }
         a.share = p.share;
         a.direct = p.direct;
         a.part_cols = ln_part_cols(a.cols);
@@ -363,7 +370,7 @@ cudaError_t launch_layer_norm_backward(LnBackward a, int dtype, cudaStream_t st)
     if ((a.dweight || a.dbias) && !a.direct) {
         // launched while the rows' kernel ends; it waits for that kernel's end before it reads
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((a.cols + 31) / 32, a.groups, 2);
+        cfg.gridDim = dim3((a.cols + 31) / 32, a.shared ? 1 : a.groups, 2);
         cfg.blockDim = dim3(256);
         cfg.stream = st;
         cudaLaunchAttribute attr[1];

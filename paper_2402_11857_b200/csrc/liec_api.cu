@@ -976,9 +976,11 @@ static Rows ln_rows(const liec_layer_norm_desc *d, const void *base, int64_t row
 
 static bool aligned_to(const void *ptr, int32_t dtype) { return (reinterpret_cast<uintptr_t>(ptr) & (dtype == LIEC_BF16 ? 1u : 3u)) == 0; }
 
+static bool ln_shared(const liec_layer_norm_desc *d) { return d->shared_grads != 0 && d->groups > 1; }
+
 size_t liec_layer_norm_workspace_bytes(const liec_layer_norm_desc *d) {
     if (ln_check(d) != LIEC_OK) return 0;
-    return align_up(layer_norm_workspace(d->groups, d->rows, d->cols), 256);
+    return align_up(layer_norm_workspace(d->groups, d->rows, d->cols, ln_shared(d)), 256);
 }
 
 liec_status liec_layer_norm_forward(const liec_layer_norm_desc *d, const void *x, const float *weight, const float *bias, void *y,
@@ -1015,9 +1017,10 @@ liec_status liec_layer_norm_backward(const liec_layer_norm_desc *d, const void *
         !aligned_to(mean, LIEC_F32) || !aligned_to(rstd, LIEC_F32) || !aligned_to(dweight, d->grad_dtype) || !aligned_to(dbias, d->grad_dtype))
         return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: a pointer is not aligned to its element size");
     if (dx && d->rows > 0 && !ln_disjoint(d, d->dx_row_stride, d->dx_group_stride)) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: the rows of dx overlap");
-    if (d->groups > 1 && ((dweight && d->dweight_stride < d->cols) || (dbias && d->dbias_stride < d->cols)))
+    const bool shared = ln_shared(d);
+    if (d->groups > 1 && !shared && ((dweight && d->dweight_stride < d->cols) || (dbias && d->dbias_stride < d->cols)))
         return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: the workers' rows of dweight or dbias overlap");
-    const size_t need = layer_norm_workspace(d->groups, d->rows, d->cols);
+    const size_t need = layer_norm_workspace(d->groups, d->rows, d->cols, shared);
     if ((dweight || dbias) && need > 0) {
         if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15u)) return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: workspace must be non-NULL and 16-byte aligned");
         if (workspace_bytes < need) return ln_refuse(LIEC_ERR_WORKSPACE, "workspace smaller than liec_layer_norm_workspace_bytes()");
@@ -1029,7 +1032,8 @@ liec_status liec_layer_norm_backward(const liec_layer_norm_desc *d, const void *
     }
     if (dweight && dbias) {
         const int size = d->grad_dtype == LIEC_BF16 ? 2 : 4;
-        if (overlap(rows_of(dweight, d->groups, 1, d->dweight_stride, 0, d->cols, size), rows_of(dbias, d->groups, 1, d->dbias_stride, 0, d->cols, size)))
+        const int vectors = shared ? 1 : d->groups;
+        if (overlap(rows_of(dweight, vectors, 1, d->dweight_stride, 0, d->cols, size), rows_of(dbias, vectors, 1, d->dbias_stride, 0, d->cols, size)))
             return ln_refuse(LIEC_ERR_INVALID_ARG, "layer norm: dweight and dbias overlap");
     }
     LnBackward a{};
@@ -1040,6 +1044,7 @@ liec_status liec_layer_norm_backward(const liec_layer_norm_desc *d, const void *
     a.x_row = d->x_row_stride; a.x_group = d->x_group_stride; a.dy_row = d->y_row_stride; a.dy_group = d->y_group_stride;
     a.dx_row = d->dx_row_stride; a.dx_group = d->dx_group_stride;
     a.weight_stride = d->weight_stride; a.dweight_stride = d->dweight_stride; a.dbias_stride = d->dbias_stride;
+    a.shared = shared;
     const cudaError_t e = launch_layer_norm_backward(a, d->dtype, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return ln_refuse(LIEC_ERR_CUDA, cudaGetErrorString(e));
     return LIEC_OK;

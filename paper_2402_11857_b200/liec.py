@@ -49,7 +49,7 @@ class liec_layer_norm_desc(C.Structure):
                 ("y_row_stride", C.c_int64), ("y_group_stride", C.c_int64),
                 ("dx_row_stride", C.c_int64), ("dx_group_stride", C.c_int64),
                 ("weight_stride", C.c_int64), ("bias_stride", C.c_int64),
-                ("dweight_stride", C.c_int64), ("dbias_stride", C.c_int64)]
+                ("dweight_stride", C.c_int64), ("dbias_stride", C.c_int64), ("shared_grads", C.c_int32)]
 
 
 def load_library(path: Optional[str] = None) -> C.CDLL:
@@ -275,9 +275,13 @@ def _ln_desc(x, y, dx, weight, bias, dweight, dbias, eps):
     if len(dweight[0]) == 1 and d.groups > 1:   # one vector for all workers: its gradient sums over their rows as well
         if d.weight_stride != 0:
             raise ValueError("workers with weights of their own need dweight and dbias [N, h]")
-        if any(t[1][0] != d.rows * t[1][1] for t in (x, y, dx)):
-            raise ValueError("a gradient shared by the workers needs x, dy and dx whose workers follow one another")
-        d.groups, d.rows = 1, d.groups * d.rows
+        if d.groups * d.rows < 1 << 31 and (d.rows <= 1 or all(t[1][0] == d.rows * t[1][1] for t in (x, y, dx))):
+            # the workers' rows follow one another in all three: rows of one worker
+            if d.rows == 1:
+                d.x_row_stride, d.y_row_stride, d.dx_row_stride = x[1][0], y[1][0], dx[1][0]
+            d.groups, d.rows = 1, d.groups * d.rows
+        else:
+            d.shared_grads = 1
     return d, C.byref(d), int(load_library().liec_layer_norm_workspace_bytes(C.byref(d)))
 
 
@@ -360,7 +364,7 @@ def _ln_backward(raw, device, dy, x, mean, rstd, weight, dx, dweight, dbias, wor
 def liec_layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias=None, workspace=None, stream=None):
     """Gradients of liec_layer_norm_forward.  dweight and dbias: [N, h] float32 or bfloat16 (any stride between
     workers, e.g. ``grads[:, a:a + h]``), or [h] for a vector that all workers share (its gradient is summed over
-    the workers too); allocated in float32, shaped like weight, where not given.  Returns (dx, dweight, dbias)."""
+    the workers too, for any layout of x, dy and dx); allocated in float32, shaped like weight, where not given.  Returns (dx, dweight, dbias)."""
     import torch
     device = _device_of("x", x)
     for name, t in (("dy", dy), ("weight", weight), ("dx", dx), ("dweight", dweight), ("dbias", dbias), ("workspace", workspace)):

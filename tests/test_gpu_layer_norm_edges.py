@@ -41,3 +41,62 @@ def test_slices_of_one_buffer(N, rows, h, dtype):
         backward(dy, x, mean, rstd, w, dweight=grads[:, 1:h + 1], dbias=grads[:, :h])
     with pytest.raises(liec.LiecError, match="overlap"):
         forward(both[..., :h], w, b, y=both[..., h - 1:2 * h - 1])
+
+
+def check_shared(x, dy, w, b, dtype, **given):
+    """Forward and backward with one weight for all workers, against the formulas over all rows."""
+    N, rows, h = x.shape
+    y, mean, rstd = forward(x, w, b)
+    dx, dw, db = backward(dy, x, mean, rstd, w, **given)
+    assert dx.shape == x.shape and dw.shape == (h,) and db.shape == (h,)
+    flat = lambda t: t.reshape(1, N * rows, *t.shape[2:])
+    check_backward(flat(dy), flat(x), flat(mean), flat(rstd), w[None], dtype, "f32", flat(dx), dw[None], db[None])
+    again = backward(dy, x, mean, rstd, w, **{k: v.clone().fill_(float("nan")) for k, v in given.items()})
+    for p, q in zip((dx, dw, db), again):
+        assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,rows,h", [(3, 10, 64), (2, 33, 255), (5, 12, 768), (300, 7, 768), (3, 300, 1001), (2, 40, 4096), (3, 8, 9000), (2, 3000, 48)])
+def test_shared_weight_any_layout(N, rows, h, dtype):
+    """One weight for all workers on what the forward pass takes: slices of the activations, workers inside, an incoming
+    gradient that is broadcast.  (Its sums over rows add at most 1024 in binary32 and the rest in binary64.)"""
+    x, dy, w, b = draw(N, rows, h, dtype, seed=12)
+    w, b = w[0].contiguous(), b[0].contiguous()
+    inside = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)
+    check_shared(x, dy, w, b, dtype)
+    check_shared(x[:, -1:], dy[:, -1:], w, b, dtype)
+    check_shared(x[:, :4], dy[:, :4], w, b, dtype)
+    check_shared(x[:, ::3], dy[:, ::3].contiguous(), w, b, dtype)
+    check_shared(inside(x), dy, w, b, dtype)
+    check_shared(x, dy[:, :1].expand(N, rows, h), w, b, dtype)
+    check_shared(x, dy[:1].expand(N, rows, h), w, b, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("h", [48, 768, 4096, 9000])
+def test_shared_weight_where_shares_meet_groups(h, dtype):
+    """Rows dealt so that workers and shares end together in some places and not in others, in a workspace that
+    holds NaN: every place of it that is joined was written."""
+    for N, rows in ((4, 1184), (8, 296), (37, 64), (296, 8), (3, 1024), (5, 333)):
+        x, dy, w, b = draw(N, rows, h if N * rows < 3000 or h < 1000 else 4096, dtype, seed=N)
+        check_shared(x, dy[:, :1].expand(x.shape), w[0].contiguous(), b[0].contiguous(), dtype,
+                     workspace=torch.full((1 << 24,), float("nan"), device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_shared_weight_without_rows_and_in_bfloat16_gradients(dtype):
+    x, w = torch.empty(3, 0, 64, dtype=DT[dtype], device="cuda"), torch.ones(64, device="cuda")
+    _, mean, rstd = forward(x, w, w)
+    dx, dw, db = backward(x, x, mean, rstd, w)
+    assert dx.shape == x.shape and (dw == 0).all() and (db == 0).all() and dw.shape == (64,)
+    x, dy, w, b = draw(3, 50, 100, dtype, seed=3)
+    w = w[0].contiguous()
+    _, mean, rstd = forward(x, w)
+    grads = torch.full((2, 100), 7.0, dtype=torch.bfloat16, device="cuda")
+    cut = slice(0, 30)
+    want = backward(dy[:, cut].contiguous(), x[:, cut].contiguous(), mean[:, cut].contiguous(), rstd[:, cut].contiguous(), w)
+    dx, dw, db = backward(dy[:, cut], x[:, cut], mean[:, cut].contiguous(), rstd[:, cut].contiguous(), w, dweight=grads[0], dbias=grads[1])
+    assert torch.equal(dx, want[0])
+    flat = lambda t: t.reshape(1, 90, *t.shape[2:])
+    check_backward(flat(dy[:, cut]), flat(x[:, cut]), flat(mean[:, cut]), flat(rstd[:, cut]), w[None], dtype, "bf16", flat(dx), dw[None], db[None])

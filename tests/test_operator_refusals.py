@@ -24,3 +24,34 @@ def test_outputs_that_overlap(lib):
     for kw in (dict(db=4 * at), dict(db=4 * at + 63 * 4), dict(db=4 * at - 63 * 4), dict(db=4 * at + 200 * 4 + 32), dict(db=4 * at + 137 * 4)):
         assert backward(desc(), **kw) == 1 and b"dweight and dbias" in lib.liec_last_error(None)
     assert backward(desc(groups=1, dweight_stride=0, dbias_stride=0), dw=4 * at, db=4 * at + 4) == 1
+
+
+def shared_layouts():
+    """x, dy and dx of the backward pass with one weight for three workers: what the forward pass takes as well."""
+    import torch
+    full = torch.empty(3, 10, 64)
+    dense = lambda t: torch.empty_like(t, memory_format=torch.contiguous_format)
+    yield "no rows", full[:, :0], dense(full[:, :0])
+    yield "the last row of each", full[:, -1:], dense(full[:, -1:])
+    yield "the first rows", full[:, :4], dense(full[:, :4])
+    yield "every second row", full[:, ::2], dense(full[:, ::2])
+    yield "workers inside", full.transpose(0, 1).contiguous().transpose(0, 1), dense(full)
+    yield "dy broadcast over rows", full, full[:, :1].expand(3, 10, 64)
+    yield "dy broadcast over workers", full, full[:1].expand(3, 10, 64)
+    yield "dy broadcast over both", full, full[:1, :1].expand(3, 10, 64)
+    yield "one after another", full, dense(full)
+
+
+@pytest.mark.parametrize("name,x,dy", list(shared_layouts()), ids=lambda v: v if isinstance(v, str) else "")
+def test_layouts_with_a_shared_gradient(lib, name, x, dy):
+    import torch
+    vector, dx = torch.empty(64), torch.empty(x.shape)
+    layout = liec._layout
+    d, _, need = liec._ln_desc(layout(x), layout(dy), layout(dx), layout(vector), None, layout(vector), layout(vector), 0.0)
+    assert d.groups * d.rows == x.shape[0] * x.shape[1] or d.rows == 0
+    # every row of the descriptor is the row of the tensors that it stands for, in the same order
+    for t, row, group in ((x, d.x_row_stride, d.x_group_stride), (dy, d.y_row_stride, d.y_group_stride), (dx, d.dx_row_stride, d.dx_group_stride)):
+        want = [n * t.stride(0) + r * t.stride(1) for n in range(x.shape[0]) for r in range(x.shape[1])]
+        assert [g * group + r * row for g in range(d.groups) for r in range(d.rows)] == want
+    assert bool(d.shared_grads) == (d.groups > 1)
+    assert need >= 0
