@@ -430,6 +430,16 @@ liec_status liec_clear_status(liec_ctx *ctx, void *stream);
 liec_status liec_set_copy_wait(liec_ctx *ctx, uint32_t poll_limit, uint32_t expect_extra_bytes);
 
 /*
+ * The same for the waits of liec_clip_grads and liec_gather_grads on one another's results (rows above 8 to 32
+ * tiles of 8192 elements, the only ones that have such waits): for the sums of a row's tiles, for a row's
+ * factor, and for room to fetch the next tile.  Each is polled at most `poll_limit` times (0 = the default,
+ * 2^21) before bit 32 of the status word is set and the kernel ends.  `withhold` (0 in operation) drives
+ * the path without any fault: 1 = the sum of every row's first tile is never handed over, 2 = no row's factor is,
+ * 3 = neither.  Takes effect from the next call.
+ */
+liec_status liec_set_norm_wait(liec_ctx *ctx, uint32_t poll_limit, uint32_t withhold);
+
+/*
  * Diagnostics: which route the top-k selections (Def. 2) of the last iteration took on one side
  * (uplink != 0: the N*T worker problems; 0: the T server problems).  Synchronises `stream`, copies
  * the selection state to the host and counts:

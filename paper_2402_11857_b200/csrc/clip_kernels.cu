@@ -271,8 +271,7 @@ constexpr int PASS_TILES = 8 * GROUP * 4;   // tile sums that row_tree takes in 
 constexpr int ROW_PASSES = 160;
 static_assert((int64_t)ROW_PASSES * PASS_TILES >= (int64_t(1) << 32) / TILE + 65535, "passes for the most tiles: dim below 2^32, at most 65535 segments");
 constexpr unsigned STATUS_NORM_TIMEOUT = 32;   // bit of the status word: a row's norm did not arrive within the wait limit
-constexpr unsigned NORM_WAIT_LIMIT = 1u << 21;   // polls of 40 ns and a load
-constexpr unsigned OP_WAIT_LIMIT = 1u << 21;     // polls of 200 ns of the producer for ops to be worked off
+// (norm_wait_limit: polls of 40 ns and a load for sums and factors, of 200 ns by the producer for ops to be worked off)
 
 template <typename ST>
 struct StreamShape {
@@ -382,20 +381,21 @@ __device__ __forceinline__ double group_tree(double warp_sum, double *warp_sums,
 }
 
 // Balanced tree over a row's tile sums as they come in (a group; result in its thread 0).  A warp takes 1024
-// consecutive sums as 16 rows of 64, two per lane; `missing` is set when one did not come within
-// the limit, or the CTA stops.
+// consecutive sums as 16 rows of 64, two per lane; `missing` is set when they did not all come within `limit` polls
+// (of the row, not of a pass), or the CTA stops.
 __device__ __noinline__ double row_tree(const double *src, int tiles, double *warp_sums /*[4]*/, double *pass_sums /*[ROW_PASSES]*/,
-                                           int g, const volatile int *stop, bool &missing) {
+                                           int g, const volatile int *stop, unsigned limit, bool &missing) {
     const int t = threadIdx.x % GROUP, warp = t / 32, lane = t & 31;
     const int passes = (tiles + PASS_TILES - 1) / PASS_TILES;
     missing = false;
+    unsigned tries = 0;
     for (int q = 0; q < passes; ++q) {
         double part[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int first = q * PASS_TILES + warp * 1024 + half * 512 + lane * 2;
             unsigned long long v[8][2];
-            for (unsigned tries = 0;; ++tries) {   // all sixteen again until they are there
+            for (;; ++tries) {   // all sixteen again until they are there
                 bool unset = false;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -404,7 +404,7 @@ __device__ __noinline__ double row_tree(const double *src, int tiles, double *wa
 #pragma unroll
                 for (int j = 0; j < 8; ++j) unset |= v[j][0] == UNSET64 || v[j][1] == UNSET64;
                 if (!__any_sync(0xffffffffu, unset)) break;
-                if (__any_sync(0xffffffffu, tries > NORM_WAIT_LIMIT || *stop)) { missing = true; break; }
+                if (__any_sync(0xffffffffu, tries >= limit || *stop)) { missing = true; break; }
                 __nanosleep(40);
             }
             double leaf[8];
@@ -414,9 +414,9 @@ __device__ __noinline__ double row_tree(const double *src, int tiles, double *wa
         }
         const double s = group_tree(__dadd_rn(part[0], part[1]), warp_sums, g);
         if (t == 0) pass_sums[q] = s;
-        group_sync(g);
+        missing = group_any(g, missing);
+        if (missing) break;
     }
-    missing = group_any(g, missing);
     return t == 0 ? balanced_join(pass_sums, passes) : 0.0;
 }
 
@@ -557,7 +557,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
                         mbar_arrive(&full[slot]);
                     }
                 }
-                if (++polls > OP_WAIT_LIMIT) { atomicOr(p.status, STATUS_NORM_TIMEOUT); stop = 1; }
+                if (++polls > p.norm_wait_limit) { atomicOr(p.status, STATUS_NORM_TIMEOUT); stop = 1; }
                 if (stopping()) return;
                 // (polling without a pause made the consumers' shuffles ten times slower: both use the shared memory pipe)
                 if (__any_sync(0xffffffffu, pending)) __nanosleep(200);
@@ -679,11 +679,12 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
                 const double s = group_tree(sum, warp_sums[g], g);
                 if (t == 0) {
                     mbar_arrive(&done[slot]);
-                    post(a.partials + (int64_t)o.row * p.TT + o.tile, (unsigned long long)__double_as_longlong(s));
+                    if (!(p.norm_withhold & WITHHOLD_SUM) || o.tile != 0)
+                        post(a.partials + (int64_t)o.row * p.TT + o.tile, (unsigned long long)__double_as_longlong(s));
                 }
             } else if (o.kind == OP_JOIN) {
                 bool missing;
-                const double sum = row_tree(a.partials + (int64_t)o.row * p.TT, p.TT, warp_sums[g], pass_sums[g], g, &stop, missing);
+                const double sum = row_tree(a.partials + (int64_t)o.row * p.TT, p.TT, warp_sums[g], pass_sums[g], g, &stop, p.norm_wait_limit, missing);
                 if (t == 0) {
                     mbar_arrive(&done[slot]);
                     if (missing) {
@@ -691,7 +692,8 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
                         stop = 1;
                     } else {
                         float norm;
-                        post(a.answer + o.row, pack_factor(row_factor(a, sum, norm)));
+                        const unsigned long long factor = pack_factor(row_factor(a, sum, norm));
+                        if (!(p.norm_withhold & WITHHOLD_FACTOR)) post(a.answer + o.row, factor);
                         if (a.norms) a.norms[o.row] = norm;
                     }
                 }
@@ -703,7 +705,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, 1) clip_stream_kernel(const __
                         while (!stop && word == UNSET64) {
                             __nanosleep(40);
                             // (a CTA that gave up ends the others' waits as well)
-                            if (++tries > NORM_WAIT_LIMIT || ((tries & 63u) == 0 && peek(a.gave_up) != UNSET64)) {
+                            if (++tries > p.norm_wait_limit || ((tries & 63u) == 0 && peek(a.gave_up) != UNSET64)) {
                                 atomicOr(p.status, STATUS_NORM_TIMEOUT);
                                 stop = 1;
                             }

@@ -391,6 +391,8 @@ liec_status liec_init(const liec_config *cfg, float *params, float *error, void 
     p.up = cfg->uplink; p.down = cfg->downlink; p.gdt = cfg->grad_dtype;
     p.copy_wait_limit = COPY_WAIT_LIMIT_DEFAULT;
     p.copy_expect_extra = 0u;
+    p.norm_wait_limit = NORM_WAIT_LIMIT_DEFAULT;
+    p.norm_withhold = 0u;
     p.seg_off = at<int64_t>(c, pl.r_seg_off);
     p.word_off = at<int64_t>(c, pl.r_word_off);
     p.k_off = at<int64_t>(c, pl.r_k_off);
@@ -687,6 +689,14 @@ liec_status liec_set_copy_wait(liec_ctx *c, uint32_t poll_limit, uint32_t expect
     if (expect_extra_bytes > 1024u) { c->err = "expect_extra_bytes must be at most 1024"; return LIEC_ERR_INVALID_ARG; }
     c->p.copy_wait_limit = poll_limit ? poll_limit : COPY_WAIT_LIMIT_DEFAULT;
     c->p.copy_expect_extra = expect_extra_bytes;
+    return LIEC_OK;
+}
+
+liec_status liec_set_norm_wait(liec_ctx *c, uint32_t poll_limit, uint32_t withhold) {
+    if (!c) return LIEC_ERR_INVALID_ARG;
+    if (withhold & ~(WITHHOLD_SUM | WITHHOLD_FACTOR)) { c->err = "withhold must be 0, 1, 2 or 3"; return LIEC_ERR_INVALID_ARG; }
+    c->p.norm_wait_limit = poll_limit ? poll_limit : NORM_WAIT_LIMIT_DEFAULT;
+    c->p.norm_withhold = withhold;
     return LIEC_OK;
 }
 

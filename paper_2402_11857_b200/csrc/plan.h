@@ -109,8 +109,12 @@ struct Params {
     // bytes added to what its barrier is told to expect (0 in operation; a diagnostic setting
     // makes the barrier never complete although the copy lands, which exercises the timeout path)
     uint32_t copy_wait_limit, copy_expect_extra;
+    // bounded waits of the clipping on what other thread groups and CTAs hand over: polls before it is declared lost, and
+    // what is never handed over (WITHHOLD_* bits; 0 in operation)
+    uint32_t norm_wait_limit, norm_withhold;
 };
-constexpr uint32_t COPY_WAIT_LIMIT_DEFAULT = 1u << 20;
+constexpr uint32_t COPY_WAIT_LIMIT_DEFAULT = 1u << 20, NORM_WAIT_LIMIT_DEFAULT = 1u << 21;
+constexpr uint32_t WITHHOLD_SUM = 1, WITHHOLD_FACTOR = 2;   // the sum of every row's first tile; every row's factor
 constexpr int SCAN_PART = THREADS * 16;   // tiles whose output offsets one CTA of the wide form's scan computes
 constexpr int LONG_SEG_TILES = 1024;   // from here on a segment's candidate passes walk its candidate region as a whole, not tile block by tile block
 

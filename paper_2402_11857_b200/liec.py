@@ -92,6 +92,8 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.liec_abort_step.restype = C.c_int
     lib.liec_set_copy_wait.argtypes = [vp, C.c_uint32, C.c_uint32]
     lib.liec_set_copy_wait.restype = C.c_int
+    lib.liec_set_norm_wait.argtypes = [vp, C.c_uint32, C.c_uint32]
+    lib.liec_set_norm_wait.restype = C.c_int
     lib.liec_average_step.argtypes = [vp, vp, C.c_float, vp]
     lib.liec_average_step.restype = C.c_int
     lib.liec_mean_params.argtypes = [vp, vp, vp]
@@ -481,6 +483,9 @@ class Context:
 
     def liec_set_copy_wait(self, poll_limit: int = 0, expect_extra_bytes: int = 0):
         self._check(self.lib.liec_set_copy_wait(self._ctx, int(poll_limit), int(expect_extra_bytes)))
+
+    def liec_set_norm_wait(self, poll_limit: int = 0, withhold: int = 0):
+        self._check(self.lib.liec_set_norm_wait(self._ctx, int(poll_limit), int(withhold)))
 
     def liec_average_step(self, grads, lr: float, stream=None):
         self._check_grads(grads)

@@ -139,3 +139,41 @@ def test_tensors_within_the_rows(tiles, src):
     ctx.liec_set_tensors([[None, None], [None, None]])      # no tensors at all
     assert (ctx.liec_gather_grads(rows) == 0).all() and (rows == 0).all()
     assert ctx.liec_device_status() == 0
+
+
+@pytest.mark.parametrize("gdt", [liec.F32, liec.BF16])
+@pytest.mark.parametrize("N,tiles", [(2, 40), (1, 9000), (3, 1500)])
+@pytest.mark.parametrize("withhold", [1, 2, 3])
+def test_norm_wait_runs_out(withhold, N, tiles, gdt):
+    """A tile's sum or a row's factor that is never handed over: whoever waits for it (a row's join, the scaling, the
+    producer once its ring is full) gives up at its limit, bit 32 is set, no row is written, and the next call is right.
+    The long rows have three passes of tile sums to join, and more tiles than the rings of all SMs hold."""
+    d = tiles * TILE - 3
+    off = [0, TILE + 1, d]
+    G, norms = small_integers(N, d, TDT[gdt], tiles)
+    ctx = liec.Context(torch.zeros(N, d, device=DEV), torch.zeros(d, device=DEV), off, SIGN, SIGN, grad_dtype=gdt)
+    out, before = torch.full_like(G, 7.0), G.clone()
+    limit = 0.5 * float(norms.min())
+    ctx.liec_set_norm_wait(poll_limit=500, withhold=withhold)
+    ctx.liec_clip_grads(G, limit, out=out)
+    assert ctx.liec_device_status() == 32
+    assert (out == 7).all() and torch.equal(G, before)
+    ctx.liec_clear_status()
+    ctx.liec_clip_grads(G, limit)                                 # in place
+    assert ctx.liec_device_status() == 32 and torch.equal(G, before)
+    ctx.liec_clear_status()
+    got = ctx.liec_clip_grads(G, float("inf"))                    # norms alone: nobody waits for a factor
+    if withhold == 2:
+        assert ctx.liec_device_status() == 0 and np.array_equal(got.cpu().numpy(), norms)
+    else:
+        assert ctx.liec_device_status() == 32
+    ctx.liec_set_norm_wait()
+    ctx.liec_clear_status()
+    assert np.array_equal(ctx.liec_clip_grads(G, limit, out=out).cpu().numpy(), norms)
+    factor = (np.float64(np.float32(limit)) / norms.astype(np.float64))
+    error = (out.double() - G.double() * torch.from_numpy(factor).to(DEV)[:, None]).abs()
+    assert (error <= G.double().abs() * (2.0 ** -8 if gdt == liec.BF16 else 2.0 ** -22) * float(factor.max())).all()
+    assert ctx.liec_device_status() == 0
+    with pytest.raises(liec.LiecError) as err:
+        ctx.liec_set_norm_wait(withhold=4)
+    assert err.value.status == 1
