@@ -403,9 +403,10 @@ liec_status liec_get_messages(const liec_ctx *ctx, liec_messages *out);
  * Synchronises `stream` and reads the device status word: 0 = clean; non-zero bits name an
  * internal check that failed (1 selection rank, 2 candidate buffer, 4 output count, 8 a bulk
  * copy into shared memory that did not complete within its bounded wait; the kernel that saw it
- * returned without touching its outputs; 16 a random-k subset entry outside its segment or out of
- * order; 32 a row's norm or another part of the clipping did not come within its bounded wait: the
- * rows and norms of that call are unspecified; 64 liec_gather_grads found no table of the type that
+ * returned without touching its outputs, but for liec_clip_grads and liec_gather_grads (below); 16 a random-k
+ * subset entry outside its segment or out of order; 32 a row's norm or another part of the clipping did not
+ * come within its bounded wait; after 8 or 32 from liec_clip_grads or liec_gather_grads the rows and norms of that call
+ * are unspecified (in place, some entries may have been scaled and others not); 64 liec_gather_grads found no table of the type that
  * liec_set_tensors was last called for: its rows are zeros).  Returns LIEC_ERR_DEVICE_CHECK when non-zero.
  */
 liec_status liec_device_status(liec_ctx *ctx, void *stream, int32_t *out);
@@ -420,7 +421,9 @@ liec_status liec_clear_status(liec_ctx *ctx, void *stream);
 /*
  * Diagnostics for the bounded waits (no counterpart in the paper).  Kernels that stage a tile in
  * shared memory with a bulk copy poll the copy's barrier at most `poll_limit` times (0 = the default,
- * 2^20) before they set bit 8 of the status word and return without touching their outputs.
+ * 2^20) before they set bit 8 of the status word and return without touching their outputs; the kernel
+ * behind liec_clip_grads and liec_gather_grads sums and scales many tiles in one launch, so its rows and norms are then
+ * unspecified, and it counts the time until a copy is issued as well (while the ring is full, or a norm late).
  * `expect_extra_bytes` (a multiple of 16, at most 1024; 0 in operation) is added to the byte count
  * that each copy's barrier is told to expect: the copy still lands, but its barrier never completes,
  * so every such wait runs out.  That is how a test drives the timeout path without any fault; a
