@@ -305,7 +305,7 @@ liec_status liec_gather_grads(liec_ctx *ctx, void *out, float max_norm, int32_t 
  *   dw = sum over the worker's rows of dy xh,  db = sum over the worker's rows of dy
  * Evaluated in binary32; outputs are rounded once to their type.  The variance is mean(x^2) - m^2 where
  * m^2 is at most a quarter of it, and summed around the mean in all other rows.  The order of the sums
- * depends on the sizes alone, not on strides or alignment (no atomics): equal calls give equal bits.  A row with an infinity or NaN gives NaN in that row (and in dw) only.
+ * depends on the sizes and types alone, not on strides or alignment (no atomics): equal calls give equal bits.  A row with an infinity or NaN gives NaN in that row (and in dw) only.
  *
  * No context is needed.  All strides are in elements and >= 0; the last axis is contiguous.  Rows that
  * are read may overlap or repeat (stride 0); rows that are written may not.  Any element alignment is

@@ -3,7 +3,8 @@
 //
 // TPR threads share a row (a "slot" of a CTA).  A chunk is 16 bytes of elements (VEC = 4 of binary32, 8 of
 // bfloat16); thread t of the slot owns the chunks v TPR + t, v < NV, of its row, whatever the row's
-// alignment, so that the order of every sum, hence every bit of the result, depends on h alone.  Rows
+// alignment, so that the order of a row's sums depends on h and the element type alone, that of the column sums of the
+// backward pass on the numbers of rows and workers as well, and no bit of a result on strides or alignment.  Rows
 // pass through a ring in shared memory, STAGES rows deep per slot; what lies beyond column h there is
 // zero.  The bytes in flight so cost no registers, which the backward pass needs for its column sums.
 // WHOLE says how a row is fetched:

@@ -100,3 +100,27 @@ def test_shared_weight_without_rows_and_in_bfloat16_gradients(dtype):
     assert torch.equal(dx, want[0])
     flat = lambda t: t.reshape(1, 90, *t.shape[2:])
     check_backward(flat(dy[:, cut]), flat(x[:, cut]), flat(mean[:, cut]), flat(rstd[:, cut]), w[None], dtype, "bf16", flat(dx), dw[None], db[None])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,rows,h", [(3, 50, 96), (2, 700, 48), (2, 500, 256), (4, 300, 512), (4, 600, 768), (2, 300, 1024), (2, 400, 2048),
+                                      (2, 300, 4096), (1, 60, 8192), (1, 70, 16384), (2, 9, 768)])
+def test_bits_do_not_depend_on_the_layout(N, rows, h, dtype):
+    """The same values on 16 bytes and off them, as rows of a wider buffer and with the workers inside: equal bits of
+    everything that the forward and the backward pass return."""
+    x, dy, w, b = draw(N, rows, h, dtype, seed=h)
+
+    def elsewhere(t, pad, at, inside):
+        shape = (rows, N, h + pad) if inside else (N, rows, h + pad)
+        wide = torch.full((shape[0] * shape[1] * shape[2] + at,), float("nan"), dtype=t.dtype, device="cuda")[at:].view(shape)
+        cut = (wide.transpose(0, 1) if inside else wide)[..., :h]
+        cut.copy_(t)
+        return cut
+
+    y, mean, rstd = forward(x, w, b)
+    want = (y, mean, rstd) + backward(dy, x, mean, rstd, w)
+    for pad, at, inside in ((1, 0, False), (8, 0, True), (5, 3, False), (0, 1, True)):
+        xs, ds = elsewhere(x, pad, at, inside), elsewhere(dy, pad, at, inside)
+        got = forward(xs, w, b) + backward(ds, xs, mean, rstd, w)
+        for name, p, q in zip(("y", "mean", "rstd", "dx", "dweight", "dbias"), got, want):
+            assert torch.equal(p, q), (name, pad, at, inside, float((p.float() - q.float()).abs().max()))
