@@ -124,3 +124,29 @@ def test_bits_do_not_depend_on_the_layout(N, rows, h, dtype):
         got = forward(xs, w, b) + backward(ds, xs, mean, rstd, w)
         for name, p, q in zip(("y", "mean", "rstd", "dx", "dweight", "dbias"), got, want):
             assert torch.equal(p, q), (name, pad, at, inside, float((p.float() - q.float()).abs().max()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,rows,h,shared", [(3, 5, 96, False), (2, 700, 768, False), (4, 1500, 1001, False), (700, 20, 48, False), (2, 300, 4096, False),
+                                             (2, 40, 9000, False), (1, 9000, 16, False), (3, 5, 96, True), (37, 64, 768, True), (2, 40, 9000, True)])
+def test_workspace_of_exactly_the_reported_size(N, rows, h, shared, dtype):
+    """Nothing beyond liec_layer_norm_workspace_bytes is written, and half of it is refused."""
+    x, dy, w, b = draw(N, rows, h, dtype, seed=N + rows)
+    vector = torch.empty(h if shared else N * h, device="cuda").view(*(() if shared else (N,)), h)
+    if shared:
+        w, b = w[0].contiguous(), b[0].contiguous()
+        dy = dy[:, :1].expand(N, rows, h)      # (not foldable into one worker)
+    _, mean, rstd = forward(x, w, b)
+    layout = liec._layout
+    d, _, need = liec._ln_desc(layout(x), layout(dy), layout(x), layout(w), None, layout(vector), layout(vector), 0.0)
+    assert need == liec.liec_layer_norm_workspace_bytes(d) and bool(d.shared_grads) == shared
+    memory = torch.full((need + (2 << 20),), 77, dtype=torch.uint8, device="cuda")
+    inside = memory[1 << 20:][:need]
+    dx, dw, db = backward(dy, x, mean, rstd, w, workspace=inside)
+    assert (memory[:1 << 20] == 77).all() and (memory[(1 << 20) + need:] == 77).all()
+    flat = (lambda t: t.reshape(1, N * rows, *t.shape[2:])) if shared else (lambda t: t)
+    one = (lambda t: t[None]) if shared else (lambda t: t)
+    check_backward(flat(dy), flat(x), flat(mean), flat(rstd), one(w), dtype, "f32", flat(dx), one(dw), one(db))
+    with pytest.raises(liec.LiecError) as err:
+        backward(dy, x, mean, rstd, w, workspace=inside[:need // 2])
+    assert err.value.status == 3

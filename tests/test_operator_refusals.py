@@ -55,3 +55,15 @@ def test_layouts_with_a_shared_gradient(lib, name, x, dy):
         assert [g * group + r * row for g in range(d.groups) for r in range(d.rows)] == want
     assert bool(d.shared_grads) == (d.groups > 1)
     assert need >= 0
+
+
+@pytest.mark.parametrize("shared", [0, 1])
+@pytest.mark.parametrize("groups,rows,cols", [(1, 1, 1), (1, 4096, 768), (32, 4096, 768), (1, 1 << 20, 1024), (2, 2_200_000, 1024), (4, 4096, 4096),
+                                              (300, 7, 96), (5000, 40, 64), (4, 4096, 16384), (1, 512, 65536), (65535, 1, 8)])
+def test_workspace_is_what_the_pieces_need(lib, groups, rows, cols, shared):
+    """A piece is two rows of column sums: one per resident CTA (148 SMs, at most 3 each) or per 1024 rows of a CTA of
+    at least one row at a time, whichever is more, and one more per worker."""
+    d = desc(groups=groups, rows=rows, cols=cols, shared_grads=shared, x_group_stride=rows * 64)
+    need = lib.liec_layer_norm_workspace_bytes(C.byref(d))
+    pieces = max(3 * 148, -(-groups * rows // 1024)) + 1 + groups
+    assert 8 * cols * groups <= need <= 8 * cols * pieces + 256
