@@ -268,7 +268,8 @@ liec_status liec_sumsq(liec_ctx *ctx, int32_t which, const void *grads, double *
  *   out       device, [N][d] of cfg.grad_dtype, 16-byte aligned: grads itself (a row with c_i = 1 is then
  *             left alone) or memory that does not overlap it
  *   max_norm  > 0; infinity asks for the norms alone (and, out of place, a copy)
- *   zero_nonfinite  != 0: the row of a worker whose norm is infinite or NaN is written as zeros, so
+ *   zero_nonfinite  != 0: the row of a worker whose norm is infinite or NaN (in binary64: one of its entries
+ *             is; a finite row's norm may only be too large for `norms`) is written as zeros, so
  *             that one bad gradient does not enter the global error for good; 0: it is treated by the
  *             formula (c_i = 0 for an infinite norm, 1 for a NaN)
  *   norms     device, [N] binary32 (rounded once), or NULL
@@ -304,7 +305,8 @@ liec_status liec_gather_grads(liec_ctx *ctx, void *out, float max_norm, int32_t 
  *   xh = (x - m) r,  dx = r (dy w - mean(dy w) - xh mean(dy w xh)),
  *   dw = sum over the worker's rows of dy xh,  db = sum over the worker's rows of dy
  * Evaluated in binary32; outputs are rounded once to their type.  The variance is mean(x^2) - m^2 where
- * m^2 is at most a quarter of it, and summed around the mean in all other rows.  The order of the sums
+ * m^2 is at most a quarter of it, and summed around the mean in all other rows.  A row of finite entries whose
+ * squares leave binary32 (magnitudes beyond about 1e19) has an infinite variance there, r = 0 and y = b.  The order of the sums
  * depends on the sizes and types alone, not on strides or alignment (no atomics): equal calls give equal bits.  A row with an infinity or NaN gives NaN in that row (and in dw) only.
  *
  * No context is needed.  All strides are in elements and >= 0; the last axis is contiguous.  Rows that

@@ -332,7 +332,9 @@ def _ln_forward(raw, device, x, weight, bias, eps, y):
 def liec_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None, stream=None):
     """Layer norm of [N, rows, h] (or [rows, h]) activations with per-worker float32 weight and bias
     [N, h] (any stride between workers, e.g. ``params[:, a:a + h]``) or one [h] vector for all.
-    Returns (y, mean, rstd); mean and rstd [N, rows] float32 are what the backward pass needs."""
+    Returns (y, mean, rstd); mean and rstd [N, rows] float32 are what the backward pass needs.  Automatic
+    differentiation does not see the call: nothing that is returned requires a gradient, whatever x, weight and bias
+    do; the gradients come from liec_layer_norm_backward."""
     device = _device_of("x", x)
     for name, t in (("weight", weight), ("bias", bias), ("y", y)):
         if t is not None and t.get_device() != device:
@@ -532,7 +534,10 @@ class Context:
     def liec_set_tensors(self, tensors, stream=None):
         """The N*T gradient tensors of liec_gather_grads: N sequences of T contiguous CUDA tensors (None: no
         gradient) with the segments' element counts, all float32 or all bfloat16.  They are referenced, not
-        copied; this object keeps them alive."""
+        copied; this object keeps them alive until the next call (a gather on another stream than the tensors'
+        own has to be over by then, and a graph that captured this call needs them for as long as it is replayed).
+        Every tensor is checked here, about 0.4 us of host time each: a program whose gradients stay in the
+        same buffers calls this once, one whose backward pass leaves new tensors before every gather."""
         t = self._torch
         if len(tensors) != self.N or any(len(ts) != self.T for ts in tensors):
             raise ValueError("tensors must be N sequences of T tensors")

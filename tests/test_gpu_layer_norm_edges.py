@@ -150,3 +150,22 @@ def test_workspace_of_exactly_the_reported_size(N, rows, h, shared, dtype):
     with pytest.raises(liec.LiecError) as err:
         backward(dy, x, mean, rstd, w, workspace=inside[:need // 2])
     assert err.value.status == 3
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("h", [5, 768, 4096, 9000])
+def test_rows_whose_squares_leave_binary32(h, dtype):
+    """Finite entries beyond 1e19: infinite variance, so r = 0 and y = b; the rows beside them are not touched by it."""
+    x, dy, w, b = draw(1, 4, h, dtype, seed=17)
+    x, want = x.clone(), forward(x, w, b)
+    x[0, 2, h // 2] = -3.0e38      # as a mask value
+    y, mean, rstd = forward(x, w, b)
+    assert rstd[0, 2] == 0 and torch.isfinite(mean).all() and torch.equal(y[0, 2], b[0].to(DT[dtype]))
+    for p, q in zip((y, mean, rstd), want):
+        assert torch.equal(p[0, [0, 1, 3]], q[0, [0, 1, 3]])
+
+
+def test_outputs_have_no_graph():
+    x, dy, w, b = draw(2, 8, 64, "f32", seed=1)
+    out = forward(x.clone().requires_grad_(), w.clone().requires_grad_(), b)
+    assert not any(t.requires_grad for t in out)
