@@ -285,7 +285,7 @@ liec_status liec_clip_grads(liec_ctx *ctx, const void *grads, void *out, float m
  *            seg_offsets[t+1] - seg_offsets[t] consecutive elements of `dtype` (LIEC_F32 or LIEC_BF16,
  *            whatever the rows' type) at any element-aligned address; NULL: no gradient, counts as zeros
  * liec_set_tensors copies the pointers (as kernel arguments: no synchronisation, and it can be
- * captured), ordered on `stream`; the tensors themselves are read by liec_gather_grads and must not
+ * captured; a context's first call takes host memory for N*T pointers), ordered on `stream`; the tensors themselves are read by liec_gather_grads and must not
  * overlap `out` (LIEC_ERR_INVALID_ARG).  The table serves any number of liec_gather_grads calls until the next
  * liec_set_tensors.  liec_gather_grads returns LIEC_ERR_STATE when no table was given.  A captured
  * liec_set_tensors writes the table whenever its graph is replayed (its tensors then have to be there still).  Where the

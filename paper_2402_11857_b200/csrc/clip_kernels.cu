@@ -8,9 +8,12 @@
 // No entry can be written before the whole row has been read, so HBM's part is one read and one write only
 // if the row is still on the chip when it is scaled.  Short rows: one cluster per row (clip_cluster_kernel).
 // Others: one kernel that sums everything, then scales everything (clip_stream_kernel); it moves its two reads and
-// one write at HBM's rate (GPT-2-small list, eight workers in bfloat16: 905 us = 6.6 TB/s).  Scaling row by row,
+// one write at HBM's rate (GPT-2-small list, eight workers in bfloat16: 914 us = 6.5 TB/s).  Scaling row by row,
 // behind the row's sum, was built and measured too: L2 keeps only the last 60 to 70 MB, and the wait
-// for each row's norm costs more than that saves (1046 us; ResNet-18 list 189 against 177 us).
+// for each row's norm costs more than that saves (1046 us; ResNet-18 list 189 against 178 us).
+// Between the two, rows of some hundred tiles are bound by neither HBM nor the launch: every tile is fetched a second time
+// although all of them would fit the rings together, and the start, the tickets of few tiles and the join of
+// each row are not hidden (8 rows of 64 tiles in binary32 17 us, of 512 tiles 73 us; bytes at HBM's rate 5 and 41).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -201,7 +204,7 @@ __device__ __forceinline__ bool table_fits(const Params &p, const ClipArgs &a) {
 // 256 threads take a tile, up to four tiles a CTA, up to eight CTAs the cluster.  Every tile sum goes to all of
 // the cluster through distributed shared memory; the cluster meets once; every warp forms the row's factor
 // from the sums; the tiles are scaled (out of L1 or L2).  One launch, nothing to prepare: what such a row
-// costs is latency: four rows of 8 tiles 4.7 us, of 32 tiles 8.8 us (binary32).
+// costs is latency: four rows of 8 tiles 4.9 us, of 32 tiles 8.8 us (binary32).
 constexpr int CLUSTER_TILES = 32, CLUSTER_SIZE = 8;
 
 template <typename ST, typename DT>

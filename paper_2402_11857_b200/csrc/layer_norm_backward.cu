@@ -2,12 +2,12 @@
 // q = dy w:  dx = r (q - mean(q) - xh mean(q xh));  per worker  dw = sum over rows of dy xh,  db = sum over
 // rows of dy.  x and dy cross HBM once: the column sums stay in the registers of the threads that own
 // the columns, for all the rows of a CTA, and meet in two steps (slots of a CTA, then CTAs).
-// Bfloat16, 32 x 4096 rows of 768: 104 us, of which 3 us the second step: 5.8 TB/s.  Wider rows are bound by the
-// instructions of 12 to 16 warps per SM, all that the column sums leave registers for: 4 x 4096 of 4096 81 us
+// Bfloat16, 32 x 4096 rows of 768: 105 us, of which 3 us the second step: 5.8 TB/s.  Wider rows are bound by the
+// instructions of 12 to 16 warps per SM, all that the column sums leave registers for: 4 x 4096 of 4096 80 us
 // = 5.0 TB/s with half of the issue slots in use, warps waiting for the row's exchange and for shared memory
 // (measured beside it: 8 elements per thread and twice the threads 93 us, 32 per thread 85 us, two rows per exchange
 // 95 us, three CTAs per SM with both rows read twice 88 us, SMs dealt rows by speed, which makes more pieces,
-// 119 us).  Binary32, 4 x 8192 of 2048: 138.5 us = 5.8 TB/s.
+// 119 us).  Binary32, 4 x 8192 of 2048: 139 us = 5.8 TB/s.
 #include "layer_norm_common.cuh"
 
 namespace liec {
@@ -355,7 +355,7 @@ cudaError_t launch_layer_norm_backward(LnBackward a, int dtype, cudaStream_t st)
                            ln_whole(a.dy, a.dy_row, a.dy_group, a.rows, a.groups, a.cols, esz) &&
                            (!a.dx || ln_whole(a.dx, a.dx_row, a.dx_group, a.rows, a.groups, a.cols, esz));
         const LnPlan p = ln_plan(a.groups, a.rows, a.cols, a.shared != 0);
-        if (a.shared && (a.dweight || a.dbias)) {   // (the places without a piece)
+        if (a.shared && (a.dweight || a.dbias)) {   // the places without a piece (all of it: 3 us of 107, 32 x 4096 of 768)
             const cudaError_t e = cudaMemsetAsync(a.part_w, 0, layer_norm_workspace(a.groups, a.rows, a.cols, true), st);
             if (e != cudaSuccess) return e;
         }

@@ -14,8 +14,8 @@
 //          they lie (cp.async of whole granules, of a part at the end; the elements of a first granule that the
 //          row does not fill one by one), and a thread cuts its chunk out of two of them; results go back through
 //          the ring and leave as granules too.  A barrier of the slot per row.  (32 x 4095 rows of 767 bfloat16:
-//          forward 110 us, backward 192 us; 114 and 846 us with 2-byte loads through registers.  768 columns,
-//          which the first form takes: 69 and 104 us.)
+//          forward 109 us, backward 191 us; 114 and 846 us with 2-byte loads through registers.  768 columns,
+//          which the first form takes: 71 and 105 us.)
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

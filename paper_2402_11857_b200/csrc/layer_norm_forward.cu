@@ -1,11 +1,11 @@
 // Layer normalisation, forward pass.  Per row: m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps),
 // y = (x - m) r w + b.  A row is read into registers once, its two sums meet (one exchange), y is written: every
-// element crosses HBM once, and HBM bounds it.  Bfloat16: 32 x 4096 rows of 768 69.5 us (5.8 TB/s; a copy of the
+// element crosses HBM once, and HBM bounds it.  Bfloat16: 32 x 4096 rows of 768 70.7 us (5.7 TB/s; a copy of the
 // array takes 62.4 us), 4 x 4096 of 4096 44.8 us (copy 42.6), 16 x 4096 of 1024 51.5 us (copy 42.6: twelve warps
 // per SM, which the 32 elements per thread leave room for); binary32, 4 x 8192 of 2048 88 us (copy 82.5).  Rows of
 // odd width cost instructions on top (see the common header), calls below a few MB are latency: 4 x 32 rows of 256
-// 2.6 us.  Two rows per turn, where the registers hold them, halve the exchanges; with E = 24 and 32 that spills
-// (93 against 70 us at 768 columns).
+// 3.5 us.  Two rows per turn, where the registers hold them, halve the exchanges; with E = 24 and 32 that spills
+// (93 against 71 us at 768 columns).
 #include "layer_norm_common.cuh"
 
 namespace liec {
