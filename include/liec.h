@@ -354,6 +354,123 @@ liec_status liec_layer_norm_backward(const liec_layer_norm_desc *desc, const voi
                                      void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Activations kept in 8 bits between the forward and the backward pass ("checkpoints").  Every 32 consecutive channels of a
+ * row (a block; the last one of a row is filled up with zeros) become 32 signed bytes q and one byte e + 127:
+ *   e = the least integer >= -126 with round(max |x| 2^-e) <= 127,   q = round(x 2^-e)   (to nearest, ties to even)
+ *   x^ = q 2^e
+ * (e is 121 at most and q held to +-127 there, so that x^ is finite.)  x^ is exact in binary32 and in bfloat16;
+ * |x - x^| <= 2^(e-1) (2^e for e = 121), which is at most max |x| / 127 where max |x| >= 2^-120.  A block with an infinity or
+ * NaN gets the byte 255 and q = 0 and comes back as NaN.  33 bytes per 32 channels.
+ *
+ * No context is needed here either.  Strides are in elements and >= 0, the last axis of every array is contiguous, any
+ * element alignment is accepted (16-byte aligned rows are faster) unless said otherwise; rows that are read may overlap or
+ * repeat, rows that are written may not, and no output may overlap an input or another output (LIEC_ERR_INVALID_ARG, where
+ * that can be told as for the layer normalisation).
+ *   x       device, [workers][rows][cols] of dtype
+ *   q       device, 16-byte aligned, [workers][rows][liec_activation_cols(cols)] without gaps
+ *   scales  device, [workers][rows][liec_activation_cols(cols) / 32] without gaps
+ */
+#define LIEC_ACTIVATION_BLOCK 32
+typedef struct {
+    int32_t workers;        /* N >= 1, at most 65535 */
+    int64_t rows;           /* rows per worker, 0 .. 2^31 - 1 */
+    int32_t cols;           /* channels of a row, 1 .. LIEC_ACTIVATION_MAX_COLS */
+    int32_t dtype;          /* liec_dtype of x */
+    int64_t x_row_stride, x_worker_stride;
+} liec_activation_desc;
+#define LIEC_ACTIVATION_MAX_COLS 65536
+
+/* cols rounded up to whole blocks; 0 for cols out of range. */
+int64_t liec_activation_cols(int64_t cols);
+liec_status liec_activation_compress(const liec_activation_desc *desc, const void *x, int8_t *q, uint8_t *scales, void *stream);
+liec_status liec_activation_restore(const liec_activation_desc *desc, const int8_t *q, const uint8_t *scales, void *x, void *stream);
+
+/*
+ * Group normalisation of N workers' images with an activation, channels last, and its backward pass.  An image (a worker's
+ * sample) has `pixels` rows of `channels`; the channels form `groups` groups of equal width, each normalised over all its
+ * channels and pixels, with the worker's own weight w and bias b per channel:
+ *   m = mean(x),  r = 1 / sqrt(mean((x - m)^2) + eps),  xh = (x - m) r,  z = xh w + b,  y = act(z)
+ *   act: z (LIEC_ACT_NONE), max(z, 0) (LIEC_ACT_RELU), z / (1 + exp(-z)) (LIEC_ACT_SILU)
+ *   dz = dy act'(z),  dx = r (dz w - mean(dz w) - xh mean(dz w xh)),
+ *   dw = sum over the worker's samples and pixels of dz xh,  db = the same of dz       (act'(z) = 1 for z > 0, else 0, for ReLU)
+ * Evaluated in binary32 (joins of partial sums in binary64), outputs rounded once to their type.  Squares are summed around a value of the channel, so
+ * a far mean costs no digits; entries whose squares leave binary32 (beyond about 1e18) are not provided for.  On which side
+ * of zero a ReLU's z lies is decided as in binary64 from the given x, mean, rstd, w and b.  Equal calls give equal bits (no
+ * atomics).  A group with an infinity or NaN gives NaN in that group of that image, and in dw and db of its channels.
+ *
+ * The forward pass can leave the checkpoint of x (q and scales, as liec_activation_compress of its [workers][samples pixels]
+ * [channels] rows would) from the same read of x, and the backward pass can read the checkpoint in place of x: the formulas
+ * then hold with x^ for x and with mean and rstd as given.  Alignment, strides and overlaps as above.
+ */
+typedef enum { LIEC_ACT_NONE = 0, LIEC_ACT_RELU = 1, LIEC_ACT_SILU = 2 } liec_activation;
+#define LIEC_GROUP_NORM_MAX_CHANNELS 65536
+typedef struct {
+    int32_t workers, samples;   /* N >= 1, at most 65535; images per worker, >= 0 */
+    int64_t pixels;             /* rows per image, 0 .. 2^31 - 1 */
+    int32_t channels, groups;   /* 1 .. LIEC_GROUP_NORM_MAX_CHANNELS; a divisor of channels */
+    int32_t dtype;              /* liec_dtype of x, y, dy, dx */
+    int32_t grad_dtype;         /* liec_dtype of dweight and dbias */
+    int32_t activation;         /* liec_activation */
+    float eps;                  /* >= 0; not used by the backward pass */
+    int64_t x_pixel_stride, x_sample_stride, x_worker_stride;
+    int64_t y_pixel_stride, y_sample_stride, y_worker_stride;      /* of y in the forward pass, of dy in the backward pass */
+    int64_t dx_pixel_stride, dx_sample_stride, dx_worker_stride;
+    int64_t weight_stride, bias_stride;     /* from worker to worker: d for a range of the parameter rows, 0 = shared */
+    int64_t dweight_stride, dbias_stride;
+    int32_t shared_grads;       /* != 0: dweight and dbias are one vector [channels] each, summed over the workers as well */
+} liec_group_norm_desc;
+
+/* Bytes of device workspace of a forward (backward = 0) or backward pass; 0 where none is needed, and for a bad desc. */
+size_t liec_group_norm_workspace_bytes(const liec_group_norm_desc *desc, int32_t backward);
+
+/*
+ *   x, y         device, [workers][samples][pixels][channels] of dtype
+ *   weight, bias device, binary32, or NULL for ones and zeros
+ *   mean, rstd   device, [workers][samples][groups] binary32 without gaps, written (undefined for images without pixels)
+ *   q, scales    device, the checkpoint to write, or both NULL
+ *   workspace    device, 16-byte aligned, scratch of this call alone (NULL where none is needed)
+ */
+liec_status liec_group_norm_forward(const liec_group_norm_desc *desc, const void *x, const float *weight, const float *bias, void *y,
+                                    float *mean, float *rstd, int8_t *q, uint8_t *scales, void *workspace, size_t workspace_bytes,
+                                    void *stream);
+
+/*
+ *   dy           device, [workers][samples][pixels][channels] of dtype
+ *   x | q, scales  the activations, or (x NULL) their checkpoint
+ *   mean, rstd   as the forward pass stored them;  weight, bias  as given to it (bias matters with an activation only)
+ *   dx           device, of dtype;  dweight, dbias  device, [workers][channels] of grad_dtype ([channels] with shared_grads):
+ *                overwritten, also without samples or pixels (zeros).  Each of the three may be NULL: it is not computed.
+ *   workspace    device, 16-byte aligned, scratch of this call alone
+ */
+liec_status liec_group_norm_backward(const liec_group_norm_desc *desc, const void *dy, const void *x, const int8_t *q, const uint8_t *scales,
+                                     const float *mean, const float *rstd, const float *weight, const float *bias, void *dx,
+                                     void *dweight, void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Weight gradient of N workers' linear layers (or 1 x 1 convolutions) from the checkpoint of their input:
+ *   dW[o][c] = sum over the worker's rows t of dy[t][o] x^[t][c]
+ * Products are exact (a bfloat16 dy times x^; a binary32 dy enters as three bfloat16 parts that add up to it) and are summed in binary32;
+ * rounded once to the gradient's type.  Equal calls give equal bits.
+ *   dy        device, [workers][rows][out] of dtype
+ *   q, scales device, checkpoint of x [workers][rows][in]
+ *   dweight   device, [workers][out][in] of grad_dtype, overwritten (zeros without rows)
+ *   workspace device, 16-byte aligned, scratch of this call alone (NULL where none is needed)
+ * Alignment, strides and overlaps as above.
+ */
+typedef struct {
+    int32_t workers;        /* N >= 1, at most 65535 */
+    int64_t rows;           /* rows (tokens, pixels) per worker, 0 .. 2^31 - 1 */
+    int32_t in, out;        /* 1 .. LIEC_ACTIVATION_MAX_COLS each */
+    int32_t dtype;          /* liec_dtype of dy */
+    int32_t grad_dtype;     /* liec_dtype of dweight */
+    int64_t dy_row_stride, dy_worker_stride;
+    int64_t dweight_row_stride, dweight_worker_stride;   /* from output to output (>= in), from worker to worker */
+} liec_weight_grad_desc;
+size_t liec_weight_grad_workspace_bytes(const liec_weight_grad_desc *desc);
+liec_status liec_weight_grad(const liec_weight_grad_desc *desc, const void *dy, const int8_t *q, const uint8_t *scales, void *dweight,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Telemetry fused into the iteration's own passes: the quantities behind the paper's figure of
  * error norms (||e_t||) and its table of measured delta (Def. 1: delta = 1 - ||x - C(x)||^2 / ||x||^2,
  * worker side x = g^i, server side x = v) at no extra pass over the model-sized arrays.

@@ -1,0 +1,156 @@
+// Group normalisation with an activation, channels last: what the kernels share.
+//
+// z = (x - m) A + b with A = r w is evaluated from d = x - m (rounded once, so a far mean costs no digits), one fused
+// operation more.  A thread owns one 16-byte chunk of channels and walks down the pixels, so what belongs to a channel
+// stays in registers and a channel's sums are the thread's until they meet those of the other pixels.
+#pragma once
+#include "activation.cuh"
+
+namespace liec {
+
+constexpr int GN_THREADS = 256;
+
+// Where a chunk of x comes from: the activations themselves, or their checkpoint.
+template <typename T>
+struct GnFromX {
+    using Raw = uint4;
+    const T *row;
+    int64_t pixel;
+    __device__ __forceinline__ GnFromX(const GnArgs &a, int worker, int sample, int64_t p)
+        : row(static_cast<const T *>(a.x) + worker * a.x_worker + sample * a.x_sample + p * a.x_pixel), pixel(a.x_pixel) {}
+    __device__ __forceinline__ Raw load(int64_t p, int c, int cols) const { return load_chunk(row + p * pixel, c, cols); }
+    template <int P>
+    static __device__ __forceinline__ void centred(const Raw &raw, const F2 (&minus)[P], F2 (&d)[P]) {
+        LnChunk<T>::read(raw, d);
+#pragma unroll
+        for (int k = 0; k < P; ++k) d[k] = add(d[k], minus[k]);
+    }
+};
+
+template <typename T>
+struct GnFromCheckpoint {
+    struct Raw { uint32_t w[Bits<T>::VEC / 4]; uint32_t byte; };
+    const int8_t *q;
+    const uint8_t *scales;
+    int64_t cols;
+    __device__ __forceinline__ GnFromCheckpoint(const GnArgs &a, int worker, int sample, int64_t p) {
+        cols = (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK;
+        const int64_t row = ((int64_t)worker * a.samples + sample) * a.pixels + p;
+        q = a.q + row * cols;
+        scales = a.scales + row * (cols / CK_BLOCK);
+    }
+    __device__ __forceinline__ Raw load(int64_t p, int c, int) const {
+        Raw r;
+        const int8_t *at = q + p * cols + c;
+        if constexpr (Bits<T>::VEC == 8) {
+            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(at));
+            r.w[0] = v.x;
+            r.w[1] = v.y;
+        } else {
+            r.w[0] = __ldg(reinterpret_cast<const uint32_t *>(at));
+        }
+        r.byte = __ldg(scales + p * (cols / CK_BLOCK) + c / CK_BLOCK);
+        return r;
+    }
+    template <int P>
+    static __device__ __forceinline__ void centred(const Raw &raw, const F2 (&minus)[P], F2 (&d)[P]) {
+        const F2 power = f2(ck_power(raw.byte));
+#pragma unroll
+        for (int k = 0; k < P; k += 2) ck_unpack(raw.w[k / 2], d[k], d[k + 1]);
+#pragma unroll
+        for (int k = 0; k < P; ++k) d[k] = fma(d[k], power, minus[k]);   // (q 2^e is exact: one rounding)
+    }
+};
+
+// The gate s = 1 / (1 + exp(-z)) of SiLU.  Results in bfloat16 take the short exponential: its relative error, |z| 2^-23,
+// is far below a bfloat16 step wherever the gate is not zero.
+template <typename T>
+__device__ __forceinline__ float gn_exp(float z) { return sizeof(T) == 4 ? fminf(expf(-z), 1e30f) : __expf(-z); }
+
+template <typename T, int ACT>
+__device__ __forceinline__ float gn_act(float z) {
+    if constexpr (ACT == LIEC_ACT_RELU) return z < 0.0f ? 0.0f : z;   // (NaN stays)
+    if constexpr (ACT == LIEC_ACT_SILU) return __fdividef(z, 1.0f + gn_exp<T>(z));
+    return z;
+}
+
+// dy silu'(z), silu' = s (1 + z (1 - s)).  1 - s = exp(-z) s keeps its digits where s is near one; in bfloat16 the
+// difference has enough of them.
+template <typename T>
+__device__ __forceinline__ float gn_silu_slope(float z, float dy) {
+    const float e = gn_exp<T>(z), s = __fdividef(1.0f, 1.0f + e);
+    return dy * (s * __fmaf_rn(z, sizeof(T) == 4 ? e * s : 1.0f - s, 1.0f));
+}
+
+// z from its definition in binary64.
+__device__ __noinline__ bool gn_positive(const GnArgs &a, int worker, int64_t image, int c, float x) {
+    const int64_t g = image * a.groups + c / (a.channels / a.groups);
+    const double w = a.weight ? (double)a.weight[worker * a.weight_stride + c] : 1.0, b = a.bias ? (double)a.bias[worker * a.bias_stride + c] : 0.0;
+    return ((double)x - (double)a.mean[g]) * (double)a.rstd[g] * w + b > 0.0;
+}
+
+// What belongs to a thread's channels: -m, A = r w, b; zeros beyond the last channel.
+template <int P>
+struct GnChannels {
+    F2 minus[P], scale[P], bias[P];
+    __device__ __forceinline__ void read(const GnArgs &a, int worker, int64_t image, int c) {
+        const int width = a.channels / a.groups;
+#pragma unroll
+        for (int k = 0; k < 2 * P; ++k) {
+            float m = 0.0f, s = 0.0f, b = 0.0f;
+            if (c + k < a.channels) {
+                const int64_t g = image * a.groups + (c + k) / width;
+                m = -a.mean[g];
+                s = a.rstd[g] * (a.weight ? __ldg(a.weight + worker * a.weight_stride + c + k) : 1.0f);
+                b = a.bias ? __ldg(a.bias + worker * a.bias_stride + c + k) : 0.0f;
+            }
+            set(minus[k / 2], k % 2, m);
+            set(scale[k / 2], k % 2, s);
+            set(bias[k / 2], k % 2, b);
+        }
+    }
+    static __device__ __forceinline__ void set(F2 &p, int odd, float v) { p = odd ? f2(lo(p), v) : f2(v, 0.0f); }
+};
+
+// dz = dy act'(z) from d = x - m.  The sign of z decides for ReLU: z carries at most 4 2^-24 (|b| + |z|) of rounding, so
+// where |z| is above 2^-20 |b| its sign is right; elsewhere it is taken from binary64.
+template <typename T, int ACT, typename X, int P>
+__device__ __forceinline__ void gn_slope(const GnArgs &a, int worker, int64_t image, int c, const GnChannels<P> &ch, const typename X::Raw &raw,
+                                         const F2 (&d)[P], const F2 (&dy)[P], F2 (&dz)[P]) {
+    if constexpr (ACT == LIEC_ACT_NONE) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) dz[k] = dy[k];
+        return;
+    }
+    F2 z[P];
+#pragma unroll
+    for (int k = 0; k < P; ++k) z[k] = fma(d[k], ch.scale[k], ch.bias[k]);
+    if constexpr (ACT == LIEC_ACT_SILU) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) dz[k] = f2(gn_silu_slope<T>(lo(z[k]), lo(dy[k])), gn_silu_slope<T>(hi(z[k]), hi(dy[k])));
+    }
+    if constexpr (ACT == LIEC_ACT_RELU) {
+        uint32_t on = 0u, near = 0u;
+        constexpr float NEAR = 9.5367431640625e-7f;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            on |= (lo(z[k]) > 0.0f ? 1u << 2 * k : 0u) | (hi(z[k]) > 0.0f ? 2u << 2 * k : 0u);
+            near |= (fabsf(lo(z[k])) <= NEAR * fabsf(lo(ch.bias[k])) ? 1u << 2 * k : 0u) | (fabsf(hi(z[k])) <= NEAR * fabsf(hi(ch.bias[k])) ? 2u << 2 * k : 0u);
+        }
+        if (near != 0u) {
+            F2 x[P];
+            const F2 none[P] = {};
+            X::centred(raw, none, x);
+#pragma unroll
+            for (int k = 0; k < 2 * P; ++k)
+                if ((near >> k & 1u) && c + k < a.channels) {
+                    const bool positive = gn_positive(a, worker, image, c + k, k % 2 ? hi(x[k / 2]) : lo(x[k / 2]));
+                    on = positive ? on | 1u << k : on & ~(1u << k);
+                }
+        }
+#pragma unroll
+        for (int k = 0; k < P; ++k) dz[k] = f2(on >> 2 * k & 1u ? lo(dy[k]) : 0.0f, on >> 2 * k & 2u ? hi(dy[k]) : 0.0f);
+    }
+}
+
+}  // namespace liec

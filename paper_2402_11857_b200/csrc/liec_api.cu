@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "../../include/liec.h"
+#include "activation.h"
 #include "kernels.h"
 #include "layer_norm.h"
 #include "overlap.h"
@@ -1067,3 +1068,5 @@ void liec_destroy(liec_ctx *c) {
 }
 
 }  // extern "C"
+
+liec_status liec::refuse(liec_status st, const char *text) { return ln_refuse(st, text); }

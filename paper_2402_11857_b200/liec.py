@@ -15,6 +15,8 @@ import numpy as np
 COMP_IDENTITY, COMP_SCALED_SIGN, COMP_TOPK, COMP_RANDK = 0, 1, 2, 3
 SUMSQ_ERROR, SUMSQ_GRADS, SUMSQ_PARAMS = 0, 1, 2
 F32, BF16 = 0, 1
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
+ACTIVATION_BLOCK = 32
 
 STATUS_NAMES = {0: "LIEC_OK", 1: "LIEC_ERR_INVALID_ARG", 2: "LIEC_ERR_UNSUPPORTED", 3: "LIEC_ERR_WORKSPACE",
                 4: "LIEC_ERR_STATE", 5: "LIEC_ERR_CUDA", 6: "LIEC_ERR_DEVICE_CHECK"}
@@ -50,6 +52,27 @@ class liec_layer_norm_desc(C.Structure):
                 ("dx_row_stride", C.c_int64), ("dx_group_stride", C.c_int64),
                 ("weight_stride", C.c_int64), ("bias_stride", C.c_int64),
                 ("dweight_stride", C.c_int64), ("dbias_stride", C.c_int64), ("shared_grads", C.c_int32)]
+
+
+class liec_activation_desc(C.Structure):
+    _fields_ = [("workers", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int32), ("dtype", C.c_int32),
+                ("x_row_stride", C.c_int64), ("x_worker_stride", C.c_int64)]
+
+
+class liec_group_norm_desc(C.Structure):
+    _fields_ = [("workers", C.c_int32), ("samples", C.c_int32), ("pixels", C.c_int64), ("channels", C.c_int32), ("groups", C.c_int32),
+                ("dtype", C.c_int32), ("grad_dtype", C.c_int32), ("activation", C.c_int32), ("eps", C.c_float),
+                ("x_pixel_stride", C.c_int64), ("x_sample_stride", C.c_int64), ("x_worker_stride", C.c_int64),
+                ("y_pixel_stride", C.c_int64), ("y_sample_stride", C.c_int64), ("y_worker_stride", C.c_int64),
+                ("dx_pixel_stride", C.c_int64), ("dx_sample_stride", C.c_int64), ("dx_worker_stride", C.c_int64),
+                ("weight_stride", C.c_int64), ("bias_stride", C.c_int64),
+                ("dweight_stride", C.c_int64), ("dbias_stride", C.c_int64), ("shared_grads", C.c_int32)]
+
+
+class liec_weight_grad_desc(C.Structure):
+    _fields_ = [("workers", C.c_int32), ("rows", C.c_int64), ("in_", C.c_int32), ("out", C.c_int32), ("dtype", C.c_int32), ("grad_dtype", C.c_int32),
+                ("dy_row_stride", C.c_int64), ("dy_worker_stride", C.c_int64),
+                ("dweight_row_stride", C.c_int64), ("dweight_worker_stride", C.c_int64)]
 
 
 def load_library(path: Optional[str] = None) -> C.CDLL:
@@ -117,6 +140,23 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.liec_layer_norm_forward.restype = C.c_int
     lib.liec_layer_norm_backward.argtypes = [lnp, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     lib.liec_layer_norm_backward.restype = C.c_int
+    acp, gnp, wgp = C.POINTER(liec_activation_desc), C.POINTER(liec_group_norm_desc), C.POINTER(liec_weight_grad_desc)
+    lib.liec_activation_cols.argtypes = [C.c_int64]
+    lib.liec_activation_cols.restype = C.c_int64
+    lib.liec_activation_compress.argtypes = [acp, vp, vp, vp, vp]
+    lib.liec_activation_compress.restype = C.c_int
+    lib.liec_activation_restore.argtypes = [acp, vp, vp, vp, vp]
+    lib.liec_activation_restore.restype = C.c_int
+    lib.liec_group_norm_workspace_bytes.argtypes = [gnp, C.c_int32]
+    lib.liec_group_norm_workspace_bytes.restype = C.c_size_t
+    lib.liec_group_norm_forward.argtypes = [gnp, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.liec_group_norm_forward.restype = C.c_int
+    lib.liec_group_norm_backward.argtypes = [gnp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.liec_group_norm_backward.restype = C.c_int
+    lib.liec_weight_grad_workspace_bytes.argtypes = [wgp]
+    lib.liec_weight_grad_workspace_bytes.restype = C.c_size_t
+    lib.liec_weight_grad.argtypes = [wgp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.liec_weight_grad.restype = C.c_int
     lib.liec_step_host.argtypes = [vp, vp, vp, C.c_float, vp, vp]
     lib.liec_step_host.restype = C.c_int
     lib.liec_get_messages.argtypes = [vp, C.POINTER(liec_messages)]
@@ -381,6 +421,313 @@ def liec_layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, dweight=No
     if workspace is not None and not workspace.is_contiguous():   # (its bytes are counted by its elements)
         raise ValueError("workspace must be contiguous")
     return _launch(device, stream, _ln_backward, device, dy, x, mean, rstd, weight, dx, dweight, dbias, workspace)
+
+
+# ---- activations of N workers: 8-bit checkpoints, group normalisation, weight gradients -------------
+
+def liec_activation_cols(cols: int) -> int:
+    """Columns of a checkpoint's rows: cols rounded up to whole blocks of ACTIVATION_BLOCK."""
+    return -(-int(cols) // ACTIVATION_BLOCK) * ACTIVATION_BLOCK
+
+
+def _pointer(t):
+    return None if t is None else t.data_ptr()
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{name} must be on the device of the first argument")
+
+
+def _dtype_code(name, dtype) -> int:
+    import torch
+    if dtype == torch.bfloat16:
+        return BF16
+    if dtype != torch.float32:
+        raise ValueError(f"{name} must be float32 or bfloat16")
+    return F32
+
+
+def _check_checkpoint(q, scales, rows, cols):
+    """q int8 [*rows, liec_activation_cols(cols)] and scales uint8 [*rows, the same / 32], both contiguous."""
+    import torch
+    wide, rows = liec_activation_cols(cols), tuple(rows)
+    if q.dtype != torch.int8 or tuple(q.shape) != rows + (wide,) or not q.is_contiguous():
+        raise ValueError(f"q must be a contiguous int8 tensor {list(rows + (wide,))}")
+    if scales.dtype != torch.uint8 or tuple(scales.shape) != rows + (wide // ACTIVATION_BLOCK,) or not scales.is_contiguous():
+        raise ValueError(f"scales must be a contiguous uint8 tensor {list(rows + (wide // ACTIVATION_BLOCK,))}")
+
+
+def _new_checkpoint(rows, cols, q, scales, device):
+    import torch
+    wide, rows = liec_activation_cols(cols), tuple(rows)
+    q = _empty(rows + (wide,), torch.int8, device) if q is None else q
+    scales = _empty(rows + (wide // ACTIVATION_BLOCK,), torch.uint8, device) if scales is None else scales
+    _check_checkpoint(q, scales, rows, cols)
+    return q, scales
+
+
+@functools.lru_cache(maxsize=1024)
+def _rows_of(name, layout):
+    """[..., cols] as (workers, rows, cols, row stride, worker stride): the axes in front of the columns, joined where
+    they follow one another without a gap; two may remain."""
+    shape, stride, _ = layout
+    cols, axes = shape[-1], []
+    if cols > 1 and stride[-1] != 1:
+        raise ValueError(f"the last axis of {name} must be contiguous")
+    for n, s in zip(shape[:-1], stride[:-1]):
+        if n == 1:
+            continue
+        if axes and axes[-1][1] == n * s:
+            axes[-1] = (axes[-1][0] * n, s)
+        else:
+            axes.append((n, s))
+    if 0 in shape[:-1]:
+        axes = [(0, cols)]
+    if len(axes) > 2 or (len(axes) == 2 and axes[0][0] > 65535):
+        raise ValueError(f"the axes of {name} in front of the last must join into at most two (the outer one of up to 65535 entries)")
+    if any(s < 0 for _, s in axes):
+        raise ValueError(f"{name} must not have negative strides")
+    axes = [(1, 0)] * (2 - len(axes)) + axes
+    return axes[0][0], axes[1][0], cols, axes[1][1], axes[0][1]
+
+
+@functools.lru_cache(maxsize=1024)
+def _activation_desc(name, layout):
+    d = liec_activation_desc()
+    d.workers, d.rows, d.cols, d.x_row_stride, d.x_worker_stride = _rows_of(name, layout)
+    d.dtype = _dtype_code(name, layout[2])
+    return d, C.byref(d)
+
+
+def _activation_call(raw, device, compress, x, q, scales, shape, dtype):
+    lib = _LIB or load_library()
+    if compress:
+        q, scales = _new_checkpoint(x.shape[:-1], x.shape[-1], q, scales, device)
+    elif x is None:
+        x = _empty(shape, dtype, device)
+    ref = _activation_desc("x", _layout(x))[1]
+    if compress:
+        st = lib.liec_activation_compress(ref, x.data_ptr(), q.data_ptr(), scales.data_ptr(), raw)
+    else:
+        st = lib.liec_activation_restore(ref, q.data_ptr(), scales.data_ptr(), x.data_ptr(), raw)
+    if st != 0:
+        _ln_failed(lib, st)
+    return (q, scales) if compress else x
+
+
+def liec_activation_compress(x, q=None, scales=None, stream=None):
+    """8-bit checkpoint of activations [..., h] (float32 or bfloat16, at least two axes): every 32 consecutive channels as
+    signed bytes and one power of two.  Returns (q, scales): int8 [..., liec_activation_cols(h)] and uint8 [..., the same / 32]."""
+    device = _device_of("x", x)
+    _same_device(device, q=q, scales=scales)
+    if x.dim() < 2:
+        raise ValueError("x must have at least two axes")
+    return _launch(device, stream, _activation_call, device, True, x, q, scales, None, None)
+
+
+def liec_activation_restore(q, scales, cols: int, dtype=None, x=None, stream=None):
+    """What a checkpoint stands for, q 2^e, as [..., cols] of `dtype` (float32 where not given; exact in bfloat16 too), or into `x`."""
+    import torch
+    device = _device_of("q", q)
+    _same_device(device, scales=scales, x=x)
+    if q.dim() < 2:
+        raise ValueError("q must have at least two axes")
+    shape = tuple(q.shape[:-1]) + (int(cols),)
+    _check_checkpoint(q, scales, shape[:-1], cols)
+    if x is not None and (tuple(x.shape) != shape or (dtype is not None and x.dtype != dtype)):
+        raise ValueError(f"x must be {list(shape)} of the given type")
+    return _launch(device, stream, _activation_call, device, False, x, q, scales, shape, dtype or torch.float32)
+
+
+def _gn_strides(name, t, x):
+    """(pixel, sample, worker) strides of [N, samples, pixels, channels] or [samples, pixels, channels]."""
+    shape, stride, dtype = t
+    if shape != x[0] or dtype != x[2]:
+        raise ValueError(f"{name} must have the shape and type of the activations")
+    if shape[-1] > 1 and stride[-1] != 1:
+        raise ValueError(f"the last axis of {name} must be contiguous")
+    return stride[-2], stride[-3], (stride[0] if len(shape) == 4 else 0)
+
+
+def _gn_vector(name, t, x, dtypes):
+    if t is None:
+        return 0
+    shape, stride, dtype = t
+    C_, N = x[0][-1], (x[0][0] if len(x[0]) == 4 else 1)
+    if dtype not in dtypes:
+        raise ValueError(f"{name} must be of type {' or '.join(str(d) for d in dtypes)}")
+    if tuple(shape) not in ((C_,), (N, C_)) or (C_ > 1 and stride[-1] != 1):
+        raise ValueError(f"{name} must be [channels] or [N, channels] with a contiguous last axis")
+    return stride[0] if len(shape) == 2 else 0
+
+
+@functools.lru_cache(maxsize=1024)
+def _gn_desc(x, given, y, dx, weight, bias, dweight, dbias, groups, activation, eps):
+    """Checks the layouts of a call and returns its descriptor and workspace size.  x: shape and type (and strides, where
+    `given`) of the activations; dx None: forward."""
+    import torch
+    both, f32 = (torch.float32, torch.bfloat16), (torch.float32,)
+    shape = x[0]
+    if x[2] not in both or len(shape) not in (3, 4):
+        raise ValueError("activations must be [N, samples, pixels, channels] or [samples, pixels, channels] of float32 or bfloat16")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
+    if groups < 1 or shape[-1] % groups:
+        raise ValueError("groups must divide the channels")
+    d = liec_group_norm_desc()
+    d.workers, d.samples, d.pixels, d.channels = (shape[0] if len(shape) == 4 else 1), shape[-3], shape[-2], shape[-1]
+    d.groups, d.dtype, d.activation, d.eps = groups, _dtype_code("x", x[2]), ACTIVATIONS[activation], eps
+    if given:
+        d.x_pixel_stride, d.x_sample_stride, d.x_worker_stride = _gn_strides("x", x, x)
+    d.y_pixel_stride, d.y_sample_stride, d.y_worker_stride = _gn_strides("y" if dx is None else "dy", y, x)
+    d.weight_stride, d.bias_stride = _gn_vector("weight", weight, x, f32), _gn_vector("bias", bias, x, f32)
+    if dx is not None:
+        d.dx_pixel_stride, d.dx_sample_stride, d.dx_worker_stride = _gn_strides("dx", dx, x)
+        d.dweight_stride, d.dbias_stride = _gn_vector("dweight", dweight, x, both), _gn_vector("dbias", dbias, x, both)
+        if dweight[2] != dbias[2] or len(dweight[0]) != len(dbias[0]):
+            raise ValueError("dweight and dbias must have the same type and number of axes")
+        d.grad_dtype = _dtype_code("dweight", dweight[2])
+        if len(dweight[0]) == 1 and d.workers > 1:
+            if d.weight_stride != 0 or d.bias_stride != 0:
+                raise ValueError("workers with weights of their own need dweight and dbias [N, channels]")
+            d.shared_grads = 1
+    return d, C.byref(d), int(load_library().liec_group_norm_workspace_bytes(C.byref(d), 0 if dx is None else 1))
+
+
+def liec_group_norm_workspace_bytes(desc: liec_group_norm_desc, backward: bool) -> int:
+    return int(load_library().liec_group_norm_workspace_bytes(C.byref(desc), 1 if backward else 0))
+
+
+def _gn_workspace(workspace, need, device):
+    import torch
+    if workspace is not None:
+        if not workspace.is_contiguous():   # (its bytes are counted by its elements)
+            raise ValueError("workspace must be contiguous")
+        return workspace.data_ptr(), workspace.nbytes, workspace
+    if need == 0:
+        return None, 0, None
+    workspace = _empty((need,), torch.uint8, device)
+    return workspace.data_ptr(), need, workspace
+
+
+def _gn_forward(raw, device, x, groups, weight, bias, eps, activation, compress, y, q, scales, workspace):
+    import torch
+    if y is None:
+        y = _empty_like(x)
+    _, ref, need = _gn_desc(_layout(x), True, _layout(y), None, _layout(weight), _layout(bias), None, None, groups, activation, eps)
+    mean = _empty(x.shape[:-2] + (groups,), torch.float32, device)
+    rstd = torch.empty_like(mean)
+    if compress:
+        q, scales = _new_checkpoint(x.shape[:-1], x.shape[-1], q, scales, device)
+    ws, size, keep = _gn_workspace(workspace, need, device)
+    lib = _LIB or load_library()
+    st = lib.liec_group_norm_forward(ref, x.data_ptr(), _pointer(weight), _pointer(bias), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                     _pointer(q), _pointer(scales), ws, size, raw)
+    if st != 0:
+        _ln_failed(lib, st)
+    return (y, mean, rstd, q, scales) if compress else (y, mean, rstd)
+
+
+def liec_group_norm_forward(x, groups: int, weight=None, bias=None, eps: float = 1e-5, activation: str = "none", compress: bool = False,
+                            y=None, q=None, scales=None, workspace=None, stream=None):
+    """Group norm of [N, samples, pixels, channels] (or [samples, pixels, channels]) activations and an activation ("none",
+    "relu", "silu"), with per-worker float32 weight and bias [N, channels] (any stride between workers, e.g.
+    ``params[:, a:a + c]``) or one [channels] vector for all.  Returns (y, mean, rstd), mean and rstd [N, samples, groups]
+    float32; with ``compress`` (or q and scales given) (y, mean, rstd, q, scales), the last two being x's 8-bit checkpoint.
+    Automatic differentiation does not see the call; the gradients come from liec_group_norm_backward."""
+    device = _device_of("x", x)
+    _same_device(device, weight=weight, bias=bias, y=y, q=q, scales=scales, workspace=workspace)
+    return _launch(device, stream, _gn_forward, device, x, int(groups), weight, bias, float(eps), activation,
+                   bool(compress) or q is not None or scales is not None, y, q, scales, workspace)
+
+
+def _gn_backward(raw, device, dy, x, q, scales, mean, rstd, weight, bias, activation, dx, dweight, dbias, workspace):
+    import torch
+    if dx is None:
+        dx = _empty_like(dy)
+    if dweight is None or dbias is None:
+        like = next((t for t in (dweight, dbias, weight, bias) if t is not None), None)
+        shape = like.shape if like is not None else dy.shape[:-3] + dy.shape[-1:]
+        dtype = next((t.dtype for t in (dweight, dbias) if t is not None), torch.float32)
+        dweight = _empty(shape, dtype, device) if dweight is None else dweight
+        dbias = _empty(shape, dtype, device) if dbias is None else dbias
+    _, ref, need = _gn_desc(_layout(dy if x is None else x), x is not None, _layout(dy), _layout(dx), _layout(weight), _layout(bias),
+                            _layout(dweight), _layout(dbias), mean.shape[-1], activation, 0.0)
+    ws, size, keep = _gn_workspace(workspace, need, device)
+    lib = _LIB or load_library()
+    st = lib.liec_group_norm_backward(ref, dy.data_ptr(), _pointer(x), _pointer(q), _pointer(scales), mean.data_ptr(), rstd.data_ptr(),
+                                      _pointer(weight), _pointer(bias), dx.data_ptr(), dweight.data_ptr(), dbias.data_ptr(), ws, size, raw)
+    if st != 0:
+        _ln_failed(lib, st)
+    return dx, dweight, dbias
+
+
+def liec_group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, activation: str = "none", dx=None, dweight=None, dbias=None,
+                             workspace=None, stream=None):
+    """Gradients of liec_group_norm_forward.  x: the activations, or their checkpoint as a pair (q, scales).  dweight and
+    dbias: [N, channels] float32 or bfloat16 (any stride between workers, e.g. ``grads[:, a:a + c]``), or [channels] for a
+    vector that all workers share (its gradient is summed over the workers too); allocated in float32, shaped like weight, where not
+    given.  Returns (dx, dweight, dbias)."""
+    import torch
+    device = _device_of("dy", dy)
+    x, q, scales = (x, None, None) if torch.is_tensor(x) else (None, *x)
+    _same_device(device, x=x, q=q, scales=scales, mean=mean, rstd=rstd, weight=weight, bias=bias, dx=dx, dweight=dweight, dbias=dbias, workspace=workspace)
+    if dy.dim() not in (3, 4):
+        raise ValueError("dy must be [N, samples, pixels, channels] or [samples, pixels, channels]")
+    if x is None:
+        _check_checkpoint(q, scales, dy.shape[:-1], dy.shape[-1])
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t.dtype != torch.float32 or t.dim() != dy.dim() - 1 or t.shape[:-1] != dy.shape[:-2] or t.shape != mean.shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be the contiguous float32 tensor that the forward pass returned")
+    return _launch(device, stream, _gn_backward, device, dy, x, q, scales, mean, rstd, weight, bias, activation, dx, dweight, dbias, workspace)
+
+
+@functools.lru_cache(maxsize=1024)
+def _wg_desc(dy, dweight, cols):
+    d = liec_weight_grad_desc()
+    (shape, stride, dtype), (wshape, wstride, wdtype) = dy, dweight
+    N = shape[0] if len(shape) == 3 else 1
+    if (shape[-1] > 1 and stride[-1] != 1) or (cols > 1 and wstride[-1] != 1):
+        raise ValueError("the last axes of dy and dweight must be contiguous")
+    if tuple(wshape) != tuple(shape[:-2]) + (shape[-1], cols):
+        raise ValueError("dweight must be [N, out, in] ([out, in] for one worker)")
+    d.workers, d.rows, d.in_, d.out = N, shape[-2], cols, shape[-1]
+    d.dtype, d.grad_dtype = _dtype_code("dy", dtype), _dtype_code("dweight", wdtype)
+    d.dy_row_stride, d.dy_worker_stride = stride[-2], (stride[0] if len(shape) == 3 else 0)
+    d.dweight_row_stride, d.dweight_worker_stride = wstride[-2], (wstride[0] if len(shape) == 3 else 0)
+    return d, C.byref(d), int(load_library().liec_weight_grad_workspace_bytes(C.byref(d)))
+
+
+def liec_weight_grad_workspace_bytes(desc: liec_weight_grad_desc) -> int:
+    return int(load_library().liec_weight_grad_workspace_bytes(C.byref(desc)))
+
+
+def _weight_grad(raw, device, dy, q, scales, cols, dweight, workspace):
+    import torch
+    if dweight is None:
+        dweight = _empty(tuple(dy.shape[:-2]) + (dy.shape[-1], cols), torch.float32, device)
+    _, ref, need = _wg_desc(_layout(dy), _layout(dweight), cols)
+    ws, size, keep = _gn_workspace(workspace, need, device)
+    lib = _LIB or load_library()
+    st = lib.liec_weight_grad(ref, dy.data_ptr(), q.data_ptr(), scales.data_ptr(), dweight.data_ptr(), ws, size, raw)
+    if st != 0:
+        _ln_failed(lib, st)
+    return dweight
+
+
+def liec_weight_grad(dy, q, scales, cols: int, dweight=None, workspace=None, stream=None):
+    """Weight gradient of linear layers from the 8-bit checkpoint (q, scales) of their input [N, rows, cols]: the sum over
+    rows of dy[n, row, out] times the input.  dy: [N, rows, out] (or [rows, out]) float32 or bfloat16.  dweight: [N, out, cols]
+    float32 or bfloat16 with any strides between workers and outputs, e.g. ``grads[:, a:a + out * cols].unflatten(1, (out, cols))``;
+    allocated in float32 where not given.  Returns dweight."""
+    device = _device_of("dy", dy)
+    _same_device(device, q=q, scales=scales, dweight=dweight, workspace=workspace)
+    if dy.dim() not in (2, 3):
+        raise ValueError("dy must be [N, rows, out] or [rows, out]")
+    _check_checkpoint(q, scales, dy.shape[:-1], cols)
+    return _launch(device, stream, _weight_grad, device, dy, q, scales, int(cols), dweight, workspace)
 
 
 class Context:
