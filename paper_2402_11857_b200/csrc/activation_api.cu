@@ -119,6 +119,7 @@ liec_status check(const liec_weight_grad_desc *d) {
     if (d->workers > 65535) return unsupported("weight grad: workers above 65535");
     if (d->in > LIEC_ACTIVATION_MAX_COLS || d->out > LIEC_ACTIVATION_MAX_COLS) return unsupported("weight grad: in or out above LIEC_ACTIVATION_MAX_COLS");
     if (d->rows >= MAX_ROWS) return unsupported("weight grad: rows must be below 2^31");
+    if ((int64_t)d->workers * d->in * d->out > int64_t(1) << 38) return unsupported("weight grad: more than 2^38 weights (launch grid)");
     if (!known(d->dtype) || !known(d->grad_dtype)) return invalid("weight grad: unknown dtype");
     if (!strides_ok({d->dy_row_stride, d->dy_worker_stride, d->dweight_row_stride, d->dweight_worker_stride}))
         return invalid("weight grad: strides must be >= 0 (and at most 2^40)");
