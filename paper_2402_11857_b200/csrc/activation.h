@@ -53,7 +53,8 @@ struct WgArgs {
     const int8_t *q;
     const uint8_t *scales;
     void *dweight;
-    float *part;
+    float *part;      // workspace: the runs' sums, [run][worker][out][in], and
+    void *packed;     // dy in bfloat16 parts, where it does not go to the products as it is
     int64_t rows, dy_row, dy_worker, dw_row, dw_worker;
     int32_t workers, in, out, grad_dtype;
 };

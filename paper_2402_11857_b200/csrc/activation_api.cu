@@ -245,9 +245,11 @@ liec_status liec_group_norm_backward(const liec_group_norm_desc *d, const void *
     return launched(launch_group_norm_backward(a, d->dtype, static_cast<cudaStream_t>(stream)));
 }
 
-size_t liec_weight_grad_workspace_bytes(const liec_weight_grad_desc *d) {
+size_t liec_weight_grad_workspace_bytes(const liec_weight_grad_desc *d, const void *dy) {
     if (check(d) != LIEC_OK) return 0;
-    return (weight_grad_workspace(wg_args(d), d->dtype) + 255) / 256 * 256;
+    WgArgs a = wg_args(d);
+    a.dy = dy;
+    return (weight_grad_workspace(a, d->dtype) + 255) / 256 * 256;
 }
 
 liec_status liec_weight_grad(const liec_weight_grad_desc *d, const void *dy, const int8_t *q, const uint8_t *scales, void *dweight, void *workspace,
@@ -260,6 +262,7 @@ liec_status liec_weight_grad(const liec_weight_grad_desc *d, const void *dy, con
     if (!aligned(q, 16)) return invalid("weight grad: q must be 16-byte aligned");
     if (!disjoint(d->in, {d->workers, d->out}, {d->dweight_worker_stride, d->dweight_row_stride})) return invalid("weight grad: the rows of dweight overlap");
     WgArgs a = wg_args(d);
+    a.dy = dy;
     st = workspace_ok(weight_grad_workspace(a, d->dtype), workspace, workspace_bytes, "weight grad: workspace must be non-NULL and 16-byte aligned",
                       "workspace smaller than liec_weight_grad_workspace_bytes()");
     if (st != LIEC_OK) return st;
@@ -270,7 +273,7 @@ liec_status liec_weight_grad(const liec_weight_grad_desc *d, const void *dy, con
             meet(out, bytes_of(q, rows, d->in)) || meet(out, powers_of(scales, rows, d->in)))
             return invalid("weight grad: dweight overlaps an input");
     }
-    a.dy = dy; a.q = q; a.scales = scales; a.dweight = dweight;
+    a.q = q; a.scales = scales; a.dweight = dweight;
     a.part = static_cast<float *>(workspace);
     return launched(launch_weight_grad(a, d->dtype, static_cast<cudaStream_t>(stream)));
 }

@@ -2,10 +2,15 @@
 // dy[t][o] x^[t][c], for N workers, on the tensor cores.
 //
 // x^ = q 2^e is a bfloat16 number, so the products are those of the definition; a binary32 dy is cut into three bfloat16
-// parts whose sum it is, and multiplied three times.  A CTA takes 256 channels c (the rows of the accumulator, two halves of
-// 128) by 256 outputs o (128 for binary32), and one run of tokens.  Eight warps bring both operands to shared memory, where
-// each token is a row of 128-byte pieces as in memory; the bytes of q are widened on the way.  One thread issues the products.
-// Lanes of the accumulator are channels, so a warp writes 32 neighbours of a row of dW.
+// parts whose sum it is, and multiplied three times.  A pair of CTAs takes a tile of 256 channels c (the rows of the
+// accumulator, 128 in each CTA) by 512 outputs o (256 for binary32), and one run of tokens.  Operands lie in shared memory
+// as in global memory, a token as a row of 128-byte pieces: one thread of each CTA has the tensor memory accelerator bring
+// q and dy, sixteen warps widen q (four groups of four, a stage each in turn, so that one's latency hides behind the
+// others), one thread of the pair issues the products.  Each CTA so widens 128 channels and reads half of the outputs: a
+// tile of the same size in one CTA would need half again the shared memory traffic of a product.  Lanes of the accumulator
+// are channels, so a warp writes 32 neighbours of a row of dW.
+#include <cuda.h>
+
 #include <algorithm>
 
 #include "activation.cuh"
@@ -14,23 +19,25 @@
 namespace liec {
 
 constexpr int WG_TOKENS = 32;                  // of a stage
-constexpr int WG_CHANNELS = 256;               // of a tile
-constexpr int WG_AHEAD = 3;                    // stages by which the copies run ahead
-constexpr int WG_WORKERS = 256, WG_THREADS = WG_WORKERS + 32;
+constexpr int WG_CHANNELS = 128;               // of a CTA
 constexpr int WG_BLOCK_BYTES = WG_TOKENS * 128;
+constexpr int WG_A_BYTES = 2 * WG_BLOCK_BYTES, WG_RAW_BYTES = WG_TOKENS * WG_CHANNELS;
+constexpr int WG_GROUPS = 4, WG_GROUP = 128;   // groups of widening threads
+constexpr int WG_WIDENERS = WG_GROUPS * WG_GROUP, WG_THREADS = WG_WIDENERS + 64;
+constexpr int WG_SLAB = 256;                   // outputs of one product of the pair, 128 from each CTA
 constexpr uint32_t WG_POLLS = 1u << 20;
 
-template <typename T>
+// PARTS: bfloat16 parts of dy.  SLABS: products side by side.
+template <int PARTS_>
 struct WgShape {
-    static constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    static constexpr int OUTPUTS = sizeof(T) == 4 ? 128 : 256;
-    static constexpr int A_BYTES = WG_CHANNELS / 64 * WG_BLOCK_BYTES, B_BYTES = OUTPUTS / 64 * WG_BLOCK_BYTES, STAGE_BYTES = A_BYTES + PARTS * B_BYTES;
-    static constexpr int STAGES = sizeof(T) == 4 ? 4 : 5;   // what fits; copies that run ahead need two more than their lead
-    static constexpr int RAW_BYTES = WG_TOKENS * WG_CHANNELS;
-    static constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + (WG_AHEAD + 1) * RAW_BYTES;
-    static constexpr int COLUMNS = 2 * OUTPUTS;
-    static constexpr int DY_CHUNKS = WG_TOKENS * OUTPUTS / Bits<T>::VEC / WG_WORKERS;   // 16-byte chunks of dy per thread and stage
+    static constexpr int PARTS = PARTS_, SLABS = PARTS == 1 ? 2 : 1, OUTPUTS = SLABS * WG_SLAB, COLUMNS = OUTPUTS;
+    static constexpr int B_BYTES = 2 * WG_BLOCK_BYTES;                       // of a slab's part
+    static constexpr int STAGE_BYTES = WG_A_BYTES + SLABS * PARTS * B_BYTES + WG_RAW_BYTES;
+    static constexpr int STAGES = PARTS == 1 ? 7 : 6;                        // what fits
+    static constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES;
 };
+inline int wg_parts(int dtype) { return dtype == 0 ? 3 : 1; }
+inline int wg_outputs(int dtype) { return dtype == 0 ? WgShape<3>::OUTPUTS : WgShape<1>::OUTPUTS; }
 
 struct WgPlan {
     int64_t tiles, run;          // per worker; tokens of a run (whole stages)
@@ -68,207 +75,224 @@ __device__ __forceinline__ void wg_split(float x, uint32_t (&p)[3]) {
     p[2] = __float_as_uint(rest - __uint_as_float(p[1]));
 }
 
-// ASYNC: rows of dy start on 16 bytes and are bfloat16; they go to shared memory without passing through registers.
-template <typename T, bool ASYNC>
-__global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ WgPlan p) {
-    using S = WgShape<T>;
+// dy as the tensor memory accelerator wants it: bfloat16 rows of a multiple of 8 columns without gaps, part after part.  A
+// thread takes 8 columns of a row.
+template <typename T>
+__global__ void __launch_bounds__(256) wg_pack_kernel(const __grid_constant__ WgArgs a, int64_t row_chunks) {
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+    const int64_t rows = a.workers * a.rows, i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / row_chunks;
+    if (row >= rows) return;
+    const int64_t w = row / a.rows;
+    const int c = (int)(i - row * row_chunks) * 8;
+    const T *from = static_cast<const T *>(a.dy) + w * a.dy_worker + (row - w * a.rows) * a.dy_row;
+    uint4 *to = reinterpret_cast<uint4 *>(a.packed) + i;
+    if constexpr (PARTS == 1) {
+        *to = load_chunk(from, c, a.out);
+    } else {
+        const uint4 lo4 = load_chunk(from, c, a.out), hi4 = c + 4 < a.out ? load_chunk(from, c + 4, a.out) : make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t x[8] = {lo4.x, lo4.y, lo4.z, lo4.w, hi4.x, hi4.y, hi4.z, hi4.w};
+        uint32_t p[8][3];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) wg_split(__uint_as_float(x[e]), p[e]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            to[k * rows * row_chunks] = make_uint4(__byte_perm(p[0][k], p[1][k], 0x7632), __byte_perm(p[2][k], p[3][k], 0x7632),
+                                                   __byte_perm(p[4][k], p[5][k], 0x7632), __byte_perm(p[6][k], p[7][k], 0x7632));
+    }
+}
+
+__device__ __forceinline__ void wg_store(float *p, float v) { *p = v; }
+__device__ __forceinline__ void wg_store(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+
+// 32 outputs of a channel, `step` elements apart.
+template <typename T>
+__device__ __forceinline__ void wg_store_column(T *to, int64_t step, int outputs, const float (&v)[32]) {
+    if (outputs >= 32) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) wg_store(to + e * step, v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+            if (e < outputs) wg_store(to + e * step, v[e]);
+    }
+}
+
+template <int PARTS>
+__global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ WgPlan p,
+                                                            const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap dy_map) {
+    using S = WgShape<PARTS>;
     extern __shared__ char wg_smem[];
-    __shared__ __align__(8) unsigned long long bars[2 * S::STAGES + 1];
+    __shared__ __align__(8) unsigned long long bars[3 * S::STAGES + 1];
     __shared__ uint32_t tmem_at;
     __shared__ int failed;
     const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars);
     const uint32_t base = ((uint32_t)__cvta_generic_to_shared(wg_smem) + 1023u) & ~1023u;
-    auto full = [&](int s) { return bar + 8u * s; };
-    auto empty = [&](int s) { return bar + 8u * (S::STAGES + s); };
-    const uint32_t done = bar + 8u * 2 * S::STAGES;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    auto loaded = [&](int s) { return bar + 8u * s; };                       // the copies of a stage, in this CTA
+    auto full = [&](int s) { return bar + 8u * (S::STAGES + s); };           // both CTAs' operands (in the first CTA)
+    auto empty = [&](int s) { return bar + 8u * (2 * S::STAGES + s); };      // the stage's products are done
+    const uint32_t done = bar + 8u * 3 * S::STAGES;
+    auto a_at = [&](int s) { return base + s * S::STAGE_BYTES; };
+    auto b_at = [&](int s) { return a_at(s) + WG_A_BYTES; };
+    auto raw_at = [&](int s) { return b_at(s) + S::SLABS * PARTS * S::B_BYTES; };
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
 
-    int64_t b = blockIdx.x;
+    int64_t b = blockIdx.x / 2;
     const int run = (int)(b % p.runs);
     b /= p.runs;
     const int worker = (int)(b / p.tiles), tile = (int)(b % p.tiles);
-    const int o0 = tile / p.c_tiles * S::OUTPUTS, c0 = tile % p.c_tiles * WG_CHANNELS;
+    const int o0 = tile / p.c_tiles * S::OUTPUTS, c0 = tile % p.c_tiles * 2 * WG_CHANNELS + rank * WG_CHANNELS;
+    const int slabs = min(S::SLABS, (a.out - o0 + WG_SLAB - 1) / WG_SLAB);
     const int64_t first = run * p.run, tokens = min(p.run, a.rows - first);
     const int turns = (int)((tokens + WG_TOKENS - 1) / WG_TOKENS);
 
-    if (warp == WG_WORKERS / 32) {
+    if (warp == WG_WIDENERS / 32 + 1) {
         if (lane == 0) {
             for (int s = 0; s < S::STAGES; ++s) {
-                barrier_init(full(s), WG_WORKERS / 32);
+                barrier_init(loaded(s), 1);
+                barrier_init(full(s), 2 * WG_GROUP / 32);
                 barrier_init(empty(s), 1);
             }
             barrier_init(done, 1);
             failed = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             async_fence();
         }
         __syncwarp();
-        tc_alloc((uint32_t)__cvta_generic_to_shared(&tmem_at), S::COLUMNS);
+        tc_alloc_pair((uint32_t)__cvta_generic_to_shared(&tmem_at), S::COLUMNS);
     }
     tc_before_sync();
     __syncthreads();
+    cluster_sync();
     tc_after_sync();
     const uint32_t tmem = tmem_at;
 
-    if (warp == WG_WORKERS / 32) {
-        if (lane == 0) {
+    if (warp == WG_WIDENERS / 32) {
+        if (lane == 0) {   // copies
+            asm volatile("griddepcontrol.wait;" ::: "memory");   // dy may come from the kernel before
+            int i = 0;
             bool ok = true;
-            for (int i = 0; i < turns && ok; ++i) {
+            for (; i < turns; ++i) {
+                const int s = i % S::STAGES, t = (int)first + i * WG_TOKENS;
+                if (i >= S::STAGES) ok = barrier_wait(empty(s), (i / S::STAGES - 1) & 1, WG_POLLS);
+                if (!ok) break;
+                barrier_expect(loaded(s), WG_RAW_BYTES + slabs * PARTS * S::B_BYTES);
+                copy_box(raw_at(s), &q_map, c0, t, worker, loaded(s));
+                for (int n = 0; n < slabs; ++n)
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            copy_box(b_at(s) + (n * PARTS + part) * S::B_BYTES + h * WG_BLOCK_BYTES, &dy_map, o0 + n * WG_SLAB + rank * 128 + h * 64, t,
+                                     part * a.workers + worker, loaded(s));
+            }
+            if (!ok) {   // nothing may be on its way into this CTA's memory when it ends
+                failed = 1;
+                for (int k = max(0, i - S::STAGES); k < i; ++k) barrier_wait(loaded(k % S::STAGES), (k / S::STAGES) & 1, WG_POLLS);
+            }
+        }
+        __syncwarp();
+    } else if (warp == WG_WIDENERS / 32 + 1) {
+        if (lane == 0 && rank == 0) {   // products
+            bool ok = true;
+            for (int i = 0; i < turns; ++i) {
                 const int s = i % S::STAGES;
                 ok = barrier_wait(full(s), (i / S::STAGES) & 1, WG_POLLS);
                 if (!ok) break;
                 tc_after_sync();
-                const uint32_t at = base + s * S::STAGE_BYTES;
 #pragma unroll
-                for (int k = 0; k < WG_TOKENS / 16; ++k)
+                for (int k = 0; k < WG_TOKENS / 16; ++k) {
+                    const uint64_t x = tc_descriptor(a_at(s) + k * 2048, WG_BLOCK_BYTES);
+                    for (int n = 0; n < slabs; ++n)
 #pragma unroll
-                    for (int part = 0; part < S::PARTS; ++part)
-#pragma unroll
-                        for (int half = 0; half < 2; ++half)
-                            tc_mma(tmem + half * S::OUTPUTS, tc_descriptor(at + half * 2 * WG_BLOCK_BYTES + k * 2048, WG_BLOCK_BYTES),
-                                   tc_descriptor(at + S::A_BYTES + part * S::B_BYTES + k * 2048, WG_BLOCK_BYTES), tc_instruction(128, S::OUTPUTS),
-                                   i > 0 || k > 0 || part > 0);
-                tc_commit(empty(s));
+                        for (int part = 0; part < PARTS; ++part)
+                            tc_mma_pair(tmem + n * WG_SLAB, x, tc_descriptor(b_at(s) + (n * PARTS + part) * S::B_BYTES + k * 2048, WG_BLOCK_BYTES),
+                                        tc_instruction(256, WG_SLAB), i > 0 || k > 0 || part > 0);
+                }
+                tc_commit_pair(empty(s));
             }
             if (!ok) {
-                failed = 1;
-                __threadfence_block();
+                const uint32_t flag = (uint32_t)__cvta_generic_to_shared(&failed);
+                for (int r = 0; r < 2; ++r) asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cta(flag, r)), "r"(1) : "memory");
+                asm volatile("fence.acq_rel.cluster;" ::: "memory");
             }
-            tc_commit(done);
+            tc_commit_pair(done);
         }
         __syncwarp();
     } else {
-        // this thread's part of a stage: two chunks of q (16 channels of one token each; a warp takes two tokens, so that
-        // the eight threads whose stores go together fill all places of the swizzle), and chunks of dy
-        const int q_block = lane >> 3 & 3, q_piece = lane & 3;
-        const int64_t q_cols = (a.in + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK, q_row0 = worker * a.rows + first;
-        const int c = c0 + q_block * 64 + q_piece * 16;
-        const bool c_live = c < q_cols;
-        const T *dy = static_cast<const T *>(a.dy) + worker * a.dy_worker + first * a.dy_row;
-        const uint32_t raw = base + S::STAGES * S::STAGE_BYTES + threadIdx.x * 16;
-        uint32_t power[WG_AHEAD + 1][2];
-        uint4 held[S::DY_CHUNKS];
-        auto q_token = [&](int j) { return j * 16 + warp * 2 + (lane >> 2 & 1); };
-        auto fetch = [&](int i, int slot) {   // turn i's copies
-            const int64_t t0 = (int64_t)i * WG_TOKENS;
-            if (i < turns) {
+        // A thread's part of a stage: two chunks of q, 16 channels of one token each.  Eight threads that load or store
+        // together meet all places of a 128-byte row, plain in one case and swizzled in the other.
+        const int group = warp / 4, parity = lane >> 2 & 1, q_block = parity ^ (lane >> 3 & 1), q_piece = lane & 3;
+        const int token = warp % 4 * 4 + (lane >> 4) * 2 + parity;           // and the one 16 further on
+        const int64_t row_powers = (a.in + CK_BLOCK - 1) / CK_BLOCK;
+        const int c = c0 + q_block * 64 + q_piece * 16, left = c < row_powers * CK_BLOCK ? (int)tokens : 0;
+        const uint8_t *powers = a.scales + (worker * a.rows + first) * row_powers + c / CK_BLOCK;
+        auto fetch = [&](int i, uint32_t (&power)[2]) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int64_t t = t0 + q_token(j);
-                    const bool live = c_live && t < tokens;
-                    copy_async(raw + slot * S::RAW_BYTES + j * WG_WORKERS * 16, live ? a.q + (q_row0 + t) * q_cols + c : a.q, live ? 16 : 0);
-                    power[slot][j] = live ? __ldg(a.scales + (q_row0 + t) * (q_cols / CK_BLOCK) + c / CK_BLOCK) : 127u;
-                }
-                if constexpr (ASYNC) {
-                    const uint32_t to = base + (i % S::STAGES) * S::STAGE_BYTES + S::A_BYTES;
-#pragma unroll
-                    for (int j = 0; j < S::DY_CHUNKS; ++j) {
-                        const int piece = threadIdx.x % 32, t = threadIdx.x / 32 + j * 8, o = o0 + piece * 8;
-                        const int bytes = t0 + t < tokens ? min(16, max(0, (a.out - o) * 2)) : 0;
-                        copy_async(to + piece / 8 * WG_BLOCK_BYTES + tc_swizzled(t, piece % 8), bytes > 0 ? dy + (t0 + t) * a.dy_row + o : dy, bytes);
-                    }
-                }
-            }
-            copy_commit();
-        };
-        auto hold = [&](int i) {   // turn i's chunks of dy into registers
-            if constexpr (!ASYNC) {
-                constexpr int ROW = S::OUTPUTS / Bits<T>::VEC;
-#pragma unroll
-                for (int j = 0; j < S::DY_CHUNKS; ++j) {
-                    const int q = threadIdx.x + j * WG_WORKERS;
-                    const int64_t t = (int64_t)i * WG_TOKENS + q / ROW;
-                    held[j] = i < turns && t < tokens && o0 + q % ROW * Bits<T>::VEC < a.out ? load_chunk(dy + t * a.dy_row, o0 + q % ROW * Bits<T>::VEC, a.out)
-                                                                                             : make_uint4(0u, 0u, 0u, 0u);
-                }
+            for (int j = 0; j < 2; ++j) {
+                const int t = i * WG_TOKENS + token + j * 16;
+                power[j] = t < left ? __ldg(powers + t * row_powers) : 127u;
             }
         };
-        auto put = [&](int s) {   // and on to shared memory
-            if constexpr (!ASYNC) {
-                constexpr int ROW = S::OUTPUTS / Bits<T>::VEC;
-                char *to = wg_smem + (base - (uint32_t)__cvta_generic_to_shared(wg_smem)) + s * S::STAGE_BYTES + S::A_BYTES;
+        auto turn = [&](int i, uint32_t (&power)[2]) {
+            const int s = i % S::STAGES;
+            if (!__all_sync(0xffffffffu, barrier_wait(loaded(s), (i / S::STAGES) & 1, WG_POLLS))) return false;
+            const uint32_t to = a_at(s) + q_block * WG_BLOCK_BYTES, from = raw_at(s) + q_block * 64 + q_piece * 16 + token * 128;
+            uint4 q[2];
 #pragma unroll
-                for (int j = 0; j < S::DY_CHUNKS; ++j) {
-                    const int q = threadIdx.x + j * WG_WORKERS, t = q / ROW, o = q % ROW * Bits<T>::VEC;
-                    char *at = to + o / 64 * WG_BLOCK_BYTES + tc_swizzled(t, o % 64 / 8) + o % 8 * 2;
-                    if constexpr (S::PARTS == 1) {
-                        *reinterpret_cast<uint4 *>(at) = held[j];
-                    } else {
-                        const uint32_t w[4] = {held[j].x, held[j].y, held[j].z, held[j].w};
-                        uint32_t part[4][3];
+            for (int j = 0; j < 2; ++j)
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[j].x), "=r"(q[j].y), "=r"(q[j].z), "=r"(q[j].w) : "r"(from + j * 2048) : "memory");
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) wg_split(__uint_as_float(w[e]), part[e]);
+            for (int j = 0; j < 2; ++j) {
+                uint4 x[2];
+                wg_widen(q[j], power[j], x);
 #pragma unroll
-                        for (int k = 0; k < 3; ++k)
-                            *reinterpret_cast<uint2 *>(at + k * S::B_BYTES) = make_uint2(__byte_perm(part[0][k], part[1][k], 0x7632), __byte_perm(part[2][k], part[3][k], 0x7632));
-                    }
-                }
+                for (int h = 0; h < 2; ++h)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + tc_swizzled(token, q_piece * 2 + h) + j * 2048),
+                                 "r"(x[h].x), "r"(x[h].y), "r"(x[h].z), "r"(x[h].w) : "memory");
             }
+            async_fence();
+            __syncwarp();
+            if (lane == 0) barrier_arrive_cluster(in_cta(full(s), 0));
+            return true;
         };
+        // the powers run two turns ahead
         bool ok = true;
-#pragma unroll
-        for (int i = 0; i < WG_AHEAD; ++i) fetch(i, i);
-        hold(0);
-        for (int i0 = 0; i0 < turns && ok; i0 += WG_AHEAD + 1) {
-#pragma unroll
-            for (int j = 0; j < WG_AHEAD + 1; ++j) {
-                const int i = i0 + j;
-                if (i < turns && ok) {
-                    // the place that is filled now is free: of the turn fetched ahead, or of this one
-                    const int next = ASYNC ? i + WG_AHEAD : i;
-                    if (next >= S::STAGES && next < turns) ok = barrier_wait(empty(next % S::STAGES), (next / S::STAGES - 1) & 1, WG_POLLS);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (ok) {
-                        fetch(i + WG_AHEAD, (j + WG_AHEAD) % (WG_AHEAD + 1));
-                        const int s = i % S::STAGES;
-                        put(s);
-                        hold(i + 1);
-                        copy_wait<WG_AHEAD>();
-                        const uint32_t to = base + s * S::STAGE_BYTES + q_block * WG_BLOCK_BYTES;
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            uint4 q, x[2];
-                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w)
-                                         : "r"(raw + j * S::RAW_BYTES + k * WG_WORKERS * 16) : "memory");
-                            wg_widen(q, power[j][k], x);
-#pragma unroll
-                            for (int h = 0; h < 2; ++h)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + tc_swizzled(q_token(k), q_piece * 2 + h)),
-                                             "r"(x[h].x), "r"(x[h].y), "r"(x[h].z), "r"(x[h].w) : "memory");
-                        }
-                        async_fence();
-                        __syncwarp();
-                        if (lane == 0) barrier_arrive(full(s));
-                    }
-                }
+        uint32_t even[2], odd[2];
+        fetch(group, even);
+        fetch(group + WG_GROUPS, odd);
+        for (int i = group; i < turns && ok; i += 2 * WG_GROUPS) {
+            ok = turn(i, even);
+            fetch(i + 2 * WG_GROUPS, even);
+            if (ok && i + WG_GROUPS < turns) {
+                ok = turn(i + WG_GROUPS, odd);
+                fetch(i + 3 * WG_GROUPS, odd);
             }
         }
-        copy_wait<0>();
         if (!ok) failed = 1;
         if (!barrier_wait(done, 0, WG_POLLS)) failed = 1;
         tc_after_sync();
-        asm volatile("bar.sync 1, %0;" ::"n"(WG_WORKERS) : "memory");   // everyone's verdict
-        const bool good = failed == 0;
-        const int half = warp / 4, ch = c0 + half * 128 + (warp % 4) * 32 + lane;
-        for (int col = 0; col < S::OUTPUTS && o0 + col < a.out; col += 32) {
+        asm volatile("bar.sync 1, %0;" ::"n"(WG_WIDENERS) : "memory");   // everyone's verdict
+        const bool good = *reinterpret_cast<volatile int *>(&failed) == 0;
+        const int ch = c0 + (warp % 4) * 32 + lane;
+        for (int col = group * 32; col < slabs * WG_SLAB && o0 + col < a.out; col += WG_GROUPS * 32) {
             float v[32];
             __syncwarp();
-            tc_load(tmem + ((uint32_t)(warp % 4) << 21) + half * S::OUTPUTS + col, v);
-            if (ch < a.in) {
+            tc_load(tmem + ((uint32_t)(warp % 4) << 21) + col, v);
+            if (ch >= a.in) continue;
+            if (!good) {   // an unfinished sum is never taken for one
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const int o = o0 + col + e;
-                    if (o >= a.out) break;
-                    const float r = !good ? __uint_as_float(0x7fffffffu) : v[e];
-                    if (p.runs > 1) a.part[(((int64_t)run * a.workers + worker) * a.out + o) * a.in + ch] = r;
-                    else if (a.grad_dtype == LIEC_F32) static_cast<float *>(a.dweight)[worker * a.dw_worker + o * a.dw_row + ch] = r;
-                    else static_cast<__nv_bfloat16 *>(a.dweight)[worker * a.dw_worker + o * a.dw_row + ch] = __float2bfloat16_rn(r);
-                }
+                for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(0x7fffffffu);
             }
+            const int o = o0 + col;
+            if (p.runs > 1) wg_store_column(a.part + (((int64_t)run * a.workers + worker) * a.out + o) * a.in + ch, a.in, a.out - o, v);
+            else if (a.grad_dtype == LIEC_F32) wg_store_column(static_cast<float *>(a.dweight) + worker * a.dw_worker + o * a.dw_row + ch, a.dw_row, a.out - o, v);
+            else wg_store_column(static_cast<__nv_bfloat16 *>(a.dweight) + worker * a.dw_worker + o * a.dw_row + ch, a.dw_row, a.out - o, v);
         }
         tc_before_sync();
     }
     __syncthreads();
-    if (warp == WG_WORKERS / 32) tc_free(tmem, S::COLUMNS);
+    cluster_sync();   // neither CTA ends while the other may still reach into it
+    if (warp == WG_WIDENERS / 32 + 1) tc_free_pair(tmem, S::COLUMNS);
 }
 
 // The runs' sums, in their order, rounded once to the gradient's type; zeros without runs.
@@ -282,21 +306,21 @@ __global__ void __launch_bounds__(256) wg_join_kernel(const __grid_constant__ Wg
     else static_cast<__nv_bfloat16 *>(a.dweight)[at] = __float2bfloat16_rn(s);
 }
 
-// Runs of tokens: as many as make the GPU's places busy, weighed against what joining them costs.  In units of a stage's
-// products (512 cycles): a CTA's start and end take about 12, writing and reading a run's sums of a tile 6.
+// Runs of tokens: as many as make the GPU's 74 pairs of SMs busy, weighed against what joining them costs.  In units of a
+// stage's products (512 cycles): a pair's start and end take about 12, writing and reading a run's sums of a tile 12.
 static WgPlan wg_plan(const WgArgs &a, int dtype) {
     WgPlan p{};
-    const int outputs = dtype == 0 ? WgShape<float>::OUTPUTS : WgShape<__nv_bfloat16>::OUTPUTS;
-    p.c_tiles = (a.in + WG_CHANNELS - 1) / WG_CHANNELS;
+    const int outputs = wg_outputs(dtype);
+    p.c_tiles = (a.in + 2 * WG_CHANNELS - 1) / (2 * WG_CHANNELS);
     p.o_tiles = (a.out + outputs - 1) / outputs;
     p.tiles = (int64_t)p.c_tiles * p.o_tiles;
     const int64_t stages = (a.rows + WG_TOKENS - 1) / WG_TOKENS, places = p.tiles * a.workers;
     double best = 0.0;
     p.runs = 0;
-    for (int runs = 1; runs <= 64 && runs <= std::max<int64_t>(stages, 1) && places * runs < int64_t(1) << 31; ++runs) {
+    for (int runs = 1; runs <= 64 && runs <= std::max<int64_t>(stages, 1) && places * runs < int64_t(1) << 30; ++runs) {
         const int64_t length = (stages + runs - 1) / runs, used = std::max<int64_t>(1, (stages + length - 1) / std::max<int64_t>(length, 1));
         if (used != runs && runs > 1) continue;
-        const double cost = (double)((places * runs + 147) / 148) * (double)(length + 12) + (runs > 1 ? 20.0 + 6.0 * (double)(places * runs) / 148.0 : 0.0);
+        const double cost = (double)((places * runs + 73) / 74) * (double)(length + 12) + (runs > 1 ? 20.0 + 12.0 * (double)(places * runs) / 74.0 : 0.0);
         if (p.runs == 0 || cost < best) {
             best = cost;
             p.runs = runs;
@@ -306,28 +330,100 @@ static WgPlan wg_plan(const WgArgs &a, int dtype) {
     return p;
 }
 
-size_t weight_grad_workspace(const WgArgs &a, int dtype) {
-    if (a.rows == 0) return 0;
-    const WgPlan p = wg_plan(a, dtype);
-    return p.runs > 1 ? sizeof(float) * (size_t)p.runs * a.workers * a.out * a.in : 0;
+// dy goes to the products as it is where it is bfloat16 and its rows start on 16 bytes, one after another.
+static bool wg_direct(const WgArgs &a, int dtype) {
+    return dtype == 1 && ln_whole(a.dy, a.dy_row, a.dy_worker, a.rows, a.workers, 8, 2) && (a.rows == 1 || a.dy_row >= a.out) &&
+           (a.workers == 1 || a.dy_worker >= a.out);
+}
+static size_t wg_part_bytes(const WgArgs &a, const WgPlan &p) {
+    return p.runs > 1 ? (sizeof(float) * (size_t)p.runs * a.workers * a.out * a.in + 255) / 256 * 256 : 0;
 }
 
-template <typename T, bool ASYNC>
-static cudaError_t wg_launch(const WgArgs &a, const WgPlan &p, cudaStream_t st) {
+size_t weight_grad_workspace(const WgArgs &a, int dtype) {
+    if (a.rows == 0) return 0;
+    const size_t packed = wg_direct(a, dtype) ? 0 : (size_t)wg_parts(dtype) * a.workers * a.rows * ((a.out + 7) / 8) * 16;
+    return wg_part_bytes(a, wg_plan(a, dtype)) + packed;
+}
+
+// The function behind cuTensorMapEncodeTiled: asked of the runtime, so that the library links without the driver's.
+typedef CUresult (*WgEncode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static WgEncode wg_encode() {
+    static std::atomic<void *> found{nullptr};
+    void *f = found.load(std::memory_order_acquire);
+    if (!f) {
+        cudaDriverEntryPointQueryResult result;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &result) != cudaSuccess || result != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            return nullptr;
+        }
+        found.store(f, std::memory_order_release);
+    }
+    return reinterpret_cast<WgEncode>(f);
+}
+
+// [workers][rows][cols], boxes of box_cols columns by a stage's tokens; what lies outside is read as zeros.
+static bool wg_map(CUtensorMap *map, const void *base, bool bytes, int64_t cols, int64_t rows, int64_t workers, int64_t row, int64_t worker, int box_cols) {
+    const WgEncode encode = wg_encode();
+    if (!encode) return false;
+    const int size = bytes ? 1 : 2;
+    // (a single row or worker is never stepped over; the map wants a step all the same)
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)workers};
+    const cuuint64_t row_step = rows > 1 ? (cuuint64_t)(row * size) : (cuuint64_t)((cols * size + 15) / 16 * 16);
+    const cuuint64_t steps[2] = {row_step, workers > 1 ? (cuuint64_t)(worker * size) : row_step * (cuuint64_t)rows};
+    const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)WG_TOKENS, 1}, one[3] = {1, 1, 1};
+    return encode(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, steps, box, one,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, bytes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+static cudaLaunchConfig_t wg_config(int64_t ctas, int threads, int smem, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    return cfg;
+}
+
+// after: the kernel before this one packs dy; this one starts while it ends and waits for it where it reads.
+template <int PARTS>
+static cudaError_t wg_launch(const WgArgs &a, const WgPlan &p, const CUtensorMap &q_map, const CUtensorMap &dy_map, bool after, cudaStream_t st) {
     static std::atomic<uint64_t> allowed{0};
-    const auto kernel = wg_kernel<T, ASYNC>;
-    const cudaError_t e = ln_allow_smem(kernel, WgShape<T>::SMEM_BYTES, allowed);
+    const auto kernel = wg_kernel<PARTS>;
+    const cudaError_t e = ln_allow_smem(kernel, WgShape<PARTS>::SMEM_BYTES, allowed);
     if (e != cudaSuccess) return e;
-    kernel<<<(unsigned)(p.tiles * a.workers * p.runs), WG_THREADS, WgShape<T>::SMEM_BYTES, st>>>(a, p);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = wg_config(p.tiles * a.workers * p.runs * 2, WG_THREADS, WgShape<PARTS>::SMEM_BYTES, st);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = after ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a, p, q_map, dy_map);
 }
 
 cudaError_t launch_weight_grad(WgArgs a, int dtype, cudaStream_t st) {
     int runs = 0;
     if (a.rows > 0) {
         const WgPlan p = wg_plan(a, dtype);
-        const bool whole = dtype == 1 && ln_whole(a.dy, a.dy_row, a.dy_worker, a.rows, a.workers, 8, 2);
-        const cudaError_t e = dtype == 0 ? wg_launch<float, false>(a, p, st) : whole ? wg_launch<__nv_bfloat16, true>(a, p, st) : wg_launch<__nv_bfloat16, false>(a, p, st);
+        const bool direct = wg_direct(a, dtype);
+        const int64_t q_cols = ck_cols(a.in), dy_cols = (a.out + 7) / 8 * 8;
+        a.packed = reinterpret_cast<char *>(a.part) + wg_part_bytes(a, p);
+        CUtensorMap q_map, dy_map;
+        if (!wg_map(&q_map, a.q, true, q_cols, a.rows, a.workers, q_cols, q_cols * a.rows, WG_CHANNELS) ||
+            !(direct ? wg_map(&dy_map, a.dy, false, a.out, a.rows, a.workers, a.dy_row, a.dy_worker, 64)
+                     : wg_map(&dy_map, a.packed, false, a.out, a.rows, (int64_t)wg_parts(dtype) * a.workers, dy_cols, dy_cols * a.rows, 64)))
+            return cudaErrorNotSupported;
+        if (!direct) {
+            const int64_t chunks = a.workers * a.rows * (dy_cols / 8);
+            const cudaLaunchConfig_t cfg = wg_config((chunks + 255) / 256, 256, 0, st);
+            const cudaError_t e = cudaLaunchKernelEx(&cfg, dtype == 0 ? wg_pack_kernel<float> : wg_pack_kernel<__nv_bfloat16>, a, dy_cols / 8);
+            if (e != cudaSuccess) return e;
+        }
+        const cudaError_t e = dtype == 0 ? wg_launch<3>(a, p, q_map, dy_map, !direct, st) : wg_launch<1>(a, p, q_map, dy_map, !direct, st);
         if (e != cudaSuccess || p.runs == 1) return e;
         runs = p.runs;
     }

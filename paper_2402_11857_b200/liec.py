@@ -153,7 +153,7 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.liec_group_norm_forward.restype = C.c_int
     lib.liec_group_norm_backward.argtypes = [gnp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     lib.liec_group_norm_backward.restype = C.c_int
-    lib.liec_weight_grad_workspace_bytes.argtypes = [wgp]
+    lib.liec_weight_grad_workspace_bytes.argtypes = [wgp, vp]
     lib.liec_weight_grad_workspace_bytes.restype = C.c_size_t
     lib.liec_weight_grad.argtypes = [wgp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     lib.liec_weight_grad.restype = C.c_int
@@ -685,7 +685,8 @@ def liec_group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, activati
 
 
 @functools.lru_cache(maxsize=1024)
-def _wg_desc(dy, dweight, cols):
+def _wg_desc(dy, dweight, cols, place):
+    """place: dy's address within 16 bytes."""
     d = liec_weight_grad_desc()
     (shape, stride, dtype), (wshape, wstride, wdtype) = dy, dweight
     N = shape[0] if len(shape) == 3 else 1
@@ -697,18 +698,18 @@ def _wg_desc(dy, dweight, cols):
     d.dtype, d.grad_dtype = _dtype_code("dy", dtype), _dtype_code("dweight", wdtype)
     d.dy_row_stride, d.dy_worker_stride = stride[-2], (stride[0] if len(shape) == 3 else 0)
     d.dweight_row_stride, d.dweight_worker_stride = wstride[-2], (wstride[0] if len(shape) == 3 else 0)
-    return d, C.byref(d), int(load_library().liec_weight_grad_workspace_bytes(C.byref(d)))
+    return d, C.byref(d), int(load_library().liec_weight_grad_workspace_bytes(C.byref(d), 256 + place))
 
 
-def liec_weight_grad_workspace_bytes(desc: liec_weight_grad_desc) -> int:
-    return int(load_library().liec_weight_grad_workspace_bytes(C.byref(desc)))
+def liec_weight_grad_workspace_bytes(desc: liec_weight_grad_desc, dy) -> int:
+    return int(load_library().liec_weight_grad_workspace_bytes(C.byref(desc), dy.data_ptr()))
 
 
 def _weight_grad(raw, device, dy, q, scales, cols, dweight, workspace):
     import torch
     if dweight is None:
         dweight = _empty(tuple(dy.shape[:-2]) + (dy.shape[-1], cols), torch.float32, device)
-    _, ref, need = _wg_desc(_layout(dy), _layout(dweight), cols)
+    _, ref, need = _wg_desc(_layout(dy), _layout(dweight), cols, dy.data_ptr() % 16)
     ws, size, keep = _gn_workspace(workspace, need, device)
     lib = _LIB or load_library()
     st = lib.liec_weight_grad(ref, dy.data_ptr(), q.data_ptr(), scales.data_ptr(), dweight.data_ptr(), ws, size, raw)
