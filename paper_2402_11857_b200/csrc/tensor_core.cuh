@@ -69,8 +69,11 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t address, int rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(address), "r"(rank));
     return to;
 }
+// An arrival at a barrier of the cluster.  Every one has to be waited for before the CTA that it goes to ends.  (What it
+// announces are the arriving CTA's own shared memory, made visible to the products by async_fence, and tensor memory; a release
+// for the whole cluster would wait for all earlier accesses to global memory as well, some 1500 cycles.)
 __device__ __forceinline__ void barrier_arrive_cluster(uint32_t cluster_address) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_address) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_address) : "memory");
 }
 __device__ __forceinline__ void barrier_expect(uint32_t barrier, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(barrier), "r"(bytes) : "memory");
@@ -79,9 +82,21 @@ __device__ __forceinline__ void barrier_expect(uint32_t barrier, uint32_t bytes)
 __device__ __forceinline__ bool barrier_wait(uint32_t barrier, uint32_t parity, uint32_t limit) {
     uint32_t done = 0;
     for (uint32_t spin = 0; spin < limit && !done; ++spin)
-        asm volatile("{ .reg .pred q; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 q, [%1], %2; selp.u32 %0, 1, 0, q; }"
+        asm volatile("{ .reg .pred q; mbarrier.try_wait.parity.shared::cta.b64 q, [%1], %2; selp.u32 %0, 1, 0, q; }"
                      : "=r"(done) : "r"(barrier), "r"(parity) : "memory");
     return done != 0;
+}
+// The same for a whole warp.
+__device__ __forceinline__ bool barrier_wait_warp(uint32_t barrier, uint32_t parity, uint32_t limit) {
+    return __all_sync(0xffffffffu, barrier_wait(barrier, parity, limit));
+}
+// True in one thread of a whole warp.  (Loops that a warp walks as one keep what they compute in uniform registers,
+// which products and copies take their operands from: with a loop in one thread alone a stage's four products took 380
+// cycles to issue.)
+__device__ __forceinline__ bool elected() {
+    uint32_t yes;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(yes));
+    return yes != 0u;
 }
 
 // A box of a three-axis array into this CTA's shared memory; x times the element's size is a multiple of 16 bytes.

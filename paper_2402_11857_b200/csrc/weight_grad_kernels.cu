@@ -3,7 +3,7 @@
 //
 // x^ = q 2^e is a bfloat16 number, so the products are those of the definition; a binary32 dy is cut into three bfloat16
 // parts whose sum it is, and multiplied three times.  A pair of CTAs takes a tile of 256 channels c (the rows of the
-// accumulator, 128 in each CTA) by 512 outputs o (256 for binary32), and one run of tokens.  Operands lie in shared memory
+// accumulator, 128 in each CTA) by 512 outputs o (256 for binary32), and as many tokens of it as its share of the work has.  Operands lie in shared memory
 // as in global memory, a token as a row of 128-byte pieces: one thread of each CTA has the tensor memory accelerator bring
 // q and dy, sixteen warps widen q (four groups of four, a stage each in turn, so that one's latency hides behind the
 // others), one thread of the pair issues the products.  Each CTA so widens 128 channels and reads half of the outputs: a
@@ -25,23 +25,77 @@ constexpr int WG_A_BYTES = 2 * WG_BLOCK_BYTES, WG_RAW_BYTES = WG_TOKENS * WG_CHA
 constexpr int WG_GROUPS = 4, WG_GROUP = 128;   // groups of widening threads
 constexpr int WG_WIDENERS = WG_GROUPS * WG_GROUP, WG_THREADS = WG_WIDENERS + 64;
 constexpr int WG_SLAB = 256;                   // outputs of one product of the pair, 128 from each CTA
+constexpr int WG_PAIRS = 74;                  // of SMs
 constexpr uint32_t WG_POLLS = 1u << 20;
 
-// PARTS: bfloat16 parts of dy.  SLABS: products side by side.
+// PARTS: bfloat16 parts of dy.  SLABS: products side by side.  A copied stage (bytes of q, parts of dy) stays from the start
+// of its copies to the end of its products, widened channels from their widening on: as many of the first as fit beside
+// one of the second per group.
 template <int PARTS_>
 struct WgShape {
     static constexpr int PARTS = PARTS_, SLABS = PARTS == 1 ? 2 : 1, OUTPUTS = SLABS * WG_SLAB, COLUMNS = OUTPUTS;
     static constexpr int B_BYTES = 2 * WG_BLOCK_BYTES;                       // of a slab's part
-    static constexpr int STAGE_BYTES = WG_A_BYTES + SLABS * PARTS * B_BYTES + WG_RAW_BYTES;
-    static constexpr int STAGES = PARTS == 1 ? 7 : 6;                        // what fits
-    static constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES;
+    static constexpr int STAGE_BYTES = SLABS * PARTS * B_BYTES + WG_RAW_BYTES;
+    static constexpr int STAGES = PARTS == 1 ? 9 : 6;
+    static constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + WG_GROUPS * WG_A_BYTES;
+    static_assert(SMEM_BYTES <= 227 * 1024 - 512, "with the barriers");
+    static_assert(STAGES >= WG_GROUPS, "the parities of the widening groups' waits");
 };
 inline int wg_parts(int dtype) { return dtype == 0 ? 3 : 1; }
 inline int wg_outputs(int dtype) { return dtype == 0 ? WgShape<3>::OUTPUTS : WgShape<1>::OUTPUTS; }
 
+// The work: all workers' tiles, full ones first, then those with the last, fewer slabs.  As many full tiles as fill the
+// pairs evenly are taken whole; the rest is cut into runs of tokens, whose sums go through the workspace and are joined by
+// another kernel.  Pair k takes items k, k + pairs, ...: neighbours in the list, which read the same operands (channels
+// vary fastest), run side by side and meet in the L2 cache.  (Equal shares of one long line of work instead, cut wherever
+// they end: neighbours then read different tokens, and 8 x 8192 x 768 x 2304 took 270 us before its join, all operands from HBM.)
+struct WgItem {
+    int64_t slot;                // where the sums go in the workspace, in floats; -1: to dW
+    int32_t worker, c_tile, o_tile, slabs, stage, stages;   // first stage and number
+};
 struct WgPlan {
-    int64_t tiles, run;          // per worker; tokens of a run (whole stages)
-    int32_t c_tiles, o_tiles, runs;
+    int64_t full, whole, last, items;              // tiles: full ones, those taken whole, with the last slabs
+    int32_t stages, runs, run, last_runs, last_run;   // stages of a tile; runs of a cut tile and their stages, full and last
+    int32_t c_tiles, o_full, slabs, last_slabs, pairs;
+    __host__ __device__ int64_t slot_size(bool is_last) const { return (int64_t)(is_last ? last_slabs : slabs) * WG_SLAB * 2 * WG_CHANNELS; }
+    __host__ __device__ int64_t slots() const {
+        return (runs > 1 ? (full - whole) * runs * slot_size(false) : 0) + (last_runs > 1 ? last * last_runs * slot_size(true) : 0);
+    }
+    __host__ __device__ WgItem tile_of(int64_t tile) const {
+        WgItem t{};
+        t.slot = -1;
+        if (tile < full) {
+            const int64_t each = (int64_t)c_tiles * o_full;
+            t.worker = (int32_t)(tile / each);
+            const int32_t rest = (int32_t)(tile - t.worker * each);
+            t.o_tile = rest / c_tiles;
+            t.c_tile = rest - t.o_tile * c_tiles;
+            t.slabs = slabs;
+        } else {
+            t.worker = (int32_t)((tile - full) / c_tiles);
+            t.c_tile = (int32_t)(tile - full - (int64_t)t.worker * c_tiles);
+            t.o_tile = o_full;
+            t.slabs = last_slabs;
+        }
+        t.stages = stages;
+        return t;
+    }
+    __host__ __device__ WgItem item(int64_t i) const {
+        if (i < whole) return tile_of(i);
+        i -= whole;
+        const int64_t cut = full - whole;
+        const bool is_last = i >= cut * runs;
+        if (is_last) i -= cut * runs;
+        const int64_t tiles = is_last ? last : cut, run_index = i / tiles;
+        const int32_t n = is_last ? last_runs : runs, length = is_last ? last_run : run;
+        WgItem t = tile_of((is_last ? full : whole) + i - run_index * tiles);
+        if (n > 1) {
+            t.slot = i * slot_size(is_last) + (is_last && runs > 1 ? cut * runs * slot_size(false) : 0);
+            t.stage = (int32_t)run_index * length;
+            t.stages = min(length, stages - t.stage);
+        }
+        return t;
+    }
 };
 
 // 16 bytes of q times their power, as 16 bfloat16 numbers.  Byte b with last seven bits l and sign bit s is l - 128 s:
@@ -122,37 +176,31 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
                                                             const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap dy_map) {
     using S = WgShape<PARTS>;
     extern __shared__ char wg_smem[];
-    __shared__ __align__(8) unsigned long long bars[3 * S::STAGES + 1];
+    __shared__ __align__(8) unsigned long long bars[2 * S::STAGES + WG_GROUPS + 2];
     __shared__ uint32_t tmem_at;
     __shared__ int failed;
     const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars);
     const uint32_t base = ((uint32_t)__cvta_generic_to_shared(wg_smem) + 1023u) & ~1023u;
     auto loaded = [&](int s) { return bar + 8u * s; };                       // the copies of a stage, in this CTA
-    auto full = [&](int s) { return bar + 8u * (S::STAGES + s); };           // both CTAs' operands (in the first CTA)
-    auto empty = [&](int s) { return bar + 8u * (2 * S::STAGES + s); };      // the stage's products are done
-    const uint32_t done = bar + 8u * 3 * S::STAGES;
-    auto a_at = [&](int s) { return base + s * S::STAGE_BYTES; };
-    auto b_at = [&](int s) { return a_at(s) + WG_A_BYTES; };
+    auto empty = [&](int s) { return bar + 8u * (S::STAGES + s); };          // its products are done
+    auto full = [&](int g) { return bar + 8u * (2 * S::STAGES + g); };       // a group's channels, in both CTAs (in the first CTA)
+    const uint32_t done = full(WG_GROUPS), drained = done + 8u;              // a tile's products; its sums are read (in the first CTA)
+    auto b_at = [&](int s) { return base + s * S::STAGE_BYTES; };
     auto raw_at = [&](int s) { return b_at(s) + S::SLABS * PARTS * S::B_BYTES; };
+    auto a_at = [&](int g) { return base + S::STAGES * S::STAGE_BYTES + g * WG_A_BYTES; };
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
-
-    int64_t b = blockIdx.x / 2;
-    const int run = (int)(b % p.runs);
-    b /= p.runs;
-    const int worker = (int)(b / p.tiles), tile = (int)(b % p.tiles);
-    const int o0 = tile / p.c_tiles * S::OUTPUTS, c0 = tile % p.c_tiles * 2 * WG_CHANNELS + rank * WG_CHANNELS;
-    const int slabs = min(S::SLABS, (a.out - o0 + WG_SLAB - 1) / WG_SLAB);
-    const int64_t first = run * p.run, tokens = min(p.run, a.rows - first);
-    const int turns = (int)((tokens + WG_TOKENS - 1) / WG_TOKENS);
+    const int64_t pair = blockIdx.x / 2;
+    auto first_channel = [&](const WgItem &g) { return g.c_tile * 2 * WG_CHANNELS + rank * WG_CHANNELS; };
 
     if (warp == WG_WIDENERS / 32 + 1) {
         if (lane == 0) {
             for (int s = 0; s < S::STAGES; ++s) {
                 barrier_init(loaded(s), 1);
-                barrier_init(full(s), 2 * WG_GROUP / 32);
                 barrier_init(empty(s), 1);
             }
+            for (int k = 0; k < WG_GROUPS; ++k) barrier_init(full(k), 2 * WG_GROUP / 32);
             barrier_init(done, 1);
+            barrier_init(drained, 2 * WG_WIDENERS / 32);
             failed = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             async_fence();
@@ -162,171 +210,260 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
     }
     tc_before_sync();
     __syncthreads();
-    cluster_sync();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+
+    if (warp == WG_WIDENERS / 32) {
+        // copies: into this CTA's memory alone, so the first need not wait for the other CTA
+        asm volatile("griddepcontrol.wait;" ::: "memory");   // dy may come from the kernel before
+        int it = 0;
+        bool ok = true;
+        for (int64_t item = pair; ok && item < p.items; item += p.pairs) {
+            const WgItem g = p.item(item);
+            const int o0 = g.o_tile * S::OUTPUTS + rank * 128, c0 = first_channel(g), t0 = g.stage * WG_TOKENS;
+            for (int i = 0; i < g.stages; ++i, ++it) {
+                const int s = it % S::STAGES, t = t0 + i * WG_TOKENS;
+                if (it >= S::STAGES) ok = barrier_wait_warp(empty(s), (it / S::STAGES - 1) & 1, WG_POLLS);
+                if (!ok) break;
+                if (elected()) {
+                    barrier_expect(loaded(s), WG_RAW_BYTES + g.slabs * PARTS * S::B_BYTES);
+                    copy_box(raw_at(s), &q_map, c0, t, g.worker, loaded(s));
+#pragma unroll
+                    for (int n = 0; n < S::SLABS; ++n)
+                        if (n < g.slabs)
+#pragma unroll
+                            for (int h = 0; h < 2 * PARTS; ++h)
+                                copy_box(b_at(s) + n * PARTS * S::B_BYTES + h * WG_BLOCK_BYTES, &dy_map, o0 + n * WG_SLAB + h % 2 * 64, t,
+                                         h / 2 * a.workers + g.worker, loaded(s));
+                }
+                __syncwarp();
+            }
+        }
+        // nothing may be on its way into this CTA's memory when it ends: the products' last arrivals, or copies
+        for (int k = max(0, it - S::STAGES); ok && k < it; ++k) ok = barrier_wait_warp(empty(k % S::STAGES), (k / S::STAGES) & 1, WG_POLLS);
+        if (!ok) {
+            failed = 1;
+            for (int k = max(0, it - S::STAGES); k < it; ++k) barrier_wait_warp(loaded(k % S::STAGES), (k / S::STAGES) & 1, WG_POLLS);
+        }
+        __syncwarp();
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else {
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");   // the other CTA has its barriers and tensor memory
+    }
     tc_after_sync();
     const uint32_t tmem = tmem_at;
 
-    if (warp == WG_WIDENERS / 32) {
-        if (lane == 0) {   // copies
-            asm volatile("griddepcontrol.wait;" ::: "memory");   // dy may come from the kernel before
-            int i = 0;
+    if (warp == WG_WIDENERS / 32 + 1) {
+        if (rank == 0) {   // products
             bool ok = true;
-            for (; i < turns; ++i) {
-                const int s = i % S::STAGES, t = (int)first + i * WG_TOKENS;
-                if (i >= S::STAGES) ok = barrier_wait(empty(s), (i / S::STAGES - 1) & 1, WG_POLLS);
-                if (!ok) break;
-                barrier_expect(loaded(s), WG_RAW_BYTES + slabs * PARTS * S::B_BYTES);
-                copy_box(raw_at(s), &q_map, c0, t, worker, loaded(s));
-                for (int n = 0; n < slabs; ++n)
+            int it = 0;
+            for (int64_t item = pair, n = 0; ok && item < p.items; item += p.pairs, ++n) {
+                const WgItem g = p.item(item);
+                if (n > 0) ok = barrier_wait_warp(drained, (n - 1) & 1, WG_POLLS);
+                for (int i = 0; ok && i < g.stages; ++i, ++it) {
+                    const int s = it % S::STAGES, k4 = it % WG_GROUPS;
+                    ok = barrier_wait_warp(full(k4), (it / WG_GROUPS) & 1, WG_POLLS);
+                    if (!ok) break;
+                    tc_after_sync();
+                    const uint64_t x = tc_descriptor(a_at(k4), WG_BLOCK_BYTES), y = tc_descriptor(b_at(s), WG_BLOCK_BYTES);
+                    if (elected()) {
 #pragma unroll
-                    for (int part = 0; part < PARTS; ++part)
+                        for (int k = 0; k < WG_TOKENS / 16; ++k)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            copy_box(b_at(s) + (n * PARTS + part) * S::B_BYTES + h * WG_BLOCK_BYTES, &dy_map, o0 + n * WG_SLAB + rank * 128 + h * 64, t,
-                                     part * a.workers + worker, loaded(s));
-            }
-            if (!ok) {   // nothing may be on its way into this CTA's memory when it ends
-                failed = 1;
-                for (int k = max(0, i - S::STAGES); k < i; ++k) barrier_wait(loaded(k % S::STAGES), (k / S::STAGES) & 1, WG_POLLS);
-            }
-        }
-        __syncwarp();
-    } else if (warp == WG_WIDENERS / 32 + 1) {
-        if (lane == 0 && rank == 0) {   // products
-            bool ok = true;
-            for (int i = 0; i < turns; ++i) {
-                const int s = i % S::STAGES;
-                ok = barrier_wait(full(s), (i / S::STAGES) & 1, WG_POLLS);
-                if (!ok) break;
-                tc_after_sync();
+                            for (int n = 0; n < S::SLABS; ++n)
+                                if (n < g.slabs)
 #pragma unroll
-                for (int k = 0; k < WG_TOKENS / 16; ++k) {
-                    const uint64_t x = tc_descriptor(a_at(s) + k * 2048, WG_BLOCK_BYTES);
-                    for (int n = 0; n < slabs; ++n)
-#pragma unroll
-                        for (int part = 0; part < PARTS; ++part)
-                            tc_mma_pair(tmem + n * WG_SLAB, x, tc_descriptor(b_at(s) + (n * PARTS + part) * S::B_BYTES + k * 2048, WG_BLOCK_BYTES),
-                                        tc_instruction(256, WG_SLAB), i > 0 || k > 0 || part > 0);
+                                    for (int part = 0; part < PARTS; ++part)   // (the address field counts 16 bytes)
+                                        tc_mma_pair(tmem + n * WG_SLAB, x + (k * 2048 >> 4), y + (((n * PARTS + part) * S::B_BYTES + k * 2048) >> 4),
+                                                    tc_instruction(256, WG_SLAB), i > 0 || k > 0 || part > 0);
+                        tc_commit_pair(empty(s));
+                    }
+                    __syncwarp();
                 }
-                tc_commit_pair(empty(s));
+                if (!ok && lane == 0) {
+                    const uint32_t flag = (uint32_t)__cvta_generic_to_shared(&failed);
+                    for (int r = 0; r < 2; ++r) asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cta(flag, r)), "r"(1) : "memory");
+                    asm volatile("fence.acq_rel.cluster;" ::: "memory");
+                }
+                __syncwarp();
+                if (elected()) tc_commit_pair(done);
+                __syncwarp();
             }
-            if (!ok) {
-                const uint32_t flag = (uint32_t)__cvta_generic_to_shared(&failed);
-                for (int r = 0; r < 2; ++r) asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_cta(flag, r)), "r"(1) : "memory");
-                asm volatile("fence.acq_rel.cluster;" ::: "memory");
-            }
-            tc_commit_pair(done);
         }
-        __syncwarp();
-    } else {
+    } else if (warp < WG_WIDENERS / 32) {
         // A thread's part of a stage: two chunks of q, 16 channels of one token each.  Eight threads that load or store
         // together meet all places of a 128-byte row, plain in one case and swizzled in the other.
         const int group = warp / 4, parity = lane >> 2 & 1, q_block = parity ^ (lane >> 3 & 1), q_piece = lane & 3;
         const int token = warp % 4 * 4 + (lane >> 4) * 2 + parity;           // and the one 16 further on
         const int64_t row_powers = (a.in + CK_BLOCK - 1) / CK_BLOCK;
-        const int c = c0 + q_block * 64 + q_piece * 16, left = c < row_powers * CK_BLOCK ? (int)tokens : 0;
-        const uint8_t *powers = a.scales + (worker * a.rows + first) * row_powers + c / CK_BLOCK;
-        auto fetch = [&](int i, uint32_t (&power)[2]) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int t = i * WG_TOKENS + token + j * 16;
-                power[j] = t < left ? __ldg(powers + t * row_powers) : 127u;
-            }
-        };
-        auto turn = [&](int i, uint32_t (&power)[2]) {
-            const int s = i % S::STAGES;
-            if (!__all_sync(0xffffffffu, barrier_wait(loaded(s), (i / S::STAGES) & 1, WG_POLLS))) return false;
-            const uint32_t to = a_at(s) + q_block * WG_BLOCK_BYTES, from = raw_at(s) + q_block * 64 + q_piece * 16 + token * 128;
-            uint4 q[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[j].x), "=r"(q[j].y), "=r"(q[j].z), "=r"(q[j].w) : "r"(from + j * 2048) : "memory");
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint4 x[2];
-                wg_widen(q[j], power[j], x);
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + tc_swizzled(token, q_piece * 2 + h) + j * 2048),
-                                 "r"(x[h].x), "r"(x[h].y), "r"(x[h].z), "r"(x[h].w) : "memory");
-            }
-            async_fence();
-            __syncwarp();
-            if (lane == 0) barrier_arrive_cluster(in_cta(full(s), 0));
-            return true;
-        };
-        // the powers run two turns ahead
         bool ok = true;
-        uint32_t even[2], odd[2];
-        fetch(group, even);
-        fetch(group + WG_GROUPS, odd);
-        for (int i = group; i < turns && ok; i += 2 * WG_GROUPS) {
-            ok = turn(i, even);
-            fetch(i + 2 * WG_GROUPS, even);
-            if (ok && i + WG_GROUPS < turns) {
-                ok = turn(i + WG_GROUPS, odd);
-                fetch(i + 3 * WG_GROUPS, odd);
-            }
-        }
-        if (!ok) failed = 1;
-        if (!barrier_wait(done, 0, WG_POLLS)) failed = 1;
-        tc_after_sync();
-        asm volatile("bar.sync 1, %0;" ::"n"(WG_WIDENERS) : "memory");   // everyone's verdict
-        const bool good = *reinterpret_cast<volatile int *>(&failed) == 0;
-        const int ch = c0 + (warp % 4) * 32 + lane;
-        for (int col = group * 32; col < slabs * WG_SLAB && o0 + col < a.out; col += WG_GROUPS * 32) {
-            float v[32];
-            __syncwarp();
-            tc_load(tmem + ((uint32_t)(warp % 4) << 21) + col, v);
-            if (ch >= a.in) continue;
-            if (!good) {   // an unfinished sum is never taken for one
+        int it0 = 0;   // stages before this tile's
+        for (int64_t item = pair, n = 0; item < p.items; item += p.pairs, ++n) {
+            const WgItem g = p.item(item);
+            const int c0 = first_channel(g), c = c0 + q_block * 64 + q_piece * 16;
+            const int64_t first = (int64_t)g.stage * WG_TOKENS;
+            const int left = c < row_powers * CK_BLOCK ? (int)min(a.rows - first, (int64_t)g.stages * WG_TOKENS) : 0;
+            const uint8_t *powers = a.scales + (g.worker * a.rows + first) * row_powers + c / CK_BLOCK;
+            auto fetch = [&](int i, uint32_t (&power)[2]) {   // i: stage of this tile
 #pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(0x7fffffffu);
+                for (int j = 0; j < 2; ++j) {
+                    const int t = i * WG_TOKENS + token + j * 16;
+                    power[j] = t < left ? __ldg(powers + t * row_powers) : 127u;
+                }
+            };
+            auto turn = [&](int i, uint32_t (&power)[2]) {
+                const int s = (it0 + i) % S::STAGES;
+                // The group's place is free when the products of its last turn, WG_GROUPS stages ago, are done.  This wait comes
+                // first: a group does not see every phase of a stage's barriers, and a parity tells a phase from its
+                // neighbours only.  After it all stages up to the last turn's are done, so both barriers are in the phase
+                // that is waited for (STAGES >= WG_GROUPS; here the last turn's own wait vouches for 2 WG_GROUPS stages ago).
+                const int before = it0 + i - WG_GROUPS;
+                if (before >= 0 && !barrier_wait_warp(empty(before % S::STAGES), (before / S::STAGES) & 1, WG_POLLS)) return false;
+                if (!barrier_wait_warp(loaded(s), ((it0 + i) / S::STAGES) & 1, WG_POLLS)) return false;
+                const uint32_t to = a_at(group) + q_block * WG_BLOCK_BYTES, from = raw_at(s) + q_block * 64 + q_piece * 16 + token * 128;
+                uint4 q[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[j].x), "=r"(q[j].y), "=r"(q[j].z), "=r"(q[j].w) : "r"(from + j * 2048) : "memory");
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    uint4 x[2];
+                    wg_widen(q[j], power[j], x);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + tc_swizzled(token, q_piece * 2 + h) + j * 2048),
+                                     "r"(x[h].x), "r"(x[h].y), "r"(x[h].z), "r"(x[h].w) : "memory");
+                }
+                async_fence();
+                __syncwarp();
+                if (lane == 0) barrier_arrive_cluster(in_cta(full(group), 0));
+                return true;
+            };
+            // the powers run two turns ahead
+            uint32_t even[2], odd[2];
+            const int begin = (group - it0 % WG_GROUPS + WG_GROUPS) % WG_GROUPS;
+            fetch(begin, even);
+            fetch(begin + WG_GROUPS, odd);
+            for (int i = begin; i < g.stages && ok; i += 2 * WG_GROUPS) {
+                ok = turn(i, even);
+                fetch(i + 2 * WG_GROUPS, even);
+                if (ok && i + WG_GROUPS < g.stages) {
+                    ok = turn(i + WG_GROUPS, odd);
+                    fetch(i + 3 * WG_GROUPS, odd);
+                }
             }
-            const int o = o0 + col;
-            if (p.runs > 1) wg_store_column(a.part + (((int64_t)run * a.workers + worker) * a.out + o) * a.in + ch, a.in, a.out - o, v);
-            else if (a.grad_dtype == LIEC_F32) wg_store_column(static_cast<float *>(a.dweight) + worker * a.dw_worker + o * a.dw_row + ch, a.dw_row, a.out - o, v);
-            else wg_store_column(static_cast<__nv_bfloat16 *>(a.dweight) + worker * a.dw_worker + o * a.dw_row + ch, a.dw_row, a.out - o, v);
+            if (ok) ok = barrier_wait(done, n & 1, WG_POLLS);
+            if (!ok) failed = 1;
+            tc_after_sync();
+            asm volatile("bar.sync 1, %0;" ::"n"(WG_WIDENERS) : "memory");   // everyone's verdict
+            if (*reinterpret_cast<volatile int *>(&failed)) ok = false;
+            const int o0 = g.o_tile * S::OUTPUTS, mine = (warp % 4) * 32 + lane, ch = c0 + mine;
+            float *part = a.part + g.slot + rank * WG_CHANNELS + mine;
+            for (int col = group * 32; col < g.slabs * WG_SLAB && o0 + col < a.out; col += WG_GROUPS * 32) {
+                float v[32];
+                __syncwarp();
+                tc_load(tmem + ((uint32_t)(warp % 4) << 21) + col, v);
+                if (!ok) {   // an unfinished sum is never taken for one
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(0x7fffffffu);
+                }
+                const int o = o0 + col;
+                if (g.slot >= 0) wg_store_column(part + col * 2 * WG_CHANNELS, 2 * WG_CHANNELS, 32, v);
+                else if (ch >= a.in) continue;
+                else if (a.grad_dtype == LIEC_F32) wg_store_column(static_cast<float *>(a.dweight) + g.worker * a.dw_worker + o * a.dw_row + ch, a.dw_row, a.out - o, v);
+                else wg_store_column(static_cast<__nv_bfloat16 *>(a.dweight) + g.worker * a.dw_worker + o * a.dw_row + ch, a.dw_row, a.out - o, v);
+            }
+            tc_before_sync();
+            __syncwarp();
+            if (lane == 0 && item + p.pairs < p.items) barrier_arrive_cluster(in_cta(drained, 0));   // the next item's products wait for this
+            it0 += g.stages;
         }
-        tc_before_sync();
     }
+    tc_before_sync();
     __syncthreads();
+    __syncwarp();
+    if (failed) {   // arrivals that nobody waited for, and products: time to come to their end
+        long long t0, t1;
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+        for (int spin = 0; spin < 1 << 22; ++spin) {
+            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
+            if (t1 - t0 > 1000000) break;
+        }
+    }
     cluster_sync();   // neither CTA ends while the other may still reach into it
     if (warp == WG_WIDENERS / 32 + 1) tc_free_pair(tmem, S::COLUMNS);
 }
 
-// The runs' sums, in their order, rounded once to the gradient's type; zeros without runs.
-__global__ void __launch_bounds__(256) wg_join_kernel(const __grid_constant__ WgArgs a, int runs) {
-    const int64_t n = (int64_t)a.workers * a.out * a.in, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    float s = 0.0f;
-    for (int r = 0; r < runs; ++r) s += __ldcs(a.part + r * n + i);
-    const int64_t row = i / a.in, c = i - row * a.in, w = row / a.out, at = w * a.dw_worker + (row - w * a.out) * a.dw_row + c;
-    if (a.grad_dtype == LIEC_F32) static_cast<float *>(a.dweight)[at] = s;
-    else static_cast<__nv_bfloat16 *>(a.dweight)[at] = __float2bfloat16_rn(s);
+// A cut tile's runs, added in their order and rounded once to the gradient's type.  Block (x, y) has 16 outputs of cut tile y.
+constexpr int WG_JOIN_OUTPUTS = 16;
+__global__ void __launch_bounds__(256) wg_join_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ WgPlan p) {
+    const int64_t cut = p.runs > 1 ? p.full - p.whole : 0;
+    const bool is_last = blockIdx.y >= cut;
+    const int64_t index = is_last ? blockIdx.y - cut : blockIdx.y, tiles = is_last ? p.last : cut, size = p.slot_size(is_last);
+    const WgItem t = p.tile_of((is_last ? p.full : p.whole) + index);
+    const int runs = is_last ? p.last_runs : p.runs, lane = threadIdx.x % 64, c = t.c_tile * 2 * WG_CHANNELS + lane * 4;
+    const float *from = a.part + index * size + (is_last ? cut * p.runs * p.slot_size(false) : 0) + lane * 4;
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // the sums are complete
+    for (int y = threadIdx.x / 64; y < WG_JOIN_OUTPUTS; y += 4) {
+        const int row = blockIdx.x * WG_JOIN_OUTPUTS + y, o = t.o_tile * p.slabs * WG_SLAB + row;
+        if (o >= a.out || row >= t.slabs * WG_SLAB || c >= a.in) continue;
+        const float4 *at = reinterpret_cast<const float4 *>(from + row * 2 * WG_CHANNELS);
+        float4 s = __ldcs(at);
+#pragma unroll 4
+        for (int r = 1; r < runs; ++r) {
+            const float4 v = __ldcs(at + r * (tiles * size / 4));
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        const float v[4] = {s.x, s.y, s.z, s.w};
+        const int64_t to = t.worker * a.dw_worker + o * a.dw_row + c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < a.in) {
+                if (a.grad_dtype == LIEC_F32) static_cast<float *>(a.dweight)[to + e] = v[e];
+                else static_cast<__nv_bfloat16 *>(a.dweight)[to + e] = __float2bfloat16_rn(v[e]);
+            }
+    }
 }
 
-// Runs of tokens: as many as make the GPU's 74 pairs of SMs busy, weighed against what joining them costs.  In units of a
-// stage's products (512 cycles): a pair's start and end take about 12, writing and reading a run's sums of a tile 12.
+__global__ void __launch_bounds__(256) wg_zero_kernel(const __grid_constant__ WgArgs a) {   // no tokens
+    const int64_t n = (int64_t)a.workers * a.out * a.in, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    const int64_t row = i / a.in, w = row / a.out, at = w * a.dw_worker + (row - w * a.out) * a.dw_row + i - row * a.in;
+    if (a.grad_dtype == LIEC_F32) static_cast<float *>(a.dweight)[at] = 0.0f;
+    else static_cast<__nv_bfloat16 *>(a.dweight)[at] = __float2bfloat16_rn(0.0f);
+}
+
+// How many runs a cut tile has: the least time of the pair that has most to do, by what was measured (us): a slab's stage
+// takes 0.18, 0.6 with three parts of dy; an item's start and end 3; a run of a cut tile 0.1 per slab (written, read, added), the
+// joining launch 4.  Tiles with half the slabs have half the runs.
 static WgPlan wg_plan(const WgArgs &a, int dtype) {
     WgPlan p{};
-    const int outputs = wg_outputs(dtype);
+    const int outputs = wg_outputs(dtype), slabs_all = (a.out + WG_SLAB - 1) / WG_SLAB;
+    p.slabs = outputs / WG_SLAB;
     p.c_tiles = (a.in + 2 * WG_CHANNELS - 1) / (2 * WG_CHANNELS);
-    p.o_tiles = (a.out + outputs - 1) / outputs;
-    p.tiles = (int64_t)p.c_tiles * p.o_tiles;
-    const int64_t stages = (a.rows + WG_TOKENS - 1) / WG_TOKENS, places = p.tiles * a.workers;
+    p.o_full = slabs_all / p.slabs;
+    p.last_slabs = slabs_all % p.slabs;
+    p.stages = (int32_t)((a.rows + WG_TOKENS - 1) / WG_TOKENS);
+    p.full = (int64_t)a.workers * p.c_tiles * p.o_full;
+    p.last = p.last_slabs ? (int64_t)a.workers * p.c_tiles : 0;
+    p.whole = p.full / WG_PAIRS * WG_PAIRS;
+    const double unit = dtype == 0 ? 0.6 : 0.18;
+    const int64_t cut = p.full - p.whole;
     double best = 0.0;
-    p.runs = 0;
-    for (int runs = 1; runs <= 64 && runs <= std::max<int64_t>(stages, 1) && places * runs < int64_t(1) << 30; ++runs) {
-        const int64_t length = (stages + runs - 1) / runs, used = std::max<int64_t>(1, (stages + length - 1) / std::max<int64_t>(length, 1));
-        if (used != runs && runs > 1) continue;
-        const double cost = (double)((places * runs + 73) / 74) * (double)(length + 12) + (runs > 1 ? 20.0 + 12.0 * (double)(places * runs) / 74.0 : 0.0);
-        if (p.runs == 0 || cost < best) {
-            best = cost;
-            p.runs = runs;
-            p.run = std::max<int64_t>(1, length) * WG_TOKENS;
-        }
+    for (int n = 1; n <= WG_PAIRS && n <= p.stages; ++n) {
+        const int run = (p.stages + n - 1) / n, runs = cut ? (p.stages + run - 1) / run : 1;
+        const int last_n = cut ? std::max(1, n * p.last_slabs / p.slabs) : n;
+        const int last_run = (p.stages + last_n - 1) / last_n, last_runs = p.last ? (p.stages + last_run - 1) / last_run : 1;
+        const int64_t items = cut * runs + p.last * last_runs;
+        if (items > 16 * WG_PAIRS && n > 1) break;
+        double cost = 0.0;
+        for (int64_t i = 0; i < items && i < 16 * WG_PAIRS; i += WG_PAIRS) cost += 3.0 + unit * (i < cut * runs ? p.slabs * run : p.last_slabs * last_run);
+        if (runs > 1 || last_runs > 1) cost += 4.0 + 0.1 * (double)((runs > 1 ? cut * runs * p.slabs : 0) + (last_runs > 1 ? p.last * last_runs * p.last_slabs : 0));
+        if (n > 1 && cost >= best) continue;
+        best = cost;
+        p.runs = runs; p.run = run; p.last_runs = last_runs; p.last_run = last_run;
+        p.items = p.whole + items;
     }
+    p.pairs = (int32_t)std::min<int64_t>(WG_PAIRS, p.items);
     return p;
 }
 
@@ -335,14 +472,12 @@ static bool wg_direct(const WgArgs &a, int dtype) {
     return dtype == 1 && ln_whole(a.dy, a.dy_row, a.dy_worker, a.rows, a.workers, 8, 2) && (a.rows == 1 || a.dy_row >= a.out) &&
            (a.workers == 1 || a.dy_worker >= a.out);
 }
-static size_t wg_part_bytes(const WgArgs &a, const WgPlan &p) {
-    return p.runs > 1 ? (sizeof(float) * (size_t)p.runs * a.workers * a.out * a.in + 255) / 256 * 256 : 0;
-}
+static size_t wg_part_bytes(const WgPlan &p) { return sizeof(float) * (size_t)p.slots(); }
 
 size_t weight_grad_workspace(const WgArgs &a, int dtype) {
     if (a.rows == 0) return 0;
     const size_t packed = wg_direct(a, dtype) ? 0 : (size_t)wg_parts(dtype) * a.workers * a.rows * ((a.out + 7) / 8) * 16;
-    return wg_part_bytes(a, wg_plan(a, dtype)) + packed;
+    return wg_part_bytes(wg_plan(a, dtype)) + packed;
 }
 
 // The function behind cuTensorMapEncodeTiled: asked of the runtime, so that the library links without the driver's.
@@ -393,7 +528,7 @@ static cudaError_t wg_launch(const WgArgs &a, const WgPlan &p, const CUtensorMap
     const auto kernel = wg_kernel<PARTS>;
     const cudaError_t e = ln_allow_smem(kernel, WgShape<PARTS>::SMEM_BYTES, allowed);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = wg_config(p.tiles * a.workers * p.runs * 2, WG_THREADS, WgShape<PARTS>::SMEM_BYTES, st);
+    cudaLaunchConfig_t cfg = wg_config((int64_t)p.pairs * 2, WG_THREADS, WgShape<PARTS>::SMEM_BYTES, st);
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
@@ -406,30 +541,37 @@ static cudaError_t wg_launch(const WgArgs &a, const WgPlan &p, const CUtensorMap
 }
 
 cudaError_t launch_weight_grad(WgArgs a, int dtype, cudaStream_t st) {
-    int runs = 0;
-    if (a.rows > 0) {
-        const WgPlan p = wg_plan(a, dtype);
-        const bool direct = wg_direct(a, dtype);
-        const int64_t q_cols = ck_cols(a.in), dy_cols = (a.out + 7) / 8 * 8;
-        a.packed = reinterpret_cast<char *>(a.part) + wg_part_bytes(a, p);
-        CUtensorMap q_map, dy_map;
-        if (!wg_map(&q_map, a.q, true, q_cols, a.rows, a.workers, q_cols, q_cols * a.rows, WG_CHANNELS) ||
-            !(direct ? wg_map(&dy_map, a.dy, false, a.out, a.rows, a.workers, a.dy_row, a.dy_worker, 64)
-                     : wg_map(&dy_map, a.packed, false, a.out, a.rows, (int64_t)wg_parts(dtype) * a.workers, dy_cols, dy_cols * a.rows, 64)))
-            return cudaErrorNotSupported;
-        if (!direct) {
-            const int64_t chunks = a.workers * a.rows * (dy_cols / 8);
-            const cudaLaunchConfig_t cfg = wg_config((chunks + 255) / 256, 256, 0, st);
-            const cudaError_t e = cudaLaunchKernelEx(&cfg, dtype == 0 ? wg_pack_kernel<float> : wg_pack_kernel<__nv_bfloat16>, a, dy_cols / 8);
-            if (e != cudaSuccess) return e;
-        }
-        const cudaError_t e = dtype == 0 ? wg_launch<3>(a, p, q_map, dy_map, !direct, st) : wg_launch<1>(a, p, q_map, dy_map, !direct, st);
-        if (e != cudaSuccess || p.runs == 1) return e;
-        runs = p.runs;
+    if (a.rows == 0) {
+        wg_zero_kernel<<<(unsigned)(((int64_t)a.workers * a.out * a.in + 255) / 256), 256, 0, st>>>(a);
+        return cudaGetLastError();
     }
-    const int64_t n = (int64_t)a.workers * a.out * a.in;
-    wg_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(a, runs);
-    return cudaGetLastError();
+    const WgPlan p = wg_plan(a, dtype);
+    const bool direct = wg_direct(a, dtype);
+    const int64_t q_cols = ck_cols(a.in), dy_cols = (a.out + 7) / 8 * 8;
+    a.packed = reinterpret_cast<char *>(a.part) + wg_part_bytes(p);
+    CUtensorMap q_map, dy_map;
+    if (!wg_map(&q_map, a.q, true, q_cols, a.rows, a.workers, q_cols, q_cols * a.rows, WG_CHANNELS) ||
+        !(direct ? wg_map(&dy_map, a.dy, false, a.out, a.rows, a.workers, a.dy_row, a.dy_worker, 64)
+                 : wg_map(&dy_map, a.packed, false, a.out, a.rows, (int64_t)wg_parts(dtype) * a.workers, dy_cols, dy_cols * a.rows, 64)))
+        return cudaErrorNotSupported;
+    cudaError_t e = cudaSuccess;
+    if (!direct) {
+        const int64_t chunks = a.workers * a.rows * (dy_cols / 8);
+        const cudaLaunchConfig_t cfg = wg_config((chunks + 255) / 256, 256, 0, st);
+        e = cudaLaunchKernelEx(&cfg, dtype == 0 ? wg_pack_kernel<float> : wg_pack_kernel<__nv_bfloat16>, a, dy_cols / 8);
+        if (e != cudaSuccess) return e;
+    }
+    e = dtype == 0 ? wg_launch<3>(a, p, q_map, dy_map, !direct, st) : wg_launch<1>(a, p, q_map, dy_map, !direct, st);
+    const int64_t joined = (p.runs > 1 ? p.full - p.whole : 0) + (p.last_runs > 1 ? p.last : 0);
+    if (e != cudaSuccess || joined == 0) return e;
+    cudaLaunchConfig_t cfg = wg_config(p.slabs * WG_SLAB / WG_JOIN_OUTPUTS, 256, 0, st);
+    cfg.gridDim.y = (unsigned)joined;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, wg_join_kernel, a, p);
 }
 
 }  // namespace liec

@@ -116,3 +116,22 @@ def test_refusals():
     big = torch.zeros(2 * 24 * 40, device="cuda")                # dy within dweight
     with pytest.raises(liec.LiecError, match="overlaps an input"):
         weight_grad(big[:2 * 20 * 24].view(2, 20, 24), q, scales, 40, dweight=big.view(2, 24, 40))
+
+
+@pytest.mark.parametrize("N,rows,h,out,dtype", [(90, 70, 40, 48, "f32"), (100, 33, 256, 600, "bf16"), (7, 2100, 600, 1300, "bf16"), (160, 200, 30, 20, "bf16"),
+                                                (3, 900, 2000, 1700, "f32"), (2, 3300, 700, 300, "bf16")])
+def test_more_tiles_than_pairs_of_sms(N, rows, h, out, dtype):
+    """Several tiles one after another, whole and cut."""
+    dy, q, scales = draw(N, rows, h, out, dtype, seed=N)
+    got = weight_grad(dy, q, scales, h)
+    check_weight_grad(dy, restored64(q, scales, h), "f32", got)
+    assert torch.equal(weight_grad(dy, q, scales, h), got)
+
+
+def test_copies_that_come_late():
+    """All operands from memory and several tiles per pair: copies lag behind the products.  Equal bits over many calls."""
+    dy, q, scales = draw(148, 1024, 256, 256, "f32", seed=31)
+    want = weight_grad(dy, q, scales, 256)
+    check_weight_grad(dy[:3], restored64(q[:3], scales[:3], 256), "f32", want[:3])
+    for _ in range(10):
+        assert torch.equal(weight_grad(dy, q, scales, 256), want)
