@@ -10,15 +10,31 @@ namespace liec {
 
 constexpr int GN_THREADS = 256;
 
+// A chunk of a row on its way to this thread's place in shared memory: asynchronously where rows start on 16 bytes.
+template <typename T>
+__device__ __forceinline__ void gn_fetch(const GnArgs &a, uint32_t to, const T *row, int c) {
+    if (a.whole) {
+        const int bytes = min(16, max(0, (a.channels - c) * (int)sizeof(T)));
+        copy_async(to, bytes > 0 ? row + c : row, bytes);
+    } else {
+        const uint4 v = c < a.channels ? load_chunk(row, c, a.channels) : make_uint4(0u, 0u, 0u, 0u);
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+    }
+}
+
 // Where a chunk of x comes from: the activations themselves, or their checkpoint.
 template <typename T>
 struct GnFromX {
+    static constexpr bool CHECKPOINT = false;
     using Raw = uint4;
     const T *row;
     int64_t pixel;
     __device__ __forceinline__ GnFromX(const GnArgs &a, int worker, int sample, int64_t p)
         : row(static_cast<const T *>(a.x) + worker * a.x_worker + sample * a.x_sample + p * a.x_pixel), pixel(a.x_pixel) {}
     __device__ __forceinline__ Raw load(int64_t p, int c, int cols) const { return load_chunk(row + p * pixel, c, cols); }
+    // the same by way of shared memory
+    __device__ __forceinline__ void fetch(const GnArgs &a, uint32_t to, uint8_t *, int64_t p, int c) const { gn_fetch(a, to, row + p * pixel, c); }
+    static __device__ __forceinline__ Raw kept(const char *place, const uint8_t *) { return *reinterpret_cast<const uint4 *>(place); }
     template <int P>
     static __device__ __forceinline__ void centred(const Raw &raw, const F2 (&minus)[P], F2 (&d)[P]) {
         LnChunk<T>::read(raw, d);
@@ -29,6 +45,7 @@ struct GnFromX {
 
 template <typename T>
 struct GnFromCheckpoint {
+    static constexpr bool CHECKPOINT = true;
     struct Raw { uint32_t w[Bits<T>::VEC / 4]; uint32_t byte; };
     const int8_t *q;
     const uint8_t *scales;
@@ -50,6 +67,22 @@ struct GnFromCheckpoint {
             r.w[0] = __ldg(reinterpret_cast<const uint32_t *>(at));
         }
         r.byte = __ldg(scales + p * (cols / CK_BLOCK) + c / CK_BLOCK);
+        return r;
+    }
+    __device__ __forceinline__ void fetch(const GnArgs &, uint32_t to, uint8_t *power, int64_t p, int c) const {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(q + p * cols + c), "n"(Bits<T>::VEC) : "memory");
+        *power = __ldg(scales + p * (cols / CK_BLOCK) + c / CK_BLOCK);
+    }
+    static __device__ __forceinline__ Raw kept(const char *place, const uint8_t *power) {
+        Raw r;
+        if constexpr (Bits<T>::VEC == 8) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(place);
+            r.w[0] = v.x;
+            r.w[1] = v.y;
+        } else {
+            r.w[0] = *reinterpret_cast<const uint32_t *>(place);
+        }
+        r.byte = *power;
         return r;
     }
     template <int P>
@@ -83,7 +116,7 @@ __device__ __forceinline__ float gn_silu_slope(float z, float dy) {
 }
 
 // z from its definition in binary64.
-__device__ __noinline__ bool gn_positive(const GnArgs &a, int worker, int64_t image, int c, float x) {
+static __device__ __noinline__ bool gn_positive(const GnArgs &a, int worker, int64_t image, int c, float x) {
     const int64_t g = image * a.groups + c / (a.channels / a.groups);
     const double w = a.weight ? (double)a.weight[worker * a.weight_stride + c] : 1.0, b = a.bias ? (double)a.bias[worker * a.bias_stride + c] : 0.0;
     return ((double)x - (double)a.mean[g]) * (double)a.rstd[g] * w + b > 0.0;
@@ -93,21 +126,29 @@ __device__ __noinline__ bool gn_positive(const GnArgs &a, int worker, int64_t im
 template <int P>
 struct GnChannels {
     F2 minus[P], scale[P], bias[P];
-    __device__ __forceinline__ void read(const GnArgs &a, int worker, int64_t image, int c) {
-        const int width = a.channels / a.groups;
+    // statistics(channel, m, r)
+    template <typename F>
+    __device__ __forceinline__ void read(const GnArgs &a, int worker, int c, F &&statistics) {
 #pragma unroll
         for (int k = 0; k < 2 * P; ++k) {
             float m = 0.0f, s = 0.0f, b = 0.0f;
             if (c + k < a.channels) {
-                const int64_t g = image * a.groups + (c + k) / width;
-                m = -a.mean[g];
-                s = a.rstd[g] * (a.weight ? __ldg(a.weight + worker * a.weight_stride + c + k) : 1.0f);
+                statistics(c + k, m, s);
+                s *= a.weight ? __ldg(a.weight + worker * a.weight_stride + c + k) : 1.0f;
                 b = a.bias ? __ldg(a.bias + worker * a.bias_stride + c + k) : 0.0f;
             }
-            set(minus[k / 2], k % 2, m);
+            set(minus[k / 2], k % 2, -m);
             set(scale[k / 2], k % 2, s);
             set(bias[k / 2], k % 2, b);
         }
+    }
+    __device__ __forceinline__ void read(const GnArgs &a, int worker, int64_t image, int c) {
+        const int width = a.channels / a.groups;
+        read(a, worker, c, [&](int channel, float &m, float &r) {
+            const int64_t g = image * a.groups + channel / width;
+            m = a.mean[g];
+            r = a.rstd[g];
+        });
     }
     static __device__ __forceinline__ void set(F2 &p, int odd, float v) { p = odd ? f2(lo(p), v) : f2(v, 0.0f); }
 };
@@ -151,6 +192,45 @@ __device__ __forceinline__ void gn_slope(const GnArgs &a, int worker, int64_t im
 #pragma unroll
         for (int k = 0; k < P; ++k) dz[k] = f2(on >> 2 * k & 1u ? lo(dy[k]) : 0.0f, on >> 2 * k & 2u ? hi(dy[k]) : 0.0f);
     }
+}
+
+// The bytes and powers of a chunk of x: the 4 or 8 threads of a block are neighbours in a warp and here together.
+template <typename T>
+__device__ __forceinline__ void gn_compress(const GnArgs &a, const F2 (&x)[Bits<T>::VEC / 2], int64_t row, int c) {
+    constexpr int VEC = Bits<T>::VEC, P = VEC / 2, LANES = CK_BLOCK / VEC;
+    const int64_t cols = (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK;
+    uint32_t top = chunk_top(x);
+    const uint32_t mates = ((1u << LANES) - 1u) << (threadIdx.x & 31 & ~(LANES - 1));
+#pragma unroll
+    for (int m = LANES / 2; m >= 1; m >>= 1) top = max(top, __shfl_xor_sync(mates, top, m));
+    const uint32_t byte = ck_scale_byte(__uint_as_float(top));
+    F2 v[P];
+#pragma unroll
+    for (int k = 0; k < P; ++k) v[k] = x[k];
+    uint32_t words[P / 2];
+    ck_bytes<P>(v, byte, words);
+    int8_t *q = a.q + row * cols + c;
+    if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(q) = make_uint2(words[0], words[1]);
+    else *reinterpret_cast<uint32_t *>(q) = words[0];
+    if (c % CK_BLOCK == 0) a.scales[(row * cols + c) / CK_BLOCK] = (uint8_t)byte;
+}
+
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+    for (int m = 16; m >= 1; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+    return v;
+}
+
+// Images that a cluster holds in shared memory (group_norm_resident.cu): sets the launch's sizes, or says no.
+bool gn_resident_plan(GnArgs &a, int dtype, bool backward, bool checkpoint, int &smem);
+cudaError_t gn_resident_forward(const GnArgs &a, int dtype, int smem, cudaStream_t st);
+cudaError_t gn_resident_backward(const GnArgs &a, int dtype, int smem, cudaStream_t st);
+
+template <typename F>
+cudaError_t gn_for_act(int act, F &&f) {
+    if (act == LIEC_ACT_RELU) return f.template operator()<LIEC_ACT_RELU>();
+    if (act == LIEC_ACT_SILU) return f.template operator()<LIEC_ACT_SILU>();
+    return f.template operator()<LIEC_ACT_NONE>();
 }
 
 }  // namespace liec

@@ -84,12 +84,6 @@ __global__ void __launch_bounds__(GN_THREADS) gn_moments_kernel(const __grid_con
 }
 
 // Joins a group's channels and parts: a warp per group, binary64, in a fixed order.
-__device__ __forceinline__ double warp_sum(double v) {
-#pragma unroll
-    for (int m = 16; m >= 1; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
-    return v;
-}
-
 __global__ void __launch_bounds__(GN_THREADS) gn_statistics_kernel(const __grid_constant__ GnArgs a) {
     const int64_t g = ((int64_t)blockIdx.x * GN_THREADS + threadIdx.x) / 32, images = (int64_t)a.workers * a.samples;
     if (g >= images * a.groups) return;
@@ -118,32 +112,20 @@ __global__ void __launch_bounds__(GN_THREADS) gn_statistics_kernel(const __grid_
 
 template <typename T, int ACT, bool COMPRESS>
 __global__ void __launch_bounds__(GN_THREADS) gn_apply_kernel(const __grid_constant__ GnArgs a) {
-    constexpr int VEC = Bits<T>::VEC, P = VEC / 2, LANES = CK_BLOCK / VEC;
+    constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
     const GnPlace at(a, VEC);
     if (!at.live) return;
     const GnFromX<T> x(a, at.worker, at.sample, at.p0);
     T *y = static_cast<T *>(a.y) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
     GnChannels<P> ch;
     ch.read(a, at.worker, at.image, at.c);
-    const int64_t q_cols = (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK;
     const int64_t row0 = at.image * a.pixels + at.p0;
     for (int64_t p = at.lane; p < at.n; p += at.lanes) {
         const uint4 raw = x.load(p, at.c, a.channels);
         F2 d[P];
         if constexpr (COMPRESS) {
-            F2 v[P];
-            LnChunk<T>::read(raw, v);
-            uint32_t top = chunk_top(v);
-            const uint32_t mates = ((1u << LANES) - 1u) << (threadIdx.x & 31 & ~(LANES - 1));
-#pragma unroll
-            for (int m = LANES / 2; m >= 1; m >>= 1) top = max(top, __shfl_xor_sync(mates, top, m));
-            const uint32_t byte = ck_scale_byte(__uint_as_float(top));
-            uint32_t words[P / 2];
-            ck_bytes<P>(v, byte, words);
-            int8_t *q = a.q + (row0 + p) * q_cols + at.c;
-            if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(q) = make_uint2(words[0], words[1]);
-            else *reinterpret_cast<uint32_t *>(q) = words[0];
-            if (at.c % CK_BLOCK == 0) a.scales[((row0 + p) * q_cols + at.c) / CK_BLOCK] = (uint8_t)byte;
+            LnChunk<T>::read(raw, d);
+            gn_compress<T>(a, d, row0 + p, at.c);
         }
         GnFromX<T>::centred(raw, ch.minus, d);
 #pragma unroll
@@ -280,18 +262,30 @@ static void gn_plan(GnArgs &a, int vec) {
     a.parts = (int)std::max<int64_t>(1, (a.pixels + a.part_pixels - 1) / a.part_pixels);
 }
 
-size_t group_norm_workspace(const GnArgs &given, int dtype, bool backward) {
-    GnArgs a = given;
+static size_t gn_streamed_workspace(GnArgs a, int dtype, bool backward) {
     gn_plan(a, dtype == 0 ? 4 : 8);
     const size_t images = (size_t)a.workers * a.samples;
     return sizeof(float) * (images * a.parts * 2 * a.channels + (backward ? images * a.groups * 2 : 0));
 }
 
-template <typename F>
-static cudaError_t gn_for_act(int act, F &&f) {
-    if (act == LIEC_ACT_RELU) return f.template operator()<LIEC_ACT_RELU>();
-    if (act == LIEC_ACT_SILU) return f.template operator()<LIEC_ACT_SILU>();
-    return f.template operator()<LIEC_ACT_NONE>();
+size_t group_norm_workspace(const GnArgs &a, int dtype, bool backward) {
+    size_t need = 0;
+    for (int checkpoint = 0; checkpoint < (backward ? 2 : 1); ++checkpoint) {   // (a descriptor does not say which)
+        GnArgs b = a;
+        int smem;
+        const bool resident = gn_resident_plan(b, dtype, backward, checkpoint != 0, smem);
+        need = std::max(need, !resident ? gn_streamed_workspace(a, dtype, backward) : backward ? sizeof(float) * a.workers * a.samples * 2 * (size_t)a.channels : 0);
+    }
+    return need;
+}
+
+static bool gn_whole(const GnArgs &a, int dtype, const void *p, int64_t pixel, int64_t sample, int64_t worker) {
+    uint64_t bits = reinterpret_cast<uintptr_t>(p);
+    const uint64_t size = dtype == 0 ? 4 : 2;
+    if (a.pixels > 1) bits |= (uint64_t)pixel * size;
+    if (a.samples > 1) bits |= (uint64_t)sample * size;
+    if (a.workers > 1) bits |= (uint64_t)worker * size;
+    return (bits & 15u) == 0;
 }
 
 static unsigned gn_group_ctas(const GnArgs &a) {
@@ -314,9 +308,14 @@ struct GnForwardLaunch {
 };
 
 cudaError_t launch_group_norm_forward(GnArgs a, int dtype, cudaStream_t st) {
+    if (a.samples == 0 || a.pixels == 0) return cudaSuccess;
+    int smem;
+    if (gn_resident_plan(a, dtype, false, false, smem)) {
+        a.whole = gn_whole(a, dtype, a.x, a.x_pixel, a.x_sample, a.x_worker);
+        return gn_resident_forward(a, dtype, smem, st);
+    }
     gn_plan(a, dtype == 0 ? 4 : 8);
     const unsigned ctas = (unsigned)((int64_t)a.workers * a.samples * a.tiles * a.parts);
-    if (ctas == 0 || a.pixels == 0) return cudaSuccess;
     return dtype == 0 ? gn_for_act(a.act, GnForwardLaunch<float>{a, ctas, st}) : gn_for_act(a.act, GnForwardLaunch<__nv_bfloat16>{a, ctas, st});
 }
 
@@ -342,10 +341,18 @@ static cudaError_t gn_backward(const GnArgs &a, unsigned ctas, cudaStream_t st) 
 }
 
 cudaError_t launch_group_norm_backward(GnArgs a, int dtype, cudaStream_t st) {
-    gn_plan(a, dtype == 0 ? 4 : 8);
-    a.level = a.part + (int64_t)a.workers * a.samples * a.parts * 2 * a.channels;
-    const unsigned ctas = (unsigned)((int64_t)a.workers * a.samples * a.tiles * a.parts);
-    if (ctas > 0 && a.pixels > 0) {
+    int smem;
+    if (a.samples == 0 || a.pixels == 0) {
+        a.parts = 1;
+    } else if (gn_resident_plan(a, dtype, true, !a.x, smem)) {
+        a.whole = gn_whole(a, dtype, a.dy, a.y_pixel, a.y_sample, a.y_worker) && (!a.x || gn_whole(a, dtype, a.x, a.x_pixel, a.x_sample, a.x_worker));
+        const cudaError_t e = gn_resident_backward(a, dtype, smem, st);
+        if (e != cudaSuccess) return e;
+        a.parts = 1;   // (the cluster's parts are one by now)
+    } else {
+        gn_plan(a, dtype == 0 ? 4 : 8);
+        a.level = a.part + (int64_t)a.workers * a.samples * a.parts * 2 * a.channels;
+        const unsigned ctas = (unsigned)((int64_t)a.workers * a.samples * a.tiles * a.parts);
         const cudaError_t e = dtype == 0 ? gn_backward<float>(a, ctas, st) : gn_backward<__nv_bfloat16>(a, ctas, st);
         if (e != cudaSuccess) return e;
     }

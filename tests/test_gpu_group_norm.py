@@ -91,11 +91,13 @@ def test_three_axes_shared_and_missing_parameters(pixels, dtype):
     dx, dw, db = backward(dy, x, mean, rstd, w1, b1, activation="relu")
     assert dw.shape == (48,)
     check_group_norm_backward(dy, x, mean, rstd, w[:1].expand(3, 48), b[:1].expand(3, 48), "relu", dtype, "f32", dx, dw, db, shared=True)
-    # one worker without the axis
-    got = forward(x[1], 6, w1, b1, activation="relu")
-    assert torch.equal(got[0], forward(x, 6, w1, b1, activation="relu")[0][1])
+    # one worker without the axis (how an image is cut depends on how many there are: the last bits may differ)
+    y1, mean1, rstd1 = forward(x[1], 6, w1, b1, activation="relu")
+    assert y1.shape == x[1].shape and mean1.shape == (2, 6)
+    check_group_norm_forward(x[1:2], w1[None], b1[None], 6, 1e-5, "relu", dtype, y1[None], mean1[None], rstd1[None])
     dx1, dw1, db1 = backward(dy[1], x[1], mean[1].contiguous(), rstd[1].contiguous(), w1, b1, activation="relu")
-    assert torch.equal(dx1, dx[1]) and dw1.shape == (48,)
+    assert dx1.shape == x[1].shape and dw1.shape == (48,)
+    check_group_norm_backward(dy[1:2], x[1:2], mean[1:2], rstd[1:2], w1[None], b1[None], "relu", dtype, "f32", dx1[None], dw1[None], db1[None])
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
