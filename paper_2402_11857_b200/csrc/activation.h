@@ -43,7 +43,7 @@ struct GnArgs {   // an image is a worker's sample; strides in elements
     float eps;
     int32_t parts, tiles, tile_chunks;   // of an image's pixels; of its channels, each of tile_chunks 16-byte chunks
     int64_t part_pixels;
-    int32_t whole;                // rows of x, y, dy and dx start on 16 bytes
+    int32_t whole, whole_out;     // rows that are read, rows that are written, start on 16 bytes
     int32_t turns;                // resident images: chunks of a thread
 };
 cudaError_t launch_group_norm_forward(GnArgs a, int dtype, cudaStream_t st);

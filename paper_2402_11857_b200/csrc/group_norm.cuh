@@ -10,18 +10,6 @@ namespace liec {
 
 constexpr int GN_THREADS = 256;
 
-// A chunk of a row on its way to this thread's place in shared memory: asynchronously where rows start on 16 bytes.
-template <typename T>
-__device__ __forceinline__ void gn_fetch(const GnArgs &a, uint32_t to, const T *row, int c) {
-    if (a.whole) {
-        const int bytes = min(16, max(0, (a.channels - c) * (int)sizeof(T)));
-        copy_async(to, bytes > 0 ? row + c : row, bytes);
-    } else {
-        const uint4 v = c < a.channels ? load_chunk(row, c, a.channels) : make_uint4(0u, 0u, 0u, 0u);
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-    }
-}
-
 // Where a chunk of x comes from: the activations themselves, or their checkpoint.
 template <typename T>
 struct GnFromX {
@@ -32,8 +20,7 @@ struct GnFromX {
     __device__ __forceinline__ GnFromX(const GnArgs &a, int worker, int sample, int64_t p)
         : row(static_cast<const T *>(a.x) + worker * a.x_worker + sample * a.x_sample + p * a.x_pixel), pixel(a.x_pixel) {}
     __device__ __forceinline__ Raw load(int64_t p, int c, int cols) const { return load_chunk(row + p * pixel, c, cols); }
-    // the same by way of shared memory
-    __device__ __forceinline__ void fetch(const GnArgs &a, uint32_t to, uint8_t *, int64_t p, int c) const { gn_fetch(a, to, row + p * pixel, c); }
+    // the same from this thread's place in shared memory
     static __device__ __forceinline__ Raw kept(const char *place, const uint8_t *) { return *reinterpret_cast<const uint4 *>(place); }
     template <int P>
     static __device__ __forceinline__ void centred(const Raw &raw, const F2 (&minus)[P], F2 (&d)[P]) {
@@ -69,10 +56,6 @@ struct GnFromCheckpoint {
         r.byte = __ldg(scales + p * (cols / CK_BLOCK) + c / CK_BLOCK);
         return r;
     }
-    __device__ __forceinline__ void fetch(const GnArgs &, uint32_t to, uint8_t *power, int64_t p, int c) const {
-        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(q + p * cols + c), "n"(Bits<T>::VEC) : "memory");
-        *power = __ldg(scales + p * (cols / CK_BLOCK) + c / CK_BLOCK);
-    }
     static __device__ __forceinline__ Raw kept(const char *place, const uint8_t *power) {
         Raw r;
         if constexpr (Bits<T>::VEC == 8) {
@@ -95,24 +78,37 @@ struct GnFromCheckpoint {
     }
 };
 
-// The gate s = 1 / (1 + exp(-z)) of SiLU.  Results in bfloat16 take the short exponential: its relative error, |z| 2^-23,
-// is far below a bfloat16 step wherever the gate is not zero.
+// SiLU of a pair.  Results in bfloat16 take the hardware's exponential and reciprocal as they are (relative errors of
+// (|z| + 2) 2^-23, far below a bfloat16 step wherever the gate is not zero; an infinite exponential gives a gate of zero).
+__device__ __forceinline__ float gn_exp2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float gn_reciprocal(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 template <typename T>
-__device__ __forceinline__ float gn_exp(float z) { return sizeof(T) == 4 ? fminf(expf(-z), 1e30f) : __expf(-z); }
+__device__ __forceinline__ F2 gn_exp(F2 z) {   // exp(-z)
+    if constexpr (sizeof(T) == 4) return f2(fminf(expf(-lo(z)), 1e30f), fminf(expf(-hi(z)), 1e30f));
+    const F2 t = mul(z, f2(-1.44269504f));
+    return f2(gn_exp2(lo(t)), gn_exp2(hi(t)));
+}
+template <typename T>
+__device__ __forceinline__ F2 gn_gate(F2 e) {   // 1 / (1 + e)
+    const F2 u = add(e, f2(1.0f));
+    if constexpr (sizeof(T) == 4) return f2(__fdividef(1.0f, lo(u)), __fdividef(1.0f, hi(u)));
+    return f2(gn_reciprocal(lo(u)), gn_reciprocal(hi(u)));
+}
 
 template <typename T, int ACT>
-__device__ __forceinline__ float gn_act(float z) {
-    if constexpr (ACT == LIEC_ACT_RELU) return z < 0.0f ? 0.0f : z;   // (NaN stays)
-    if constexpr (ACT == LIEC_ACT_SILU) return __fdividef(z, 1.0f + gn_exp<T>(z));
+__device__ __forceinline__ F2 gn_act(F2 z) {
+    if constexpr (ACT == LIEC_ACT_RELU) return f2(lo(z) < 0.0f ? 0.0f : lo(z), hi(z) < 0.0f ? 0.0f : hi(z));   // (NaN stays)
+    if constexpr (ACT == LIEC_ACT_SILU) return mul(z, gn_gate<T>(gn_exp<T>(z)));
     return z;
 }
 
-// dy silu'(z), silu' = s (1 + z (1 - s)).  1 - s = exp(-z) s keeps its digits where s is near one; in bfloat16 the
-// difference has enough of them.
+// silu'(z) = s (1 + z (1 - s)).  1 - s = exp(-z) s keeps its digits where s is near one; in bfloat16 the difference has
+// enough of them.
 template <typename T>
-__device__ __forceinline__ float gn_silu_slope(float z, float dy) {
-    const float e = gn_exp<T>(z), s = __fdividef(1.0f, 1.0f + e);
-    return dy * (s * __fmaf_rn(z, sizeof(T) == 4 ? e * s : 1.0f - s, 1.0f));
+__device__ __forceinline__ F2 gn_silu_slope(F2 z) {
+    const F2 e = gn_exp<T>(z), s = gn_gate<T>(e);
+    const F2 rest = sizeof(T) == 4 ? mul(e, s) : fma(s, f2(-1.0f), f2(1.0f));
+    return mul(s, fma(z, rest, f2(1.0f)));
 }
 
 // z from its definition in binary64.
@@ -122,18 +118,32 @@ static __device__ __noinline__ bool gn_positive(const GnArgs &a, int worker, int
     return ((double)x - (double)a.mean[g]) * (double)a.rstd[g] * w + b > 0.0;
 }
 
+// The group of a channel, channel after channel.
+struct GnGroup {
+    uint32_t group, rest;
+    __device__ __forceinline__ GnGroup(uint32_t c, uint32_t width) : group(c / width), rest(c - c / width * width) {}
+    __device__ __forceinline__ void next(uint32_t width) {
+        if (++rest == width) {
+            rest = 0;
+            ++group;
+        }
+    }
+};
+
 // What belongs to a thread's channels: -m, A = r w, b; zeros beyond the last channel.
 template <int P>
 struct GnChannels {
     F2 minus[P], scale[P], bias[P];
-    // statistics(channel, m, r)
+    // statistics(group, m, r)
     template <typename F>
     __device__ __forceinline__ void read(const GnArgs &a, int worker, int c, F &&statistics) {
+        const uint32_t width = (uint32_t)a.channels / (uint32_t)a.groups;
+        GnGroup g(c, width);
 #pragma unroll
-        for (int k = 0; k < 2 * P; ++k) {
+        for (int k = 0; k < 2 * P; ++k, g.next(width)) {
             float m = 0.0f, s = 0.0f, b = 0.0f;
             if (c + k < a.channels) {
-                statistics(c + k, m, s);
+                statistics(g.group, m, s);
                 s *= a.weight ? __ldg(a.weight + worker * a.weight_stride + c + k) : 1.0f;
                 b = a.bias ? __ldg(a.bias + worker * a.bias_stride + c + k) : 0.0f;
             }
@@ -143,11 +153,10 @@ struct GnChannels {
         }
     }
     __device__ __forceinline__ void read(const GnArgs &a, int worker, int64_t image, int c) {
-        const int width = a.channels / a.groups;
-        read(a, worker, c, [&](int channel, float &m, float &r) {
-            const int64_t g = image * a.groups + channel / width;
-            m = a.mean[g];
-            r = a.rstd[g];
+        const float *mean = a.mean + image * a.groups, *rstd = a.rstd + image * a.groups;
+        read(a, worker, c, [&](uint32_t g, float &m, float &r) {
+            m = __ldg(mean + g);
+            r = __ldg(rstd + g);
         });
     }
     static __device__ __forceinline__ void set(F2 &p, int odd, float v) { p = odd ? f2(lo(p), v) : f2(v, 0.0f); }
@@ -168,7 +177,7 @@ __device__ __forceinline__ void gn_slope(const GnArgs &a, int worker, int64_t im
     for (int k = 0; k < P; ++k) z[k] = fma(d[k], ch.scale[k], ch.bias[k]);
     if constexpr (ACT == LIEC_ACT_SILU) {
 #pragma unroll
-        for (int k = 0; k < P; ++k) dz[k] = f2(gn_silu_slope<T>(lo(z[k]), lo(dy[k])), gn_silu_slope<T>(hi(z[k]), hi(dy[k])));
+        for (int k = 0; k < P; ++k) dz[k] = mul(gn_silu_slope<T>(z[k]), dy[k]);
     }
     if constexpr (ACT == LIEC_ACT_RELU) {
         uint32_t on = 0u, near = 0u;

@@ -130,8 +130,7 @@ __global__ void __launch_bounds__(GN_THREADS) gn_apply_kernel(const __grid_const
         GnFromX<T>::centred(raw, ch.minus, d);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-            const F2 z = fma(d[k], ch.scale[k], ch.bias[k]);
-            d[k] = f2(gn_act<T, ACT>(lo(z)), gn_act<T, ACT>(hi(z)));
+            d[k] = gn_act<T, ACT>(fma(d[k], ch.scale[k], ch.bias[k]));
         }
         store_chunk(y + p * a.y_pixel, at.c, a.channels, d);
     }
@@ -312,6 +311,7 @@ cudaError_t launch_group_norm_forward(GnArgs a, int dtype, cudaStream_t st) {
     int smem;
     if (gn_resident_plan(a, dtype, false, false, smem)) {
         a.whole = gn_whole(a, dtype, a.x, a.x_pixel, a.x_sample, a.x_worker);
+        a.whole_out = a.channels % (dtype == 0 ? 4 : 8) == 0 && gn_whole(a, dtype, a.y, a.y_pixel, a.y_sample, a.y_worker);
         return gn_resident_forward(a, dtype, smem, st);
     }
     gn_plan(a, dtype == 0 ? 4 : 8);
@@ -346,6 +346,7 @@ cudaError_t launch_group_norm_backward(GnArgs a, int dtype, cudaStream_t st) {
         a.parts = 1;
     } else if (gn_resident_plan(a, dtype, true, !a.x, smem)) {
         a.whole = gn_whole(a, dtype, a.dy, a.y_pixel, a.y_sample, a.y_worker) && (!a.x || gn_whole(a, dtype, a.x, a.x_pixel, a.x_sample, a.x_worker));
+        a.whole_out = a.channels % (dtype == 0 ? 4 : 8) == 0 && gn_whole(a, dtype, a.dx, a.dx_pixel, a.dx_sample, a.dx_worker);
         const cudaError_t e = gn_resident_backward(a, dtype, smem, st);
         if (e != cudaSuccess) return e;
         a.parts = 1;   // (the cluster's parts are one by now)

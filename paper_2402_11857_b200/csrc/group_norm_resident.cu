@@ -8,7 +8,8 @@
 
 namespace liec {
 
-// What lies in dynamic shared memory, in bytes: planes of chunks ([turn][thread]), then the exchange.
+// What lies in dynamic shared memory, in bytes: planes of chunks ([turn][thread]), the sums that meet ([rank][sum][channel]),
+// the CTA's own on their way there, and per channel and group what follows from them.
 template <typename T, bool CHECKPOINT, int DZ_PLANES>
 struct GnMemory {
     static constexpr int VEC = Bits<T>::VEC, X_BYTES = CHECKPOINT ? VEC : 16;
@@ -16,9 +17,8 @@ struct GnMemory {
     __host__ __device__ static int powers(int turns) { return CHECKPOINT ? turns * GN_THREADS : 0; }
     __host__ __device__ static int dz_plane(int turns) { return turns * GN_THREADS * 16; }
     __host__ __device__ static int planes(int turns) { return x_plane(turns) + DZ_PLANES * dz_plane(turns) + powers(turns); }
-    __host__ __device__ static int exchange(int ranks, int width) { return ranks * 2 * width * 4; }   // [rank][sum][channel]
     __host__ __device__ static int total(int turns, int ranks, int width) {
-        return planes(turns) + exchange(ranks, width) + GN_THREADS * VEC * 4 + 2 * width * 4;          // box; two values per group
+        return planes(turns) + ranks * 2 * width * 4 + GN_THREADS * VEC * 4 + 3 * width * 4;
     }
 };
 
@@ -28,33 +28,32 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 // Where this CTA and thread are.
 template <int VEC>
 struct GnSpot {
-    int64_t image, p0;
-    int worker, sample, tile, rank, ranks, chunk, lane, lanes, c, c0, width, n;   // n: pixels of this CTA
-    bool live;
+    int64_t image, p0;   // p0: the thread's first pixel
+    int worker, sample, rank, ranks, chunk, lane, lanes, c, c0, width, turns;   // turns: the thread's chunks
     __device__ __forceinline__ GnSpot(const GnArgs &a) {
         ranks = a.parts;
-        rank = (int)(blockIdx.x % ranks);
-        const int64_t unit = blockIdx.x / ranks;
-        tile = (int)(unit % a.tiles);
-        image = unit / a.tiles;
-        worker = (int)(image / a.samples);
-        sample = (int)(image - (int64_t)worker * a.samples);
-        p0 = rank * a.part_pixels;
-        n = (int)max((int64_t)0, min(a.part_pixels, a.pixels - p0));
-        chunk = threadIdx.x % a.tile_chunks;
-        lane = threadIdx.x / a.tile_chunks;
-        lanes = GN_THREADS / a.tile_chunks;
+        const uint32_t unit = blockIdx.x / (uint32_t)ranks, picture = unit / (uint32_t)a.tiles;
+        rank = (int)(blockIdx.x - unit * ranks);
+        image = picture;
+        worker = (int)(picture / (uint32_t)a.samples);
+        sample = (int)(picture - (uint32_t)worker * a.samples);
+        lane = (int)(threadIdx.x / (uint32_t)a.tile_chunks);
+        chunk = (int)threadIdx.x - lane * a.tile_chunks;
+        lanes = (int)(GN_THREADS / (uint32_t)a.tile_chunks);
         width = a.tile_chunks * VEC;
-        c0 = tile * width;
+        c0 = (int)(unit - picture * a.tiles) * width;
         c = c0 + chunk * VEC;
-        live = lane < lanes && c < (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK;
+        p0 = rank * a.part_pixels + lane;
+        const int64_t end = min((int64_t)(rank + 1) * a.part_pixels, a.pixels);
+        const bool live = lane < lanes && c < (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK;
+        turns = live && p0 < end ? ((int)(end - p0) + lanes - 1) / lanes : 0;
     }
     __device__ __forceinline__ int channels(const GnArgs &a) const { return min(width, a.channels - c0); }   // of the tile
 };
 
-// The channels' sums over the CTA's pixel lanes, then over the cluster: every CTA ends up with sums[rank][which][channel].
+// The channels' sums over the CTA's pixel lanes, handed to every CTA of the cluster: sums[rank][which][channel].
 template <int VEC>
-__device__ __forceinline__ void gn_exchange(const GnSpot<VEC> &at, const F2 (&v)[VEC / 2], int which, float *box, float *sums, bool last) {
+__device__ __forceinline__ void gn_hand_over(const GnSpot<VEC> &at, const F2 (&v)[VEC / 2], int which, float *box, float *sums) {
     const int width = at.width;
     if (at.lane < at.lanes) {
 #pragma unroll
@@ -62,38 +61,101 @@ __device__ __forceinline__ void gn_exchange(const GnSpot<VEC> &at, const F2 (&v)
             *reinterpret_cast<float4 *>(box + at.lane * width + at.chunk * VEC + 2 * k) = make_float4(lo(v[k]), hi(v[k]), lo(v[k + 1]), hi(v[k + 1]));
     }
     __syncthreads();
-    // 256 / width threads share a channel, then one adds their sums
-    const int ways = max(1, GN_THREADS / width), way = threadIdx.x / width, column = threadIdx.x - way * width;
-    float s = 0.0f;
-    for (int q = threadIdx.x; q < width; q += GN_THREADS) {   // (tiles wider than the CTA: a thread takes several channels)
-        if (width <= GN_THREADS) break;
-        float t = 0.0f;
-        for (int l = 0; l < at.lanes; ++l) t += box[l * width + q];
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(sums + (at.rank * 2 + which) * width);
+    auto hand = [&](int column, float s) {
         for (int r = 0; r < at.ranks; ++r) {
-            uint32_t to;
-            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(sums + (at.rank * 2 + which) * width + q)), "r"(r));
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(t) : "memory");
+            uint32_t there;
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(to + column * 4), "r"(r));
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(s) : "memory");
         }
-    }
-    if (width <= GN_THREADS) {
+    };
+    if (2 * width > GN_THREADS) {   // a thread per channel, or several channels
+        for (int q = threadIdx.x; q < width; q += GN_THREADS) {
+            float s = 0.0f;
+            for (int l = 0; l < at.lanes; ++l) s += box[l * width + q];
+            hand(q, s);
+        }
+    } else {                        // several threads per channel, then one adds their sums
+        const uint32_t ways = GN_THREADS / (uint32_t)width, way = threadIdx.x / (uint32_t)width;
+        const int column = (int)(threadIdx.x - way * width);
+        float s = 0.0f;
         if (way < ways)
+#pragma unroll 4
             for (int l = way; l < at.lanes; l += ways) s += box[l * width + column];
         __syncthreads();
         if (way < ways && way > 0) box[way * width + column] = s;
         __syncthreads();
         if (way == 0) {
-            for (int w = 1; w < ways; ++w) s += box[w * width + column];
-            for (int r = 0; r < at.ranks; ++r) {
-                uint32_t to;
-                asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(sums + (at.rank * 2 + which) * width + column)), "r"(r));
-                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(s) : "memory");
-            }
+            for (uint32_t w = 1; w < ways; ++w) s += box[w * width + column];
+            hand(column, s);
         }
     }
-    if (!last) __syncthreads();   // the box is used again
+    __syncthreads();   // the box is used again
+}
+
+// f(group, its sum) for every group of the tile: a thread adds the channels of a narrow one, a warp those of a wide one.
+template <int N, typename V, typename F>
+__device__ __forceinline__ void gn_over_groups(int channels, int width, V &&values, F &&f) {
+    const int groups = (int)((uint32_t)channels / (uint32_t)width);
+    if (width <= 16) {
+        for (int g = threadIdx.x; g < groups; g += GN_THREADS) {
+            float s[N] = {};
+            for (int q = g * width; q < (g + 1) * width; ++q) values(g, q, s);
+            f(g, s);
+        }
+    } else {
+        const int lane = threadIdx.x & 31;
+        for (int g = threadIdx.x >> 5; g < groups; g += GN_THREADS / 32) {
+            float s[N] = {};
+            for (int q = g * width + lane; q < (g + 1) * width; q += 32) values(g, q, s);
+#pragma unroll
+            for (int m = 16; m >= 1; m >>= 1)
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], m);
+            f(g, s);   // (the same in every lane)
+        }
+    }
 }
 
 constexpr int GN_PHASES = 4;   // a thread's chunks are summed in four goes, each as its copies are in
+
+// One array's chunks of a thread on their way to its places, asynchronously where rows start on 16 bytes: turns from to to
+// end - 1.
+template <typename T>
+__device__ __forceinline__ void gn_fetch(const GnArgs &a, uint32_t place, const T *first, int64_t step, int c, int from, int end) {
+    if (a.whole) {
+        const int bytes = min(16, max(0, (a.channels - c) * (int)sizeof(T)));
+        const T *p = (bytes > 0 ? first + c : first) + from * step;
+        for (int k = from; k < end; ++k, p += step) copy_async(place + k * (GN_THREADS * 16), p, bytes);
+    } else {
+#pragma unroll 4
+        for (int k = from; k < end; ++k) {
+            const uint4 v = c < a.channels ? load_chunk(first + k * step, c, a.channels) : make_uint4(0u, 0u, 0u, 0u);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place + k * (GN_THREADS * 16)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+        }
+    }
+}
+
+// Results of a thread's chunks: results(k, d) for every turn, stored 16 bytes at a time where all rows start there.
+template <typename T, typename F>
+__device__ __forceinline__ void gn_store(const GnArgs &a, T *first, int64_t step, int c, int turns, F &&results) {
+    constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
+    T *p = first + c;
+    if (a.whole_out) {   // (the same way for all threads: those of a checkpoint's block find its maximum in results())
+#pragma unroll 2
+        for (int k = 0; k < turns; ++k, p += step) {
+            F2 d[P];
+            results(k, d);
+            if (c < a.channels) LnChunk<T>::write(p, d);
+        }
+    } else {
+        for (int k = 0; k < turns; ++k) {
+            F2 d[P];
+            results(k, d);
+            store_chunk(first + k * step, c, a.channels, d);
+        }
+    }
+}
 
 template <typename T, int ACT, bool COMPRESS>
 __global__ void __launch_bounds__(GN_THREADS, 3) gn_resident_forward_kernel(const __grid_constant__ GnArgs a) {
@@ -101,25 +163,31 @@ __global__ void __launch_bounds__(GN_THREADS, 3) gn_resident_forward_kernel(cons
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
     extern __shared__ __align__(16) char gn_memory[];
     const GnSpot<VEC> at(a);
-    float *sums = reinterpret_cast<float *>(gn_memory + M::planes(a.turns)), *box = sums + at.ranks * 2 * at.width, *value = box + GN_THREADS * VEC;
-    uint4 *place = reinterpret_cast<uint4 *>(gn_memory) + threadIdx.x;
+    float *sums = reinterpret_cast<float *>(gn_memory + M::planes(a.turns)), *box = sums + at.ranks * 2 * at.width;
+    float *origin = box + GN_THREADS * VEC, *value = origin + at.width;
+    const uint4 *place = reinterpret_cast<const uint4 *>(gn_memory) + threadIdx.x;
     const uint32_t place_u32 = (uint32_t)__cvta_generic_to_shared(place);
     cluster_arrive();
-    const T *image = static_cast<const T *>(a.x) + at.worker * a.x_worker + at.sample * a.x_sample, *x = image + (at.p0 + at.lane) * a.x_pixel;
-    const int per = (a.turns + GN_PHASES - 1) / GN_PHASES, turns = at.live ? (at.n - at.lane + at.lanes - 1) / at.lanes : 0;   // (at.n - at.lane <= 0: none)
-    const int64_t step = at.lanes * a.x_pixel;
+    const T *image = static_cast<const T *>(a.x) + at.worker * a.x_worker + at.sample * a.x_sample, *x = image + at.p0 * a.x_pixel;
+    const int per = (a.turns + GN_PHASES - 1) / GN_PHASES, turns = at.turns;
 #pragma unroll
     for (int q = 0; q < GN_PHASES; ++q) {
-        for (int k = q * per; k < min((q + 1) * per, turns); ++k) gn_fetch(a, place_u32 + k * GN_THREADS * 16, x + k * step, at.c);
+        gn_fetch(a, place_u32, x, at.lanes * a.x_pixel, at.c, q * per, min((q + 1) * per, turns));
         copy_commit();
     }
     // sums about the image's first pixel
     F2 s[P] = {}, t[P] = {}, minus[P] = {};
-    if (at.live && at.c < a.channels) {
+    if (at.lane < at.lanes && at.c < a.channels) {
         F2 v[P];
         LnChunk<T>::read(load_chunk(image, at.c, a.channels), v);
 #pragma unroll
-        for (int k = 0; k < P; ++k) minus[k] = f2(-lo(v[k]), -hi(v[k]));
+        for (int k = 0; k < P; ++k) {
+            minus[k] = f2(-lo(v[k]), -hi(v[k]));
+            if (at.lane == 0) {
+                origin[at.chunk * VEC + 2 * k] = lo(v[k]);
+                origin[at.chunk * VEC + 2 * k + 1] = hi(v[k]);
+            }
+        }
     }
     auto go = [&](int q) {
 #pragma unroll 2
@@ -139,68 +207,57 @@ __global__ void __launch_bounds__(GN_THREADS, 3) gn_resident_forward_kernel(cons
     copy_wait<1>(); go(2);
     copy_wait<0>(); go(3);
     cluster_wait();                                     // all CTAs of the cluster are there
-    gn_exchange<VEC>(at, s, 0, box, sums, false);
-    gn_exchange<VEC>(at, t, 1, box, sums, true);
+    gn_hand_over<VEC>(at, s, 0, box, sums);
+    gn_hand_over<VEC>(at, t, 1, box, sums);
     cluster_arrive();
     cluster_wait();
-    // every channel's mean and squares around it, then the groups'
-    const int channels = at.channels(a), width = a.channels / a.groups, groups = channels / width;
-    float *mean_c = sums, *square_c = sums + at.width;   // (rank 0's sums, read and written by the same thread)
+    // every channel's mean (about the first pixel) and squares around it, then the groups'
+    const int channels = at.channels(a), width = (int)((uint32_t)a.channels / (uint32_t)a.groups);
+    const float pixels = (float)a.pixels;
     for (int q = threadIdx.x; q < channels; q += GN_THREADS) {
         float v = 0.0f, w = 0.0f;
         for (int r = 0; r < at.ranks; ++r) {
             v += sums[r * 2 * at.width + q];
             w += sums[(r * 2 + 1) * at.width + q];
         }
-        const float m = v / (float)a.pixels;
-        box[q] = m;                                      // mean about the first pixel
-        mean_c[q] = (float)image[at.c0 + q];
-        square_c[q] = fmaxf(__fmaf_rn(-v, m, w), 0.0f);
+        const float m = v / pixels;
+        box[q] = m;
+        box[at.width + q] = fmaxf(__fmaf_rn(-v, m, w), 0.0f);
     }
     __syncthreads();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int g = warp; g < groups; g += GN_THREADS / 32) {
-        double v = 0.0, w = 0.0;
-        for (int q = lane; q < width; q += 32) v += (double)mean_c[g * width + q] + (double)box[g * width + q];
-        const double mean = warp_sum(v) / width;
-        for (int q = lane; q < width; q += 32) {
-            const double off = (double)mean_c[g * width + q] + (double)box[g * width + q] - mean;
-            w += (double)square_c[g * width + q] + (double)a.pixels * off * off;
-        }
-        const double var = warp_sum(w) / ((double)a.pixels * width);
-        if (lane == 0) {
-            const float m = (float)mean, r = (float)(1.0 / sqrt(var + (double)a.eps));
-            value[2 * g] = m;
-            value[2 * g + 1] = r;
-            if (at.rank == 0) {
-                const int64_t to = at.image * a.groups + at.c0 / width + g;
-                a.mean[to] = m;
-                a.rstd[to] = r;
-            }
-        }
-    }
+    // (about the mean of the group's first channel: a far mean costs no digits)
+    auto off = [&](int g, int q) { return (origin[q] - origin[g * width]) + box[q]; };
+    gn_over_groups<1>(channels, width, [&](int g, int q, float (&v)[1]) { v[0] += off(g, q); }, [&](int g, float (&v)[1]) { value[g] = v[0] / (float)width; });
+    if (width > 16) __syncwarp();
+    gn_over_groups<1>(channels, width, [&](int g, int q, float (&v)[1]) { const float o = off(g, q) - value[g]; v[0] += __fmaf_rn(pixels * o, o, box[at.width + q]); },
+                      [&](int g, float (&v)[1]) {
+                          const float m = origin[g * width] + value[g], r = 1.0f / sqrtf(v[0] / (pixels * (float)width) + a.eps);
+                          if (width <= 16 || (threadIdx.x & 31) == 0) {
+                              sums[2 * g] = m;
+                              sums[2 * g + 1] = r;
+                              if (at.rank == 0) {
+                                  const int64_t to = at.image * a.groups + (int)((uint32_t)at.c0 / (uint32_t)width) + g;
+                                  a.mean[to] = m;
+                                  a.rstd[to] = r;
+                              }
+                          }
+                      });
     __syncthreads();
-    if (!at.live) return;
+    if (turns == 0) return;
     GnChannels<P> ch;
-    ch.read(a, at.worker, at.c, [&](int c, float &m, float &r) {
-        const int g = (c - at.c0) / width;
-        m = value[2 * g];
-        r = value[2 * g + 1];
+    const uint32_t first_group = (uint32_t)at.c0 / (uint32_t)width;
+    ch.read(a, at.worker, at.c, [&](uint32_t g, float &m, float &r) {
+        m = sums[2 * (g - first_group)];
+        r = sums[2 * (g - first_group) + 1];
     });
-    T *y = static_cast<T *>(a.y) + at.worker * a.y_worker + at.sample * a.y_sample + (at.p0 + at.lane) * a.y_pixel;
-    const int64_t y_step = at.lanes * a.y_pixel, row0 = at.image * a.pixels + at.p0 + at.lane;
-#pragma unroll 2
-    for (int k = 0; k < turns; ++k) {
-        F2 d[P];
+    T *y = static_cast<T *>(a.y) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
+    int64_t row = at.image * a.pixels + at.p0;
+    gn_store<T>(a, y, at.lanes * a.y_pixel, at.c, turns, [&](int k, F2 (&d)[P]) {
         LnChunk<T>::read(place[k * GN_THREADS], d);
-        if constexpr (COMPRESS) gn_compress<T>(a, d, row0 + (int64_t)k * at.lanes, at.c);
+        if constexpr (COMPRESS) gn_compress<T>(a, d, row + (int64_t)k * at.lanes, at.c);
 #pragma unroll
-        for (int j = 0; j < P; ++j) {
-            const F2 z = fma(add(d[j], ch.minus[j]), ch.scale[j], ch.bias[j]);
-            d[j] = f2(gn_act<T, ACT>(lo(z)), gn_act<T, ACT>(hi(z)));
-        }
-        store_chunk(y + k * y_step, at.c, a.channels, d);
-    }
+        for (int j = 0; j < P; ++j) d[j] = gn_act<T, ACT>(fma(add(d[j], ch.minus[j]), ch.scale[j], ch.bias[j]));
+    });
 }
 
 // dz is kept for the second go: as dy's type where it is dy or zero, else in binary32.
@@ -217,21 +274,32 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_resident_backward_kernel(con
     uint8_t *power_place = reinterpret_cast<uint8_t *>(gn_memory) + M::dz_plane(a.turns) * (WIDE ? 2 : 1) + M::x_plane(a.turns) + threadIdx.x;
     float *sums = reinterpret_cast<float *>(gn_memory + M::planes(a.turns)), *box = sums + at.ranks * 2 * at.width, *value = box + GN_THREADS * VEC;
     cluster_arrive();
-    const T *dy = static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + (at.p0 + at.lane) * a.y_pixel;
-    const int per = (a.turns + GN_PHASES - 1) / GN_PHASES, turns = at.live ? (at.n - at.lane + at.lanes - 1) / at.lanes : 0;
-    const int64_t step = at.lanes * a.y_pixel;
-    const X x(a, at.worker, at.sample, at.p0 + at.lane);
+    const T *dy = static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
+    const int per = (a.turns + GN_PHASES - 1) / GN_PHASES, turns = at.turns;
+    const X x(a, at.worker, at.sample, at.p0);
     const uint32_t dz_u32 = (uint32_t)__cvta_generic_to_shared(dz_place), x_u32 = (uint32_t)__cvta_generic_to_shared(x_place);
 #pragma unroll
     for (int q = 0; q < GN_PHASES; ++q) {
-        for (int k = q * per; k < min((q + 1) * per, turns); ++k) {
-            gn_fetch(a, dz_u32 + k * GN_THREADS * 16, dy + k * step, at.c);
-            x.fetch(a, x_u32 + k * GN_THREADS * M::X_BYTES, power_place + k * GN_THREADS, (int64_t)k * at.lanes, at.c);
+        const int end = min((q + 1) * per, turns);
+        gn_fetch(a, dz_u32, dy, at.lanes * a.y_pixel, at.c, q * per, end);
+        if constexpr (CHECKPOINT) {
+            const int64_t step = at.lanes * x.cols, power_step = step / CK_BLOCK;
+            const int8_t *from = x.q + at.c + q * per * step;
+            for (int k = q * per; k < end; ++k, from += step)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(x_u32 + k * (GN_THREADS * M::X_BYTES)), "l"(from), "n"(M::X_BYTES) : "memory");
+            const uint8_t *power = x.scales + at.c / CK_BLOCK + q * per * power_step;
+#pragma unroll 4
+            for (int k = q * per; k < end; ++k) power_place[k * GN_THREADS] = __ldg(power + (k - q * per) * power_step);
+        } else {
+            gn_fetch(a, x_u32, x.row, at.lanes * x.pixel, at.c, q * per, end);
         }
         copy_commit();
     }
+    const int channels = at.channels(a), width = (int)((uint32_t)a.channels / (uint32_t)a.groups);
+    const float *rstd = a.rstd + at.image * a.groups, *weight = a.weight ? a.weight + at.worker * a.weight_stride : nullptr;
+    const uint32_t first_group = (uint32_t)at.c0 / (uint32_t)width;
     GnChannels<P> ch;
-    if (at.live) ch.read(a, at.worker, at.image, at.c);
+    if (turns > 0) ch.read(a, at.worker, at.image, at.c);
     F2 s[P] = {}, t[P] = {};
     auto go = [&](int q) {
 #pragma unroll 2
@@ -259,58 +327,53 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_resident_backward_kernel(con
     copy_wait<1>(); go(2);
     copy_wait<0>(); go(3);
     cluster_wait();
-    gn_exchange<VEC>(at, s, 0, box, sums, false);
-    gn_exchange<VEC>(at, t, 1, box, sums, true);
+    gn_hand_over<VEC>(at, s, 0, box, sums);
+    gn_hand_over<VEC>(at, t, 1, box, sums);
     cluster_arrive();
+    // (loaded while the sums cross)
+    const float my_rstd = (int)threadIdx.x < channels ? __ldg(rstd + (at.c0 + threadIdx.x) / (uint32_t)width) : 0.0f;
+    const float my_weight = (int)threadIdx.x < channels && weight ? __ldg(weight + at.c0 + threadIdx.x) : 1.0f;
     cluster_wait();
-    const int channels = at.channels(a), width = a.channels / a.groups, groups = channels / width;
     for (int q = threadIdx.x; q < channels; q += GN_THREADS) {
         float v = 0.0f, w = 0.0f;
         for (int r = 0; r < at.ranks; ++r) {
             v += sums[r * 2 * at.width + q];
             w += sums[(r * 2 + 1) * at.width + q];
         }
-        w *= a.rstd[at.image * a.groups + (at.c0 + q) / width];
-        if (at.rank == 0 && a.part) {   // the image's share of db and dw
+        const bool mine = q == (int)threadIdx.x;
+        w *= mine ? my_rstd : __ldg(rstd + (uint32_t)(at.c0 + q) / (uint32_t)width);
+        if (at.rank == 0) {   // the image's share of db and dw
             a.part[at.image * 2 * a.channels + at.c0 + q] = v;
             a.part[(at.image * 2 + 1) * a.channels + at.c0 + q] = w;
         }
-        const float weight = a.weight ? __ldg(a.weight + at.worker * a.weight_stride + at.c0 + q) : 1.0f;
-        sums[q] = v * weight;
-        sums[at.width + q] = w * weight;
+        const float by = mine || !weight ? my_weight : __ldg(weight + at.c0 + q);
+        box[q] = v * by;
+        box[at.width + q] = w * by;
     }
     if (!a.dx) return;
     __syncthreads();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int g = warp; g < groups; g += GN_THREADS / 32) {
-        double v = 0.0, w = 0.0;
-        for (int q = lane; q < width; q += 32) {
-            v += (double)sums[g * width + q];
-            w += (double)sums[at.width + g * width + q];
-        }
-        v = warp_sum(v);
-        w = warp_sum(w);
-        if (lane == 0) {
-            const double n = (double)a.pixels * width, r = (double)a.rstd[at.image * a.groups + at.c0 / width + g];
-            value[2 * g] = (float)(-r * v / n);
-            value[2 * g + 1] = (float)(-r * r * w / n);
-        }
-    }
+    gn_over_groups<2>(channels, width, [&](int, int q, float (&v)[2]) { v[0] += box[q]; v[1] += box[at.width + q]; },
+                      [&](int g, float (&v)[2]) {
+                          const float r = __ldg(rstd + first_group + g), by = r / ((float)a.pixels * (float)width);
+                          if (width <= 16 || (threadIdx.x & 31) == 0) {
+                              value[2 * g] = -by * v[0];
+                              value[2 * g + 1] = -by * r * v[1];
+                          }
+                      });
     __syncthreads();
-    if (!at.live || at.c >= a.channels) return;
+    if (turns == 0 || at.c >= a.channels) return;
     F2 level[P], along[P];
+    GnGroup group(at.c - at.c0, width);
 #pragma unroll
-    for (int k = 0; k < 2 * P; ++k) {
-        const int g = (min(at.c + k, a.channels - 1) - at.c0) / width;
-        GnChannels<P>::set(level[k / 2], k % 2, value[2 * g]);
-        GnChannels<P>::set(along[k / 2], k % 2, value[2 * g + 1]);
+    for (int k = 0; k < 2 * P; ++k, group.next(width)) {
+        const bool in = at.c + k < a.channels;
+        GnChannels<P>::set(level[k / 2], k % 2, in ? value[2 * group.group] : 0.0f);
+        GnChannels<P>::set(along[k / 2], k % 2, in ? value[2 * group.group + 1] : 0.0f);
     }
-    T *dx = static_cast<T *>(a.dx) + at.worker * a.dx_worker + at.sample * a.dx_sample + (at.p0 + at.lane) * a.dx_pixel;
-    const int64_t dx_step = at.lanes * a.dx_pixel;
-#pragma unroll 2
-    for (int k = 0; k < turns; ++k) {
+    T *dx = static_cast<T *>(a.dx) + at.worker * a.dx_worker + at.sample * a.dx_sample + at.p0 * a.dx_pixel;
+    gn_store<T>(a, dx, at.lanes * a.dx_pixel, at.c, turns, [&](int k, F2 (&d)[P]) {
         const typename X::Raw raw = X::kept(x_place + k * GN_THREADS * M::X_BYTES, power_place + k * GN_THREADS);
-        F2 d[P], g[P];
+        F2 g[P];
         X::centred(raw, ch.minus, d);
         if constexpr (WIDE) {
             F2 low[2], high[2];
@@ -322,8 +385,7 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_resident_backward_kernel(con
         }
 #pragma unroll
         for (int j = 0; j < P; ++j) d[j] = fma(g[j], ch.scale[j], fma(d[j], along[j], level[j]));
-        store_chunk(dx + k * dx_step, at.c, a.channels, d);
-    }
+    });
 }
 
 // ---- launches --------------------------------------------------------------------------------------------
@@ -375,54 +437,48 @@ static int gn_memory_bytes(bool backward, bool checkpoint, int act, int turns, i
     return wide ? GnMemory<T, false, 2>::total(turns, ranks, width) : GnMemory<T, false, 1>::total(turns, ranks, width);
 }
 
-// Channels per cluster: whole groups and whole blocks of a checkpoint, at least 128 bytes of a pixel (or all of it); more while an image
-// is small and there are CTAs enough.  CTAs per cluster: as few as leave room for three CTAs on an SM,
-// then two, then one, so that the copies of one hide behind the sums and stores of the others; more, down to two
-// turns per thread, while SMs are idle.
+// Channels per cluster: whole groups and whole blocks of a checkpoint, at least 128 bytes of a pixel (or all of it; 64
+// where more would not fit); more while an image is small and there are CTAs enough.  CTAs per cluster: as few as leave
+// room for three CTAs on an SM (forward; the backward pass has registers for two), then two, then one, so that the copies
+// of one hide behind the sums and stores of the others; more, down to two turns per thread, while SMs are idle.
 bool gn_resident_plan(GnArgs &a, int dtype, bool backward, bool checkpoint, int &smem) {
     const int vec = dtype == 0 ? 4 : 8, group = a.channels / a.groups;
     int unit = group;
     while (unit % CK_BLOCK != 0) unit += group;
     const int64_t images = (int64_t)a.workers * a.samples;
-    const int most = 8;
+    constexpr int MOST = 8;
     auto fits = [&](int channels, int ranks, int budget) {
         const int chunks = (int)(ck_cols(channels) / vec);
-        if (chunks > GN_THREADS) return false;
+        if (chunks > GN_THREADS / 2) return false;
         a.tile_chunks = chunks;
         a.tiles = (a.channels + channels - 1) / channels;
         a.part_pixels = (a.pixels + ranks - 1) / ranks;
         a.parts = ranks;
         const int lanes = GN_THREADS / chunks;
         const int64_t turns = (a.part_pixels + lanes - 1) / lanes;
-        if (turns > 1024) return false;
+        if (turns > 1024 || images * a.tiles * ranks >= (int64_t(1) << 31)) return false;
         a.turns = (int)turns;
         smem = dtype == 0 ? gn_memory_bytes<float>(backward, checkpoint, a.act, a.turns, ranks, chunks * vec)
                           : gn_memory_bytes<__nv_bfloat16>(backward, checkpoint, a.act, a.turns, ranks, chunks * vec);
         return smem <= budget;
     };
-    int channels = std::min(unit, a.channels);
-    auto wider = [&]() {
-        if (channels >= a.channels) return false;
-        channels = 2 * channels >= a.channels ? a.channels : 2 * channels;
-        return true;
+    auto at_least = [&](int bytes) {   // (a range that is doubled is still a multiple of the unit, or all channels)
+        int channels = std::min(unit, a.channels);
+        while (channels < a.channels && channels * (16 / vec) < bytes) channels = std::min(2 * channels, a.channels);
+        return channels;
     };
-    while (channels * (16 / vec) < 128 && wider()) {}
-    // (a range that is doubled is still a multiple of the unit, or all channels)
-    while (channels < a.channels && channels * 2 <= 32 * vec && a.pixels * channels <= 4 * GN_THREADS * vec && images * ((a.channels + channels - 1) / channels) > 4 * LN_SMS)
-        wider();
-    const int budgets[3] = {75 * 1024, 112 * 1024, GN_MAX_MEMORY};
+    int ranges[2] = {at_least(128), at_least(64)};
+    while (ranges[0] < a.channels && ranges[0] * 2 <= 32 * vec && a.pixels * ranges[0] <= 4 * GN_THREADS * vec &&
+           images * ((a.channels + ranges[0] - 1) / ranges[0]) > 4 * LN_SMS)
+        ranges[0] = std::min(2 * ranges[0], a.channels);
+    const int budgets[3] = {backward ? 0 : 75 * 1024, 112 * 1024, GN_MAX_MEMORY};
     for (int budget : budgets)
-        for (int ranks = 1; ranks <= most; ++ranks) {
-            if (ranks > 1 && ranks > a.pixels) break;
-            if (!fits(channels, ranks, budget)) continue;
-            int better = ranks;
-            while (better < most && images * a.tiles * better * 2 <= LN_SMS && a.turns > 2) {
-                better = std::min(2 * better, most);
-                if (better > a.pixels || !fits(channels, better, budget)) break;
-                ranks = better;
+        for (int channels : ranges)
+            for (int ranks = 1; ranks <= MOST && ranks <= a.pixels; ++ranks) {
+                if (!fits(channels, ranks, budget)) continue;
+                while (2 * ranks <= MOST && 2 * ranks <= a.pixels && images * a.tiles * ranks * 2 <= LN_SMS && a.turns > 2 && fits(channels, 2 * ranks, budget)) ranks *= 2;
+                return fits(channels, ranks, budget);
             }
-            return fits(channels, ranks, budget) && images * a.tiles * a.parts < (int64_t(1) << 31);
-        }
     return false;
 }
 
