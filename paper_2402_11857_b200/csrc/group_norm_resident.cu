@@ -8,17 +8,19 @@
 
 namespace liec {
 
+constexpr int GR_THREADS = 128;   // few threads with many chunks each: what is done once per thread is as much as a dozen chunks cost
+
 // What lies in dynamic shared memory, in bytes: planes of chunks ([turn][thread]), the sums that meet ([rank][sum][channel]),
 // the CTA's own on their way there, and per channel and group what follows from them.
 template <typename T, bool CHECKPOINT, int DZ_PLANES>
 struct GnMemory {
     static constexpr int VEC = Bits<T>::VEC, X_BYTES = CHECKPOINT ? VEC : 16;
-    __host__ __device__ static int x_plane(int turns) { return turns * GN_THREADS * X_BYTES; }
-    __host__ __device__ static int powers(int turns) { return CHECKPOINT ? turns * GN_THREADS : 0; }
-    __host__ __device__ static int dz_plane(int turns) { return turns * GN_THREADS * 16; }
+    __host__ __device__ static int x_plane(int turns) { return turns * GR_THREADS * X_BYTES; }
+    __host__ __device__ static int powers(int turns) { return CHECKPOINT ? turns * GR_THREADS : 0; }
+    __host__ __device__ static int dz_plane(int turns) { return turns * GR_THREADS * 16; }
     __host__ __device__ static int planes(int turns) { return x_plane(turns) + DZ_PLANES * dz_plane(turns) + powers(turns); }
     __host__ __device__ static int total(int turns, int ranks, int width) {
-        return planes(turns) + ranks * 2 * width * 4 + GN_THREADS * VEC * 4 + 3 * width * 4;
+        return planes(turns) + ranks * 2 * width * 4 + GR_THREADS * VEC * 4 + 3 * width * 4;
     }
 };
 
@@ -39,7 +41,7 @@ struct GnSpot {
         sample = (int)(picture - (uint32_t)worker * a.samples);
         lane = (int)(threadIdx.x / (uint32_t)a.tile_chunks);
         chunk = (int)threadIdx.x - lane * a.tile_chunks;
-        lanes = (int)(GN_THREADS / (uint32_t)a.tile_chunks);
+        lanes = (int)(GR_THREADS / (uint32_t)a.tile_chunks);
         width = a.tile_chunks * VEC;
         c0 = (int)(unit - picture * a.tiles) * width;
         c = c0 + chunk * VEC;
@@ -53,12 +55,16 @@ struct GnSpot {
 
 // The channels' sums over the CTA's pixel lanes, handed to every CTA of the cluster: sums[rank][which][channel].
 template <int VEC>
-__device__ __forceinline__ void gn_hand_over(const GnSpot<VEC> &at, const F2 (&v)[VEC / 2], int which, float *box, float *sums) {
+__device__ __forceinline__ void gn_hand_over(const GnSpot<VEC> &at, const F2 (&a)[VEC / 2], const F2 (&b)[VEC / 2], float *box, float *sums) {
     const int width = at.width;
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
     if (at.lane < at.lanes) {
 #pragma unroll
-        for (int k = 0; k < VEC / 2; k += 2)
-            *reinterpret_cast<float4 *>(box + at.lane * width + at.chunk * VEC + 2 * k) = make_float4(lo(v[k]), hi(v[k]), lo(v[k + 1]), hi(v[k + 1]));
+        for (int k = 0; k < VEC / 2; k += 2) {
+            const F2 v = which ? b[k] : a[k], w = which ? b[k + 1] : a[k + 1];
+            *reinterpret_cast<float4 *>(box + at.lane * width + at.chunk * VEC + 2 * k) = make_float4(lo(v), hi(v), lo(w), hi(w));
+        }
     }
     __syncthreads();
     const uint32_t to = (uint32_t)__cvta_generic_to_shared(sums + (at.rank * 2 + which) * width);
@@ -69,14 +75,14 @@ __device__ __forceinline__ void gn_hand_over(const GnSpot<VEC> &at, const F2 (&v
             asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(s) : "memory");
         }
     };
-    if (2 * width > GN_THREADS) {   // a thread per channel, or several channels
-        for (int q = threadIdx.x; q < width; q += GN_THREADS) {
+    if (2 * width > GR_THREADS) {   // a thread per channel, or several channels
+        for (int q = threadIdx.x; q < width; q += GR_THREADS) {
             float s = 0.0f;
             for (int l = 0; l < at.lanes; ++l) s += box[l * width + q];
             hand(q, s);
         }
     } else {                        // several threads per channel, then one adds their sums
-        const uint32_t ways = GN_THREADS / (uint32_t)width, way = threadIdx.x / (uint32_t)width;
+        const uint32_t ways = GR_THREADS / (uint32_t)width, way = threadIdx.x / (uint32_t)width;
         const int column = (int)(threadIdx.x - way * width);
         float s = 0.0f;
         if (way < ways)
@@ -91,6 +97,7 @@ __device__ __forceinline__ void gn_hand_over(const GnSpot<VEC> &at, const F2 (&v
         }
     }
     __syncthreads();   // the box is used again
+    }
 }
 
 // f(group, its sum) for every group of the tile: a thread adds the channels of a narrow one, a warp those of a wide one.
@@ -98,14 +105,14 @@ template <int N, typename V, typename F>
 __device__ __forceinline__ void gn_over_groups(int channels, int width, V &&values, F &&f) {
     const int groups = (int)((uint32_t)channels / (uint32_t)width);
     if (width <= 16) {
-        for (int g = threadIdx.x; g < groups; g += GN_THREADS) {
+        for (int g = threadIdx.x; g < groups; g += GR_THREADS) {
             float s[N] = {};
             for (int q = g * width; q < (g + 1) * width; ++q) values(g, q, s);
             f(g, s);
         }
     } else {
         const int lane = threadIdx.x & 31;
-        for (int g = threadIdx.x >> 5; g < groups; g += GN_THREADS / 32) {
+        for (int g = threadIdx.x >> 5; g < groups; g += GR_THREADS / 32) {
             float s[N] = {};
             for (int q = g * width + lane; q < (g + 1) * width; q += 32) values(g, q, s);
 #pragma unroll
@@ -119,6 +126,13 @@ __device__ __forceinline__ void gn_over_groups(int channels, int width, V &&valu
 
 constexpr int GN_PHASES = 4;   // a thread's chunks are summed in four goes, each as its copies are in
 
+__device__ __forceinline__ void gn_wait_phase(int q) {
+    if (q == 0) copy_wait<3>();
+    else if (q == 1) copy_wait<2>();
+    else if (q == 2) copy_wait<1>();
+    else copy_wait<0>();
+}
+
 // One array's chunks of a thread on their way to its places, asynchronously where rows start on 16 bytes: turns from to to
 // end - 1.
 template <typename T>
@@ -126,12 +140,12 @@ __device__ __forceinline__ void gn_fetch(const GnArgs &a, uint32_t place, const 
     if (a.whole) {
         const int bytes = min(16, max(0, (a.channels - c) * (int)sizeof(T)));
         const T *p = (bytes > 0 ? first + c : first) + from * step;
-        for (int k = from; k < end; ++k, p += step) copy_async(place + k * (GN_THREADS * 16), p, bytes);
+        for (int k = from; k < end; ++k, p += step) copy_async(place + k * (GR_THREADS * 16), p, bytes);
     } else {
 #pragma unroll 4
         for (int k = from; k < end; ++k) {
             const uint4 v = c < a.channels ? load_chunk(first + k * step, c, a.channels) : make_uint4(0u, 0u, 0u, 0u);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place + k * (GN_THREADS * 16)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place + k * (GR_THREADS * 16)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
         }
     }
 }
@@ -158,19 +172,19 @@ __device__ __forceinline__ void gn_store(const GnArgs &a, T *first, int64_t step
 }
 
 template <typename T, int ACT, bool COMPRESS>
-__global__ void __launch_bounds__(GN_THREADS, 3) gn_resident_forward_kernel(const __grid_constant__ GnArgs a) {
+__global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_forward_kernel(const __grid_constant__ GnArgs a) {
     using M = GnMemory<T, false, 0>;
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
     extern __shared__ __align__(16) char gn_memory[];
     const GnSpot<VEC> at(a);
     float *sums = reinterpret_cast<float *>(gn_memory + M::planes(a.turns)), *box = sums + at.ranks * 2 * at.width;
-    float *origin = box + GN_THREADS * VEC, *value = origin + at.width;
+    float *origin = box + GR_THREADS * VEC, *value = origin + at.width;
     const uint4 *place = reinterpret_cast<const uint4 *>(gn_memory) + threadIdx.x;
     const uint32_t place_u32 = (uint32_t)__cvta_generic_to_shared(place);
     cluster_arrive();
     const T *image = static_cast<const T *>(a.x) + at.worker * a.x_worker + at.sample * a.x_sample, *x = image + at.p0 * a.x_pixel;
     const int per = (a.turns + GN_PHASES - 1) / GN_PHASES, turns = at.turns;
-#pragma unroll
+#pragma unroll 1
     for (int q = 0; q < GN_PHASES; ++q) {
         gn_fetch(a, place_u32, x, at.lanes * a.x_pixel, at.c, q * per, min((q + 1) * per, turns));
         copy_commit();
@@ -189,11 +203,13 @@ __global__ void __launch_bounds__(GN_THREADS, 3) gn_resident_forward_kernel(cons
             }
         }
     }
-    auto go = [&](int q) {
+#pragma unroll 1
+    for (int q = 0; q < GN_PHASES; ++q) {
+        gn_wait_phase(q);
 #pragma unroll 2
         for (int k = q * per; k < min((q + 1) * per, turns); ++k) {
             F2 d[P];
-            LnChunk<T>::read(place[k * GN_THREADS], d);
+            LnChunk<T>::read(place[k * GR_THREADS], d);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
                 d[j] = add(d[j], minus[j]);
@@ -201,20 +217,15 @@ __global__ void __launch_bounds__(GN_THREADS, 3) gn_resident_forward_kernel(cons
                 t[j] = fma(d[j], d[j], t[j]);
             }
         }
-    };
-    copy_wait<3>(); go(0);
-    copy_wait<2>(); go(1);
-    copy_wait<1>(); go(2);
-    copy_wait<0>(); go(3);
+    }
     cluster_wait();                                     // all CTAs of the cluster are there
-    gn_hand_over<VEC>(at, s, 0, box, sums);
-    gn_hand_over<VEC>(at, t, 1, box, sums);
+    gn_hand_over<VEC>(at, s, t, box, sums);
     cluster_arrive();
     cluster_wait();
     // every channel's mean (about the first pixel) and squares around it, then the groups'
     const int channels = at.channels(a), width = (int)((uint32_t)a.channels / (uint32_t)a.groups);
     const float pixels = (float)a.pixels;
-    for (int q = threadIdx.x; q < channels; q += GN_THREADS) {
+    for (int q = threadIdx.x; q < channels; q += GR_THREADS) {
         float v = 0.0f, w = 0.0f;
         for (int r = 0; r < at.ranks; ++r) {
             v += sums[r * 2 * at.width + q];
@@ -253,7 +264,7 @@ __global__ void __launch_bounds__(GN_THREADS, 3) gn_resident_forward_kernel(cons
     T *y = static_cast<T *>(a.y) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
     int64_t row = at.image * a.pixels + at.p0;
     gn_store<T>(a, y, at.lanes * a.y_pixel, at.c, turns, [&](int k, F2 (&d)[P]) {
-        LnChunk<T>::read(place[k * GN_THREADS], d);
+        LnChunk<T>::read(place[k * GR_THREADS], d);
         if constexpr (COMPRESS) gn_compress<T>(a, d, row + (int64_t)k * at.lanes, at.c);
 #pragma unroll
         for (int j = 0; j < P; ++j) d[j] = gn_act<T, ACT>(fma(add(d[j], ch.minus[j]), ch.scale[j], ch.bias[j]));
@@ -262,23 +273,23 @@ __global__ void __launch_bounds__(GN_THREADS, 3) gn_resident_forward_kernel(cons
 
 // dz is kept for the second go: as dy's type where it is dy or zero, else in binary32.
 template <typename T, typename X, int ACT>
-__global__ void __launch_bounds__(GN_THREADS, 2) gn_resident_backward_kernel(const __grid_constant__ GnArgs a) {
+__global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_backward_kernel(const __grid_constant__ GnArgs a) {
     constexpr bool CHECKPOINT = X::CHECKPOINT, WIDE = ACT == LIEC_ACT_SILU && sizeof(T) == 2;
     using M = GnMemory<T, CHECKPOINT, WIDE ? 2 : 1>;
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
     extern __shared__ __align__(16) char gn_memory[];
     const GnSpot<VEC> at(a);
     uint4 *dz_place = reinterpret_cast<uint4 *>(gn_memory) + threadIdx.x;
-    const int plane = a.turns * GN_THREADS;   // chunks of a plane
+    const int plane = a.turns * GR_THREADS;   // chunks of a plane
     char *x_place = gn_memory + M::dz_plane(a.turns) * (WIDE ? 2 : 1) + threadIdx.x * M::X_BYTES;
     uint8_t *power_place = reinterpret_cast<uint8_t *>(gn_memory) + M::dz_plane(a.turns) * (WIDE ? 2 : 1) + M::x_plane(a.turns) + threadIdx.x;
-    float *sums = reinterpret_cast<float *>(gn_memory + M::planes(a.turns)), *box = sums + at.ranks * 2 * at.width, *value = box + GN_THREADS * VEC;
+    float *sums = reinterpret_cast<float *>(gn_memory + M::planes(a.turns)), *box = sums + at.ranks * 2 * at.width, *value = box + GR_THREADS * VEC;
     cluster_arrive();
     const T *dy = static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
     const int per = (a.turns + GN_PHASES - 1) / GN_PHASES, turns = at.turns;
     const X x(a, at.worker, at.sample, at.p0);
     const uint32_t dz_u32 = (uint32_t)__cvta_generic_to_shared(dz_place), x_u32 = (uint32_t)__cvta_generic_to_shared(x_place);
-#pragma unroll
+#pragma unroll 1
     for (int q = 0; q < GN_PHASES; ++q) {
         const int end = min((q + 1) * per, turns);
         gn_fetch(a, dz_u32, dy, at.lanes * a.y_pixel, at.c, q * per, end);
@@ -286,10 +297,10 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_resident_backward_kernel(con
             const int64_t step = at.lanes * x.cols, power_step = step / CK_BLOCK;
             const int8_t *from = x.q + at.c + q * per * step;
             for (int k = q * per; k < end; ++k, from += step)
-                asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(x_u32 + k * (GN_THREADS * M::X_BYTES)), "l"(from), "n"(M::X_BYTES) : "memory");
+                asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(x_u32 + k * (GR_THREADS * M::X_BYTES)), "l"(from), "n"(M::X_BYTES) : "memory");
             const uint8_t *power = x.scales + at.c / CK_BLOCK + q * per * power_step;
 #pragma unroll 4
-            for (int k = q * per; k < end; ++k) power_place[k * GN_THREADS] = __ldg(power + (k - q * per) * power_step);
+            for (int k = q * per; k < end; ++k) power_place[k * GR_THREADS] = __ldg(power + (k - q * per) * power_step);
         } else {
             gn_fetch(a, x_u32, x.row, at.lanes * x.pixel, at.c, q * per, end);
         }
@@ -301,19 +312,21 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_resident_backward_kernel(con
     GnChannels<P> ch;
     if (turns > 0) ch.read(a, at.worker, at.image, at.c);
     F2 s[P] = {}, t[P] = {};
-    auto go = [&](int q) {
+#pragma unroll 1
+    for (int q = 0; q < GN_PHASES; ++q) {
+        gn_wait_phase(q);
 #pragma unroll 2
         for (int k = q * per; k < min((q + 1) * per, turns); ++k) {
-            const typename X::Raw raw = X::kept(x_place + k * GN_THREADS * M::X_BYTES, power_place + k * GN_THREADS);
+            const typename X::Raw raw = X::kept(x_place + k * GR_THREADS * M::X_BYTES, power_place + k * GR_THREADS);
             F2 d[P], g[P];
             X::centred(raw, ch.minus, d);
-            LnChunk<T>::read(dz_place[k * GN_THREADS], g);
+            LnChunk<T>::read(dz_place[k * GR_THREADS], g);
             gn_slope<T, ACT, X>(a, at.worker, at.image, at.c, ch, raw, d, g, g);
             if constexpr (WIDE) {
-                LnChunk<float>::write(dz_place + k * GN_THREADS, {g[0], g[1]});
-                LnChunk<float>::write(dz_place + plane + k * GN_THREADS, {g[2], g[3]});
+                LnChunk<float>::write(dz_place + k * GR_THREADS, {g[0], g[1]});
+                LnChunk<float>::write(dz_place + plane + k * GR_THREADS, {g[2], g[3]});
             } else if constexpr (ACT != LIEC_ACT_NONE) {
-                LnChunk<T>::write(dz_place + k * GN_THREADS, g);
+                LnChunk<T>::write(dz_place + k * GR_THREADS, g);
             }
 #pragma unroll
             for (int j = 0; j < P; ++j) {
@@ -321,20 +334,15 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_resident_backward_kernel(con
                 t[j] = fma(g[j], d[j], t[j]);
             }
         }
-    };
-    copy_wait<3>(); go(0);
-    copy_wait<2>(); go(1);
-    copy_wait<1>(); go(2);
-    copy_wait<0>(); go(3);
+    }
     cluster_wait();
-    gn_hand_over<VEC>(at, s, 0, box, sums);
-    gn_hand_over<VEC>(at, t, 1, box, sums);
+    gn_hand_over<VEC>(at, s, t, box, sums);
     cluster_arrive();
     // (loaded while the sums cross)
     const float my_rstd = (int)threadIdx.x < channels ? __ldg(rstd + (at.c0 + threadIdx.x) / (uint32_t)width) : 0.0f;
     const float my_weight = (int)threadIdx.x < channels && weight ? __ldg(weight + at.c0 + threadIdx.x) : 1.0f;
     cluster_wait();
-    for (int q = threadIdx.x; q < channels; q += GN_THREADS) {
+    for (int q = threadIdx.x; q < channels; q += GR_THREADS) {
         float v = 0.0f, w = 0.0f;
         for (int r = 0; r < at.ranks; ++r) {
             v += sums[r * 2 * at.width + q];
@@ -372,16 +380,16 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_resident_backward_kernel(con
     }
     T *dx = static_cast<T *>(a.dx) + at.worker * a.dx_worker + at.sample * a.dx_sample + at.p0 * a.dx_pixel;
     gn_store<T>(a, dx, at.lanes * a.dx_pixel, at.c, turns, [&](int k, F2 (&d)[P]) {
-        const typename X::Raw raw = X::kept(x_place + k * GN_THREADS * M::X_BYTES, power_place + k * GN_THREADS);
+        const typename X::Raw raw = X::kept(x_place + k * GR_THREADS * M::X_BYTES, power_place + k * GR_THREADS);
         F2 g[P];
         X::centred(raw, ch.minus, d);
         if constexpr (WIDE) {
             F2 low[2], high[2];
-            LnChunk<float>::read(dz_place[k * GN_THREADS], low);
-            LnChunk<float>::read(dz_place[plane + k * GN_THREADS], high);
+            LnChunk<float>::read(dz_place[k * GR_THREADS], low);
+            LnChunk<float>::read(dz_place[plane + k * GR_THREADS], high);
             g[0] = low[0]; g[1] = low[1]; g[2] = high[0]; g[3] = high[1];
         } else {
-            LnChunk<T>::read(dz_place[k * GN_THREADS], g);
+            LnChunk<T>::read(dz_place[k * GR_THREADS], g);
         }
 #pragma unroll
         for (int j = 0; j < P; ++j) d[j] = fma(g[j], ch.scale[j], fma(d[j], along[j], level[j]));
@@ -391,13 +399,16 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_resident_backward_kernel(con
 // ---- launches --------------------------------------------------------------------------------------------
 
 constexpr int GN_MAX_MEMORY = 224 * 1024;
+#ifndef GN_BUDGET
+#define GN_BUDGET 56 * 1024
+#endif
 
 template <auto KERNEL>
 static cudaError_t gn_resident_launch(const GnArgs &a, int smem, cudaStream_t st) {
     static std::atomic<uint64_t> allowed{0};
     const cudaError_t e = ln_allow_smem(KERNEL, GN_MAX_MEMORY, allowed);
     if (e != cudaSuccess) return e;
-    return ln_launch(KERNEL, a, (int64_t)a.workers * a.samples * a.tiles, a.parts, GN_THREADS, smem, st);
+    return ln_launch(KERNEL, a, (int64_t)a.workers * a.samples * a.tiles, a.parts, GR_THREADS, smem, st);
 }
 
 template <typename T>
@@ -449,12 +460,12 @@ bool gn_resident_plan(GnArgs &a, int dtype, bool backward, bool checkpoint, int 
     constexpr int MOST = 8;
     auto fits = [&](int channels, int ranks, int budget) {
         const int chunks = (int)(ck_cols(channels) / vec);
-        if (chunks > GN_THREADS / 2) return false;
+        if (chunks > GR_THREADS / 2) return false;
         a.tile_chunks = chunks;
         a.tiles = (a.channels + channels - 1) / channels;
         a.part_pixels = (a.pixels + ranks - 1) / ranks;
         a.parts = ranks;
-        const int lanes = GN_THREADS / chunks;
+        const int lanes = GR_THREADS / chunks;
         const int64_t turns = (a.part_pixels + lanes - 1) / lanes;
         if (turns > 1024 || images * a.tiles * ranks >= (int64_t(1) << 31)) return false;
         a.turns = (int)turns;
@@ -468,10 +479,10 @@ bool gn_resident_plan(GnArgs &a, int dtype, bool backward, bool checkpoint, int 
         return channels;
     };
     int ranges[2] = {at_least(128), at_least(64)};
-    while (ranges[0] < a.channels && ranges[0] * 2 <= 32 * vec && a.pixels * ranges[0] <= 4 * GN_THREADS * vec &&
+    while (ranges[0] < a.channels && ranges[0] * 2 <= 32 * vec && a.pixels * ranges[0] <= 4 * GR_THREADS * vec &&
            images * ((a.channels + ranges[0] - 1) / ranges[0]) > 4 * LN_SMS)
         ranges[0] = std::min(2 * ranges[0], a.channels);
-    const int budgets[3] = {backward ? 0 : 75 * 1024, 112 * 1024, GN_MAX_MEMORY};
+    const int budgets[3] = {GN_BUDGET, 112 * 1024, GN_MAX_MEMORY};
     for (int budget : budgets)
         for (int channels : ranges)
             for (int ranks = 1; ranks <= MOST && ranks <= a.pixels; ++ranks) {
