@@ -4,61 +4,109 @@
 // operation more.  A thread owns one 16-byte chunk of channels and walks down the pixels, so what belongs to a channel
 // stays in registers and a channel's sums are the thread's until they meet those of the other pixels.
 #pragma once
+#include <type_traits>
+
 #include "activation.cuh"
 
 namespace liec {
 
 constexpr int GN_THREADS = 256;
 
-// Where a chunk of x comes from: the activations themselves, or their checkpoint.
-template <typename T>
-struct GnFromX {
+// A thread's chunks of one array: turn k is pixel k step rows further.  Raw is what a load leaves in registers, so that several
+// can be under way; rows off the 16-byte grid (not WHOLE) give two granules each, cut when they are used.
+template <typename T, bool WHOLE>
+struct GnReader {
+    static constexpr int VEC = Bits<T>::VEC;
+    struct Pair { uint4 a, b; };
+    struct One { uint4 a; };
+    using Raw = std::conditional_t<WHOLE, One, Pair>;
+    const T *row;   // of the first turn
+    int64_t step;
+    int c, cols;
+    __device__ __forceinline__ GnReader(const T *row, int64_t step, int c, int cols) : row(row), step(step), c(c), cols(cols) {}
+    __device__ __forceinline__ Raw load(int64_t k) const {
+        Raw r;
+        const T *now = row + k * step;
+        if constexpr (WHOLE) {   // (cols is a multiple of a chunk)
+            r.a = c < cols ? __ldg(reinterpret_cast<const uint4 *>(now + c)) : make_uint4(0u, 0u, 0u, 0u);
+        } else {
+        const int back = (int)(reinterpret_cast<uintptr_t>(now + c) & 15u) / (int)sizeof(T);
+        if (c >= back && c - back + 2 * VEC <= cols) {
+            const uint4 *g = reinterpret_cast<const uint4 *>(now + c - back);
+            r.a = __ldg(g);
+            r.b = __ldg(g + 1);
+        } else {
+            r.a = c < cols ? load_chunk_edge(now + c, cols - c) : make_uint4(0u, 0u, 0u, 0u);
+        }
+        }
+        return r;
+    }
+    __device__ __forceinline__ void read(const Raw &r, int64_t k, F2 (&out)[VEC / 2]) const {
+        uint4 q = r.a;
+        if constexpr (!WHOLE) {
+            const uint32_t shift = (uint32_t)reinterpret_cast<uintptr_t>(row + k * step + c) & 15u;
+            const int back = (int)shift / (int)sizeof(T);
+            if (c >= back && c - back + 2 * VEC <= cols) q = cut_granules<(int)sizeof(T)>(r.a, r.b, shift);
+        }
+        LnChunk<T>::read(q, out);
+    }
+};
+
+// Where x comes from: the activations themselves, or their checkpoint.
+template <typename T, bool WHOLE>
+struct GnFromX : GnReader<T, WHOLE> {
     static constexpr bool CHECKPOINT = false;
-    using Raw = uint4;
-    const T *row;
-    int64_t pixel;
-    __device__ __forceinline__ GnFromX(const GnArgs &a, int worker, int sample, int64_t p)
-        : row(static_cast<const T *>(a.x) + worker * a.x_worker + sample * a.x_sample + p * a.x_pixel), pixel(a.x_pixel) {}
-    __device__ __forceinline__ Raw load(int64_t p, int c, int cols) const { return load_chunk(row + p * pixel, c, cols); }
-    // the same from this thread's place in shared memory
-    static __device__ __forceinline__ Raw kept(const char *place, const uint8_t *) { return *reinterpret_cast<const uint4 *>(place); }
+    using Raw = typename GnReader<T, WHOLE>::Raw;
+    using Kept = uint4;
+    __device__ __forceinline__ GnFromX(const GnArgs &a, int worker, int sample, int64_t p, int lanes, int c)
+        : GnReader<T, WHOLE>(static_cast<const T *>(a.x) + worker * a.x_worker + sample * a.x_sample + p * a.x_pixel, lanes * a.x_pixel, c, a.channels) {}
+    static __device__ __forceinline__ Kept kept(const char *place, const uint8_t *) { return *reinterpret_cast<const uint4 *>(place); }
     template <int P>
-    static __device__ __forceinline__ void centred(const Raw &raw, const F2 (&minus)[P], F2 (&d)[P]) {
+    static __device__ __forceinline__ void centred(const Kept &raw, const F2 (&minus)[P], F2 (&d)[P]) {
         LnChunk<T>::read(raw, d);
 #pragma unroll
         for (int k = 0; k < P; ++k) d[k] = add(d[k], minus[k]);
+    }
+    template <int P>
+    __device__ __forceinline__ void centred(const Raw &raw, int64_t k, const F2 (&minus)[P], F2 (&d)[P]) const {
+        this->read(raw, k, d);
+#pragma unroll
+        for (int j = 0; j < P; ++j) d[j] = add(d[j], minus[j]);
     }
 };
 
 template <typename T>
 struct GnFromCheckpoint {
     static constexpr bool CHECKPOINT = true;
-    struct Raw { uint32_t w[Bits<T>::VEC / 4]; uint32_t byte; };
+    static constexpr int VEC = Bits<T>::VEC;
+    struct Raw { uint32_t w[VEC / 4]; uint32_t byte; };
+    using Kept = Raw;
     const int8_t *q;
     const uint8_t *scales;
-    int64_t cols;
-    __device__ __forceinline__ GnFromCheckpoint(const GnArgs &a, int worker, int sample, int64_t p) {
+    int64_t cols, step;
+    __device__ __forceinline__ GnFromCheckpoint(const GnArgs &a, int worker, int sample, int64_t p, int lanes, int c) {
         cols = (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK;
         const int64_t row = ((int64_t)worker * a.samples + sample) * a.pixels + p;
-        q = a.q + row * cols;
-        scales = a.scales + row * (cols / CK_BLOCK);
+        q = a.q + row * cols + c;
+        scales = a.scales + row * (cols / CK_BLOCK) + c / CK_BLOCK;
+        step = lanes * cols;
     }
-    __device__ __forceinline__ Raw load(int64_t p, int c, int) const {
+    __device__ __forceinline__ Raw load(int64_t k) const {
         Raw r;
-        const int8_t *at = q + p * cols + c;
-        if constexpr (Bits<T>::VEC == 8) {
+        const int8_t *at = q + k * step;
+        if constexpr (VEC == 8) {
             const uint2 v = __ldg(reinterpret_cast<const uint2 *>(at));
             r.w[0] = v.x;
             r.w[1] = v.y;
         } else {
             r.w[0] = __ldg(reinterpret_cast<const uint32_t *>(at));
         }
-        r.byte = __ldg(scales + p * (cols / CK_BLOCK) + c / CK_BLOCK);
+        r.byte = __ldg(scales + k * (step / CK_BLOCK));
         return r;
     }
-    static __device__ __forceinline__ Raw kept(const char *place, const uint8_t *power) {
+    static __device__ __forceinline__ Kept kept(const char *place, const uint8_t *power) {
         Raw r;
-        if constexpr (Bits<T>::VEC == 8) {
+        if constexpr (VEC == 8) {
             const uint2 v = *reinterpret_cast<const uint2 *>(place);
             r.w[0] = v.x;
             r.w[1] = v.y;
@@ -69,14 +117,32 @@ struct GnFromCheckpoint {
         return r;
     }
     template <int P>
-    static __device__ __forceinline__ void centred(const Raw &raw, const F2 (&minus)[P], F2 (&d)[P]) {
+    static __device__ __forceinline__ void centred(const Kept &raw, const F2 (&minus)[P], F2 (&d)[P]) {
         const F2 power = f2(ck_power(raw.byte));
 #pragma unroll
         for (int k = 0; k < P; k += 2) ck_unpack(raw.w[k / 2], d[k], d[k + 1]);
 #pragma unroll
         for (int k = 0; k < P; ++k) d[k] = fma(d[k], power, minus[k]);   // (q 2^e is exact: one rounding)
     }
+    template <int P>
+    __device__ __forceinline__ void centred(const Raw &raw, int64_t, const F2 (&minus)[P], F2 (&d)[P]) const { centred(raw, minus, d); }
 };
+
+// use(k, raw) for all turns, the loads of N of them issued together.
+template <int N, typename L, typename U>
+__device__ __forceinline__ void gn_turns(int64_t turns, L &&load, U &&use) {
+    int64_t k = 0;
+#pragma unroll 1
+    for (; k + N <= turns; k += N) {
+        decltype(load(k)) raw[N];
+#pragma unroll
+        for (int u = 0; u < N; ++u) raw[u] = load(k + u);
+#pragma unroll
+        for (int u = 0; u < N; ++u) use(k + u, raw[u]);
+    }
+#pragma unroll 1
+    for (; k < turns; ++k) use(k, load(k));
+}
 
 // SiLU of a pair.  Results in bfloat16 take the hardware's exponential and reciprocal as they are (relative errors of
 // (|z| + 2) 2^-23, far below a bfloat16 step wherever the gate is not zero; an infinite exponential gives a gate of zero).
@@ -164,8 +230,8 @@ struct GnChannels {
 
 // dz = dy act'(z) from d = x - m.  The sign of z decides for ReLU: z carries at most 4 2^-24 (|b| + |z|) of rounding, so
 // where |z| is above 2^-20 |b| its sign is right; elsewhere it is taken from binary64.
-template <typename T, int ACT, typename X, int P>
-__device__ __forceinline__ void gn_slope(const GnArgs &a, int worker, int64_t image, int c, const GnChannels<P> &ch, const typename X::Raw &raw,
+template <typename T, int ACT, int P, typename E>
+__device__ __forceinline__ void gn_slope(const GnArgs &a, int worker, int64_t image, int c, const GnChannels<P> &ch, E &&exact,
                                          const F2 (&d)[P], const F2 (&dy)[P], F2 (&dz)[P]) {
     if constexpr (ACT == LIEC_ACT_NONE) {
 #pragma unroll
@@ -189,8 +255,7 @@ __device__ __forceinline__ void gn_slope(const GnArgs &a, int worker, int64_t im
         }
         if (near != 0u) {
             F2 x[P];
-            const F2 none[P] = {};
-            X::centred(raw, none, x);
+            exact(x);   // x itself
 #pragma unroll
             for (int k = 0; k < 2 * P; ++k)
                 if ((near >> k & 1u) && c + k < a.channels) {

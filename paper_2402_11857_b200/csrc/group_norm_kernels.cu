@@ -1,91 +1,101 @@
-// Group normalisation with an activation over N workers' images, channels last, forward and backward.  Images are
-// cut into parts of their pixels; the parts' sums per channel go through the workspace.
+// Group normalisation with an activation over N workers' images, channels last, forward and backward: images of any size,
+// read twice.  They are cut into tiles of channels and parts of pixels; a CTA's threads walk down the pixels of its part, and
+// the parts' sums per channel go through the workspace.  The second reading takes the CTAs in the opposite order: what was
+// read last is still in the L2 cache.
 #include "group_norm.cuh"
 
 namespace liec {
 
+template <int VEC>
 struct GnPlace {   // what a CTA and its thread work on
-    int64_t image, p0, n;   // first pixel of the part and their number
-    int worker, sample, tile, part, chunk, lane, lanes, c;
-    bool live;
-    __device__ __forceinline__ GnPlace(const GnArgs &a, int vec) {
-        int64_t b = blockIdx.x;
-        part = (int)(b % a.parts);
-        b /= a.parts;
-        tile = (int)(b % a.tiles);
-        image = b / a.tiles;
-        worker = (int)(image / a.samples);
-        sample = (int)(image - (int64_t)worker * a.samples);
-        p0 = part * a.part_pixels;
-        n = max((int64_t)0, min(a.part_pixels, a.pixels - p0));
-        chunk = threadIdx.x % a.tile_chunks;
-        lane = threadIdx.x / a.tile_chunks;
-        lanes = GN_THREADS / a.tile_chunks;
-        c = (tile * a.tile_chunks + chunk) * vec;
-        live = lane < lanes && c < (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK;
+    int64_t image, p0, turns;   // the thread's first pixel and its chunks
+    int worker, sample, part, chunk, lane, lanes, c, c0;
+    __device__ __forceinline__ GnPlace(const GnArgs &a, bool backwards) {
+        const uint32_t block = backwards ? gridDim.x - 1 - blockIdx.x : blockIdx.x, unit = block / (uint32_t)a.parts, picture = unit / (uint32_t)a.tiles;
+        part = (int)(block - unit * a.parts);
+        image = picture;
+        worker = (int)(picture / (uint32_t)a.samples);
+        sample = (int)(picture - (uint32_t)worker * a.samples);
+        lane = (int)(threadIdx.x / (uint32_t)a.tile_chunks);
+        chunk = (int)threadIdx.x - lane * a.tile_chunks;
+        lanes = (int)(GN_THREADS / (uint32_t)a.tile_chunks);
+        c0 = (int)(unit - picture * a.tiles) * a.tile_chunks * VEC;
+        c = c0 + chunk * VEC;
+        p0 = part * a.part_pixels + lane;
+        const int64_t end = min((part + 1) * a.part_pixels, a.pixels);
+        const bool live = lane < lanes && c < (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK;
+        turns = live && p0 < end ? (end - p0 + lanes - 1) / lanes : 0;
     }
 };
 
-// The channels' sums of all pixel lanes, in a fixed order: two per channel of the tile, through `box`.
+// Two sums per channel over all pixel lanes, in a fixed order: out[which][channel].
 template <int VEC>
-__device__ __forceinline__ void gn_channel_sums(const GnPlace &at, int tile_chunks, const F2 (&s)[VEC / 2], const F2 (&t)[VEC / 2], float *box) {
+__device__ __forceinline__ void gn_channel_sums(const GnPlace<VEC> &at, int tile_chunks, const F2 (&s)[VEC / 2], const F2 (&t)[VEC / 2], float *box) {
     const int width = tile_chunks * VEC;
-    if (at.live) {
+    if (at.lane < at.lanes) {
+        float4 *b = reinterpret_cast<float4 *>(box + at.lane * 2 * width + at.chunk * VEC);
 #pragma unroll
-        for (int k = 0; k < VEC / 2; ++k) {
-            float *b = box + (at.lane * 2) * width + at.chunk * VEC + 2 * k;
-            b[0] = lo(s[k]);
-            b[1] = hi(s[k]);
-            b[width] = lo(t[k]);
-            b[width + 1] = hi(t[k]);
+        for (int k = 0; k < VEC / 2; k += 2) {
+            b[k / 2] = make_float4(lo(s[k]), hi(s[k]), lo(s[k + 1]), hi(s[k + 1]));
+            b[width / 4 + k / 2] = make_float4(lo(t[k]), hi(t[k]), lo(t[k + 1]), hi(t[k + 1]));
         }
     }
     __syncthreads();
     for (int q = threadIdx.x; q < 2 * width; q += GN_THREADS) {
         float v = 0.0f;
+#pragma unroll 4
         for (int l = 0; l < at.lanes; ++l) v += box[l * 2 * width + q];
         box[q] = v;   // (own column: nobody else reads it)
     }
     __syncthreads();
 }
 
+__device__ __forceinline__ void gn_wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Mean and squares around it of every channel of a part, about the part's first pixel.
-template <typename T>
-__global__ void __launch_bounds__(GN_THREADS) gn_moments_kernel(const __grid_constant__ GnArgs a) {
+template <typename T, bool WHOLE>
+__global__ void __launch_bounds__(GN_THREADS, WHOLE ? 4 : 3) gn_moments_kernel(const __grid_constant__ GnArgs a) {
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
-    __shared__ float box[GN_THREADS * 2 * VEC];
-    const GnPlace at(a, VEC);
+    __shared__ __align__(16) float box[GN_THREADS * 2 * VEC];
+    __shared__ float origin[GN_THREADS * VEC];
+    const GnPlace<VEC> at(a, false);
     F2 s[P] = {}, t[P] = {};
-    if (at.live && at.n > 0) {
-        const GnFromX<T> x(a, at.worker, at.sample, at.p0);
+    if (at.turns > 0) {
+        const GnFromX<T, WHOLE> x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
         F2 minus[P], d[P];
-        const F2 none[P] = {};
-        GnFromX<T>::centred(x.load(0, at.c, a.channels), none, minus);
+        LnChunk<T>::read(at.c < a.channels ? load_chunk(x.row - at.lane * a.x_pixel, at.c, a.channels) : make_uint4(0u, 0u, 0u, 0u), d);
 #pragma unroll
-        for (int k = 0; k < P; ++k) minus[k] = f2(-lo(minus[k]), -hi(minus[k]));
-        for (int64_t p = at.lane; p < at.n; p += at.lanes) {
-            GnFromX<T>::centred(x.load(p, at.c, a.channels), minus, d);
-#pragma unroll
-            for (int k = 0; k < P; ++k) {
-                s[k] = add(s[k], d[k]);
-                t[k] = fma(d[k], d[k], t[k]);
+        for (int k = 0; k < P; ++k) {
+            minus[k] = f2(-lo(d[k]), -hi(d[k]));
+            if (at.lane == 0) {
+                origin[at.chunk * VEC + 2 * k] = lo(d[k]);
+                origin[at.chunk * VEC + 2 * k + 1] = hi(d[k]);
             }
         }
+        gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int64_t k) { return x.load(k); }, [&](int64_t k, const typename GnFromX<T, WHOLE>::Raw &raw) {
+            x.centred(raw, k, minus, d);
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                s[j] = add(s[j], d[j]);
+                t[j] = fma(d[j], d[j], t[j]);
+            }
+        });
     }
     gn_channel_sums<VEC>(at, a.tile_chunks, s, t, box);
-    const int width = a.tile_chunks * VEC, c0 = at.tile * width;
-    float *out = a.part + (at.image * a.parts + at.part) * 2 * a.channels;
-    const GnFromX<T> x(a, at.worker, at.sample, at.p0);
-    for (int q = threadIdx.x; q < width && c0 + q < a.channels; q += GN_THREADS) {
-        const float n = (float)at.n, mean = at.n > 0 ? box[q] / n : 0.0f;
-        out[c0 + q] = at.n > 0 ? (float)x.row[c0 + q] + mean : 0.0f;
-        out[a.channels + c0 + q] = at.n > 0 ? fmaxf(__fmaf_rn(-box[q], mean, box[width + q]), 0.0f) : 0.0f;
+    const int width = a.tile_chunks * VEC;
+    float *out = a.part + (at.image * a.parts + at.part) * 2 * a.channels + at.c0;
+    const float n = (float)(min((at.part + 1) * a.part_pixels, a.pixels) - at.part * a.part_pixels);
+    for (int q = threadIdx.x; q < width && at.c0 + q < a.channels; q += GN_THREADS) {
+        const float mean = box[q] / n;
+        out[q] = origin[q] + mean;
+        out[a.channels + q] = fmaxf(__fmaf_rn(-box[q], mean, box[width + q]), 0.0f);
     }
 }
 
 // Joins a group's channels and parts: a warp per group, binary64, in a fixed order.
 __global__ void __launch_bounds__(GN_THREADS) gn_statistics_kernel(const __grid_constant__ GnArgs a) {
     const int64_t g = ((int64_t)blockIdx.x * GN_THREADS + threadIdx.x) / 32, images = (int64_t)a.workers * a.samples;
+    gn_wait_for_kernel_before();
     if (g >= images * a.groups) return;
     const int lane = threadIdx.x & 31, width = a.channels / a.groups, entries = width * a.parts;
     const int64_t image = g / a.groups;
@@ -110,68 +120,105 @@ __global__ void __launch_bounds__(GN_THREADS) gn_statistics_kernel(const __grid_
     }
 }
 
-template <typename T, int ACT, bool COMPRESS>
-__global__ void __launch_bounds__(GN_THREADS) gn_apply_kernel(const __grid_constant__ GnArgs a) {
+template <typename T, bool WHOLE, int ACT, bool COMPRESS>
+__global__ void __launch_bounds__(GN_THREADS, 3) gn_apply_kernel(const __grid_constant__ GnArgs a) {
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
-    const GnPlace at(a, VEC);
-    if (!at.live) return;
-    const GnFromX<T> x(a, at.worker, at.sample, at.p0);
+    const GnPlace<VEC> at(a, true);
+    const GnFromX<T, WHOLE> x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
     T *y = static_cast<T *>(a.y) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
+    const int64_t row0 = at.image * a.pixels + at.p0, y_step = at.lanes * a.y_pixel;
+    gn_wait_for_kernel_before();
+    if (at.turns == 0) return;
     GnChannels<P> ch;
     ch.read(a, at.worker, at.image, at.c);
-    const int64_t row0 = at.image * a.pixels + at.p0;
-    for (int64_t p = at.lane; p < at.n; p += at.lanes) {
-        const uint4 raw = x.load(p, at.c, a.channels);
+    gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int64_t k) { return x.load(k); }, [&](int64_t k, const typename GnFromX<T, WHOLE>::Raw &raw) {
         F2 d[P];
         if constexpr (COMPRESS) {
-            LnChunk<T>::read(raw, d);
-            gn_compress<T>(a, d, row0 + p, at.c);
-        }
-        GnFromX<T>::centred(raw, ch.minus, d);
+            x.read(raw, k, d);
+            gn_compress<T>(a, d, row0 + k * at.lanes, at.c);
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-            d[k] = gn_act<T, ACT>(fma(d[k], ch.scale[k], ch.bias[k]));
+            for (int j = 0; j < P; ++j) d[j] = add(d[j], ch.minus[j]);
+        } else {
+            x.centred(raw, k, ch.minus, d);
         }
-        store_chunk(y + p * a.y_pixel, at.c, a.channels, d);
-    }
+#pragma unroll
+        for (int j = 0; j < P; ++j) d[j] = gn_act<T, ACT>(fma(d[j], ch.scale[j], ch.bias[j]));
+        if (a.whole_out) {
+            if (at.c < a.channels) LnChunk<T>::write(y + k * y_step + at.c, d);
+        } else {
+            store_chunk(y + k * y_step, at.c, a.channels, d);
+        }
+    });
 }
 
 // Backward: sums of dz and dz xh of every channel of a part.
-template <typename T, typename X, int ACT>
-__global__ void __launch_bounds__(GN_THREADS) gn_slopes_kernel(const __grid_constant__ GnArgs a) {
+template <typename T, bool WHOLE, typename X, int ACT>
+__global__ void __launch_bounds__(GN_THREADS, 2) gn_slopes_kernel(const __grid_constant__ GnArgs a) {
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
-    __shared__ float box[GN_THREADS * 2 * VEC];
-    const GnPlace at(a, VEC);
+    __shared__ __align__(16) float box[GN_THREADS * 2 * VEC];
+    const GnPlace<VEC> at(a, false);
     F2 s[P] = {}, t[P] = {};
-    if (at.live) {
-        const X x(a, at.worker, at.sample, at.p0);
-        const T *dy = static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
+    if (at.turns > 0) {
+        const X x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
+        const GnReader<T, WHOLE> dy(static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel, at.lanes * a.y_pixel, at.c,
+                                    a.channels);
         GnChannels<P> ch;
         ch.read(a, at.worker, at.image, at.c);
-        for (int64_t p = at.lane; p < at.n; p += at.lanes) {
-            const typename X::Raw raw = x.load(p, at.c, a.channels);
+        struct Raw { typename X::Raw x; typename GnReader<T, WHOLE>::Raw dy; };
+        gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int64_t k) { return Raw{x.load(k), dy.load(k)}; }, [&](int64_t k, const Raw &raw) {
             F2 d[P], g[P];
-            X::centred(raw, ch.minus, d);
-            LnChunk<T>::read(load_chunk(dy + p * a.y_pixel, at.c, a.channels), g);
-            gn_slope<T, ACT, X>(a, at.worker, at.image, at.c, ch, raw, d, g, g);
+            x.centred(raw.x, k, ch.minus, d);
+            dy.read(raw.dy, k, g);
+            gn_slope<T, ACT>(a, at.worker, at.image, at.c, ch, [&](F2 (&v)[P]) { const F2 none[P] = {}; x.centred(raw.x, k, none, v); }, d, g, g);
 #pragma unroll
-            for (int k = 0; k < P; ++k) {
-                s[k] = add(s[k], g[k]);
-                t[k] = fma(g[k], d[k], t[k]);
+            for (int j = 0; j < P; ++j) {
+                s[j] = add(s[j], g[j]);
+                t[j] = fma(g[j], d[j], t[j]);
             }
-        }
+        });
     }
     gn_channel_sums<VEC>(at, a.tile_chunks, s, t, box);
-    const int width = a.tile_chunks * VEC, c0 = at.tile * width;
-    float *out = a.part + (at.image * a.parts + at.part) * 2 * a.channels;
-    for (int q = threadIdx.x; q < width && c0 + q < a.channels; q += GN_THREADS) {
-        out[c0 + q] = box[q];
-        out[a.channels + c0 + q] = box[width + q] * a.rstd[at.image * a.groups + (c0 + q) / (a.channels / a.groups)];
+    const int width = a.tile_chunks * VEC;
+    float *out = a.part + (at.image * a.parts + at.part) * 2 * a.channels + at.c0;
+    for (int q = threadIdx.x; q < width && at.c0 + q < a.channels; q += GN_THREADS) {
+        out[q] = box[q];
+        out[a.channels + q] = box[width + q] * a.rstd[at.image * a.groups + (uint32_t)(at.c0 + q) / (uint32_t)(a.channels / a.groups)];
     }
 }
 
-// Per group: r mean(dz w) and r^2 mean(dz w xh).
-__global__ void __launch_bounds__(GN_THREADS) gn_levels_kernel(const __grid_constant__ GnArgs a) {
+// dw and db: a worker's images and parts (all workers', where they share the gradient) in binary64, rounded once.  A
+// warp takes 32 channels, eight warps share the parts.
+__device__ __forceinline__ void gn_join(const GnArgs &a, uint32_t block) {
+    __shared__ double box[GN_THREADS / 32][32];
+    const uint32_t columns = (uint32_t)(a.channels + 31) / 32, pair = block / columns;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, worker = (int)(pair >> 1), c = (int)(block - pair * columns) * 32 + lane;
+    const bool weight = (pair & 1) == 0;
+    void *out = weight ? a.dweight : a.dbias;
+    if (!out) return;
+    const int64_t rows = a.pixels == 0 ? 0 : (int64_t)(a.shared ? a.workers : 1) * a.samples * a.parts, first = a.shared ? 0 : (int64_t)worker * a.samples * a.parts;
+    double s = 0.0;
+    if (c < a.channels) {
+        const float *from = a.part + (first * 2 + (weight ? 1 : 0)) * a.channels + c;
+#pragma unroll 4
+        for (int64_t i = warp; i < rows; i += GN_THREADS / 32) s += (double)from[i * 2 * a.channels];
+    }
+    box[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && c < a.channels) {
+        for (int w = 1; w < GN_THREADS / 32; ++w) s += box[w][lane];
+        const int64_t at = worker * (weight ? a.dweight_stride : a.dbias_stride) + c;
+        if (a.grad_dtype == LIEC_F32) static_cast<float *>(out)[at] = (float)s;
+        else static_cast<__nv_bfloat16 *>(out)[at] = __float2bfloat16_rn((float)s);
+    }
+}
+
+// The first `level_ctas` CTAs: per group r mean(dz w) and r^2 mean(dz w xh).  The others: dw and db.
+__global__ void __launch_bounds__(GN_THREADS) gn_levels_kernel(const __grid_constant__ GnArgs a, uint32_t level_ctas) {
+    gn_wait_for_kernel_before();
+    if (blockIdx.x >= level_ctas) {
+        gn_join(a, blockIdx.x - level_ctas);
+        return;
+    }
     const int64_t g = ((int64_t)blockIdx.x * GN_THREADS + threadIdx.x) / 32, images = (int64_t)a.workers * a.samples;
     if (g >= images * a.groups) return;
     const int lane = threadIdx.x & 31, width = a.channels / a.groups, entries = width * a.parts;
@@ -190,73 +237,61 @@ __global__ void __launch_bounds__(GN_THREADS) gn_levels_kernel(const __grid_cons
     t = warp_sum(t);
     if (lane == 0) {
         const double n = (double)a.pixels * width, r = (double)a.rstd[g];
-        a.level[2 * g] = (float)(r * s / n);
-        a.level[2 * g + 1] = (float)(r * r * t / n);
+        a.level[2 * g] = (float)(-r * s / n);
+        a.level[2 * g + 1] = (float)(-r * r * t / n);
     }
 }
 
 // dx = A dz - r mean(dz w) - d r^2 mean(dz w xh)
-template <typename T, typename X, int ACT>
-__global__ void __launch_bounds__(GN_THREADS) gn_dx_kernel(const __grid_constant__ GnArgs a) {
+template <typename T, bool WHOLE, typename X, int ACT>
+__global__ void __launch_bounds__(GN_THREADS, 2) gn_dx_kernel(const __grid_constant__ GnArgs a) {
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
-    const GnPlace at(a, VEC);
-    if (!at.live || at.c >= a.channels) return;
-    const X x(a, at.worker, at.sample, at.p0);
-    const T *dy = static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
+    const GnPlace<VEC> at(a, true);
+    const X x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
+    const GnReader<T, WHOLE> dy(static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel, at.lanes * a.y_pixel, at.c, a.channels);
     T *dx = static_cast<T *>(a.dx) + at.worker * a.dx_worker + at.sample * a.dx_sample + at.p0 * a.dx_pixel;
+    const int64_t dx_step = at.lanes * a.dx_pixel;
     GnChannels<P> ch;
-    ch.read(a, at.worker, at.image, at.c);
+    if (at.turns > 0) ch.read(a, at.worker, at.image, at.c);
+    gn_wait_for_kernel_before();
+    if (at.turns == 0 || at.c >= a.channels) return;
     F2 level[P], along[P];
+    const uint32_t width = (uint32_t)a.channels / (uint32_t)a.groups;
+    GnGroup group(at.c, width);
+    const float *levels = a.level + at.image * a.groups * 2;
 #pragma unroll
-    for (int k = 0; k < 2 * P; ++k) {
-        const int64_t g = at.image * a.groups + min(at.c + k, a.channels - 1) / (a.channels / a.groups);
-        GnChannels<P>::set(level[k / 2], k % 2, -a.level[2 * g]);
-        GnChannels<P>::set(along[k / 2], k % 2, -a.level[2 * g + 1]);
+    for (int k = 0; k < 2 * P; ++k, group.next(width)) {
+        const bool in = at.c + k < a.channels;
+        GnChannels<P>::set(level[k / 2], k % 2, in ? levels[2 * group.group] : 0.0f);
+        GnChannels<P>::set(along[k / 2], k % 2, in ? levels[2 * group.group + 1] : 0.0f);
     }
-    for (int64_t p = at.lane; p < at.n; p += at.lanes) {
-        const typename X::Raw raw = x.load(p, at.c, a.channels);
+    struct Raw { typename X::Raw x; typename GnReader<T, WHOLE>::Raw dy; };
+    gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int64_t k) { return Raw{x.load(k), dy.load(k)}; }, [&](int64_t k, const Raw &raw) {
         F2 d[P], g[P];
-        X::centred(raw, ch.minus, d);
-        LnChunk<T>::read(load_chunk(dy + p * a.y_pixel, at.c, a.channels), g);
-        gn_slope<T, ACT, X>(a, at.worker, at.image, at.c, ch, raw, d, g, g);
+        x.centred(raw.x, k, ch.minus, d);
+        dy.read(raw.dy, k, g);
+        gn_slope<T, ACT>(a, at.worker, at.image, at.c, ch, [&](F2 (&v)[P]) { const F2 none[P] = {}; x.centred(raw.x, k, none, v); }, d, g, g);
 #pragma unroll
-        for (int k = 0; k < P; ++k) d[k] = fma(g[k], ch.scale[k], fma(d[k], along[k], level[k]));
-        store_chunk(dx + p * a.dx_pixel, at.c, a.channels, d);
-    }
-}
-
-// dw and db: a worker's images and parts (all workers', where they share the gradient) in binary64, rounded once.  A
-// warp takes 32 channels, eight warps share the parts.
-__global__ void __launch_bounds__(GN_THREADS) gn_join_kernel(const __grid_constant__ GnArgs a) {
-    __shared__ double box[GN_THREADS / 32][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, worker = blockIdx.y, c = blockIdx.x * 32 + lane;
-    const bool weight = blockIdx.z == 0;
-    void *out = weight ? a.dweight : a.dbias;
-    if (!out) return;
-    const int64_t rows = a.pixels == 0 ? 0 : (int64_t)(a.shared ? a.workers : 1) * a.samples * a.parts, first = a.shared ? 0 : (int64_t)worker * a.samples * a.parts;
-    double s = 0.0;
-    if (c < a.channels)
-        for (int64_t i = warp; i < rows; i += GN_THREADS / 32) s += (double)a.part[((first + i) * 2 + (weight ? 1 : 0)) * a.channels + c];
-    box[warp][lane] = s;
-    __syncthreads();
-    if (warp == 0 && c < a.channels) {
-        for (int w = 1; w < GN_THREADS / 32; ++w) s += box[w][lane];
-        const int64_t at = worker * (weight ? a.dweight_stride : a.dbias_stride) + c;
-        if (a.grad_dtype == LIEC_F32) static_cast<float *>(out)[at] = (float)s;
-        else static_cast<__nv_bfloat16 *>(out)[at] = __float2bfloat16_rn((float)s);
-    }
+        for (int j = 0; j < P; ++j) d[j] = fma(g[j], ch.scale[j], fma(d[j], along[j], level[j]));
+        if (a.whole_out) LnChunk<T>::write(dx + k * dx_step + at.c, d);
+        else store_chunk(dx + k * dx_step, at.c, a.channels, d);
+    });
 }
 
 // ---- launches --------------------------------------------------------------------------------------------
 
+// Threads of a CTA share the chunks of a tile, so that few images still give a thread 16 pixels or more; parts of an
+// image's pixels as there are places for CTAs (six on an SM), four times as many while a thread keeps 64 pixels.
 static void gn_plan(GnArgs &a, int vec) {
-    const int chunks = (int)(ck_cols(a.channels) / vec);
-    a.tile_chunks = chunks < 64 ? chunks : 64;
+    const int chunks = (int)(ck_cols(a.channels) / vec), step = CK_BLOCK / vec;
+    int64_t lanes = std::max<int64_t>(1, std::min<int64_t>(GN_THREADS / step, a.pixels / 16));
+    a.tile_chunks = (int)std::min<int64_t>(chunks, std::max<int64_t>(std::min(chunks, 32), GN_THREADS / lanes / step * step));
     a.tiles = (chunks + a.tile_chunks - 1) / a.tile_chunks;
-    const int lanes = GN_THREADS / a.tile_chunks;
-    const int64_t images = (int64_t)a.workers * a.samples, places = images * a.tiles;
-    const int64_t most = (a.pixels + 8 * lanes - 1) / (8 * lanes), want = (148 * 16 + places - 1) / std::max<int64_t>(places, 1);
-    const int64_t parts = std::max<int64_t>(1, std::min(most, want));
+    a.tile_chunks = ((chunks + a.tiles - 1) / a.tiles + step - 1) / step * step;
+    lanes = GN_THREADS / a.tile_chunks;
+    const int64_t places = (int64_t)a.workers * a.samples * a.tiles;
+    const int64_t few = std::min((LN_SMS * 6 + places - 1) / places, a.pixels / (lanes * 16)), many = std::min((LN_SMS * 24 + places - 1) / places, a.pixels / (lanes * 64));
+    const int64_t parts = std::max<int64_t>(1, std::max(few, many));
     a.part_pixels = std::max<int64_t>(1, (a.pixels + parts - 1) / parts);
     a.parts = (int)std::max<int64_t>(1, (a.pixels + a.part_pixels - 1) / a.part_pixels);
 }
@@ -281,87 +316,93 @@ size_t group_norm_workspace(const GnArgs &a, int dtype, bool backward) {
 static bool gn_whole(const GnArgs &a, int dtype, const void *p, int64_t pixel, int64_t sample, int64_t worker) {
     uint64_t bits = reinterpret_cast<uintptr_t>(p);
     const uint64_t size = dtype == 0 ? 4 : 2;
+    bits |= (uint64_t)a.channels * size;
     if (a.pixels > 1) bits |= (uint64_t)pixel * size;
     if (a.samples > 1) bits |= (uint64_t)sample * size;
     if (a.workers > 1) bits |= (uint64_t)worker * size;
     return (bits & 15u) == 0;
 }
 
-static unsigned gn_group_ctas(const GnArgs &a) {
-    return (unsigned)(((int64_t)a.workers * a.samples * a.groups * 32 + GN_THREADS - 1) / GN_THREADS);
+// after: starts while the kernel before ends, and waits for it where it needs it.
+template <typename... A>
+static cudaError_t gn_launch(void (*kernel)(A...), int64_t ctas, bool after, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(GN_THREADS);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = after ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <typename T>
+static int64_t gn_group_ctas(const GnArgs &a) { return ((int64_t)a.workers * a.samples * a.groups * 32 + GN_THREADS - 1) / GN_THREADS; }
+static int64_t gn_join_ctas(const GnArgs &a) { return a.dweight || a.dbias ? (int64_t)((a.channels + 31) / 32) * (a.shared ? 1 : a.workers) * 2 : 0; }
+
+template <typename T, bool WHOLE>
 struct GnForwardLaunch {
     const GnArgs &a;
-    unsigned ctas;
     cudaStream_t st;
     template <int ACT>
     cudaError_t operator()() {
-        gn_moments_kernel<T><<<ctas, GN_THREADS, 0, st>>>(a);
-        gn_statistics_kernel<<<gn_group_ctas(a), GN_THREADS, 0, st>>>(a);
-        if (a.q) gn_apply_kernel<T, ACT, true><<<ctas, GN_THREADS, 0, st>>>(a);
-        else gn_apply_kernel<T, ACT, false><<<ctas, GN_THREADS, 0, st>>>(a);
-        return cudaGetLastError();
+        const int64_t ctas = (int64_t)a.workers * a.samples * a.tiles * a.parts;
+        cudaError_t e = gn_launch(gn_moments_kernel<T, WHOLE>, ctas, false, st, a);
+        if (e == cudaSuccess) e = gn_launch(gn_statistics_kernel, gn_group_ctas(a), true, st, a);
+        if (e != cudaSuccess) return e;
+        return a.q ? gn_launch(gn_apply_kernel<T, WHOLE, ACT, true>, ctas, true, st, a) : gn_launch(gn_apply_kernel<T, WHOLE, ACT, false>, ctas, true, st, a);
     }
 };
 
 cudaError_t launch_group_norm_forward(GnArgs a, int dtype, cudaStream_t st) {
     if (a.samples == 0 || a.pixels == 0) return cudaSuccess;
     int smem;
-    if (gn_resident_plan(a, dtype, false, false, smem)) {
-        a.whole = gn_whole(a, dtype, a.x, a.x_pixel, a.x_sample, a.x_worker);
-        a.whole_out = a.channels % (dtype == 0 ? 4 : 8) == 0 && gn_whole(a, dtype, a.y, a.y_pixel, a.y_sample, a.y_worker);
-        return gn_resident_forward(a, dtype, smem, st);
-    }
+    a.whole = gn_whole(a, dtype, a.x, a.x_pixel, a.x_sample, a.x_worker);
+    a.whole_out = gn_whole(a, dtype, a.y, a.y_pixel, a.y_sample, a.y_worker);
+    if (gn_resident_plan(a, dtype, false, false, smem)) return gn_resident_forward(a, dtype, smem, st);
     gn_plan(a, dtype == 0 ? 4 : 8);
-    const unsigned ctas = (unsigned)((int64_t)a.workers * a.samples * a.tiles * a.parts);
-    return dtype == 0 ? gn_for_act(a.act, GnForwardLaunch<float>{a, ctas, st}) : gn_for_act(a.act, GnForwardLaunch<__nv_bfloat16>{a, ctas, st});
+    if (dtype == 0) return a.whole ? gn_for_act(a.act, GnForwardLaunch<float, true>{a, st}) : gn_for_act(a.act, GnForwardLaunch<float, false>{a, st});
+    return a.whole ? gn_for_act(a.act, GnForwardLaunch<__nv_bfloat16, true>{a, st}) : gn_for_act(a.act, GnForwardLaunch<__nv_bfloat16, false>{a, st});
 }
 
-template <typename T, typename X>
+template <typename T, bool WHOLE, typename X>
 struct GnBackwardLaunch {
     const GnArgs &a;
-    unsigned ctas;
     cudaStream_t st;
     template <int ACT>
     cudaError_t operator()() {
-        gn_slopes_kernel<T, X, ACT><<<ctas, GN_THREADS, 0, st>>>(a);
-        if (a.dx) {
-            gn_levels_kernel<<<gn_group_ctas(a), GN_THREADS, 0, st>>>(a);
-            gn_dx_kernel<T, X, ACT><<<ctas, GN_THREADS, 0, st>>>(a);
-        }
-        return cudaGetLastError();
+        const int64_t ctas = (int64_t)a.workers * a.samples * a.tiles * a.parts, levels = a.dx ? gn_group_ctas(a) : 0;
+        cudaError_t e = gn_launch(gn_slopes_kernel<T, WHOLE, X, ACT>, ctas, false, st, a);
+        if (e == cudaSuccess) e = gn_launch(gn_levels_kernel, levels + gn_join_ctas(a), true, st, a, (uint32_t)levels);
+        if (e == cudaSuccess && a.dx) e = gn_launch(gn_dx_kernel<T, WHOLE, X, ACT>, ctas, true, st, a);
+        return e;
     }
 };
 
-template <typename T>
-static cudaError_t gn_backward(const GnArgs &a, unsigned ctas, cudaStream_t st) {
-    return a.x ? gn_for_act(a.act, GnBackwardLaunch<T, GnFromX<T>>{a, ctas, st}) : gn_for_act(a.act, GnBackwardLaunch<T, GnFromCheckpoint<T>>{a, ctas, st});
+template <typename T, bool WHOLE>
+static cudaError_t gn_backward(const GnArgs &a, cudaStream_t st) {
+    return a.x ? gn_for_act(a.act, GnBackwardLaunch<T, WHOLE, GnFromX<T, WHOLE>>{a, st}) : gn_for_act(a.act, GnBackwardLaunch<T, WHOLE, GnFromCheckpoint<T>>{a, st});
 }
 
 cudaError_t launch_group_norm_backward(GnArgs a, int dtype, cudaStream_t st) {
     int smem;
     if (a.samples == 0 || a.pixels == 0) {
         a.parts = 1;
-    } else if (gn_resident_plan(a, dtype, true, !a.x, smem)) {
-        a.whole = gn_whole(a, dtype, a.dy, a.y_pixel, a.y_sample, a.y_worker) && (!a.x || gn_whole(a, dtype, a.x, a.x_pixel, a.x_sample, a.x_worker));
-        a.whole_out = a.channels % (dtype == 0 ? 4 : 8) == 0 && gn_whole(a, dtype, a.dx, a.dx_pixel, a.dx_sample, a.dx_worker);
+        return gn_launch(gn_levels_kernel, gn_join_ctas(a), false, st, a, 0u);
+    }
+    a.whole = gn_whole(a, dtype, a.dy, a.y_pixel, a.y_sample, a.y_worker) && (!a.x || gn_whole(a, dtype, a.x, a.x_pixel, a.x_sample, a.x_worker));
+    a.whole_out = gn_whole(a, dtype, a.dx, a.dx_pixel, a.dx_sample, a.dx_worker);
+    if (gn_resident_plan(a, dtype, true, !a.x, smem)) {
         const cudaError_t e = gn_resident_backward(a, dtype, smem, st);
-        if (e != cudaSuccess) return e;
+        if (e != cudaSuccess || gn_join_ctas(a) == 0) return e;
         a.parts = 1;   // (the cluster's parts are one by now)
-    } else {
-        gn_plan(a, dtype == 0 ? 4 : 8);
-        a.level = a.part + (int64_t)a.workers * a.samples * a.parts * 2 * a.channels;
-        const unsigned ctas = (unsigned)((int64_t)a.workers * a.samples * a.tiles * a.parts);
-        const cudaError_t e = dtype == 0 ? gn_backward<float>(a, ctas, st) : gn_backward<__nv_bfloat16>(a, ctas, st);
-        if (e != cudaSuccess) return e;
+        return gn_launch(gn_levels_kernel, gn_join_ctas(a), true, st, a, 0u);
     }
-    if (a.dweight || a.dbias) {
-        gn_join_kernel<<<dim3((a.channels + 31) / 32, a.shared ? 1 : a.workers, 2), GN_THREADS, 0, st>>>(a);
-        return cudaGetLastError();
-    }
-    return cudaSuccess;
+    gn_plan(a, dtype == 0 ? 4 : 8);
+    a.level = a.part + (int64_t)a.workers * a.samples * a.parts * 2 * a.channels;
+    if (dtype == 0) return a.whole ? gn_backward<float, true>(a, st) : gn_backward<float, false>(a, st);
+    return a.whole ? gn_backward<__nv_bfloat16, true>(a, st) : gn_backward<__nv_bfloat16, false>(a, st);
 }
 
 }  // namespace liec

@@ -138,7 +138,7 @@ __device__ __forceinline__ void gn_wait_phase(int q) {
 template <typename T>
 __device__ __forceinline__ void gn_fetch(const GnArgs &a, uint32_t place, const T *first, int64_t step, int c, int from, int end) {
     if (a.whole) {
-        const int bytes = min(16, max(0, (a.channels - c) * (int)sizeof(T)));
+        const int bytes = c < a.channels ? 16 : 0;
         const T *p = (bytes > 0 ? first + c : first) + from * step;
         for (int k = from; k < end; ++k, p += step) copy_async(place + k * (GR_THREADS * 16), p, bytes);
     } else {
@@ -287,22 +287,22 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_backward_kernel(con
     cluster_arrive();
     const T *dy = static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
     const int per = (a.turns + GN_PHASES - 1) / GN_PHASES, turns = at.turns;
-    const X x(a, at.worker, at.sample, at.p0);
+    const X x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
     const uint32_t dz_u32 = (uint32_t)__cvta_generic_to_shared(dz_place), x_u32 = (uint32_t)__cvta_generic_to_shared(x_place);
 #pragma unroll 1
     for (int q = 0; q < GN_PHASES; ++q) {
         const int end = min((q + 1) * per, turns);
         gn_fetch(a, dz_u32, dy, at.lanes * a.y_pixel, at.c, q * per, end);
         if constexpr (CHECKPOINT) {
-            const int64_t step = at.lanes * x.cols, power_step = step / CK_BLOCK;
-            const int8_t *from = x.q + at.c + q * per * step;
+            const int64_t step = x.step, power_step = step / CK_BLOCK;
+            const int8_t *from = x.q + q * per * step;
             for (int k = q * per; k < end; ++k, from += step)
                 asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(x_u32 + k * (GR_THREADS * M::X_BYTES)), "l"(from), "n"(M::X_BYTES) : "memory");
-            const uint8_t *power = x.scales + at.c / CK_BLOCK + q * per * power_step;
+            const uint8_t *power = x.scales + q * per * power_step;
 #pragma unroll 4
             for (int k = q * per; k < end; ++k) power_place[k * GR_THREADS] = __ldg(power + (k - q * per) * power_step);
         } else {
-            gn_fetch(a, x_u32, x.row, at.lanes * x.pixel, at.c, q * per, end);
+            gn_fetch(a, x_u32, x.row, x.step, at.c, q * per, end);
         }
         copy_commit();
     }
@@ -317,11 +317,11 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_backward_kernel(con
         gn_wait_phase(q);
 #pragma unroll 2
         for (int k = q * per; k < min((q + 1) * per, turns); ++k) {
-            const typename X::Raw raw = X::kept(x_place + k * GR_THREADS * M::X_BYTES, power_place + k * GR_THREADS);
+            const typename X::Kept raw = X::kept(x_place + k * GR_THREADS * M::X_BYTES, power_place + k * GR_THREADS);
             F2 d[P], g[P];
             X::centred(raw, ch.minus, d);
             LnChunk<T>::read(dz_place[k * GR_THREADS], g);
-            gn_slope<T, ACT, X>(a, at.worker, at.image, at.c, ch, raw, d, g, g);
+            gn_slope<T, ACT>(a, at.worker, at.image, at.c, ch, [&](F2 (&v)[P]) { const F2 none[P] = {}; X::centred(raw, none, v); }, d, g, g);
             if constexpr (WIDE) {
                 LnChunk<float>::write(dz_place + k * GR_THREADS, {g[0], g[1]});
                 LnChunk<float>::write(dz_place + plane + k * GR_THREADS, {g[2], g[3]});
@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_backward_kernel(con
     }
     T *dx = static_cast<T *>(a.dx) + at.worker * a.dx_worker + at.sample * a.dx_sample + at.p0 * a.dx_pixel;
     gn_store<T>(a, dx, at.lanes * a.dx_pixel, at.c, turns, [&](int k, F2 (&d)[P]) {
-        const typename X::Raw raw = X::kept(x_place + k * GR_THREADS * M::X_BYTES, power_place + k * GR_THREADS);
+        const typename X::Kept raw = X::kept(x_place + k * GR_THREADS * M::X_BYTES, power_place + k * GR_THREADS);
         F2 g[P];
         X::centred(raw, ch.minus, d);
         if constexpr (WIDE) {
@@ -432,7 +432,7 @@ struct GnResidentBackward {
     cudaStream_t st;
     template <int ACT>
     cudaError_t operator()() {
-        return a.x ? gn_resident_launch<gn_resident_backward_kernel<T, GnFromX<T>, ACT>>(a, smem, st)
+        return a.x ? gn_resident_launch<gn_resident_backward_kernel<T, GnFromX<T, true>, ACT>>(a, smem, st)
                    : gn_resident_launch<gn_resident_backward_kernel<T, GnFromCheckpoint<T>, ACT>>(a, smem, st);
     }
 };
@@ -453,6 +453,9 @@ static int gn_memory_bytes(bool backward, bool checkpoint, int act, int turns, i
 // room for three CTAs on an SM (forward; the backward pass has registers for two), then two, then one, so that the copies
 // of one hide behind the sums and stores of the others; more, down to two turns per thread, while SMs are idle.
 bool gn_resident_plan(GnArgs &a, int dtype, bool backward, bool checkpoint, int &smem) {
+#ifdef GN_STREAM
+    return false;
+#endif
     const int vec = dtype == 0 ? 4 : 8, group = a.channels / a.groups;
     int unit = group;
     while (unit % CK_BLOCK != 0) unit += group;
