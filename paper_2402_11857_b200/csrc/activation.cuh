@@ -95,14 +95,22 @@ __device__ __forceinline__ void ck_unpack(uint32_t w, F2 &a, F2 &b) {
     b = add(f2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443))), off);
 }
 
-// Largest magnitude of a chunk; NaN (as bits: larger than infinity) where there is one.
-__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-template <int P>
-__device__ __forceinline__ uint32_t chunk_top(const F2 (&x)[P]) {
-    uint32_t top = 0u;
-#pragma unroll
-    for (int k = 0; k < P; ++k) top = max(top, max(abs_bits(lo(x[k])), abs_bits(hi(x[k]))));
-    return top;
+// Largest magnitude of a chunk, as bits: those of magnitudes order like the numbers, NaN above infinity.  Bfloat16: two at
+// a time, the two halves apart until ck_top_bits.
+template <typename T>
+__device__ __forceinline__ uint32_t ck_larger(uint32_t a, uint32_t b) {
+    if constexpr (sizeof(T) == 4) return max(a, b);
+    else return __vmaxu2(a, b);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t ck_top(uint4 q) {
+    constexpr uint32_t MAGNITUDE = sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
+    return ck_larger<T>(ck_larger<T>(q.x & MAGNITUDE, q.y & MAGNITUDE), ck_larger<T>(q.z & MAGNITUDE, q.w & MAGNITUDE));
+}
+template <typename T>
+__device__ __forceinline__ uint32_t ck_top_bits(uint32_t top) {
+    if constexpr (sizeof(T) == 4) return top;
+    else return max(top & 0xffff0000u, top << 16);
 }
 
 }  // namespace liec

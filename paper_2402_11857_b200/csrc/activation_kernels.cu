@@ -15,15 +15,17 @@ __global__ void __launch_bounds__(CK_THREADS) ck_compress_kernel(const __grid_co
     const int64_t row = i / row_chunks;
     const int c = (int)(i - row * row_chunks) * VEC;
     const bool live = i < chunks;
-    F2 x[P] = {};
+    uint4 chunk = make_uint4(0u, 0u, 0u, 0u);
     if (live) {
         const int64_t w = row / a.rows;
-        LnChunk<T>::read(load_chunk(static_cast<const T *>(a.in) + w * a.x_worker + (row - w * a.rows) * a.x_row, c, a.cols), x);
+        chunk = load_chunk(static_cast<const T *>(a.in) + w * a.x_worker + (row - w * a.rows) * a.x_row, c, a.cols);
     }
-    uint32_t top = chunk_top(x);
+    uint32_t top = ck_top<T>(chunk);
 #pragma unroll
-    for (int m = LANES / 2; m >= 1; m >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
-    const uint32_t byte = ck_scale_byte(__uint_as_float(top));
+    for (int m = LANES / 2; m >= 1; m >>= 1) top = ck_larger<T>(top, __shfl_xor_sync(0xffffffffu, top, m));
+    const uint32_t byte = ck_scale_byte(__uint_as_float(ck_top_bits<T>(top)));
+    F2 x[P];
+    LnChunk<T>::read(chunk, x);
     if (!live) return;
     uint32_t words[P / 2];
     ck_bytes<P>(x, byte, words);

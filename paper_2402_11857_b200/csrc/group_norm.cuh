@@ -12,43 +12,48 @@ namespace liec {
 
 constexpr int GN_THREADS = 256;
 
-// A thread's chunks of one array: turn k is pixel k step rows further.  Raw is what a load leaves in registers, so that several
-// can be under way; rows off the 16-byte grid (not WHOLE) give two granules each, cut when they are used.
+// A thread's chunks of one array, walked pixel by pixel (`step` elements): load(u) is u turns ahead.  Raw is what a load leaves in
+// registers, so that several can be under way; rows off the 16-byte grid (not WHOLE) give two granules each, cut when
+// they are used.
 template <typename T, bool WHOLE>
 struct GnReader {
     static constexpr int VEC = Bits<T>::VEC;
     struct Pair { uint4 a, b; };
     struct One { uint4 a; };
     using Raw = std::conditional_t<WHOLE, One, Pair>;
-    const T *row;   // of the first turn
+    const T *row;   // this turn's chunk
     int64_t step;
     int c, cols;
-    __device__ __forceinline__ GnReader(const T *row, int64_t step, int c, int cols) : row(row), step(step), c(c), cols(cols) {}
-    __device__ __forceinline__ Raw load(int64_t k) const {
+    __device__ __forceinline__ GnReader(const T *first, int64_t step, int c, int cols) : row(first + c), step(step), c(c), cols(cols) {}
+    __device__ __forceinline__ void advance(int turns) { row += turns * step; }
+    __device__ __forceinline__ bool inside(const T *now, uint32_t &shift) const {   // two whole granules hold the chunk
+        shift = (uint32_t)reinterpret_cast<uintptr_t>(now) & 15u;
+        const int back = (int)shift / (int)sizeof(T);
+        return c >= back && c - back + 2 * VEC <= cols;
+    }
+    __device__ __forceinline__ Raw load(int u) const {
         Raw r;
-        const T *now = row + k * step;
+        const T *now = row + u * step;
         if constexpr (WHOLE) {   // (cols is a multiple of a chunk)
-            r.a = c < cols ? __ldg(reinterpret_cast<const uint4 *>(now + c)) : make_uint4(0u, 0u, 0u, 0u);
+            r.a = c < cols ? __ldg(reinterpret_cast<const uint4 *>(now)) : make_uint4(0u, 0u, 0u, 0u);
         } else {
-        const int back = (int)(reinterpret_cast<uintptr_t>(now + c) & 15u) / (int)sizeof(T);
-        if (c >= back && c - back + 2 * VEC <= cols) {
-            const uint4 *g = reinterpret_cast<const uint4 *>(now + c - back);
-            r.a = __ldg(g);
-            r.b = __ldg(g + 1);
-        } else {
-            r.a = c < cols ? load_chunk_edge(now + c, cols - c) : make_uint4(0u, 0u, 0u, 0u);
-        }
+            uint32_t shift;
+            if (inside(now, shift)) {
+                const uint4 *g = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(now) & ~uintptr_t(15));
+                r.a = __ldg(g);
+                r.b = __ldg(g + 1);
+            } else {
+                r.a = c < cols ? load_chunk_edge(now, cols - c) : make_uint4(0u, 0u, 0u, 0u);
+            }
         }
         return r;
     }
-    __device__ __forceinline__ void read(const Raw &r, int64_t k, F2 (&out)[VEC / 2]) const {
-        uint4 q = r.a;
+    __device__ __forceinline__ uint4 chunk(const Raw &r, int u) const {
         if constexpr (!WHOLE) {
-            const uint32_t shift = (uint32_t)reinterpret_cast<uintptr_t>(row + k * step + c) & 15u;
-            const int back = (int)shift / (int)sizeof(T);
-            if (c >= back && c - back + 2 * VEC <= cols) q = cut_granules<(int)sizeof(T)>(r.a, r.b, shift);
+            uint32_t shift;
+            if (inside(row + u * step, shift)) return cut_granules<(int)sizeof(T)>(r.a, r.b, shift);
         }
-        LnChunk<T>::read(q, out);
+        return r.a;
     }
 };
 
@@ -60,18 +65,13 @@ struct GnFromX : GnReader<T, WHOLE> {
     using Kept = uint4;
     __device__ __forceinline__ GnFromX(const GnArgs &a, int worker, int sample, int64_t p, int lanes, int c)
         : GnReader<T, WHOLE>(static_cast<const T *>(a.x) + worker * a.x_worker + sample * a.x_sample + p * a.x_pixel, lanes * a.x_pixel, c, a.channels) {}
+    __device__ __forceinline__ Kept keep(const Raw &r, int u) const { return this->chunk(r, u); }
     static __device__ __forceinline__ Kept kept(const char *place, const uint8_t *) { return *reinterpret_cast<const uint4 *>(place); }
     template <int P>
-    static __device__ __forceinline__ void centred(const Kept &raw, const F2 (&minus)[P], F2 (&d)[P]) {
-        LnChunk<T>::read(raw, d);
+    static __device__ __forceinline__ void centred(const Kept &chunk, const F2 (&minus)[P], F2 (&d)[P]) {
+        LnChunk<T>::read(chunk, d);
 #pragma unroll
         for (int k = 0; k < P; ++k) d[k] = add(d[k], minus[k]);
-    }
-    template <int P>
-    __device__ __forceinline__ void centred(const Raw &raw, int64_t k, const F2 (&minus)[P], F2 (&d)[P]) const {
-        this->read(raw, k, d);
-#pragma unroll
-        for (int j = 0; j < P; ++j) d[j] = add(d[j], minus[j]);
     }
 };
 
@@ -83,17 +83,20 @@ struct GnFromCheckpoint {
     using Kept = Raw;
     const int8_t *q;
     const uint8_t *scales;
-    int64_t cols, step;
+    int64_t step;
     __device__ __forceinline__ GnFromCheckpoint(const GnArgs &a, int worker, int sample, int64_t p, int lanes, int c) {
-        cols = (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK;
-        const int64_t row = ((int64_t)worker * a.samples + sample) * a.pixels + p;
+        const int64_t cols = (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK, row = ((int64_t)worker * a.samples + sample) * a.pixels + p;
         q = a.q + row * cols + c;
         scales = a.scales + row * (cols / CK_BLOCK) + c / CK_BLOCK;
-        step = lanes * cols;
+        step = lanes * (cols / CK_BLOCK);   // of the powers
     }
-    __device__ __forceinline__ Raw load(int64_t k) const {
+    __device__ __forceinline__ void advance(int turns) {
+        q += turns * (step * CK_BLOCK);
+        scales += turns * step;
+    }
+    __device__ __forceinline__ Raw load(int u) const {
         Raw r;
-        const int8_t *at = q + k * step;
+        const int8_t *at = q + u * (step * CK_BLOCK);
         if constexpr (VEC == 8) {
             const uint2 v = __ldg(reinterpret_cast<const uint2 *>(at));
             r.w[0] = v.x;
@@ -101,9 +104,10 @@ struct GnFromCheckpoint {
         } else {
             r.w[0] = __ldg(reinterpret_cast<const uint32_t *>(at));
         }
-        r.byte = __ldg(scales + k * (step / CK_BLOCK));
+        r.byte = __ldg(scales + u * step);
         return r;
     }
+    __device__ __forceinline__ Kept keep(const Raw &r, int) const { return r; }
     static __device__ __forceinline__ Kept kept(const char *place, const uint8_t *power) {
         Raw r;
         if constexpr (VEC == 8) {
@@ -124,24 +128,25 @@ struct GnFromCheckpoint {
 #pragma unroll
         for (int k = 0; k < P; ++k) d[k] = fma(d[k], power, minus[k]);   // (q 2^e is exact: one rounding)
     }
-    template <int P>
-    __device__ __forceinline__ void centred(const Raw &raw, int64_t, const F2 (&minus)[P], F2 (&d)[P]) const { centred(raw, minus, d); }
 };
 
-// use(k, raw) for all turns, the loads of N of them issued together.
-template <int N, typename L, typename U>
-__device__ __forceinline__ void gn_turns(int64_t turns, L &&load, U &&use) {
-    int64_t k = 0;
+// use(u, raw) for all turns, the loads of N of them issued together; advance(n) then walks n turns on.
+template <int N, typename L, typename U, typename A>
+__device__ __forceinline__ void gn_turns(int64_t turns, L &&load, U &&use, A &&advance) {
 #pragma unroll 1
-    for (; k + N <= turns; k += N) {
-        decltype(load(k)) raw[N];
+    for (; turns >= N; turns -= N) {
+        decltype(load(0)) raw[N];
 #pragma unroll
-        for (int u = 0; u < N; ++u) raw[u] = load(k + u);
+        for (int u = 0; u < N; ++u) raw[u] = load(u);
 #pragma unroll
-        for (int u = 0; u < N; ++u) use(k + u, raw[u]);
+        for (int u = 0; u < N; ++u) use(u, raw[u]);
+        advance(N);
     }
 #pragma unroll 1
-    for (; k < turns; ++k) use(k, load(k));
+    for (; turns > 0; --turns) {
+        use(0, load(0));
+        advance(1);
+    }
 }
 
 // SiLU of a pair.  Results in bfloat16 take the hardware's exponential and reciprocal as they are (relative errors of
@@ -268,26 +273,42 @@ __device__ __forceinline__ void gn_slope(const GnArgs &a, int worker, int64_t im
     }
 }
 
-// The bytes and powers of a chunk of x: the 4 or 8 threads of a block are neighbours in a warp and here together.
+// The checkpoint of a thread's chunks: the 4 or 8 threads of a block are neighbours in a warp and come here together.
 template <typename T>
-__device__ __forceinline__ void gn_compress(const GnArgs &a, const F2 (&x)[Bits<T>::VEC / 2], int64_t row, int c) {
-    constexpr int VEC = Bits<T>::VEC, P = VEC / 2, LANES = CK_BLOCK / VEC;
-    const int64_t cols = (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK;
-    uint32_t top = chunk_top(x);
-    const uint32_t mates = ((1u << LANES) - 1u) << (threadIdx.x & 31 & ~(LANES - 1));
+struct GnCompressor {
+    static constexpr int VEC = Bits<T>::VEC, P = VEC / 2, LANES = CK_BLOCK / VEC;
+    int8_t *q;
+    uint8_t *scales;
+    int64_t step;
+    uint32_t mates;
+    bool first;
+    __device__ __forceinline__ GnCompressor(const GnArgs &a, int64_t row, int lanes, int c) {
+        const int64_t cols = (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK;
+        q = a.q + row * cols + c;
+        scales = a.scales + row * (cols / CK_BLOCK) + c / CK_BLOCK;
+        step = lanes * (cols / CK_BLOCK);
+        mates = ((1u << LANES) - 1u) << (threadIdx.x & 31 & ~(LANES - 1));
+        first = c % CK_BLOCK == 0;
+    }
+    __device__ __forceinline__ void advance(int turns) {
+        q += turns * (step * CK_BLOCK);
+        scales += turns * step;
+    }
+    __device__ __forceinline__ void store(int u, uint4 chunk) const {
+        uint32_t top = ck_top<T>(chunk);
 #pragma unroll
-    for (int m = LANES / 2; m >= 1; m >>= 1) top = max(top, __shfl_xor_sync(mates, top, m));
-    const uint32_t byte = ck_scale_byte(__uint_as_float(top));
-    F2 v[P];
-#pragma unroll
-    for (int k = 0; k < P; ++k) v[k] = x[k];
-    uint32_t words[P / 2];
-    ck_bytes<P>(v, byte, words);
-    int8_t *q = a.q + row * cols + c;
-    if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(q) = make_uint2(words[0], words[1]);
-    else *reinterpret_cast<uint32_t *>(q) = words[0];
-    if (c % CK_BLOCK == 0) a.scales[(row * cols + c) / CK_BLOCK] = (uint8_t)byte;
-}
+        for (int m = LANES / 2; m >= 1; m >>= 1) top = ck_larger<T>(top, __shfl_xor_sync(mates, top, m));
+        const uint32_t byte = ck_scale_byte(__uint_as_float(ck_top_bits<T>(top)));
+        F2 v[P];
+        LnChunk<T>::read(chunk, v);
+        uint32_t words[P / 2];
+        ck_bytes<P>(v, byte, words);
+        int8_t *to = q + u * (step * CK_BLOCK);
+        if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(words[0], words[1]);
+        else *reinterpret_cast<uint32_t *>(to) = words[0];
+        if (first) scales[u * step] = (uint8_t)byte;
+    }
+};
 
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll

@@ -61,9 +61,9 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 4 : 3) gn_moments_kernel(c
     const GnPlace<VEC> at(a, false);
     F2 s[P] = {}, t[P] = {};
     if (at.turns > 0) {
-        const GnFromX<T, WHOLE> x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
+        GnFromX<T, WHOLE> x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
         F2 minus[P], d[P];
-        LnChunk<T>::read(at.c < a.channels ? load_chunk(x.row - at.lane * a.x_pixel, at.c, a.channels) : make_uint4(0u, 0u, 0u, 0u), d);
+        LnChunk<T>::read(at.c < a.channels ? load_chunk(x.row - at.c - at.lane * a.x_pixel, at.c, a.channels) : make_uint4(0u, 0u, 0u, 0u), d);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
             minus[k] = f2(-lo(d[k]), -hi(d[k]));
@@ -72,14 +72,14 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 4 : 3) gn_moments_kernel(c
                 origin[at.chunk * VEC + 2 * k + 1] = hi(d[k]);
             }
         }
-        gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int64_t k) { return x.load(k); }, [&](int64_t k, const typename GnFromX<T, WHOLE>::Raw &raw) {
-            x.centred(raw, k, minus, d);
+        gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int u) { return x.load(u); }, [&](int u, const typename GnFromX<T, WHOLE>::Raw &raw) {
+            x.centred(x.keep(raw, u), minus, d);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
                 s[j] = add(s[j], d[j]);
                 t[j] = fma(d[j], d[j], t[j]);
             }
-        });
+        }, [&](int n) { x.advance(n); });
     }
     gn_channel_sums<VEC>(at, a.tile_chunks, s, t, box);
     const int width = a.tile_chunks * VEC;
@@ -92,62 +92,76 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 4 : 3) gn_moments_kernel(c
     }
 }
 
-// Joins a group's channels and parts: a warp per group, binary64, in a fixed order.
+// f(image, group, lane) with LANES threads per group of an image.
+template <int LANES, typename F>
+__device__ __forceinline__ void gn_per_group(const GnArgs &a, F &&f) {
+    const int64_t g = ((int64_t)blockIdx.x * GN_THREADS + threadIdx.x) / LANES;
+    const uint32_t image = (uint32_t)(g / a.groups);
+    f(g < (int64_t)a.workers * a.samples * a.groups, image, (uint32_t)(g - (int64_t)image * a.groups), (uint32_t)threadIdx.x % LANES);
+}
+template <int LANES>
+__device__ __forceinline__ double gn_sum_lanes(double v) {
+#pragma unroll
+    for (int m = LANES / 2; m >= 1; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+    return v;
+}
+
+// Joins a group's channels and parts, in binary64 and in a fixed order.
+template <int LANES>
 __global__ void __launch_bounds__(GN_THREADS) gn_statistics_kernel(const __grid_constant__ GnArgs a) {
-    const int64_t g = ((int64_t)blockIdx.x * GN_THREADS + threadIdx.x) / 32, images = (int64_t)a.workers * a.samples;
     gn_wait_for_kernel_before();
-    if (g >= images * a.groups) return;
-    const int lane = threadIdx.x & 31, width = a.channels / a.groups, entries = width * a.parts;
-    const int64_t image = g / a.groups;
-    const float *part = a.part + image * a.parts * 2 * a.channels + (g - image * a.groups) * width;
-    const double n = (double)a.pixels * width;
-    double s = 0.0, t = 0.0;
-    for (int i = lane; i < entries; i += 32) {
-        const int q = i / width;
-        s += (double)min(a.part_pixels, a.pixels - q * a.part_pixels) * part[(int64_t)q * 2 * a.channels + i % width];
-    }
-    const double mean = warp_sum(s) / n;
-    for (int i = lane; i < entries; i += 32) {
-        const int q = i / width;
-        const float *at = part + (int64_t)q * 2 * a.channels + i % width;
-        const double off = (double)at[0] - mean;
-        t += (double)at[a.channels] + (double)min(a.part_pixels, a.pixels - q * a.part_pixels) * off * off;
-    }
-    const double var = warp_sum(t) / n;
-    if (lane == 0) {
-        a.mean[g] = (float)mean;
-        a.rstd[g] = (float)(1.0 / sqrt(var + (double)a.eps));
-    }
+    gn_per_group<LANES>(a, [&](bool live, uint32_t image, uint32_t group, uint32_t lane) {
+        const uint32_t width = (uint32_t)a.channels / (uint32_t)a.groups, entries = live ? width * a.parts : 0u;
+        const float *part = a.part + (int64_t)image * a.parts * 2 * a.channels + group * width;
+        const double n = (double)a.pixels * width;
+        auto each = [&](auto &&f) {   // channel's mean, squares around it, number of pixels
+            for (uint32_t i = lane; i < entries; i += LANES) {
+                const uint32_t q = i / width;
+                const float *at = part + (int64_t)q * 2 * a.channels + (i - q * width);
+                f((double)at[0], (double)at[a.channels], (double)min(a.part_pixels, a.pixels - q * a.part_pixels));
+            }
+        };
+        double s = 0.0, t = 0.0;
+        each([&](double mean, double, double count) { s += count * mean; });
+        const double mean = gn_sum_lanes<LANES>(s) / n;
+        each([&](double m, double squares, double count) { t += squares + count * (m - mean) * (m - mean); });
+        const double var = gn_sum_lanes<LANES>(t) / n;
+        if (live && lane == 0) {
+            a.mean[(int64_t)image * a.groups + group] = (float)mean;
+            a.rstd[(int64_t)image * a.groups + group] = 1.0f / sqrtf((float)var + a.eps);
+        }
+    });
 }
 
 template <typename T, bool WHOLE, int ACT, bool COMPRESS>
 __global__ void __launch_bounds__(GN_THREADS, 3) gn_apply_kernel(const __grid_constant__ GnArgs a) {
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
     const GnPlace<VEC> at(a, true);
-    const GnFromX<T, WHOLE> x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
+    GnFromX<T, WHOLE> x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
     T *y = static_cast<T *>(a.y) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
-    const int64_t row0 = at.image * a.pixels + at.p0, y_step = at.lanes * a.y_pixel;
+    const int64_t y_step = at.lanes * a.y_pixel;
+    GnCompressor<T> checkpoint(a, at.image * a.pixels + at.p0, at.lanes, at.c);
     gn_wait_for_kernel_before();
     if (at.turns == 0) return;
     GnChannels<P> ch;
     ch.read(a, at.worker, at.image, at.c);
-    gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int64_t k) { return x.load(k); }, [&](int64_t k, const typename GnFromX<T, WHOLE>::Raw &raw) {
+    gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int u) { return x.load(u); }, [&](int u, const typename GnFromX<T, WHOLE>::Raw &raw) {
+        const uint4 chunk = x.keep(raw, u);
+        if constexpr (COMPRESS) checkpoint.store(u, chunk);
         F2 d[P];
-        if constexpr (COMPRESS) {
-            x.read(raw, k, d);
-            gn_compress<T>(a, d, row0 + k * at.lanes, at.c);
-#pragma unroll
-            for (int j = 0; j < P; ++j) d[j] = add(d[j], ch.minus[j]);
-        } else {
-            x.centred(raw, k, ch.minus, d);
-        }
+        GnFromX<T, WHOLE>::centred(chunk, ch.minus, d);
 #pragma unroll
         for (int j = 0; j < P; ++j) d[j] = gn_act<T, ACT>(fma(d[j], ch.scale[j], ch.bias[j]));
+        T *to = y + u * y_step;
         if (a.whole_out) {
-            if (at.c < a.channels) LnChunk<T>::write(y + k * y_step + at.c, d);
+            if (at.c < a.channels) LnChunk<T>::write(to + at.c, d);
         } else {
-            store_chunk(y + k * y_step, at.c, a.channels, d);
+            store_chunk(to, at.c, a.channels, d);
         }
+    }, [&](int n) {
+        x.advance(n);
+        y += n * y_step;
+        if constexpr (COMPRESS) checkpoint.advance(n);
     });
 }
 
@@ -159,23 +173,24 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_slopes_kernel(const __grid_c
     const GnPlace<VEC> at(a, false);
     F2 s[P] = {}, t[P] = {};
     if (at.turns > 0) {
-        const X x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
-        const GnReader<T, WHOLE> dy(static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel, at.lanes * a.y_pixel, at.c,
+        X x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
+        GnReader<T, WHOLE> dy(static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel, at.lanes * a.y_pixel, at.c,
                                     a.channels);
         GnChannels<P> ch;
         ch.read(a, at.worker, at.image, at.c);
         struct Raw { typename X::Raw x; typename GnReader<T, WHOLE>::Raw dy; };
-        gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int64_t k) { return Raw{x.load(k), dy.load(k)}; }, [&](int64_t k, const Raw &raw) {
+        gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int u) { return Raw{x.load(u), dy.load(u)}; }, [&](int u, const Raw &raw) {
             F2 d[P], g[P];
-            x.centred(raw.x, k, ch.minus, d);
-            dy.read(raw.dy, k, g);
-            gn_slope<T, ACT>(a, at.worker, at.image, at.c, ch, [&](F2 (&v)[P]) { const F2 none[P] = {}; x.centred(raw.x, k, none, v); }, d, g, g);
+            const typename X::Kept kept = x.keep(raw.x, u);
+            X::centred(kept, ch.minus, d);
+            LnChunk<T>::read(dy.chunk(raw.dy, u), g);
+            gn_slope<T, ACT>(a, at.worker, at.image, at.c, ch, [&](F2 (&v)[P]) { const F2 none[P] = {}; X::centred(kept, none, v); }, d, g, g);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
                 s[j] = add(s[j], g[j]);
                 t[j] = fma(g[j], d[j], t[j]);
             }
-        });
+        }, [&](int n) { x.advance(n); dy.advance(n); });
     }
     gn_channel_sums<VEC>(at, a.tile_chunks, s, t, box);
     const int width = a.tile_chunks * VEC;
@@ -213,33 +228,34 @@ __device__ __forceinline__ void gn_join(const GnArgs &a, uint32_t block) {
 }
 
 // The first `level_ctas` CTAs: per group r mean(dz w) and r^2 mean(dz w xh).  The others: dw and db.
+template <int LANES>
 __global__ void __launch_bounds__(GN_THREADS) gn_levels_kernel(const __grid_constant__ GnArgs a, uint32_t level_ctas) {
     gn_wait_for_kernel_before();
     if (blockIdx.x >= level_ctas) {
         gn_join(a, blockIdx.x - level_ctas);
         return;
     }
-    const int64_t g = ((int64_t)blockIdx.x * GN_THREADS + threadIdx.x) / 32, images = (int64_t)a.workers * a.samples;
-    if (g >= images * a.groups) return;
-    const int lane = threadIdx.x & 31, width = a.channels / a.groups, entries = width * a.parts;
-    const int64_t image = g / a.groups;
-    const int c0 = (int)(g - image * a.groups) * width, worker = (int)(image / a.samples);
-    const float *part = a.part + image * a.parts * 2 * a.channels + c0;
-    double s = 0.0, t = 0.0;
-    for (int i = lane; i < entries; i += 32) {
-        const int q = i / width, c = i % width;
-        const double w = a.weight ? (double)a.weight[worker * a.weight_stride + c0 + c] : 1.0;
-        const float *at = part + (int64_t)q * 2 * a.channels + c;
-        s += w * at[0];
-        t += w * at[a.channels];
-    }
-    s = warp_sum(s);
-    t = warp_sum(t);
-    if (lane == 0) {
-        const double n = (double)a.pixels * width, r = (double)a.rstd[g];
-        a.level[2 * g] = (float)(-r * s / n);
-        a.level[2 * g + 1] = (float)(-r * r * t / n);
-    }
+    gn_per_group<LANES>(a, [&](bool live, uint32_t image, uint32_t group, uint32_t lane) {
+        const uint32_t width = (uint32_t)a.channels / (uint32_t)a.groups, entries = live ? width * a.parts : 0u, worker = image / (uint32_t)a.samples;
+        const float *part = a.part + (int64_t)image * a.parts * 2 * a.channels + group * width;
+        const float *weight = a.weight ? a.weight + worker * a.weight_stride + group * width : nullptr;
+        double s = 0.0, t = 0.0;
+        for (uint32_t i = lane; i < entries; i += LANES) {
+            const uint32_t q = i / width, c = i - q * width;
+            const double w = weight ? (double)weight[c] : 1.0;
+            const float *at = part + (int64_t)q * 2 * a.channels + c;
+            s += w * at[0];
+            t += w * at[a.channels];
+        }
+        s = gn_sum_lanes<LANES>(s);
+        t = gn_sum_lanes<LANES>(t);
+        if (live && lane == 0) {
+            const int64_t g = (int64_t)image * a.groups + group;
+            const double n = (double)a.pixels * width, r = (double)a.rstd[g];
+            a.level[2 * g] = (float)(-r * s / n);
+            a.level[2 * g + 1] = (float)(-r * r * t / n);
+        }
+    });
 }
 
 // dx = A dz - r mean(dz w) - d r^2 mean(dz w xh)
@@ -247,8 +263,8 @@ template <typename T, bool WHOLE, typename X, int ACT>
 __global__ void __launch_bounds__(GN_THREADS, 2) gn_dx_kernel(const __grid_constant__ GnArgs a) {
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
     const GnPlace<VEC> at(a, true);
-    const X x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
-    const GnReader<T, WHOLE> dy(static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel, at.lanes * a.y_pixel, at.c, a.channels);
+    X x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
+    GnReader<T, WHOLE> dy(static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel, at.lanes * a.y_pixel, at.c, a.channels);
     T *dx = static_cast<T *>(a.dx) + at.worker * a.dx_worker + at.sample * a.dx_sample + at.p0 * a.dx_pixel;
     const int64_t dx_step = at.lanes * a.dx_pixel;
     GnChannels<P> ch;
@@ -266,15 +282,20 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_dx_kernel(const __grid_const
         GnChannels<P>::set(along[k / 2], k % 2, in ? levels[2 * group.group + 1] : 0.0f);
     }
     struct Raw { typename X::Raw x; typename GnReader<T, WHOLE>::Raw dy; };
-    gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int64_t k) { return Raw{x.load(k), dy.load(k)}; }, [&](int64_t k, const Raw &raw) {
+    gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int u) { return Raw{x.load(u), dy.load(u)}; }, [&](int u, const Raw &raw) {
         F2 d[P], g[P];
-        x.centred(raw.x, k, ch.minus, d);
-        dy.read(raw.dy, k, g);
-        gn_slope<T, ACT>(a, at.worker, at.image, at.c, ch, [&](F2 (&v)[P]) { const F2 none[P] = {}; x.centred(raw.x, k, none, v); }, d, g, g);
+        const typename X::Kept kept = x.keep(raw.x, u);
+        X::centred(kept, ch.minus, d);
+        LnChunk<T>::read(dy.chunk(raw.dy, u), g);
+        gn_slope<T, ACT>(a, at.worker, at.image, at.c, ch, [&](F2 (&v)[P]) { const F2 none[P] = {}; X::centred(kept, none, v); }, d, g, g);
 #pragma unroll
         for (int j = 0; j < P; ++j) d[j] = fma(g[j], ch.scale[j], fma(d[j], along[j], level[j]));
-        if (a.whole_out) LnChunk<T>::write(dx + k * dx_step + at.c, d);
-        else store_chunk(dx + k * dx_step, at.c, a.channels, d);
+        if (a.whole_out) LnChunk<T>::write(dx + u * dx_step + at.c, d);
+        else store_chunk(dx + u * dx_step, at.c, a.channels, d);
+    }, [&](int n) {
+        x.advance(n);
+        dy.advance(n);
+        dx += n * dx_step;
     });
 }
 
@@ -338,7 +359,9 @@ static cudaError_t gn_launch(void (*kernel)(A...), int64_t ctas, bool after, cud
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-static int64_t gn_group_ctas(const GnArgs &a) { return ((int64_t)a.workers * a.samples * a.groups * 32 + GN_THREADS - 1) / GN_THREADS; }
+// A warp for groups of many channels and parts, eight threads for others.
+static int gn_group_lanes(const GnArgs &a) { return a.channels / a.groups * a.parts > 64 ? 32 : 8; }
+static int64_t gn_group_ctas(const GnArgs &a) { return ((int64_t)a.workers * a.samples * a.groups * gn_group_lanes(a) + GN_THREADS - 1) / GN_THREADS; }
 static int64_t gn_join_ctas(const GnArgs &a) { return a.dweight || a.dbias ? (int64_t)((a.channels + 31) / 32) * (a.shared ? 1 : a.workers) * 2 : 0; }
 
 template <typename T, bool WHOLE>
@@ -349,7 +372,7 @@ struct GnForwardLaunch {
     cudaError_t operator()() {
         const int64_t ctas = (int64_t)a.workers * a.samples * a.tiles * a.parts;
         cudaError_t e = gn_launch(gn_moments_kernel<T, WHOLE>, ctas, false, st, a);
-        if (e == cudaSuccess) e = gn_launch(gn_statistics_kernel, gn_group_ctas(a), true, st, a);
+        if (e == cudaSuccess) e = gn_launch(gn_group_lanes(a) == 8 ? gn_statistics_kernel<8> : gn_statistics_kernel<32>, gn_group_ctas(a), true, st, a);
         if (e != cudaSuccess) return e;
         return a.q ? gn_launch(gn_apply_kernel<T, WHOLE, ACT, true>, ctas, true, st, a) : gn_launch(gn_apply_kernel<T, WHOLE, ACT, false>, ctas, true, st, a);
     }
@@ -374,7 +397,7 @@ struct GnBackwardLaunch {
     cudaError_t operator()() {
         const int64_t ctas = (int64_t)a.workers * a.samples * a.tiles * a.parts, levels = a.dx ? gn_group_ctas(a) : 0;
         cudaError_t e = gn_launch(gn_slopes_kernel<T, WHOLE, X, ACT>, ctas, false, st, a);
-        if (e == cudaSuccess) e = gn_launch(gn_levels_kernel, levels + gn_join_ctas(a), true, st, a, (uint32_t)levels);
+        if (e == cudaSuccess) e = gn_launch(gn_group_lanes(a) == 8 ? gn_levels_kernel<8> : gn_levels_kernel<32>, levels + gn_join_ctas(a), true, st, a, (uint32_t)levels);
         if (e == cudaSuccess && a.dx) e = gn_launch(gn_dx_kernel<T, WHOLE, X, ACT>, ctas, true, st, a);
         return e;
     }
@@ -389,7 +412,7 @@ cudaError_t launch_group_norm_backward(GnArgs a, int dtype, cudaStream_t st) {
     int smem;
     if (a.samples == 0 || a.pixels == 0) {
         a.parts = 1;
-        return gn_launch(gn_levels_kernel, gn_join_ctas(a), false, st, a, 0u);
+        return gn_launch(gn_levels_kernel<8>, gn_join_ctas(a), false, st, a, 0u);
     }
     a.whole = gn_whole(a, dtype, a.dy, a.y_pixel, a.y_sample, a.y_worker) && (!a.x || gn_whole(a, dtype, a.x, a.x_pixel, a.x_sample, a.x_worker));
     a.whole_out = gn_whole(a, dtype, a.dx, a.dx_pixel, a.dx_sample, a.dx_worker);
@@ -397,7 +420,7 @@ cudaError_t launch_group_norm_backward(GnArgs a, int dtype, cudaStream_t st) {
         const cudaError_t e = gn_resident_backward(a, dtype, smem, st);
         if (e != cudaSuccess || gn_join_ctas(a) == 0) return e;
         a.parts = 1;   // (the cluster's parts are one by now)
-        return gn_launch(gn_levels_kernel, gn_join_ctas(a), true, st, a, 0u);
+        return gn_launch(gn_levels_kernel<8>, gn_join_ctas(a), true, st, a, 0u);
     }
     gn_plan(a, dtype == 0 ? 4 : 8);
     a.level = a.part + (int64_t)a.workers * a.samples * a.parts * 2 * a.channels;

@@ -262,10 +262,11 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_forward_kernel(cons
         r = sums[2 * (g - first_group) + 1];
     });
     T *y = static_cast<T *>(a.y) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
-    int64_t row = at.image * a.pixels + at.p0;
+    const GnCompressor<T> checkpoint(a, at.image * a.pixels + at.p0, at.lanes, at.c);
     gn_store<T>(a, y, at.lanes * a.y_pixel, at.c, turns, [&](int k, F2 (&d)[P]) {
-        LnChunk<T>::read(place[k * GR_THREADS], d);
-        if constexpr (COMPRESS) gn_compress<T>(a, d, row + (int64_t)k * at.lanes, at.c);
+        const uint4 chunk = place[k * GR_THREADS];
+        LnChunk<T>::read(chunk, d);
+        if constexpr (COMPRESS) checkpoint.store(k, chunk);
 #pragma unroll
         for (int j = 0; j < P; ++j) d[j] = gn_act<T, ACT>(fma(add(d[j], ch.minus[j]), ch.scale[j], ch.bias[j]));
     });
@@ -294,7 +295,7 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_backward_kernel(con
         const int end = min((q + 1) * per, turns);
         gn_fetch(a, dz_u32, dy, at.lanes * a.y_pixel, at.c, q * per, end);
         if constexpr (CHECKPOINT) {
-            const int64_t step = x.step, power_step = step / CK_BLOCK;
+            const int64_t power_step = x.step, step = power_step * CK_BLOCK;
             const int8_t *from = x.q + q * per * step;
             for (int k = q * per; k < end; ++k, from += step)
                 asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(x_u32 + k * (GR_THREADS * M::X_BYTES)), "l"(from), "n"(M::X_BYTES) : "memory");
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_backward_kernel(con
 #pragma unroll 4
             for (int k = q * per; k < end; ++k) power_place[k * GR_THREADS] = __ldg(power + (k - q * per) * power_step);
         } else {
-            gn_fetch(a, x_u32, x.row, x.step, at.c, q * per, end);
+            gn_fetch(a, x_u32, x.row - at.c, x.step, at.c, q * per, end);
         }
         copy_commit();
     }
