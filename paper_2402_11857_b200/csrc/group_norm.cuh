@@ -26,6 +26,7 @@ struct GnReader {
     int c, cols;
     __device__ __forceinline__ GnReader(const T *first, int64_t step, int c, int cols) : row(first + c), step(step), c(c), cols(cols) {}
     __device__ __forceinline__ void advance(int turns) { row += turns * step; }
+    __device__ __forceinline__ const void *place() const { return row; }
     __device__ __forceinline__ bool inside(const T *now, uint32_t &shift) const {   // two whole granules hold the chunk
         shift = (uint32_t)reinterpret_cast<uintptr_t>(now) & 15u;
         const int back = (int)shift / (int)sizeof(T);
@@ -66,6 +67,10 @@ struct GnFromX : GnReader<T, WHOLE> {
     __device__ __forceinline__ GnFromX(const GnArgs &a, int worker, int sample, int64_t p, int lanes, int c)
         : GnReader<T, WHOLE>(static_cast<const T *>(a.x) + worker * a.x_worker + sample * a.x_sample + p * a.x_pixel, lanes * a.x_pixel, c, a.channels) {}
     __device__ __forceinline__ Kept keep(const Raw &r, int u) const { return this->chunk(r, u); }
+    struct Ahead {};   // nothing but the chunk itself is needed of a later turn
+    __device__ __forceinline__ void announce(bool) const {}
+    __device__ __forceinline__ Ahead ahead(int, bool) const { return {}; }
+    static __device__ __forceinline__ Kept kept(uint4 chunk, Ahead) { return chunk; }
     static __device__ __forceinline__ Kept kept(const char *place, const uint8_t *) { return *reinterpret_cast<const uint4 *>(place); }
     template <int P>
     static __device__ __forceinline__ void centred(const Kept &chunk, const F2 (&minus)[P], F2 (&d)[P]) {
@@ -94,6 +99,7 @@ struct GnFromCheckpoint {
         q += turns * (step * CK_BLOCK);
         scales += turns * step;
     }
+    __device__ __forceinline__ const void *place() const { return q; }
     __device__ __forceinline__ Raw load(int u) const {
         Raw r;
         const int8_t *at = q + u * (step * CK_BLOCK);
@@ -108,6 +114,18 @@ struct GnFromCheckpoint {
         return r;
     }
     __device__ __forceinline__ Kept keep(const Raw &r, int) const { return r; }
+    using Ahead = uint32_t;   // the power
+    __device__ __forceinline__ void announce(bool live) const {   // (it is a byte among few: no copy of its own brings it)
+        if (live) asm volatile("prefetch.global.L2 [%0];" ::"l"(scales));
+    }
+    __device__ __forceinline__ Ahead ahead(int u, bool live) const { return live ? (uint32_t)__ldg(scales + u * step) : 127u; }
+    static __device__ __forceinline__ Kept kept(uint4 chunk, Ahead power) {
+        Raw r;
+        r.w[0] = chunk.x;
+        if constexpr (VEC == 8) r.w[1] = chunk.y;
+        r.byte = power;
+        return r;
+    }
     static __device__ __forceinline__ Kept kept(const char *place, const uint8_t *power) {
         Raw r;
         if constexpr (VEC == 8) {
@@ -146,6 +164,60 @@ __device__ __forceinline__ void gn_turns(int64_t turns, L &&load, U &&use, A &&a
     for (; turns > 0; --turns) {
         use(0, load(0));
         advance(1);
+    }
+}
+
+// ---- a thread's ring in shared memory: its chunks of the next turns on their way, at no cost of registers ----
+//
+// Two turns make a stage.  Only the thread that copies a chunk reads it again, so no barrier guards the ring.
+constexpr int GN_STAGES = 4;
+template <int BYTES>
+struct GnRing {
+    static constexpr int SIZE = GN_STAGES * 2 * GN_THREADS * BYTES;
+    uint32_t place;
+    __device__ __forceinline__ explicit GnRing(char *memory) : place((uint32_t)__cvta_generic_to_shared(memory) + threadIdx.x * BYTES) {}
+    __device__ __forceinline__ void copy(int slot, const void *from, bool live) const {
+        const uint32_t to = place + slot * (GN_THREADS * BYTES);
+        if (live) {
+            if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+        }
+    }
+    __device__ __forceinline__ uint4 read(int slot) const {
+        const uint32_t at = place + slot * (GN_THREADS * BYTES);
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (BYTES == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+        else if constexpr (BYTES == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+        else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v.x) : "r"(at) : "memory");
+        return v;
+    }
+};
+
+// copy(slot, live) for every turn in order, each a few stages before its use(slot, u, live), u = 0 or 1 within a stage;
+// after(2) ends a stage.
+template <typename C, typename U, typename A>
+__device__ __forceinline__ void gn_ring_turns(int64_t turns, C &&copy, U &&use, A &&after) {
+    int64_t ahead = 0;   // turns whose copies are under way
+#pragma unroll
+    for (int s = 0; s < GN_STAGES - 1; ++s) {
+        copy(2 * s, ahead < turns);
+        copy(2 * s + 1, ahead + 1 < turns);
+        ahead += 2;
+        copy_commit();
+    }
+    int now = 0, fill = 2 * (GN_STAGES - 1);
+#pragma unroll 1
+    for (int64_t k = 0; k < turns; k += 2) {
+        copy(fill, ahead < turns);
+        copy(fill + 1, ahead + 1 < turns);
+        ahead += 2;
+        copy_commit();
+        copy_wait<GN_STAGES - 1>();
+        use(now, 0, true);
+        use(now + 1, 1, k + 1 < turns);
+        after(2);
+        now = now == 2 * (GN_STAGES - 1) ? 0 : now + 2;
+        fill = fill == 2 * (GN_STAGES - 1) ? 0 : fill + 2;
     }
 }
 
@@ -251,25 +323,30 @@ __device__ __forceinline__ void gn_slope(const GnArgs &a, int worker, int64_t im
         for (int k = 0; k < P; ++k) dz[k] = mul(gn_silu_slope<T>(z[k]), dy[k]);
     }
     if constexpr (ACT == LIEC_ACT_RELU) {
-        uint32_t on = 0u, near = 0u;
         constexpr float NEAR = 9.5367431640625e-7f;
+        bool near = false;
+        F2 kept[P];   // (dz may be dy)
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-            on |= (lo(z[k]) > 0.0f ? 1u << 2 * k : 0u) | (hi(z[k]) > 0.0f ? 2u << 2 * k : 0u);
-            near |= (fabsf(lo(z[k])) <= NEAR * fabsf(lo(ch.bias[k])) ? 1u << 2 * k : 0u) | (fabsf(hi(z[k])) <= NEAR * fabsf(hi(ch.bias[k])) ? 2u << 2 * k : 0u);
+            const float l = lo(z[k]), h = hi(z[k]);
+            near |= fabsf(l) <= NEAR * fabsf(lo(ch.bias[k]));
+            near |= fabsf(h) <= NEAR * fabsf(hi(ch.bias[k]));
+            kept[k] = dy[k];
+            dz[k] = f2(l > 0.0f ? lo(dy[k]) : 0.0f, h > 0.0f ? hi(dy[k]) : 0.0f);
         }
-        if (near != 0u) {
+        if (near) {
             F2 x[P];
             exact(x);   // x itself
 #pragma unroll
-            for (int k = 0; k < 2 * P; ++k)
-                if ((near >> k & 1u) && c + k < a.channels) {
-                    const bool positive = gn_positive(a, worker, image, c + k, k % 2 ? hi(x[k / 2]) : lo(x[k / 2]));
-                    on = positive ? on | 1u << k : on & ~(1u << k);
-                }
-        }
+            for (int k = 0; k < P; ++k) {
+                float v[2] = {lo(dz[k]), hi(dz[k])};
+                const float each[2] = {lo(x[k]), hi(x[k])}, was[2] = {lo(kept[k]), hi(kept[k])}, at[2] = {lo(z[k]), hi(z[k])}, b[2] = {lo(ch.bias[k]), hi(ch.bias[k])};
 #pragma unroll
-        for (int k = 0; k < P; ++k) dz[k] = f2(on >> 2 * k & 1u ? lo(dy[k]) : 0.0f, on >> 2 * k & 2u ? hi(dy[k]) : 0.0f);
+                for (int e = 0; e < 2; ++e)
+                    if (fabsf(at[e]) <= NEAR * fabsf(b[e]) && c + 2 * k + e < a.channels) v[e] = gn_positive(a, worker, image, c + 2 * k + e, each[e]) ? was[e] : 0.0f;
+                dz[k] = f2(v[0], v[1]);
+            }
+        }
     }
 }
 

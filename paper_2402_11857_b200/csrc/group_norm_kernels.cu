@@ -56,6 +56,7 @@ __device__ __forceinline__ void gn_wait_for_kernel_before() { asm volatile("grid
 template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 4 : 3) gn_moments_kernel(const __grid_constant__ GnArgs a) {
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
+    extern __shared__ __align__(16) char gn_ring[];
     __shared__ __align__(16) float box[GN_THREADS * 2 * VEC];
     __shared__ float origin[GN_THREADS * VEC];
     const GnPlace<VEC> at(a, false);
@@ -72,14 +73,22 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 4 : 3) gn_moments_kernel(c
                 origin[at.chunk * VEC + 2 * k + 1] = hi(d[k]);
             }
         }
-        gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int u) { return x.load(u); }, [&](int u, const typename GnFromX<T, WHOLE>::Raw &raw) {
-            x.centred(x.keep(raw, u), minus, d);
+        auto take = [&](uint4 chunk) {
+            GnFromX<T, WHOLE>::centred(chunk, minus, d);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
                 s[j] = add(s[j], d[j]);
                 t[j] = fma(d[j], d[j], t[j]);
             }
-        }, [&](int n) { x.advance(n); });
+        };
+        if constexpr (WHOLE) {
+            const GnRing<16> ring(gn_ring);
+            const bool in = at.c < a.channels;
+            gn_ring_turns(at.turns, [&](int slot, bool live) { ring.copy(slot, x.row, live && in); x.advance(1); },
+                          [&](int slot, int, bool live) { if (live && in) take(ring.read(slot)); }, [](int) {});
+        } else {
+            gn_turns<2>(at.turns, [&](int u) { return x.load(u); }, [&](int u, const typename GnFromX<T, WHOLE>::Raw &raw) { take(x.keep(raw, u)); }, [&](int n) { x.advance(n); });
+        }
     }
     gn_channel_sums<VEC>(at, a.tile_chunks, s, t, box);
     const int width = a.tile_chunks * VEC;
@@ -136,6 +145,7 @@ __global__ void __launch_bounds__(GN_THREADS) gn_statistics_kernel(const __grid_
 template <typename T, bool WHOLE, int ACT, bool COMPRESS>
 __global__ void __launch_bounds__(GN_THREADS, 3) gn_apply_kernel(const __grid_constant__ GnArgs a) {
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
+    extern __shared__ __align__(16) char gn_ring[];
     const GnPlace<VEC> at(a, true);
     GnFromX<T, WHOLE> x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
     T *y = static_cast<T *>(a.y) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
@@ -145,8 +155,7 @@ __global__ void __launch_bounds__(GN_THREADS, 3) gn_apply_kernel(const __grid_co
     if (at.turns == 0) return;
     GnChannels<P> ch;
     ch.read(a, at.worker, at.image, at.c);
-    gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int u) { return x.load(u); }, [&](int u, const typename GnFromX<T, WHOLE>::Raw &raw) {
-        const uint4 chunk = x.keep(raw, u);
+    auto take = [&](uint4 chunk, int u) {
         if constexpr (COMPRESS) checkpoint.store(u, chunk);
         F2 d[P];
         GnFromX<T, WHOLE>::centred(chunk, ch.minus, d);
@@ -158,17 +167,67 @@ __global__ void __launch_bounds__(GN_THREADS, 3) gn_apply_kernel(const __grid_co
         } else {
             store_chunk(to, at.c, a.channels, d);
         }
-    }, [&](int n) {
-        x.advance(n);
+    };
+    auto advance = [&](int n) {
         y += n * y_step;
         if constexpr (COMPRESS) checkpoint.advance(n);
-    });
+    };
+    if constexpr (WHOLE) {
+        const GnRing<16> ring(gn_ring);
+        const bool in = at.c < a.channels;
+        gn_ring_turns(at.turns, [&](int slot, bool live) { ring.copy(slot, x.row, live && in); x.advance(1); },
+                      [&](int slot, int u, bool live) { if (live) take(in ? ring.read(slot) : make_uint4(0u, 0u, 0u, 0u), u); }, advance);
+    } else {
+        gn_turns<2>(at.turns, [&](int u) { return x.load(u); }, [&](int u, const typename GnFromX<T, WHOLE>::Raw &raw) { take(x.keep(raw, u), u); },
+                    [&](int n) { x.advance(n); advance(n); });
+    }
+}
+
+// take(x, chunk of dy, u) for all turns of a backward kernel, u of them before the next advance(n).
+template <typename T, bool WHOLE, typename X, typename F, typename A>
+__device__ __forceinline__ void gn_backward_turns(const GnArgs &a, const GnPlace<Bits<T>::VEC> &at, X &x, GnReader<T, WHOLE> &dy, char *memory, F &&take, A &&advance) {
+    if constexpr (WHOLE) {
+        if (at.c >= a.channels) return;
+        constexpr int X_BYTES = X::CHECKPOINT ? Bits<T>::VEC : 16;
+        const GnRing<16> dy_ring(memory);
+        const GnRing<X_BYTES> x_ring(memory + GnRing<16>::SIZE);
+        X later = x;   // where the copies are; x stays with the turns that are used
+        typename X::Ahead next[2] = {x.ahead(0, true), x.ahead(1, at.turns > 1)}, now[2];
+        int64_t left = at.turns;
+        gn_ring_turns(at.turns,
+                      [&](int slot, bool live) {
+                          dy_ring.copy(slot, dy.row, live);
+                          dy.advance(1);
+                          x_ring.copy(slot, later.place(), live);
+                          later.announce(live);
+                          later.advance(1);
+                      },
+                      [&](int slot, int u, bool live) {
+                          if (u == 0) {   // the powers of the next stage
+                              now[0] = next[0];
+                              now[1] = next[1];
+                              next[0] = x.ahead(2, left > 2);
+                              next[1] = x.ahead(3, left > 3);
+                          }
+                          if (live) take(X::kept(x_ring.read(slot), now[u]), dy_ring.read(slot), u);
+                      },
+                      [&](int n) {
+                          x.advance(n);
+                          left -= n;
+                          advance(n);
+                      });
+    } else {
+        struct Raw { typename X::Raw x; typename GnReader<T, WHOLE>::Raw dy; };
+        gn_turns<2>(at.turns, [&](int u) { return Raw{x.load(u), dy.load(u)}; }, [&](int u, const Raw &raw) { take(x.keep(raw.x, u), dy.chunk(raw.dy, u), u); },
+                    [&](int n) { x.advance(n); dy.advance(n); advance(n); });
+    }
 }
 
 // Backward: sums of dz and dz xh of every channel of a part.
 template <typename T, bool WHOLE, typename X, int ACT>
 __global__ void __launch_bounds__(GN_THREADS, 2) gn_slopes_kernel(const __grid_constant__ GnArgs a) {
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
+    extern __shared__ __align__(16) char gn_ring[];
     __shared__ __align__(16) float box[GN_THREADS * 2 * VEC];
     const GnPlace<VEC> at(a, false);
     F2 s[P] = {}, t[P] = {};
@@ -178,19 +237,18 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_slopes_kernel(const __grid_c
                                     a.channels);
         GnChannels<P> ch;
         ch.read(a, at.worker, at.image, at.c);
-        struct Raw { typename X::Raw x; typename GnReader<T, WHOLE>::Raw dy; };
-        gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int u) { return Raw{x.load(u), dy.load(u)}; }, [&](int u, const Raw &raw) {
+        auto take = [&](const typename X::Kept &kept, uint4 chunk) {
             F2 d[P], g[P];
-            const typename X::Kept kept = x.keep(raw.x, u);
             X::centred(kept, ch.minus, d);
-            LnChunk<T>::read(dy.chunk(raw.dy, u), g);
+            LnChunk<T>::read(chunk, g);
             gn_slope<T, ACT>(a, at.worker, at.image, at.c, ch, [&](F2 (&v)[P]) { const F2 none[P] = {}; X::centred(kept, none, v); }, d, g, g);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
                 s[j] = add(s[j], g[j]);
                 t[j] = fma(g[j], d[j], t[j]);
             }
-        }, [&](int n) { x.advance(n); dy.advance(n); });
+        };
+        gn_backward_turns<T, WHOLE>(a, at, x, dy, gn_ring, [&](const typename X::Kept &kept, uint4 chunk, int) { take(kept, chunk); }, [](int) {});
     }
     gn_channel_sums<VEC>(at, a.tile_chunks, s, t, box);
     const int width = a.tile_chunks * VEC;
@@ -262,6 +320,7 @@ __global__ void __launch_bounds__(GN_THREADS) gn_levels_kernel(const __grid_cons
 template <typename T, bool WHOLE, typename X, int ACT>
 __global__ void __launch_bounds__(GN_THREADS, 2) gn_dx_kernel(const __grid_constant__ GnArgs a) {
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
+    extern __shared__ __align__(16) char gn_ring[];
     const GnPlace<VEC> at(a, true);
     X x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
     GnReader<T, WHOLE> dy(static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel, at.lanes * a.y_pixel, at.c, a.channels);
@@ -281,22 +340,16 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_dx_kernel(const __grid_const
         GnChannels<P>::set(level[k / 2], k % 2, in ? levels[2 * group.group] : 0.0f);
         GnChannels<P>::set(along[k / 2], k % 2, in ? levels[2 * group.group + 1] : 0.0f);
     }
-    struct Raw { typename X::Raw x; typename GnReader<T, WHOLE>::Raw dy; };
-    gn_turns<WHOLE ? 4 : 2>(at.turns, [&](int u) { return Raw{x.load(u), dy.load(u)}; }, [&](int u, const Raw &raw) {
+    gn_backward_turns<T, WHOLE>(a, at, x, dy, gn_ring, [&](const typename X::Kept &kept, uint4 chunk, int u) {
         F2 d[P], g[P];
-        const typename X::Kept kept = x.keep(raw.x, u);
         X::centred(kept, ch.minus, d);
-        LnChunk<T>::read(dy.chunk(raw.dy, u), g);
+        LnChunk<T>::read(chunk, g);
         gn_slope<T, ACT>(a, at.worker, at.image, at.c, ch, [&](F2 (&v)[P]) { const F2 none[P] = {}; X::centred(kept, none, v); }, d, g, g);
 #pragma unroll
         for (int j = 0; j < P; ++j) d[j] = fma(g[j], ch.scale[j], fma(d[j], along[j], level[j]));
         if (a.whole_out) LnChunk<T>::write(dx + u * dx_step + at.c, d);
         else store_chunk(dx + u * dx_step, at.c, a.channels, d);
-    }, [&](int n) {
-        x.advance(n);
-        dy.advance(n);
-        dx += n * dx_step;
-    });
+    }, [&](int n) { dx += n * dx_step; });
 }
 
 // ---- launches --------------------------------------------------------------------------------------------
@@ -344,10 +397,17 @@ static bool gn_whole(const GnArgs &a, int dtype, const void *p, int64_t pixel, i
     return (bits & 15u) == 0;
 }
 
+template <auto KERNEL>
+static cudaError_t gn_allow(int memory) {
+    static std::atomic<uint64_t> allowed{0};
+    return ln_allow_smem(KERNEL, memory, allowed);
+}
+
 // after: starts while the kernel before ends, and waits for it where it needs it.
 template <typename... A>
-static cudaError_t gn_launch(void (*kernel)(A...), int64_t ctas, bool after, cudaStream_t st, A... args) {
+static cudaError_t gn_launch(void (*kernel)(A...), int64_t ctas, int memory, bool after, cudaStream_t st, A... args) {
     cudaLaunchConfig_t cfg = {};
+    cfg.dynamicSmemBytes = (size_t)memory;
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(GN_THREADS);
     cfg.stream = st;
@@ -370,11 +430,14 @@ struct GnForwardLaunch {
     cudaStream_t st;
     template <int ACT>
     cudaError_t operator()() {
+        constexpr int RING = WHOLE ? GnRing<16>::SIZE : 0;
+        constexpr auto moments = gn_moments_kernel<T, WHOLE>;
         const int64_t ctas = (int64_t)a.workers * a.samples * a.tiles * a.parts;
-        cudaError_t e = gn_launch(gn_moments_kernel<T, WHOLE>, ctas, false, st, a);
-        if (e == cudaSuccess) e = gn_launch(gn_group_lanes(a) == 8 ? gn_statistics_kernel<8> : gn_statistics_kernel<32>, gn_group_ctas(a), true, st, a);
+        cudaError_t e = gn_allow<moments>(RING + 40 * 1024);
+        if (e == cudaSuccess) e = gn_launch(moments, ctas, RING, false, st, a);
+        if (e == cudaSuccess) e = gn_launch(gn_group_lanes(a) == 8 ? gn_statistics_kernel<8> : gn_statistics_kernel<32>, gn_group_ctas(a), 0, true, st, a);
         if (e != cudaSuccess) return e;
-        return a.q ? gn_launch(gn_apply_kernel<T, WHOLE, ACT, true>, ctas, true, st, a) : gn_launch(gn_apply_kernel<T, WHOLE, ACT, false>, ctas, true, st, a);
+        return gn_launch(a.q ? gn_apply_kernel<T, WHOLE, ACT, true> : gn_apply_kernel<T, WHOLE, ACT, false>, ctas, RING, true, st, a);
     }
 };
 
@@ -395,10 +458,15 @@ struct GnBackwardLaunch {
     cudaStream_t st;
     template <int ACT>
     cudaError_t operator()() {
+        constexpr int RING = WHOLE ? GnRing<16>::SIZE + GnRing<X::CHECKPOINT ? Bits<T>::VEC : 16>::SIZE : 0;
+        constexpr auto slopes = gn_slopes_kernel<T, WHOLE, X, ACT>;
+        constexpr auto dx = gn_dx_kernel<T, WHOLE, X, ACT>;
         const int64_t ctas = (int64_t)a.workers * a.samples * a.tiles * a.parts, levels = a.dx ? gn_group_ctas(a) : 0;
-        cudaError_t e = gn_launch(gn_slopes_kernel<T, WHOLE, X, ACT>, ctas, false, st, a);
-        if (e == cudaSuccess) e = gn_launch(gn_group_lanes(a) == 8 ? gn_levels_kernel<8> : gn_levels_kernel<32>, levels + gn_join_ctas(a), true, st, a, (uint32_t)levels);
-        if (e == cudaSuccess && a.dx) e = gn_launch(gn_dx_kernel<T, WHOLE, X, ACT>, ctas, true, st, a);
+        cudaError_t e = gn_allow<slopes>(RING + 40 * 1024);
+        if (e == cudaSuccess) e = gn_allow<dx>(RING + 40 * 1024);
+        if (e == cudaSuccess) e = gn_launch(slopes, ctas, RING, false, st, a);
+        if (e == cudaSuccess) e = gn_launch(gn_group_lanes(a) == 8 ? gn_levels_kernel<8> : gn_levels_kernel<32>, levels + gn_join_ctas(a), 0, true, st, a, (uint32_t)levels);
+        if (e == cudaSuccess && a.dx) e = gn_launch(dx, ctas, RING, true, st, a);
         return e;
     }
 };
@@ -412,7 +480,7 @@ cudaError_t launch_group_norm_backward(GnArgs a, int dtype, cudaStream_t st) {
     int smem;
     if (a.samples == 0 || a.pixels == 0) {
         a.parts = 1;
-        return gn_launch(gn_levels_kernel<8>, gn_join_ctas(a), false, st, a, 0u);
+        return gn_launch(gn_levels_kernel<8>, gn_join_ctas(a), 0, false, st, a, 0u);
     }
     a.whole = gn_whole(a, dtype, a.dy, a.y_pixel, a.y_sample, a.y_worker) && (!a.x || gn_whole(a, dtype, a.x, a.x_pixel, a.x_sample, a.x_worker));
     a.whole_out = gn_whole(a, dtype, a.dx, a.dx_pixel, a.dx_sample, a.dx_worker);
@@ -420,7 +488,7 @@ cudaError_t launch_group_norm_backward(GnArgs a, int dtype, cudaStream_t st) {
         const cudaError_t e = gn_resident_backward(a, dtype, smem, st);
         if (e != cudaSuccess || gn_join_ctas(a) == 0) return e;
         a.parts = 1;   // (the cluster's parts are one by now)
-        return gn_launch(gn_levels_kernel<8>, gn_join_ctas(a), true, st, a, 0u);
+        return gn_launch(gn_levels_kernel<8>, gn_join_ctas(a), 0, true, st, a, 0u);
     }
     gn_plan(a, dtype == 0 ? 4 : 8);
     a.level = a.part + (int64_t)a.workers * a.samples * a.parts * 2 * a.channels;
