@@ -67,10 +67,12 @@ struct GnFromX : GnReader<T, WHOLE> {
     __device__ __forceinline__ GnFromX(const GnArgs &a, int worker, int sample, int64_t p, int lanes, int c)
         : GnReader<T, WHOLE>(static_cast<const T *>(a.x) + worker * a.x_worker + sample * a.x_sample + p * a.x_pixel, lanes * a.x_pixel, c, a.channels) {}
     __device__ __forceinline__ Kept keep(const Raw &r, int u) const { return this->chunk(r, u); }
-    struct Ahead {};   // nothing but the chunk itself is needed of a later turn
-    __device__ __forceinline__ void announce(bool) const {}
-    __device__ __forceinline__ Ahead ahead(int, bool) const { return {}; }
-    static __device__ __forceinline__ Kept kept(uint4 chunk, Ahead) { return chunk; }
+    struct Powers {};   // nothing but the chunk itself is needed
+    __device__ __forceinline__ Powers powers(int) const { return {}; }
+    static __device__ __forceinline__ void announce(const Powers &, int) {}
+    static __device__ __forceinline__ Kept kept(uint4 chunk, const Powers &, int) { return chunk; }
+    static __device__ __forceinline__ void walk(Powers &, int) {}
+    __device__ __forceinline__ void next() { this->row += this->step; }
     static __device__ __forceinline__ Kept kept(const char *place, const uint8_t *) { return *reinterpret_cast<const uint4 *>(place); }
     template <int P>
     static __device__ __forceinline__ void centred(const Kept &chunk, const F2 (&minus)[P], F2 (&d)[P]) {
@@ -114,17 +116,51 @@ struct GnFromCheckpoint {
         return r;
     }
     __device__ __forceinline__ Kept keep(const Raw &r, int) const { return r; }
-    using Ahead = uint32_t;   // the power
-    __device__ __forceinline__ void announce(bool live) const {   // (it is a byte among few: no copy of its own brings it)
-        if (live) asm volatile("prefetch.global.L2 [%0];" ::"l"(scales));
+    // A byte among few: no copy of its own brings it to the ring.  It is announced to the L2 cache when its chunk's copy
+    // starts and loaded one stage before it is used.
+    struct Powers {
+        const uint8_t *at;   // of the stage after the present one
+        int64_t step;
+        int left;            // turns from there on
+        uint32_t now[2], next[2];
+        __device__ __forceinline__ void load() {
+            next[0] = left > 0 ? (uint32_t)__ldg(at) : 127u;
+            next[1] = left > 1 ? (uint32_t)__ldg(at + step) : 127u;
+        }
+    };
+    __device__ __forceinline__ Powers powers(int turns) const {
+        Powers p{scales, step, turns, {}, {}};
+        p.load();
+        walk(p, 2);
+        return p;
     }
-    __device__ __forceinline__ Ahead ahead(int u, bool live) const { return live ? (uint32_t)__ldg(scales + u * step) : 127u; }
-    static __device__ __forceinline__ Kept kept(uint4 chunk, Ahead power) {
+    static __device__ __forceinline__ void walk(Powers &p, int n) {   // a stage on; single turns only at the end
+        if (n == 2) {
+            p.now[0] = p.next[0];
+            p.now[1] = p.next[1];
+            p.at += 2 * p.step;
+            p.left -= 2;
+            p.load();
+        } else {
+            p.now[0] = p.now[1];
+            p.now[1] = p.next[0];
+            p.next[0] = p.next[1];
+            p.at += p.step;
+            p.left -= 1;
+            p.next[1] = p.left > 1 ? (uint32_t)__ldg(p.at + p.step) : 127u;
+        }
+    }
+    __device__ __forceinline__ void announce(const Powers &, int) const { asm volatile("prefetch.global.L2 [%0];" ::"l"(scales)); }
+    static __device__ __forceinline__ Kept kept(uint4 chunk, const Powers &p, int u) {
         Raw r;
         r.w[0] = chunk.x;
         if constexpr (VEC == 8) r.w[1] = chunk.y;
-        r.byte = power;
+        r.byte = p.now[u];
         return r;
+    }
+    __device__ __forceinline__ void next() {
+        q += step * CK_BLOCK;
+        scales += step;
     }
     static __device__ __forceinline__ Kept kept(const char *place, const uint8_t *power) {
         Raw r;
@@ -176,15 +212,13 @@ struct GnRing {
     static constexpr int SIZE = GN_STAGES * 2 * GN_THREADS * BYTES;
     uint32_t place;
     __device__ __forceinline__ explicit GnRing(char *memory) : place((uint32_t)__cvta_generic_to_shared(memory) + threadIdx.x * BYTES) {}
-    __device__ __forceinline__ void copy(int slot, const void *from, bool live) const {
-        const uint32_t to = place + slot * (GN_THREADS * BYTES);
-        if (live) {
-            if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-            else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
-        }
+    __device__ __forceinline__ void copy(int at, const void *from) const {
+        const uint32_t to = place + at * BYTES;
+        if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
     }
-    __device__ __forceinline__ uint4 read(int slot) const {
-        const uint32_t at = place + slot * (GN_THREADS * BYTES);
+    __device__ __forceinline__ uint4 read(int turn) const {
+        const uint32_t at = place + turn * BYTES;
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
         if constexpr (BYTES == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
         else if constexpr (BYTES == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
@@ -193,31 +227,44 @@ struct GnRing {
     }
 };
 
-// copy(slot, live) for every turn in order, each a few stages before its use(slot, u, live), u = 0 or 1 within a stage;
-// after(2) ends a stage.
+// copy(place) for every turn in order, each a few stages before its use(place, u); place: bytes from the ring's start for chunks of one
+// byte, u = 0 or 1 within a stage; after(n) ends a stage of n turns.
 template <typename C, typename U, typename A>
-__device__ __forceinline__ void gn_ring_turns(int64_t turns, C &&copy, U &&use, A &&after) {
-    int64_t ahead = 0;   // turns whose copies are under way
+__device__ __forceinline__ void gn_ring_turns(int turns, C &&copy, U &&use, A &&after) {
+    constexpr int TURN = GN_THREADS, RING = 2 * GN_STAGES * TURN;
+    static_assert((RING & (RING - 1)) == 0, "places wrap by a mask");
+    int ahead = 0;   // turns whose copies are under way
 #pragma unroll
     for (int s = 0; s < GN_STAGES - 1; ++s) {
-        copy(2 * s, ahead < turns);
-        copy(2 * s + 1, ahead + 1 < turns);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (ahead + u < turns) copy((2 * s + u) * TURN);
         ahead += 2;
         copy_commit();
     }
-    int now = 0, fill = 2 * (GN_STAGES - 1);
+    int now = 0;
+    // while both turns of the stage to copy are there, so are those to use
 #pragma unroll 1
-    for (int64_t k = 0; k < turns; k += 2) {
-        copy(fill, ahead < turns);
-        copy(fill + 1, ahead + 1 < turns);
-        ahead += 2;
+    for (; ahead + 1 < turns; ahead += 2) {
+        const int fill = (now + 2 * (GN_STAGES - 1) * TURN) & (RING - 1);
+        copy(fill);
+        copy(fill + TURN);
         copy_commit();
         copy_wait<GN_STAGES - 1>();
-        use(now, 0, true);
-        use(now + 1, 1, k + 1 < turns);
+        use(now, 0);
+        use(now + TURN, 1);
         after(2);
-        now = now == 2 * (GN_STAGES - 1) ? 0 : now + 2;
-        fill = fill == 2 * (GN_STAGES - 1) ? 0 : fill + 2;
+        now = (now + 2 * TURN) & (RING - 1);
+    }
+    const int left = turns - (ahead - 2 * (GN_STAGES - 1));
+    if (ahead < turns) copy((now + 2 * (GN_STAGES - 1) * TURN) & (RING - 1));
+    copy_commit();
+    copy_wait<0>();
+#pragma unroll 1
+    for (int k = 0; k < left; ++k) {
+        use(now, 0);
+        after(1);
+        now = (now + TURN) & (RING - 1);
     }
 }
 

@@ -83,9 +83,7 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 4 : 3) gn_moments_kernel(c
         };
         if constexpr (WHOLE) {
             const GnRing<16> ring(gn_ring);
-            const bool in = at.c < a.channels;
-            gn_ring_turns(at.turns, [&](int slot, bool live) { ring.copy(slot, x.row, live && in); x.advance(1); },
-                          [&](int slot, int, bool live) { if (live && in) take(ring.read(slot)); }, [](int) {});
+            if (at.c < a.channels) gn_ring_turns((int)at.turns, [&](int place) { ring.copy(place, x.row); x.next(); }, [&](int place, int) { take(ring.read(place)); }, [](int) {});
         } else {
             gn_turns<2>(at.turns, [&](int u) { return x.load(u); }, [&](int u, const typename GnFromX<T, WHOLE>::Raw &raw) { take(x.keep(raw, u)); }, [&](int n) { x.advance(n); });
         }
@@ -175,8 +173,9 @@ __global__ void __launch_bounds__(GN_THREADS, 3) gn_apply_kernel(const __grid_co
     if constexpr (WHOLE) {
         const GnRing<16> ring(gn_ring);
         const bool in = at.c < a.channels;
-        gn_ring_turns(at.turns, [&](int slot, bool live) { ring.copy(slot, x.row, live && in); x.advance(1); },
-                      [&](int slot, int u, bool live) { if (live) take(in ? ring.read(slot) : make_uint4(0u, 0u, 0u, 0u), u); }, advance);
+        // (threads beyond the last channel have zeros for the blocks that they share)
+        gn_ring_turns((int)at.turns, [&](int place) { if (in) ring.copy(place, x.row); x.next(); },
+                      [&](int place, int u) { take(in ? ring.read(place) : make_uint4(0u, 0u, 0u, 0u), u); }, advance);
     } else {
         gn_turns<2>(at.turns, [&](int u) { return x.load(u); }, [&](int u, const typename GnFromX<T, WHOLE>::Raw &raw) { take(x.keep(raw, u), u); },
                     [&](int n) { x.advance(n); advance(n); });
@@ -191,29 +190,18 @@ __device__ __forceinline__ void gn_backward_turns(const GnArgs &a, const GnPlace
         constexpr int X_BYTES = X::CHECKPOINT ? Bits<T>::VEC : 16;
         const GnRing<16> dy_ring(memory);
         const GnRing<X_BYTES> x_ring(memory + GnRing<16>::SIZE);
-        X later = x;   // where the copies are; x stays with the turns that are used
-        typename X::Ahead next[2] = {x.ahead(0, true), x.ahead(1, at.turns > 1)}, now[2];
-        int64_t left = at.turns;
-        gn_ring_turns(at.turns,
-                      [&](int slot, bool live) {
-                          dy_ring.copy(slot, dy.row, live);
-                          dy.advance(1);
-                          x_ring.copy(slot, later.place(), live);
-                          later.announce(live);
-                          later.advance(1);
+        typename X::Powers powers = x.powers((int)at.turns);
+        gn_ring_turns((int)at.turns,
+                      [&](int place) {
+                          dy_ring.copy(place, dy.row);
+                          dy.row += dy.step;
+                          x_ring.copy(place, x.place());
+                          x.announce(powers, 0);
+                          x.next();
                       },
-                      [&](int slot, int u, bool live) {
-                          if (u == 0) {   // the powers of the next stage
-                              now[0] = next[0];
-                              now[1] = next[1];
-                              next[0] = x.ahead(2, left > 2);
-                              next[1] = x.ahead(3, left > 3);
-                          }
-                          if (live) take(X::kept(x_ring.read(slot), now[u]), dy_ring.read(slot), u);
-                      },
+                      [&](int place, int u) { take(X::kept(x_ring.read(place), powers, u), dy_ring.read(place), u); },
                       [&](int n) {
-                          x.advance(n);
-                          left -= n;
+                          X::walk(powers, n);
                           advance(n);
                       });
     } else {
