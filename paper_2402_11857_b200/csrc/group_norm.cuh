@@ -440,7 +440,7 @@ __device__ __forceinline__ double warp_sum(double v) {
     return v;
 }
 
-// Images that a cluster holds in shared memory (group_norm_resident.cu): sets the launch's sizes, or says no.
+// Images that CTAs hold in shared memory (group_norm_resident.cu): sets the launch's sizes, or says no.
 bool gn_resident_plan(GnArgs &a, int dtype, bool backward, bool checkpoint, int &smem);
 cudaError_t gn_resident_forward(const GnArgs &a, int dtype, int smem, cudaStream_t st);
 cudaError_t gn_resident_backward(const GnArgs &a, int dtype, int smem, cudaStream_t st);

@@ -343,8 +343,10 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_dx_kernel(const __grid_const
 // ---- launches --------------------------------------------------------------------------------------------
 
 // Threads of a CTA share the chunks of a tile, so that few images still give a thread 16 pixels or more; parts of an
-// image's pixels as there are places for CTAs (six on an SM), four times as many while a thread keeps 64 pixels.
-static void gn_plan(GnArgs &a, int vec) {
+// image's pixels as there are places for CTAs (forward four on an SM, backward two), twice as many while a thread keeps
+// 64 pixels (8 x 32 images of 56 x 56 x 64 backward with six on an SM: 117 us, two: 107; 4 of 256 x 256 x 128: 94 and 76).
+static void gn_plan(GnArgs &a, int vec, bool backward) {
+    const int places_per_sm = backward ? 2 : 4;
     const int chunks = (int)(ck_cols(a.channels) / vec), step = CK_BLOCK / vec;
     int64_t lanes = std::max<int64_t>(1, std::min<int64_t>(GN_THREADS / step, a.pixels / 16));
     a.tile_chunks = (int)std::min<int64_t>(chunks, std::max<int64_t>(std::min(chunks, 32), GN_THREADS / lanes / step * step));
@@ -352,14 +354,15 @@ static void gn_plan(GnArgs &a, int vec) {
     a.tile_chunks = ((chunks + a.tiles - 1) / a.tiles + step - 1) / step * step;
     lanes = GN_THREADS / a.tile_chunks;
     const int64_t places = (int64_t)a.workers * a.samples * a.tiles;
-    const int64_t few = std::min((LN_SMS * 6 + places - 1) / places, a.pixels / (lanes * 16)), many = std::min((LN_SMS * 24 + places - 1) / places, a.pixels / (lanes * 64));
+    const int64_t few = std::min((LN_SMS * places_per_sm + places - 1) / places, a.pixels / (lanes * 16));
+    const int64_t many = std::min((LN_SMS * 2 * places_per_sm + places - 1) / places, a.pixels / (lanes * 64));
     const int64_t parts = std::max<int64_t>(1, std::max(few, many));
     a.part_pixels = std::max<int64_t>(1, (a.pixels + parts - 1) / parts);
     a.parts = (int)std::max<int64_t>(1, (a.pixels + a.part_pixels - 1) / a.part_pixels);
 }
 
 static size_t gn_streamed_workspace(GnArgs a, int dtype, bool backward) {
-    gn_plan(a, dtype == 0 ? 4 : 8);
+    gn_plan(a, dtype == 0 ? 4 : 8, backward);
     const size_t images = (size_t)a.workers * a.samples;
     return sizeof(float) * (images * a.parts * 2 * a.channels + (backward ? images * a.groups * 2 : 0));
 }
@@ -435,7 +438,7 @@ cudaError_t launch_group_norm_forward(GnArgs a, int dtype, cudaStream_t st) {
     a.whole = gn_whole(a, dtype, a.x, a.x_pixel, a.x_sample, a.x_worker);
     a.whole_out = gn_whole(a, dtype, a.y, a.y_pixel, a.y_sample, a.y_worker);
     if (gn_resident_plan(a, dtype, false, false, smem)) return gn_resident_forward(a, dtype, smem, st);
-    gn_plan(a, dtype == 0 ? 4 : 8);
+    gn_plan(a, dtype == 0 ? 4 : 8, false);
     if (dtype == 0) return a.whole ? gn_for_act(a.act, GnForwardLaunch<float, true>{a, st}) : gn_for_act(a.act, GnForwardLaunch<float, false>{a, st});
     return a.whole ? gn_for_act(a.act, GnForwardLaunch<__nv_bfloat16, true>{a, st}) : gn_for_act(a.act, GnForwardLaunch<__nv_bfloat16, false>{a, st});
 }
@@ -475,10 +478,10 @@ cudaError_t launch_group_norm_backward(GnArgs a, int dtype, cudaStream_t st) {
     if (gn_resident_plan(a, dtype, true, !a.x, smem)) {
         const cudaError_t e = gn_resident_backward(a, dtype, smem, st);
         if (e != cudaSuccess || gn_join_ctas(a) == 0) return e;
-        a.parts = 1;   // (the cluster's parts are one by now)
+        a.parts = 1;
         return gn_launch(gn_levels_kernel<8>, gn_join_ctas(a), 0, true, st, a, 0u);
     }
-    gn_plan(a, dtype == 0 ? 4 : 8);
+    gn_plan(a, dtype == 0 ? 4 : 8, true);
     a.level = a.part + (int64_t)a.workers * a.samples * a.parts * 2 * a.channels;
     if (dtype == 0) return a.whole ? gn_backward<float, true>(a, st) : gn_backward<float, false>(a, st);
     return a.whole ? gn_backward<__nv_bfloat16, true>(a, st) : gn_backward<__nv_bfloat16, false>(a, st);

@@ -1,17 +1,14 @@
-// Group normalisation of images that a cluster of CTAs holds in shared memory: every element crosses HBM once each way,
-// in one launch (backward: a second one joins the images' gradients of weight and bias).
-//
-// A cluster takes the channels of some groups of one image, a CTA a part of the pixels.  Its threads copy their chunks
-// (16 bytes of a pixel's channels) into places that they alone read again, sum them per channel, and the sums of all
-// CTAs meet: each CTA hands its own to every other, and all add them in the same order.
+// Group normalisation of small images in one launch: a CTA holds some groups' channels of an image in shared memory, so
+// every element crosses HBM once each way (backward: a second launch joins the images' gradients of weight and bias).  Its
+// threads copy their chunks into places that they alone read again.
 #include "group_norm.cuh"
 
 namespace liec {
 
 constexpr int GR_THREADS = 128;   // few threads with many chunks each: what is done once per thread is as much as a dozen chunks cost
 
-// What lies in dynamic shared memory, in bytes: planes of chunks ([turn][thread]), the sums that meet ([rank][sum][channel]),
-// the CTA's own on their way there, and per channel and group what follows from them.
+// What lies in dynamic shared memory, in bytes: planes of chunks ([turn][thread]), the channels' two sums, those of the pixel
+// lanes on their way there, and per channel and group what follows from them.
 template <typename T, bool CHECKPOINT, int DZ_PLANES>
 struct GnMemory {
     static constexpr int VEC = Bits<T>::VEC, X_BYTES = CHECKPOINT ? VEC : 16;
@@ -19,23 +16,16 @@ struct GnMemory {
     __host__ __device__ static int powers(int turns) { return CHECKPOINT ? turns * GR_THREADS : 0; }
     __host__ __device__ static int dz_plane(int turns) { return turns * GR_THREADS * 16; }
     __host__ __device__ static int planes(int turns) { return x_plane(turns) + DZ_PLANES * dz_plane(turns) + powers(turns); }
-    __host__ __device__ static int total(int turns, int ranks, int width) {
-        return planes(turns) + ranks * 2 * width * 4 + GR_THREADS * VEC * 4 + 3 * width * 4;
-    }
+    __host__ __device__ static int total(int turns, int width) { return planes(turns) + 2 * width * 4 + GR_THREADS * VEC * 4 + 3 * width * 4; }
 };
-
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // Where this CTA and thread are.
 template <int VEC>
 struct GnSpot {
     int64_t image, p0;   // p0: the thread's first pixel
-    int worker, sample, rank, ranks, chunk, lane, lanes, c, c0, width, turns;   // turns: the thread's chunks
+    int worker, sample, chunk, lane, lanes, c, c0, width, turns;   // turns: the thread's chunks
     __device__ __forceinline__ GnSpot(const GnArgs &a) {
-        ranks = a.parts;
-        const uint32_t unit = blockIdx.x / (uint32_t)ranks, picture = unit / (uint32_t)a.tiles;
-        rank = (int)(blockIdx.x - unit * ranks);
+        const uint32_t picture = blockIdx.x / (uint32_t)a.tiles;
         image = picture;
         worker = (int)(picture / (uint32_t)a.samples);
         sample = (int)(picture - (uint32_t)worker * a.samples);
@@ -43,60 +33,51 @@ struct GnSpot {
         chunk = (int)threadIdx.x - lane * a.tile_chunks;
         lanes = (int)(GR_THREADS / (uint32_t)a.tile_chunks);
         width = a.tile_chunks * VEC;
-        c0 = (int)(unit - picture * a.tiles) * width;
+        c0 = (int)(blockIdx.x - picture * a.tiles) * width;
         c = c0 + chunk * VEC;
-        p0 = rank * a.part_pixels + lane;
-        const int64_t end = min((int64_t)(rank + 1) * a.part_pixels, a.pixels);
+        p0 = lane;
         const bool live = lane < lanes && c < (a.channels + CK_BLOCK - 1) / CK_BLOCK * CK_BLOCK;
-        turns = live && p0 < end ? ((int)(end - p0) + lanes - 1) / lanes : 0;
+        turns = live && lane < a.pixels ? ((int)a.pixels - lane + lanes - 1) / lanes : 0;
     }
     __device__ __forceinline__ int channels(const GnArgs &a) const { return min(width, a.channels - c0); }   // of the tile
 };
 
-// The channels' sums over the CTA's pixel lanes, handed to every CTA of the cluster: sums[rank][which][channel].
+// The channels' two sums over the pixel lanes: sums[which][channel], complete for all threads.
 template <int VEC>
-__device__ __forceinline__ void gn_hand_over(const GnSpot<VEC> &at, const F2 (&a)[VEC / 2], const F2 (&b)[VEC / 2], float *box, float *sums) {
+__device__ __forceinline__ void gn_add_lanes(const GnSpot<VEC> &at, const F2 (&a)[VEC / 2], const F2 (&b)[VEC / 2], float *box, float *sums) {
     const int width = at.width;
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
-    if (at.lane < at.lanes) {
+        if (at.lane < at.lanes) {
 #pragma unroll
-        for (int k = 0; k < VEC / 2; k += 2) {
-            const F2 v = which ? b[k] : a[k], w = which ? b[k + 1] : a[k + 1];
-            *reinterpret_cast<float4 *>(box + at.lane * width + at.chunk * VEC + 2 * k) = make_float4(lo(v), hi(v), lo(w), hi(w));
+            for (int k = 0; k < VEC / 2; k += 2) {
+                const F2 v = which ? b[k] : a[k], w = which ? b[k + 1] : a[k + 1];
+                *reinterpret_cast<float4 *>(box + at.lane * width + at.chunk * VEC + 2 * k) = make_float4(lo(v), hi(v), lo(w), hi(w));
+            }
         }
-    }
-    __syncthreads();
-    const uint32_t to = (uint32_t)__cvta_generic_to_shared(sums + (at.rank * 2 + which) * width);
-    auto hand = [&](int column, float s) {
-        for (int r = 0; r < at.ranks; ++r) {
-            uint32_t there;
-            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(to + column * 4), "r"(r));
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(s) : "memory");
-        }
-    };
-    if (2 * width > GR_THREADS) {   // a thread per channel, or several channels
-        for (int q = threadIdx.x; q < width; q += GR_THREADS) {
+        __syncthreads();
+        if (2 * width > GR_THREADS) {   // a thread per channel, or several channels
+            for (int q = threadIdx.x; q < width; q += GR_THREADS) {
+                float s = 0.0f;
+                for (int l = 0; l < at.lanes; ++l) s += box[l * width + q];
+                sums[which * width + q] = s;
+            }
+        } else {                        // several threads per channel, then one adds their sums
+            const uint32_t ways = GR_THREADS / (uint32_t)width, way = threadIdx.x / (uint32_t)width;
+            const int column = (int)(threadIdx.x - way * width);
             float s = 0.0f;
-            for (int l = 0; l < at.lanes; ++l) s += box[l * width + q];
-            hand(q, s);
-        }
-    } else {                        // several threads per channel, then one adds their sums
-        const uint32_t ways = GR_THREADS / (uint32_t)width, way = threadIdx.x / (uint32_t)width;
-        const int column = (int)(threadIdx.x - way * width);
-        float s = 0.0f;
-        if (way < ways)
+            if (way < ways)
 #pragma unroll 4
-            for (int l = way; l < at.lanes; l += ways) s += box[l * width + column];
-        __syncthreads();
-        if (way < ways && way > 0) box[way * width + column] = s;
-        __syncthreads();
-        if (way == 0) {
-            for (uint32_t w = 1; w < ways; ++w) s += box[w * width + column];
-            hand(column, s);
+                for (int l = way; l < at.lanes; l += ways) s += box[l * width + column];
+            __syncthreads();
+            if (way < ways && way > 0) box[way * width + column] = s;
+            __syncthreads();
+            if (way == 0) {
+                for (uint32_t w = 1; w < ways; ++w) s += box[w * width + column];
+                sums[which * width + column] = s;
+            }
         }
-    }
-    __syncthreads();   // the box is used again
+        __syncthreads();   // the box is used again
     }
 }
 
@@ -177,11 +158,10 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_forward_kernel(cons
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
     extern __shared__ __align__(16) char gn_memory[];
     const GnSpot<VEC> at(a);
-    float *sums = reinterpret_cast<float *>(gn_memory + M::planes(a.turns)), *box = sums + at.ranks * 2 * at.width;
+    float *sums = reinterpret_cast<float *>(gn_memory + M::planes(a.turns)), *box = sums + 2 * at.width;
     float *origin = box + GR_THREADS * VEC, *value = origin + at.width;
     const uint4 *place = reinterpret_cast<const uint4 *>(gn_memory) + threadIdx.x;
     const uint32_t place_u32 = (uint32_t)__cvta_generic_to_shared(place);
-    cluster_arrive();
     const T *image = static_cast<const T *>(a.x) + at.worker * a.x_worker + at.sample * a.x_sample, *x = image + at.p0 * a.x_pixel;
     const int per = (a.turns + GN_PHASES - 1) / GN_PHASES, turns = at.turns;
 #pragma unroll 1
@@ -218,19 +198,12 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_forward_kernel(cons
             }
         }
     }
-    cluster_wait();                                     // all CTAs of the cluster are there
-    gn_hand_over<VEC>(at, s, t, box, sums);
-    cluster_arrive();
-    cluster_wait();
+    gn_add_lanes<VEC>(at, s, t, box, sums);
     // every channel's mean (about the first pixel) and squares around it, then the groups'
     const int channels = at.channels(a), width = (int)((uint32_t)a.channels / (uint32_t)a.groups);
     const float pixels = (float)a.pixels;
     for (int q = threadIdx.x; q < channels; q += GR_THREADS) {
-        float v = 0.0f, w = 0.0f;
-        for (int r = 0; r < at.ranks; ++r) {
-            v += sums[r * 2 * at.width + q];
-            w += sums[(r * 2 + 1) * at.width + q];
-        }
+        const float v = sums[q], w = sums[at.width + q];
         const float m = v / pixels;
         box[q] = m;
         box[at.width + q] = fmaxf(__fmaf_rn(-v, m, w), 0.0f);
@@ -246,11 +219,9 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_forward_kernel(cons
                           if (width <= 16 || (threadIdx.x & 31) == 0) {
                               sums[2 * g] = m;
                               sums[2 * g + 1] = r;
-                              if (at.rank == 0) {
-                                  const int64_t to = at.image * a.groups + (int)((uint32_t)at.c0 / (uint32_t)width) + g;
-                                  a.mean[to] = m;
-                                  a.rstd[to] = r;
-                              }
+                              const int64_t to = at.image * a.groups + (int)((uint32_t)at.c0 / (uint32_t)width) + g;
+                              a.mean[to] = m;
+                              a.rstd[to] = r;
                           }
                       });
     __syncthreads();
@@ -284,8 +255,7 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_backward_kernel(con
     const int plane = a.turns * GR_THREADS;   // chunks of a plane
     char *x_place = gn_memory + M::dz_plane(a.turns) * (WIDE ? 2 : 1) + threadIdx.x * M::X_BYTES;
     uint8_t *power_place = reinterpret_cast<uint8_t *>(gn_memory) + M::dz_plane(a.turns) * (WIDE ? 2 : 1) + M::x_plane(a.turns) + threadIdx.x;
-    float *sums = reinterpret_cast<float *>(gn_memory + M::planes(a.turns)), *box = sums + at.ranks * 2 * at.width, *value = box + GR_THREADS * VEC;
-    cluster_arrive();
+    float *sums = reinterpret_cast<float *>(gn_memory + M::planes(a.turns)), *box = sums + 2 * at.width, *value = box + GR_THREADS * VEC;
     const T *dy = static_cast<const T *>(a.dy) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
     const int per = (a.turns + GN_PHASES - 1) / GN_PHASES, turns = at.turns;
     const X x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
@@ -336,25 +306,17 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_backward_kernel(con
             }
         }
     }
-    cluster_wait();
-    gn_hand_over<VEC>(at, s, t, box, sums);
-    cluster_arrive();
-    // (loaded while the sums cross)
+    // (loaded while the sums meet)
     const float my_rstd = (int)threadIdx.x < channels ? __ldg(rstd + (at.c0 + threadIdx.x) / (uint32_t)width) : 0.0f;
     const float my_weight = (int)threadIdx.x < channels && weight ? __ldg(weight + at.c0 + threadIdx.x) : 1.0f;
-    cluster_wait();
+    gn_add_lanes<VEC>(at, s, t, box, sums);
     for (int q = threadIdx.x; q < channels; q += GR_THREADS) {
-        float v = 0.0f, w = 0.0f;
-        for (int r = 0; r < at.ranks; ++r) {
-            v += sums[r * 2 * at.width + q];
-            w += sums[(r * 2 + 1) * at.width + q];
-        }
+        const float v = sums[q];
+        float w = sums[at.width + q];
         const bool mine = q == (int)threadIdx.x;
         w *= mine ? my_rstd : __ldg(rstd + (uint32_t)(at.c0 + q) / (uint32_t)width);
-        if (at.rank == 0) {   // the image's share of db and dw
-            a.part[at.image * 2 * a.channels + at.c0 + q] = v;
-            a.part[(at.image * 2 + 1) * a.channels + at.c0 + q] = w;
-        }
+        a.part[at.image * 2 * a.channels + at.c0 + q] = v;   // the image's share of db and dw
+        a.part[(at.image * 2 + 1) * a.channels + at.c0 + q] = w;
         const float by = mine || !weight ? my_weight : __ldg(weight + at.c0 + q);
         box[q] = v * by;
         box[at.width + q] = w * by;
@@ -399,17 +361,18 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_backward_kernel(con
 
 // ---- launches --------------------------------------------------------------------------------------------
 
-constexpr int GN_MAX_MEMORY = 224 * 1024;
-#ifndef GN_BUDGET
-#define GN_BUDGET 56 * 1024
-#endif
+constexpr int GN_MAX_MEMORY = 112 * 1024;
+// Beyond, reading twice is as fast or faster: its threads walk down many more pixels for what each does once (forward /
+// backward from the checkpoint, held and read twice: 32 images of 196 pixels x 128 bfloat16 12 / 18 and 18 / 25 us, 256 of
+// 64 x 256 16 / 27 and 18 / 27, 256 of 256 x 256 29 / 43 and 33 / 57; 256 of 196 x 1024 68 / 192 and 71 / 131).
+constexpr int64_t GN_RESIDENT_ELEMENTS = 1 << 24;
 
 template <auto KERNEL>
 static cudaError_t gn_resident_launch(const GnArgs &a, int smem, cudaStream_t st) {
     static std::atomic<uint64_t> allowed{0};
     const cudaError_t e = ln_allow_smem(KERNEL, GN_MAX_MEMORY, allowed);
     if (e != cudaSuccess) return e;
-    return ln_launch(KERNEL, a, (int64_t)a.workers * a.samples * a.tiles, a.parts, GR_THREADS, smem, st);
+    return ln_launch(KERNEL, a, (int64_t)a.workers * a.samples * a.tiles, 1, GR_THREADS, smem, st);
 }
 
 template <typename T>
@@ -442,59 +405,41 @@ cudaError_t gn_resident_backward(const GnArgs &a, int dtype, int smem, cudaStrea
 }
 
 template <typename T>
-static int gn_memory_bytes(bool backward, bool checkpoint, int act, int turns, int ranks, int width) {
-    if (!backward) return GnMemory<T, false, 0>::total(turns, ranks, width);
+static int gn_memory_bytes(bool backward, bool checkpoint, int act, int turns, int width) {
+    if (!backward) return GnMemory<T, false, 0>::total(turns, width);
     const bool wide = act == LIEC_ACT_SILU && sizeof(T) == 2;
-    if (checkpoint) return wide ? GnMemory<T, true, 2>::total(turns, ranks, width) : GnMemory<T, true, 1>::total(turns, ranks, width);
-    return wide ? GnMemory<T, false, 2>::total(turns, ranks, width) : GnMemory<T, false, 1>::total(turns, ranks, width);
+    if (checkpoint) return wide ? GnMemory<T, true, 2>::total(turns, width) : GnMemory<T, true, 1>::total(turns, width);
+    return wide ? GnMemory<T, false, 2>::total(turns, width) : GnMemory<T, false, 1>::total(turns, width);
 }
 
-// Channels per cluster: whole groups and whole blocks of a checkpoint, at least 128 bytes of a pixel (or all of it; 64
-// where more would not fit); more while an image is small and there are CTAs enough.  CTAs per cluster: as few as leave
-// room for three CTAs on an SM (forward; the backward pass has registers for two), then two, then one, so that the copies
-// of one hide behind the sums and stores of the others; more, down to two turns per thread, while SMs are idle.
+// Channels per CTA: whole groups and whole blocks of a checkpoint, at least 64 bytes of a pixel (or all of it); more, to 128
+// bytes and then to a thread per pixel and chunk, while there are CTAs enough.
 bool gn_resident_plan(GnArgs &a, int dtype, bool backward, bool checkpoint, int &smem) {
-#ifdef GN_STREAM
-    return false;
-#endif
     const int vec = dtype == 0 ? 4 : 8, group = a.channels / a.groups;
+    const int64_t images = (int64_t)a.workers * a.samples;
+    if (a.pixels > 4096 || images * a.pixels * a.channels > GN_RESIDENT_ELEMENTS) return false;
     int unit = group;
     while (unit % CK_BLOCK != 0) unit += group;
-    const int64_t images = (int64_t)a.workers * a.samples;
-    constexpr int MOST = 8;
-    auto fits = [&](int channels, int ranks, int budget) {
+    auto fits = [&](int channels) {
         const int chunks = (int)(ck_cols(channels) / vec);
         if (chunks > GR_THREADS / 2) return false;
         a.tile_chunks = chunks;
         a.tiles = (a.channels + channels - 1) / channels;
-        a.part_pixels = (a.pixels + ranks - 1) / ranks;
-        a.parts = ranks;
         const int lanes = GR_THREADS / chunks;
-        const int64_t turns = (a.part_pixels + lanes - 1) / lanes;
-        if (turns > 1024 || images * a.tiles * ranks >= (int64_t(1) << 31)) return false;
-        a.turns = (int)turns;
-        smem = dtype == 0 ? gn_memory_bytes<float>(backward, checkpoint, a.act, a.turns, ranks, chunks * vec)
-                          : gn_memory_bytes<__nv_bfloat16>(backward, checkpoint, a.act, a.turns, ranks, chunks * vec);
-        return smem <= budget;
+        a.turns = (int)((a.pixels + lanes - 1) / lanes);
+        smem = dtype == 0 ? gn_memory_bytes<float>(backward, checkpoint, a.act, a.turns, chunks * vec)
+                          : gn_memory_bytes<__nv_bfloat16>(backward, checkpoint, a.act, a.turns, chunks * vec);
+        return smem <= GN_MAX_MEMORY;
     };
-    auto at_least = [&](int bytes) {   // (a range that is doubled is still a multiple of the unit, or all channels)
-        int channels = std::min(unit, a.channels);
-        while (channels < a.channels && channels * (16 / vec) < bytes) channels = std::min(2 * channels, a.channels);
-        return channels;
-    };
-    int ranges[2] = {at_least(128), at_least(64)};
-    while (ranges[0] < a.channels && ranges[0] * 2 <= 32 * vec && a.pixels * ranges[0] <= 4 * GR_THREADS * vec &&
-           images * ((a.channels + ranges[0] - 1) / ranges[0]) > 4 * LN_SMS)
-        ranges[0] = std::min(2 * ranges[0], a.channels);
-    const int budgets[3] = {GN_BUDGET, 112 * 1024, GN_MAX_MEMORY};
-    for (int budget : budgets)
-        for (int channels : ranges)
-            for (int ranks = 1; ranks <= MOST && ranks <= a.pixels; ++ranks) {
-                if (!fits(channels, ranks, budget)) continue;
-                while (2 * ranks <= MOST && 2 * ranks <= a.pixels && images * a.tiles * ranks * 2 <= LN_SMS && a.turns > 2 && fits(channels, 2 * ranks, budget)) ranks *= 2;
-                return fits(channels, ranks, budget);
-            }
-    return false;
+    // (a range that is doubled is still a multiple of the unit, or all channels)
+    int channels = std::min(unit, a.channels);
+    while (channels < a.channels && channels * (16 / vec) < 64) channels = std::min(2 * channels, a.channels);
+    while (channels < a.channels) {
+        const int wider = std::min(2 * channels, a.channels);
+        if (images * ((a.channels + wider - 1) / wider) < 4 * LN_SMS || !fits(wider) || (a.turns > 16 && channels * (16 / vec) >= 128)) break;
+        channels = wider;
+    }
+    return fits(channels);
 }
 
 }  // namespace liec
