@@ -35,31 +35,70 @@ __global__ void __launch_bounds__(CK_THREADS) ck_compress_kernel(const __grid_co
     if (i % LANES == 0) a.scales[i / LANES] = (uint8_t)byte;
 }
 
+// A row's chunks, each with its neighbour in the warp: chunks off the 16-byte grid leave as granules, put together from the end
+// of the chunk before and the start of this one; what has no neighbour goes element by element.  Whole warps.  (Bfloat16, 32 x
+// 4096 rows of 767: 100 us, all element by element 225.  Binary32 has half the elements per chunk: 8 x 8192 rows of 1001
+// 108 us, element by element 90.)
+__device__ __forceinline__ void store_chunks(__nv_bfloat16 *row, int c, int cols, uint4 chunk, bool live) {
+    constexpr int VEC = 8, SIZE = 2;
+    const int lane = threadIdx.x & 31, shift = live ? (int)(reinterpret_cast<uintptr_t>(row + c) & 15u) : 0, head = (16 - shift) / SIZE;   // elements up to the next granule
+    uint4 before;
+    before.x = __shfl_up_sync(0xffffffffu, chunk.x, 1);
+    before.y = __shfl_up_sync(0xffffffffu, chunk.y, 1);
+    before.z = __shfl_up_sync(0xffffffffu, chunk.z, 1);
+    before.w = __shfl_up_sync(0xffffffffu, chunk.w, 1);
+    if (!live || c >= cols) return;
+    char *to = reinterpret_cast<char *>(row + c);
+    int first = 0, end = min(VEC, cols - c);   // elements that are left
+    if (shift == 0) {
+        if (end == VEC) {
+            *reinterpret_cast<uint4 *>(to) = chunk;
+            return;
+        }
+    } else {
+        if (lane > 0 && c > 0 && c + head <= cols) {
+            *reinterpret_cast<uint4 *>(to - shift) = cut_granules<SIZE>(before, chunk, (uint32_t)(16 - shift));
+            first = head;
+        }
+        if (lane < 31 && c + VEC + head <= cols) end = head;   // the next thread takes them
+    }
+    const uint32_t words[4] = {chunk.x, chunk.y, chunk.z, chunk.w};
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+        if (e >= first && e < end) reinterpret_cast<unsigned short *>(to)[e] = (unsigned short)(words[e / 2] >> (e % 2 * 16));
+}
+
+// Rows of any width and place.
 template <typename T>
 __global__ void __launch_bounds__(CK_THREADS) ck_restore_kernel(const __grid_constant__ CkArgs a, int64_t row_chunks, int64_t chunks) {
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2, LANES = CK_BLOCK / VEC;
     const int64_t i = (int64_t)blockIdx.x * CK_THREADS + threadIdx.x;
-    if (i >= chunks) return;
-    const int64_t row = i / row_chunks, w = row / a.rows;
+    const bool live = i < chunks;
+    const int64_t row = live ? i / row_chunks : 0, w = row / a.rows;
     const int c = (int)(i - row * row_chunks) * VEC;
-    if (c >= a.cols) return;
-    const F2 power = f2(ck_power(__ldg(a.scales + i / LANES)));
-    const int8_t *q = a.q + i * VEC;
-    F2 x[P];
-    if constexpr (VEC == 8) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(q));
-        ck_unpack(v.x, x[0], x[1]);
-        ck_unpack(v.y, x[2], x[3]);
-    } else {
-        ck_unpack(__ldg(reinterpret_cast<const uint32_t *>(q)), x[0], x[1]);
-    }
+    uint4 chunk = make_uint4(0u, 0u, 0u, 0u);
+    if (live) {
+        const F2 power = f2(ck_power(__ldg(a.scales + i / LANES)));
+        const int8_t *q = a.q + i * VEC;
+        F2 x[P];
+        if constexpr (VEC == 8) {
+            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(q));
+            ck_unpack(v.x, x[0], x[1]);
+            ck_unpack(v.y, x[2], x[3]);
+        } else {
+            ck_unpack(__ldg(reinterpret_cast<const uint32_t *>(q)), x[0], x[1]);
+        }
 #pragma unroll
-    for (int k = 0; k < P; ++k) x[k] = mul(x[k], power);
-    store_chunk(static_cast<T *>(a.x) + w * a.x_worker + (row - w * a.rows) * a.x_row, c, a.cols, x);
+        for (int k = 0; k < P; ++k) x[k] = mul(x[k], power);
+        if constexpr (VEC == 8) chunk = make_uint4(LnChunk<T>::word(x[0]), LnChunk<T>::word(x[1]), LnChunk<T>::word(x[2]), LnChunk<T>::word(x[3]));
+        else if (c < a.cols) store_chunk(static_cast<T *>(a.x) + w * a.x_worker + (row - w * a.rows) * a.x_row, c, a.cols, x);
+    }
+    if constexpr (VEC == 8) store_chunks(static_cast<T *>(a.x) + w * a.x_worker + (row - w * a.rows) * a.x_row, c, a.cols, chunk, live);
 }
 
 // Rows of whole blocks that start on 32 bytes: a thread takes a block, in 32-byte pieces, so that no threads have to meet and a
-// warp's powers are 32 bytes that lie together.  (32 x 4096 rows of 768 bfloat16 COMPARE)
+// warp's powers are 32 bytes that lie together.  HBM bounds it: 32 x 4096 rows of 768 bfloat16 51 us each way (6.0 TB/s; four
+// threads per block and 16-byte pieces: 71).
 struct Piece { uint32_t w[8]; };
 __device__ __forceinline__ Piece load_piece(const void *p) {
     Piece r;

@@ -109,7 +109,16 @@ __device__ __forceinline__ void gn_per_group(const GnArgs &a, F &&f) {
 template <int LANES>
 __device__ __forceinline__ double gn_sum_lanes(double v) {
 #pragma unroll
-    for (int m = LANES / 2; m >= 1; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+    for (int m = (LANES < 32 ? LANES : 32) / 2; m >= 1; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+    if constexpr (LANES == GN_THREADS) {   // a CTA
+        __shared__ double box[GN_THREADS / 32];
+        __syncthreads();
+        if (threadIdx.x % 32 == 0) box[threadIdx.x / 32] = v;
+        __syncthreads();
+        v = 0.0;
+#pragma unroll
+        for (int w = 0; w < GN_THREADS / 32; ++w) v += box[w];
+    }
     return v;
 }
 
@@ -122,6 +131,7 @@ __global__ void __launch_bounds__(GN_THREADS) gn_statistics_kernel(const __grid_
         const float *part = a.part + (int64_t)image * a.parts * 2 * a.channels + group * width;
         const double n = (double)a.pixels * width;
         auto each = [&](auto &&f) {   // channel's mean, squares around it, number of pixels
+#pragma unroll 4
             for (uint32_t i = lane; i < entries; i += LANES) {
                 const uint32_t q = i / width;
                 const float *at = part + (int64_t)q * 2 * a.channels + (i - q * width);
@@ -286,6 +296,7 @@ __global__ void __launch_bounds__(GN_THREADS) gn_levels_kernel(const __grid_cons
         const float *part = a.part + (int64_t)image * a.parts * 2 * a.channels + group * width;
         const float *weight = a.weight ? a.weight + worker * a.weight_stride + group * width : nullptr;
         double s = 0.0, t = 0.0;
+#pragma unroll 4
         for (uint32_t i = lane; i < entries; i += LANES) {
             const uint32_t q = i / width, c = i - q * width;
             const double w = weight ? (double)weight[c] : 1.0;
@@ -342,7 +353,7 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_dx_kernel(const __grid_const
 
 // ---- launches --------------------------------------------------------------------------------------------
 
-// Threads of a CTA share the chunks of a tile, so that few images still give a thread 16 pixels or more; parts of an
+// Threads of a CTA share the chunks of a tile, so that few images still give a thread 16 pixels or more (4 of a part); parts of an
 // image's pixels as there are places for CTAs (forward four on an SM, backward two), twice as many while a thread keeps
 // 64 pixels (8 x 32 images of 56 x 56 x 64 backward with six on an SM: 117 us, two: 107; 4 of 256 x 256 x 128: 94 and 76).
 static void gn_plan(GnArgs &a, int vec, bool backward) {
@@ -354,7 +365,7 @@ static void gn_plan(GnArgs &a, int vec, bool backward) {
     a.tile_chunks = ((chunks + a.tiles - 1) / a.tiles + step - 1) / step * step;
     lanes = GN_THREADS / a.tile_chunks;
     const int64_t places = (int64_t)a.workers * a.samples * a.tiles;
-    const int64_t few = std::min((LN_SMS * places_per_sm + places - 1) / places, a.pixels / (lanes * 16));
+    const int64_t few = std::min((LN_SMS * places_per_sm + places - 1) / places, a.pixels / (lanes * 4));
     const int64_t many = std::min((LN_SMS * 2 * places_per_sm + places - 1) / places, a.pixels / (lanes * 64));
     const int64_t parts = std::max<int64_t>(1, std::max(few, many));
     a.part_pixels = std::max<int64_t>(1, (a.pixels + parts - 1) / parts);
@@ -410,8 +421,14 @@ static cudaError_t gn_launch(void (*kernel)(A...), int64_t ctas, int memory, boo
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// A warp for groups of many channels and parts, eight threads for others.
-static int gn_group_lanes(const GnArgs &a) { return a.channels / a.groups * a.parts > 64 ? 32 : 8; }
+// Threads that join a group: eight, a warp where it has many channels and parts, a CTA where very many.
+static int gn_group_lanes(const GnArgs &a) {
+    const int64_t entries = (int64_t)(a.channels / a.groups) * a.parts;
+    return entries > 512 ? GN_THREADS : entries > 64 ? 32 : 8;
+}
+template <int LANES> using GnLanes = std::integral_constant<int, LANES>;
+template <typename F>
+static cudaError_t gn_for_lanes(int lanes, F &&f) { return lanes == 8 ? f(GnLanes<8>{}) : lanes == 32 ? f(GnLanes<32>{}) : f(GnLanes<GN_THREADS>{}); }
 static int64_t gn_group_ctas(const GnArgs &a) { return ((int64_t)a.workers * a.samples * a.groups * gn_group_lanes(a) + GN_THREADS - 1) / GN_THREADS; }
 static int64_t gn_join_ctas(const GnArgs &a) { return a.dweight || a.dbias ? (int64_t)((a.channels + 31) / 32) * (a.shared ? 1 : a.workers) * 2 : 0; }
 
@@ -426,7 +443,7 @@ struct GnForwardLaunch {
         const int64_t ctas = (int64_t)a.workers * a.samples * a.tiles * a.parts;
         cudaError_t e = gn_allow<moments>(RING + 40 * 1024);
         if (e == cudaSuccess) e = gn_launch(moments, ctas, RING, false, st, a);
-        if (e == cudaSuccess) e = gn_launch(gn_group_lanes(a) == 8 ? gn_statistics_kernel<8> : gn_statistics_kernel<32>, gn_group_ctas(a), 0, true, st, a);
+        if (e == cudaSuccess) e = gn_for_lanes(gn_group_lanes(a), [&](auto lanes) { return gn_launch(gn_statistics_kernel<decltype(lanes)::value>, gn_group_ctas(a), 0, true, st, a); });
         if (e != cudaSuccess) return e;
         return gn_launch(a.q ? gn_apply_kernel<T, WHOLE, ACT, true> : gn_apply_kernel<T, WHOLE, ACT, false>, ctas, RING, true, st, a);
     }
@@ -456,7 +473,8 @@ struct GnBackwardLaunch {
         cudaError_t e = gn_allow<slopes>(RING + 40 * 1024);
         if (e == cudaSuccess) e = gn_allow<dx>(RING + 40 * 1024);
         if (e == cudaSuccess) e = gn_launch(slopes, ctas, RING, false, st, a);
-        if (e == cudaSuccess) e = gn_launch(gn_group_lanes(a) == 8 ? gn_levels_kernel<8> : gn_levels_kernel<32>, levels + gn_join_ctas(a), 0, true, st, a, (uint32_t)levels);
+        if (e == cudaSuccess) 
+            e = gn_for_lanes(gn_group_lanes(a), [&](auto lanes) { return gn_launch(gn_levels_kernel<decltype(lanes)::value>, levels + gn_join_ctas(a), 0, true, st, a, (uint32_t)levels); });
         if (e == cudaSuccess && a.dx) e = gn_launch(dx, ctas, RING, true, st, a);
         return e;
     }
