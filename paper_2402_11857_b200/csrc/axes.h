@@ -64,8 +64,13 @@ inline bool meet(const Axes &a, const Axes &b) {
     const int64_t na = a.used > 2 ? a.n[2] : 1, nb = b.used > 2 ? b.n[2] : 1;
     if (na * nb > 1024) return false;
     for (int64_t i = 0; i < na; ++i)
-        for (int64_t j = 0; j < nb; ++j)
-            if (overlap(rows(a, i), rows(b, j))) return true;
+        for (int64_t j = 0; j < nb; ++j) {
+            const Rows x = rows(a, i), y = rows(b, j);
+            // (of unequal counts `overlap` can tell blocks only)
+            if ((x.rows == y.rows && x.groups == y.groups) || x.block() || y.block()) {
+                if (overlap(x, y)) return true;
+            }
+        }
     return false;
 }
 
