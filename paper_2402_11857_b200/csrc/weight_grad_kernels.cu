@@ -30,7 +30,8 @@ constexpr uint32_t WG_POLLS = 1u << 20;
 // one of the second per group.
 template <int PARTS_>
 struct WgShape {
-    static constexpr int PARTS = PARTS_, SLABS = PARTS == 1 ? 2 : 1, OUTPUTS = SLABS * WG_SLAB, COLUMNS = OUTPUTS;
+    static constexpr int PARTS = PARTS_, SLABS = PARTS == 1 ? 2 : 1, OUTPUTS = SLABS * WG_SLAB;
+    static constexpr int COLUMNS = 2 * WG_SLAB;   // two slabs; or one, and the products of the smaller parts of dy beside it
     static constexpr int B_BYTES = 2 * WG_BLOCK_BYTES;                       // of a slab's part
     static constexpr int STAGE_BYTES = SLABS * PARTS * B_BYTES + WG_RAW_BYTES;
     static constexpr int STAGES = PARTS == 1 ? 9 : 6;
@@ -112,6 +113,25 @@ __device__ __forceinline__ void wg_store_column(T *to, int64_t step, int outputs
         for (int e = 0; e < 32; ++e)
             if (e < outputs) wg_store(to + e * step, v[e]);
     }
+}
+
+// Adds 32 outputs to what this thread stored there; in its order, so equal calls give equal bits.
+__device__ __forceinline__ void wg_add_column(float *to, int64_t step, int outputs, const float (&v)[32]) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+        if (e < outputs) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(to + e * step), "f"(v[e]) : "memory");
+}
+
+// Stages of an item that one sum in tensor memory takes.  The products' additions there cut what does not fit: always
+// towards zero, which over 8192 tokens comes to 6e-6 of a gradient (measured), ten times what rounded additions lose.  So a
+// binary32 gradient is summed there 1792 tokens at a time at most, and these sums are added with rounding: 8e-7.  Each such
+// sum takes 10 us, 5 of them an SM's way out for its 256 KB: 8 x 8192 x 768 x 2304 takes 242 us (186 in one sum, 203 with 4096
+// tokens and 2.5e-6, 233 with 2048 and 1.2e-6).  A bfloat16 gradient keeps 2^-9 anyway, and is summed at once.
+constexpr int WG_SUM_STAGES = 56;
+__device__ __forceinline__ int wg_sum_stages(const WgArgs &a, int stages) {
+    if (a.grad_dtype != LIEC_F32 || stages <= WG_SUM_STAGES) return stages;
+    const int sums = (stages + WG_SUM_STAGES - 1) / WG_SUM_STAGES;
+    return (stages + sums - 1) / sums;
 }
 
 template <int PARTS>
@@ -199,15 +219,18 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
         if (rank == 0) {   // products
             bool ok = true;
             int it = 0;
-            for (int64_t item = pair, n = 0; ok && item < p.items; item += p.pairs, ++n) {
+            int64_t n = 0;   // sums so far
+            for (int64_t item = pair; ok && item < p.items; item += p.pairs) {
                 const WgItem g = p.item(item);
-                if (n > 0) ok = barrier_wait_warp(drained, (n - 1) & 1, WG_POLLS);
-                for (int i = 0; ok && i < g.stages; ++i, ++it) {
+                const int length = wg_sum_stages(a, g.stages);
+                for (int i = 0, in_sum = 0; ok && i < g.stages; ++i, ++it) {
                     const int s = it % S::STAGES, k4 = it % WG_GROUPS;
-                    ok = barrier_wait_warp(full(k4), (it / WG_GROUPS) & 1, WG_POLLS);
+                    if (in_sum == 0 && n > 0) ok = barrier_wait_warp(drained, (n - 1) & 1, WG_POLLS);
+                    ok = ok && barrier_wait_warp(full(k4), (it / WG_GROUPS) & 1, WG_POLLS);
                     if (!ok) break;
                     tc_after_sync();
                     const uint64_t x = tc_descriptor(a_at(k4), WG_BLOCK_BYTES), y = tc_descriptor(b_at(s), WG_BLOCK_BYTES);
+                    const bool last = ++in_sum == length || i + 1 == g.stages;
                     if (elected()) {
 #pragma unroll
                         for (int k = 0; k < WG_TOKENS / 16; ++k)
@@ -216,11 +239,16 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
                                 if (n < g.slabs)
 #pragma unroll
                                     for (int part = 0; part < PARTS; ++part)   // (the address field counts 16 bytes)
-                                        tc_mma_pair(tmem + n * WG_SLAB, x + (k * 2048 >> 4), y + (((n * PARTS + part) * S::B_BYTES + k * 2048) >> 4),
-                                                    tc_instruction(256, WG_SLAB), i > 0 || k > 0 || part > 0);
+                                        tc_mma_pair(tmem + (n + (part > 0)) * WG_SLAB, x + (k * 2048 >> 4), y + (((n * PARTS + part) * S::B_BYTES + k * 2048) >> 4),
+                                                    tc_instruction(256, WG_SLAB), in_sum > 1 || k > 0 || part > 1);
                         tc_commit_pair(empty(s));
+                        if (last) tc_commit_pair(done);
                     }
                     __syncwarp();
+                    if (last) {
+                        in_sum = 0;
+                        ++n;
+                    }
                 }
                 if (!ok && lane == 0) {
                     const uint32_t flag = (uint32_t)__cvta_generic_to_shared(&failed);
@@ -228,9 +256,9 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
                     asm volatile("fence.acq_rel.cluster;" ::: "memory");
                 }
                 __syncwarp();
-                if (elected()) tc_commit_pair(done);
-                __syncwarp();
             }
+            if (!ok && elected()) tc_commit_pair(done);   // nobody is to wait for its limit
+            __syncwarp();
         }
     } else if (warp < WG_WIDENERS / 32) {
         // A thread's part of a stage: two chunks of q, 16 channels of one token each.  Eight threads that load or store
@@ -240,84 +268,107 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
         const int64_t row_powers = (a.in + CK_BLOCK - 1) / CK_BLOCK;
         bool ok = true;
         int it0 = 0;   // stages before this tile's
-        for (int64_t item = pair, n = 0; item < p.items; item += p.pairs, ++n) {
+        int64_t n = 0;   // sums so far
+        for (int64_t item = pair; item < p.items; item += p.pairs) {
             const WgItem g = p.item(item);
-            const int c0 = first_channel(g), c = c0 + q_block * 64 + q_piece * 16;
-            const int64_t first = (int64_t)g.stage * WG_TOKENS;
-            const int left = c < row_powers * CK_BLOCK ? (int)min(a.rows - first, (int64_t)g.stages * WG_TOKENS) : 0;
-            const uint8_t *powers = a.scales + (g.worker * a.rows + first) * row_powers + c / CK_BLOCK;
-            auto fetch = [&](int i, uint32_t (&power)[2]) {   // i: stage of this tile
+            const int length = wg_sum_stages(a, g.stages);
+            for (int sum = 0, from = 0; sum < g.stages; sum += length, ++n) {
+                // A group widens one stage of the next sum before it takes this one, so that its products wait for that alone.
+                const int end = min(sum + length, g.stages), until = min(end + WG_GROUPS, g.stages);
+                const int c0 = first_channel(g), c = c0 + q_block * 64 + q_piece * 16;
+                const int64_t first = (int64_t)g.stage * WG_TOKENS;
+                const int left = c < row_powers * CK_BLOCK ? (int)min(a.rows - first, (int64_t)g.stages * WG_TOKENS) : 0;
+                const uint8_t *powers = a.scales + (g.worker * a.rows + first) * row_powers + c / CK_BLOCK;
+                auto fetch = [&](int i, uint32_t (&power)[2]) {   // i: stage of this tile
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int t = i * WG_TOKENS + token + j * 16;
-                    power[j] = t < left ? __ldg(powers + t * row_powers) : 127u;
+                    for (int j = 0; j < 2; ++j) {
+                        const int t = i * WG_TOKENS + token + j * 16;
+                        power[j] = t < left ? __ldg(powers + t * row_powers) : 127u;
+                    }
+                };
+                auto turn = [&](int i, uint32_t (&power)[2]) {
+                    const int s = (it0 + i) % S::STAGES;
+                    // The group's place is free when the products of its last turn, WG_GROUPS stages ago, are done.  This wait comes
+                    // first: a group does not see every phase of a stage's barriers, and a parity tells a phase from its
+                    // neighbours only.  After it all stages up to the last turn's are done, so both barriers are in the phase
+                    // that is waited for (STAGES >= WG_GROUPS; here the last turn's own wait vouches for 2 WG_GROUPS stages ago).
+                    const int before = it0 + i - WG_GROUPS;
+                    if (before >= 0 && !barrier_wait_warp(empty(before % S::STAGES), (before / S::STAGES) & 1, WG_POLLS)) return false;
+                    if (!barrier_wait_warp(loaded(s), ((it0 + i) / S::STAGES) & 1, WG_POLLS)) return false;
+                    const uint32_t to = a_at(group) + q_block * WG_BLOCK_BYTES, from = raw_at(s) + q_block * 64 + q_piece * 16 + token * 128;
+                    uint4 q[2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[j].x), "=r"(q[j].y), "=r"(q[j].z), "=r"(q[j].w) : "r"(from + j * 2048) : "memory");
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint4 x[2];
+                        wg_widen(q[j], power[j], x);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + tc_swizzled(token, q_piece * 2 + h) + j * 2048),
+                                         "r"(x[h].x), "r"(x[h].y), "r"(x[h].z), "r"(x[h].w) : "memory");
+                    }
+                    async_fence();
+                    __syncwarp();
+                    if (lane == 0) barrier_arrive_cluster(in_cta(full(group), 0));
+                    return true;
+                };
+                // the powers run two turns ahead
+                uint32_t even[2], odd[2];
+                const int begin = from + (group - (it0 + from) % WG_GROUPS + WG_GROUPS) % WG_GROUPS;
+                fetch(begin, even);
+                fetch(begin + WG_GROUPS, odd);
+                for (int i = begin; i < until && ok; i += 2 * WG_GROUPS) {
+                    ok = turn(i, even);
+                    fetch(i + 2 * WG_GROUPS, even);
+                    if (ok && i + WG_GROUPS < until) {
+                        ok = turn(i + WG_GROUPS, odd);
+                        fetch(i + 3 * WG_GROUPS, odd);
+                    }
                 }
-            };
-            auto turn = [&](int i, uint32_t (&power)[2]) {
-                const int s = (it0 + i) % S::STAGES;
-                // The group's place is free when the products of its last turn, WG_GROUPS stages ago, are done.  This wait comes
-                // first: a group does not see every phase of a stage's barriers, and a parity tells a phase from its
-                // neighbours only.  After it all stages up to the last turn's are done, so both barriers are in the phase
-                // that is waited for (STAGES >= WG_GROUPS; here the last turn's own wait vouches for 2 WG_GROUPS stages ago).
-                const int before = it0 + i - WG_GROUPS;
-                if (before >= 0 && !barrier_wait_warp(empty(before % S::STAGES), (before / S::STAGES) & 1, WG_POLLS)) return false;
-                if (!barrier_wait_warp(loaded(s), ((it0 + i) / S::STAGES) & 1, WG_POLLS)) return false;
-                const uint32_t to = a_at(group) + q_block * WG_BLOCK_BYTES, from = raw_at(s) + q_block * 64 + q_piece * 16 + token * 128;
-                uint4 q[2];
+                if (ok) ok = barrier_wait(done, n & 1, WG_POLLS);
+                if (!ok) failed = 1;
+                tc_after_sync();
+                asm volatile("bar.sync 1, %0;" ::"n"(WG_WIDENERS) : "memory");   // everyone's verdict
+                if (*reinterpret_cast<volatile int *>(&failed)) ok = false;
+                const int o0 = g.o_tile * S::OUTPUTS, mine = (warp % 4) * 32 + lane, ch = c0 + mine;
+                float *part = a.part + g.slot + rank * WG_CHANNELS + mine;
+                for (int col = group * 32; col < g.slabs * WG_SLAB && o0 + col < a.out; col += WG_GROUPS * 32) {
+                    float v[32];
+                    __syncwarp();
+                    tc_load(tmem + ((uint32_t)(warp % 4) << 21) + col, v);
+                    if constexpr (PARTS > 1) {
+                        float rest[32];
+                        tc_load(tmem + ((uint32_t)(warp % 4) << 21) + WG_SLAB + col, rest);
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[j].x), "=r"(q[j].y), "=r"(q[j].z), "=r"(q[j].w) : "r"(from + j * 2048) : "memory");
+                        for (int e = 0; e < 32; ++e) v[e] += rest[e];
+                    }
+                    if (!ok) {   // an unfinished sum is never taken for one (and stays NaN whatever is added)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    uint4 x[2];
-                    wg_widen(q[j], power[j], x);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + tc_swizzled(token, q_piece * 2 + h) + j * 2048),
-                                     "r"(x[h].x), "r"(x[h].y), "r"(x[h].z), "r"(x[h].w) : "memory");
+                        for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(0x7fffffffu);
+                    }
+                    const int o = o0 + col;
+                    float *to = nullptr;
+                    int64_t step = 2 * WG_CHANNELS;
+                    int outputs = 32;
+                    if (g.slot >= 0) {
+                        to = part + col * step;
+                    } else {
+                        if (ch >= a.in) continue;
+                        step = a.dw_row;
+                        outputs = a.out - o;
+                        if (a.grad_dtype == LIEC_F32) to = static_cast<float *>(a.dweight) + g.worker * a.dw_worker + o * step + ch;
+                    }
+                    if (!to) wg_store_column(static_cast<__nv_bfloat16 *>(a.dweight) + g.worker * a.dw_worker + o * step + ch, step, outputs, v);
+                    else if (sum == 0) wg_store_column(to, step, outputs, v);
+                    else wg_add_column(to, step, outputs, v);
                 }
-                async_fence();
+                tc_before_sync();
                 __syncwarp();
-                if (lane == 0) barrier_arrive_cluster(in_cta(full(group), 0));
-                return true;
-            };
-            // the powers run two turns ahead
-            uint32_t even[2], odd[2];
-            const int begin = (group - it0 % WG_GROUPS + WG_GROUPS) % WG_GROUPS;
-            fetch(begin, even);
-            fetch(begin + WG_GROUPS, odd);
-            for (int i = begin; i < g.stages && ok; i += 2 * WG_GROUPS) {
-                ok = turn(i, even);
-                fetch(i + 2 * WG_GROUPS, even);
-                if (ok && i + WG_GROUPS < g.stages) {
-                    ok = turn(i + WG_GROUPS, odd);
-                    fetch(i + 3 * WG_GROUPS, odd);
-                }
+                if (lane == 0 && (end < g.stages || item + p.pairs < p.items)) barrier_arrive_cluster(in_cta(drained, 0));   // the next sum's products wait for this
+                from = until;
             }
-            if (ok) ok = barrier_wait(done, n & 1, WG_POLLS);
-            if (!ok) failed = 1;
-            tc_after_sync();
-            asm volatile("bar.sync 1, %0;" ::"n"(WG_WIDENERS) : "memory");   // everyone's verdict
-            if (*reinterpret_cast<volatile int *>(&failed)) ok = false;
-            const int o0 = g.o_tile * S::OUTPUTS, mine = (warp % 4) * 32 + lane, ch = c0 + mine;
-            float *part = a.part + g.slot + rank * WG_CHANNELS + mine;
-            for (int col = group * 32; col < g.slabs * WG_SLAB && o0 + col < a.out; col += WG_GROUPS * 32) {
-                float v[32];
-                __syncwarp();
-                tc_load(tmem + ((uint32_t)(warp % 4) << 21) + col, v);
-                if (!ok) {   // an unfinished sum is never taken for one
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(0x7fffffffu);
-                }
-                const int o = o0 + col;
-                if (g.slot >= 0) wg_store_column(part + col * 2 * WG_CHANNELS, 2 * WG_CHANNELS, 32, v);
-                else if (ch >= a.in) continue;
-                else if (a.grad_dtype == LIEC_F32) wg_store_column(static_cast<float *>(a.dweight) + g.worker * a.dw_worker + o * a.dw_row + ch, a.dw_row, a.out - o, v);
-                else wg_store_column(static_cast<__nv_bfloat16 *>(a.dweight) + g.worker * a.dw_worker + o * a.dw_row + ch, a.dw_row, a.out - o, v);
-            }
-            tc_before_sync();
-            __syncwarp();
-            if (lane == 0 && item + p.pairs < p.items) barrier_arrive_cluster(in_cta(drained, 0));   // the next item's products wait for this
             it0 += g.stages;
         }
     }
