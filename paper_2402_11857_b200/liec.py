@@ -440,6 +440,12 @@ def _same_device(device, **tensors):
             raise ValueError(f"{name} must be on the device of the first argument")
 
 
+def _below_2_31(*sizes):
+    """Sizes of 32 bits in a descriptor: ctypes would cut them."""
+    if max(sizes) >= 1 << 31:
+        raise ValueError("workers, samples, channels and columns must be below 2^31")
+
+
 def _dtype_code(name, dtype) -> int:
     import torch
     if dtype == torch.bfloat16:
@@ -490,6 +496,7 @@ def _rows_of(name, layout):
     if any(s < 0 for _, s in axes):
         raise ValueError(f"{name} must not have negative strides")
     axes = [(1, 0)] * (2 - len(axes)) + axes
+    _below_2_31(cols)
     return axes[0][0], axes[1][0], cols, axes[1][1], axes[0][1]
 
 
@@ -576,6 +583,7 @@ def _gn_desc(x, given, y, dx, weight, bias, dweight, dbias, groups, activation, 
         raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
     if groups < 1 or shape[-1] % groups:
         raise ValueError("groups must divide the channels")
+    _below_2_31(shape[0], shape[-3], shape[-1])
     d = liec_group_norm_desc()
     d.workers, d.samples, d.pixels, d.channels = (shape[0] if len(shape) == 4 else 1), shape[-3], shape[-2], shape[-1]
     d.groups, d.dtype, d.activation, d.eps = groups, _dtype_code("x", x[2]), ACTIVATIONS[activation], eps
@@ -694,6 +702,7 @@ def _wg_desc(dy, dweight, cols, place):
         raise ValueError("the last axes of dy and dweight must be contiguous")
     if tuple(wshape) != tuple(shape[:-2]) + (shape[-1], cols):
         raise ValueError("dweight must be [N, out, in] ([out, in] for one worker)")
+    _below_2_31(N, shape[-1], cols)
     d.workers, d.rows, d.in_, d.out = N, shape[-2], cols, shape[-1]
     d.dtype, d.grad_dtype = _dtype_code("dy", dtype), _dtype_code("dweight", wdtype)
     d.dy_row_stride, d.dy_worker_stride = stride[-2], (stride[0] if len(shape) == 3 else 0)

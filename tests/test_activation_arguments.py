@@ -158,3 +158,24 @@ def test_weight_grad_pointers_and_workspace(lib):
     assert need(rows=0) == 0
     # runs of tokens never take more than a place for each of some 16 x 74 pieces of 256 x 512
     assert need(dtype=liec.BF16, rows=1 << 20, dy_worker_stride=24 << 20) <= 16 * 74 * 256 * 512 * 4
+
+
+def test_sizes_that_the_descriptor_cannot_hold(lib):
+    """Sizes beyond 32 bits are refused, not cut to what is left of them (broadcast tensors reach them without memory)."""
+    import torch
+    bf16, wide = torch.bfloat16, (1 << 32) + 2
+    f32 = torch.float32
+    vector = ((8,), (1,), f32)
+    for shape in ((wide, 1, 1, 8), (1, wide, 1, 8)):
+        images = (shape, (0, 0, 8, 1), bf16)
+        with pytest.raises(ValueError, match="2\\^31"):
+            liec._gn_desc(images, True, images, None, None, None, None, None, 4, "none", 1e-5)
+        with pytest.raises(ValueError, match="2\\^31"):
+            liec._gn_desc(images, True, images, images, None, None, vector, vector, 4, "none", 1e-5)
+    with pytest.raises(ValueError, match="2\\^31"):
+        liec._activation_desc("x", ((3, wide), (0, 1), bf16))
+    for dy, dweight, cols in ((((wide, 4, 8), (0, 8, 1), bf16), ((wide, 8, 8), (64, 8, 1), f32), 8),
+                              (((2, 4, wide), (0, 0, 1), bf16), ((2, wide, 8), (0, 8, 1), f32), 8),
+                              (((2, 4, 8), (32, 8, 1), bf16), ((2, 8, wide), (0, 0, 1), f32), wide)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            liec._wg_desc(dy, dweight, cols, 0)

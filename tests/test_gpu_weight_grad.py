@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from activation_helpers import DT, check_weight_grad, restored64
+from activation_helpers import DT, U, check_weight_grad, restored64
 from paper_2402_11857_b200 import liec
 
 pytestmark = pytest.mark.gpu
@@ -135,3 +135,16 @@ def test_copies_that_come_late():
     check_weight_grad(dy[:3], restored64(q[:3], scales[:3], 256), "f32", want[:3])
     for _ in range(10):
         assert torch.equal(weight_grad(dy, q, scales, 256), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_sums_keep_their_digits(dtype):
+    """Positive terms, so that sums grow evenly.  At most 112 additions (of 16 products each) to a sum in tensor memory, each
+    cutting less than 2 u of the part so far: 113 u in all, then a few rounded additions of u each; 120 u."""
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    dy = (torch.rand(80, 8192, 80, generator=gen, device="cuda") + 0.5).to(DT[dtype])
+    q, scales = liec.liec_activation_compress(torch.rand(80, 8192, 96, generator=gen, device="cuda") + 0.5)
+    got = weight_grad(dy, q, scales, 96)
+    for n in (0, 41, 79):
+        want = dy[n].double().t() @ restored64(q[n], scales[n], 96)
+        assert ((got[n].double() - want).abs() <= 120 * U * want).all()
