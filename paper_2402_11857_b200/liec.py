@@ -455,21 +455,29 @@ def _dtype_code(name, dtype) -> int:
     return F32
 
 
+@functools.lru_cache(maxsize=1024)
+def _checkpoint_shapes(rows, cols):
+    wide, rows = liec_activation_cols(cols), tuple(rows)
+    return rows + (wide,), rows + (wide // ACTIVATION_BLOCK,)
+
+
 def _check_checkpoint(q, scales, rows, cols):
     """q int8 [*rows, liec_activation_cols(cols)] and scales uint8 [*rows, the same / 32], both contiguous."""
     import torch
-    wide, rows = liec_activation_cols(cols), tuple(rows)
-    if q.dtype != torch.int8 or tuple(q.shape) != rows + (wide,) or not q.is_contiguous():
-        raise ValueError(f"q must be a contiguous int8 tensor {list(rows + (wide,))}")
-    if scales.dtype != torch.uint8 or tuple(scales.shape) != rows + (wide // ACTIVATION_BLOCK,) or not scales.is_contiguous():
-        raise ValueError(f"scales must be a contiguous uint8 tensor {list(rows + (wide // ACTIVATION_BLOCK,))}")
+    wide, powers = _checkpoint_shapes(rows, cols)
+    if q.shape != wide or q.dtype != torch.int8 or not q.is_contiguous():
+        raise ValueError(f"q must be a contiguous int8 tensor {list(wide)}")
+    if scales.shape != powers or scales.dtype != torch.uint8 or not scales.is_contiguous():
+        raise ValueError(f"scales must be a contiguous uint8 tensor {list(powers)}")
 
 
 def _new_checkpoint(rows, cols, q, scales, device):
     import torch
-    wide, rows = liec_activation_cols(cols), tuple(rows)
-    q = _empty(rows + (wide,), torch.int8, device) if q is None else q
-    scales = _empty(rows + (wide // ACTIVATION_BLOCK,), torch.uint8, device) if scales is None else scales
+    wide, powers = _checkpoint_shapes(rows, cols)
+    if q is None and scales is None:
+        return _empty(wide, torch.int8, device), _empty(powers, torch.uint8, device)
+    q = _empty(wide, torch.int8, device) if q is None else q
+    scales = _empty(powers, torch.uint8, device) if scales is None else scales
     _check_checkpoint(q, scales, rows, cols)
     return q, scales
 
