@@ -387,35 +387,41 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
     if (warp == WG_WIDENERS / 32 + 1) tc_free_pair(tmem, S::COLUMNS);
 }
 
-// A cut tile's runs, added in their order and rounded once to the gradient's type.  Block (x, y) has 16 outputs of cut tile y.
-constexpr int WG_JOIN_OUTPUTS = 16;
+// A cut tile's runs, added in their order and rounded once to the gradient's type.  Block (x, y) has 4 outputs of cut tile y,
+// a thread 4 channels of one: many threads with eight loads under way each (16 outputs per block, four loads: 13 us for six
+// tiles in 11 and 5 runs, now 7).
+constexpr int WG_JOIN_OUTPUTS = 4;
 __global__ void __launch_bounds__(256) wg_join_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ WgPlan p) {
     const int64_t cut = p.runs > 1 ? p.full - p.whole : 0;
     const bool is_last = blockIdx.y >= cut;
     const int64_t index = is_last ? blockIdx.y - cut : blockIdx.y, tiles = is_last ? p.last : cut, size = p.slot_size(is_last);
     const WgItem t = p.tile_of((is_last ? p.full : p.whole) + index);
     const int runs = is_last ? p.last_runs : p.runs, lane = threadIdx.x % 64, c = t.c_tile * 2 * WG_CHANNELS + lane * 4;
-    const float *from = a.part + index * size + (is_last ? cut * p.runs * p.slot_size(false) : 0) + lane * 4;
+    const int row = blockIdx.x * WG_JOIN_OUTPUTS + threadIdx.x / 64, o = t.o_tile * p.slabs * WG_SLAB + row;
+    const float4 *from = reinterpret_cast<const float4 *>(a.part + index * size + (is_last ? cut * p.runs * p.slot_size(false) : 0) + row * 2 * WG_CHANNELS + lane * 4);
+    const int64_t step = tiles * size / 4;
     asm volatile("griddepcontrol.wait;" ::: "memory");   // the sums are complete
-    for (int y = threadIdx.x / 64; y < WG_JOIN_OUTPUTS; y += 4) {
-        const int row = blockIdx.x * WG_JOIN_OUTPUTS + y, o = t.o_tile * p.slabs * WG_SLAB + row;
-        if (o >= a.out || row >= t.slabs * WG_SLAB || c >= a.in) continue;
-        const float4 *at = reinterpret_cast<const float4 *>(from + row * 2 * WG_CHANNELS);
-        float4 s = __ldcs(at);
-#pragma unroll 4
-        for (int r = 1; r < runs; ++r) {
-            const float4 v = __ldcs(at + r * (tiles * size / 4));
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
-        const float v[4] = {s.x, s.y, s.z, s.w};
-        const int64_t to = t.worker * a.dw_worker + o * a.dw_row + c;
+    if (o >= a.out || row >= t.slabs * WG_SLAB || c >= a.in) return;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    int r = 0;
+    auto add = [&](const float4 &v) { s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w; };
+    for (; r + 8 <= runs; r += 8, from += 8 * step) {
+        float4 v[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (c + e < a.in) {
-                if (a.grad_dtype == LIEC_F32) static_cast<float *>(a.dweight)[to + e] = v[e];
-                else static_cast<__nv_bfloat16 *>(a.dweight)[to + e] = __float2bfloat16_rn(v[e]);
-            }
+        for (int k = 0; k < 8; ++k) v[k] = __ldcs(from + k * step);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) add(v[k]);
     }
+#pragma unroll 4
+    for (; r < runs; ++r, from += step) add(__ldcs(from));
+    const float v[4] = {s.x, s.y, s.z, s.w};
+    const int64_t to = t.worker * a.dw_worker + o * a.dw_row + c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < a.in) {
+            if (a.grad_dtype == LIEC_F32) static_cast<float *>(a.dweight)[to + e] = v[e];
+            else static_cast<__nv_bfloat16 *>(a.dweight)[to + e] = __float2bfloat16_rn(v[e]);
+        }
 }
 
 __global__ void __launch_bounds__(256) wg_zero_kernel(const __grid_constant__ WgArgs a) {   // no tokens

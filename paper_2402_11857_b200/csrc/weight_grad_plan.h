@@ -71,9 +71,9 @@ struct WgPlan {
     }
 };
 
-// How many runs a cut tile has: the least time of the pair that has most to do, by what was measured (us): a slab's stage
-// takes 0.18, 0.6 with three parts of dy; an item's start and end 3; a run of a cut tile 0.1 per slab (written, read, added), the
-// joining launch 4.  Tiles with half the slabs have half the runs.
+// How many runs a cut tile has: the least time of the pair that has most to do, by what was measured (us): an item's start
+// takes 2, a slab's stage 0.18 (0.6 with three parts of dy), a slab's end 2 (an SM's way out for its sums); a run of a cut tile
+// 0.07 per slab (read and added), the joining launch 5.  Tiles with half the slabs have half the runs.
 inline WgPlan wg_plan(int workers, int64_t rows, int in, int out, int dtype) {
     WgPlan p{};
     const int slabs_all = (out + WG_SLAB - 1) / WG_SLAB;
@@ -95,8 +95,8 @@ inline WgPlan wg_plan(int workers, int64_t rows, int in, int out, int dtype) {
         const int64_t items = cut * runs + p.last * last_runs;
         if (items > 16 * WG_PAIRS && n > 1) break;
         double cost = 0.0;
-        for (int64_t i = 0; i < items && i < 16 * WG_PAIRS; i += WG_PAIRS) cost += 3.0 + unit * (i < cut * runs ? p.slabs * run : p.last_slabs * last_run);
-        if (runs > 1 || last_runs > 1) cost += 4.0 + 0.1 * (double)((runs > 1 ? cut * runs * p.slabs : 0) + (last_runs > 1 ? p.last * last_runs * p.last_slabs : 0));
+        for (int64_t i = 0; i < items && i < 16 * WG_PAIRS; i += WG_PAIRS) cost += 2.0 + (i < cut * runs ? p.slabs * (2.0 + unit * run) : p.last_slabs * (2.0 + unit * last_run));
+        if (runs > 1 || last_runs > 1) cost += 5.0 + 0.07 * (double)((runs > 1 ? cut * runs * p.slabs : 0) + (last_runs > 1 ? p.last * last_runs * p.last_slabs : 0));
         if (n > 1 && cost >= best) continue;
         best = cost;
         p.runs = runs; p.run = run; p.last_runs = last_runs; p.last_run = last_run;
