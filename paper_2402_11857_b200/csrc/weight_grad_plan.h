@@ -72,8 +72,9 @@ struct WgPlan {
 };
 
 // How many runs a cut tile has: the least time of the pair that has most to do, by what was measured (us): an item's start
-// takes 2, a slab's stage 0.18 (0.6 with three parts of dy), a slab's end 2 (an SM's way out for its sums); a run of a cut tile
-// 0.07 per slab (read and added), the joining launch 5.  Tiles with half the slabs have half the runs.
+// takes 2, a stage 0.36, with one slab 0.26 (0.6 with three parts of dy), a slab's end 2 (an SM's way out for its sums); a run
+// of a cut tile 0.07 per slab (read and added), the joining launch 5.  Full tiles and those with fewer slabs have runs that take
+// as long.
 inline WgPlan wg_plan(int workers, int64_t rows, int in, int out, int dtype) {
     WgPlan p{};
     const int slabs_all = (out + WG_SLAB - 1) / WG_SLAB;
@@ -85,17 +86,17 @@ inline WgPlan wg_plan(int workers, int64_t rows, int in, int out, int dtype) {
     p.full = (int64_t)workers * p.c_tiles * p.o_full;
     p.last = p.last_slabs ? (int64_t)workers * p.c_tiles : 0;
     p.whole = p.full / WG_PAIRS * WG_PAIRS;
-    const double unit = dtype == 0 ? 0.6 : 0.18;
+    const auto stage = [dtype](int slabs) { return dtype == 0 ? 0.6 * slabs : 0.16 + 0.1 * slabs; };
     const int64_t cut = p.full - p.whole;
     double best = 0.0;
     for (int n = 1; n <= WG_PAIRS && n <= p.stages; ++n) {
         const int run = (p.stages + n - 1) / n, runs = cut ? (p.stages + run - 1) / run : 1;
-        const int last_n = cut ? std::max(1, n * p.last_slabs / p.slabs) : n;
+        const int last_n = cut ? std::max(1, (int)(n * stage(p.last_slabs) / stage(p.slabs) + 0.5)) : n;
         const int last_run = (p.stages + last_n - 1) / last_n, last_runs = p.last ? (p.stages + last_run - 1) / last_run : 1;
         const int64_t items = cut * runs + p.last * last_runs;
         if (items > 16 * WG_PAIRS && n > 1) break;
         double cost = 0.0;
-        for (int64_t i = 0; i < items && i < 16 * WG_PAIRS; i += WG_PAIRS) cost += 2.0 + (i < cut * runs ? p.slabs * (2.0 + unit * run) : p.last_slabs * (2.0 + unit * last_run));
+        for (int64_t i = 0; i < items && i < 16 * WG_PAIRS; i += WG_PAIRS) cost += 2.0 + (i < cut * runs ? p.slabs * 2.0 + stage(p.slabs) * run : p.last_slabs * 2.0 + stage(p.last_slabs) * last_run);
         if (runs > 1 || last_runs > 1) cost += 5.0 + 0.07 * (double)((runs > 1 ? cut * runs * p.slabs : 0) + (last_runs > 1 ? p.last * last_runs * p.last_slabs : 0));
         if (n > 1 && cost >= best) continue;
         best = cost;
