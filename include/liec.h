@@ -467,8 +467,8 @@ typedef struct {
     int64_t dy_row_stride, dy_worker_stride;
     int64_t dweight_row_stride, dweight_worker_stride;   /* from output to output (>= in), from worker to worker */
 } liec_weight_grad_desc;
-/* Bytes of device workspace; 0 where none is needed, and for a bad desc.  A dy that is bfloat16 with rows that start on 16
- * bytes (its address counts; it is not read) needs room for partial sums only, any other a copy of dy in bfloat16 parts too. */
+/* Bytes of device workspace; 0 where none is needed, and for a bad desc.  A dy whose rows start on 16 bytes (its address counts;
+ * it is not read) needs room for partial sums only, any other a copy of dy too. */
 size_t liec_weight_grad_workspace_bytes(const liec_weight_grad_desc *desc, const void *dy);
 liec_status liec_weight_grad(const liec_weight_grad_desc *desc, const void *dy, const int8_t *q, const uint8_t *scales, void *dweight,
                              void *workspace, size_t workspace_bytes, void *stream);

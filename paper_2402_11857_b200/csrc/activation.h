@@ -56,7 +56,7 @@ struct WgArgs {
     const uint8_t *scales;
     void *dweight;
     float *part;      // workspace: the runs' sums, [run][worker][out][in], and
-    void *packed;     // dy in bfloat16 parts, where it does not go to the products as it is
+    void *packed;     // dy in rows of whole 16 bytes, where its own are not
     int64_t rows, dy_row, dy_worker, dw_row, dw_worker;
     int32_t workers, in, out, grad_dtype;
 };

@@ -25,22 +25,24 @@ constexpr int WG_GROUPS = 4, WG_GROUP = 128;   // groups of widening threads
 constexpr int WG_WIDENERS = WG_GROUPS * WG_GROUP, WG_THREADS = WG_WIDENERS + 64;
 constexpr uint32_t WG_POLLS = 1u << 20;
 
-// PARTS: bfloat16 parts of dy.  SLABS: products side by side.  A copied stage (bytes of q, parts of dy) stays from the start
-// of its copies to the end of its products, widened channels from their widening on: as many of the first as fit beside
-// one of the second per group.
+// PARTS: bfloat16 parts of dy; three of a binary32 dy, which comes as it is and is cut by those who widen q.  SLABS: products side by
+// side.  A copied stage (bytes of q, dy) stays from the start of its copies to the end of its products, what the widening threads
+// make of it (a group's place: channels, and parts of dy) from its widening on: as many of the first as fit beside one of
+// the second per group.
 template <int PARTS_>
 struct WgShape {
     static constexpr int PARTS = PARTS_, SLABS = PARTS == 1 ? 2 : 1, OUTPUTS = SLABS * WG_SLAB;
     static constexpr int COLUMNS = 2 * WG_SLAB;   // two slabs; or one, and the products of the smaller parts of dy beside it
     static constexpr int B_BYTES = 2 * WG_BLOCK_BYTES;                       // of a slab's part
-    static constexpr int STAGE_BYTES = SLABS * PARTS * B_BYTES + WG_RAW_BYTES;
-    static constexpr int STAGES = PARTS == 1 ? 9 : 6;
-    static constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + WG_GROUPS * WG_A_BYTES;
+    static constexpr int DY_BYTES = PARTS == 1 ? B_BYTES : 2 * B_BYTES;      // of a slab's dy as it comes
+    static constexpr int STAGE_BYTES = SLABS * DY_BYTES + WG_RAW_BYTES;
+    static constexpr int PLACE_BYTES = WG_A_BYTES + (PARTS == 1 ? 0 : PARTS * B_BYTES);
+    static constexpr int STAGES = PARTS == 1 ? 9 : 4;
+    static constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + WG_GROUPS * PLACE_BYTES;
     static_assert(SMEM_BYTES <= 227 * 1024 - 512, "with the barriers");
     static_assert(STAGES >= WG_GROUPS, "the parities of the widening groups' waits");
 };
 static_assert(WgShape<1>::SLABS == wg_slabs(1) && WgShape<3>::SLABS == wg_slabs(0), "the plan's tiles");
-inline int wg_parts(int dtype) { return dtype == 0 ? 3 : 1; }
 
 // 16 bytes of q times their power, as 16 bfloat16 numbers.  Byte b with last seven bits l and sign bit s is l - 128 s:
 // as bfloat16, 0x4300 | l is 128 + l and 0x4300 | (b & 0x80) is 128 + 128 s.
@@ -59,44 +61,29 @@ __device__ __forceinline__ void wg_widen(uint4 q, uint32_t byte, uint4 (&out)[2]
     out[1] = make_uint4(r[4], r[5], r[6], r[7]);
 }
 
-// x = p[0] + p[1] + p[2], each the upper half of a binary32 number: 8 bits of the significand at a time.
+// x = p[0] + p[1] + p[2], each the upper half of a binary32 number: 8 bits of the significand at a time (what lies below the last
+// is zero).  An infinity or NaN would leave NaN as rest.
 __device__ __forceinline__ void wg_split(float x, uint32_t (&p)[3]) {
-    const uint32_t bits = __float_as_uint(x);
-    if ((bits & 0x7f800000u) == 0x7f800000u) {   // infinities and NaN as they are
-        p[0] = (bits & 0x007fffffu) != 0u ? bits | 0x00400000u : bits;
-        p[1] = p[2] = 0u;
-        return;
-    }
-    p[0] = bits & 0xffff0000u;
+    p[0] = __float_as_uint(x) & 0xffff0000u;
     const float rest = x - __uint_as_float(p[0]);
     p[1] = __float_as_uint(rest) & 0xffff0000u;
     p[2] = __float_as_uint(rest - __uint_as_float(p[1]));
 }
+__device__ __forceinline__ void wg_split_special(float x, uint32_t (&p)[3]) {   // infinities and NaN as they are
+    const uint32_t bits = __float_as_uint(x);
+    if ((bits & 0x7f800000u) != 0x7f800000u) return;
+    p[0] = (bits & 0x007fffffu) != 0u ? bits | 0x00400000u : bits;
+    p[1] = p[2] = 0u;
+}
 
-// dy as the tensor memory accelerator wants it: bfloat16 rows of a multiple of 8 columns without gaps, part after part.  A
-// thread takes 8 columns of a row.
+// dy as the tensor memory accelerator wants it: rows of a multiple of 16 bytes without gaps.  A thread takes 16 bytes.
 template <typename T>
 __global__ void __launch_bounds__(256) wg_pack_kernel(const __grid_constant__ WgArgs a, int64_t row_chunks) {
-    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    const int64_t rows = a.workers * a.rows, i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / row_chunks;
-    if (row >= rows) return;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / row_chunks;
+    if (row >= a.workers * a.rows) return;
     const int64_t w = row / a.rows;
-    const int c = (int)(i - row * row_chunks) * 8;
-    const T *from = static_cast<const T *>(a.dy) + w * a.dy_worker + (row - w * a.rows) * a.dy_row;
-    uint4 *to = reinterpret_cast<uint4 *>(a.packed) + i;
-    if constexpr (PARTS == 1) {
-        *to = load_chunk(from, c, a.out);
-    } else {
-        const uint4 lo4 = load_chunk(from, c, a.out), hi4 = c + 4 < a.out ? load_chunk(from, c + 4, a.out) : make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t x[8] = {lo4.x, lo4.y, lo4.z, lo4.w, hi4.x, hi4.y, hi4.z, hi4.w};
-        uint32_t p[8][3];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) wg_split(__uint_as_float(x[e]), p[e]);
-#pragma unroll
-        for (int k = 0; k < 3; ++k)
-            to[k * rows * row_chunks] = make_uint4(__byte_perm(p[0][k], p[1][k], 0x7632), __byte_perm(p[2][k], p[3][k], 0x7632),
-                                                   __byte_perm(p[4][k], p[5][k], 0x7632), __byte_perm(p[6][k], p[7][k], 0x7632));
-    }
+    const int c = (int)(i - row * row_chunks) * Bits<T>::VEC;
+    reinterpret_cast<uint4 *>(a.packed)[i] = load_chunk(static_cast<const T *>(a.dy) + w * a.dy_worker + (row - w * a.rows) * a.dy_row, c, a.out);
 }
 
 __device__ __forceinline__ void wg_store(float *p, float v) { *p = v; }
@@ -149,8 +136,8 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
     auto full = [&](int g) { return bar + 8u * (2 * S::STAGES + g); };       // a group's channels, in both CTAs (in the first CTA)
     const uint32_t done = full(WG_GROUPS), drained = done + 8u;              // a tile's products; its sums are read (in the first CTA)
     auto b_at = [&](int s) { return base + s * S::STAGE_BYTES; };
-    auto raw_at = [&](int s) { return b_at(s) + S::SLABS * PARTS * S::B_BYTES; };
-    auto a_at = [&](int g) { return base + S::STAGES * S::STAGE_BYTES + g * WG_A_BYTES; };
+    auto raw_at = [&](int s) { return b_at(s) + S::SLABS * S::DY_BYTES; };
+    auto a_at = [&](int g) { return base + S::STAGES * S::STAGE_BYTES + g * S::PLACE_BYTES; };
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
     const int64_t pair = blockIdx.x / 2;
     auto first_channel = [&](const WgItem &g) { return g.c_tile * 2 * WG_CHANNELS + rank * WG_CHANNELS; };
@@ -188,15 +175,18 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
                 if (it >= S::STAGES) ok = barrier_wait_warp(empty(s), (it / S::STAGES - 1) & 1, WG_POLLS);
                 if (!ok) break;
                 if (elected()) {
-                    barrier_expect(loaded(s), WG_RAW_BYTES + g.slabs * PARTS * S::B_BYTES);
+                    barrier_expect(loaded(s), WG_RAW_BYTES + g.slabs * S::DY_BYTES);
                     copy_box(raw_at(s), &q_map, c0, t, g.worker, loaded(s));
+                    if constexpr (PARTS == 1) {
 #pragma unroll
-                    for (int n = 0; n < S::SLABS; ++n)
-                        if (n < g.slabs)
+                        for (int n = 0; n < S::SLABS; ++n)
+                            if (n < g.slabs)
 #pragma unroll
-                            for (int h = 0; h < 2 * PARTS; ++h)
-                                copy_box(b_at(s) + n * PARTS * S::B_BYTES + h * WG_BLOCK_BYTES, &dy_map, o0 + n * WG_SLAB + h % 2 * 64, t,
-                                         h / 2 * a.workers + g.worker, loaded(s));
+                                for (int h = 0; h < 2; ++h)
+                                    copy_box(b_at(s) + n * S::B_BYTES + h * WG_BLOCK_BYTES, &dy_map, o0 + n * WG_SLAB + h * 64, t, g.worker, loaded(s));
+                    } else {
+                        copy_box(b_at(s), &dy_map, o0, t, g.worker, loaded(s));
+                    }
                 }
                 __syncwarp();
             }
@@ -229,7 +219,7 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
                     ok = ok && barrier_wait_warp(full(k4), (it / WG_GROUPS) & 1, WG_POLLS);
                     if (!ok) break;
                     tc_after_sync();
-                    const uint64_t x = tc_descriptor(a_at(k4), WG_BLOCK_BYTES), y = tc_descriptor(b_at(s), WG_BLOCK_BYTES);
+                    const uint64_t x = tc_descriptor(a_at(k4), WG_BLOCK_BYTES), y = tc_descriptor(PARTS == 1 ? b_at(s) : a_at(k4) + WG_A_BYTES, WG_BLOCK_BYTES);
                     const bool last = ++in_sum == length || i + 1 == g.stages;
                     if (elected()) {
 #pragma unroll
@@ -308,6 +298,32 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
                         for (int h = 0; h < 2; ++h)
                             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + tc_swizzled(token, q_piece * 2 + h) + j * 2048),
                                          "r"(x[h].x), "r"(x[h].y), "r"(x[h].z), "r"(x[h].w) : "memory");
+                    }
+                    if constexpr (PARTS > 1) {   // 8 outputs of a token at a time
+#pragma unroll 2
+                        for (int j = 0; j < 4; ++j) {
+                            const int dy_token = warp % 4 * 8 + j * 2 + (lane >> 4), piece = lane & 15;
+                            float v[8];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[4 * h]), "=f"(v[4 * h + 1]), "=f"(v[4 * h + 2]), "=f"(v[4 * h + 3])
+                                             : "r"(b_at(s) + dy_token * 512 + piece * 32 + h * 16) : "memory");
+                            uint32_t x[8][3], most = 0u;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                wg_split(v[e], x[e]);
+                                most = max(most, __float_as_uint(v[e]) & 0x7fffffffu);
+                            }
+                            if (most >= 0x7f800000u)
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) wg_split_special(v[e], x[e]);
+#pragma unroll
+                            for (int part = 0; part < 3; ++part)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a_at(group) + WG_A_BYTES + part * S::B_BYTES + (piece >> 3) * WG_BLOCK_BYTES +
+                                                                                              tc_swizzled(dy_token, piece & 7)),
+                                             "r"(__byte_perm(x[0][part], x[1][part], 0x7632)), "r"(__byte_perm(x[2][part], x[3][part], 0x7632)),
+                                             "r"(__byte_perm(x[4][part], x[5][part], 0x7632)), "r"(__byte_perm(x[6][part], x[7][part], 0x7632)) : "memory");
+                        }
                     }
                     async_fence();
                     __syncwarp();
@@ -432,16 +448,17 @@ __global__ void __launch_bounds__(256) wg_zero_kernel(const __grid_constant__ Wg
     else static_cast<__nv_bfloat16 *>(a.dweight)[at] = __float2bfloat16_rn(0.0f);
 }
 
-// dy goes to the products as it is where it is bfloat16 and its rows start on 16 bytes, one after another.
+// dy goes to the kernel as it is where its rows start on 16 bytes, one after another.
 static bool wg_direct(const WgArgs &a, int dtype) {
-    return dtype == 1 && ln_whole(a.dy, a.dy_row, a.dy_worker, a.rows, a.workers, 8, 2) && (a.rows == 1 || a.dy_row >= a.out) &&
+    return ln_whole(a.dy, a.dy_row, a.dy_worker, a.rows, a.workers, dtype == 0 ? 4 : 8, dtype == 0 ? 4 : 2) && (a.rows == 1 || a.dy_row >= a.out) &&
            (a.workers == 1 || a.dy_worker >= a.out);
 }
 static size_t wg_part_bytes(const WgPlan &p) { return sizeof(float) * (size_t)p.slots(); }
 
 size_t weight_grad_workspace(const WgArgs &a, int dtype) {
     if (a.rows == 0) return 0;
-    const size_t packed = wg_direct(a, dtype) ? 0 : (size_t)wg_parts(dtype) * a.workers * a.rows * ((a.out + 7) / 8) * 16;
+    const int vec = dtype == 0 ? 4 : 8;
+    const size_t packed = wg_direct(a, dtype) ? 0 : (size_t)a.workers * a.rows * ((a.out + vec - 1) / vec) * 16;
     return wg_part_bytes(wg_plan(a.workers, a.rows, a.in, a.out, dtype)) + packed;
 }
 
@@ -463,17 +480,16 @@ static WgEncode wg_encode() {
 }
 
 // [workers][rows][cols], boxes of box_cols columns by a stage's tokens; what lies outside is read as zeros.
-static bool wg_map(CUtensorMap *map, const void *base, bool bytes, int64_t cols, int64_t rows, int64_t workers, int64_t row, int64_t worker, int box_cols) {
+static bool wg_map(CUtensorMap *map, const void *base, int size, int64_t cols, int64_t rows, int64_t workers, int64_t row, int64_t worker, int box_cols) {
     const WgEncode encode = wg_encode();
     if (!encode) return false;
-    const int size = bytes ? 1 : 2;
     // (a single row or worker is never stepped over; the map wants a step all the same)
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)workers};
     const cuuint64_t row_step = rows > 1 ? (cuuint64_t)(row * size) : (cuuint64_t)((cols * size + 15) / 16 * 16);
     const cuuint64_t steps[2] = {row_step, workers > 1 ? (cuuint64_t)(worker * size) : row_step * (cuuint64_t)rows};
     const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)WG_TOKENS, 1}, one[3] = {1, 1, 1};
-    return encode(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, steps, box, one,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, bytes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+    return encode(map, size == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : size == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void *>(base), dims, steps, box, one,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, size == 2 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -512,18 +528,19 @@ cudaError_t launch_weight_grad(WgArgs a, int dtype, cudaStream_t st) {
     }
     const WgPlan p = wg_plan(a.workers, a.rows, a.in, a.out, dtype);
     const bool direct = wg_direct(a, dtype);
-    const int64_t q_cols = ck_cols(a.in), dy_cols = (a.out + 7) / 8 * 8;
+    const int size = dtype == 0 ? 4 : 2, vec = 16 / size, box = dtype == 0 ? 128 : 64;
+    const int64_t q_cols = ck_cols(a.in), dy_cols = (a.out + vec - 1) / vec * vec;
     a.packed = reinterpret_cast<char *>(a.part) + wg_part_bytes(p);
     CUtensorMap q_map, dy_map;
-    if (!wg_map(&q_map, a.q, true, q_cols, a.rows, a.workers, q_cols, q_cols * a.rows, WG_CHANNELS) ||
-        !(direct ? wg_map(&dy_map, a.dy, false, a.out, a.rows, a.workers, a.dy_row, a.dy_worker, 64)
-                 : wg_map(&dy_map, a.packed, false, a.out, a.rows, (int64_t)wg_parts(dtype) * a.workers, dy_cols, dy_cols * a.rows, 64)))
+    if (!wg_map(&q_map, a.q, 1, q_cols, a.rows, a.workers, q_cols, q_cols * a.rows, WG_CHANNELS) ||
+        !(direct ? wg_map(&dy_map, a.dy, size, a.out, a.rows, a.workers, a.dy_row, a.dy_worker, box)
+                 : wg_map(&dy_map, a.packed, size, a.out, a.rows, a.workers, dy_cols, dy_cols * a.rows, box)))
         return cudaErrorNotSupported;
     cudaError_t e = cudaSuccess;
     if (!direct) {
-        const int64_t chunks = a.workers * a.rows * (dy_cols / 8);
+        const int64_t chunks = a.workers * a.rows * (dy_cols / vec);
         const cudaLaunchConfig_t cfg = wg_config((chunks + 255) / 256, 256, 0, st);
-        e = cudaLaunchKernelEx(&cfg, dtype == 0 ? wg_pack_kernel<float> : wg_pack_kernel<__nv_bfloat16>, a, dy_cols / 8);
+        e = cudaLaunchKernelEx(&cfg, dtype == 0 ? wg_pack_kernel<float> : wg_pack_kernel<__nv_bfloat16>, a, dy_cols / vec);
         if (e != cudaSuccess) return e;
     }
     e = dtype == 0 ? wg_launch<3>(a, p, q_map, dy_map, !direct, st) : wg_launch<1>(a, p, q_map, dy_map, !direct, st);

@@ -145,16 +145,19 @@ def test_bad_weight_grad_descs(lib, kw, status):
 def test_weight_grad_pointers_and_workspace(lib):
     def call(d, dy=AT, q=2 * AT, s=3 * AT, dw=4 * AT, ws=5 * AT, size=1 << 30):
         return lib.liec_weight_grad(C.byref(d), dy, q, s, dw, ws, size, None)
-    for kw in (dict(dy=None), dict(q=None), dict(s=None), dict(dw=None), dict(ws=None), dict(ws=5 * AT + 8), dict(dy=AT + 2), dict(dw=4 * AT + 2), dict(q=2 * AT + 8),
+    for kw in (dict(dy=None), dict(q=None), dict(s=None), dict(dw=None), dict(dy=AT + 2), dict(dw=4 * AT + 2), dict(q=2 * AT + 8),
                dict(dw=AT), dict(dw=2 * AT), dict(dw=3 * AT + 4), dict(dw=AT + 4 * 2399)):
         assert call(weight_grad(), **kw) == 1, kw
-    assert call(weight_grad(), size=0) == 3
+    for kw in (dict(ws=None), dict(ws=5 * AT + 8)):
+        assert call(weight_grad(dy_row_stride=25), **kw) == 1, kw
+    assert call(weight_grad(dy_row_stride=25), size=0) == 3
     assert call(weight_grad(dweight_row_stride=39)) == 1 and call(weight_grad(dweight_worker_stride=0)) == 1 and call(weight_grad(dweight_worker_stride=959)) == 1
     need = lambda at=AT, **kw: lib.liec_weight_grad_workspace_bytes(C.byref(weight_grad(**kw)), at)
-    # a bfloat16 dy on 16 bytes goes as it is; one that is not, and any binary32, is packed into 1 and 3 parts
+    # a dy with rows on 16 bytes goes as it is, any other is packed
     bf = dict(dtype=liec.BF16, workers=40)
     assert need(**bf) == 0 and need(at=AT + 2, **bf) >= 40 * 50 * 24 * 2 and need(dy_row_stride=25, **bf) >= 40 * 50 * 24 * 2
-    assert need(dtype=liec.F32, workers=40) >= 3 * 40 * 50 * 24 * 2
+    f32 = dict(dtype=liec.F32, workers=40)
+    assert need(**f32) == 0 and need(at=AT + 4, **f32) >= 40 * 50 * 24 * 4 and need(dy_row_stride=26, **f32) >= 40 * 50 * 24 * 4
     assert need(rows=0) == 0
     # runs of tokens never take more than a place for each of some 16 x 74 pieces of 256 x 512
     assert need(dtype=liec.BF16, rows=1 << 20, dy_worker_stride=24 << 20) <= 16 * 74 * 256 * 512 * 4
