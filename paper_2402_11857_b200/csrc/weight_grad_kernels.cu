@@ -26,7 +26,8 @@ constexpr int WG_WIDENERS = WG_GROUPS * WG_GROUP, WG_THREADS = WG_WIDENERS + 64;
 constexpr uint32_t WG_POLLS = 1u << 20;
 
 // PARTS: bfloat16 parts of dy; three of a binary32 dy, which comes as it is and is cut by those who widen q.  SLABS: products side by
-// side.  A copied stage (bytes of q, dy) stays from the start of its copies to the end of its products, what the widening threads
+// side.  A copied stage (bytes of q, dy) stays from the start of its copies to the end of its products (to the end of the cutting, where dy
+// is cut), what the widening threads
 // make of it (a group's place: channels, and parts of dy) from its widening on: as many of the first as fit beside one of
 // the second per group.
 template <int PARTS_>
@@ -126,7 +127,7 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
                                                             const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap dy_map) {
     using S = WgShape<PARTS>;
     extern __shared__ char wg_smem[];
-    __shared__ __align__(8) unsigned long long bars[2 * S::STAGES + WG_GROUPS + 2];
+    __shared__ __align__(8) unsigned long long bars[3 * S::STAGES + WG_GROUPS + 2];
     __shared__ uint32_t tmem_at;
     __shared__ int failed;
     const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars);
@@ -135,6 +136,7 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
     auto empty = [&](int s) { return bar + 8u * (S::STAGES + s); };          // its products are done
     auto full = [&](int g) { return bar + 8u * (2 * S::STAGES + g); };       // a group's channels, in both CTAs (in the first CTA)
     const uint32_t done = full(WG_GROUPS), drained = done + 8u;              // a tile's products; its sums are read (in the first CTA)
+    auto read = [&](int s) { return drained + 8u + 8u * s; };                // PARTS > 1: the widening threads are done with a stage, in this CTA
     auto b_at = [&](int s) { return base + s * S::STAGE_BYTES; };
     auto raw_at = [&](int s) { return b_at(s) + S::SLABS * S::DY_BYTES; };
     auto a_at = [&](int g) { return base + S::STAGES * S::STAGE_BYTES + g * S::PLACE_BYTES; };
@@ -147,6 +149,7 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
             for (int s = 0; s < S::STAGES; ++s) {
                 barrier_init(loaded(s), 1);
                 barrier_init(empty(s), 1);
+                barrier_init(read(s), WG_GROUP / 32);
             }
             for (int k = 0; k < WG_GROUPS; ++k) barrier_init(full(k), 2 * WG_GROUP / 32);
             barrier_init(done, 1);
@@ -172,7 +175,7 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
             const int o0 = g.o_tile * S::OUTPUTS + rank * 128, c0 = first_channel(g), t0 = g.stage * WG_TOKENS;
             for (int i = 0; i < g.stages; ++i, ++it) {
                 const int s = it % S::STAGES, t = t0 + i * WG_TOKENS;
-                if (it >= S::STAGES) ok = barrier_wait_warp(empty(s), (it / S::STAGES - 1) & 1, WG_POLLS);
+                if (it >= S::STAGES) ok = barrier_wait_warp(PARTS == 1 ? empty(s) : read(s), (it / S::STAGES - 1) & 1, WG_POLLS);
                 if (!ok) break;
                 if (elected()) {
                     barrier_expect(loaded(s), WG_RAW_BYTES + g.slabs * S::DY_BYTES);
@@ -192,7 +195,11 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
             }
         }
         // nothing may be on its way into this CTA's memory when it ends: the products' last arrivals, or copies
-        for (int k = max(0, it - S::STAGES); ok && k < it; ++k) ok = barrier_wait_warp(empty(k % S::STAGES), (k / S::STAGES) & 1, WG_POLLS);
+        // (PARTS > 1: a stage that has been read had its last products done, so a parity of `empty` tells its phase)
+        for (int k = max(0, it - S::STAGES); ok && k < it; ++k) {
+            if constexpr (PARTS > 1) ok = barrier_wait_warp(read(k % S::STAGES), (k / S::STAGES) & 1, WG_POLLS);
+            ok = ok && barrier_wait_warp(empty(k % S::STAGES), (k / S::STAGES) & 1, WG_POLLS);
+        }
         if (!ok) {
             failed = 1;
             for (int k = max(0, it - S::STAGES); k < it; ++k) barrier_wait_warp(loaded(k % S::STAGES), (k / S::STAGES) & 1, WG_POLLS);
@@ -302,12 +309,14 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
                     if constexpr (PARTS > 1) {   // 8 outputs of a token at a time
 #pragma unroll 2
                         for (int j = 0; j < 4; ++j) {
-                            const int dy_token = warp % 4 * 8 + j * 2 + (lane >> 4), piece = lane & 15;
-                            float v[8];
+                            const int dy_token = warp % 4 * 8 + j * 2 + (lane >> 4), piece = lane & 15, swap = lane >> 2 & 1;   // (of eight lanes, four start with their second half: all places of a row)
+                            float u[8], v[8];
 #pragma unroll
                             for (int h = 0; h < 2; ++h)
-                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[4 * h]), "=f"(v[4 * h + 1]), "=f"(v[4 * h + 2]), "=f"(v[4 * h + 3])
-                                             : "r"(b_at(s) + dy_token * 512 + piece * 32 + h * 16) : "memory");
+                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(u[4 * h]), "=f"(u[4 * h + 1]), "=f"(u[4 * h + 2]), "=f"(u[4 * h + 3])
+                                             : "r"(b_at(s) + dy_token * 512 + piece * 32 + (h ^ swap) * 16) : "memory");
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] = swap ? u[e ^ 4] : u[e];
                             uint32_t x[8][3], most = 0u;
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {
@@ -327,7 +336,10 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
                     }
                     async_fence();
                     __syncwarp();
-                    if (lane == 0) barrier_arrive_cluster(in_cta(full(group), 0));
+                    if (lane == 0) {
+                        barrier_arrive_cluster(in_cta(full(group), 0));
+                        if constexpr (PARTS > 1) barrier_arrive_cluster(in_cta(read(s), rank));
+                    }
                     return true;
                 };
                 // the powers run two turns ahead

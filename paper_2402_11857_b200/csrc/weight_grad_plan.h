@@ -72,7 +72,7 @@ struct WgPlan {
 };
 
 // How many runs a cut tile has: the least time of the pair that has most to do, by what was measured (us): an item's start
-// takes 2, a stage 0.36, with one slab 0.26 (0.6 with three parts of dy), a slab's end 2 (an SM's way out for its sums); a run
+// takes 2, a stage 0.36, with one slab 0.26 (0.7 with three parts of dy), a slab's end 2 (an SM's way out for its sums); a run
 // of a cut tile 0.07 per slab (read and added), the joining launch 5.  Full tiles and those with fewer slabs have runs that take
 // as long.
 inline WgPlan wg_plan(int workers, int64_t rows, int in, int out, int dtype) {
@@ -86,7 +86,7 @@ inline WgPlan wg_plan(int workers, int64_t rows, int in, int out, int dtype) {
     p.full = (int64_t)workers * p.c_tiles * p.o_full;
     p.last = p.last_slabs ? (int64_t)workers * p.c_tiles : 0;
     p.whole = p.full / WG_PAIRS * WG_PAIRS;
-    const auto stage = [dtype](int slabs) { return dtype == 0 ? 0.6 * slabs : 0.16 + 0.1 * slabs; };
+    const auto stage = [dtype](int slabs) { return dtype == 0 ? 0.7 * slabs : 0.16 + 0.1 * slabs; };
     const int64_t cut = p.full - p.whole;
     double best = 0.0;
     for (int n = 1; n <= WG_PAIRS && n <= p.stages; ++n) {
