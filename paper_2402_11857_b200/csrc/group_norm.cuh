@@ -43,8 +43,16 @@ struct GnReader {
                 const uint4 *g = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(now) & ~uintptr_t(15));
                 r.a = __ldg(g);
                 r.b = __ldg(g + 1);
-            } else {
-                r.a = c < cols ? load_chunk_edge(now, cols - c) : make_uint4(0u, 0u, 0u, 0u);
+            } else {   // at a row's ends, element by element, put together in chunk(): nothing waits here
+                uint32_t w[8] = {};
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (c + e < cols) {
+                        if constexpr (sizeof(T) == 4) w[e] = __ldg(reinterpret_cast<const unsigned *>(now) + e);
+                        else w[e] = __ldg(reinterpret_cast<const unsigned short *>(now) + e);
+                    }
+                r.a = make_uint4(w[0], w[1], w[2], w[3]);
+                r.b = make_uint4(w[4], w[5], w[6], w[7]);
             }
         }
         return r;
@@ -53,6 +61,7 @@ struct GnReader {
         if constexpr (!WHOLE) {
             uint32_t shift;
             if (inside(row + u * step, shift)) return cut_granules<(int)sizeof(T)>(r.a, r.b, shift);
+            if constexpr (sizeof(T) == 2) return make_uint4(r.a.x | r.a.y << 16, r.a.z | r.a.w << 16, r.b.x | r.b.y << 16, r.b.z | r.b.w << 16);
         }
         return r.a;
     }
