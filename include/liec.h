@@ -393,10 +393,11 @@ liec_status liec_activation_restore(const liec_activation_desc *desc, const int8
  *   act: z (LIEC_ACT_NONE), max(z, 0) (LIEC_ACT_RELU), z / (1 + exp(-z)) (LIEC_ACT_SILU)
  *   dz = dy act'(z),  dx = r (dz w - mean(dz w) - xh mean(dz w xh)),
  *   dw = sum over the worker's samples and pixels of dz xh,  db = the same of dz       (act'(z) = 1 for z > 0, else 0, for ReLU)
- * Evaluated in binary32 (joins of partial sums in binary64), outputs rounded once to their type.  Squares are summed around a value of the channel, so
- * a far mean costs no digits; entries whose squares leave binary32 (beyond about 1e18) are not provided for.  On which side
- * of zero a ReLU's z lies is decided as in binary64 from the given x, mean, rstd, w and b.  Equal calls give equal bits (no
- * atomics).  A group with an infinity or NaN gives NaN in that group of that image, and in dw and db of its channels.
+ * Evaluated in binary32 (joins of partial sums in binary64), outputs rounded once to their type.  Squares are summed about means
+ * of the entries so far, so neither a far mean nor a single entry far from the others costs digits of r; m is stored as a
+ * binary32 number, and a mean of k deviations so leaves errors of up to k 2^-24 in xh.  Entries whose squares leave binary32
+ * (beyond about 1e18) are not provided for.  On which side of zero a ReLU's z lies is decided as in binary64 from the given x,
+ * mean, rstd, w and b.  Equal calls give equal bits (no atomics).  A group with an infinity or NaN gives NaN in that group of that image, and in dw and db of its channels.
  *
  * The forward pass can leave the checkpoint of x (q and scales, as liec_activation_compress of its [workers][samples pixels]
  * [channels] rows would) from the same read of x, and the backward pass can read the checkpoint in place of x: the formulas

@@ -34,7 +34,7 @@ struct GnArgs {   // an image is a worker's sample; strides in elements
     int8_t *q;
     uint8_t *scales;
     float *mean, *rstd;           // [workers][samples][groups]
-    float *part;                  // two sums per channel of every part of an image, [image][part][2][channels]
+    float *part;                  // per channel of every part of an image: forward three numbers, backward two, [image][part][2 or 3][channels]
     float *level;                 // backward: r mean(dz w) and r^2 mean(dz w xh), [image][groups][2]
     int64_t x_pixel, x_sample, x_worker, y_pixel, y_sample, y_worker, dx_pixel, dx_sample, dx_worker;   // y: of dy in the backward pass
     int64_t weight_stride, bias_stride, dweight_stride, dbias_stride;

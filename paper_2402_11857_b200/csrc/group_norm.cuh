@@ -406,6 +406,48 @@ __device__ __forceinline__ void gn_slope(const GnArgs &a, int worker, int64_t im
     }
 }
 
+// Mean and squares of a thread's entries in one pass: sums s of d and t of d^2 about an origin (minus is its negative) that
+// starts as the thread's own first entry and moves to the mean so far as the entries become more.  N entries that lie about
+// their mean and n further ones about that mean: the squares of the n are at most n / N times those of all about their common
+// mean, so nothing is lost however far the first entry, or any other, lies from the rest.
+template <int P>
+struct GnMoments {
+    F2 minus[P] = {}, s[P] = {}, t[P] = {};   // (minus is zero without entries)
+    template <typename T>
+    __device__ __forceinline__ void start(uint4 first) {
+        LnChunk<T>::read(first, minus);
+#pragma unroll
+        for (int k = 0; k < P; ++k) minus[k] = mul(minus[k], f2(-1.0f));
+    }
+    __device__ __forceinline__ void take(const F2 (&x)[P]) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const F2 d = add(x[k], minus[k]);
+            s[k] = add(s[k], d);
+            t[k] = fma(d, d, t[k]);
+        }
+    }
+    // Sums about an origin h further on: n entries.
+    static __device__ __forceinline__ void moved(F2 &s, F2 &t, F2 h, F2 minus_n) {
+        const F2 was = s;
+        s = fma(minus_n, h, s);
+        t = fma(mul(h, f2(-1.0f)), add(was, s), t);
+    }
+    // To the mean of the n entries taken; inverse is about 1 / n.
+    __device__ __forceinline__ void move(float n, float inverse) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const F2 to = fma(s[k], f2(-inverse), minus[k]), h = fma(to, f2(-1.0f), minus[k]);
+            minus[k] = to;
+            moved(s[k], t[k], h, f2(-n));
+        }
+    }
+    // To an origin that the threads of a channel share.
+    __device__ __forceinline__ void move_to(int k, F2 origin, float n) { moved(s[k], t[k], add(origin, minus[k]), f2(-n)); }
+    // The sum of the n entries themselves.
+    __device__ __forceinline__ F2 whole(int k, float n) const { return fma(minus[k], f2(-n), s[k]); }
+};
+
 // The checkpoint of a thread's chunks: the 4 or 8 threads of a block are neighbours in a warp and come here together.
 template <typename T>
 struct GnCompressor {

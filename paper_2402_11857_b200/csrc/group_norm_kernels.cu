@@ -52,50 +52,89 @@ __device__ __forceinline__ void gn_channel_sums(const GnPlace<VEC> &at, int tile
 
 __device__ __forceinline__ void gn_wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// Mean and squares around it of every channel of a part, about the part's first pixel.
+// Sums over all pixel lanes of a column of N boxes, in a fixed order.
+template <int N>
+__device__ __forceinline__ void gn_column_sums(const float *box, int lanes, int width, int column, float (&sum)[N]) {
+    float v[N][4] = {};
+    int l = 0;
+#pragma unroll 2
+    for (; l + 4 <= lanes; l += 4)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int n = 0; n < N; ++n) v[n][i] += box[(n * lanes + l + i) * width + column];
+    for (; l < lanes; ++l)
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n][0] += box[(n * lanes + l) * width + column];
+#pragma unroll
+    for (int n = 0; n < N; ++n) sum[n] = (v[n][0] + v[n][1]) + (v[n][2] + v[n][3]);
+}
+
+// What the forward pass knows of a channel in a part of an image: its mean in two parts, the second what the first, a binary32
+// number, leaves; and the squares around the mean.
+constexpr int GN_FORWARD_PARTS = 3, GN_BACKWARD_PARTS = 2;
+
+// A thread's entries about their own mean; then all threads' about one number per channel, their mean as far as it is known then.
 template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 4 : 3) gn_moments_kernel(const __grid_constant__ GnArgs a) {
     constexpr int VEC = Bits<T>::VEC, P = VEC / 2;
     extern __shared__ __align__(16) char gn_ring[];
     __shared__ __align__(16) float box[GN_THREADS * 2 * VEC];
-    __shared__ float origin[GN_THREADS * VEC];
+    __shared__ __align__(16) float about[GN_THREADS * VEC];
     const GnPlace<VEC> at(a, false);
-    F2 s[P] = {}, t[P] = {};
-    if (at.turns > 0) {
-        GnFromX<T, WHOLE> x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
-        F2 minus[P], d[P];
-        LnChunk<T>::read(at.c < a.channels ? load_chunk(x.row - at.c - at.lane * a.x_pixel, at.c, a.channels) : make_uint4(0u, 0u, 0u, 0u), d);
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-            minus[k] = f2(-lo(d[k]), -hi(d[k]));
-            if (at.lane == 0) {
-                origin[at.chunk * VEC + 2 * k] = lo(d[k]);
-                origin[at.chunk * VEC + 2 * k + 1] = hi(d[k]);
-            }
-        }
-        auto take = [&](uint4 chunk) {
-            GnFromX<T, WHOLE>::centred(chunk, minus, d);
-#pragma unroll
-            for (int j = 0; j < P; ++j) {
-                s[j] = add(s[j], d[j]);
-                t[j] = fma(d[j], d[j], t[j]);
-            }
-        };
-        if constexpr (WHOLE) {
-            const GnRing<16> ring(gn_ring);
-            if (at.c < a.channels) gn_ring_turns((int)at.turns, [&](int place) { ring.copy(place, x.row); x.next(); }, [&](int place, int) { take(ring.read(place)); }, [](int) {});
-        } else {
-            gn_turns<2>(at.turns, [&](int u) { return x.load(u); }, [&](int u, const typename GnFromX<T, WHOLE>::Raw &raw) { take(x.keep(raw, u)); }, [&](int n) { x.advance(n); });
-        }
+    const bool in = at.turns > 0 && at.c < a.channels;
+    GnFromX<T, WHOLE> x(a, at.worker, at.sample, at.p0, at.lanes, at.c);
+    GnMoments<P> m;
+    if (in) m.template start<T>(load_chunk(x.row - at.c, at.c, a.channels));
+    int done = 0;
+    auto take = [&](uint4 chunk) {
+        F2 v[P];
+        LnChunk<T>::read(chunk, v);
+        m.take(v);
+    };
+    auto after = [&](int n) {
+        done += n;
+        if (done == 4 || done == 16) m.move((float)done, done == 4 ? 0.25f : 0.0625f);
+    };
+    if constexpr (WHOLE) {
+        const GnRing<16> ring(gn_ring);
+        if (in) gn_ring_turns((int)at.turns, [&](int place) { ring.copy(place, x.row); x.next(); }, [&](int place, int) { take(ring.read(place)); }, after);
+    } else {
+        gn_turns<2>(at.turns, [&](int u) { return x.load(u); }, [&](int u, const typename GnFromX<T, WHOLE>::Raw &raw) { take(x.keep(raw, u)); }, [&](int n) { x.advance(n); after(n); });
     }
-    gn_channel_sums<VEC>(at, a.tile_chunks, s, t, box);
     const int width = a.tile_chunks * VEC;
-    float *out = a.part + (at.image * a.parts + at.part) * 2 * a.channels + at.c0;
-    const float n = (float)(min((at.part + 1) * a.part_pixels, a.pixels) - at.part * a.part_pixels);
+    const float n = (float)at.turns, inverse = 1.0f / (float)(min((at.part + 1) * a.part_pixels, a.pixels) - at.part * a.part_pixels);
+    float *out = a.part + (at.image * a.parts + at.part) * GN_FORWARD_PARTS * a.channels + at.c0;
+    auto put = [&](int plane, auto &&value) {
+        float4 *to = reinterpret_cast<float4 *>(box + (plane * at.lanes + at.lane) * width + at.chunk * VEC);
+#pragma unroll
+        for (int k = 0; k < P; k += 2) {
+            const F2 v = value(k), w = value(k + 1);
+            to[k / 2] = make_float4(lo(v), hi(v), lo(w), hi(w));
+        }
+    };
+    if (at.lane < at.lanes) put(0, [&](int k) { return m.whole(k, n); });
+    __syncthreads();
+    for (int q = threadIdx.x; q < width; q += GN_THREADS) {
+        float sum[1];
+        gn_column_sums(box, at.lanes, width, q, sum);
+        about[q] = sum[0] * inverse;
+        if (at.c0 + q < a.channels) out[q] = about[q];
+    }
+    __syncthreads();
+    if (at.lane < at.lanes) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) m.move_to(k, f2(about[at.chunk * VEC + 2 * k], about[at.chunk * VEC + 2 * k + 1]), n);
+        put(0, [&](int k) { return m.s[k]; });
+        put(1, [&](int k) { return m.t[k]; });
+    }
+    __syncthreads();
     for (int q = threadIdx.x; q < width && at.c0 + q < a.channels; q += GN_THREADS) {
-        const float mean = box[q] / n;
-        out[q] = origin[q] + mean;
-        out[a.channels + q] = fmaxf(__fmaf_rn(-box[q], mean, box[width + q]), 0.0f);
+        float sum[2];
+        gn_column_sums(box, at.lanes, width, q, sum);
+        const float left = sum[0] * inverse;
+        out[a.channels + q] = left;
+        out[2 * a.channels + q] = fmaxf(__fmaf_rn(-sum[0], left, sum[1]), 0.0f);
     }
 }
 
@@ -128,14 +167,14 @@ __global__ void __launch_bounds__(GN_THREADS) gn_statistics_kernel(const __grid_
     gn_wait_for_kernel_before();
     gn_per_group<LANES>(a, [&](bool live, uint32_t image, uint32_t group, uint32_t lane) {
         const uint32_t width = (uint32_t)a.channels / (uint32_t)a.groups, entries = live ? width * a.parts : 0u;
-        const float *part = a.part + (int64_t)image * a.parts * 2 * a.channels + group * width;
+        const float *part = a.part + (int64_t)image * a.parts * GN_FORWARD_PARTS * a.channels + group * width;
         const double n = (double)a.pixels * width;
         auto each = [&](auto &&f) {   // channel's mean, squares around it, number of pixels
 #pragma unroll 4
             for (uint32_t i = lane; i < entries; i += LANES) {
                 const uint32_t q = i / width;
-                const float *at = part + (int64_t)q * 2 * a.channels + (i - q * width);
-                f((double)at[0], (double)at[a.channels], (double)min(a.part_pixels, a.pixels - q * a.part_pixels));
+                const float *at = part + (int64_t)q * GN_FORWARD_PARTS * a.channels + (i - q * width);
+                f((double)at[0] + (double)at[a.channels], (double)at[2 * a.channels], (double)min(a.part_pixels, a.pixels - q * a.part_pixels));
             }
         };
         double s = 0.0, t = 0.0;
@@ -250,7 +289,7 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_slopes_kernel(const __grid_c
     }
     gn_channel_sums<VEC>(at, a.tile_chunks, s, t, box);
     const int width = a.tile_chunks * VEC;
-    float *out = a.part + (at.image * a.parts + at.part) * 2 * a.channels + at.c0;
+    float *out = a.part + (at.image * a.parts + at.part) * GN_BACKWARD_PARTS * a.channels + at.c0;
     for (int q = threadIdx.x; q < width && at.c0 + q < a.channels; q += GN_THREADS) {
         out[q] = box[q];
         out[a.channels + q] = box[width + q] * a.rstd[at.image * a.groups + (uint32_t)(at.c0 + q) / (uint32_t)(a.channels / a.groups)];
@@ -293,14 +332,14 @@ __global__ void __launch_bounds__(GN_THREADS) gn_levels_kernel(const __grid_cons
     }
     gn_per_group<LANES>(a, [&](bool live, uint32_t image, uint32_t group, uint32_t lane) {
         const uint32_t width = (uint32_t)a.channels / (uint32_t)a.groups, entries = live ? width * a.parts : 0u, worker = image / (uint32_t)a.samples;
-        const float *part = a.part + (int64_t)image * a.parts * 2 * a.channels + group * width;
+        const float *part = a.part + (int64_t)image * a.parts * GN_BACKWARD_PARTS * a.channels + group * width;
         const float *weight = a.weight ? a.weight + worker * a.weight_stride + group * width : nullptr;
         double s = 0.0, t = 0.0;
 #pragma unroll 4
         for (uint32_t i = lane; i < entries; i += LANES) {
             const uint32_t q = i / width, c = i - q * width;
             const double w = weight ? (double)weight[c] : 1.0;
-            const float *at = part + (int64_t)q * 2 * a.channels + c;
+            const float *at = part + (int64_t)q * GN_BACKWARD_PARTS * a.channels + c;
             s += w * at[0];
             t += w * at[a.channels];
         }
@@ -375,7 +414,7 @@ static void gn_plan(GnArgs &a, int vec, bool backward) {
 static size_t gn_streamed_workspace(GnArgs a, int dtype, bool backward) {
     gn_plan(a, dtype == 0 ? 4 : 8, backward);
     const size_t images = (size_t)a.workers * a.samples;
-    return sizeof(float) * (images * a.parts * 2 * a.channels + (backward ? images * a.groups * 2 : 0));
+    return sizeof(float) * (images * a.parts * (backward ? GN_BACKWARD_PARTS : GN_FORWARD_PARTS) * a.channels + (backward ? images * a.groups * 2 : 0));
 }
 
 size_t group_norm_workspace(const GnArgs &a, int dtype, bool backward) {
@@ -500,7 +539,7 @@ cudaError_t launch_group_norm_backward(GnArgs a, int dtype, cudaStream_t st) {
         return gn_launch(gn_levels_kernel<8>, gn_join_ctas(a), 0, true, st, a, 0u);
     }
     gn_plan(a, dtype == 0 ? 4 : 8, true);
-    a.level = a.part + (int64_t)a.workers * a.samples * a.parts * 2 * a.channels;
+    a.level = a.part + (int64_t)a.workers * a.samples * a.parts * GN_BACKWARD_PARTS * a.channels;
     if (dtype == 0) return a.whole ? gn_backward<float, true>(a, st) : gn_backward<float, false>(a, st);
     return a.whole ? gn_backward<__nv_bfloat16, true>(a, st) : gn_backward<__nv_bfloat16, false>(a, st);
 }

@@ -42,42 +42,48 @@ struct GnSpot {
     __device__ __forceinline__ int channels(const GnArgs &a) const { return min(width, a.channels - c0); }   // of the tile
 };
 
-// The channels' two sums over the pixel lanes: sums[which][channel], complete for all threads.
+// A sum per channel over the pixel lanes, complete for all threads.
+template <int VEC>
+__device__ __forceinline__ void gn_add_lanes(const GnSpot<VEC> &at, const F2 (&mine)[VEC / 2], float *box, float *sums) {
+    const int width = at.width;
+    if (at.lane < at.lanes) {
+#pragma unroll
+        for (int k = 0; k < VEC / 2; k += 2)
+            *reinterpret_cast<float4 *>(box + at.lane * width + at.chunk * VEC + 2 * k) = make_float4(lo(mine[k]), hi(mine[k]), lo(mine[k + 1]), hi(mine[k + 1]));
+    }
+    __syncthreads();
+    if (2 * width > GR_THREADS) {   // a thread per channel, or several channels
+        for (int q = threadIdx.x; q < width; q += GR_THREADS) {
+            float s = 0.0f;
+            for (int l = 0; l < at.lanes; ++l) s += box[l * width + q];
+            sums[q] = s;
+        }
+    } else {                        // several threads per channel, then one adds their sums
+        const uint32_t ways = GR_THREADS / (uint32_t)width, way = threadIdx.x / (uint32_t)width;
+        const int column = (int)(threadIdx.x - way * width);
+        float s = 0.0f;
+        if (way < ways)
+#pragma unroll 4
+            for (int l = way; l < at.lanes; l += ways) s += box[l * width + column];
+        __syncthreads();
+        if (way < ways && way > 0) box[way * width + column] = s;
+        __syncthreads();
+        if (way == 0) {
+            for (uint32_t w = 1; w < ways; ++w) s += box[w * width + column];
+            sums[column] = s;
+        }
+    }
+    __syncthreads();   // the box is used again
+}
+// The channels' two sums: sums[which][channel].
 template <int VEC>
 __device__ __forceinline__ void gn_add_lanes(const GnSpot<VEC> &at, const F2 (&a)[VEC / 2], const F2 (&b)[VEC / 2], float *box, float *sums) {
-    const int width = at.width;
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
-        if (at.lane < at.lanes) {
+        F2 mine[VEC / 2];
 #pragma unroll
-            for (int k = 0; k < VEC / 2; k += 2) {
-                const F2 v = which ? b[k] : a[k], w = which ? b[k + 1] : a[k + 1];
-                *reinterpret_cast<float4 *>(box + at.lane * width + at.chunk * VEC + 2 * k) = make_float4(lo(v), hi(v), lo(w), hi(w));
-            }
-        }
-        __syncthreads();
-        if (2 * width > GR_THREADS) {   // a thread per channel, or several channels
-            for (int q = threadIdx.x; q < width; q += GR_THREADS) {
-                float s = 0.0f;
-                for (int l = 0; l < at.lanes; ++l) s += box[l * width + q];
-                sums[which * width + q] = s;
-            }
-        } else {                        // several threads per channel, then one adds their sums
-            const uint32_t ways = GR_THREADS / (uint32_t)width, way = threadIdx.x / (uint32_t)width;
-            const int column = (int)(threadIdx.x - way * width);
-            float s = 0.0f;
-            if (way < ways)
-#pragma unroll 4
-                for (int l = way; l < at.lanes; l += ways) s += box[l * width + column];
-            __syncthreads();
-            if (way < ways && way > 0) box[way * width + column] = s;
-            __syncthreads();
-            if (way == 0) {
-                for (uint32_t w = 1; w < ways; ++w) s += box[w * width + column];
-                sums[which * width + column] = s;
-            }
-        }
-        __syncthreads();   // the box is used again
+        for (int k = 0; k < VEC / 2; ++k) mine[k] = which ? b[k] : a[k];
+        gn_add_lanes<VEC>(at, mine, box, sums + which * at.width);
     }
 }
 
@@ -169,58 +175,54 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_forward_kernel(cons
         gn_fetch(a, place_u32, x, at.lanes * a.x_pixel, at.c, q * per, min((q + 1) * per, turns));
         copy_commit();
     }
-    // sums about the image's first pixel
-    F2 s[P] = {}, t[P] = {}, minus[P] = {};
-    if (at.lane < at.lanes && at.c < a.channels) {
-        F2 v[P];
-        LnChunk<T>::read(load_chunk(image, at.c, a.channels), v);
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-            minus[k] = f2(-lo(v[k]), -hi(v[k]));
-            if (at.lane == 0) {
-                origin[at.chunk * VEC + 2 * k] = lo(v[k]);
-                origin[at.chunk * VEC + 2 * k + 1] = hi(v[k]);
-            }
-        }
-    }
+    // a thread's entries about their own mean; then all threads' about one number per channel, their mean as far as it is known then
+    GnMoments<P> m;
 #pragma unroll 1
     for (int q = 0; q < GN_PHASES; ++q) {
         gn_wait_phase(q);
+        if (q == 0 && turns > 0) m.template start<T>(place[0]);
+        const int end = min((q + 1) * per, turns);
 #pragma unroll 2
-        for (int k = q * per; k < min((q + 1) * per, turns); ++k) {
-            F2 d[P];
-            LnChunk<T>::read(place[k * GR_THREADS], d);
-#pragma unroll
-            for (int j = 0; j < P; ++j) {
-                d[j] = add(d[j], minus[j]);
-                s[j] = add(s[j], d[j]);
-                t[j] = fma(d[j], d[j], t[j]);
-            }
+        for (int k = q * per; k < end; ++k) {
+            F2 v[P];
+            LnChunk<T>::read(place[k * GR_THREADS], v);
+            m.take(v);
         }
+        if (q < 2 && end > 1) m.move((float)end, __fdividef(1.0f, (float)end));   // (the second half about the first half's mean)
     }
-    gn_add_lanes<VEC>(at, s, t, box, sums);
-    // every channel's mean (about the first pixel) and squares around it, then the groups'
+    const float entries = (float)turns, pixels = (float)a.pixels, inverse = 1.0f / pixels;
+    F2 whole[P];
+#pragma unroll
+    for (int k = 0; k < P; ++k) whole[k] = m.whole(k, entries);
+    gn_add_lanes<VEC>(at, whole, box, origin);
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+        const float2 sum = *reinterpret_cast<const float2 *>(origin + at.chunk * VEC + 2 * k);
+        m.move_to(k, f2(sum.x * inverse, sum.y * inverse), entries);
+    }
+    gn_add_lanes<VEC>(at, m.s, m.t, box, sums);
+    for (int q = threadIdx.x; q < at.width; q += GR_THREADS) origin[q] *= inverse;   // (as above)
+    // every channel's mean (about its number) and squares around it, then the groups'
     const int channels = at.channels(a), width = (int)((uint32_t)a.channels / (uint32_t)a.groups);
-    const float pixels = (float)a.pixels;
     for (int q = threadIdx.x; q < channels; q += GR_THREADS) {
         const float v = sums[q], w = sums[at.width + q];
-        const float m = v / pixels;
-        box[q] = m;
-        box[at.width + q] = fmaxf(__fmaf_rn(-v, m, w), 0.0f);
+        const float mean = v / pixels;
+        box[q] = mean;
+        box[at.width + q] = fmaxf(__fmaf_rn(-v, mean, w), 0.0f);
     }
     __syncthreads();
-    // (about the mean of the group's first channel: a far mean costs no digits)
+    // (about the first channel's number: a far mean costs no digits)
     auto off = [&](int g, int q) { return (origin[q] - origin[g * width]) + box[q]; };
     gn_over_groups<1>(channels, width, [&](int g, int q, float (&v)[1]) { v[0] += off(g, q); }, [&](int g, float (&v)[1]) { value[g] = v[0] / (float)width; });
     if (width > 16) __syncwarp();
     gn_over_groups<1>(channels, width, [&](int g, int q, float (&v)[1]) { const float o = off(g, q) - value[g]; v[0] += __fmaf_rn(pixels * o, o, box[at.width + q]); },
                       [&](int g, float (&v)[1]) {
-                          const float m = origin[g * width] + value[g], r = 1.0f / sqrtf(v[0] / (pixels * (float)width) + a.eps);
+                          const float mean = origin[g * width] + value[g], r = 1.0f / sqrtf(v[0] / (pixels * (float)width) + a.eps);
                           if (width <= 16 || (threadIdx.x & 31) == 0) {
-                              sums[2 * g] = m;
+                              sums[2 * g] = mean;
                               sums[2 * g + 1] = r;
                               const int64_t to = at.image * a.groups + (int)((uint32_t)at.c0 / (uint32_t)width) + g;
-                              a.mean[to] = m;
+                              a.mean[to] = mean;
                               a.rstd[to] = r;
                           }
                       });
