@@ -395,6 +395,9 @@ __global__ void __launch_bounds__(GN_THREADS, 2) gn_dx_kernel(const __grid_const
 // Threads of a CTA share the chunks of a tile, so that few images still give a thread 16 pixels or more (4 of a part); parts of an
 // image's pixels as there are places for CTAs (forward four on an SM, backward two), twice as many while a thread keeps
 // 64 pixels (8 x 32 images of 56 x 56 x 64 backward with six on an SM: 117 us, two: 107; 4 of 256 x 256 x 128: 94 and 76).
+// Never more than GN_CHAIN pixels to a thread, however many images there are: its sums are chains of binary32 additions, which lose up
+// to 2^-24 in each (600 images of 65,536 x 128 with 4096: a constant dy came to 7e-5 less than it is).
+constexpr int GN_CHAIN = 64;
 static void gn_plan(GnArgs &a, int vec, bool backward) {
     const int places_per_sm = backward ? 2 : 4;
     const int chunks = (int)(ck_cols(a.channels) / vec), step = CK_BLOCK / vec;
@@ -406,7 +409,7 @@ static void gn_plan(GnArgs &a, int vec, bool backward) {
     const int64_t places = (int64_t)a.workers * a.samples * a.tiles;
     const int64_t few = std::min((LN_SMS * places_per_sm + places - 1) / places, a.pixels / (lanes * 4));
     const int64_t many = std::min((LN_SMS * 2 * places_per_sm + places - 1) / places, a.pixels / (lanes * 64));
-    const int64_t parts = std::max<int64_t>(1, std::max(few, many));
+    const int64_t least = (a.pixels + lanes * GN_CHAIN - 1) / (lanes * GN_CHAIN), parts = std::max({int64_t(1), few, many, least});
     a.part_pixels = std::max<int64_t>(1, (a.pixels + parts - 1) / parts);
     a.parts = (int)std::max<int64_t>(1, (a.pixels + a.part_pixels - 1) / a.part_pixels);
 }

@@ -1,13 +1,15 @@
-"""Sums keep their digits: where the first pixel of an image, or any other, is far from all others."""
+"""Sums keep their digits: where the first pixel of an image, or any other, is far from all others, and where chains of
+additions would be long."""
+import ctypes as C
 
 import pytest
 import torch
 
-from activation_helpers import DT, U
+from activation_helpers import DT, U, restored64
 from paper_2402_11857_b200 import liec
 
 pytestmark = pytest.mark.gpu
-forward = liec.liec_group_norm_forward
+forward, backward = liec.liec_group_norm_forward, liec.liec_group_norm_backward
 
 
 def statistics64(x, groups, eps):
@@ -59,3 +61,72 @@ def test_one_pixel_far_from_all_others(pixels, where, dtype):
     x[:, :, where] = 1e4
     _, m, r = forward(x, 8)
     check_statistics(x, 8, 1e-5, m, r)
+
+
+def test_equal_squares_in_long_images():
+    """Images of so many pixels and so many of them that a thread has thousands; every square is the same number, so the roundings of
+    a chain all go the same way."""
+    pixels, ch, images = 65536, 128, 600
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    for a in (1.0003, 1.137, 0.771):
+        sign = torch.randint(0, 2, (1, 1, pixels, ch), generator=gen, device="cuda") * 2 - 1
+        x = (sign * a).float()
+        x[:, :, 0] = 0
+        _, m, r = forward(x.expand(1, images, pixels, ch), 32)
+        assert torch.equal(r, r[:, :1].expand_as(r))
+        check_statistics(x, 32, 1e-5, m[:, :1], r[:, :1])
+
+
+@pytest.mark.parametrize("source", ["x", "checkpoint"])
+def test_gradients_of_equal_terms_in_long_images(source):
+    """dy is one number everywhere, in images as above.  (dx, which would need memory, is not asked for.)  Chains of at most 64
+    additions, 64 where threads meet, the rest in binary64; 4 roundings of a term, one of the result: 134 u."""
+    pixels, ch, images, groups = 65536, 128, 600, 32
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(1, 1, pixels, ch, generator=gen, device="cuda")
+    x = x.abs() if source == "x" else torch.rand(1, 1, pixels, ch, generator=gen, device="cuda").bfloat16().float()
+    mean, rstd = torch.zeros(1, images, groups, device="cuda"), torch.full((1, images, groups), 0.7, device="cuda")
+    q, scales = liec.liec_activation_compress(x.expand(1, images, pixels, ch)) if source == "checkpoint" else (None, None)
+    read = restored64(q[:, :1], scales[:, :1], ch) if source == "checkpoint" else x.double()
+    lib = liec.load_library()
+    for c in (1.0003, 1.137, 0.771):
+        dy = torch.full((ch,), c, device="cuda")
+        dw, db = torch.empty(ch, device="cuda"), torch.empty(ch, device="cuda")
+        d = liec.liec_group_norm_desc()
+        d.workers, d.samples, d.pixels, d.channels, d.groups = 1, images, pixels, ch, groups
+        d.dtype, d.grad_dtype, d.activation = liec.F32, liec.F32, 0
+        d.x_pixel_stride = ch                                       # samples repeat
+        need = lib.liec_group_norm_workspace_bytes(C.byref(d), 1)
+        space = torch.empty(need, dtype=torch.uint8, device="cuda")
+        st = lib.liec_group_norm_backward(C.byref(d), dy.data_ptr(), x.data_ptr() if q is None else None, None if q is None else q.data_ptr(),
+                                          None if q is None else scales.data_ptr(), mean.data_ptr(), rstd.data_ptr(), None, None, None,
+                                          dw.data_ptr(), db.data_ptr(), space.data_ptr(), need, torch.cuda.current_stream().cuda_stream)
+        assert st == 0
+        c = float(dy[0])
+        want = images * c * float(rstd[0, 0, 0]) * read[0, 0].sum(0)
+        assert float(((dw.double() - want).abs() / want).max()) <= 134 * U, "dweight"
+        assert float((db.double() / (images * pixels * c) - 1).abs().max()) <= 134 * U, "dbias"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,S,pixels,ch,groups,act", [(2, 3, 49, 64, 8, "none"), (1, 2, 3136, 64, 32, "silu"), (1, 1, 9001, 40, 8, "relu"), (1, 1, 65536, 32, 4, "none"),
+                                                      (30, 40, 3136, 48, 6, "silu")])
+def test_gradients_keep_their_digits(N, S, pixels, ch, groups, act, dtype):
+    """Ordinary data.  Each sum: 64 + 64 + 8 roundings of at most u of the sum of the magnitudes, the short exponential of bfloat16 (2^-22 (4 + 2 |z|)
+    of the slope, |z| below 8: 2^-17.6), a slope's own 40 u at |z| below 8."""
+    gen = torch.Generator(device="cuda").manual_seed(ch)
+    r = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+    x, dy = (r(N, S, pixels, ch) + r(ch)).to(DT[dtype]), r(N, S, pixels, ch).to(DT[dtype])
+    w, b = 1 + 0.1 * r(N, ch), 0.1 * r(N, ch)
+    _, mean, rstd = forward(x, groups, w, b, activation=act)
+    check_statistics(x[-1:], groups, 1e-5, mean[-1:], rstd[-1:])
+    _, dw, db = backward(dy, x, mean, rstd, w, b, activation=act)
+    width = ch // groups
+    xh = (x[-1].double() - mean[-1].double().repeat_interleave(width, -1)[:, None]) * rstd[-1].double().repeat_interleave(width, -1)[:, None]
+    z = xh * w[-1].double() + b[-1].double()
+    s = torch.sigmoid(z)
+    slope = (z > 0).double() if act == "relu" else s * (1 + z * (1 - s)) if act == "silu" else torch.ones_like(z)
+    each = (136 + (40 if act == "silu" else 0)) * U + (2.0 ** -17.6 if act == "silu" and dtype == "bf16" else 0)
+    for got, term in ((dw, dy[-1].double() * slope * xh), (db, dy[-1].double() * slope)):
+        off = (got[-1].double() - term.sum((0, 1))).abs() / term.abs().sum((0, 1))
+        assert float(off.max()) <= each, f"{float(off.max()) / U:.0f} u"
