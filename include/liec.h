@@ -451,8 +451,9 @@ liec_status liec_group_norm_backward(const liec_group_norm_desc *desc, const voi
  * Weight gradient of N workers' linear layers (or 1 x 1 convolutions) from the checkpoint of their input:
  *   dW[o][c] = sum over the worker's rows t of dy[t][o] x^[t][c]
  * Products are exact (a bfloat16 dy times x^; a binary32 dy enters as three bfloat16 parts that add up to it) and are summed in
- * binary32 by the tensor cores, whose additions cut towards zero; a binary32 gradient is summed there at most 1792 rows at a time,
- * and these sums are added with rounding.  Rounded once to the gradient's type.  Equal calls give equal bits.
+ * binary32 by the tensor cores, whose additions cut towards zero; they take at most 1792 rows at a time for a binary32 gradient and
+ * 16,384 for a bfloat16 one (which cuts 2^-13 of a sum at most), and these sums are added in binary32 with rounding.  Rounded once to
+ * the gradient's type.  Equal calls give equal bits.
  *   dy        device, [workers][rows][out] of dtype
  *   q, scales device, checkpoint of x [workers][rows][in]
  *   dweight   device, [workers][out][in] of grad_dtype, overwritten (zeros without rows)

@@ -114,15 +114,11 @@ __device__ __forceinline__ void wg_add_column(float *to, int64_t step, int outpu
         if (e < outputs) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(to + e * step), "f"(v[e]) : "memory");
 }
 
-// Stages of an item that one sum in tensor memory takes.  The products' additions there cut what does not fit: always
-// towards zero, which over 8192 tokens comes to 6e-6 of a gradient (measured), ten times what rounded additions lose.  So a
-// binary32 gradient is summed there 1792 tokens at a time at most, and these sums are added with rounding: 8e-7.  Each such
-// sum takes 10 us, 5 of them an SM's way out for its 256 KB: 8 x 8192 x 768 x 2304 takes 242 us (186 in one sum, 203 with 4096
-// tokens and 2.5e-6, 233 with 2048 and 1.2e-6).  A bfloat16 gradient keeps 2^-9 anyway, and is summed at once.
-constexpr int WG_SUM_STAGES = 56;
+// Stages of each sum of an item.
 __device__ __forceinline__ int wg_sum_stages(const WgArgs &a, int stages) {
-    if (a.grad_dtype != LIEC_F32 || stages <= WG_SUM_STAGES) return stages;
-    const int sums = (stages + WG_SUM_STAGES - 1) / WG_SUM_STAGES;
+    const int most = a.grad_dtype == LIEC_F32 ? WG_SUM_STAGES : WG_SUM_STAGES_BF16;
+    if (stages <= most) return stages;
+    const int sums = (stages + most - 1) / most;
     return (stages + sums - 1) / sums;
 }
 
@@ -419,17 +415,18 @@ __global__ void __launch_bounds__(WG_THREADS, 1) wg_kernel(const __grid_constant
     if (warp == WG_WIDENERS / 32 + 1) tc_free_pair(tmem, S::COLUMNS);
 }
 
-// A cut tile's runs, added in their order and rounded once to the gradient's type.  Block (x, y) has 4 outputs of cut tile y,
-// a thread 4 channels of one: many threads with eight loads under way each (16 outputs per block, four loads: 13 us for six
+// A cut tile's runs, added in their order and rounded once to the gradient's type.  A block has 4 outputs of a cut tile, a thread 4
+// channels of one: many threads with eight loads under way each (16 outputs per block, four loads: 13 us for six
 // tiles in 11 and 5 runs, now 7).
 constexpr int WG_JOIN_OUTPUTS = 4;
 __global__ void __launch_bounds__(256) wg_join_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ WgPlan p) {
-    const int64_t cut = p.runs > 1 ? p.full - p.whole : 0;
-    const bool is_last = blockIdx.y >= cut;
-    const int64_t index = is_last ? blockIdx.y - cut : blockIdx.y, tiles = is_last ? p.last : cut, size = p.slot_size(is_last);
+    const uint32_t blocks = (uint32_t)p.slabs * WG_SLAB / WG_JOIN_OUTPUTS, tile = blockIdx.x / blocks, block = blockIdx.x - tile * blocks;
+    const int64_t cut = p.cut_joins() ? p.full - p.whole : 0;
+    const bool is_last = tile >= cut;
+    const int64_t index = is_last ? tile - cut : tile, tiles = is_last ? p.last : cut, size = p.slot_size(is_last);
     const WgItem t = p.tile_of((is_last ? p.full : p.whole) + index);
     const int runs = is_last ? p.last_runs : p.runs, lane = threadIdx.x % 64, c = t.c_tile * 2 * WG_CHANNELS + lane * 4;
-    const int row = blockIdx.x * WG_JOIN_OUTPUTS + threadIdx.x / 64, o = t.o_tile * p.slabs * WG_SLAB + row;
+    const int row = (int)block * WG_JOIN_OUTPUTS + threadIdx.x / 64, o = t.o_tile * p.slabs * WG_SLAB + row;
     const float4 *from = reinterpret_cast<const float4 *>(a.part + index * size + (is_last ? cut * p.runs * p.slot_size(false) : 0) + row * 2 * WG_CHANNELS + lane * 4);
     const int64_t step = tiles * size / 4;
     asm volatile("griddepcontrol.wait;" ::: "memory");   // the sums are complete
@@ -475,7 +472,7 @@ size_t weight_grad_workspace(const WgArgs &a, int dtype) {
     if (a.rows == 0) return 0;
     const int vec = dtype == 0 ? 4 : 8;
     const size_t packed = wg_direct(a, dtype) ? 0 : (size_t)a.workers * a.rows * ((a.out + vec - 1) / vec) * 16;
-    return wg_part_bytes(wg_plan(a.workers, a.rows, a.in, a.out, dtype)) + packed;
+    return wg_part_bytes(wg_plan(a.workers, a.rows, a.in, a.out, dtype, a.grad_dtype == LIEC_BF16)) + packed;
 }
 
 // The function behind cuTensorMapEncodeTiled: asked of the runtime, so that the library links without the driver's.
@@ -542,7 +539,7 @@ cudaError_t launch_weight_grad(WgArgs a, int dtype, cudaStream_t st) {
         wg_zero_kernel<<<(unsigned)(((int64_t)a.workers * a.out * a.in + 255) / 256), 256, 0, st>>>(a);
         return cudaGetLastError();
     }
-    const WgPlan p = wg_plan(a.workers, a.rows, a.in, a.out, dtype);
+    const WgPlan p = wg_plan(a.workers, a.rows, a.in, a.out, dtype, a.grad_dtype == LIEC_BF16);
     const bool direct = wg_direct(a, dtype);
     const int size = dtype == 0 ? 4 : 2, vec = 16 / size, box = dtype == 0 ? 128 : 64;
     const int64_t q_cols = ck_cols(a.in), dy_cols = (a.out + vec - 1) / vec * vec;
@@ -560,10 +557,9 @@ cudaError_t launch_weight_grad(WgArgs a, int dtype, cudaStream_t st) {
         if (e != cudaSuccess) return e;
     }
     e = dtype == 0 ? wg_launch<3>(a, p, q_map, dy_map, !direct, st) : wg_launch<1>(a, p, q_map, dy_map, !direct, st);
-    const int64_t joined = (p.runs > 1 ? p.full - p.whole : 0) + (p.last_runs > 1 ? p.last : 0);
+    const int64_t joined = (p.cut_joins() ? p.full - p.whole : 0) + (p.last_joins() ? p.last : 0);
     if (e != cudaSuccess || joined == 0) return e;
-    cudaLaunchConfig_t cfg = wg_config(p.slabs * WG_SLAB / WG_JOIN_OUTPUTS, 256, 0, st);
-    cfg.gridDim.y = (unsigned)joined;
+    cudaLaunchConfig_t cfg = wg_config(joined * (p.slabs * WG_SLAB / WG_JOIN_OUTPUTS), 256, 0, st);
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;

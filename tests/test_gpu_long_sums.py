@@ -1,11 +1,11 @@
-"""Sums keep their digits: where the first pixel of an image, or any other, is far from all others, and where chains of
-additions would be long."""
+"""Sums keep their digits: where the first pixel of an image, or any other, is far from all others, where chains of
+additions would be long, and where what the tensor cores cut would add up."""
 import ctypes as C
 
 import pytest
 import torch
 
-from activation_helpers import DT, U, restored64
+from activation_helpers import DT, U, U_BF, check_weight_grad, restored64
 from paper_2402_11857_b200 import liec
 
 pytestmark = pytest.mark.gpu
@@ -130,3 +130,40 @@ def test_gradients_keep_their_digits(N, S, pixels, ch, groups, act, dtype):
     for got, term in ((dw, dy[-1].double() * slope * xh), (db, dy[-1].double() * slope)):
         off = (got[-1].double() - term.sum((0, 1))).abs() / term.abs().sum((0, 1))
         assert float(off.max()) <= each, f"{float(off.max()) / U:.0f} u"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1 << 16, 1 << 20])
+def test_bfloat16_weight_gradients_of_many_tokens(rows, dtype):
+    """Positive terms, a tile for every pair of SMs, so that no plan cuts them.  At most 1024 additions (of 16 products each) to a sum in tensor
+    memory, each cutting less than 2 u of it: 2048 u = 2^-13; these sums are added with rounding, at most 64 of them.  Then half a
+    bfloat16 step.  On the average over the 18,944 outputs what is cut stays: against the outputs' own roundings, an output is a step of
+    2^-8 lower where a border between steps lies within what was cut from it.  The outputs of 2^16 tokens are spread by 107 around 2^16, a step
+    below which is 256, so that the share of them between two places is at most 0.4 / 107 of the distance: at most 0.4 / 107 x 256 = 0.96 of 2^-13 on the
+    average, and six standard deviations of that count (at most 290) are 2e-5.  (The outputs' own roundings have an average that is not zero, as
+    nearly all of them lie less than two steps from 2^16: 3.9e-4.)"""
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    dy = (torch.rand(74, rows, 8, generator=gen, device="cuda") + 0.5).to(DT[dtype])
+    q, scales = liec.liec_activation_compress((torch.rand(74, rows, 32, generator=gen, device="cuda") + 0.5).bfloat16())
+    got = liec.liec_weight_grad(dy, q, scales, 32, dweight=torch.empty(74, 8, 32, dtype=torch.bfloat16, device="cuda")).double()
+    want = torch.stack([dy[n].double().t() @ restored64(q[n], scales[n], 32) for n in range(74)])
+    off = got / want - 1
+    assert float(off.abs().max()) <= U_BF + 2.0 ** -13 + 64 * U
+    assert abs(float((off - (want.to(torch.bfloat16).double() / want - 1)).mean())) <= 2.0 ** -13 + 64 * U + 2e-5
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,rows,h,out", [(1, 16385, 40, 30), (2, 40000, 300, 600), (75, 16500, 33, 520), (160, 17000, 20, 8)])
+def test_bfloat16_weight_gradients_through_the_workspace(N, rows, h, out, dtype):
+    """Tiles of one run and of several, full ones and those with fewer outputs: what lies beside the gradient is left alone, equal calls give
+    equal bits."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    dy = torch.randn(N, rows, out, generator=gen, device="cuda").to(DT[dtype])
+    q, scales = liec.liec_activation_compress(torch.randn(N, rows, h, generator=gen, device="cuda").bfloat16())
+    grads = torch.full((N, out * h + 9), 5.0, dtype=torch.bfloat16, device="cuda")
+    got = liec.liec_weight_grad(dy, q, scales, h, dweight=grads[:, 4:4 + out * h].unflatten(1, (out, h)))
+    for n in (0, N - 1):
+        check_weight_grad(dy[n:n + 1], restored64(q[n:n + 1], scales[n:n + 1], h), "bf16", got[n:n + 1])
+    assert (grads[:, :4] == 5).all() and (grads[:, -5:] == 5).all()
+    again = liec.liec_weight_grad(dy, q, scales, h, dweight=torch.empty(N, out, h, dtype=torch.bfloat16, device="cuda"))
+    assert torch.equal(again, got)
