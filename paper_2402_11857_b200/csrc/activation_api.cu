@@ -220,9 +220,9 @@ liec_status liec_group_norm_backward(const liec_group_norm_desc *d, const void *
                           "workspace smaller than liec_group_norm_workspace_bytes()");
         if (st != LIEC_OK) return st;
     }
-    Axes in[6], out[3];
+    Axes in[7], out[3];   // (x, or q and scales)
     int ins = 0, outs = 0;
-    const int64_t rows = (int64_t)d->workers * d->samples * d->pixels;
+    const int64_t rows = (int64_t)d->workers * d->samples * d->pixels, stats = (int64_t)d->workers * d->samples * d->groups;
     if (any) {
         in[ins++] = images(d, dy, d->y_worker_stride, d->y_sample_stride, d->y_pixel_stride);
         if (x) in[ins++] = images(d, x, d->x_worker_stride, d->x_sample_stride, d->x_pixel_stride);
@@ -232,6 +232,8 @@ liec_status liec_group_norm_backward(const liec_group_norm_desc *d, const void *
         }
         if (weight) in[ins++] = vectors(weight, d->weight_stride, d->workers, d->channels, 4);
         if (bias) in[ins++] = vectors(bias, d->bias_stride, d->workers, d->channels, 4);
+        in[ins++] = axes_of(mean, stats, 4, {}, {});
+        in[ins++] = axes_of(rstd, stats, 4, {}, {});
         if (dx) out[outs++] = images(d, dx, d->dx_worker_stride, d->dx_sample_stride, d->dx_pixel_stride);
     }
     if (dweight) out[outs++] = vectors(dweight, d->dweight_stride, count, d->channels, grad);
