@@ -397,11 +397,14 @@ liec_status liec_activation_restore(const liec_activation_desc *desc, const int8
  * of the entries so far, so neither a far mean nor a single entry far from the others costs digits of r; m is stored as a
  * binary32 number, and a mean of k deviations so leaves errors of up to k 2^-24 in xh.  Entries whose squares leave binary32
  * (beyond about 1e18) are not provided for.  On which side of zero a ReLU's z lies is decided as in binary64 from the given x,
- * mean, rstd, w and b.  Equal calls give equal bits (no atomics).  A group with an infinity or NaN gives NaN in that group of that image, and in dw and db of its channels.
+ * mean, rstd, w and b.  Equal calls give equal bits (no atomics).  A group with an infinity or NaN gives NaN in y and dx of that
+ * group of that image and in dw of its channels.  db is the sum of dz alone: NaN with SiLU; with ReLU a z that is NaN counts as not
+ * above zero, and without an activation db does not see x.
  *
  * The forward pass can leave the checkpoint of x (q and scales, as liec_activation_compress of its [workers][samples pixels]
  * [channels] rows would) from the same read of x, and the backward pass can read the checkpoint in place of x: the formulas
- * then hold with x^ for x and with mean and rstd as given.  Alignment, strides and overlaps as above.
+ * then hold with x^ for x and with mean and rstd as given (a NaN there is one of all 32 channels of its block).  Alignment, strides
+ * and overlaps as above.
  */
 typedef enum { LIEC_ACT_NONE = 0, LIEC_ACT_RELU = 1, LIEC_ACT_SILU = 2 } liec_activation;
 #define LIEC_GROUP_NORM_MAX_CHANNELS 65536
