@@ -664,7 +664,10 @@ def _gn_backward(raw, device, dy, x, q, scales, mean, rstd, weight, bias, activa
     if dx is None:
         dx = _empty_like(dy)
     if dweight is None or dbias is None:
-        like = next((t for t in (dweight, dbias, weight, bias) if t is not None), None)
+        # (a vector that all workers share beside one of their own: gradients per worker)
+        like = next((t for t in (dweight, dbias) if t is not None), None)
+        if like is None:
+            like = max((t for t in (weight, bias) if t is not None), key=lambda t: t.dim(), default=None)
         shape = like.shape if like is not None else dy.shape[:-3] + dy.shape[-1:]
         dtype = next((t.dtype for t in (dweight, dbias) if t is not None), torch.float32)
         dweight = _empty(shape, dtype, device) if dweight is None else dweight
@@ -684,8 +687,8 @@ def liec_group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, activati
                              workspace=None, stream=None):
     """Gradients of liec_group_norm_forward.  x: the activations, or their checkpoint as a pair (q, scales).  dweight and
     dbias: [N, channels] float32 or bfloat16 (any stride between workers, e.g. ``grads[:, a:a + c]``), or [channels] for a
-    vector that all workers share (its gradient is summed over the workers too); allocated in float32, shaped like weight, where not
-    given.  Returns (dx, dweight, dbias)."""
+    vector that all workers share (its gradient is summed over the workers too); allocated in float32, shaped like weight and bias
+    (per worker where one of them is), where not given.  Returns (dx, dweight, dbias)."""
     import torch
     device = _device_of("dy", dy)
     x, q, scales = (x, None, None) if torch.is_tensor(x) else (None, *x)
