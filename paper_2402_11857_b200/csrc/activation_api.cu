@@ -65,7 +65,7 @@ liec_status check(const liec_group_norm_desc *d) {
     if (d->channels % d->groups != 0) return invalid("group norm: groups must divide channels");
     if (d->workers > 65535) return unsupported("group norm: workers above 65535");
     if (d->pixels >= MAX_ROWS) return unsupported("group norm: pixels must be below 2^31");
-    if ((int64_t)d->workers * d->samples > (int64_t(1) << 31) / d->channels) return unsupported("group norm: images times channels above 2^31 (launch grid)");
+    if ((int64_t)d->workers * d->samples > ((int64_t(1) << 31) - (d->channels == 1)) / d->channels) return unsupported("group norm: images times channels above 2^31, or 2^31 images (launch grid)");
     if ((int64_t)d->workers * d->samples > 0 && d->pixels > (int64_t(1) << 40) / ((int64_t)d->workers * d->samples * d->channels))
         return unsupported("group norm: more than 2^40 elements");
     if (!known(d->dtype) || !known(d->grad_dtype)) return invalid("group norm: unknown dtype");
