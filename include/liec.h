@@ -360,7 +360,8 @@ liec_status liec_layer_norm_backward(const liec_layer_norm_desc *desc, const voi
  *   x^ = q 2^e
  * (e is 121 at most and q held to +-127 there, so that x^ is finite.)  x^ is exact in binary32 and in bfloat16;
  * |x - x^| <= 2^(e-1) (2^e for e = 121), which is at most max |x| / 127 where max |x| >= 2^-120.  A block with an infinity or
- * NaN gets the byte 255 and q = 0 and comes back as NaN.  33 bytes per 32 channels.
+ * NaN gets the byte 255 and q = 0 and comes back as NaN.  33 bytes per 32 channels, begun ones included: rows of up to 16 bfloat16
+ * or 8 binary32 channels take less as they are.
  *
  * No context is needed here either.  Strides are in elements and >= 0, the last axis of every array is contiguous, any
  * element alignment is accepted (16-byte aligned rows are faster) unless said otherwise; rows that are read may overlap or
@@ -453,10 +454,10 @@ liec_status liec_group_norm_backward(const liec_group_norm_desc *desc, const voi
 /*
  * Weight gradient of N workers' linear layers (or 1 x 1 convolutions) from the checkpoint of their input:
  *   dW[o][c] = sum over the worker's rows t of dy[t][o] x^[t][c]
- * Products are exact (a bfloat16 dy times x^; a binary32 dy enters as three bfloat16 parts that add up to it) and are summed in
- * binary32 by the tensor cores, whose additions cut towards zero; they take at most 1792 rows at a time for a binary32 gradient and
- * 16,384 for a bfloat16 one (which cuts 2^-13 of a sum at most), and these sums are added in binary32 with rounding.  Rounded once to
- * the gradient's type.  Equal calls give equal bits.
+ * Products are exact (a bfloat16 dy times x^; a binary32 dy enters as three bfloat16 parts that add up to it, but for what of it
+ * lies below 2^-133) and are summed in binary32 by the tensor cores, whose additions cut towards zero; they take at most 1792 rows
+ * at a time for a binary32 gradient and 16,384 for a bfloat16 one (which cuts 2^-13 of a sum at most), and these sums are added in
+ * binary32 with rounding.  Rounded once to the gradient's type.  Equal calls give equal bits.
  *   dy        device, [workers][rows][out] of dtype
  *   q, scales device, checkpoint of x [workers][rows][in]
  *   dweight   device, [workers][out][in] of grad_dtype, overwritten (zeros without rows)

@@ -534,7 +534,7 @@ def _activation_call(raw, device, compress, x, q, scales, shape, dtype):
 
 def liec_activation_compress(x, q=None, scales=None, stream=None):
     """8-bit checkpoint of activations [..., h] (float32 or bfloat16, at least two axes): every 32 consecutive channels as
-    signed bytes and one power of two.  Returns (q, scales): int8 [..., liec_activation_cols(h)] and uint8 [..., the same / 32]."""
+    signed bytes and one power of two, the last of a row filled up (so rows of a few channels only grow).  Returns (q, scales): int8 [..., liec_activation_cols(h)] and uint8 [..., the same / 32]."""
     device = _device_of("x", x)
     _same_device(device, q=q, scales=scales)
     if x.dim() < 2:
