@@ -11,8 +11,9 @@
 // of a product.  Lanes of the accumulator are channels, so a warp writes 32 neighbours of a row of dW.
 //
 // What bounds it: shared memory (bytes in, widened bytes out and in again, and the products' own reads share 128 bytes a cycle) and,
-// where sums leave tensor memory, an SM's way out, 27 bytes a cycle.  16 x 3136 tokens of 512 x 2048 into bfloat16: 85 us, 1.24
-// PFLOP/s; 8 x 8192 of 768 x 2304 into binary32: 242 us, 0.96; binary32 dy, 8 x 4096 of 1024 x 1024: 184 us, three times 0.37.
+// where sums leave tensor memory, an SM's way out, 27 bytes a cycle.  In bursts at 1965 MHz: 16 x 3136 tokens of 512 x 2048 into
+// bfloat16 86 us, 1.22 PFLOP/s; 8 x 8192 of 768 x 2304 into binary32 241 us, 0.96; binary32 dy, 8 x 4096 of 1024 x 1024, 184 us, three times
+// 0.37.  (In a loop of seconds the power cap holds the SMs at 1425 to 1580 MHz: 104 and 284 us.)
 #include <cuda.h>
 
 #include <algorithm>
@@ -67,7 +68,7 @@ __device__ __forceinline__ void wg_widen(uint4 q, uint32_t byte, uint4 (&out)[2]
 }
 
 // x = p[0] + p[1] + p[2], each the upper half of a binary32 number: 8 bits of the significand at a time (what lies below the last
-// is zero).  An infinity or NaN would leave NaN as rest.
+// is zero; next to the end of the range it is not, and what of x lies below 2^-133 is cut).  An infinity or NaN would leave NaN as rest.
 __device__ __forceinline__ void wg_split(float x, uint32_t (&p)[3]) {
     p[0] = __float_as_uint(x) & 0xffff0000u;
     const float rest = x - __uint_as_float(p[0]);
