@@ -161,30 +161,46 @@ __device__ __forceinline__ double gn_sum_lanes(double v) {
     return v;
 }
 
-// Joins a group's channels and parts, in binary64 and in a fixed order.
+// Joins a group's channels and parts, in binary64 and in a fixed order: about one of their means, which is one of `entries`, so the squares about
+// it are at most that many times those about the mean of all.
 template <int LANES>
 __global__ void __launch_bounds__(GN_THREADS) gn_statistics_kernel(const __grid_constant__ GnArgs a) {
     gn_wait_for_kernel_before();
     gn_per_group<LANES>(a, [&](bool live, uint32_t image, uint32_t group, uint32_t lane) {
         const uint32_t width = (uint32_t)a.channels / (uint32_t)a.groups, entries = live ? width * a.parts : 0u;
         const float *part = a.part + (int64_t)image * a.parts * GN_FORWARD_PARTS * a.channels + group * width;
-        const double n = (double)a.pixels * width;
-        auto each = [&](auto &&f) {   // channel's mean, squares around it, number of pixels
-#pragma unroll 4
-            for (uint32_t i = lane; i < entries; i += LANES) {
-                const uint32_t q = i / width;
-                const float *at = part + (int64_t)q * GN_FORWARD_PARTS * a.channels + (i - q * width);
-                f((double)at[0] + (double)at[a.channels], (double)at[2 * a.channels], (double)min(a.part_pixels, a.pixels - q * a.part_pixels));
-            }
-        };
+        const double n = (double)a.pixels * width, about = live ? (double)part[0] : 0.0;
+        const double pixels = (double)a.part_pixels, last_pixels = (double)(a.pixels - (a.parts - 1) * a.part_pixels);
         double s = 0.0, t = 0.0;
-        each([&](double mean, double, double count) { s += count * mean; });
-        const double mean = gn_sum_lanes<LANES>(s) / n;
-        each([&](double m, double squares, double count) { t += squares + count * (m - mean) * (m - mean); });
-        const double var = gn_sum_lanes<LANES>(t) / n;
+        constexpr uint32_t BATCH = 4;   // entries whose loads are under way together
+        for (uint32_t first = lane; first < entries; first += BATCH * LANES) {
+            float mean[BATCH], left[BATCH], squares[BATCH];
+            uint32_t q[BATCH];
+#pragma unroll
+            for (uint32_t k = 0; k < BATCH; ++k) {
+                const uint32_t i = first + k * LANES;
+                q[k] = i / width;
+                if (i < entries) {
+                    const float *at = part + (int64_t)q[k] * GN_FORWARD_PARTS * a.channels + (i - q[k] * width);
+                    mean[k] = at[0];
+                    left[k] = at[a.channels];
+                    squares[k] = at[2 * a.channels];
+                }
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < BATCH; ++k)
+                if (first + k * LANES < entries) {
+                    const double d = ((double)mean[k] - about) + (double)left[k], count = q[k] + 1 == (uint32_t)a.parts ? last_pixels : pixels;
+                    s += count * d;
+                    t += (double)squares[k] + count * d * d;
+                }
+        }
+        s = gn_sum_lanes<LANES>(s);
+        t = gn_sum_lanes<LANES>(t);
         if (live && lane == 0) {
-            a.mean[(int64_t)image * a.groups + group] = (float)mean;
-            a.rstd[(int64_t)image * a.groups + group] = 1.0f / sqrtf((float)var + a.eps);
+            const double var = (t - s * s / n) / n;
+            a.mean[(int64_t)image * a.groups + group] = (float)(about + s / n);
+            a.rstd[(int64_t)image * a.groups + group] = 1.0f / sqrtf((var < 0.0 ? 0.0f : (float)var) + a.eps);   // (NaN stays)
         }
     });
 }
