@@ -75,6 +75,15 @@ __device__ __forceinline__ void gn_add_lanes(const GnSpot<VEC> &at, const F2 (&m
     }
     __syncthreads();   // the box is used again
 }
+// Sums over a warp's pixel lanes, in all of its threads: 4, 8 or 16 chunks, so that lanes are neighbours in it.
+template <int P>
+__device__ __forceinline__ void gn_add_warp_lanes(F2 (&v)[P], int chunks) {
+#pragma unroll
+    for (int m = 4; m < 32; m <<= 1)
+        if (m >= chunks)
+#pragma unroll
+            for (int k = 0; k < P; ++k) v[k] = add(v[k], F2{__shfl_xor_sync(0xffffffffu, v[k].v, m)});
+}
 // The channels' two sums: sums[which][channel].
 template <int VEC>
 __device__ __forceinline__ void gn_add_lanes(const GnSpot<VEC> &at, const F2 (&a)[VEC / 2], const F2 (&b)[VEC / 2], float *box, float *sums) {
@@ -194,33 +203,79 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_forward_kernel(cons
     F2 whole[P];
 #pragma unroll
     for (int k = 0; k < P; ++k) whole[k] = m.whole(k, entries);
-    gn_add_lanes<VEC>(at, whole, box, origin);
-#pragma unroll
-    for (int k = 0; k < P; ++k) {
-        const float2 sum = *reinterpret_cast<const float2 *>(origin + at.chunk * VEC + 2 * k);
-        m.move_to(k, f2(sum.x * inverse, sum.y * inverse), entries);
-    }
-    gn_add_lanes<VEC>(at, m.s, m.t, box, sums);
-    for (int q = threadIdx.x; q < at.width; q += GR_THREADS) origin[q] *= inverse;   // (as above)
-    // every channel's mean (about its number) and squares around it, then the groups'
     const int channels = at.channels(a), width = (int)((uint32_t)a.channels / (uint32_t)a.groups);
-    for (int q = threadIdx.x; q < channels; q += GR_THREADS) {
-        const float v = sums[q], w = sums[at.width + q];
-        const float mean = v / pixels;
-        box[q] = mean;
-        box[at.width + q] = fmaxf(__fmaf_rn(-v, mean, w), 0.0f);
+    // every channel's mean (about its number) and squares around it
+    auto channel = [&](int q, float left, float squares) {
+        const float mean = left * inverse;
+        sums[q] = mean;
+        sums[at.width + q] = fmaxf(__fmaf_rn(-left, mean, squares), 0.0f);
+    };
+    const int chunks = a.tile_chunks;
+    if (chunks == 4 || chunks == 8 || chunks == 16) {   // a warp's lanes meet by shuffles: two or three barriers in place of a dozen
+        constexpr int WARPS = GR_THREADS / 32;
+        const int warp = threadIdx.x / 32, first = at.chunk * VEC;
+        const bool writes = (int)(threadIdx.x & 31) < chunks;
+        auto put = [&](float *plane, const F2 (&v)[P]) {
+#pragma unroll
+            for (int k = 0; k < P; k += 2)
+                if (writes) *reinterpret_cast<float4 *>(plane + warp * at.width + first + 2 * k) = make_float4(lo(v[k]), hi(v[k]), lo(v[k + 1]), hi(v[k + 1]));
+        };
+        gn_add_warp_lanes(whole, chunks);
+        put(box, whole);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            F2 sum = f2(0.0f);
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                const float2 v = *reinterpret_cast<const float2 *>(box + w * at.width + first + 2 * k);
+                sum = add(sum, f2(v.x, v.y));
+            }
+            sum = mul(sum, f2(inverse));
+            if (at.lane == 0) *reinterpret_cast<float2 *>(origin + first + 2 * k) = make_float2(lo(sum), hi(sum));
+            m.move_to(k, sum, entries);
+        }
+        float *planes = box + WARPS * at.width;   // (three of them, where they fit)
+        if (chunks > 8) {
+            planes = box;
+            __syncthreads();
+        }
+        gn_add_warp_lanes(m.s, chunks);
+        gn_add_warp_lanes(m.t, chunks);
+        put(planes, m.s);
+        put(planes + WARPS * at.width, m.t);
+        __syncthreads();
+        for (int q = threadIdx.x; q < channels; q += GR_THREADS) {
+            float left = 0.0f, squares = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                left += planes[w * at.width + q];
+                squares += planes[(WARPS + w) * at.width + q];
+            }
+            channel(q, left, squares);
+        }
+    } else {
+        gn_add_lanes<VEC>(at, whole, box, origin);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const float2 sum = *reinterpret_cast<const float2 *>(origin + at.chunk * VEC + 2 * k);
+            m.move_to(k, f2(sum.x * inverse, sum.y * inverse), entries);
+        }
+        gn_add_lanes<VEC>(at, m.s, m.t, box, sums);
+        for (int q = threadIdx.x; q < at.width; q += GR_THREADS) origin[q] *= inverse;   // (as above)
+        for (int q = threadIdx.x; q < channels; q += GR_THREADS) channel(q, sums[q], sums[at.width + q]);
     }
     __syncthreads();
-    // (about the first channel's number: a far mean costs no digits)
-    auto off = [&](int g, int q) { return (origin[q] - origin[g * width]) + box[q]; };
+    // the groups', about the first channel's number: a far mean costs no digits
+    auto off = [&](int g, int q) { return (origin[q] - origin[g * width]) + sums[q]; };
     gn_over_groups<1>(channels, width, [&](int g, int q, float (&v)[1]) { v[0] += off(g, q); }, [&](int g, float (&v)[1]) { value[g] = v[0] / (float)width; });
     if (width > 16) __syncwarp();
-    gn_over_groups<1>(channels, width, [&](int g, int q, float (&v)[1]) { const float o = off(g, q) - value[g]; v[0] += __fmaf_rn(pixels * o, o, box[at.width + q]); },
+    gn_over_groups<1>(channels, width, [&](int g, int q, float (&v)[1]) { const float o = off(g, q) - value[g]; v[0] += __fmaf_rn(pixels * o, o, sums[at.width + q]); },
                       [&](int g, float (&v)[1]) {
                           const float mean = origin[g * width] + value[g], r = 1.0f / sqrtf(v[0] / (pixels * (float)width) + a.eps);
                           if (width <= 16 || (threadIdx.x & 31) == 0) {
-                              sums[2 * g] = mean;
-                              sums[2 * g + 1] = r;
+                              box[2 * g] = mean;
+                              box[2 * g + 1] = r;
                               const int64_t to = at.image * a.groups + (int)((uint32_t)at.c0 / (uint32_t)width) + g;
                               a.mean[to] = mean;
                               a.rstd[to] = r;
@@ -231,8 +286,8 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_forward_kernel(cons
     GnChannels<P> ch;
     const uint32_t first_group = (uint32_t)at.c0 / (uint32_t)width;
     ch.read(a, at.worker, at.c, [&](uint32_t g, float &m, float &r) {
-        m = sums[2 * (g - first_group)];
-        r = sums[2 * (g - first_group) + 1];
+        m = box[2 * (g - first_group)];
+        r = box[2 * (g - first_group) + 1];
     });
     T *y = static_cast<T *>(a.y) + at.worker * a.y_worker + at.sample * a.y_sample + at.p0 * a.y_pixel;
     const GnCompressor<T> checkpoint(a, at.image * a.pixels + at.p0, at.lanes, at.c);
