@@ -43,6 +43,8 @@ struct GnArgs {   // an image is a worker's sample; strides in elements
     float eps;
     int32_t parts, tiles, tile_chunks;   // of an image's pixels; of its channels, each of tile_chunks 16-byte chunks
     int64_t part_pixels;
+    int32_t again_parts;          // as cut for the second reading
+    int64_t again_pixels;
     int32_t whole, whole_out;     // rows that are read, rows that are written, start on 16 bytes
     int32_t turns;                // resident images: chunks of a thread
 };

@@ -425,10 +425,21 @@ static void gn_plan(GnArgs &a, int vec, bool backward) {
     const int64_t places = (int64_t)a.workers * a.samples * a.tiles;
     const int64_t few = std::min((LN_SMS * places_per_sm + places - 1) / places, a.pixels / (lanes * 4));
     const int64_t many = std::min((LN_SMS * 2 * places_per_sm + places - 1) / places, a.pixels / (lanes * 64));
-    const int64_t least = (a.pixels + lanes * GN_CHAIN - 1) / (lanes * GN_CHAIN), parts = std::max({int64_t(1), few, many, least});
-    a.part_pixels = std::max<int64_t>(1, (a.pixels + parts - 1) / parts);
-    a.parts = (int)std::max<int64_t>(1, (a.pixels + a.part_pixels - 1) / a.part_pixels);
+    const int64_t again = std::max({int64_t(1), few, many}), parts = std::max(again, (a.pixels + lanes * GN_CHAIN - 1) / (lanes * GN_CHAIN));
+    const auto cut = [&](int64_t into, int64_t &pixels, int32_t &number) {
+        pixels = std::max<int64_t>(1, (a.pixels + into - 1) / into);
+        number = (int32_t)std::max<int64_t>(1, (a.pixels + pixels - 1) / pixels);
+    };
+    cut(parts, a.part_pixels, a.parts);
+    cut(again, a.again_pixels, a.again_parts);
 }
+// What the kernels of the second reading get; it sums nothing, so its parts may be long.
+static GnArgs gn_again(GnArgs a) {
+    a.parts = a.again_parts;
+    a.part_pixels = a.again_pixels;
+    return a;
+}
+static int64_t gn_ctas(const GnArgs &a) { return (int64_t)a.workers * a.samples * a.tiles * a.parts; }
 
 static size_t gn_streamed_workspace(GnArgs a, int dtype, bool backward) {
     gn_plan(a, dtype == 0 ? 4 : 8, backward);
@@ -498,12 +509,12 @@ struct GnForwardLaunch {
     cudaError_t operator()() {
         constexpr int RING = WHOLE ? GnRing<16>::SIZE : 0;
         constexpr auto moments = gn_moments_kernel<T, WHOLE>;
-        const int64_t ctas = (int64_t)a.workers * a.samples * a.tiles * a.parts;
+        const GnArgs again = gn_again(a);
         cudaError_t e = gn_allow<moments>(RING + 40 * 1024);
-        if (e == cudaSuccess) e = gn_launch(moments, ctas, RING, false, st, a);
+        if (e == cudaSuccess) e = gn_launch(moments, gn_ctas(a), RING, false, st, a);
         if (e == cudaSuccess) e = gn_for_lanes(gn_group_lanes(a), [&](auto lanes) { return gn_launch(gn_statistics_kernel<decltype(lanes)::value>, gn_group_ctas(a), 0, true, st, a); });
         if (e != cudaSuccess) return e;
-        return gn_launch(a.q ? gn_apply_kernel<T, WHOLE, ACT, true> : gn_apply_kernel<T, WHOLE, ACT, false>, ctas, RING, true, st, a);
+        return gn_launch(a.q ? gn_apply_kernel<T, WHOLE, ACT, true> : gn_apply_kernel<T, WHOLE, ACT, false>, gn_ctas(again), RING, true, st, again);
     }
 };
 
@@ -527,13 +538,14 @@ struct GnBackwardLaunch {
         constexpr int RING = WHOLE ? GnRing<16>::SIZE + GnRing<X::CHECKPOINT ? Bits<T>::VEC : 16>::SIZE : 0;
         constexpr auto slopes = gn_slopes_kernel<T, WHOLE, X, ACT>;
         constexpr auto dx = gn_dx_kernel<T, WHOLE, X, ACT>;
-        const int64_t ctas = (int64_t)a.workers * a.samples * a.tiles * a.parts, levels = a.dx ? gn_group_ctas(a) : 0;
+        const GnArgs again = gn_again(a);
+        const int64_t levels = a.dx ? gn_group_ctas(a) : 0;
         cudaError_t e = gn_allow<slopes>(RING + 40 * 1024);
         if (e == cudaSuccess) e = gn_allow<dx>(RING + 40 * 1024);
-        if (e == cudaSuccess) e = gn_launch(slopes, ctas, RING, false, st, a);
+        if (e == cudaSuccess) e = gn_launch(slopes, gn_ctas(a), RING, false, st, a);
         if (e == cudaSuccess) 
             e = gn_for_lanes(gn_group_lanes(a), [&](auto lanes) { return gn_launch(gn_levels_kernel<decltype(lanes)::value>, levels + gn_join_ctas(a), 0, true, st, a, (uint32_t)levels); });
-        if (e == cudaSuccess && a.dx) e = gn_launch(dx, ctas, RING, true, st, a);
+        if (e == cudaSuccess && a.dx) e = gn_launch(dx, gn_ctas(again), RING, true, st, again);
         return e;
     }
 };
