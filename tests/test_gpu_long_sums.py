@@ -167,3 +167,19 @@ def test_bfloat16_weight_gradients_through_the_workspace(N, rows, h, out, dtype)
     assert (grads[:, :4] == 5).all() and (grads[:, -5:] == 5).all()
     again = liec.liec_weight_grad(dy, q, scales, h, dweight=torch.empty(N, out, h, dtype=torch.bfloat16, device="cuda"))
     assert torch.equal(again, got)
+
+
+@pytest.mark.parametrize("pixels,ch,groups", [(64, 64, 8), (200, 96, 3), (49, 90, 5), (5000, 64, 8)])
+def test_channels_far_apart_in_a_group(pixels, ch, groups):
+    """Two channels of each group at 1000 and -1000: their sum is exact in binary64, so a group's mean is off by what its channels' own sums lose, 64 + 64 + 8
+    roundings of what lies about a channel's mean, and by the roundings of its own."""
+    gen = torch.Generator(device="cuda").manual_seed(ch)
+    x = torch.randn(2, 4, pixels, ch, generator=gen, device="cuda")
+    width = ch // groups
+    x[..., 0::width] += 1000
+    x[..., 1::width] -= 1000
+    _, mean, rstd = forward(x, groups)
+    m, _, r = statistics64(x, groups, 1e-5)
+    about = (x.double() - x.double().mean(2, keepdim=True)).abs().mean(2).unflatten(-1, (groups, width)).mean(-1)
+    assert ((mean.double() - m).abs() <= 2 * U * m.abs() + 136 * U * about).all(), float(((mean.double() - m).abs() / about).max() / U)
+    assert ((rstd.double() - r).abs() <= RSTD * r).all()
