@@ -423,9 +423,9 @@ __global__ void __launch_bounds__(GR_THREADS, 4) gn_resident_backward_kernel(con
 // ---- launches --------------------------------------------------------------------------------------------
 
 constexpr int GN_MAX_MEMORY = 112 * 1024;
-// Beyond, reading twice is as fast or faster: its threads walk down many more pixels for what each does once (forward /
-// backward from the checkpoint, SiLU, held and read twice: 32 images of 196 pixels x 128 bfloat16 8 / 10 and 10 / 12 us, 256 of
-// 64 x 256 12 / 21 and 18 / 28, 256 of 256 x 256 23 / 52 and 31 / 52; 256 of 196 x 1024 65 / 134 and 61 / 116).
+// Beyond, reading twice is faster backward, which is most of the two passes: its threads walk down many more pixels for what each does once
+// (forward / backward from the checkpoint, SiLU, held and read twice: 32 images of 196 pixels x 128 bfloat16 6 / 10 and 10 / 12 us, 256 of
+// 64 x 256 11 / 21 and 17 / 29, 256 of 256 x 256 19 / 52 and 30 / 52; 256 of 196 x 1024 54 / 135 and 60 / 117).
 constexpr int64_t GN_RESIDENT_ELEMENTS = 1 << 24;
 
 template <auto KERNEL>

@@ -11,9 +11,9 @@
 // of a product.  Lanes of the accumulator are channels, so a warp writes 32 neighbours of a row of dW.
 //
 // What bounds it: shared memory (bytes in, widened bytes out and in again, and the products' own reads share 128 bytes a cycle) and,
-// where sums leave tensor memory, an SM's way out, 27 bytes a cycle.  In bursts at 1965 MHz: 16 x 3136 tokens of 512 x 2048 into
-// bfloat16 86 us, 1.22 PFLOP/s; 8 x 8192 of 768 x 2304 into binary32 241 us, 0.96; binary32 dy, 8 x 4096 of 1024 x 1024, 184 us, three times
-// 0.37.  (In a loop of seconds the power cap holds the SMs at 1425 to 1580 MHz: 104 and 284 us.)
+// where sums leave tensor memory, an SM's way out, 27 bytes a cycle.  In bursts at 1965 MHz, by the card: 16 x 3136 tokens of 512 x 2048
+// into bfloat16 84 to 91 us, up to 1.25 PFLOP/s; 8 x 8192 of 768 x 2304 into binary32 235 to 250 us, 0.99; binary32 dy, 8 x 4096 of
+// 1024 x 1024, 184 us, three times 0.37.  (In a loop of seconds the power cap holds the SMs at 1390 to 1590 MHz: 102 and 278 us.)
 #include <cuda.h>
 
 #include <algorithm>

@@ -18,8 +18,8 @@ constexpr int WG_PAIRS = 74;       // of SMs
 // Stages that one sum in tensor memory takes.  The products' additions there cut what does not fit: always towards zero, which over
 // 8192 tokens comes to 6e-6 of a gradient (measured), ten times what rounded additions lose, and grows with the tokens.  So a binary32
 // gradient is summed there 1792 tokens at a time at most, and these sums are added with rounding: 8e-7.  Each such sum takes 10 us, 5 of
-// them an SM's way out for its 256 KB: 8 x 8192 x 768 x 2304 takes 241 us (186 in one sum, 203 with 4096 tokens and 2.5e-6, 233
-// with 2048 and 1.2e-6).  A bfloat16 gradient keeps 2^-9 anyway: 16,384 tokens at a time, which cut at most 2^-13 and 2e-5 on the
+// them an SM's way out for its 256 KB: 8 x 8192 x 768 x 2304 took 242 us with them on one card (186 in one sum, 203 with 4096 tokens
+// and 2.5e-6, 233 with 2048 and 1.2e-6).  A bfloat16 gradient keeps 2^-9 anyway: 16,384 tokens at a time, which cut at most 2^-13 and 2e-5 on the
 // average, a hundredth of that.
 constexpr int WG_SUM_STAGES = 56, WG_SUM_STAGES_BF16 = 512;
 constexpr int wg_slabs(int dtype) { return dtype == 0 ? 1 : 2; }   // of a tile
